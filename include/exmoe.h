@@ -47,7 +47,8 @@ enum {
     EXMOE_ERR_NONFINITE = -5,     /* exmoe_pack: a weight is NaN/Inf or a scale overflows FP16 */
     EXMOE_ERR_BAD_EXPERT_ID = -6, /* a top-k id was outside [0, E); that pair contributed nothing */
     EXMOE_ERR_TIMEOUT = -7,       /* a bounded device-side wait expired */
-    EXMOE_ERR_STATE = -8          /* call order: e.g. debug plan asked for a layer that did not run last */
+    EXMOE_ERR_STATE = -8,         /* call order: e.g. debug plan asked for a layer that did not run last */
+    EXMOE_ERR_BAD_ADAPTER_ID = -9 /* an adapter id was outside [-1, num_adapters); that token got no adapter */
 };
 
 /* Geometry of one sparse layer (Sec. 4.1 gives OLMoE's: 2048, 1024, 64, 8).  group_size must be 128. */
@@ -194,6 +195,86 @@ int exmoe_cache_prefetch(exmoe_cache* cache, int layer, const int32_t* expert_id
  * allocates nothing; T = 0 is a no-op.  EXMOE_ERR_SHAPE / EXMOE_ERR_ARG before any work is queued. */
 int exmoe_route(const exmoe_shape* shape, const void* hidden_bf16, const void* router_bf16, const float* bias,
                 int T, int32_t* topk_ids, float* topk_weights, void* stream);
+
+/* Gate of a sparse block (the paper keeps the model's own router; exmoe_route is the one of the model it measures, this the
+ * family that other sparse models use).  With z the logits of a token (Eq. 1):
+ *   scores       s_e = softmax(z)_e over all E experts, or 1 / (1 + exp(-z_e))
+ *   choice       c_e = s_e + balance_e: the bias that balances the experts' load decides which are chosen and does not enter a weight
+ *   groups       the experts in num_groups runs of E / num_groups; a group's value is its largest c_e, or the sum of its two
+ *                largest; only the top_groups groups of the largest values keep their experts, equal values ordered by ascending group
+ *   experts      the k largest c_e of these groups, in descending order, equal values by ascending id
+ *   weights      s_e of the chosen, divided by their sum if `renormalise` is set, times `weight_scale`
+ * Everything is decided as in binary64 (experts without a balance bias by z_e itself, of which s_e is a monotone function), whatever the
+ * number of tokens; weights are binary32.  A logit of -infinity switches its expert off: score 0, chosen after all others of the kept
+ * groups, absent from its group's value.  A token without any expert left gets the first k of the first groups, with weights of
+ * zero.  A NaN logit comes behind those; with softmax it makes the token's weights NaN. */
+enum { EXMOE_SCORE_SOFTMAX = 0, EXMOE_SCORE_SIGMOID = 1 };
+enum { EXMOE_GROUP_MAX = 0, EXMOE_GROUP_TOP2 = 1 };
+typedef struct {
+    int score;          /* EXMOE_SCORE_* */
+    int num_groups;     /* 1: no groups; at most 32, a divisor of num_experts */
+    int top_groups;     /* 1 .. num_groups; top_k <= top_groups * (num_experts / num_groups) */
+    int group_score;    /* EXMOE_GROUP_* */
+    int renormalise;    /* 0 or 1 */
+    float weight_scale; /* 1 for none */
+} exmoe_gate;
+
+/* The gate on hidden states: z_t = W_r h_t (+ bias) (+ addend_t), then the choice above.
+ *   hidden_bf16  : dev, BF16 [T, H], 16-byte aligned     router_bf16 : dev, BF16 [E, H], 16-byte aligned
+ *   bias         : dev, float32 [E], or NULL (added to the logits, as exmoe_route's)
+ *   addend       : dev, float32 [T, E], or NULL: what else a token's logits hold, e.g. the product of its router adapter
+ *                  (exmoe_lora), noise, or -infinity for experts it may not use
+ *   balance      : dev, float32 [E], or NULL
+ *   topk_ids     : dev, int32 [T, k]                      topk_weights : dev, float32 [T, k]
+ * Limits as exmoe_route's: d_model a multiple of 8, num_experts <= 4096, 2 * d_model + 16 * num_experts <= 204,800 bytes.
+ * Asynchronous on `stream`; allocates nothing; T = 0 is a no-op.  EXMOE_ERR_SHAPE / EXMOE_ERR_ARG before any work is queued. */
+int exmoe_route_gated(const exmoe_shape* shape, const exmoe_gate* gate, const void* hidden_bf16, const void* router_bf16,
+                      const float* bias, const float* addend, const float* balance, int T, int32_t* topk_ids,
+                      float* topk_weights, void* stream);
+
+/* The gate on logits that were computed elsewhere: dev, float32 or BF16 (`type`) [T, E], rows `row_stride` elements apart.
+ * Uses shape->num_experts and top_k; otherwise as exmoe_route_gated. */
+enum { EXMOE_F32 = 0, EXMOE_BF16 = 1 };
+int exmoe_gate_logits(const exmoe_shape* shape, const exmoe_gate* gate, const void* logits, int type, int64_t row_stride,
+                      const float* balance, int T, int32_t* topk_ids, float* topk_weights, void* stream);
+
+/* Low-rank adapters of many requests beside a projection that all of them share (the paper has none; packed int4 weights cannot
+ * take an adapter in, and the requests of a batch bring different ones).  For token t with adapter a:
+ *   out_t = base_t + scale_a * B_a (A_a x_t)
+ * with base what the shared projection gave: a BF16 projection, the sparse block's output, or the router's logits in float32.
+ * Products are summed in binary32 and rounded once, to the type of `out`. */
+typedef struct {
+    int num_adapters;   /* n, 1 .. 1024 */
+    int d_in;           /* K, a multiple of 8 */
+    int d_out;          /* N */
+    int rank;           /* r, a multiple of 8, at most 128; adapters of smaller rank are padded with zeros */
+} exmoe_lora_shape;
+
+/* Which tokens go together, once per step: a plan serves every projection of the step's layers.
+ *   adapter_ids : dev, int32 [T], -1: no adapter; any order, any repeats.  Another id outside [0, n) counts as none and is
+ *                 reported by exmoe_lora_plan_status
+ *   plan        : dev, exmoe_lora_plan_bytes(T, n) bytes, 16-byte aligned, written here
+ * Asynchronous on `stream`; a plan of T = 0 tokens is one too. */
+int exmoe_lora_plan_bytes(int T, int num_adapters, size_t* bytes);
+int exmoe_lora_plan(const int32_t* adapter_ids, int T, int num_adapters, void* plan, void* stream);
+/* What the device found in a plan's ids or in its use (synchronises the device): EXMOE_OK, EXMOE_ERR_BAD_ADAPTER_ID, or
+ * EXMOE_ERR_STATE where exmoe_lora was called with a T or a number of adapters that are not the plan's (its outputs were then left as
+ * they were). */
+int exmoe_lora_plan_status(const void* plan);
+
+/* One projection's adapters.
+ *   plan  : dev, from exmoe_lora_plan for the same T and num_adapters
+ *   x     : dev, BF16 [T, K], rows ld_x elements apart (a multiple of 8), 16-byte aligned
+ *   a, b  : dev, BF16 [n, r, K] and [n, N, r], 16-byte aligned        scale : dev, float32 [n]
+ *   base  : dev, [T, N] of `type`, rows ld_base elements apart, or NULL for zeros
+ *   out   : dev, [T, N] of `type`, rows ld_out elements apart, fully overwritten; may be `base` itself with the same rows and
+ *           otherwise overlaps none of the inputs (EXMOE_ERR_ARG)
+ *   type  : EXMOE_F32 or EXMOE_BF16, of base and out
+ * A token's result depends on its own row and adapter alone, not on the batch around it.  Asynchronous on `stream`; allocates
+ * nothing; T = 0 is a no-op. */
+int exmoe_lora(const exmoe_lora_shape* shape, void* plan, const void* x, int64_t ld_x, const void* a, const void* b,
+               const float* scale, int T, const void* base, int64_t ld_base, void* out, int64_t ld_out, int type,
+               void* stream);
 
 /* Tiny-batch forward that allocates nothing and needs no cache object (the paper has no counterpart: this
  * is a service for one kind of caller, not a step of the method).

@@ -8,7 +8,8 @@ an exception is raised.
 import ctypes
 import importlib.util
 import os
-from ctypes import POINTER, byref, c_char_p, c_float, c_int, c_int32, c_size_t, c_uint64, c_void_p
+from ctypes import POINTER, byref, c_char_p, c_float, c_int, c_int32, c_int64, c_size_t, c_uint64, c_void_p
+from dataclasses import dataclass
 
 import torch
 
@@ -27,6 +28,7 @@ EXMOE_ERR_NONFINITE = -5
 EXMOE_ERR_BAD_EXPERT_ID = -6
 EXMOE_ERR_TIMEOUT = -7
 EXMOE_ERR_STATE = -8
+EXMOE_ERR_BAD_ADAPTER_ID = -9
 
 
 class ExmoeError(RuntimeError):
@@ -44,6 +46,15 @@ class exmoe_stats(ctypes.Structure):
                 ("h2d_bytes", c_uint64), ("forwards", c_uint64)]
 
 
+class exmoe_gate(ctypes.Structure):
+    _fields_ = [("score", c_int), ("num_groups", c_int), ("top_groups", c_int), ("group_score", c_int), ("renormalise", c_int),
+                ("weight_scale", c_float)]
+
+
+class exmoe_lora_shape(ctypes.Structure):
+    _fields_ = [("num_adapters", c_int), ("d_in", c_int), ("d_out", c_int), ("rank", c_int)]
+
+
 _SIGNATURES = {
     "exmoe_strerror": (c_char_p, [c_int]),
     "exmoe_packed_bytes": (c_int, [POINTER(exmoe_shape), POINTER(c_size_t)]),
@@ -58,6 +69,13 @@ _SIGNATURES = {
     "exmoe_debug_last_host_copy_bytes": (c_int, [c_void_p, POINTER(c_size_t)]),
     "exmoe_moe_forward_static": (c_int, [POINTER(exmoe_shape), c_void_p, c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_void_p]),
     "exmoe_route": (c_int, [POINTER(exmoe_shape), c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_void_p]),
+    "exmoe_route_gated": (c_int, [POINTER(exmoe_shape), POINTER(exmoe_gate)] + [c_void_p] * 5 + [c_int] + [c_void_p] * 3),
+    "exmoe_gate_logits": (c_int, [POINTER(exmoe_shape), POINTER(exmoe_gate), c_void_p, c_int, c_int64, c_void_p, c_int] + [c_void_p] * 3),
+    "exmoe_lora_plan_bytes": (c_int, [c_int, c_int, POINTER(c_size_t)]),
+    "exmoe_lora_plan": (c_int, [c_void_p, c_int, c_int, c_void_p, c_void_p]),
+    "exmoe_lora_plan_status": (c_int, [c_void_p]),
+    "exmoe_lora": (c_int, [POINTER(exmoe_lora_shape), c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int, c_void_p,
+                           c_int64, c_void_p, c_int64, c_int, c_void_p]),
     "exmoe_cache_get_state": (c_int, [c_void_p, c_int, c_void_p, c_void_p, c_void_p, c_void_p]),
     "exmoe_debug_last_plan": (c_int, [c_void_p, c_int] + [c_void_p] * 9),
     "exmoe_debug_last_path": (c_int, [c_void_p]),
@@ -112,7 +130,8 @@ def _serving():
         native = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(native)
         native.set_entry_points(*(ctypes.cast(getattr(lib(), name), c_void_p).value for name in
-                                  ("exmoe_route", "exmoe_moe_forward", "exmoe_moe_forward_host")))
+                                  ("exmoe_route", "exmoe_moe_forward", "exmoe_moe_forward_host", "exmoe_route_gated", "exmoe_gate_logits",
+                                   "exmoe_lora_plan_bytes", "exmoe_lora_plan", "exmoe_lora")))
         _native = native
     return _native
 
@@ -192,6 +211,56 @@ def exmoe_route(shape, hidden, w_router, bias=None, topk_ids=None, topk_weights=
     r = (_native or _serving()).route(shape, hidden, w_router, bias, topk_ids, topk_weights, stream)
     if r.__class__ is int:
         raise ExmoeError(r, "exmoe_route")
+    return r
+
+
+@dataclass(frozen=True)
+class Gate:
+    """The gate of a sparse block (exmoe_gate): scores, groups of experts, weights.  The entry points take anything with these attributes."""
+    score: str = "softmax"          # or "sigmoid"
+    num_groups: int = 1             # the experts in as many runs of equal size,
+    top_groups: int = 1             # of which a token keeps these many,
+    group_score: str = "max"        # by their largest choice value, or by the sum of the two largest: "top2"
+    renormalise: bool = False       # weights divided by their sum
+    scale: float = 1.0              # factor on the weights
+
+
+def exmoe_route_gated(shape, gate, hidden, w_router, bias=None, addend=None, balance=None, topk_ids=None, topk_weights=None, stream=None):
+    """The gate on hidden states BF16 [T, H]: logits W_r h (+ bias [E]) (+ addend [T, E]), scores, the balance bias [E] that enters
+    the choice only, groups, top-k, weights.  Returns (ids int32 [T, k], weights fp32 [T, k])."""
+    r = (_native or _serving()).route_gated(shape, gate, hidden, w_router, bias, addend, balance, topk_ids, topk_weights, stream)
+    if r.__class__ is int:
+        raise ExmoeError(r, "exmoe_route_gated")
+    return r
+
+
+def exmoe_gate_logits(shape, gate, logits, balance=None, topk_ids=None, topk_weights=None, stream=None):
+    """The same choice from logits fp32 or BF16 [T, E], whose rows may be apart.  Returns (ids int32 [T, k], weights fp32 [T, k])."""
+    r = (_native or _serving()).gate_logits(shape, gate, logits, balance, topk_ids, topk_weights, stream)
+    if r.__class__ is int:
+        raise ExmoeError(r, "exmoe_gate_logits")
+    return r
+
+
+def exmoe_lora_plan(adapter_ids, num_adapters, plan=None, stream=None):
+    """Groups a step's tokens by adapter (ids int32 [T], -1: none).  Returns the plan (int32, device) for every exmoe_lora of the step."""
+    r = (_native or _serving()).lora_plan(adapter_ids, num_adapters, plan, stream)
+    if r.__class__ is int:
+        raise ExmoeError(r, "exmoe_lora_plan")
+    return r
+
+
+def exmoe_lora_plan_status(plan):
+    """EXMOE_OK, EXMOE_ERR_BAD_ADAPTER_ID or EXMOE_ERR_STATE: what the device found in the plan's ids or its use (synchronises)."""
+    return int(lib().exmoe_lora_plan_status(_dev(plan, torch.int32, "plan")))
+
+
+def exmoe_lora(plan, x, a, b, scale, base=None, out=None, out_dtype=None, stream=None):
+    """base + scale_a * B_a (A_a x) for every token's adapter: x BF16 [T, K], a BF16 [n, r, K], b BF16 [n, N, r], scale fp32 [n]; base and
+    out fp32 or BF16 [T, N] (`out_dtype` where neither is given, BF16 by default).  Rows of x, base and out may be apart; out may be base."""
+    r = (_native or _serving()).lora(plan, x, a, b, scale, base, out, out_dtype, stream)
+    if r.__class__ is int:
+        raise ExmoeError(r, "exmoe_lora")
     return r
 
 

@@ -261,6 +261,7 @@ const char* exmoe_strerror(int code) {
         case EXMOE_ERR_BAD_EXPERT_ID: return "expert id out of range";
         case EXMOE_ERR_TIMEOUT: return "bounded device wait expired";
         case EXMOE_ERR_STATE: return "call order";
+        case EXMOE_ERR_BAD_ADAPTER_ID: return "adapter id out of range";
         default: return "unknown error";
     }
 }
