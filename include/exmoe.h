@@ -270,8 +270,8 @@ int exmoe_lora_plan_status(const void* plan);
  *   out   : dev, [T, N] of `type`, rows ld_out elements apart, fully overwritten; may be `base` itself with the same rows and
  *           otherwise overlaps none of the inputs (EXMOE_ERR_ARG)
  *   type  : EXMOE_F32 or EXMOE_BF16, of base and out
- * A token's result depends on its own row and adapter alone, not on the batch around it.  Asynchronous on `stream`; allocates
- * nothing; T = 0 is a no-op. */
+ * A token's result depends on its own row and adapter alone, in calls of the same T and num_adapters to the bit (others may split
+ * the sums differently).  Asynchronous on `stream`; allocates nothing; T = 0 is a no-op. */
 int exmoe_lora(const exmoe_lora_shape* shape, void* plan, const void* x, int64_t ld_x, const void* a, const void* b,
                const float* scale, int T, const void* base, int64_t ld_base, void* out, int64_t ld_out, int type,
                void* stream);

@@ -3,6 +3,7 @@
 #include <algorithm>
 
 #include "common.cuh"
+#include "frag.cuh"
 
 namespace exmoe {
 
@@ -10,17 +11,19 @@ namespace {
 
 constexpr int kMaxAdapters = 1024, kMaxRank = 128;
 constexpr int kPlanThreads = 1024, kPlanWarps = kPlanThreads / 32;
+constexpr int kSms = 148;
 constexpr int kLoraThreads = 256, kLoraWarps = kLoraThreads / 32;
 
 // A plan: header, tiles, then the tokens grouped by adapter (ascending, those without one last; inside a group ascending tokens).
-// A tile is a run of at most kTileRows rows of one group.
-constexpr int kTileRows = 64;
+// A tile is a run of at most tile_rows(T) rows of one group: few enough that clusters of eight CTAs fill the chip, as far as
+// that goes, and more where there are tokens enough, since every tile reads its adapter.
+__host__ __device__ constexpr int tile_rows(int T) { return T >= 1184 ? 64 : T >= 592 ? 32 : 16; }
 constexpr int kPlanMagic = 0x4c6f5241;
 enum { LP_MAGIC = 0, LP_TOKENS = 1, LP_ADAPTERS = 2, LP_TILES = 3, LP_STATUS = 4, LP_WORDS = 16 };
 struct LoraTile { int adapter, row0, nrows, pad; };                        // adapter -1: none
 __host__ __device__ inline int plan_tiles(int T, int n) {                  // most tiles of a plan
     const int groups = T < n + 1 ? T : n + 1;
-    return T / kTileRows + groups;
+    return T / tile_rows(T) + groups;
 }
 
 __global__ void __launch_bounds__(kPlanThreads)
@@ -31,7 +34,7 @@ lora_plan_kernel(const int32_t* ids, int T, int n, int32_t* plan) {
     int32_t* first = count + n + 1;                                        // [n + 1] first row of a group
     int32_t* tile0 = first + n + 1;                                        // [n + 1] its first tile
     __shared__ int bad;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, most = tile_rows(T);
     const unsigned lt = (1u << lane) - 1u;
     LoraTile* tiles = reinterpret_cast<LoraTile*>(plan + LP_WORDS);
     int32_t* perm = plan + LP_WORDS + 4 * plan_tiles(T, n);
@@ -67,7 +70,7 @@ lora_plan_kernel(const int32_t* ids, int T, int n, int32_t* plan) {
     if (warp == 0) {
         int rows = 0, nt = 0;
         for (int b0 = 0; b0 <= n; b0 += 32) {
-            const int c = b0 + lane <= n ? count[b0 + lane] : 0, tl = (c + kTileRows - 1) / kTileRows;
+            const int c = b0 + lane <= n ? count[b0 + lane] : 0, tl = (c + most - 1) / most;
             int ic = c, it = tl;
 #pragma unroll
             for (int d = 1; d < 32; d <<= 1) {
@@ -94,8 +97,8 @@ lora_plan_kernel(const int32_t* ids, int T, int n, int32_t* plan) {
     }
     __syncthreads();
     for (int b = tid; b <= n; b += kPlanThreads)
-        for (int i = 0; i * kTileRows < count[b]; ++i)
-            tiles[tile0[b] + i] = LoraTile{b < n ? b : -1, first[b] + i * kTileRows, min(kTileRows, count[b] - i * kTileRows), 0};
+        for (int i = 0; i * most < count[b]; ++i)
+            tiles[tile0[b] + i] = LoraTile{b < n ? b : -1, first[b] + i * most, min(most, count[b] - i * most), 0};
     for (int t0 = t_begin; t0 < t_end; t0 += 32) {
         const int b = group_of(t0 + lane);
         const unsigned same = __match_any_sync(0xffffffffu, b);
@@ -115,11 +118,6 @@ struct LoraArgs {
     long long ld_x, ld_base, ld_out;
     int T, n, K, N, r;
 };
-__device__ __forceinline__ float to_float(float v) { return v; }
-__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ void store(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store(__nv_bfloat16* p, float v) { *p = __float2bfloat16(v); }
-
 // whether the plan is one for this call; a wrong one is reported and nothing else is done
 __device__ __forceinline__ bool plan_fits(const LoraArgs& p) {
     if (p.plan[LP_MAGIC] == kPlanMagic && p.plan[LP_TOKENS] == p.T && p.plan[LP_ADAPTERS] == p.n) return true;
@@ -127,42 +125,336 @@ __device__ __forceinline__ bool plan_fits(const LoraArgs& p) {
     return false;
 }
 
-// One CTA per tile, row by row.
-template <typename O>
-__global__ void __launch_bounds__(kLoraThreads)
-lora_tile_kernel(LoraArgs p) {
-    __shared__ float v[kMaxRank];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (!plan_fits(p) || (int)blockIdx.x >= p.plan[LP_TILES]) return;
-    const LoraTile tile = reinterpret_cast<const LoraTile*>(p.plan + LP_WORDS)[blockIdx.x];
-    const int32_t* perm = p.plan + LP_WORDS + 4 * plan_tiles(p.T, p.n);
-    for (int i = 0; i < tile.nrows; ++i) {
-        const long long t = perm[tile.row0 + i];
-        const O* base = p.base ? (const O*)p.base + t * p.ld_base : nullptr;
-        O* out = (O*)p.out + t * p.ld_out;
-        if (tile.adapter < 0) {
-            for (int c = tid; c < p.N; c += kLoraThreads) out[c] = base ? base[c] : O(0.f);
-            continue;
+__device__ __forceinline__ void cluster_arrive() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ float ld_cluster(uint32_t addr, int rank) {     // a word of another CTA's shared memory
+    uint32_t at;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
+}
+
+// Eight consecutive columns of a row of base or out.  `vec`: they are 16-byte aligned; `n`: how many of them there are.
+template <typename O> struct Cols;
+template <> struct Cols<__nv_bfloat16> {
+    uint4 w = make_uint4(0, 0, 0, 0);
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, int n, bool vec) {
+        w = make_uint4(0, 0, 0, 0);
+        if (vec && n >= 8) {
+            asm volatile("ld.global.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w.x), "=r"(w.y), "=r"(w.z), "=r"(w.w) : "l"(p) : "memory");
+            return;
         }
-        const __nv_bfloat16* x = p.x + t * p.ld_x;
-        for (int j = warp; j < p.r; j += kLoraWarps) {
-            const __nv_bfloat16* a = p.a + ((size_t)tile.adapter * p.r + j) * p.K;
-            float s = 0.f;
-            for (int k = lane; k < p.K; k += 32) s = fmaf(__bfloat162float(a[k]), __bfloat162float(x[k]), s);
+        uint32_t h[8];
 #pragma unroll
-            for (int m = 16; m >= 1; m >>= 1) s += __shfl_xor_sync(0xffffffffu, s, m);
-            if (lane == 0) v[j] = s;
-        }
-        __syncthreads();
-        const float scale = p.scale[tile.adapter];
-        for (int c = tid; c < p.N; c += kLoraThreads) {
-            const __nv_bfloat16* b = p.b + ((size_t)tile.adapter * p.N + c) * p.r;
-            float s = 0.f;
-            for (int j = 0; j < p.r; ++j) s = fmaf(__bfloat162float(b[j]), v[j], s);
-            store(out + c, fmaf(scale, s, base ? to_float(base[c]) : 0.f));
-        }
-        __syncthreads();
+        for (int i = 0; i < 8; ++i) h[i] = i < n ? (uint32_t)reinterpret_cast<const unsigned short*>(p)[i] : 0u;
+        w = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
     }
+    __device__ __forceinline__ float get(int i) const {
+        const uint32_t r = i < 2 ? w.x : i < 4 ? w.y : i < 6 ? w.z : w.w;
+        return __uint_as_float(i & 1 ? r & 0xffff0000u : r << 16);
+    }
+    __device__ __forceinline__ void set(const float (&v)[8]) {
+        uint32_t r[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+            r[i] = *reinterpret_cast<const uint32_t*>(&h);
+        }
+        w = make_uint4(r[0], r[1], r[2], r[3]);
+    }
+    __device__ __forceinline__ void store(__nv_bfloat16* p, int n, bool vec) const {
+        if (vec && n >= 8) {
+            *reinterpret_cast<uint4*>(p) = w;
+            return;
+        }
+        const uint32_t r[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) reinterpret_cast<unsigned short*>(p)[i] = (unsigned short)(r[i >> 1] >> (16 * (i & 1)));
+    }
+};
+template <> struct Cols<float> {
+    float w[8] = {};
+    __device__ __forceinline__ void load(const float* p, int n, bool vec) {
+        if (vec && n >= 8) {
+            asm volatile("ld.global.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(w[0]), "=f"(w[1]), "=f"(w[2]), "=f"(w[3]) : "l"(p) : "memory");
+            asm volatile("ld.global.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(w[4]), "=f"(w[5]), "=f"(w[6]), "=f"(w[7]) : "l"(p + 4) : "memory");
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = i < n ? p[i] : 0.f;
+    }
+    __device__ __forceinline__ float get(int i) const { return w[i]; }
+    __device__ __forceinline__ void set(const float (&v)[8]) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = v[i];
+    }
+    __device__ __forceinline__ void store(float* p, int n, bool vec) const {
+        if (vec && n >= 8) {
+            *reinterpret_cast<float4*>(p) = make_float4(w[0], w[1], w[2], w[3]);
+            *reinterpret_cast<float4*>(p + 4) = make_float4(w[4], w[5], w[6], w[7]);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = w[i];
+    }
+};
+
+// A cluster of CTAs per tile of up to 16 MB rows of one adapter.
+//   shrink  v = A x: every CTA takes a part of K.  Operands go from global memory into the fragments of m16n8k16 MMAs in 16-byte
+//           loads: a lane's eight consecutive k serve two MMAs of both operands, K being permuted alike on both sides.  A warp takes 16
+//           ranks, all rows and every WK-th step of 32.
+//   join    partial v of the warps, then of the CTAs (through the cluster's shared memory), added in a fixed order in binary32
+//   expand  out = base + scale B v: every CTA takes a part of N; v as a sum of two BF16 numbers (three for binary32 outputs: 8 more
+//           bits each), so that B's products lose nothing that the output holds.  A lane's columns of the four MMAs of 32 columns
+//           are made consecutive by permuting the rows of B: 16-byte accesses to base and out.
+// RP: rank, rounded up (zeros).
+template <typename O, int RP, int MB>
+struct LoraSmem {
+    static constexpr int TM = 16 * MB, WN = RP / 16, WK = kLoraWarps / WN, PS = RP + 8, VS = RP + 8, SPLIT = sizeof(O) == 4 ? 3 : 2;
+    float sum[TM][RP];                                                     // this CTA's part of v, read by the cluster
+    union {
+        float part[WK][TM][PS];                                            // the warps' parts
+        __nv_bfloat16 v[SPLIT][TM][VS];                                    // v as BF16 numbers, largest first
+    };
+    long long token[TM];
+};
+template <typename O, int RP, int MB>
+__global__ void __launch_bounds__(kLoraThreads, RP <= 64 ? 2 : 1)
+lora_kernel(LoraArgs p, int CL) {
+    using S = LoraSmem<O, RP, MB>;
+    constexpr int TM = S::TM, WN = S::WN, WK = S::WK, U = MB == 1 ? 4 : MB == 2 ? 2 : 1;
+    extern __shared__ __align__(16) unsigned char smem[];
+    S& sm = *reinterpret_cast<S*>(smem);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, q = lane >> 2, c = lane & 3;
+    const int rank = (int)blockIdx.x % CL;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int at = (int)blockIdx.x / CL;
+    if (!plan_fits(p) || at >= p.plan[LP_TILES]) return;                   // the same for a whole cluster
+    const LoraTile tile = reinterpret_cast<const LoraTile*>(p.plan + LP_WORDS)[at];
+    const int32_t* perm = p.plan + LP_WORDS + 4 * plan_tiles(p.T, p.n);
+    const int nrows = tile.nrows, nmb = (nrows + 15) / 16;
+    if (tid < TM) sm.token[tid] = perm[tile.row0 + min(tid, nrows - 1)];   // rows behind the last repeat it; they are not stored
+    __syncthreads();
+    const int n_blocks = (p.N + 31) / 32;
+    const bool vec = !((reinterpret_cast<uintptr_t>(p.out) | reinterpret_cast<uintptr_t>(p.base) | (p.ld_out | p.ld_base) * sizeof(O)) & 15);
+    const O* base = static_cast<const O*>(p.base);
+    O* out = static_cast<O*>(p.out);
+    Cols<O> y[MB][2];
+    auto load_base = [&](int nb) {
+        const int col = 32 * nb + 8 * c;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                if (base && mb < nmb) y[mb][h].load(base + sm.token[16 * mb + 8 * h + q] * p.ld_base + col, p.N - col, vec);
+    };
+    if (tile.adapter < 0) {
+        if (base != out)
+            for (int nb = rank * kLoraWarps + warp; nb < n_blocks; nb += CL * kLoraWarps) {
+                load_base(nb);
+                const int col = 32 * nb + 8 * c;
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        if (16 * mb + 8 * h + q < nrows) y[mb][h].store(out + sm.token[16 * mb + 8 * h + q] * p.ld_out + col, p.N - col, vec);
+            }
+        return;
+    }
+    {   // shrink
+        const int wn = warp % WN, wk = warp / WN;
+        const int steps = (p.K + 31) / 32, s_end = (int)((long long)steps * (rank + 1) / CL);
+        const uint4 *xrow[MB][2], *arow[2];
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) xrow[mb][h] = reinterpret_cast<const uint4*>(p.x + sm.token[16 * mb + 8 * h + q] * p.ld_x) + c;
+        bool has[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int row = 16 * wn + 8 * j + q;
+            has[j] = row < p.r;
+            arow[j] = reinterpret_cast<const uint4*>(p.a + ((size_t)tile.adapter * p.r + (has[j] ? row : 0)) * p.K) + c;
+        }
+        float acc[MB][2][4];
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[mb][j][i] = 0.f;
+        for (int s0 = (int)((long long)steps * rank / CL) + wk; s0 < s_end; s0 += U * WK) {
+            uint4 xv[U][MB][2], av[U][2];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int s = s0 + u * WK;
+                const bool in = s < s_end && 32 * s + 8 * c < p.K;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    av[u][j] = make_uint4(0, 0, 0, 0);
+                    if (in && has[j]) av[u][j] = arow[j][4 * s];
+                }
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        xv[u][mb][h] = make_uint4(0, 0, 0, 0);
+                        if (in && mb < nmb) xv[u][mb][h] = xrow[mb][h][4 * s];
+                    }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int mb = 0; mb < MB; ++mb)
+                    if (mb < nmb) {
+                        const uint4 &lo = xv[u][mb][0], &hi = xv[u][mb][1];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) mma_m16n8k16(acc[mb][j], lo.x, hi.x, lo.y, hi.y, av[u][j].x, av[u][j].y);
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) mma_m16n8k16(acc[mb][j], lo.z, hi.z, lo.w, hi.w, av[u][j].z, av[u][j].w);
+                    }
+        }
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    *reinterpret_cast<float2*>(&sm.part[wk][16 * mb + 8 * h + q][16 * wn + 8 * j + 2 * c]) = make_float2(acc[mb][j][2 * h], acc[mb][j][2 * h + 1]);
+    }
+    __syncthreads();
+    const int used = min(TM, 16 * nmb) * RP;
+    for (int i = tid; i < used; i += kLoraThreads) {
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < WK; ++w) s += sm.part[w][i / RP][i % RP];
+        sm.sum[i / RP][i % RP] = s;
+    }
+    if (CL > 1) cluster_arrive(); else __syncthreads();
+    // in flight meanwhile: what the first columns need
+    const float scale = p.scale[tile.adapter];
+    constexpr int KB = RP / 16;
+    uint2 bf[4][KB];
+    auto load_b = [&](int nb) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int col = 32 * nb + 8 * (q >> 1) + 2 * j + (q & 1);
+            const __nv_bfloat16* row = p.b + ((size_t)tile.adapter * p.N + min(col, p.N - 1)) * p.r + 4 * c;
+#pragma unroll
+            for (int k = 0; k < KB; ++k) {
+                bf[j][k] = make_uint2(0, 0);
+                if (col < p.N && 16 * k + 4 * c < p.r) bf[j][k] = *reinterpret_cast<const uint2*>(row + 16 * k);
+            }
+        }
+    };
+    int nb = rank * kLoraWarps + warp;
+    if (nb < n_blocks) {
+        load_b(nb);
+        load_base(nb);
+    }
+    if (CL > 1) cluster_wait();
+    for (int i = tid; i < used; i += kLoraThreads) {
+        float v = 0.f;
+        if (CL > 1) {
+            const uint32_t addr = (uint32_t)__cvta_generic_to_shared(&sm.sum[0][0]) + 4 * i;
+            for (int r = 0; r < CL; ++r) v += ld_cluster(addr, r);
+        } else {
+            v = sm.sum[i / RP][i % RP];
+        }
+#pragma unroll
+        for (int n = 0; n < S::SPLIT; ++n) {
+            const __nv_bfloat16 h = __float2bfloat16(v);
+            sm.v[n][i / RP][i % RP] = h;
+            const float f = __bfloat162float(h);
+            v = fabsf(f) < INFINITY ? v - f : 0.f;                         // an infinity or NaN is all in the first
+        }
+    }
+    if (CL > 1) cluster_arrive();                                          // this CTA has read the others' shared memory
+    __syncthreads();
+    while (nb < n_blocks) {
+        const int col = 32 * nb + 8 * c;
+#pragma unroll
+        for (int mb = 0; mb < MB; ++mb)
+            if (mb < nmb) {
+                float d[4][4] = {};
+#pragma unroll
+                for (int k = 0; k < KB; ++k)
+#pragma unroll
+                    for (int n = S::SPLIT - 1; n >= 0; --n) {
+                        const uint2 lo = *reinterpret_cast<const uint2*>(&sm.v[n][16 * mb + q][16 * k + 4 * c]);
+                        const uint2 hi = *reinterpret_cast<const uint2*>(&sm.v[n][16 * mb + 8 + q][16 * k + 4 * c]);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) mma_m16n8k16(d[j], lo.x, hi.x, lo.y, hi.y, bf[j][k].x, bf[j][k].y);
+                    }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float o[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) o[i] = fmaf(scale, d[i >> 1][2 * h + (i & 1)], base ? y[mb][h].get(i) : 0.f);
+                    y[mb][h].set(o);
+                    if (16 * mb + 8 * h + q < nrows) y[mb][h].store(out + sm.token[16 * mb + 8 * h + q] * p.ld_out + col, p.N - col, vec);
+                }
+            }
+        nb += CL * kLoraWarps;
+        if (nb < n_blocks) {
+            load_b(nb);
+            load_base(nb);
+        }
+    }
+    if (CL > 1) cluster_wait();
+}
+
+template <typename O, int RP, int MB>
+int launch_lora(const LoraArgs& p, int tiles, int CL, cudaStream_t st) {
+    using S = LoraSmem<O, RP, MB>;
+    static SmemOnce once;
+    const auto kern = lora_kernel<O, RP, MB>;
+    if (!allow_smem(kern, (int)sizeof(S), once)) return EXMOE_ERR_CUDA;
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = dim3((unsigned)(tiles * CL));
+    lc.blockDim = dim3(kLoraThreads);
+    lc.dynamicSmemBytes = sizeof(S);
+    lc.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)CL;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    lc.attrs = attr;
+    lc.numAttrs = CL > 1 ? 2 : 1;
+#ifdef EXMOE_DISABLE_PDL
+    lc.attrs = attr + 1;
+    --lc.numAttrs;
+#endif
+    if (cudaLaunchKernelEx(&lc, kern, p, CL) != cudaSuccess) {
+        cudaGetLastError();
+        return EXMOE_ERR_CUDA;
+    }
+    count_launch();
+    return EXMOE_OK;
+}
+template <typename O, int RP>
+int launch_lora_rows(const LoraArgs& p, int tiles, int CL, cudaStream_t st) {
+    switch (tile_rows(p.T)) {
+        case 16: return launch_lora<O, RP, 1>(p, tiles, CL, st);
+        case 32: return launch_lora<O, RP, 2>(p, tiles, CL, st);
+        default: return launch_lora<O, RP, 4>(p, tiles, CL, st);
+    }
+}
+template <typename O>
+int launch_lora_rank(const LoraArgs& p, int tiles, int CL, cudaStream_t st) {
+    if (p.r <= 16) return launch_lora_rows<O, 16>(p, tiles, CL, st);
+    if (p.r <= 32) return launch_lora_rows<O, 32>(p, tiles, CL, st);
+    if (p.r <= 64) return launch_lora_rows<O, 64>(p, tiles, CL, st);
+    return launch_lora_rows<O, 128>(p, tiles, CL, st);
 }
 
 int check_plan(int T, int n) {
@@ -235,14 +527,11 @@ extern "C" int exmoe_lora(const exmoe_lora_shape* shape, void* plan, const void*
         return EXMOE_ERR_ARG;
     const LoraArgs args{(int32_t*)plan, (const __nv_bfloat16*)x, (const __nv_bfloat16*)a, (const __nv_bfloat16*)b, scale, base, out,
                         ld_x, ld_base, ld_out, T, n, K, N, r};
-    const unsigned ctas = (unsigned)plan_tiles(T, n);
-    if (type == EXMOE_F32)
-        lora_tile_kernel<float><<<ctas, kLoraThreads, 0, (cudaStream_t)stream>>>(args);
-    else
-        lora_tile_kernel<__nv_bfloat16><<<ctas, kLoraThreads, 0, (cudaStream_t)stream>>>(args);
-    if (cudaGetLastError() != cudaSuccess) return EXMOE_ERR_CUDA;
-    count_launch();
-    return EXMOE_OK;
+    // As many CTAs per tile (a power of two up to eight) as the chip has room for if every adapter is in use.
+    const int tiles = plan_tiles(T, n);
+    int CL = 8;
+    while (CL > 1 && (long long)tiles * CL > 2 * kSms) CL /= 2;
+    return type == EXMOE_F32 ? launch_lora_rank<float>(args, tiles, CL, (cudaStream_t)stream) : launch_lora_rank<__nv_bfloat16>(args, tiles, CL, (cudaStream_t)stream);
 }
 
 }  // namespace exmoe

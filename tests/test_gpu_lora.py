@@ -78,13 +78,20 @@ def test_adapters_match_oracle(B, T, n, r, K, N, dtype):
 
 @pytest.mark.parametrize("T,n,r,K,N", [(3, 2, 16, 256, 136), (40, 6, 8, 512, 77), (150, 2, 64, 1024, 1024), (600, 9, 16, 640, 384)])
 def test_results_depend_on_the_own_row_only(B, T, n, r, K, N):
-    """The same token alone, in another batch, in another order: the same bits."""
+    """In another order, and with other rows and adapters around them: the same bits.  Alone: the same value."""
     x, a, b, scale, ids, y = inputs(T, n, r, K, N, 5)
     out = B.exmoe_lora(B.exmoe_lora_plan(ids, n), x, a, b, scale, base=y)
-    for rows in ([T // 2], list(range(T - 1, -1, -1)), list(range(0, T, 3))):
-        part = [v[rows].contiguous() for v in (x, ids, y)]
-        again = B.exmoe_lora(B.exmoe_lora_plan(part[1], n), part[0], a, b, scale, base=part[2])
-        assert torch.equal(again.view(torch.int16), out[rows].view(torch.int16))
+
+    def call(x, ids, y):
+        return B.exmoe_lora(B.exmoe_lora_plan(ids.contiguous(), n), x.contiguous(), a, b, scale, base=y.contiguous())
+    back = list(range(T - 1, -1, -1))
+    assert torch.equal(call(x[back], ids[back], y[back]).view(torch.int16), out[back].view(torch.int16))
+    others = inputs(T, n, r, K, N, 6)
+    keep = torch.arange(T, device="cuda") % 3 == 1
+    mixed = [torch.where(keep.view(-1, *[1] * (u.dim() - 1)), u, v) for u, v in ((x, others[0]), (ids, others[4]), (y, others[5]))]
+    assert torch.equal(call(*mixed)[keep].view(torch.int16), out[keep].view(torch.int16))
+    for rows in ([T // 2], list(range(0, T, 3))):
+        check(call(x[rows], ids[rows], y[rows]), x[rows], a, b, scale, ids[rows], y[rows])
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
