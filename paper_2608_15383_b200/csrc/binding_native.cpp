@@ -62,6 +62,10 @@ bool int_attr(PyObject* o, PyObject* name, int* v) {
     Py_DECREF(a);
     return ok;
 }
+bool gate_shape_of(PyObject* o, exmoe_shape* s, bool d_model) {            // what a gate needs of a layer's shape
+    *s = exmoe_shape{};
+    return (!d_model || int_attr(o, s_d_model, &s->d_model)) && int_attr(o, s_experts, &s->num_experts) && int_attr(o, s_top_k, &s->top_k);
+}
 bool shape_of(PyObject* o, exmoe_shape* s) {
     if (!int_attr(o, s_d_model, &s->d_model) || !int_attr(o, s_d_ff, &s->d_ff) || !int_attr(o, s_experts, &s->num_experts) ||
         !int_attr(o, s_top_k, &s->top_k))
@@ -287,7 +291,7 @@ PyObject* route_gated(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         exmoe_shape s;
         exmoe_gate g;
-        if (!shape_of(a[0], &s) || !gate_of(a[1], &g)) return nullptr;
+        if (!gate_shape_of(a[0], &s, true) || !gate_of(a[1], &g)) return nullptr;
         const at::Tensor *h, *w;
         if (!(h = tensor(a[2], at::kBFloat16, true, "hidden", kBf16))) return nullptr;
         if (!(w = tensor(a[3], at::kBFloat16, true, "w_router", kBf16))) return nullptr;
@@ -322,7 +326,7 @@ PyObject* gate_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         exmoe_shape s;
         exmoe_gate g;
-        if (!shape_of(a[0], &s) || !gate_of(a[1], &g)) return nullptr;
+        if (!gate_shape_of(a[0], &s, false) || !gate_of(a[1], &g)) return nullptr;
         const bool bf16 = THPVariable_Check(a[2]) && THPVariable_Unpack(a[2]).scalar_type() == at::kBFloat16;
         const at::Tensor* z = rows(a[2], bf16 ? at::kBFloat16 : at::kFloat, "logits", "a CUDA matrix of torch.float32 or torch.bfloat16 with rows of consecutive elements");
         if (!z) return nullptr;

@@ -1,14 +1,64 @@
 // The gate of a sparse block (exmoe_gate): scores, balance bias, groups, top-k, weights; from hidden states or from logits.
+#include <cooperative_groups.h>
+
 #include <algorithm>
 
+#include "frag.cuh"
 #include "gate.cuh"
 
 namespace exmoe {
 
 namespace {
 
+namespace cg = cooperative_groups;
+
 constexpr int kGateThreads = 256, kGateWarps = kGateThreads / 32;
 constexpr int kGateSmemMax = 200 * 1024;
+
+__device__ __forceinline__ void unpack8(const uint4& a, float (&x)[8]) {
+    const uint32_t r[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(r[i] << 16);
+        x[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ float dot8(const float (&w)[8], const float (&x)[8]) {
+    float d = 0.f;
+#pragma unroll
+    for (int n = 0; n < 8; ++n) d = fmaf(w[n], x[n], d);
+    return d;
+}
+__device__ __forceinline__ float square8(const uint4& a) {
+    float x[8];
+    unpack8(a, x);
+    return dot8(x, x);
+}
+// A logit by one warp in binary64; products of BF16 values are exact in binary32.
+__device__ __noinline__ double logit_f64(const uint4* x, const uint4* w, int chunks, int lane) {
+    double s = 0.0;
+    for (int i0 = 0; i0 < chunks; i0 += 128) {
+        uint4 wv[4], xv[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = i0 + 32 * j + lane;
+            wv[j] = xv[j] = make_uint4(0, 0, 0, 0);
+            if (i < chunks) {
+                wv[j] = w[i];
+                xv[j] = x[i];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float wf[8], xf[8];
+            unpack8(wv[j], wf);
+            unpack8(xv[j], xf);
+#pragma unroll
+            for (int n = 0; n < 8; ++n) s += (double)(wf[n] * xf[n]);
+        }
+    }
+    return warp_sum_f64(s);
+}
 
 // One CTA per token, everything in binary64: products of BF16 values are exact in binary32.
 __global__ void __launch_bounds__(kGateThreads)
@@ -20,41 +70,192 @@ gate_token_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__
     uint4* xs = reinterpret_cast<uint4*>(smem + (((size_t)g.E * 16 + 15) & ~size_t(15)));
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, chunks = H / 8;
     const size_t t = blockIdx.x;
+    grid_dependency_wait();
     const uint4* xrow = reinterpret_cast<const uint4*>(hidden + t * H);
     for (int i = tid; i < chunks; i += kGateThreads) xs[i] = xrow[i];
     __syncthreads();
     for (int e = warp; e < g.E; e += kGateWarps) {
-        const uint4* wrow = reinterpret_cast<const uint4*>(w_router + (size_t)e * H);
-        double s = 0.0;
-        for (int i = lane; i < chunks; i += 32) {
-            const uint4 wv = wrow[i], xv = xs[i];
-            const uint32_t wr[4] = {wv.x, wv.y, wv.z, wv.w}, xr[4] = {xv.x, xv.y, xv.z, xv.w};
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                s += (double)(__uint_as_float(wr[n] << 16) * __uint_as_float(xr[n] << 16));
-                s += (double)(__uint_as_float(wr[n] & 0xffff0000u) * __uint_as_float(xr[n] & 0xffff0000u));
-            }
-        }
-        s = warp_sum_f64(s);
+        const double s = logit_f64(xs, reinterpret_cast<const uint4*>(w_router + (size_t)e * H), chunks, lane);
         if (lane == 0) z[e] = s + (bias ? (double)bias[e] : 0.0) + (addend ? (double)addend[t * g.E + e] : 0.0);
     }
     __syncthreads();
     if (warp == 0) choose_exact(g, z, key, lane, ids + t * g.k, weights + t * g.k);
 }
 
-// One warp per token.
-template <typename Z>
+// One warp per token; 16 bytes of shared memory per expert and warp.  PER: experts per lane of choose_fast, 0: all in binary64.
+template <typename Z, int PER>
 __global__ void __launch_bounds__(kGateThreads)
 gate_logits_kernel(const Z* logits, long long ld, int T, GateArgs g, int32_t* ids, float* weights) {
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    double* z = reinterpret_cast<double*>(smem) + (size_t)warp * 2 * g.E;
-    unsigned long long* key = reinterpret_cast<unsigned long long*>(z + g.E);
+    unsigned char* mine = smem + (size_t)warp * 16 * g.E;
     const size_t t = (size_t)blockIdx.x * (blockDim.x >> 5) + warp;
+    grid_dependency_wait();
+    grid_launch_dependents();
     if (t >= (size_t)T) return;
-    for (int e = lane; e < g.E; e += 32) z[e] = (double)(float)logits[(long long)t * ld + e];
+    const Z* row = logits + (long long)t * ld;
+    if constexpr (PER > 0) {
+        float *z = reinterpret_cast<float*>(mine), *c = z + g.E;
+        float v[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) v[i] = lane + 32 * i < g.E ? (float)row[lane + 32 * i] : 0.f;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (lane + 32 * i < g.E) z[lane + 32 * i] = v[i];
+        __syncwarp();
+        __shared__ uint32_t todos[kGateWarps][kTodoWords];
+        uint32_t* todo = todos[warp];
+        for (bool decided = false;; decided = true) {
+            if (!choose_fast<PER>(g, z, c, 0.f, 0.f, lane, decided, todo, ids + t * g.k, weights + t * g.k)) return;
+            if (todo[kTodoStage] == GATE_EXPERTS) return choose_again<PER>(g, z, c, nullptr, todo, lane, ids + t * g.k, weights + t * g.k);
+            if (todo[kTodoStage] == GATE_ALL) break;
+            choose_groups<PER>(g, z, c, nullptr, reinterpret_cast<double*>(c + g.E), todo, lane);
+        }
+        __syncwarp();
+    }
+    double* z = reinterpret_cast<double*>(mine);
+    for (int e = lane; e < g.E; e += 32) z[e] = (double)(float)row[e];
     __syncwarp();
-    choose_exact(g, z, key, lane, ids + t * g.k, weights + t * g.k);
+    choose_exact(g, z, reinterpret_cast<unsigned long long*>(z + g.E), lane, ids + t * g.k, weights + t * g.k);
+}
+
+constexpr float kAddedRel = 3.f * 0x1p-24f;                                // bias and addend: 2^-24 (|sum before| + |z|), with |sum before| <= 2 |z| + 16
+
+// ---- few tokens: a cluster of eight CTAs shares the experts of TB tokens -----------------------------------------------
+// As many warps as a 64-expert router has rows, so that a row's 4 KB are in flight at once.  Logits in binary32: chains of 8 products,
+// H / 256 + 1 chunks of a lane, a tree over the lanes: each addition off by 2^-24 of what is summed, so by
+// (8 + H / 256 + 1 + 5) 2^-24 |x| |w| together; bias and addend are off by 2^-24 of the sum before and of the logit (where the
+// former is larger than twice the latter + 16, all logits are computed again).  They travel through the cluster's shared
+// memory to the CTA that owns the token (i % 8), whose first warp chooses; where that rests on less than the bound, its warps
+// compute the logits that matter once more in binary64.
+constexpr int kFewCluster = 8, kFewFour = 48;                              // four tokens per cluster from here on
+template <int TB, int PER>
+__global__ void __launch_bounds__(kGateThreads)
+gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w_router, const float* __restrict__ bias, const float* addend, int T, int H,
+                GateArgs g, int32_t* ids, float* weights) {
+    static_assert(TB <= kFewCluster, "a CTA owns at most one token");
+    extern __shared__ __align__(16) unsigned char smem[];
+    double* z64 = reinterpret_cast<double*>(smem);
+    unsigned long long* key = reinterpret_cast<unsigned long long*>(z64 + g.E);
+    float *z = reinterpret_cast<float*>(key + g.E), *c = z + g.E;
+    uint4* xs = reinterpret_cast<uint4*>(smem + (((size_t)g.E * 24 + 15) & ~size_t(15)));   // [TB][H / 8]
+    __shared__ float w2_of[kFewCluster * kGateWarps], x2_of[kGateWarps];
+    __shared__ uint32_t todo[kTodoWords];
+    __shared__ int cancelled;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, chunks = H / 8;
+    const int rank = blockIdx.x % kFewCluster, t0 = (blockIdx.x / kFewCluster) * TB, n_tok = min(TB, T - t0);
+    grid_dependency_wait();
+    grid_launch_dependents();
+    constexpr int JB = 8;                                                  // chunks of an expert in flight
+    const int gw = rank * kGateWarps + warp;
+    uint4 raw[JB];
+    auto fetch = [&](int e, int j0) {
+#pragma unroll
+        for (int j = 0; j < JB; ++j) {
+            const int i = lane + 32 * (j0 + j);
+            raw[j] = make_uint4(0, 0, 0, 0);
+            if (i < chunks && e < g.E) raw[j] = reinterpret_cast<const uint4*>(w_router + (size_t)e * H)[i];
+        }
+    };
+    fetch(gw, 0);                                                          // in flight while the hidden rows are staged
+    const uint4* xrow = reinterpret_cast<const uint4*>(hidden + (size_t)t0 * H);
+    for (int i = tid; i < n_tok * chunks; i += kGateThreads) xs[i] = xrow[i];
+    for (int i = n_tok * chunks + tid; i < TB * chunks; i += kGateThreads) xs[i] = make_uint4(0, 0, 0, 0);
+    cg::cluster_group cluster = cg::this_cluster();
+    if (tid == 0) cancelled = 0;
+    __syncthreads();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // every CTA runs: its memory may be written
+    {
+        float x2 = 0.f;                                                    // |x|^2 of the token that this CTA owns
+        if (rank < n_tok)
+            for (int i = tid; i < chunks; i += kGateThreads) x2 += square8(xs[(size_t)rank * chunks + i]);
+        x2 = warp_sum_f32(x2);
+        if (lane == 0) x2_of[warp] = x2;
+    }
+    const int nj = (chunks + 31) / 32;
+    bool joined = false;
+    float w2_top = 0.f;
+    for (int e = gw; e < g.E; e += kFewCluster * kGateWarps) {
+        float acc[TB], w2 = 0.f;
+#pragma unroll
+        for (int t = 0; t < TB; ++t) acc[t] = 0.f;
+        for (int j0 = 0; j0 < nj; j0 += JB) {
+            if (j0 > 0 || e != gw) fetch(e, j0);
+#pragma unroll
+            for (int j = 0; j < JB; ++j) {
+                if (j0 + j >= nj) break;
+                const int i = lane + 32 * (j0 + j);
+                float w[8];
+                unpack8(raw[j], w);
+                w2 += dot8(w, w);
+#pragma unroll
+                for (int t = 0; t < TB; ++t) {
+                    float x[8];
+                    unpack8(i < chunks ? xs[t * chunks + i] : make_uint4(0, 0, 0, 0), x);
+                    acc[t] += dot8(w, x);
+                }
+            }
+        }
+        if (!joined) {                                                     // before the first store into another CTA's memory
+            asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+            joined = true;
+        }
+        w2_top = fmaxf(w2_top, warp_sum_f32(w2));
+        const float b = bias ? bias[e] : 0.f;
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+            float sum = warp_sum_f32(acc[t]);
+            if (lane == 0 && t < n_tok) {
+                sum += b;
+                if (addend) {
+                    const float before = fabsf(sum);
+                    sum += addend[(size_t)(t0 + t) * g.E + e];
+                    if (before > 2.f * fabsf(sum) + 16.f) *cluster.map_shared_rank(&cancelled, t) = 1;
+                }
+                cluster.map_shared_rank(z, t)[e] = sum;
+            }
+        }
+    }
+    if (!joined) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (lane < kFewCluster) cluster.map_shared_rank(w2_of, lane)[gw] = w2_top;
+    cluster.sync();
+    if (rank >= n_tok) return;
+    const size_t t = t0 + rank;
+    float dz = 0.f;
+    if (warp == 0) {
+        float w2 = 0.f, x2 = 0.f;
+#pragma unroll
+        for (int i = 0; i < kFewCluster * kGateWarps; i += 32) w2 = fmaxf(w2, w2_of[i + lane]);
+        w2 = warp_max(w2);
+#pragma unroll
+        for (int i = 0; i < kGateWarps; ++i) x2 += x2_of[i];
+        // the norms come out of binary32 sums, short by less than 1 %
+        dz = 1.01f * (float)(14 + (H + 255) / 256) * 0x1p-24f * sqrtf(x2) * sqrtf(w2) + (addend ? 16.f * 0x1p-24f : 0.f);
+        if (cancelled) dz = INFINITY;
+    }
+    for (bool decided = false;; decided = true) {
+        const bool again = warp == 0 && choose_fast<PER>(g, z, c, dz, bias || addend ? kAddedRel : 0.f, lane, decided, todo, ids + t * g.k, weights + t * g.k);
+        if (!__syncthreads_or(again)) return;
+        const uint32_t stage = todo[kTodoStage];
+        int item = 0;
+        for (int b = 0; 32 * b < g.E; ++b)
+            for (unsigned es = todo[b]; es; es &= es - 1, ++item) {
+                if (item % kGateWarps != warp) continue;
+                const int e = 32 * b + __ffs(es) - 1;
+                const double v = logit_f64(xs + (size_t)rank * chunks, reinterpret_cast<const uint4*>(w_router + (size_t)e * H), chunks, lane);
+                if (lane == 0) z64[e] = v + (bias ? (double)bias[e] : 0.0) + (addend ? (double)addend[t * g.E + e] : 0.0);
+            }
+        __syncthreads();
+        if (warp == 0) {
+            if (stage == GATE_ALL)
+                choose_exact(g, z64, key, lane, ids + t * g.k, weights + t * g.k);
+            else if (stage == GATE_EXPERTS)
+                choose_again<PER>(g, z, c, z64, todo, lane, ids + t * g.k, weights + t * g.k);
+            else
+                choose_groups<PER>(g, z, c, z64, reinterpret_cast<double*>(key), todo, lane);
+        }
+        if (stage != GATE_GROUPS) return;
+    }
 }
 
 int check_gate(const exmoe_shape* shape, const exmoe_gate* gate, int T, GateArgs* a) {
@@ -68,14 +269,71 @@ int check_gate(const exmoe_shape* shape, const exmoe_gate* gate, int T, GateArgs
         return EXMOE_ERR_SHAPE;
     const int size = shape->num_experts / gate->num_groups;
     if (shape->top_k > gate->top_groups * size) return EXMOE_ERR_SHAPE;
+    int log_lanes = 5;
+    while (gate->num_groups << log_lanes > 32) --log_lanes;
     *a = GateArgs{shape->num_experts, shape->top_k, gate->num_groups, size, gate->top_groups, gate->score == EXMOE_SCORE_SIGMOID,
-                  gate->group_score == EXMOE_GROUP_TOP2, gate->renormalise != 0, gate->weight_scale, nullptr};
+                  gate->group_score == EXMOE_GROUP_TOP2, gate->renormalise != 0, gate->weight_scale, nullptr, 1 << log_lanes, log_lanes, (size + (1 << log_lanes) - 1) >> log_lanes, 1.f / (float)size};
     return EXMOE_OK;
 }
-int launched() {
-    if (cudaGetLastError() != cudaSuccess) return EXMOE_ERR_CUDA;
+
+// every form is a programmatic dependent of the kernel before it in the stream (it waits for it before it reads anything)
+template <typename... P, typename... A>
+int launch(void (*kern)(P...), unsigned ctas, int threads, int cluster, size_t smem, SmemOnce& once, cudaStream_t st, A... args) {
+    if (!allow_smem(kern, kGateSmemMax, once)) return EXMOE_ERR_CUDA;
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = dim3(ctas);
+    lc.blockDim = dim3((unsigned)threads);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    lc.attrs = attr;
+    lc.numAttrs = cluster > 1 ? 2 : 1;
+#ifdef EXMOE_DISABLE_PDL
+    lc.attrs = attr + 1;
+    --lc.numAttrs;
+#endif
+    if (cudaLaunchKernelEx(&lc, kern, args...) != cudaSuccess) {
+        cudaGetLastError();
+        return EXMOE_ERR_CUDA;
+    }
     count_launch();
     return EXMOE_OK;
+}
+
+// A call's kernels by the number of experts: what choose_fast holds per lane.
+template <int TB, int PER>
+int launch_few(const __nv_bfloat16* x, const __nv_bfloat16* w, const float* bias, const float* addend, int T, int H, const GateArgs& g, int32_t* ids,
+               float* wts, cudaStream_t st) {
+    static SmemOnce once;
+    const size_t smem = (((size_t)g.E * 24 + 15) & ~size_t(15)) + (size_t)TB * H * 2;
+    return launch(gate_few_kernel<TB, PER>, (unsigned)((T + TB - 1) / TB * kFewCluster), kGateThreads, kFewCluster, smem, once, st, x, w, bias, addend, T, H, g, ids, wts);
+}
+template <int TB>
+int launch_few(const __nv_bfloat16* x, const __nv_bfloat16* w, const float* bias, const float* addend, int T, int H, const GateArgs& g, int32_t* ids,
+               float* wts, cudaStream_t st) {
+    if (g.E <= 64) return launch_few<TB, 2>(x, w, bias, addend, T, H, g, ids, wts, st);
+    if (g.E <= 128) return launch_few<TB, 4>(x, w, bias, addend, T, H, g, ids, wts, st);
+    if (g.E <= 256) return launch_few<TB, 8>(x, w, bias, addend, T, H, g, ids, wts, st);
+    return launch_few<TB, 16>(x, w, bias, addend, T, H, g, ids, wts, st);
+}
+template <typename Z, int PER>
+int launch_logits(const Z* z, long long ld, int T, const GateArgs& g, int32_t* ids, float* wts, cudaStream_t st) {
+    static SmemOnce once;
+    const int warps = std::max(1, std::min(kGateWarps, (int)(kGateSmemMax / (16 * (size_t)g.E))));   // more than one for choose_fast's
+    return launch(gate_logits_kernel<Z, PER>, (unsigned)(((long long)T + warps - 1) / warps), 32 * warps, 1, (size_t)warps * 16 * g.E, once, st, z, ld, T, g, ids, wts);
+}
+template <typename Z>
+int launch_logits(const Z* z, long long ld, int T, const GateArgs& g, int32_t* ids, float* wts, cudaStream_t st) {
+    if (g.E > kFastExperts || g.k > kFastChoices) return launch_logits<Z, 0>(z, ld, T, g, ids, wts, st);
+    if (g.E <= 64) return launch_logits<Z, 2>(z, ld, T, g, ids, wts, st);
+    if (g.E <= 128) return launch_logits<Z, 4>(z, ld, T, g, ids, wts, st);
+    if (g.E <= 256) return launch_logits<Z, 8>(z, ld, T, g, ids, wts, st);
+    return launch_logits<Z, 16>(z, ld, T, g, ids, wts, st);
 }
 
 }  // namespace
@@ -92,11 +350,12 @@ extern "C" int exmoe_route_gated(const exmoe_shape* shape, const exmoe_gate* gat
     if (!hidden_bf16 || !router_bf16 || !topk_ids || !topk_weights) return EXMOE_ERR_ARG;
     if ((reinterpret_cast<uintptr_t>(hidden_bf16) | reinterpret_cast<uintptr_t>(router_bf16)) & 15) return EXMOE_ERR_ARG;
     g.balance = balance;
+    const __nv_bfloat16 *x = (const __nv_bfloat16*)hidden_bf16, *w = (const __nv_bfloat16*)router_bf16;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (g.E <= kFastExperts && g.k <= kFastChoices && 24 * (size_t)g.E + 8 * (size_t)H + 16 <= (size_t)kGateSmemMax)
+        return T < kFewFour ? launch_few<1>(x, w, bias, addend, T, H, g, topk_ids, topk_weights, st) : launch_few<4>(x, w, bias, addend, T, H, g, topk_ids, topk_weights, st);
     static SmemOnce once;
-    if (!allow_smem(gate_token_kernel, kGateSmemMax, once)) return EXMOE_ERR_CUDA;
-    gate_token_kernel<<<T, kGateThreads, 2 * (size_t)H + 16 * (size_t)g.E, (cudaStream_t)stream>>>(
-        (const __nv_bfloat16*)hidden_bf16, (const __nv_bfloat16*)router_bf16, bias, addend, H, g, topk_ids, topk_weights);
-    return launched();
+    return launch(gate_token_kernel, (unsigned)T, kGateThreads, 1, 2 * (size_t)H + 16 * (size_t)g.E, once, st, x, w, bias, addend, H, g, topk_ids, topk_weights);
 }
 
 extern "C" int exmoe_gate_logits(const exmoe_shape* shape, const exmoe_gate* gate, const void* logits, int type, int64_t row_stride,
@@ -108,18 +367,9 @@ extern "C" int exmoe_gate_logits(const exmoe_shape* shape, const exmoe_gate* gat
     if (T == 0) return EXMOE_OK;
     if (!logits || !topk_ids || !topk_weights) return EXMOE_ERR_ARG;
     g.balance = balance;
-    const int warps = std::max(1, std::min(kGateWarps, (int)(kGateSmemMax / (16 * (size_t)g.E))));
-    const size_t smem = (size_t)warps * 16 * g.E;
-    const unsigned ctas = (unsigned)(((long long)T + warps - 1) / warps);
-    static SmemOnce once[2];
-    if (type == EXMOE_F32) {
-        if (!allow_smem(gate_logits_kernel<float>, kGateSmemMax, once[0])) return EXMOE_ERR_CUDA;
-        gate_logits_kernel<float><<<ctas, 32 * warps, smem, (cudaStream_t)stream>>>((const float*)logits, row_stride, T, g, topk_ids, topk_weights);
-    } else {
-        if (!allow_smem(gate_logits_kernel<__nv_bfloat16>, kGateSmemMax, once[1])) return EXMOE_ERR_CUDA;
-        gate_logits_kernel<__nv_bfloat16><<<ctas, 32 * warps, smem, (cudaStream_t)stream>>>((const __nv_bfloat16*)logits, row_stride, T, g, topk_ids, topk_weights);
-    }
-    return launched();
+    cudaStream_t st = (cudaStream_t)stream;
+    return type == EXMOE_F32 ? launch_logits((const float*)logits, row_stride, T, g, topk_ids, topk_weights, st)
+                             : launch_logits((const __nv_bfloat16*)logits, row_stride, T, g, topk_ids, topk_weights, st);
 }
 
 }  // namespace exmoe

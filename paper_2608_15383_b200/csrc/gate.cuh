@@ -9,7 +9,14 @@ struct GateArgs {
     bool sigmoid, top2, renorm;
     float scale;
     const float* balance;              // [E] or null
+    int lanes, log_lanes;              // lanes per group where a warp looks at all of them: 32 / (groups rounded up to a power of two)
+    int turns;                         // ceil(size / lanes)
+    float inv_size;                    // 1 / size
 };
+constexpr int kFastExperts = 512, kFastChoices = 32;                       // what choose_fast takes
+// What it leaves where it cannot decide: a bit per expert whose logit decides, the groups kept, and what is to be done with these logits
+constexpr int kTodoKept = kFastExperts / 32, kTodoStage = kTodoKept + 1, kTodoWords = kTodoKept + 2;
+enum { GATE_EXPERTS = 0, GATE_ALL = 1, GATE_GROUPS = 2 };
 
 // Doubles as integers of the same order: 0 is left for an expert that cannot be chosen, 1 is a NaN, -infinity follows; zeros of both signs are equal.
 __device__ __forceinline__ unsigned long long order_key(double v) {
@@ -23,15 +30,37 @@ __device__ __forceinline__ double warp_sum_f64(double s) {
     return s;
 }
 
-// The groups that keep their experts (a bit each), from lane g's value of group g.
+// The groups that keep their experts (bit o * g.lanes: group o), from the value of group lane / g.lanes.
 template <typename T>
-__device__ __forceinline__ unsigned kept_groups(T value, int G, int top_groups, int lane) {
+__device__ __forceinline__ unsigned kept_groups(const GateArgs& g, T value, int lane) {
+    const int mine = lane >> g.log_lanes;
     int before = 0;
-    for (int g = 0; g < G; ++g) {
-        const T v = __shfl_sync(0xffffffffu, value, g);
-        before += v > value || (v == value && g < lane);
+    for (int o = 0; o < g.G; ++o) {
+        const T v = __shfl_sync(0xffffffffu, value, o << g.log_lanes);
+        before += v > value || (v == value && o < mine);
     }
-    return __ballot_sync(0xffffffffu, lane < G && before < top_groups);
+    return __ballot_sync(0xffffffffu, mine < g.G && before < g.top_groups);
+}
+__device__ __forceinline__ int group_lane(const GateArgs& g, int e) { return (int)(((float)e + 0.5f) * g.inv_size) << g.log_lanes; }
+__device__ __forceinline__ bool in_kept(const GateArgs& g, unsigned kept, int e) { return kept >> group_lane(g, e) & 1u; }
+// The largest and second largest of a group's values v [E], in all of its lanes; a NaN is none.
+template <typename T>
+__device__ __forceinline__ void two_largest(const GateArgs& g, const T* v, int lane, T& a, T& b) {
+    const int grp = lane >> g.log_lanes, sub = lane & (g.lanes - 1);
+    a = b = -INFINITY;
+    if (grp < g.G)
+        for (int i = 0, at = grp % g.turns; i < g.turns; ++i, at = at + 1 == g.turns ? 0 : at + 1) {     // groups start apart: other banks
+            const int idx = sub + (at << g.log_lanes);
+            T x = idx < g.size ? v[grp * g.size + idx] : -INFINITY;
+            if (x != x) x = -INFINITY;
+            b = max(b, min(a, x));
+            a = max(a, x);
+        }
+    for (int m = g.lanes / 2; m >= 1; m /= 2) {
+        const T oa = __shfl_xor_sync(0xffffffffu, a, m), ob = __shfl_xor_sync(0xffffffffu, b, m);
+        b = max(max(b, ob), min(a, oa));
+        a = max(a, oa);
+    }
 }
 
 // The whole choice in binary64, by one warp.  z: the token's logits, key: room for as many integers (both in shared memory).
@@ -59,25 +88,14 @@ __device__ __noinline__ void choose_exact(const GateArgs& g, const double* z, un
     __syncwarp();
     const double* by = g.balance ? c : z;                                  // what orders the experts
     if (grouped) {
-        double value = kMasked;
-        if (lane < g.G) {
-            const double* v = (g.top2 ? c : by) + lane * g.size;
-            double a = kMasked, b = kMasked;
-            for (int i = 0; i < g.size; ++i) {
-                if (v[i] > a) {
-                    b = a;
-                    a = v[i];
-                } else if (v[i] > b) {
-                    b = v[i];
-                }
-            }
-            value = g.top2 && b > kMasked ? a + b : a;
-        }
-        kept = kept_groups(value, g.G, g.top_groups, lane);
+        double a, b;
+        two_largest(g, g.top2 ? c : by, lane, a, b);
+        const double value = g.top2 && b > kMasked ? a + b : a;
+        kept = kept_groups(g, value, lane);
         __syncwarp();
     }
-    for (int e = lane; e < g.E; e += 32) key[e] = !grouped || (kept >> (e / g.size) & 1u) ? order_key(by[e]) : 0ull;
-    double total = 0.0;
+    for (int e = lane; e < g.E; e += 32) key[e] = !grouped || in_kept(g, kept, e) ? order_key(by[e]) : 0ull;
+    double top = kMasked;                                                  // of the chosen
     for (int j = 0; j < g.k; ++j) {
         unsigned long long best = 0;
         int at = 0x7fffffff;
@@ -90,15 +108,305 @@ __device__ __noinline__ void choose_exact(const GateArgs& g, const double* z, un
         const unsigned lo = __reduce_max_sync(0xffffffffu, (unsigned)(best >> 32) == hi ? (unsigned)best : 0u);
         const bool mine = (unsigned)(best >> 32) == hi && (unsigned)best == lo;
         const int e = (int)__reduce_min_sync(0xffffffffu, mine ? (unsigned)at : 0x7fffffffu);
-        total += score(z[e]);
+        top = fmax(top, z[e]);
         if (lane == 0) {
             ids[j] = e;
             key[e] = 0ull;
         }
         __syncwarp();
     }
-    const double f = g.renorm ? (total == 0.0 ? 0.0 : 1.0 / total) : 1.0;
+    double f = 1.0;
+    if (g.renorm) {
+        if (!g.sigmoid && inv == inv && top > kMasked) {                   // relative to the largest chosen: the others may all be below 2^-1074 of the largest of all
+            mx = top;
+            inv = 1.0;
+        }
+        double total = 0.0;
+        for (int j = lane; j < g.k; j += 32) total += score(z[ids[j]]);
+        total = warp_sum_f64(total);
+        f = total == 0.0 ? 0.0 : 1.0 / total;
+    }
     for (int j = lane; j < g.k; j += 32) weights[j] = (float)(score(z[ids[j]]) * f * (double)g.scale);
+}
+
+// ---- the choice in binary32, with what it cannot decide left to choose_exact -------------------------------------------------
+// The logits are within dz + rel |z| of the true ones (for what follows, within dz), and a score computed from them within a few roundings of the true one.  With
+// |ds/dz| <= 1/4 for a sigmoid and |ds_e| <= 2 s_e (1 - s_e) dz <= dz / 2 for a softmax whose logits are all off by dz at most (0.26 and 0.55
+// with the terms of second order, for dz <= 0.05) two choice values that are further apart than `near` below are in their true
+// order.  Where a decision rests on a smaller distance, the experts that it concerns are marked, to be looked at again.
+__device__ __forceinline__ uint32_t order_key(float v) {                   // as above; no NaN comes here; 0: cannot be chosen
+    const uint32_t b = __float_as_uint(v + 0.f);
+    return b >> 31 ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k); }
+__device__ __forceinline__ float warp_max(float v) { return key_value(__reduce_max_sync(0xffffffffu, order_key(v))); }
+__device__ __forceinline__ float warp_sum_f32(float s) {
+#pragma unroll
+    for (int m = 16; m >= 1; m >>= 1) s += __shfl_xor_sync(0xffffffffu, s, m);
+    return s;
+}
+__device__ __forceinline__ float sigmoid(float z) {
+    const float e = expf(-fabsf(z));
+    return (z >= 0.f ? 1.f : e) / (1.f + e);
+}
+// exp(z - top): the rounding of the difference, 2^-24 of it, is put back
+__device__ __forceinline__ float exp_below(float z, float top) {
+    const float d = z - top, back = d + top;
+    const float err = (z - back) + ((back - d) - top);
+    const float e = expf(d);
+    return d > -INFINITY ? fmaf(e, err, e) : 0.f;
+}
+
+// Lane j's choice and its weight; mx: the largest logit, sum: of the exponentials below it.  False: too small for binary32, nothing written.
+__device__ __forceinline__ bool write_choice(const GateArgs& g, float z, float mx, float sum, int mine, int lane, int32_t* ids, float* weights) {
+    float s;
+    if (g.sigmoid) {
+        s = sigmoid(z);
+    } else {
+        const float top = g.renorm ? warp_max(lane < g.k ? z : -INFINITY) : mx;
+        s = top > -INFINITY ? exp_below(z, top) : 0.f;
+        if (!g.renorm) s /= sum;
+    }
+    if (g.renorm) {
+        const float total = warp_sum_f32(lane < g.k ? s : 0.f);
+        if (g.sigmoid && total < 1e-30f) return false;                     // nothing left, or nearly
+        s = total > 0.f ? s / total : 0.f;
+    }
+    if (lane < g.k) {
+        ids[lane] = mine;
+        weights[lane] = s * g.scale;
+    }
+    return true;
+}
+
+// By one warp, lane l holding experts l, l + 32, ...; z [E] and c [E]: shared memory, logits and room; at most kFastChoices choices.
+// `decided`: the groups are those of todo[kTodoKept].  True: nothing is written, and `todo` says what is to be done.
+template <int PER>
+__device__ __forceinline__ bool choose_fast(const GateArgs& g, const float* z, float* c, float dz, float rel, int lane, bool decided, uint32_t* todo,
+                                            int32_t* ids, float* weights) {
+    const bool grouped = g.top_groups < g.G, by_score = g.balance || (grouped && g.top2);
+    float by[PER], bias[PER];
+    float mx = -INFINITY;
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int e = lane + 32 * i;
+        bias[i] = g.balance && e < g.E ? g.balance[e] : 0.f;
+        by[i] = e < g.E ? z[e] : -INFINITY;
+        odd |= !(by[i] < INFINITY);                                        // a NaN or +infinity
+        mx = fmaxf(mx, by[i]);
+    }
+    mx = warp_max(mx);
+    // rel: |z| s (1 - s) < 0.23 for a sigmoid; in a softmax logits 100 below the largest have no part
+    const float dzs = dz + (g.sigmoid ? rel : rel * (fabsf(mx) + 100.f));
+    odd = __any_sync(0xffffffffu, odd) || mx == -INFINITY || !(dzs <= 0.05f);
+    // a sigmoid is within 5 x 2^-24 of the true one, a probability (an argument off by 2^-24 of itself, p |argument| < 0.37; up to 25
+    // roundings in exponentials, sum and quotient) within 2e-6; c itself rounds once more
+    const float score_near = (g.sigmoid ? 2.f * 0.26f : 2.f * 0.55f) * dzs + (g.sigmoid ? 6e-7f : 4e-6f);
+    const float near0 = g.balance ? score_near : 2.f * dz, near1 = g.balance ? 1.2e-7f : rel;            // near = near0 + near1 (|a| + |b|)
+    float sum = 1.f;
+    if (!odd) {
+        float t[PER];
+        if (!g.sigmoid && (by_score || !g.renorm)) {
+            float part[PER];
+#pragma unroll
+            for (int i = 0; i < PER; ++i) part[i] = t[i] = expf(by[i] - mx);
+#pragma unroll
+            for (int n = PER / 2; n >= 1; n /= 2)
+#pragma unroll
+                for (int i = 0; i < n; ++i) part[i] += part[i + n];
+            sum = warp_sum_f32(part[0]);
+        }
+        if (by_score) {
+            const float inv = 1.f / sum;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int e = lane + 32 * i;
+                if (e < g.E) {
+                    const float v = by[i] == -INFINITY ? -INFINITY : (g.sigmoid ? sigmoid(by[i]) : t[i] * inv) + bias[i];
+                    odd |= !(v < INFINITY);                                // of a bias
+                    c[e] = v;
+                    if (g.balance) by[i] = v;
+                }
+            }
+            odd = __any_sync(0xffffffffu, odd);
+            __syncwarp();
+        }
+    }
+    int stage = odd ? GATE_ALL : GATE_EXPERTS, mine = 0;
+    unsigned again = 0, kept = decided ? todo[kTodoKept] : 0xffffffffu;
+    if (grouped && !decided && !odd) {
+        float a, b;
+        two_largest(g, by_score ? c : z, lane, a, b);
+        const float value = g.top2 && b > -INFINITY ? a + b : a;
+        kept = kept_groups(g, value, lane);
+        const bool real = lane >> g.log_lanes < g.G, keep = kept >> (lane & -g.lanes) & 1u;
+        // the smallest value kept against the largest dropped; a masked group's -infinity is exact
+        const float low = -warp_max(real && keep ? -value : -INFINITY), high = warp_max(real && !keep ? value : -INFINITY);
+        const float near_v = by_score ? score_near : 2.f * dz, rel_v = by_score ? 2.4e-7f : rel;
+        const float near = (g.top2 ? 2.f : 1.f) * near_v + rel_v * (fabsf(low) + fabsf(high));
+        if (near > 0.f && high > -INFINITY && low - high <= near) {
+            // the groups on the border, and of each the experts that may be its largest (two)
+            const bool border = real && (keep ? value <= high + near : value >= low - near);
+            const float least = border ? (g.top2 && b > -INFINITY ? b : a) : INFINITY;
+            const float reach = near_v + 2.f * rel_v * fabsf(least);
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int e = lane + 32 * i, at = group_lane(g, min(e, g.E - 1));
+                const float t0 = __shfl_sync(0xffffffffu, least, at), t1 = __shfl_sync(0xffffffffu, reach, at);
+                if (e < g.E && t0 < INFINITY && (by_score ? c[e] : z[e]) >= t0 - t1) again |= 1u << i;
+            }
+            stage = GATE_GROUPS;
+        }
+    }
+    if (stage == GATE_EXPERTS) {
+        uint32_t key[PER];
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int e = lane + 32 * i;
+            key[i] = e < g.E && (!grouped || in_kept(g, kept, e)) ? order_key(by[i]) : 0u;
+        }
+        float prev = 0.f;
+        int prev_e = 0;
+        const bool exact = near0 == 0.f;
+        for (int j = 0; j < g.k + (exact ? 0 : 1); ++j) {
+            uint32_t best = 0;
+            int be = 0x7fffffff;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (key[i] > best) {                                       // ascending experts: the first maximum wins
+                    best = key[i];
+                    be = lane + 32 * i;
+                }
+            const uint32_t top = __reduce_max_sync(0xffffffffu, best);
+            if (!top) break;                                               // no other expert can be chosen
+            const int e = (int)__reduce_min_sync(0xffffffffu, best == top ? (unsigned)be : 0x7fffffffu);
+            if (!exact) {
+                const float v = key_value(top);
+                const float near = near0 + near1 * (fabsf(prev) + fabsf(v));
+                if (j > 0 && v > -INFINITY && prev - v <= near) {
+                    if (lane == (prev_e & 31)) again |= 1u << (prev_e >> 5);
+                    if (lane == (e & 31)) again |= 1u << (e >> 5);
+                    if (j == g.k)                                          // whatever could displace the last choice
+#pragma unroll
+                        for (int i = 0; i < PER; ++i)
+                            if (key[i] && key_value(key[i]) >= prev - near) again |= 1u << i;
+                }
+                prev = v;
+                prev_e = e;
+            }
+            if (j == lane) mine = e;
+            if (lane == (e & 31))
+#pragma unroll
+                for (int i = 0; i < PER; ++i)
+                    if (i == e >> 5) key[i] = 0;
+        }
+    }
+    const bool some = __any_sync(0xffffffffu, again != 0);
+    if (some && !g.sigmoid && g.balance) stage = GATE_ALL;                 // a softmax with a bias: all logits enter every choice value
+    if (stage == GATE_EXPERTS && !some) {
+        if (write_choice(g, z[mine], mx, sum, mine, lane, ids, weights)) return false;
+        stage = GATE_ALL;
+    }
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const unsigned m = __ballot_sync(0xffffffffu, (stage == GATE_ALL || (again >> i & 1u)) && lane + 32 * i < g.E);
+        if (lane == 0) todo[i] = m;
+    }
+    if (lane == 0) {
+        todo[kTodoKept] = kept;
+        todo[kTodoStage] = stage;
+    }
+    __syncwarp();
+    return true;
+}
+
+// A marked expert's logit: from z64, or z itself where that is exact (z64 null).
+__device__ __forceinline__ double marked_logit(const double* z64, const float* z, int e) { return z64 ? z64[e] : (double)z[e]; }
+// The groups kept, from the exact logits of the marked experts, for choose_fast to go on from there; v [E]: room.
+template <int PER>
+__device__ __noinline__ void choose_groups(const GateArgs& g, float* z, const float* c, const double* z64, double* v, uint32_t* todo, int lane) {
+    const bool by_score = g.balance || g.top2;
+    float mx = -INFINITY, sum = 0.f;
+    if (!g.sigmoid && by_score) {                                          // as choose_fast: a common factor of all
+        for (int e = lane; e < g.E; e += 32) mx = fmaxf(mx, z[e]);
+        mx = warp_max(mx);
+        for (int e = lane; e < g.E; e += 32) sum += expf(z[e] - mx);
+        sum = warp_sum_f32(sum);
+    }
+    for (int i = 0; i < PER; ++i) {
+        const int e = lane + 32 * i;
+        if (e >= g.E) break;
+        double x = by_score ? (double)c[e] : (double)z[e];
+        if (todo[i] >> lane & 1u) {
+            x = marked_logit(z64, z, e);
+            z[e] = (float)x;
+            if (by_score && x > -INFINITY)
+                x = (g.sigmoid ? 1.0 / (1.0 + exp(-x)) : exp(x - (double)mx) / (double)sum) + (g.balance ? (double)g.balance[e] : 0.0);
+        }
+        v[e] = x;
+    }
+    __syncwarp();
+    double a, b;
+    two_largest(g, v, lane, a, b);
+    const unsigned kept = kept_groups(g, g.top2 && b > -INFINITY ? a + b : a, lane);
+    if (lane == 0) todo[kTodoKept] = kept;
+    __syncwarp();
+}
+
+// The experts chosen again by one warp, from the exact logits of the marked ones.  What was not marked is far enough from everything else to be ordered by its binary32 value.
+template <int PER>
+__device__ __noinline__ void choose_again(const GateArgs& g, float* z, const float* c, const double* z64, const uint32_t* todo, int lane, int32_t* ids,
+                                          float* weights) {
+    const bool grouped = g.top_groups < g.G;
+    const unsigned kept = todo[kTodoKept];
+    unsigned long long key[PER];
+    float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int e = lane + 32 * i;
+        key[i] = 0;
+        if (e < g.E) {
+            double v = g.balance ? (double)c[e] : (double)z[e];
+            if (todo[i] >> lane & 1u) {
+                const double x = marked_logit(z64, z, e);
+                v = x;
+                if (g.balance) v = x == -INFINITY ? x : 1.0 / (1.0 + exp(-x)) + (double)g.balance[e];      // a sigmoid: a softmax with a bias marks all
+                z[e] = (float)x;
+            }
+            if (!grouped || in_kept(g, kept, e)) key[i] = order_key(v);
+            mx = fmaxf(mx, z[e]);
+        }
+    }
+    mx = warp_max(mx);
+    if (!g.sigmoid && !g.renorm) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (lane + 32 * i < g.E) sum += expf(z[lane + 32 * i] - mx);
+        sum = warp_sum_f32(sum);
+    }
+    int mine = 0;
+    for (int j = 0; j < g.k; ++j) {
+        unsigned long long best = 0;
+        int at = 0x7fffffff;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (key[i] > best) {
+                best = key[i];
+                at = lane + 32 * i;
+            }
+        const unsigned hi = __reduce_max_sync(0xffffffffu, (unsigned)(best >> 32));
+        const unsigned lo = __reduce_max_sync(0xffffffffu, (unsigned)(best >> 32) == hi ? (unsigned)best : 0u);
+        const bool is = (unsigned)(best >> 32) == hi && (unsigned)best == lo;
+        const int e = (int)__reduce_min_sync(0xffffffffu, is ? (unsigned)at : 0x7fffffffu);
+        if (j == lane) mine = e;
+        if (lane == (e & 31))
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                if (i == e >> 5) key[i] = 0;
+    }
+    __syncwarp();
+    write_choice(g, z[mine], mx, sum, mine, lane, ids, weights);
 }
 
 }  // namespace exmoe
