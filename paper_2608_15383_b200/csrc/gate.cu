@@ -82,41 +82,58 @@ gate_token_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__
     if (warp == 0) choose_exact(g, z, key, lane, ids + t * g.k, weights + t * g.k);
 }
 
-// One warp per token; 16 bytes of shared memory per expert and warp.  PER: experts per lane of choose_fast, 0: all in binary64.
+// One warp per token.  PER: experts per lane of choose_fast, 0: all in binary64.  Shared memory, per warp: logits_room(), and the balance
+// bias where choose_fast reads it.
+template <int PER>
+__host__ __device__ constexpr size_t logits_room(int E) {
+    if constexpr (PER > 0)
+        return sizeof(ChoiceRoom<PER>) + 8 * 32 * PER;
+    else
+        return 16 * (size_t)E;
+}
 template <typename Z, int PER>
 __global__ void __launch_bounds__(kGateThreads)
 gate_logits_kernel(const Z* logits, long long ld, int T, GateArgs g, int32_t* ids, float* weights) {
     extern __shared__ __align__(16) unsigned char smem[];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    unsigned char* mine = smem + (size_t)warp * 16 * g.E;
-    const size_t t = (size_t)blockIdx.x * (blockDim.x >> 5) + warp;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    unsigned char* mine = smem + warp * logits_room<PER>(g.E);
+    const size_t t = (size_t)blockIdx.x * warps + warp;
     grid_dependency_wait();
     grid_launch_dependents();
-    if (t >= (size_t)T) return;
     const Z* row = logits + (long long)t * ld;
+    double *z64, *key;
     if constexpr (PER > 0) {
-        float *z = reinterpret_cast<float*>(mine), *c = z + g.E;
+        float* balance = nullptr;
+        if (g.balance) {
+            balance = reinterpret_cast<float*>(smem + warps * logits_room<PER>(g.E));
+            for (int e = threadIdx.x; e < 32 * PER; e += blockDim.x) balance[e] = e < g.E ? g.balance[e] : 0.f;
+            __syncthreads();
+        }
+        if (t >= (size_t)T) return;
+        ChoiceRoom<PER>& room = *reinterpret_cast<ChoiceRoom<PER>*>(mine);
         float v[PER];
 #pragma unroll
-        for (int i = 0; i < PER; ++i) v[i] = lane + 32 * i < g.E ? (float)row[lane + 32 * i] : 0.f;
+        for (int i = 0; i < PER; ++i) v[i] = lane + 32 * i < g.E ? (float)row[lane + 32 * i] : -INFINITY;
 #pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (lane + 32 * i < g.E) z[lane + 32 * i] = v[i];
+        for (int i = 0; i < PER; ++i) room.z[lane + 32 * i] = v[i];
         __syncwarp();
-        __shared__ uint32_t todos[kGateWarps][kTodoWords];
-        uint32_t* todo = todos[warp];
+        z64 = reinterpret_cast<double*>(mine + sizeof(ChoiceRoom<PER>));
+        key = reinterpret_cast<double*>(room.z);                           // z and c
         for (bool decided = false;; decided = true) {
-            if (!choose_fast<PER>(g, z, c, 0.f, 0.f, lane, decided, todo, ids + t * g.k, weights + t * g.k)) return;
-            if (todo[kTodoStage] == GATE_EXPERTS) return choose_again<PER>(g, z, c, nullptr, todo, lane, ids + t * g.k, weights + t * g.k);
-            if (todo[kTodoStage] == GATE_ALL) break;
-            choose_groups<PER>(g, z, c, nullptr, reinterpret_cast<double*>(c + g.E), todo, lane);
+            if (!choose_fast<PER>(g, room, balance, 0.f, 0.f, lane, decided, ids + t * g.k, weights + t * g.k)) return;
+            if (room.todo[kTodoStage] == GATE_EXPERTS) return choose_again<PER>(g, room, nullptr, lane, ids + t * g.k, weights + t * g.k);
+            if (room.todo[kTodoStage] == GATE_ALL) break;
+            choose_groups<PER>(g, room, nullptr, z64, lane);
         }
         __syncwarp();
+    } else {
+        if (t >= (size_t)T) return;
+        z64 = reinterpret_cast<double*>(mine);
+        key = z64 + g.E;
     }
-    double* z = reinterpret_cast<double*>(mine);
-    for (int e = lane; e < g.E; e += 32) z[e] = (double)(float)row[e];
+    for (int e = lane; e < g.E; e += 32) z64[e] = (double)(float)row[e];
     __syncwarp();
-    choose_exact(g, z, reinterpret_cast<unsigned long long*>(z + g.E), lane, ids + t * g.k, weights + t * g.k);
+    choose_exact(g, z64, reinterpret_cast<unsigned long long*>(key), lane, ids + t * g.k, weights + t * g.k);
 }
 
 constexpr float kAddedRel = 3.f * 0x1p-24f;                                // bias and addend: 2^-24 (|sum before| + |z|), with |sum before| <= 2 |z| + 16
@@ -128,6 +145,12 @@ constexpr float kAddedRel = 3.f * 0x1p-24f;                                // bi
 // former is larger than twice the latter + 16, all logits are computed again).  They travel through the cluster's shared
 // memory to the CTA that owns the token (i % 8), whose first warp chooses; where that rests on less than the bound, its warps
 // compute the logits that matter once more in binary64.
+template <int PER>
+struct __align__(16) FewRoom {
+    ChoiceRoom<PER> room;
+    float balance[32 * PER];
+    double z64[32 * PER], key[32 * PER];
+};
 constexpr int kFewCluster = 8, kFewFour = 48;                              // four tokens per cluster from here on
 template <int TB, int PER>
 __global__ void __launch_bounds__(kGateThreads)
@@ -135,12 +158,11 @@ gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w
                 GateArgs g, int32_t* ids, float* weights) {
     static_assert(TB <= kFewCluster, "a CTA owns at most one token");
     extern __shared__ __align__(16) unsigned char smem[];
-    double* z64 = reinterpret_cast<double*>(smem);
-    unsigned long long* key = reinterpret_cast<unsigned long long*>(z64 + g.E);
-    float *z = reinterpret_cast<float*>(key + g.E), *c = z + g.E;
-    uint4* xs = reinterpret_cast<uint4*>(smem + (((size_t)g.E * 24 + 15) & ~size_t(15)));   // [TB][H / 8]
+    FewRoom<PER>& sm = *reinterpret_cast<FewRoom<PER>*>(smem);
+    ChoiceRoom<PER>& room = sm.room;
+    float* z = room.z;
+    uint4* xs = reinterpret_cast<uint4*>(smem + sizeof(FewRoom<PER>));     // [TB][H / 8]
     __shared__ float w2_of[kFewCluster * kGateWarps], x2_of[kGateWarps];
-    __shared__ uint32_t todo[kTodoWords];
     __shared__ int cancelled;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, chunks = H / 8;
     const int rank = blockIdx.x % kFewCluster, t0 = (blockIdx.x / kFewCluster) * TB, n_tok = min(TB, T - t0);
@@ -163,6 +185,10 @@ gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w
     for (int i = n_tok * chunks + tid; i < TB * chunks; i += kGateThreads) xs[i] = make_uint4(0, 0, 0, 0);
     cg::cluster_group cluster = cg::this_cluster();
     if (tid == 0) cancelled = 0;
+    for (int e = tid; e < 32 * PER; e += kGateThreads) {
+        if (e >= g.E) z[e] = -INFINITY;
+        if (g.balance) sm.balance[e] = e < g.E ? g.balance[e] : 0.f;
+    }
     __syncthreads();
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // every CTA runs: its memory may be written
     {
@@ -234,25 +260,26 @@ gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w
         if (cancelled) dz = INFINITY;
     }
     for (bool decided = false;; decided = true) {
-        const bool again = warp == 0 && choose_fast<PER>(g, z, c, dz, bias || addend ? kAddedRel : 0.f, lane, decided, todo, ids + t * g.k, weights + t * g.k);
+        const bool again = warp == 0 && choose_fast<PER>(g, room, g.balance ? sm.balance : nullptr, dz, bias || addend ? kAddedRel : 0.f, lane, decided,
+                                                         ids + t * g.k, weights + t * g.k);
         if (!__syncthreads_or(again)) return;
-        const uint32_t stage = todo[kTodoStage];
+        const uint32_t stage = room.todo[kTodoStage];
         int item = 0;
         for (int b = 0; 32 * b < g.E; ++b)
-            for (unsigned es = todo[b]; es; es &= es - 1, ++item) {
+            for (unsigned es = room.todo[b]; es; es &= es - 1, ++item) {
                 if (item % kGateWarps != warp) continue;
                 const int e = 32 * b + __ffs(es) - 1;
                 const double v = logit_f64(xs + (size_t)rank * chunks, reinterpret_cast<const uint4*>(w_router + (size_t)e * H), chunks, lane);
-                if (lane == 0) z64[e] = v + (bias ? (double)bias[e] : 0.0) + (addend ? (double)addend[t * g.E + e] : 0.0);
+                if (lane == 0) sm.z64[e] = v + (bias ? (double)bias[e] : 0.0) + (addend ? (double)addend[t * g.E + e] : 0.0);
             }
         __syncthreads();
         if (warp == 0) {
             if (stage == GATE_ALL)
-                choose_exact(g, z64, key, lane, ids + t * g.k, weights + t * g.k);
+                choose_exact(g, sm.z64, reinterpret_cast<unsigned long long*>(sm.key), lane, ids + t * g.k, weights + t * g.k);
             else if (stage == GATE_EXPERTS)
-                choose_again<PER>(g, z, c, z64, todo, lane, ids + t * g.k, weights + t * g.k);
+                choose_again<PER>(g, room, sm.z64, lane, ids + t * g.k, weights + t * g.k);
             else
-                choose_groups<PER>(g, z, c, z64, reinterpret_cast<double*>(key), todo, lane);
+                choose_groups<PER>(g, room, sm.z64, sm.key, lane);
         }
         if (stage != GATE_GROUPS) return;
     }
@@ -272,7 +299,12 @@ int check_gate(const exmoe_shape* shape, const exmoe_gate* gate, int T, GateArgs
     int log_lanes = 5;
     while (gate->num_groups << log_lanes > 32) --log_lanes;
     *a = GateArgs{shape->num_experts, shape->top_k, gate->num_groups, size, gate->top_groups, gate->score == EXMOE_SCORE_SIGMOID,
-                  gate->group_score == EXMOE_GROUP_TOP2, gate->renormalise != 0, gate->weight_scale, nullptr, 1 << log_lanes, log_lanes, (size + (1 << log_lanes) - 1) >> log_lanes, 1.f / (float)size};
+                  gate->group_score == EXMOE_GROUP_TOP2, gate->renormalise != 0, gate->weight_scale, nullptr, 1 << log_lanes, log_lanes, (size + (1 << log_lanes) - 1) >> log_lanes, -1, 1.f / (float)size};
+    if (shape->num_experts <= kFastExperts) {                              // choose_fast's run of a lane
+        const int run = shape->num_experts <= 64 ? 2 : shape->num_experts <= 128 ? 4 : shape->num_experts <= 256 ? 8 : 16;
+        for (int l = 0; l <= 5; ++l)
+            if (run << l == size) a->log_run = l;
+    }
     return EXMOE_OK;
 }
 
@@ -310,7 +342,7 @@ template <int TB, int PER>
 int launch_few(const __nv_bfloat16* x, const __nv_bfloat16* w, const float* bias, const float* addend, int T, int H, const GateArgs& g, int32_t* ids,
                float* wts, cudaStream_t st) {
     static SmemOnce once;
-    const size_t smem = (((size_t)g.E * 24 + 15) & ~size_t(15)) + (size_t)TB * H * 2;
+    const size_t smem = sizeof(FewRoom<PER>) + (size_t)TB * H * 2;
     return launch(gate_few_kernel<TB, PER>, (unsigned)((T + TB - 1) / TB * kFewCluster), kGateThreads, kFewCluster, smem, once, st, x, w, bias, addend, T, H, g, ids, wts);
 }
 template <int TB>
@@ -324,8 +356,9 @@ int launch_few(const __nv_bfloat16* x, const __nv_bfloat16* w, const float* bias
 template <typename Z, int PER>
 int launch_logits(const Z* z, long long ld, int T, const GateArgs& g, int32_t* ids, float* wts, cudaStream_t st) {
     static SmemOnce once;
-    const int warps = std::max(1, std::min(kGateWarps, (int)(kGateSmemMax / (16 * (size_t)g.E))));   // more than one for choose_fast's
-    return launch(gate_logits_kernel<Z, PER>, (unsigned)(((long long)T + warps - 1) / warps), 32 * warps, 1, (size_t)warps * 16 * g.E, once, st, z, ld, T, g, ids, wts);
+    const size_t bias = PER && g.balance ? 128 * PER : 0, room = logits_room<PER>(g.E);
+    const int warps = std::max(1, std::min(kGateWarps, (int)((kGateSmemMax - bias) / room)));
+    return launch(gate_logits_kernel<Z, PER>, (unsigned)(((long long)T + warps - 1) / warps), 32 * warps, 1, warps * room + bias, once, st, z, ld, T, g, ids, wts);
 }
 template <typename Z>
 int launch_logits(const Z* z, long long ld, int T, const GateArgs& g, int32_t* ids, float* wts, cudaStream_t st) {
@@ -352,7 +385,7 @@ extern "C" int exmoe_route_gated(const exmoe_shape* shape, const exmoe_gate* gat
     g.balance = balance;
     const __nv_bfloat16 *x = (const __nv_bfloat16*)hidden_bf16, *w = (const __nv_bfloat16*)router_bf16;
     cudaStream_t st = (cudaStream_t)stream;
-    if (g.E <= kFastExperts && g.k <= kFastChoices && 24 * (size_t)g.E + 8 * (size_t)H + 16 <= (size_t)kGateSmemMax)
+    if (g.E <= kFastExperts && g.k <= kFastChoices && sizeof(FewRoom<16>) + 8 * (size_t)H <= (size_t)kGateSmemMax)
         return T < kFewFour ? launch_few<1>(x, w, bias, addend, T, H, g, topk_ids, topk_weights, st) : launch_few<4>(x, w, bias, addend, T, H, g, topk_ids, topk_weights, st);
     static SmemOnce once;
     return launch(gate_token_kernel, (unsigned)T, kGateThreads, 1, 2 * (size_t)H + 16 * (size_t)g.E, once, st, x, w, bias, addend, H, g, topk_ids, topk_weights);

@@ -11,6 +11,7 @@ struct GateArgs {
     const float* balance;              // [E] or null
     int lanes, log_lanes;              // lanes per group where a warp looks at all of them: 32 / (groups rounded up to a power of two)
     int turns;                         // ceil(size / lanes)
+    int log_run;                       // a group is 2^log_run lanes' experts where a lane holds choose_fast's run of them; -1: it is not
     float inv_size;                    // 1 / size
 };
 constexpr int kFastExperts = 512, kFastChoices = 32;                       // what choose_fast takes
@@ -30,20 +31,19 @@ __device__ __forceinline__ double warp_sum_f64(double s) {
     return s;
 }
 
-// The groups that keep their experts (bit o * g.lanes: group o), from the value of group lane / g.lanes.
+// The groups that keep their experts (a bit each), from lane o's value of group o.
 template <typename T>
 __device__ __forceinline__ unsigned kept_groups(const GateArgs& g, T value, int lane) {
-    const int mine = lane >> g.log_lanes;
     int before = 0;
     for (int o = 0; o < g.G; ++o) {
-        const T v = __shfl_sync(0xffffffffu, value, o << g.log_lanes);
-        before += v > value || (v == value && o < mine);
+        const T v = __shfl_sync(0xffffffffu, value, o);
+        before += v > value || (v == value && o < lane);
     }
-    return __ballot_sync(0xffffffffu, mine < g.G && before < g.top_groups);
+    return __ballot_sync(0xffffffffu, lane < g.G && before < g.top_groups);
 }
-__device__ __forceinline__ int group_lane(const GateArgs& g, int e) { return (int)(((float)e + 0.5f) * g.inv_size) << g.log_lanes; }
-__device__ __forceinline__ bool in_kept(const GateArgs& g, unsigned kept, int e) { return kept >> group_lane(g, e) & 1u; }
-// The largest and second largest of a group's values v [E], in all of its lanes; a NaN is none.
+__device__ __forceinline__ int group_of(const GateArgs& g, int e) { return (int)(((float)e + 0.5f) * g.inv_size); }
+__device__ __forceinline__ bool in_kept(const GateArgs& g, unsigned kept, int e) { return kept >> group_of(g, e) & 1u; }
+// The largest and second largest of group `lane`'s values v [E]; a NaN is none.
 template <typename T>
 __device__ __forceinline__ void two_largest(const GateArgs& g, const T* v, int lane, T& a, T& b) {
     const int grp = lane >> g.log_lanes, sub = lane & (g.lanes - 1);
@@ -61,6 +61,8 @@ __device__ __forceinline__ void two_largest(const GateArgs& g, const T* v, int l
         b = max(max(b, ob), min(a, oa));
         a = max(a, oa);
     }
+    a = __shfl_sync(0xffffffffu, a, (lane << g.log_lanes) & 31);
+    b = __shfl_sync(0xffffffffu, b, (lane << g.log_lanes) & 31);
 }
 
 // The whole choice in binary64, by one warp.  z: the token's logits, key: room for as many integers (both in shared memory).
@@ -157,53 +159,83 @@ __device__ __forceinline__ float exp_below(float z, float top) {
     return d > -INFINITY ? fmaf(e, err, e) : 0.f;
 }
 
-// Lane j's choice and its weight; mx: the largest logit, sum: of the exponentials below it.  False: too small for binary32, nothing written.
-__device__ __forceinline__ bool write_choice(const GateArgs& g, float z, float mx, float sum, int mine, int lane, int32_t* ids, float* weights) {
-    float s;
+// The weight of a chosen expert's logit, by the lanes that hold one (`chosen`); mx: the largest logit of all, sum: of the exponentials below
+// it.  False: too small for binary32.
+__device__ __forceinline__ bool choice_weight(const GateArgs& g, float z, bool chosen, float mx, float sum, float& s) {
     if (g.sigmoid) {
         s = sigmoid(z);
     } else {
-        const float top = g.renorm ? warp_max(lane < g.k ? z : -INFINITY) : mx;
+        const float top = g.renorm ? warp_max(chosen ? z : -INFINITY) : mx;
         s = top > -INFINITY ? exp_below(z, top) : 0.f;
         if (!g.renorm) s /= sum;
     }
     if (g.renorm) {
-        const float total = warp_sum_f32(lane < g.k ? s : 0.f);
+        const float total = warp_sum_f32(chosen ? s : 0.f);
         if (g.sigmoid && total < 1e-30f) return false;                     // nothing left, or nearly
         s = total > 0.f ? s / total : 0.f;
     }
-    if (lane < g.k) {
-        ids[lane] = mine;
-        weights[lane] = s * g.scale;
-    }
+    s *= g.scale;
     return true;
 }
 
-// By one warp, lane l holding experts l, l + 32, ...; z [E] and c [E]: shared memory, logits and room; at most kFastChoices choices.
-// `decided`: the groups are those of todo[kTodoKept].  True: nothing is written, and `todo` says what is to be done.
+// What a warp needs in shared memory for a token's choice.
 template <int PER>
-__device__ __forceinline__ bool choose_fast(const GateArgs& g, const float* z, float* c, float dz, float rel, int lane, bool decided, uint32_t* todo,
+struct __align__(16) ChoiceRoom {
+    float z[32 * PER];                                                     // logits, -infinity behind the last
+    float c[32 * PER];                                                     // choice values
+    float value[32];                                                       // candidates
+    int expert[32];
+    uint32_t todo[kTodoWords];
+};
+template <int PER>
+__device__ __forceinline__ void load_run(const float* p, float (&v)[PER]) {
+    if constexpr (PER == 2) {
+        const float2 a = *reinterpret_cast<const float2*>(p);
+        v[0] = a.x, v[1] = a.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; i += 4) {
+            const float4 a = *reinterpret_cast<const float4*>(p + i);
+            v[i] = a.x, v[i + 1] = a.y, v[i + 2] = a.z, v[i + 3] = a.w;
+        }
+    }
+}
+template <int PER>
+__device__ __forceinline__ void store_run(float* p, const float (&v)[PER]) {
+    if constexpr (PER == 2) {
+        *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < PER; i += 4) *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    }
+}
+
+// By one warp; lane l holds the PER experts from PER l on; `balance`: g.balance in shared memory, padded to 32 PER, or null; at most kFastChoices
+// choices.  `decided`: the groups are those of todo[kTodoKept].  True: nothing is written, and `todo` says what is to be done.
+// The choice itself: the k-th largest of the lanes' largest values is no more than the k-th largest value, so what is not below
+// it (by more than `near`) are all candidates, k and a few more; they go to a lane each, which counts those before its own.  (Instead
+// of k rounds of arg-max, which took twice the instructions.)
+template <int PER>
+__device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& room, const float* balance, float dz, float rel, int lane, bool decided,
                                             int32_t* ids, float* weights) {
-    const bool grouped = g.top_groups < g.G, by_score = g.balance || (grouped && g.top2);
-    float by[PER], bias[PER];
-    float mx = -INFINITY;
+    const bool grouped = g.top_groups < g.G, by_score = balance || (grouped && g.top2);
+    float by[PER], other[PER];                                             // what orders the experts; scores where these are not it
+    load_run<PER>(room.z + PER * lane, by);
+    float mx = by[0];
     bool odd = false;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        const int e = lane + 32 * i;
-        bias[i] = g.balance && e < g.E ? g.balance[e] : 0.f;
-        by[i] = e < g.E ? z[e] : -INFINITY;
         odd |= !(by[i] < INFINITY);                                        // a NaN or +infinity
         mx = fmaxf(mx, by[i]);
     }
-    mx = warp_max(mx);
+    mx = warp_max(mx == mx ? mx : -INFINITY);
     // rel: |z| s (1 - s) < 0.23 for a sigmoid; in a softmax logits 100 below the largest have no part
     const float dzs = dz + (g.sigmoid ? rel : rel * (fabsf(mx) + 100.f));
     odd = __any_sync(0xffffffffu, odd) || mx == -INFINITY || !(dzs <= 0.05f);
     // a sigmoid is within 5 x 2^-24 of the true one, a probability (an argument off by 2^-24 of itself, p |argument| < 0.37; up to 25
     // roundings in exponentials, sum and quotient) within 2e-6; c itself rounds once more
     const float score_near = (g.sigmoid ? 2.f * 0.26f : 2.f * 0.55f) * dzs + (g.sigmoid ? 6e-7f : 4e-6f);
-    const float near0 = g.balance ? score_near : 2.f * dz, near1 = g.balance ? 1.2e-7f : rel;            // near = near0 + near1 (|a| + |b|)
+    const float near0 = balance ? score_near : 2.f * dz, near1 = balance ? 1.2e-7f : rel;                // near = near0 + near1 (|a| + |b|)
     float sum = 1.f;
     if (!odd) {
         float t[PER];
@@ -219,28 +251,54 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, const float* z, f
         }
         if (by_score) {
             const float inv = 1.f / sum;
+            float bias[PER];
+            if (balance) load_run<PER>(balance + PER * lane, bias);
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int e = lane + 32 * i;
-                if (e < g.E) {
-                    const float v = by[i] == -INFINITY ? -INFINITY : (g.sigmoid ? sigmoid(by[i]) : t[i] * inv) + bias[i];
-                    odd |= !(v < INFINITY);                                // of a bias
-                    c[e] = v;
-                    if (g.balance) by[i] = v;
-                }
+                const float v = by[i] == -INFINITY ? -INFINITY : (g.sigmoid ? sigmoid(by[i]) : t[i] * inv) + (balance ? bias[i] : 0.f);
+                odd |= !(v < INFINITY);                                    // of a bias
+                other[i] = v;
             }
+            store_run<PER>(room.c + PER * lane, other);
+            if (balance)
+#pragma unroll
+                for (int i = 0; i < PER; ++i) by[i] = other[i];
             odd = __any_sync(0xffffffffu, odd);
             __syncwarp();
         }
     }
-    int stage = odd ? GATE_ALL : GATE_EXPERTS, mine = 0;
-    unsigned again = 0, kept = decided ? todo[kTodoKept] : 0xffffffffu;
+    int stage = odd ? GATE_ALL : GATE_EXPERTS;
+    unsigned kept = decided ? room.todo[kTodoKept] : 0xffffffffu;
+    if (lane < kTodoKept) room.todo[lane] = 0;
+    __syncwarp();
+    bool marked = false;
+    auto mark = [&](int e) {
+        atomicOr(&room.todo[e >> 5], 1u << (e & 31));
+        marked = true;
+    };
     if (grouped && !decided && !odd) {
         float a, b;
-        two_largest(g, by_score ? c : z, lane, a, b);
+        if (g.log_run >= 0) {
+            a = b = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const float x = by_score ? other[i] : by[i];
+                b = fmaxf(b, fminf(a, x));
+                a = fmaxf(a, x);
+            }
+            for (int m = 1 << g.log_run >> 1; m >= 1; m >>= 1) {
+                const float oa = __shfl_xor_sync(0xffffffffu, a, m), ob = __shfl_xor_sync(0xffffffffu, b, m);
+                b = fmaxf(fmaxf(b, ob), fminf(a, oa));
+                a = fmaxf(a, oa);
+            }
+            a = __shfl_sync(0xffffffffu, a, (lane << g.log_run) & 31);
+            b = __shfl_sync(0xffffffffu, b, (lane << g.log_run) & 31);
+        } else {
+            two_largest(g, by_score ? room.c : room.z, lane, a, b);
+        }
         const float value = g.top2 && b > -INFINITY ? a + b : a;
         kept = kept_groups(g, value, lane);
-        const bool real = lane >> g.log_lanes < g.G, keep = kept >> (lane & -g.lanes) & 1u;
+        const bool real = lane < g.G, keep = kept >> lane & 1u;
         // the smallest value kept against the largest dropped; a masked group's -infinity is exact
         const float low = -warp_max(real && keep ? -value : -INFINITY), high = warp_max(real && !keep ? value : -INFINITY);
         const float near_v = by_score ? score_near : 2.f * dz, rel_v = by_score ? 2.4e-7f : rel;
@@ -248,74 +306,128 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, const float* z, f
         if (near > 0.f && high > -INFINITY && low - high <= near) {
             // the groups on the border, and of each the experts that may be its largest (two)
             const bool border = real && (keep ? value <= high + near : value >= low - near);
-            const float least = border ? (g.top2 && b > -INFINITY ? b : a) : INFINITY;
-            const float reach = near_v + 2.f * rel_v * fabsf(least);
+            const float least = g.top2 && b > -INFINITY ? b : a, from = border ? least - near_v - 2.f * rel_v * fabsf(least) : INFINITY;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int e = lane + 32 * i, at = group_lane(g, min(e, g.E - 1));
-                const float t0 = __shfl_sync(0xffffffffu, least, at), t1 = __shfl_sync(0xffffffffu, reach, at);
-                if (e < g.E && t0 < INFINITY && (by_score ? c[e] : z[e]) >= t0 - t1) again |= 1u << i;
+                const int e = PER * lane + i;
+                const float t = __shfl_sync(0xffffffffu, from, min(group_of(g, e), 31));
+                if (e < g.E && (by_score ? other[i] : by[i]) >= t) mark(e);
             }
             stage = GATE_GROUPS;
         }
     }
     if (stage == GATE_EXPERTS) {
-        uint32_t key[PER];
+        const bool exact = near0 == 0.f;
+        uint32_t key[PER], best = 0;
+        const bool lane_in = !grouped || g.log_run < 0 || (kept >> (lane >> g.log_run) & 1u);
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int e = lane + 32 * i;
-            key[i] = e < g.E && (!grouped || in_kept(g, kept, e)) ? order_key(by[i]) : 0u;
+            const int e = PER * lane + i;
+            const bool in = e < g.E && lane_in && (!grouped || g.log_run >= 0 || in_kept(g, kept, e));
+            key[i] = in ? order_key(by[i]) : 0u;
+            best = max(best, key[i]);
         }
-        float prev = 0.f;
-        int prev_e = 0;
-        const bool exact = near0 == 0.f;
-        for (int j = 0; j < g.k + (exact ? 0 : 1); ++j) {
-            uint32_t best = 0;
-            int be = 0x7fffffff;
+        uint32_t from = 0;
+        for (int j = 0; j < g.k; ++j) {                                    // equal largest values go together: the bound is only lower
+            from = __reduce_max_sync(0xffffffffu, best);
+            if (best == from) best = 0;
+            if (!from) break;
+        }
+        if (from && !exact) {
+            const float v = key_value(from);
+            from = order_key(v - near0 - 2.f * near1 * fabsf(v));
+        }
+        int n = 0, at = 0;
+        const unsigned lt = (1u << lane) - 1u;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const unsigned m = __ballot_sync(0xffffffffu, key[i] && key[i] >= from);
+            n += __popc(m);
+            at += __popc(m & lt);                                          // candidates in ascending experts
+        }
+        if (n <= 32) {
 #pragma unroll
             for (int i = 0; i < PER; ++i)
-                if (key[i] > best) {                                       // ascending experts: the first maximum wins
-                    best = key[i];
-                    be = lane + 32 * i;
+                if (key[i] && key[i] >= from) {
+                    room.value[at] = by[i];
+                    room.expert[at++] = PER * lane + i;
                 }
-            const uint32_t top = __reduce_max_sync(0xffffffffu, best);
-            if (!top) break;                                               // no other expert can be chosen
-            const int e = (int)__reduce_min_sync(0xffffffffu, best == top ? (unsigned)be : 0x7fffffffu);
+            __syncwarp();
+            const float v = lane < n ? room.value[lane] : 0.f;
+            const int e = lane < n ? room.expert[lane] : 0;
+            int before = 0;
+            bool near = false;
+            for (int j = 0; j < n; ++j) {
+                const float o = __shfl_sync(0xffffffffu, v, j);
+                before += o > v || (o == v && j < lane);
+                near |= j != lane && fabsf(o - v) <= near0 + near1 * (fabsf(o) + fabsf(v));
+            }
+            const bool chosen = lane < n && before < g.k;
             if (!exact) {
-                const float v = key_value(top);
-                const float near = near0 + near1 * (fabsf(prev) + fabsf(v));
-                if (j > 0 && v > -INFINITY && prev - v <= near) {
-                    if (lane == (prev_e & 31)) again |= 1u << (prev_e >> 5);
-                    if (lane == (e & 31)) again |= 1u << (e >> 5);
+                const float last = __shfl_sync(0xffffffffu, v, __ffs(__ballot_sync(0xffffffffu, lane < n && before == g.k - 1)) - 1);
+                if (lane < n && v > -INFINITY && (chosen ? near : v >= last - near0 - near1 * (fabsf(v) + fabsf(last)))) mark(e);
+            }
+            if (!__any_sync(0xffffffffu, marked)) {
+                float s;
+                if (choice_weight(g, room.z[e], chosen, mx, sum, s)) {
+                    if (chosen) {
+                        ids[before] = e;
+                        weights[before] = s;
+                    }
+                    return false;
+                }
+                stage = GATE_ALL;
+            }
+        } else {                                                           // many equal values: k rounds
+            float prev = 0.f;
+            int prev_e = 0, mine = 0;
+            for (int j = 0; j <= g.k; ++j) {
+                uint32_t top = 0;
+                int be = 0x7fffffff;
+#pragma unroll
+                for (int i = 0; i < PER; ++i)
+                    if (key[i] > top) {                                    // ascending experts: the first maximum wins
+                        top = key[i];
+                        be = PER * lane + i;
+                    }
+                best = __reduce_max_sync(0xffffffffu, top);
+                if (!best) break;                                          // no other expert can be chosen
+                const int e = (int)__reduce_min_sync(0xffffffffu, top == best ? (unsigned)be : 0x7fffffffu);
+                const float v = key_value(best), near = near0 + near1 * (fabsf(prev) + fabsf(v));
+                if (!exact && j > 0 && v > -INFINITY && prev - v <= near) {
+                    if (lane == 0) mark(prev_e), mark(e);
                     if (j == g.k)                                          // whatever could displace the last choice
 #pragma unroll
                         for (int i = 0; i < PER; ++i)
-                            if (key[i] && key_value(key[i]) >= prev - near) again |= 1u << i;
+                            if (key[i] && key_value(key[i]) >= prev - near) mark(PER * lane + i);
                 }
                 prev = v;
                 prev_e = e;
-            }
-            if (j == lane) mine = e;
-            if (lane == (e & 31))
+                if (j == lane) mine = e;
 #pragma unroll
                 for (int i = 0; i < PER; ++i)
-                    if (i == e >> 5) key[i] = 0;
+                    if (PER * lane + i == e) key[i] = 0;
+            }
+            if (!__any_sync(0xffffffffu, marked)) {
+                float s;
+                if (choice_weight(g, room.z[mine], lane < g.k, mx, sum, s)) {
+                    if (lane < g.k) {
+                        ids[lane] = mine;
+                        weights[lane] = s;
+                    }
+                    return false;
+                }
+                stage = GATE_ALL;
+            }
         }
     }
-    const bool some = __any_sync(0xffffffffu, again != 0);
-    if (some && !g.sigmoid && g.balance) stage = GATE_ALL;                 // a softmax with a bias: all logits enter every choice value
-    if (stage == GATE_EXPERTS && !some) {
-        if (write_choice(g, z[mine], mx, sum, mine, lane, ids, weights)) return false;
-        stage = GATE_ALL;
-    }
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const unsigned m = __ballot_sync(0xffffffffu, (stage == GATE_ALL || (again >> i & 1u)) && lane + 32 * i < g.E);
-        if (lane == 0) todo[i] = m;
-    }
+    if (!g.sigmoid && balance && stage != GATE_ALL) stage = GATE_ALL;      // a softmax with a bias: all logits enter every choice value
+    __syncwarp();
+    if (stage == GATE_ALL)
+        for (int i = lane; 32 * i < g.E; i += 32) room.todo[i] = g.E - 32 * i >= 32 ? 0xffffffffu : (1u << (g.E - 32 * i)) - 1u;
     if (lane == 0) {
-        todo[kTodoKept] = kept;
-        todo[kTodoStage] = stage;
+        room.todo[kTodoKept] = kept;
+        room.todo[kTodoStage] = stage;
     }
     __syncwarp();
     return true;
@@ -325,7 +437,10 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, const float* z, f
 __device__ __forceinline__ double marked_logit(const double* z64, const float* z, int e) { return z64 ? z64[e] : (double)z[e]; }
 // The groups kept, from the exact logits of the marked experts, for choose_fast to go on from there; v [E]: room.
 template <int PER>
-__device__ __noinline__ void choose_groups(const GateArgs& g, float* z, const float* c, const double* z64, double* v, uint32_t* todo, int lane) {
+__device__ __noinline__ void choose_groups(const GateArgs& g, ChoiceRoom<PER>& room, const double* z64, double* v, int lane) {
+    float* z = room.z;
+    const float* c = room.c;
+    uint32_t* todo = room.todo;
     const bool by_score = g.balance || g.top2;
     float mx = -INFINITY, sum = 0.f;
     if (!g.sigmoid && by_score) {                                          // as choose_fast: a common factor of all
@@ -356,14 +471,16 @@ __device__ __noinline__ void choose_groups(const GateArgs& g, float* z, const fl
 
 // The experts chosen again by one warp, from the exact logits of the marked ones.  What was not marked is far enough from everything else to be ordered by its binary32 value.
 template <int PER>
-__device__ __noinline__ void choose_again(const GateArgs& g, float* z, const float* c, const double* z64, const uint32_t* todo, int lane, int32_t* ids,
-                                          float* weights) {
+__device__ __noinline__ void choose_again(const GateArgs& g, ChoiceRoom<PER>& room, const double* z64, int lane, int32_t* ids, float* weights) {
+    float* z = room.z;
+    const float* c = room.c;
+    const uint32_t* todo = room.todo;
     const bool grouped = g.top_groups < g.G;
     const unsigned kept = todo[kTodoKept];
     unsigned long long key[PER];
     float mx = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) {
+    for (int i = 0; i < PER; ++i) {                                        // lane l: experts l, l + 32, ...
         const int e = lane + 32 * i;
         key[i] = 0;
         if (e < g.E) {
@@ -406,7 +523,16 @@ __device__ __noinline__ void choose_again(const GateArgs& g, float* z, const flo
                 if (i == e >> 5) key[i] = 0;
     }
     __syncwarp();
-    write_choice(g, z[mine], mx, sum, mine, lane, ids, weights);
+    float s;
+    const bool fits = choice_weight(g, z[mine], lane < g.k, mx, sum, s);
+    if (lane < g.k) {
+        ids[lane] = mine;
+        weights[lane] = s;
+    }
+    if (fits) return;
+    // sigmoids of which nothing is left in binary32
+    const double x = lane < g.k ? (double)z[mine] : -INFINITY, d = 1.0 / (1.0 + exp(-x)), total = warp_sum_f64(lane < g.k ? d : 0.0);
+    if (lane < g.k) weights[lane] = total > 0.0 ? (float)(d / total * (double)g.scale) : 0.f;
 }
 
 }  // namespace exmoe
