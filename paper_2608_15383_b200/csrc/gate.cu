@@ -92,7 +92,7 @@ __host__ __device__ constexpr size_t logits_room(int E) {
         return 16 * (size_t)E;
 }
 template <typename Z, int PER>
-__global__ void __launch_bounds__(kGateThreads)
+__global__ void __launch_bounds__(kGateThreads, PER <= 8 ? 4 : 2)
 gate_logits_kernel(const Z* logits, long long ld, int T, GateArgs g, int32_t* ids, float* weights) {
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;

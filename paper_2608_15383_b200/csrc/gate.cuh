@@ -141,7 +141,11 @@ __device__ __forceinline__ uint32_t order_key(float v) {                   // as
     return b >> 31 ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k); }
-__device__ __forceinline__ float warp_max(float v) { return key_value(__reduce_max_sync(0xffffffffu, order_key(v))); }
+__device__ __forceinline__ float warp_max(float v) {                        // a NaN is left out
+    float m;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(m) : "f"(v));
+    return m;
+}
 __device__ __forceinline__ float warp_sum_f32(float s) {
 #pragma unroll
     for (int m = 16; m >= 1; m >>= 1) s += __shfl_xor_sync(0xffffffffu, s, m);
@@ -318,54 +322,53 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
     }
     if (stage == GATE_EXPERTS) {
         const bool exact = near0 == 0.f;
-        uint32_t key[PER], best = 0;
         const bool lane_in = !grouped || g.log_run < 0 || (kept >> (lane >> g.log_run) & 1u);
+        if (grouped && g.log_run < 0)
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int e = PER * lane + i;
-            const bool in = e < g.E && lane_in && (!grouped || g.log_run >= 0 || in_kept(g, kept, e));
-            key[i] = in ? order_key(by[i]) : 0u;
-            best = max(best, key[i]);
-        }
-        uint32_t from = 0;
+            for (int i = 0; i < PER; ++i)
+                if (!in_kept(g, kept, min(PER * lane + i, g.E - 1))) by[i] = -INFINITY;
+        float best = -INFINITY;
+        if (lane_in)
+#pragma unroll
+            for (int i = 0; i < PER; ++i) best = fmaxf(best, by[i]);
+        float from = -INFINITY, largest = 0.f;
         for (int j = 0; j < g.k; ++j) {                                    // equal largest values go together: the bound is only lower
-            from = __reduce_max_sync(0xffffffffu, best);
-            if (best == from) best = 0;
-            if (!from) break;
+            from = warp_max(best);
+            if (j == 0) largest = from;
+            if (best == from) best = -INFINITY;
         }
-        if (from && !exact) {
-            const float v = key_value(from);
-            from = order_key(v - near0 - 2.f * near1 * fabsf(v));
-        }
+        const float near = near0 + 2.f * near1 * fmaxf(fabsf(largest), fabsf(from));
+        if (!exact) from -= near;
         int n = 0, at = 0;
         const unsigned lt = (1u << lane) - 1u;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const unsigned m = __ballot_sync(0xffffffffu, key[i] && key[i] >= from);
+            const unsigned m = __ballot_sync(0xffffffffu, lane_in && by[i] >= from);
             n += __popc(m);
             at += __popc(m & lt);                                          // candidates in ascending experts
         }
-        if (n <= 32) {
+        if (n <= 32 && from > -INFINITY) {
+            if (lane_in && at < n)
 #pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (key[i] && key[i] >= from) {
-                    room.value[at] = by[i];
-                    room.expert[at++] = PER * lane + i;
-                }
+                for (int i = 0; i < PER; ++i)
+                    if (by[i] >= from) {
+                        room.value[at] = by[i];
+                        room.expert[at++] = PER * lane + i;
+                    }
             __syncwarp();
-            const float v = lane < n ? room.value[lane] : 0.f;
+            const float v = lane < n ? room.value[lane] : -INFINITY;
             const int e = lane < n ? room.expert[lane] : 0;
-            int before = 0;
-            bool near = false;
+            int before = 0, close = 0;
+#pragma unroll 4
             for (int j = 0; j < n; ++j) {
                 const float o = __shfl_sync(0xffffffffu, v, j);
                 before += o > v || (o == v && j < lane);
-                near |= j != lane && fabsf(o - v) <= near0 + near1 * (fabsf(o) + fabsf(v));
+                close += fabsf(o - v) <= near;                             // itself among them
             }
             const bool chosen = lane < n && before < g.k;
             if (!exact) {
                 const float last = __shfl_sync(0xffffffffu, v, __ffs(__ballot_sync(0xffffffffu, lane < n && before == g.k - 1)) - 1);
-                if (lane < n && v > -INFINITY && (chosen ? near : v >= last - near0 - near1 * (fabsf(v) + fabsf(last)))) mark(e);
+                if (lane < n && (chosen ? close > 1 : v >= last - near)) mark(e);
             }
             if (!__any_sync(0xffffffffu, marked)) {
                 float s;
@@ -378,7 +381,13 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
                 }
                 stage = GATE_ALL;
             }
-        } else {                                                           // many equal values: k rounds
+        } else {                                                           // many equal values, or few logits that are not -infinity: k rounds
+            uint32_t key[PER];
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int e = PER * lane + i;
+                key[i] = e < g.E && (!grouped || in_kept(g, kept, e)) ? order_key(by[i]) : 0u;
+            }
             float prev = 0.f;
             int prev_e = 0, mine = 0;
             for (int j = 0; j <= g.k; ++j) {
@@ -390,10 +399,10 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
                         top = key[i];
                         be = PER * lane + i;
                     }
-                best = __reduce_max_sync(0xffffffffu, top);
-                if (!best) break;                                          // no other expert can be chosen
-                const int e = (int)__reduce_min_sync(0xffffffffu, top == best ? (unsigned)be : 0x7fffffffu);
-                const float v = key_value(best), near = near0 + near1 * (fabsf(prev) + fabsf(v));
+                const uint32_t most = __reduce_max_sync(0xffffffffu, top);
+                if (!most) break;                                          // no other expert can be chosen
+                const int e = (int)__reduce_min_sync(0xffffffffu, top == most ? (unsigned)be : 0x7fffffffu);
+                const float v = key_value(most);
                 if (!exact && j > 0 && v > -INFINITY && prev - v <= near) {
                     if (lane == 0) mark(prev_e), mark(e);
                     if (j == g.k)                                          // whatever could displace the last choice
