@@ -63,7 +63,7 @@ __device__ __noinline__ double logit_f64(const uint4* x, const uint4* w, int chu
 // One CTA per token, everything in binary64: products of BF16 values are exact in binary32.
 __global__ void __launch_bounds__(kGateThreads)
 gate_token_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w_router, const float* __restrict__ bias,
-                  const float* addend, int H, GateArgs g, int32_t* ids, float* weights) {
+                  const float* addend, int H, const __grid_constant__ GateArgs g, int32_t* ids, float* weights) {
     extern __shared__ __align__(16) unsigned char smem[];
     double* z = reinterpret_cast<double*>(smem);
     unsigned long long* key = reinterpret_cast<unsigned long long*>(z + g.E);
@@ -93,7 +93,7 @@ __host__ __device__ constexpr size_t logits_room(int E) {
 }
 template <typename Z, int PER>
 __global__ void __launch_bounds__(kGateThreads, PER <= 8 ? 4 : 2)
-gate_logits_kernel(const Z* logits, long long ld, int T, GateArgs g, int32_t* ids, float* weights) {
+gate_logits_kernel(const Z* logits, long long ld, int T, const __grid_constant__ GateArgs g, int32_t* ids, float* weights) {
     extern __shared__ __align__(16) unsigned char smem[];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     unsigned char* mine = smem + warp * logits_room<PER>(g.E);
@@ -155,7 +155,7 @@ constexpr int kFewCluster = 8, kFewFour = 48;                              // fo
 template <int TB, int PER>
 __global__ void __launch_bounds__(kGateThreads)
 gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w_router, const float* __restrict__ bias, const float* addend, int T, int H,
-                GateArgs g, int32_t* ids, float* weights) {
+                const __grid_constant__ GateArgs g, int32_t* ids, float* weights) {
     static_assert(TB <= kFewCluster, "a CTA owns at most one token");
     extern __shared__ __align__(16) unsigned char smem[];
     FewRoom<PER>& sm = *reinterpret_cast<FewRoom<PER>*>(smem);

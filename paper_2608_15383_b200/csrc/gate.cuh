@@ -155,6 +155,7 @@ __device__ __forceinline__ float sigmoid(float z) {
     const float e = expf(-fabsf(z));
     return (z >= 0.f ? 1.f : e) / (1.f + e);
 }
+__device__ __forceinline__ float quick_sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
 // exp(z - top): the rounding of the difference, 2^-24 of it, is put back
 __device__ __forceinline__ float exp_below(float z, float top) {
     const float d = z - top, back = d + top;
@@ -187,8 +188,7 @@ template <int PER>
 struct __align__(16) ChoiceRoom {
     float z[32 * PER];                                                     // logits, -infinity behind the last
     float c[32 * PER];                                                     // choice values
-    float value[32];                                                       // candidates
-    int expert[32];
+    int expert[32];                                                        // candidates
     uint32_t todo[kTodoWords];
 };
 template <int PER>
@@ -236,9 +236,10 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
     // rel: |z| s (1 - s) < 0.23 for a sigmoid; in a softmax logits 100 below the largest have no part
     const float dzs = dz + (g.sigmoid ? rel : rel * (fabsf(mx) + 100.f));
     odd = __any_sync(0xffffffffu, odd) || mx == -INFINITY || !(dzs <= 0.05f);
-    // a sigmoid is within 5 x 2^-24 of the true one, a probability (an argument off by 2^-24 of itself, p |argument| < 0.37; up to 25
-    // roundings in exponentials, sum and quotient) within 2e-6; c itself rounds once more
-    const float score_near = (g.sigmoid ? 2.f * 0.26f : 2.f * 0.55f) * dzs + (g.sigmoid ? 6e-7f : 4e-6f);
+    // quick_sigmoid is within 3.5e-7 of the true one (__expf's argument off by 2^-23 |z|, its result by 2^-22 of itself, each times s (1 - s); the quotient
+    // by 2^-22 s), a probability (an argument off by 2^-24 of itself, p |argument| < 0.37; up to 25 roundings in exponentials, sum and
+    // quotient) within 2e-6; c itself rounds once more
+    const float score_near = (g.sigmoid ? 2.f * 0.26f : 2.f * 0.55f) * dzs + (g.sigmoid ? 7e-7f : 4e-6f);
     const float near0 = balance ? score_near : 2.f * dz, near1 = balance ? 1.2e-7f : rel;                // near = near0 + near1 (|a| + |b|)
     float sum = 1.f;
     if (!odd) {
@@ -259,7 +260,7 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
             if (balance) load_run<PER>(balance + PER * lane, bias);
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const float v = by[i] == -INFINITY ? -INFINITY : (g.sigmoid ? sigmoid(by[i]) : t[i] * inv) + (balance ? bias[i] : 0.f);
+                const float v = by[i] == -INFINITY ? -INFINITY : (g.sigmoid ? quick_sigmoid(by[i]) : t[i] * inv) + (balance ? bias[i] : 0.f);
                 odd |= !(v < INFINITY);                                    // of a bias
                 other[i] = v;
             }
@@ -339,25 +340,25 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
         }
         const float near = near0 + 2.f * near1 * fmaxf(fabsf(largest), fabsf(from));
         if (!exact) from -= near;
-        int n = 0, at = 0;
+        int mine = 0, n = 0, at = 0;                                       // candidates of this lane, of all, before this lane's
         const unsigned lt = (1u << lane) - 1u;
+        if (lane_in)
 #pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const unsigned m = __ballot_sync(0xffffffffu, lane_in && by[i] >= from);
+            for (int i = 0; i < PER; ++i) mine += by[i] >= from;
+        for (int c = 1;; ++c) {
+            const unsigned m = __ballot_sync(0xffffffffu, mine >= c);
+            if (!m) break;
             n += __popc(m);
-            at += __popc(m & lt);                                          // candidates in ascending experts
+            at += __popc(m & lt);
         }
         if (n <= 32 && from > -INFINITY) {
-            if (lane_in && at < n)
+            if (mine)
 #pragma unroll
                 for (int i = 0; i < PER; ++i)
-                    if (by[i] >= from) {
-                        room.value[at] = by[i];
-                        room.expert[at++] = PER * lane + i;
-                    }
+                    if (by[i] >= from) room.expert[at++] = PER * lane + i; // in ascending experts
             __syncwarp();
-            const float v = lane < n ? room.value[lane] : -INFINITY;
             const int e = lane < n ? room.expert[lane] : 0;
+            const float v = lane < n ? (balance ? room.c : room.z)[e] : -INFINITY;
             int before = 0, close = 0;
 #pragma unroll 4
             for (int j = 0; j < n; ++j) {
