@@ -238,6 +238,11 @@ enum { EXMOE_F32 = 0, EXMOE_BF16 = 1 };
 int exmoe_gate_logits(const exmoe_shape* shape, const exmoe_gate* gate, const void* logits, int type, int64_t row_stride,
                       const float* balance, int T, int32_t* topk_ids, float* topk_weights, void* stream);
 
+/* Sticky device-side status of exmoe_route_gated on the current device: synchronises it, returns EXMOE_OK, or EXMOE_ERR_TIMEOUT if a
+ * bounded wait of the tensor-core form expired since the previous call of this function (the tokens of its cluster were then left
+ * unwritten), and clears it. */
+int exmoe_gate_status(void);
+
 /* Low-rank adapters of many requests beside a projection that all of them share (the paper has none; packed int4 weights cannot
  * take an adapter in, and the requests of a batch bring different ones).  For token t with adapter a:
  *   out_t = base_t + scale_a * B_a (A_a x_t)

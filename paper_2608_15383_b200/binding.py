@@ -71,6 +71,7 @@ _SIGNATURES = {
     "exmoe_route": (c_int, [POINTER(exmoe_shape), c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_void_p]),
     "exmoe_route_gated": (c_int, [POINTER(exmoe_shape), POINTER(exmoe_gate)] + [c_void_p] * 5 + [c_int] + [c_void_p] * 3),
     "exmoe_gate_logits": (c_int, [POINTER(exmoe_shape), POINTER(exmoe_gate), c_void_p, c_int, c_int64, c_void_p, c_int] + [c_void_p] * 3),
+    "exmoe_gate_status": (c_int, []),
     "exmoe_lora_plan_bytes": (c_int, [c_int, c_int, POINTER(c_size_t)]),
     "exmoe_lora_plan": (c_int, [c_void_p, c_int, c_int, c_void_p, c_void_p]),
     "exmoe_lora_plan_status": (c_int, [c_void_p]),
@@ -232,6 +233,11 @@ def exmoe_route_gated(shape, gate, hidden, w_router, bias=None, addend=None, bal
     if r.__class__ is int:
         raise ExmoeError(r, "exmoe_route_gated")
     return r
+
+
+def exmoe_gate_status():
+    """EXMOE_OK, or EXMOE_ERR_TIMEOUT if a bounded wait of exmoe_route_gated expired since the last call (synchronises, clears)."""
+    return int(lib().exmoe_gate_status())
 
 
 def exmoe_gate_logits(shape, gate, logits, balance=None, topk_ids=None, topk_weights=None, stream=None):

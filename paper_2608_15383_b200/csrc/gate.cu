@@ -13,52 +13,6 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kGateThreads = 256, kGateWarps = kGateThreads / 32;
-constexpr int kGateSmemMax = 200 * 1024;
-
-__device__ __forceinline__ void unpack8(const uint4& a, float (&x)[8]) {
-    const uint32_t r[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(r[i] << 16);
-        x[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
-    }
-}
-__device__ __forceinline__ float dot8(const float (&w)[8], const float (&x)[8]) {
-    float d = 0.f;
-#pragma unroll
-    for (int n = 0; n < 8; ++n) d = fmaf(w[n], x[n], d);
-    return d;
-}
-__device__ __forceinline__ float square8(const uint4& a) {
-    float x[8];
-    unpack8(a, x);
-    return dot8(x, x);
-}
-// A logit by one warp in binary64; products of BF16 values are exact in binary32.
-__device__ __noinline__ double logit_f64(const uint4* x, const uint4* w, int chunks, int lane) {
-    double s = 0.0;
-    for (int i0 = 0; i0 < chunks; i0 += 128) {
-        uint4 wv[4], xv[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int i = i0 + 32 * j + lane;
-            wv[j] = xv[j] = make_uint4(0, 0, 0, 0);
-            if (i < chunks) {
-                wv[j] = w[i];
-                xv[j] = x[i];
-            }
-        }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            float wf[8], xf[8];
-            unpack8(wv[j], wf);
-            unpack8(xv[j], xf);
-#pragma unroll
-            for (int n = 0; n < 8; ++n) s += (double)(wf[n] * xf[n]);
-        }
-    }
-    return warp_sum_f64(s);
-}
 
 // One CTA per token, everything in binary64: products of BF16 values are exact in binary32.
 __global__ void __launch_bounds__(kGateThreads)
@@ -136,7 +90,6 @@ gate_logits_kernel(const Z* logits, long long ld, int T, const __grid_constant__
     choose_exact(g, z64, reinterpret_cast<unsigned long long*>(key), lane, ids + t * g.k, weights + t * g.k);
 }
 
-constexpr float kAddedRel = 3.f * 0x1p-24f;                                // bias and addend: 2^-24 (|sum before| + |z|), with |sum before| <= 2 |z| + 16
 
 // ---- few tokens: a cluster of eight CTAs shares the experts of TB tokens -----------------------------------------------
 // As many warps as a 64-expert router has rows, so that a row's 4 KB are in flight at once.  Logits in binary32: chains of 8 products,
@@ -308,34 +261,7 @@ int check_gate(const exmoe_shape* shape, const exmoe_gate* gate, int T, GateArgs
     return EXMOE_OK;
 }
 
-// every form is a programmatic dependent of the kernel before it in the stream (it waits for it before it reads anything)
-template <typename... P, typename... A>
-int launch(void (*kern)(P...), unsigned ctas, int threads, int cluster, size_t smem, SmemOnce& once, cudaStream_t st, A... args) {
-    if (!allow_smem(kern, kGateSmemMax, once)) return EXMOE_ERR_CUDA;
-    cudaLaunchConfig_t lc{};
-    lc.gridDim = dim3(ctas);
-    lc.blockDim = dim3((unsigned)threads);
-    lc.dynamicSmemBytes = smem;
-    lc.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)cluster;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
-    lc.attrs = attr;
-    lc.numAttrs = cluster > 1 ? 2 : 1;
-#ifdef EXMOE_DISABLE_PDL
-    lc.attrs = attr + 1;
-    --lc.numAttrs;
-#endif
-    if (cudaLaunchKernelEx(&lc, kern, args...) != cudaSuccess) {
-        cudaGetLastError();
-        return EXMOE_ERR_CUDA;
-    }
-    count_launch();
-    return EXMOE_OK;
-}
+constexpr int kManyTokens = 64, kManyExperts = 256;                        // tensor cores from here on, up to there
 
 // A call's kernels by the number of experts: what choose_fast holds per lane.
 template <int TB, int PER>
@@ -385,6 +311,7 @@ extern "C" int exmoe_route_gated(const exmoe_shape* shape, const exmoe_gate* gat
     g.balance = balance;
     const __nv_bfloat16 *x = (const __nv_bfloat16*)hidden_bf16, *w = (const __nv_bfloat16*)router_bf16;
     cudaStream_t st = (cudaStream_t)stream;
+    if (g.E <= kManyExperts && g.k <= kFastChoices && T >= kManyTokens && H >= 64) return launch_gate_tc(x, w, bias, addend, T, H, g, topk_ids, topk_weights, st);
     if (g.E <= kFastExperts && g.k <= kFastChoices && sizeof(FewRoom<16>) + 8 * (size_t)H <= (size_t)kGateSmemMax)
         return T < kFewFour ? launch_few<1>(x, w, bias, addend, T, H, g, topk_ids, topk_weights, st) : launch_few<4>(x, w, bias, addend, T, H, g, topk_ids, topk_weights, st);
     static SmemOnce once;

@@ -1,6 +1,9 @@
 // The choice of a gate (exmoe_gate) from a token's logits, shared by the kernels that end in it.
 #pragma once
+#include <algorithm>
+
 #include "common.cuh"
+#include "frag.cuh"
 
 namespace exmoe {
 
@@ -66,7 +69,7 @@ __device__ __forceinline__ void two_largest(const GateArgs& g, const T* v, int l
 }
 
 // The whole choice in binary64, by one warp.  z: the token's logits, key: room for as many integers (both in shared memory).
-__device__ __noinline__ void choose_exact(const GateArgs& g, const double* z, unsigned long long* key, int lane, int32_t* ids, float* weights) {
+static __device__ __noinline__ void choose_exact(const GateArgs& g, const double* z, unsigned long long* key, int lane, int32_t* ids, float* weights) {
     const double kMasked = -INFINITY;
     double* c = reinterpret_cast<double*>(key);
     const bool grouped = g.top_groups < g.G;
@@ -338,8 +341,18 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
             if (j == 0) largest = from;
             if (best == from) best = -INFINITY;
         }
-        const float near = near0 + 2.f * near1 * fmaxf(fabsf(largest), fabsf(from));
-        if (!exact) from -= near;
+        const bool few = from == -INFINITY;                                // lanes with experts that can be chosen: all of these are candidates
+        if (few && largest > -INFINITY) {
+            float least = INFINITY;
+            if (lane_in)
+#pragma unroll
+                for (int i = 0; i < PER; ++i)
+                    if (by[i] > -INFINITY) least = fminf(least, by[i]);
+            from = -warp_max(-least);
+        }
+        // the same for all pairs of candidates: these lie between the two
+        const float near = near0 + (from > -INFINITY ? 2.f * near1 * fmaxf(fabsf(largest), fabsf(from)) : 0.f);
+        if (!exact && !few) from -= near;
         int mine = 0, n = 0, at = 0;                                       // candidates of this lane, of all, before this lane's
         const unsigned lt = (1u << lane) - 1u;
         if (lane_in)
@@ -351,7 +364,7 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
             n += __popc(m);
             at += __popc(m & lt);
         }
-        if (n <= 32 && from > -INFINITY) {
+        if (n >= g.k && n <= 32 && from > -INFINITY) {
             if (mine)
 #pragma unroll
                 for (int i = 0; i < PER; ++i)
@@ -404,12 +417,12 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
                 if (!most) break;                                          // no other expert can be chosen
                 const int e = (int)__reduce_min_sync(0xffffffffu, top == most ? (unsigned)be : 0x7fffffffu);
                 const float v = key_value(most);
-                if (!exact && j > 0 && v > -INFINITY && prev - v <= near) {
+                if (!exact && j > 0 && v > -INFINITY && prev - v <= near0 + near1 * (fabsf(prev) + fabsf(v))) {
                     if (lane == 0) mark(prev_e), mark(e);
-                    if (j == g.k)                                          // whatever could displace the last choice
+                    if (j == g.k)                                          // whatever could displace the last choice, and a little more
 #pragma unroll
                         for (int i = 0; i < PER; ++i)
-                            if (key[i] && key_value(key[i]) >= prev - near) mark(PER * lane + i);
+                            if (key[i] && key_value(key[i]) >= v - near0 - 2.f * near1 * fabsf(v)) mark(PER * lane + i);
                 }
                 prev = v;
                 prev_e = e;
@@ -544,5 +557,87 @@ __device__ __noinline__ void choose_again(const GateArgs& g, ChoiceRoom<PER>& ro
     const double x = lane < g.k ? (double)z[mine] : -INFINITY, d = 1.0 / (1.0 + exp(-x)), total = warp_sum_f64(lane < g.k ? d : 0.0);
     if (lane < g.k) weights[lane] = total > 0.0 ? (float)(d / total * (double)g.scale) : 0.f;
 }
+
+// ---- what the kernels share --------------------------------------------------------------------------------------------
+constexpr int kGateSmemMax = 200 * 1024, kSms = 148;
+constexpr float kAddedRel = 3.f * 0x1p-24f;                                // bias and addend: 2^-24 (|sum before| + |z|), with |sum before| <= 2 |z| + 16
+
+__device__ __forceinline__ void unpack8(const uint4& a, float (&x)[8]) {
+    const uint32_t r[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(r[i] << 16);
+        x[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ float dot8(const float (&w)[8], const float (&x)[8]) {
+    float d = 0.f;
+#pragma unroll
+    for (int n = 0; n < 8; ++n) d = fmaf(w[n], x[n], d);
+    return d;
+}
+__device__ __forceinline__ float square8(const uint4& a) {
+    float x[8];
+    unpack8(a, x);
+    return dot8(x, x);
+}
+// A logit by one warp in binary64; products of BF16 values are exact in binary32.
+static __device__ __noinline__ double logit_f64(const uint4* x, const uint4* w, int chunks, int lane) {
+    double s = 0.0;
+    for (int i0 = 0; i0 < chunks; i0 += 128) {
+        uint4 wv[4], xv[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = i0 + 32 * j + lane;
+            wv[j] = xv[j] = make_uint4(0, 0, 0, 0);
+            if (i < chunks) {
+                wv[j] = w[i];
+                xv[j] = x[i];
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float wf[8], xf[8];
+            unpack8(wv[j], wf);
+            unpack8(xv[j], xf);
+#pragma unroll
+            for (int n = 0; n < 8; ++n) s += (double)(wf[n] * xf[n]);
+        }
+    }
+    return warp_sum_f64(s);
+}
+
+// every form is a programmatic dependent of the kernel before it in the stream (it waits for it before it reads anything)
+template <typename... P, typename... A>
+int launch(void (*kern)(P...), unsigned ctas, int threads, int cluster, size_t smem, SmemOnce& once, cudaStream_t st, const A&... args) {
+    if (!allow_smem(kern, std::max(kGateSmemMax, (int)smem), once)) return EXMOE_ERR_CUDA;
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = dim3(ctas);
+    lc.blockDim = dim3((unsigned)threads);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    lc.attrs = attr;
+    lc.numAttrs = cluster > 1 ? 2 : 1;
+#ifdef EXMOE_DISABLE_PDL
+    lc.attrs = attr + 1;
+    --lc.numAttrs;
+#endif
+    if (cudaLaunchKernelEx(&lc, kern, args...) != cudaSuccess) {
+        cudaGetLastError();
+        return EXMOE_ERR_CUDA;
+    }
+    count_launch();
+    return EXMOE_OK;
+}
+
+// Many tokens, at most 256 experts: the logits on tensor cores (gate_tc.cu).
+int launch_gate_tc(const __nv_bfloat16* x, const __nv_bfloat16* w, const float* bias, const float* addend, int T, int H, const GateArgs& g, int32_t* ids,
+                   float* weights, cudaStream_t st);
 
 }  // namespace exmoe

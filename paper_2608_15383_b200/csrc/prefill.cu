@@ -844,7 +844,7 @@ size_t prefill_scratch_bytes(int max_pairs, int num_experts) {
 static_assert(sizeof(CUtensorMap) == 128, "PrefillMaps mirrors CUtensorMap objects");
 
 // 2-D row-major BF16 matrix [rows, cols] -> tensor map with a 64-column x `box_rows`-row box, 128-byte swizzle
-static int encode_map(CUtensorMap* out, const void* base, int rows, int cols, int box_rows) {
+int encode_map(CUtensorMap* out, const void* base, int rows, int cols, int box_rows) {
     typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
