@@ -372,17 +372,22 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
             __syncwarp();
             const int e = lane < n ? room.expert[lane] : 0;
             const float v = lane < n ? (balance ? room.c : room.z)[e] : -INFINITY;
+            float close_by = near;
+            if (balance && g.sigmoid) {                                    // the candidates' own slopes: they lie where a sigmoid is flat
+                const float e1 = lane < n ? quick_sigmoid(room.z[e]) : 0.f;
+                close_by = near - near0 + 2.f * 1.06f * dzs * warp_max(e1 * (1.f - e1) + 4e-7f) + 7e-7f;
+            }
             int before = 0, close = 0;
 #pragma unroll 4
             for (int j = 0; j < n; ++j) {
                 const float o = __shfl_sync(0xffffffffu, v, j);
                 before += o > v || (o == v && j < lane);
-                close += fabsf(o - v) <= near;                             // itself among them
+                close += fabsf(o - v) <= close_by;                         // itself among them
             }
             const bool chosen = lane < n && before < g.k;
             if (!exact) {
                 const float last = __shfl_sync(0xffffffffu, v, __ffs(__ballot_sync(0xffffffffu, lane < n && before == g.k - 1)) - 1);
-                if (lane < n && (chosen ? close > 1 : v >= last - near)) mark(e);
+                if (lane < n && (chosen ? close > 1 : v >= last - close_by)) mark(e);
             }
             if (!__any_sync(0xffffffffu, marked)) {
                 float s;
@@ -583,11 +588,12 @@ __device__ __forceinline__ float square8(const uint4& a) {
 }
 // A logit by one warp in binary64; products of BF16 values are exact in binary32.
 static __device__ __noinline__ double logit_f64(const uint4* x, const uint4* w, int chunks, int lane) {
-    double s = 0.0;
-    for (int i0 = 0; i0 < chunks; i0 += 128) {
-        uint4 wv[4], xv[4];
+    constexpr int U = 8;                                                   // chunks in flight, sums side by side
+    double s[U] = {};
+    for (int i0 = 0; i0 < chunks; i0 += 32 * U) {
+        uint4 wv[U], xv[U];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < U; ++j) {
             const int i = i0 + 32 * j + lane;
             wv[j] = xv[j] = make_uint4(0, 0, 0, 0);
             if (i < chunks) {
@@ -596,15 +602,14 @@ static __device__ __noinline__ double logit_f64(const uint4* x, const uint4* w, 
             }
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            float wf[8], xf[8];
-            unpack8(wv[j], wf);
-            unpack8(xv[j], xf);
+        for (int n = 0; n < 8; ++n)
 #pragma unroll
-            for (int n = 0; n < 8; ++n) s += (double)(wf[n] * xf[n]);
-        }
+            for (int j = 0; j < U; ++j) {
+                const uint32_t a = n < 2 ? wv[j].x : n < 4 ? wv[j].y : n < 6 ? wv[j].z : wv[j].w, b = n < 2 ? xv[j].x : n < 4 ? xv[j].y : n < 6 ? xv[j].z : xv[j].w;
+                s[j] += (double)(n & 1 ? __uint_as_float(a & 0xffff0000u) * __uint_as_float(b & 0xffff0000u) : __uint_as_float(a << 16) * __uint_as_float(b << 16));
+            }
     }
-    return warp_sum_f64(s);
+    return warp_sum_f64(((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])));
 }
 
 // every form is a programmatic dependent of the kernel before it in the stream (it waits for it before it reads anything)

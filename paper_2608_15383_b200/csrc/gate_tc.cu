@@ -81,6 +81,19 @@ __device__ __forceinline__ void square(__nv_bfloat162& sum, const uint4& v) {
     }
 }
 
+// the choosing warps' barrier
+__device__ __forceinline__ void choosers_sync() {
+    __syncwarp();
+    asm volatile("barrier.cta.sync.aligned 1, %0;" ::"n"(32 * kDrainWarps) : "memory");
+}
+__device__ __forceinline__ bool choosers_or(bool v) {
+    uint32_t r;
+    __syncwarp();
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred.aligned q, 1, %2, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                 : "=r"(r) : "r"((uint32_t)v), "n"(32 * kDrainWarps) : "memory");
+    return r != 0;
+}
+
 template <int MT, int PER>
 struct Warp {                                                              // a choosing warp's share of shared memory
     ChoiceRoom<PER> room;
@@ -98,6 +111,7 @@ struct __align__(1024) Shared {
     };
     float x2[kTokens], w2[MT * 128], balance[32 * PER];
     float w2_max[kDrainWarps];
+    int items, item[kDrainWarps * 32 * PER];                               // logits to compute again: warp << 16 | expert
     uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2];
     uint32_t tmem;
     int abort_flag;
@@ -254,49 +268,64 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         for (int i = 0; i < kDrainWarps; ++i) w2 = fmaxf(w2, sm.w2_max[i]);
         const float* balance = g.balance ? sm.balance : nullptr;
         const int owned = kTokens / CL, chunks = H / 8;
-        for (int i = d; i < owned; i += kDrainWarps) {
+        for (int i = d; i - d < owned; i += kDrainWarps) {                 // the warps together, so that they share what is computed again
             const int tok = rank * owned + i;
             const long long t = t0 + tok;
-            if (t >= T) break;
-            float v[PER], x2 = 0.f;
+            const bool live = i < owned && t < T;
+            if (tid == 128) sm.items = 0;
+            float dz = 0.f;
+            if (live) {
+                float v[PER], x2 = 0.f;
 #pragma unroll
-            for (int j = 0; j < PER; ++j) v[j] = 0.f;
-            for (int r = 0; r < CL; ++r) {
-                add_run<PER>(smem_u32(&sm.s.part[tok][PER * lane]), r, v);
-                x2 += ld_rank(smem_u32(&sm.x2[tok]), r);
-            }
-            bool cancelled = false;
-#pragma unroll
-            for (int j = 0; j < PER; ++j) {
-                const int e = PER * lane + j;
-                if (e < g.E) {
-                    if (bias) v[j] += bias[e];
-                    if (addend) {
-                        const float before = fabsf(v[j]);
-                        v[j] += addend[t * g.E + e];
-                        cancelled |= before > 2.f * fabsf(v[j]) + 16.f;
-                    }
-                } else {
-                    v[j] = -INFINITY;
+                for (int j = 0; j < PER; ++j) v[j] = 0.f;
+                for (int r = 0; r < CL; ++r) {
+                    add_run<PER>(smem_u32(&sm.s.part[tok][PER * lane]), r, v);
+                    x2 += ld_rank(smem_u32(&sm.x2[tok]), r);
                 }
+                bool cancelled = false;
+#pragma unroll
+                for (int j = 0; j < PER; ++j) {
+                    const int e = PER * lane + j;
+                    if (e < g.E) {
+                        if (bias) v[j] += bias[e];
+                        if (addend) {
+                            const float before = fabsf(v[j]);
+                            v[j] += addend[t * g.E + e];
+                            cancelled |= before > 2.f * fabsf(v[j]) + 16.f;
+                        }
+                    } else {
+                        v[j] = -INFINITY;
+                    }
+                }
+                store_run<PER>(room.z + PER * lane, v);
+                __syncwarp();
+                // the tensor cores' 2 x 21, an addition per stage, one per CTA; the norms are short by less than 2 %
+                dz = 1.02f * (float)(42 + (blocks + CL - 1) / CL + CL) * 0x1p-24f * sqrtf(x2) * sqrtf(w2) + (addend ? 16.f * 0x1p-24f : 0.f);
+                if (__any_sync(0xffffffffu, cancelled)) dz = INFINITY;
             }
-            store_run<PER>(room.z + PER * lane, v);
-            __syncwarp();
-            // the tensor cores' 2 x 21, an addition per stage, one per CTA; the norms are short by less than 2 %
-            float dz = 1.02f * (float)(42 + (blocks + CL - 1) / CL + CL) * 0x1p-24f * sqrtf(x2) * sqrtf(w2) + (addend ? 16.f * 0x1p-24f : 0.f);
-            if (__any_sync(0xffffffffu, cancelled)) dz = INFINITY;
             int32_t* ids_t = ids + t * g.k;
             float* weights_t = weights + t * g.k;
+            bool open = live;                                              // not chosen yet
             for (bool decided = false;; decided = true) {
-                if (!choose_fast<PER>(g, room, balance, dz, bias || addend ? kAddedRel : 0.f, lane, decided, ids_t, weights_t)) break;
+                open = open && choose_fast<PER>(g, room, balance, dz, bias || addend ? kAddedRel : 0.f, lane, decided, ids_t, weights_t);
+                if (!choosers_or(open)) break;
+                if (open) {
+                    unsigned es = 32 * lane < g.E ? room.todo[lane] : 0u;  // a word per lane
+                    int at = 0;
+                    if (es) at = atomicAdd(&sm.items, __popc(es));
+                    for (; es; es &= es - 1) sm.item[at++] = d << 16 | (32 * lane + __ffs(es) - 1);
+                }
+                choosers_sync();
+                for (int j = d; j < sm.items; j += kDrainWarps) {
+                    const int who = sm.item[j] >> 16, e = sm.item[j] & 0xffff;
+                    const long long u = t - d + who;                       // that warp's token
+                    const double z = logit_f64(reinterpret_cast<const uint4*>(hidden + u * H), reinterpret_cast<const uint4*>(w_router + (size_t)e * H), chunks, lane);
+                    if (lane == 0) sm.s.warp[who].z64[e] = z + (bias ? (double)bias[e] : 0.0) + (addend ? (double)addend[u * g.E + e] : 0.0);
+                }
+                choosers_sync();
+                if (tid == 128) sm.items = 0;
+                if (!open) continue;
                 const uint32_t stage = room.todo[kTodoStage];
-                for (int b = 0; 32 * b < g.E; ++b)
-                    for (unsigned es = room.todo[b]; es; es &= es - 1) {
-                        const int e = 32 * b + __ffs(es) - 1;
-                        const double z = logit_f64(reinterpret_cast<const uint4*>(hidden + t * H), reinterpret_cast<const uint4*>(w_router + (size_t)e * H), chunks, lane);
-                        if (lane == 0) my.z64[e] = z + (bias ? (double)bias[e] : 0.0) + (addend ? (double)addend[t * g.E + e] : 0.0);
-                    }
-                __syncwarp();
                 if (stage == GATE_GROUPS) {
                     choose_groups<PER>(g, room, my.z64, my.z64, lane);
                     continue;
@@ -305,7 +334,7 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                     choose_again<PER>(g, room, my.z64, lane, ids_t, weights_t);
                 else
                     choose_exact(g, my.z64, reinterpret_cast<unsigned long long*>(room.z), lane, ids_t, weights_t);       // z and c
-                break;
+                open = false;
             }
             __syncwarp();
         }
