@@ -38,6 +38,7 @@ __device__ __forceinline__ double warp_sum_f64(double s) {
 template <typename T>
 __device__ __forceinline__ unsigned kept_groups(const GateArgs& g, T value, int lane) {
     int before = 0;
+#pragma unroll 4
     for (int o = 0; o < g.G; ++o) {
         const T v = __shfl_sync(0xffffffffu, value, o);
         before += v > value || (v == value && o < lane);
@@ -228,52 +229,61 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
     const bool grouped = g.top_groups < g.G, by_score = balance || (grouped && g.top2);
     float by[PER], other[PER];                                             // what orders the experts; scores where these are not it
     load_run<PER>(room.z + PER * lane, by);
-    float mx = by[0];
-    bool odd = false;
+    float mx = -INFINITY, any = 0.f;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
-        odd |= !(by[i] < INFINITY);                                        // a NaN or +infinity
         mx = fmaxf(mx, by[i]);
+        any += by[i];                                                      // a NaN where there is one, or infinities of both signs
     }
-    mx = warp_max(mx == mx ? mx : -INFINITY);
+    mx = warp_max(mx);
     // rel: |z| s (1 - s) < 0.23 for a sigmoid; in a softmax logits 100 below the largest have no part
     const float dzs = dz + (g.sigmoid ? rel : rel * (fabsf(mx) + 100.f));
-    odd = __any_sync(0xffffffffu, odd) || mx == -INFINITY || !(dzs <= 0.05f);
+    bool odd = __any_sync(0xffffffffu, any != any) || !(fabsf(mx) < INFINITY) || !(dzs <= 0.05f);
     // quick_sigmoid is within 3.5e-7 of the true one (__expf's argument off by 2^-23 |z|, its result by 2^-22 of itself, each times s (1 - s); the quotient
     // by 2^-22 s), a probability (an argument off by 2^-24 of itself, p |argument| < 0.37; up to 25 roundings in exponentials, sum and
     // quotient) within 2e-6; c itself rounds once more
     const float score_near = (g.sigmoid ? 2.f * 0.26f : 2.f * 0.55f) * dzs + (g.sigmoid ? 7e-7f : 4e-6f);
     const float near0 = balance ? score_near : 2.f * dz, near1 = balance ? 1.2e-7f : rel;                // near = near0 + near1 (|a| + |b|)
     float sum = 1.f;
-    if (!odd) {
-        float t[PER];
-        if (!g.sigmoid && (by_score || !g.renorm)) {
-            float part[PER];
+    // branches around loops that all lanes take alike, not choices per expert: both sides of these would be computed
+    if (!odd && !g.sigmoid && (by_score || !g.renorm)) {
+        float part[PER];
 #pragma unroll
-            for (int i = 0; i < PER; ++i) part[i] = t[i] = expf(by[i] - mx);
+        for (int i = 0; i < PER; ++i) part[i] = other[i] = expf(by[i] - mx);
 #pragma unroll
-            for (int n = PER / 2; n >= 1; n /= 2)
+        for (int n = PER / 2; n >= 1; n /= 2)
 #pragma unroll
-                for (int i = 0; i < n; ++i) part[i] += part[i + n];
-            sum = warp_sum_f32(part[0]);
-        }
-        if (by_score) {
+            for (int i = 0; i < n; ++i) part[i] += part[i + n];
+        sum = warp_sum_f32(part[0]);
+    }
+    if (!odd && by_score) {
+        if (g.sigmoid) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) other[i] = quick_sigmoid(by[i]);
+        } else {
             const float inv = 1.f / sum;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) other[i] *= inv;
+        }
+        if (balance) {
             float bias[PER];
-            if (balance) load_run<PER>(balance + PER * lane, bias);
+            load_run<PER>(balance + PER * lane, bias);
+            float all = 0.f;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const float v = by[i] == -INFINITY ? -INFINITY : (g.sigmoid ? quick_sigmoid(by[i]) : t[i] * inv) + (balance ? bias[i] : 0.f);
-                odd |= !(v < INFINITY);                                    // of a bias
-                other[i] = v;
+                other[i] += bias[i];
+                all += fabsf(bias[i]);
             }
-            store_run<PER>(room.c + PER * lane, other);
-            if (balance)
-#pragma unroll
-                for (int i = 0; i < PER; ++i) by[i] = other[i];
-            odd = __any_sync(0xffffffffu, odd);
-            __syncwarp();
+            odd = __any_sync(0xffffffffu, !(all < INFINITY));
         }
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (by[i] == -INFINITY) other[i] = -INFINITY;
+        store_run<PER>(room.c + PER * lane, other);
+        if (balance)
+#pragma unroll
+            for (int i = 0; i < PER; ++i) by[i] = other[i];
+        __syncwarp();
     }
     int stage = odd ? GATE_ALL : GATE_EXPERTS;
     unsigned kept = decided ? room.todo[kTodoKept] : 0xffffffffu;
@@ -288,11 +298,15 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
         float a, b;
         if (g.log_run >= 0) {
             a = b = -INFINITY;
+            if (by_score) {
 #pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const float x = by_score ? other[i] : by[i];
-                b = fmaxf(b, fminf(a, x));
-                a = fmaxf(a, x);
+                for (int i = 0; i < PER; ++i) {
+                    b = fmaxf(b, fminf(a, other[i]));
+                    a = fmaxf(a, other[i]);
+                }
+            } else {                                                       // the largest is all that is asked for
+#pragma unroll
+                for (int i = 0; i < PER; ++i) a = fmaxf(a, by[i]);
             }
             for (int m = 1 << g.log_run >> 1; m >= 1; m >>= 1) {
                 const float oa = __shfl_xor_sync(0xffffffffu, a, m), ob = __shfl_xor_sync(0xffffffffu, b, m);
@@ -372,17 +386,25 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
             __syncwarp();
             const int e = lane < n ? room.expert[lane] : 0;
             const float v = lane < n ? (balance ? room.c : room.z)[e] : -INFINITY;
-            float close_by = near;
-            if (balance && g.sigmoid) {                                    // the candidates' own slopes: they lie where a sigmoid is flat
-                const float e1 = lane < n ? quick_sigmoid(room.z[e]) : 0.f;
-                close_by = near - near0 + 2.f * 1.06f * dzs * warp_max(e1 * (1.f - e1) + 4e-7f) + 7e-7f;
-            }
             int before = 0, close = 0;
+            float close_by = near;
+            if (exact) {
 #pragma unroll 4
-            for (int j = 0; j < n; ++j) {
-                const float o = __shfl_sync(0xffffffffu, v, j);
-                before += o > v || (o == v && j < lane);
-                close += fabsf(o - v) <= close_by;                         // itself among them
+                for (int j = 0; j < n; ++j) {
+                    const float o = __shfl_sync(0xffffffffu, v, j);
+                    before += o > v || (o == v && j < lane);
+                }
+            } else {
+                if (balance && g.sigmoid) {                                // the candidates' own slopes: they lie where a sigmoid is flat
+                    const float e1 = lane < n ? quick_sigmoid(room.z[e]) : 0.f;
+                    close_by = near - near0 + 2.f * 1.06f * dzs * warp_max(e1 * (1.f - e1) + 4e-7f) + 7e-7f;
+                }
+#pragma unroll 4
+                for (int j = 0; j < n; ++j) {
+                    const float o = __shfl_sync(0xffffffffu, v, j);
+                    before += o > v || (o == v && j < lane);
+                    close += fabsf(o - v) <= close_by;                     // itself among them
+                }
             }
             const bool chosen = lane < n && before < g.k;
             if (!exact) {
