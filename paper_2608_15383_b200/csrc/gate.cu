@@ -75,8 +75,8 @@ gate_logits_kernel(const Z* logits, long long ld, int T, const __grid_constant__
         key = reinterpret_cast<double*>(room.z);                           // z and c
         for (bool decided = false;; decided = true) {
             if (!choose_fast<PER>(g, room, balance, 0.f, 0.f, lane, decided, ids + t * g.k, weights + t * g.k)) return;
-            if (room.todo[kTodoStage] == GATE_EXPERTS) return choose_again<PER>(g, room, nullptr, lane, ids + t * g.k, weights + t * g.k);
-            if (room.todo[kTodoStage] == GATE_ALL) break;
+            if (room.todo[kTodoStage] == GATE_EXPERTS && choose_again<PER>(g, room, nullptr, 0.f, lane, ids + t * g.k, weights + t * g.k)) return;
+            if (room.todo[kTodoStage] != GATE_GROUPS) break;
             choose_groups<PER>(g, room, nullptr, z64, lane);
         }
         __syncwarp();
@@ -102,7 +102,7 @@ template <int PER>
 struct __align__(16) FewRoom {
     ChoiceRoom<PER> room;
     float balance[32 * PER];
-    double z64[32 * PER], key[32 * PER];
+    double z64[32 * PER];
 };
 constexpr int kFewCluster = 8, kFewFour = 48;                              // four tokens per cluster from here on
 template <int TB, int PER>
@@ -212,11 +212,10 @@ gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w
         dz = 1.01f * (float)(14 + (H + 255) / 256) * 0x1p-24f * sqrtf(x2) * sqrtf(w2) + (addend ? 16.f * 0x1p-24f : 0.f);
         if (cancelled) dz = INFINITY;
     }
-    for (bool decided = false;; decided = true) {
-        const bool again = warp == 0 && choose_fast<PER>(g, room, g.balance ? sm.balance : nullptr, dz, bias || addend ? kAddedRel : 0.f, lane, decided,
-                                                         ids + t * g.k, weights + t * g.k);
-        if (!__syncthreads_or(again)) return;
-        const uint32_t stage = room.todo[kTodoStage];
+    const float* balance = g.balance ? sm.balance : nullptr;
+    const float rel = bias || addend ? kAddedRel : 0.f;
+    bool open = warp == 0 && choose_fast<PER>(g, room, balance, dz, rel, lane, false, ids + t * g.k, weights + t * g.k);
+    while (__syncthreads_or(open)) {
         int item = 0;
         for (int b = 0; 32 * b < g.E; ++b)
             for (unsigned es = room.todo[b]; es; es &= es - 1, ++item) {
@@ -226,15 +225,7 @@ gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w
                 if (lane == 0) sm.z64[e] = v + (bias ? (double)bias[e] : 0.0) + (addend ? (double)addend[t * g.E + e] : 0.0);
             }
         __syncthreads();
-        if (warp == 0) {
-            if (stage == GATE_ALL)
-                choose_exact(g, sm.z64, reinterpret_cast<unsigned long long*>(sm.key), lane, ids + t * g.k, weights + t * g.k);
-            else if (stage == GATE_EXPERTS)
-                choose_again<PER>(g, room, sm.z64, lane, ids + t * g.k, weights + t * g.k);
-            else
-                choose_groups<PER>(g, room, sm.z64, sm.key, lane);
-        }
-        if (stage != GATE_GROUPS) return;
+        if (warp == 0) open = !resolve<PER>(g, room, balance, sm.z64, dz, rel, lane, ids + t * g.k, weights + t * g.k);
     }
 }
 

@@ -218,6 +218,14 @@ __device__ __forceinline__ void store_run(float* p, const float (&v)[PER]) {
     }
 }
 
+// All logits are to be computed again.
+template <int PER>
+__device__ __forceinline__ void choose_all(const GateArgs& g, ChoiceRoom<PER>& room, int lane) {
+    for (int i = lane; 32 * i < g.E; i += 32) room.todo[i] = g.E - 32 * i >= 32 ? 0xffffffffu : (1u << (g.E - 32 * i)) - 1u;
+    if (lane == 0) room.todo[kTodoStage] = GATE_ALL;
+    __syncwarp();
+}
+
 // By one warp; lane l holds the PER experts from PER l on; `balance`: g.balance in shared memory, padded to 32 PER, or null; at most kFastChoices
 // choices.  `decided`: the groups are those of todo[kTodoKept].  True: nothing is written, and `todo` says what is to be done.
 // The choice itself: the k-th largest of the lanes' largest values is no more than the k-th largest value, so what is not below
@@ -395,9 +403,13 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
                     before += o > v || (o == v && j < lane);
                 }
             } else {
-                if (balance && g.sigmoid) {                                // the candidates' own slopes: they lie where a sigmoid is flat
-                    const float e1 = lane < n ? quick_sigmoid(room.z[e]) : 0.f;
-                    close_by = near - near0 + 2.f * 1.06f * dzs * warp_max(e1 * (1.f - e1) + 4e-7f) + 7e-7f;
+                if (balance) {                                             // the candidates' own slopes: they lie where a sigmoid is flat
+                    float slope = 0.f;
+                    if (lane < n) {
+                        const float p = g.sigmoid ? quick_sigmoid(room.z[e]) : expf(room.z[e] - mx) / sum;
+                        slope = (g.sigmoid ? p : 2.f * p) * (1.f - p);
+                    }
+                    close_by = near - near0 + 2.f * 1.06f * dzs * (warp_max(slope) + 1e-5f) + score_near - (g.sigmoid ? 2.f * 0.26f : 2.f * 0.55f) * dzs;
                 }
 #pragma unroll 4
                 for (int j = 0; j < n; ++j) {
@@ -471,14 +483,13 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
             }
         }
     }
-    if (!g.sigmoid && balance && stage != GATE_ALL) stage = GATE_ALL;      // a softmax with a bias: all logits enter every choice value
+    if (!g.sigmoid && balance && stage == GATE_GROUPS) stage = GATE_ALL;   // a softmax with a bias: all logits enter every choice value
     __syncwarp();
-    if (stage == GATE_ALL)
-        for (int i = lane; 32 * i < g.E; i += 32) room.todo[i] = g.E - 32 * i >= 32 ? 0xffffffffu : (1u << (g.E - 32 * i)) - 1u;
     if (lane == 0) {
         room.todo[kTodoKept] = kept;
         room.todo[kTodoStage] = stage;
     }
+    if (stage == GATE_ALL) choose_all<PER>(g, room, lane);
     __syncwarp();
     return true;
 }
@@ -487,7 +498,7 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
 __device__ __forceinline__ double marked_logit(const double* z64, const float* z, int e) { return z64 ? z64[e] : (double)z[e]; }
 // The groups kept, from the exact logits of the marked experts, for choose_fast to go on from there; v [E]: room.
 template <int PER>
-__device__ __noinline__ void choose_groups(const GateArgs& g, ChoiceRoom<PER>& room, const double* z64, double* v, int lane) {
+static __device__ __noinline__ void choose_groups(const GateArgs& g, ChoiceRoom<PER>& room, const double* z64, double* v, int lane) {
     float* z = room.z;
     const float* c = room.c;
     uint32_t* todo = room.todo;
@@ -519,16 +530,29 @@ __device__ __noinline__ void choose_groups(const GateArgs& g, ChoiceRoom<PER>& r
     __syncwarp();
 }
 
-// The experts chosen again by one warp, from the exact logits of the marked ones.  What was not marked is far enough from everything else to be ordered by its binary32 value.
+// The experts chosen again by one warp, from the exact logits of the marked ones.  What was not marked is far enough from everything
+// else to be ordered by its binary32 value.  False (a softmax with a bias only): p_e = exp(z_e - mx) / sum with a sum of logits that are off by dz
+// leaves c_a - c_b off by dz |p_a - p_b|, and that is not enough here.
 template <int PER>
-__device__ __noinline__ void choose_again(const GateArgs& g, ChoiceRoom<PER>& room, const double* z64, int lane, int32_t* ids, float* weights) {
+static __device__ __noinline__ bool choose_again(const GateArgs& g, ChoiceRoom<PER>& room, const double* z64, float dz, int lane, int32_t* ids, float* weights) {
     float* z = room.z;
     const float* c = room.c;
     const uint32_t* todo = room.todo;
-    const bool grouped = g.top_groups < g.G;
+    const bool grouped = g.top_groups < g.G, soft = !g.sigmoid && g.balance;
     const unsigned kept = todo[kTodoKept];
     unsigned long long key[PER];
     float mx = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+        if (lane + 32 * i < g.E) mx = fmaxf(mx, z[lane + 32 * i]);
+    mx = warp_max(mx);
+    if (!g.sigmoid && (soft || !g.renorm)) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (lane + 32 * i < g.E) sum += expf(z[lane + 32 * i] - mx);
+        sum = warp_sum_f32(sum);
+    }
+    unsigned marked = 0;
 #pragma unroll
     for (int i = 0; i < PER; ++i) {                                        // lane l: experts l, l + 32, ...
         const int e = lane + 32 * i;
@@ -538,35 +562,45 @@ __device__ __noinline__ void choose_again(const GateArgs& g, ChoiceRoom<PER>& ro
             if (todo[i] >> lane & 1u) {
                 const double x = marked_logit(z64, z, e);
                 v = x;
-                if (g.balance) v = x == -INFINITY ? x : 1.0 / (1.0 + exp(-x)) + (double)g.balance[e];      // a sigmoid: a softmax with a bias marks all
+                if (g.balance)
+                    v = x == -INFINITY ? x : (g.sigmoid ? 1.0 / (1.0 + exp(-x)) : exp(x - (double)mx) / (double)sum) + (double)g.balance[e];
                 z[e] = (float)x;
+                marked |= 1u << i;
             }
             if (!grouped || in_kept(g, kept, e)) key[i] = order_key(v);
-            mx = fmaxf(mx, z[e]);
         }
     }
-    mx = warp_max(mx);
-    if (!g.sigmoid && !g.renorm) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (lane + 32 * i < g.E) sum += expf(z[lane + 32 * i] - mx);
-        sum = warp_sum_f32(sum);
-    }
     int mine = 0;
-    for (int j = 0; j < g.k; ++j) {
+    double last = 0.0, last_p = 0.0;
+    bool last_marked = false;
+    for (int j = 0; j < g.k + (soft ? g.E : 0); ++j) {
         unsigned long long best = 0;
-        int at = 0x7fffffff;
+        int at = 0;
 #pragma unroll
         for (int i = 0; i < PER; ++i)
             if (key[i] > best) {
                 best = key[i];
-                at = lane + 32 * i;
+                at = i;
             }
         const unsigned hi = __reduce_max_sync(0xffffffffu, (unsigned)(best >> 32));
+        if (!hi) break;
         const unsigned lo = __reduce_max_sync(0xffffffffu, (unsigned)(best >> 32) == hi ? (unsigned)best : 0u);
         const bool is = (unsigned)(best >> 32) == hi && (unsigned)best == lo;
-        const int e = (int)__reduce_min_sync(0xffffffffu, is ? (unsigned)at : 0x7fffffffu);
-        if (j == lane) mine = e;
+        const int e = (int)__reduce_min_sync(0xffffffffu, is ? (unsigned)(lane + 32 * at) : 0x7fffffffu);
+        if (soft) {
+            const unsigned long long top = (unsigned long long)hi << 32 | lo;
+            const double v = __longlong_as_double((long long)(top >> 63 ? top & 0x7fffffffffffffffull : ~top)), p = v - (double)g.balance[e];
+            const bool m = todo[e >> 5] >> (e & 31) & 1u;
+            // against the one before, and behind the last choice against that one, as long as the marked ones go on
+            if (j > 0 && m && last_marked && v > -INFINITY && last - v <= 1.1 * (double)dz * fabs(last_p - p) + 1e-12) return false;
+            if (j >= g.k && !m) break;
+            if (j < g.k) {
+                last = v;
+                last_p = p;
+                last_marked = m;
+            }
+        }
+        if (j < g.k && j == lane) mine = e;
         if (lane == (e & 31))
 #pragma unroll
             for (int i = 0; i < PER; ++i)
@@ -579,10 +613,47 @@ __device__ __noinline__ void choose_again(const GateArgs& g, ChoiceRoom<PER>& ro
         ids[lane] = mine;
         weights[lane] = s;
     }
-    if (fits) return;
+    if (fits) return true;
     // sigmoids of which nothing is left in binary32
     const double x = lane < g.k ? (double)z[mine] : -INFINITY, d = 1.0 / (1.0 + exp(-x)), total = warp_sum_f64(lane < g.k ? d : 0.0);
     if (lane < g.k) weights[lane] = total > 0.0 ? (float)(d / total * (double)g.scale) : 0.f;
+    return true;
+}
+
+// The choice values of a token whose logits are back in `room` (as choose_fast leaves them).
+template <int PER>
+static __device__ __noinline__ void choice_values(const GateArgs& g, ChoiceRoom<PER>& room, const float* balance, int lane) {
+    if (!balance && !(g.top_groups < g.G && g.top2)) return;
+    float mx = -INFINITY, sum = 0.f;
+    if (!g.sigmoid) {
+        for (int e = lane; e < g.E; e += 32) mx = fmaxf(mx, room.z[e]);
+        mx = warp_max(mx);
+        for (int e = lane; e < g.E; e += 32) sum += expf(room.z[e] - mx);
+        sum = warp_sum_f32(sum);
+    }
+    for (int e = lane; e < g.E; e += 32) {
+        const float v = room.z[e], s = g.sigmoid ? quick_sigmoid(v) : expf(v - mx) / sum;
+        room.c[e] = v == -INFINITY ? v : s + (balance ? balance[e] : 0.f);
+    }
+    __syncwarp();
+}
+// A step on from choose_fast's `true`, the marked logits being in z64 (room for all): true, and the token is done; or false, and todo says
+// which logits come next.
+template <int PER>
+static __device__ __noinline__ bool resolve(const GateArgs& g, ChoiceRoom<PER>& room, const float* balance, double* z64, float dz, float rel, int lane,
+                                        int32_t* ids, float* weights) {
+    const uint32_t stage = room.todo[kTodoStage];
+    if (stage == GATE_GROUPS) {
+        choose_groups<PER>(g, room, z64, z64, lane);
+        return !choose_fast<PER>(g, room, balance, dz, rel, lane, true, ids, weights);
+    }
+    if (stage == GATE_ALL) {
+        choose_exact(g, z64, reinterpret_cast<unsigned long long*>(room.z), lane, ids, weights);       // z and c
+        return true;
+    }
+    if (choose_again<PER>(g, room, z64, dz, lane, ids, weights)) return true;
+    choose_all<PER>(g, room, lane);
+    return false;
 }
 
 // ---- what the kernels share --------------------------------------------------------------------------------------------

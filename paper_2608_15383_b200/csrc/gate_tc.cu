@@ -18,7 +18,7 @@ namespace exmoe {
 
 namespace {
 
-constexpr int kTokens = 128, kStages = 4, kDrainWarps = 16, kThreads = 32 * (4 + kDrainWarps);
+constexpr int kTokens = 128, kStages = 4, kChain = 1, kDrainWarps = 16, kThreads = 32 * (4 + kDrainWarps);
 constexpr int kRowBytes = 128;                                             // 64 elements
 __device__ int g_gate_status;                                              // sticky: EXMOE_ERR_TIMEOUT
 
@@ -51,25 +51,49 @@ __device__ __forceinline__ float ld_rank(uint32_t addr, int rank) {
     asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at_rank(addr, rank)) : "memory");
     return v;
 }
+// The parts of a token's logits, added to z [32 PER], and of its size: from this CTA's on, four CTAs' in flight.  A lane's pieces of 16
+// bytes (8: PER = 2) are as far apart as a warp reads at once.
 template <int PER>
-__device__ __forceinline__ void add_run(uint32_t addr, int rank, float (&v)[PER]) {
-    const uint32_t at = at_rank(addr, rank);
-    if constexpr (PER == 2) {
-        float a, b;
-        asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(a), "=f"(b) : "r"(at) : "memory");
-        v[0] += a;
-        v[1] += b;
-    } else {
+__device__ __forceinline__ void load_logits(uint32_t part, uint32_t size_at, int rank, int CL, int lane, float* z, float& size) {
+    constexpr int W = PER == 2 ? 2 : 4, N = PER / W;
+    float v[PER];
 #pragma unroll
-        for (int i = 0; i < PER; i += 4) {
-            float a, b, c, d;
-            asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(a), "=f"(b), "=f"(c), "=f"(d) : "r"(at + 4 * i) : "memory");
-            v[i] += a;
-            v[i + 1] += b;
-            v[i + 2] += c;
-            v[i + 3] += d;
-        }
+    for (int j = 0; j < PER; ++j) v[j] = 0.f;
+    for (int i0 = 0; i0 < CL; i0 += 4) {
+        float from[4][PER], s[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i0 + i < CL) {
+                const uint32_t at = at_rank(part, (rank + i0 + i) & (CL - 1)) + 4 * W * lane;
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    if constexpr (W == 2)
+                        asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(from[i][0]), "=f"(from[i][1]) : "r"(at) : "memory");
+                    else
+                        asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];"
+                                     : "=f"(from[i][4 * j]), "=f"(from[i][4 * j + 1]), "=f"(from[i][4 * j + 2]), "=f"(from[i][4 * j + 3]) : "r"(at + 512 * j) : "memory");
+                }
+                s[i] = ld_rank(size_at, (rank + i0 + i) & (CL - 1));
+            }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i0 + i < CL) {
+#pragma unroll
+                for (int j = 0; j < PER; ++j) v[j] += from[i][j];
+                size += s[i];
+            }
     }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        if constexpr (W == 2)
+            *reinterpret_cast<float2*>(z + 2 * lane) = make_float2(v[0], v[1]);
+        else
+            *reinterpret_cast<float4*>(z + 4 * lane + 128 * j) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+    }
+    __syncwarp();
+}
+__device__ __forceinline__ void add_pair(float& a, float& b, uint32_t x, uint32_t y) {      // two binary32 additions in one instruction
+    asm("{\n\t.reg .b64 s, t;\n\tmov.b64 s, {%0, %1};\n\tmov.b64 t, {%2, %3};\n\tadd.rn.f32x2 s, s, t;\n\tmov.b64 {%0, %1}, s;\n\t}" : "+f"(a), "+f"(b) : "r"(x), "r"(y));
 }
 // sum of squares of 16 bytes of BF16, in pairs of BF16 sums: short by less than 4 2^-9 of itself
 __device__ __forceinline__ void square(__nv_bfloat162& sum, const uint4& v) {
@@ -94,10 +118,17 @@ __device__ __forceinline__ bool choosers_or(bool v) {
     return r != 0;
 }
 
-template <int MT, int PER>
+template <int PER>
 struct Warp {                                                              // a choosing warp's share of shared memory
     ChoiceRoom<PER> room;
-    double z64[32 * PER];
+    double z64[32 * PER];                                                  // logits computed again
+};
+constexpr int kItems = 1024;
+// A token that waits for logits to be computed again; its logits are back in its row of `part`, which no other CTA reads.
+struct Waiting {
+    int token, first;                                                      // in the tile; first item, -1: no room for it in this round
+    float dz;
+    uint32_t todo[kTodoWords];
 };
 template <int MT, int PER>
 struct __align__(1024) Shared {
@@ -106,12 +137,15 @@ struct __align__(1024) Shared {
         unsigned char ring[kStages][kStage];                               // weights, then tokens; rows of 128 bytes, swizzled
         struct {
             float part[kTokens][MT * 128];                                 // this CTA's part of the logits, read by the cluster
-            Warp<MT, PER> warp[kDrainWarps];
+            Warp<PER> warp[kDrainWarps];
         } s;
     };
-    float x2[kTokens], w2[MT * 128], balance[32 * PER];
+    float size[kTokens], balance[32 * PER];
     float w2_max[kDrainWarps];
-    int items, item[kDrainWarps * 32 * PER];                               // logits to compute again: warp << 16 | expert
+    int n_waiting, n_items;
+    Waiting waiting[kTokens];
+    double item_z[kItems];                                                 // logits to compute again
+    unsigned short item_expert[kItems], item_waiting[kItems];
     uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2];
     uint32_t tmem;
     int abort_flag;
@@ -123,7 +157,7 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                const __nv_bfloat16* __restrict__ w_router, const float* __restrict__ bias, const float* addend, int T, int H,
                const __grid_constant__ GateArgs g, int CL, int32_t* ids, float* weights) {
     using S = Shared<MT, PER>;
-    constexpr int EP = MT * 128, COLS = MT * kTokens / 4;                  // accumulator columns of a drain warp: a quarter of them, on its 32 lanes
+    constexpr int COLS = MT * kTokens / 4;                  // accumulator columns of a drain warp: a quarter of them, on its 32 lanes
     extern __shared__ unsigned char raw[];
     S& sm = *reinterpret_cast<S*>(raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u));
     const int tid = threadIdx.x, lane = tid & 31, warp = warp_uniform(tid >> 5);
@@ -139,6 +173,7 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
             mbar_init(&sm.acc_empty[b], kDrainWarps);
         }
         sm.abort_flag = 0;
+        sm.n_waiting = sm.n_items = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {
@@ -153,31 +188,49 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     grid_launch_dependents();
     const int blocks = (H + 63) / 64, kb0 = blocks * rank / CL, n = blocks * (rank + 1) / CL - kb0;
     const uint32_t full = smem_u32(sm.full), empty = smem_u32(sm.empty), acc_full = smem_u32(sm.acc_full), acc_empty = smem_u32(sm.acc_empty);
-    float acc[COLS];
+    float acc[COLS], x2 = 0.f;
 #pragma unroll
     for (int i = 0; i < COLS; ++i) acc[i] = 0.f;
     const int d = warp - 4, quarter = warp & 3;                            // drain warps: d of kDrainWarps
     const int mt = MT == 2 ? d >> 3 : 0, col0 = (d >> 2) * COLS % kTokens; // experts mt * 128 + 32 quarter + lane, tokens col0 ..
     bool ok = true;
     if (warp == 0) {
-        const uint32_t idesc = make_idesc(kTokens);
-        for (int i = 0; i < n; ++i) {
-            const int s = i % kStages, buf = i & 1;
-            if (i >= 2) ok = mbar_wait_warp(acc_empty + 8 * buf, ((i >> 1) - 1) & 1, abort_flag, &g_gate_status);
-            if (ok) ok = mbar_wait_warp(full + 8 * s, (i / kStages) & 1, abort_flag, &g_gate_status);
-            if (!ok) break;
-            tc_fence_after();
-            const uint64_t dw = make_desc_b(smem_u32(sm.ring[s])), dx = make_desc_b(smem_u32(sm.ring[s]) + MT * 128 * kRowBytes);
-            if (elect_one()) {
+        // The ring unrolled, so that the MMAs' operands are constants away from two descriptors, and the next stage's barrier looked at
+        // before this stage's MMAs: what stands between two MMAs is time that the tensor pipe may run dry.
+        constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTokens >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
+        static_assert(kStages % (2 * kChain) == 0, "a turn of the ring leaves off where it began");
+        constexpr int kTurns = kStages / (2 * kChain);                     // of the two accumulators in a turn of the ring
+        const uint64_t dw0 = make_desc_b(smem_u32(sm.ring[0])), dx0 = make_desc_b(smem_u32(sm.ring[0]) + MT * 128 * kRowBytes);
+        uint32_t turn = 0;                                                 // parity of the ring's turn
+        bool ready = false;
+        for (int i0 = 0; i0 < n && ok; i0 += kStages, turn ^= 1) {
 #pragma unroll
-                for (int m = 0; m < MT; ++m)
+            for (int s = 0; s < kStages; ++s) {
+                if (i0 + s >= n) break;
+                const int buf = s / kChain & 1, use = s / (2 * kChain), next = (s + 1) % kStages;
+                if (s % kChain == 0 && (i0 > 0 || use > 0)) {              // the accumulator's use number i0 / kStages * kTurns + use
+                    ok = mbar_wait_warp(acc_empty + 8 * buf, (kTurns % 2 ? turn + use + 1 : use + 1) & 1, abort_flag, &g_gate_status);
+                    if (!ok) break;
+                }
+                if (!ready) {
+                    ok = mbar_wait_warp(full + 8 * s, turn, abort_flag, &g_gate_status);
+                    if (!ok) break;
+                }
+                tc_fence_after();
+                const bool seen = i0 + s + 1 < n && mbar_look_at(full + 8 * next, next ? turn : turn ^ 1);
+                if (elect_one()) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)                            // K = 16: 32 bytes on
-                        mma_f16(tmem + (buf * MT + m) * kTokens, dw + (uint64_t)(m * 128 * kRowBytes + 32 * j >> 4), dx + (uint64_t)(32 * j >> 4), idesc, j > 0);
-                tc_commit_at(empty + 8 * s);
-                tc_commit_at(acc_full + 8 * buf);
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)                        // K = 16: 32 bytes on
+                            mma_f16(tmem + (buf * MT + m) * kTokens, dw0 + (uint64_t)(s * S::kStage + m * 128 * kRowBytes + 32 * j >> 4),
+                                    dx0 + (uint64_t)(s * S::kStage + 32 * j >> 4), idesc, j > 0 || s % kChain > 0);
+                    tc_commit_at(empty + 8 * s);
+                    if (s % kChain == kChain - 1 || i0 + s == n - 1) tc_commit_at(acc_full + 8 * buf);
+                }
+                __syncwarp();
+                ready = __all_sync(0xffffffffu, seen);
             }
-            __syncwarp();
         }
     } else if (warp == 1) {
         for (int i = 0; i < n; ++i) {
@@ -197,33 +250,43 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         // a quarter of a token's row, and a half (MT = 2) or a quarter of an expert's
         constexpr int WQ = MT == 2 ? 4 : 2;                                // 16-byte pieces
         const int u = tid - 128, xr = u >> 2, wr = MT == 2 ? u >> 1 : u >> 2;
-        float x2 = 0.f, w2 = 0.f;
+        float w2 = 0.f;
         for (int i = 0; i < n; ++i) {
-            const int s = i % kStages, buf = i & 1;
+            const int s = i % kStages, c = i / kChain, buf = c & 1;
             ok = mbar_wait_warp(full + 8 * s, (i / kStages) & 1, abort_flag, &g_gate_status);
             if (!ok) break;
             const __nv_bfloat162 zero(__float2bfloat16(0.f), __float2bfloat16(0.f));
-            __nv_bfloat162 a = zero, b = zero;
+            __nv_bfloat162 a[2] = {zero, zero}, b[WQ];
             const unsigned char *wt = sm.ring[s] + wr * kRowBytes, *xt = sm.ring[s] + (MT * 128 + xr) * kRowBytes;
+            uint4 xv[2], wv[WQ];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) square(a, *reinterpret_cast<const uint4*>(xt + ((((u & 3) * 2 + j) ^ (xr & 7)) << 4)));
+            for (int j = 0; j < 2; ++j) xv[j] = *reinterpret_cast<const uint4*>(xt + ((((u & 3) * 2 + j) ^ (xr & 7)) << 4));
 #pragma unroll
-            for (int j = 0; j < WQ; ++j) square(b, *reinterpret_cast<const uint4*>(wt + ((((MT == 2 ? u & 1 : u & 3) * WQ + j) ^ (wr & 7)) << 4)));
+            for (int j = 0; j < WQ; ++j) wv[j] = *reinterpret_cast<const uint4*>(wt + ((((MT == 2 ? u & 1 : u & 3) * WQ + j) ^ (wr & 7)) << 4));
+#pragma unroll
+            for (int j = 0; j < 2; ++j) square(a[j], xv[j]);
+#pragma unroll
+            for (int j = 0; j < WQ; ++j) {
+                b[j] = zero;
+                square(b[j], wv[j]);
+            }
             __syncwarp();
             if (lane == 0) mbar_arrive_at(empty + 8 * s);
-            x2 += __low2float(a) + __high2float(a);
-            w2 += __low2float(b) + __high2float(b);
-            ok = mbar_wait_warp(acc_full + 8 * buf, (i >> 1) & 1, abort_flag, &g_gate_status);
+            x2 += __low2float(a[0]) + __high2float(a[0]) + (__low2float(a[1]) + __high2float(a[1]));
+#pragma unroll
+            for (int j = 0; j < WQ; ++j) w2 += __low2float(b[j]) + __high2float(b[j]);
+            if (i % kChain < kChain - 1 && i < n - 1) continue;
+            ok = mbar_wait_warp(acc_full + 8 * buf, (c >> 1) & 1, abort_flag, &g_gate_status);
             if (!ok) break;
             tc_fence_after();
             const uint32_t at = tmem + ((uint32_t)(32 * quarter) << 16) + (buf * MT + mt) * kTokens + col0;
 #pragma unroll
-            for (int c = 0; c < COLS; c += 16) {
+            for (int k = 0; k < COLS; k += 16) {
                 uint32_t r[16];
-                tmem_ld16(at + c, r);
+                tmem_ld16(at + k, r);
                 tc_wait_ld();
 #pragma unroll
-                for (int j = 0; j < 16; ++j) acc[c + j] += __uint_as_float(r[j]);
+                for (int j = 0; j < 16; j += 2) add_pair(acc[k + j], acc[k + j + 1], r[j], r[j + 1]);
             }
             tc_fence_before();
             __syncwarp();
@@ -233,114 +296,144 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         x2 += __shfl_xor_sync(0xffffffffu, x2, 2);
         w2 += __shfl_xor_sync(0xffffffffu, w2, 1);
         if (MT == 1) w2 += __shfl_xor_sync(0xffffffffu, w2, 2);
-        if ((u & 3) == 0) sm.x2[xr] = x2;
-        if (MT == 2 ? (u & 1) == 0 : (u & 3) == 0) sm.w2[wr] = w2;
+        if (!ok) w2 = INFINITY;                                            // nothing is known of the logits: all will be computed again
+        w2 = warp_max(w2);                                                 // rows behind the last expert are zeros
+        if (lane == 0) sm.w2_max[d] = w2;
     }
     __syncthreads();                                                       // the ring has been read, the accumulators too
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * MT * kTokens));
-    if (warp >= 4)
+    if (warp >= 4) {
 #pragma unroll
         for (int i = 0; i < COLS; ++i) sm.s.part[col0 + i][mt * 128 + 32 * quarter + lane] = acc[i];
-    cluster_arrive();
-    cluster_wait();
-    if (warp >= 4) {
-        float w2 = 0.f;
-        for (int e = tid - 128; e < EP; e += 32 * kDrainWarps) {
-            float v = 0.f;
-            for (int r = 0; r < CL; ++r) v += ld_rank(smem_u32(&sm.w2[e]), r);
-            w2 = v;                                                        // rows behind the last expert are zeros
-        }
-        w2 = warp_max(w2);
-        if (lane == 0) sm.w2_max[d] = w2;
-    }
-    bool all_ok = true;                                                    // of the whole cluster: a part of the logits is missing otherwise
-    for (int r = 0; r < CL; ++r) {
-        int f;
-        asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(f) : "r"(at_rank(smem_u32(&sm.abort_flag), r)) : "memory");
-        all_ok &= f == 0;
-    }
-    __syncthreads();
-    if (warp >= 4 && all_ok) {
-        Warp<MT, PER>& my = sm.s.warp[d];
-        ChoiceRoom<PER>& room = my.room;
         float w2 = 0.f;
 #pragma unroll
         for (int i = 0; i < kDrainWarps; ++i) w2 = fmaxf(w2, sm.w2_max[i]);
+        const int u = tid - 128;                                           // |x| |w| of this part of K, the largest |w| of all experts
+        if ((u & 3) == 0) sm.size[u >> 2] = w2 < INFINITY ? sqrtf(x2) * sqrtf(w2) : INFINITY;
+    }
+    cluster_arrive();
+    cluster_wait();
+    if (warp >= 4) {
+        Warp<PER>& my = sm.s.warp[d];
+        ChoiceRoom<PER>& room = my.room;
         const float* balance = g.balance ? sm.balance : nullptr;
+        const float rel = bias || addend ? kAddedRel : 0.f;
         const int owned = kTokens / CL, chunks = H / 8;
-        for (int i = d; i - d < owned; i += kDrainWarps) {                 // the warps together, so that they share what is computed again
+        for (int i = d; i < owned; i += kDrainWarps) {
             const int tok = rank * owned + i;
             const long long t = t0 + tok;
-            const bool live = i < owned && t < T;
-            if (tid == 128) sm.items = 0;
-            float dz = 0.f;
-            if (live) {
-                float v[PER], x2 = 0.f;
+            if (t >= T) break;
+            float size = 0.f;
+            load_logits<PER>(smem_u32(&sm.s.part[tok][0]), smem_u32(&sm.size[tok]), rank, CL, lane, room.z, size);
+            bool cancelled = false;
 #pragma unroll
-                for (int j = 0; j < PER; ++j) v[j] = 0.f;
-                for (int r = 0; r < CL; ++r) {
-                    add_run<PER>(smem_u32(&sm.s.part[tok][PER * lane]), r, v);
-                    x2 += ld_rank(smem_u32(&sm.x2[tok]), r);
-                }
-                bool cancelled = false;
-#pragma unroll
-                for (int j = 0; j < PER; ++j) {
-                    const int e = PER * lane + j;
-                    if (e < g.E) {
-                        if (bias) v[j] += bias[e];
-                        if (addend) {
-                            const float before = fabsf(v[j]);
-                            v[j] += addend[t * g.E + e];
-                            cancelled |= before > 2.f * fabsf(v[j]) + 16.f;
-                        }
-                    } else {
-                        v[j] = -INFINITY;
+            for (int j = 0; j < PER; ++j) {
+                const int e = lane + 32 * j;
+                float v = -INFINITY;
+                if (e < g.E) {
+                    v = room.z[e];
+                    if (bias) v += bias[e];
+                    if (addend) {
+                        const float before = fabsf(v);
+                        v += addend[t * g.E + e];
+                        cancelled |= before > 2.f * fabsf(v) + 16.f;
                     }
                 }
-                store_run<PER>(room.z + PER * lane, v);
-                __syncwarp();
-                // the tensor cores' 2 x 21, an addition per stage, one per CTA; the norms are short by less than 2 %
-                dz = 1.02f * (float)(42 + (blocks + CL - 1) / CL + CL) * 0x1p-24f * sqrtf(x2) * sqrtf(w2) + (addend ? 16.f * 0x1p-24f : 0.f);
-                if (__any_sync(0xffffffffu, cancelled)) dz = INFINITY;
-            }
-            int32_t* ids_t = ids + t * g.k;
-            float* weights_t = weights + t * g.k;
-            bool open = live;                                              // not chosen yet
-            for (bool decided = false;; decided = true) {
-                open = open && choose_fast<PER>(g, room, balance, dz, bias || addend ? kAddedRel : 0.f, lane, decided, ids_t, weights_t);
-                if (!choosers_or(open)) break;
-                if (open) {
-                    unsigned es = 32 * lane < g.E ? room.todo[lane] : 0u;  // a word per lane
-                    int at = 0;
-                    if (es) at = atomicAdd(&sm.items, __popc(es));
-                    for (; es; es &= es - 1) sm.item[at++] = d << 16 | (32 * lane + __ffs(es) - 1);
-                }
-                choosers_sync();
-                for (int j = d; j < sm.items; j += kDrainWarps) {
-                    const int who = sm.item[j] >> 16, e = sm.item[j] & 0xffff;
-                    const long long u = t - d + who;                       // that warp's token
-                    const double z = logit_f64(reinterpret_cast<const uint4*>(hidden + u * H), reinterpret_cast<const uint4*>(w_router + (size_t)e * H), chunks, lane);
-                    if (lane == 0) sm.s.warp[who].z64[e] = z + (bias ? (double)bias[e] : 0.0) + (addend ? (double)addend[u * g.E + e] : 0.0);
-                }
-                choosers_sync();
-                if (tid == 128) sm.items = 0;
-                if (!open) continue;
-                const uint32_t stage = room.todo[kTodoStage];
-                if (stage == GATE_GROUPS) {
-                    choose_groups<PER>(g, room, my.z64, my.z64, lane);
-                    continue;
-                }
-                if (stage == GATE_EXPERTS)
-                    choose_again<PER>(g, room, my.z64, lane, ids_t, weights_t);
-                else
-                    choose_exact(g, my.z64, reinterpret_cast<unsigned long long*>(room.z), lane, ids_t, weights_t);       // z and c
-                open = false;
+                if (bias || addend || e >= g.E) room.z[e] = v;
             }
             __syncwarp();
+            // the tensor cores' 2 x 21 per stage of a chain, an addition per chain, one per CTA; the norms are short by less than 2 %
+            float dz = 1.02f * (float)(42 * kChain + (blocks + kChain * CL - 1) / (kChain * CL) + 1 + CL) * 0x1p-24f * size + (addend ? 16.f * 0x1p-24f : 0.f);
+            if (__any_sync(0xffffffffu, cancelled)) dz = INFINITY;
+            int32_t* ids_t = ids + t * g.k;
+            float* weights_t = weights + t * g.k;
+            if (!choose_fast<PER>(g, room, balance, dz, rel, lane, false, ids_t, weights_t)) continue;
+            int at = 0;
+            if (lane == 0) at = atomicAdd(&sm.n_waiting, 1);
+            at = __shfl_sync(0xffffffffu, at, 0);
+            if (lane < kTodoWords) sm.waiting[at].todo[lane] = room.todo[lane];
+            if (lane == 0) {
+                sm.waiting[at].token = tok;
+                sm.waiting[at].dz = dz;
+            }
+#pragma unroll
+            for (int j = 0; j < PER; ++j) sm.s.part[tok][lane + 32 * j] = room.z[lane + 32 * j];
         }
+        cluster_arrive();                                                  // this warp has read the others' shared memory
+        choosers_sync();
+        // The tokens that wait are done by the warps together: first the logits, then the choices.
+        const int n_waiting = sm.n_waiting;
+        for (bool open = n_waiting > 0; open;) {
+            for (int f = d; f < n_waiting; f += kDrainWarps) {
+                Waiting& w = sm.waiting[f];
+                const unsigned es = w.token >= 0 && 32 * lane < g.E ? w.todo[lane] : 0u;       // a word per lane
+                int before = __popc(es);
+#pragma unroll
+                for (int m = 1; m < 32; m <<= 1) {
+                    const int o = __shfl_up_sync(0xffffffffu, before, m);
+                    if (lane >= m) before += o;
+                }
+                const int total = __shfl_sync(0xffffffffu, before, 31);
+                int first = 0;
+                if (lane == 0 && total) first = atomicAdd(&sm.n_items, total);
+                first = __shfl_sync(0xffffffffu, first, 0);
+                const bool fits = first + total <= kItems;
+                if (lane == 0) w.first = fits ? first : -1;
+                int at = first + before - __popc(es);
+                for (unsigned r = es; r; r &= r - 1, ++at)
+                    if (at < kItems) {
+                        sm.item_expert[at] = (unsigned short)(32 * lane + __ffs(r) - 1);
+                        sm.item_waiting[at] = (unsigned short)f;
+                    }
+            }
+            choosers_sync();
+            const int n_items = min(sm.n_items, kItems);
+            for (int j = d; j < n_items; j += kDrainWarps) {
+                const long long t = t0 + sm.waiting[sm.item_waiting[j]].token;
+                const int e = sm.item_expert[j];
+                const double z = logit_f64(reinterpret_cast<const uint4*>(hidden + t * H), reinterpret_cast<const uint4*>(w_router + (size_t)e * H), chunks, lane);
+                if (lane == 0) sm.item_z[j] = z + (bias ? (double)bias[e] : 0.0) + (addend ? (double)addend[t * g.E + e] : 0.0);
+            }
+            choosers_sync();
+            if (tid == 128) sm.n_items = 0;
+            open = false;
+            for (int f = d; f < n_waiting; f += kDrainWarps) {
+                Waiting& w = sm.waiting[f];
+                const int tok = w.token;
+                if (tok < 0) continue;
+                if (w.first < 0) {
+                    open = true;
+                    continue;
+                }
+#pragma unroll
+                for (int j = 0; j < PER; ++j) room.z[lane + 32 * j] = sm.s.part[tok][lane + 32 * j];
+                if (lane < kTodoWords) room.todo[lane] = w.todo[lane];
+                __syncwarp();
+                int j = w.first;
+                for (int b = 0; 32 * b < g.E; ++b)                         // the items are in ascending experts
+                    for (unsigned es = room.todo[b]; es; es &= es - 1, ++j)
+                        if (lane == 0) my.z64[32 * b + __ffs(es) - 1] = sm.item_z[j];
+                choice_values<PER>(g, room, balance, lane);
+                __syncwarp();
+                const long long t = t0 + tok;
+                const bool done = resolve<PER>(g, room, balance, my.z64, w.dz, rel, lane, ids + t * g.k, weights + t * g.k);
+                __syncwarp();
+                if (done) {
+                    if (lane == 0) w.token = -1;
+                } else {
+                    open = true;
+                    if (lane < kTodoWords) w.todo[lane] = room.todo[lane];
+#pragma unroll
+                    for (int j = 0; j < PER; ++j) sm.s.part[tok][lane + 32 * j] = room.z[lane + 32 * j];
+                }
+                __syncwarp();
+            }
+            open = choosers_or(open);
+        }
+    } else {
+        cluster_arrive();
     }
-    cluster_arrive();                                                      // nobody reads this CTA's shared memory any more
-    cluster_wait();
+    cluster_wait();                                                        // nobody reads this CTA's shared memory any more
 }
 
 template <int MT, int PER>
