@@ -73,11 +73,14 @@ gate_logits_kernel(const Z* logits, long long ld, int T, const __grid_constant__
         __syncwarp();
         z64 = reinterpret_cast<double*>(mine + sizeof(ChoiceRoom<PER>));
         key = reinterpret_cast<double*>(room.z);                           // z and c
-        for (bool decided = false;; decided = true) {
-            if (!choose_fast<PER>(g, room, balance, 0.f, 0.f, lane, decided, ids + t * g.k, weights + t * g.k)) return;
-            if (room.todo[kTodoStage] == GATE_EXPERTS && choose_again<PER>(g, room, nullptr, 0.f, lane, ids + t * g.k, weights + t * g.k)) return;
-            if (room.todo[kTodoStage] != GATE_GROUPS) break;
-            choose_groups<PER>(g, room, nullptr, z64, lane);
+        for (int mode = GATE_NEW;;) {
+            if (!choose_fast<PER>(g, room, balance, 0.f, 0.f, lane, mode, nullptr, ids + t * g.k, weights + t * g.k)) return;
+            if (room.todo[kTodoStage] == GATE_ALL) break;
+            mode = GATE_EXACT;
+            if (room.todo[kTodoStage] == GATE_GROUPS) {
+                choose_groups<PER>(g, room, nullptr, z64, lane);
+                mode = GATE_DECIDED;
+            }
         }
         __syncwarp();
     } else {
@@ -214,8 +217,11 @@ gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w
     }
     const float* balance = g.balance ? sm.balance : nullptr;
     const float rel = bias || addend ? kAddedRel : 0.f;
-    bool open = warp == 0 && choose_fast<PER>(g, room, balance, dz, rel, lane, false, ids + t * g.k, weights + t * g.k);
-    while (__syncthreads_or(open)) {
+    int32_t* ids_t = ids + t * g.k;
+    float* weights_t = weights + t * g.k;
+    for (int mode = GATE_NEW;;) {
+        const bool open = warp == 0 && mode >= 0 && choose_fast<PER>(g, room, balance, dz, rel, lane, mode, sm.z64, ids_t, weights_t);
+        if (!__syncthreads_or(open)) return;
         int item = 0;
         for (int b = 0; 32 * b < g.E; ++b)
             for (unsigned es = room.todo[b]; es; es &= es - 1, ++item) {
@@ -225,7 +231,7 @@ gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w
                 if (lane == 0) sm.z64[e] = v + (bias ? (double)bias[e] : 0.0) + (addend ? (double)addend[t * g.E + e] : 0.0);
             }
         __syncthreads();
-        if (warp == 0) open = !resolve<PER>(g, room, balance, sm.z64, dz, rel, lane, ids + t * g.k, weights + t * g.k);
+        if (warp == 0) mode = go_on<PER>(g, room, sm.z64, lane, ids_t, weights_t);
     }
 }
 

@@ -21,6 +21,7 @@ constexpr int kFastExperts = 512, kFastChoices = 32;                       // wh
 // What it leaves where it cannot decide: a bit per expert whose logit decides, the groups kept, and what is to be done with these logits
 constexpr int kTodoKept = kFastExperts / 32, kTodoStage = kTodoKept + 1, kTodoWords = kTodoKept + 2;
 enum { GATE_EXPERTS = 0, GATE_ALL = 1, GATE_GROUPS = 2 };
+enum { GATE_NEW = 0, GATE_DECIDED = 1, GATE_EXACT = 2 };                   // how a choice begins
 
 // Doubles as integers of the same order: 0 is left for an expert that cannot be chosen, 1 is a NaN, -infinity follows; zeros of both signs are equal.
 __device__ __forceinline__ unsigned long long order_key(double v) {
@@ -187,6 +188,83 @@ __device__ __forceinline__ bool choice_weight(const GateArgs& g, float z, bool c
     return true;
 }
 
+// What few tokens come to is kept out of the way of what all of them do (registers, instruction cache).
+// Experts of group o whose value is at least lane o's `from` are marked.
+static __device__ __noinline__ void mark_from(const GateArgs& g, uint32_t* todo, const float* v, float from, int lane) {
+    for (int e0 = 0; e0 < g.E; e0 += 32) {
+        const int e = e0 + lane;
+        const float t = __shfl_sync(0xffffffffu, from, group_of(g, min(e, g.E - 1)));
+        const unsigned m = __ballot_sync(0xffffffffu, e < g.E && v[e] >= t);
+        if (lane == 0) todo[e0 >> 5] |= m;
+    }
+    __syncwarp();
+}
+// Candidates (expert e with value v in lanes 0 .. n - 1) before this lane's, the marked ones by their exact logits; the others are far
+// enough from everything to be ordered by v.  -1 in all lanes: that does not decide.  It may not for a softmax with a bias: p_e = exp(z_e -
+// mx) / sum with a sum of logits that are off by dz leaves c_a - c_b off by dz |p_a - p_b|.
+static __device__ __noinline__ int rank_exact(const GateArgs& g, const uint32_t* todo, const float* z, const double* z64, const float* balance, float v, int e,
+                                              int n, float dz, float mx, float sum, int lane) {
+    const bool m = lane < n && (todo[e >> 5] >> (e & 31) & 1u), soft = balance && !g.sigmoid;
+    const double b = balance && lane < n ? (double)balance[e] : 0.0;
+    double w = (double)v;
+    if (m) {
+        const double x = z64 ? z64[e] : (double)z[e];
+        w = x;
+        if (balance) w = x == -INFINITY ? x : (g.sigmoid ? 1.0 / (1.0 + exp(-x)) : exp(x - (double)mx) / (double)sum) + b;
+    }
+    int before = 0;
+    bool unsure = false;
+    for (int j = 0; j < n; ++j) {
+        const double o = __shfl_sync(0xffffffffu, w, j);
+        before += o > w || (o == w && j < lane);
+        if (soft) {
+            const double ob = __shfl_sync(0xffffffffu, b, j);
+            const bool om = __shfl_sync(0xffffffffu, m, j);
+            unsure |= m && om && j != lane && w > -INFINITY && o > -INFINITY && fabs(o - w) <= 1.1 * (double)dz * fabs((o - ob) - (w - b)) + 1e-12;
+        }
+    }
+    return __any_sync(0xffffffffu, unsure && before <= g.k) ? -1 : before;
+}
+// k rounds of arg-max over v [E]: lane j gets the j-th choice (-1: none).  True: near-ties were marked instead.
+static __device__ __noinline__ bool choose_rounds(const GateArgs& g, uint32_t* todo, const float* v, unsigned kept, float near0, float near1, int lane, int& mine) {
+    const bool grouped = g.top_groups < g.G, exact = near0 == 0.f;
+    unsigned taken = 0;                                                    // of experts lane, lane + 32, ...
+    bool marked = false;
+    float prev = 0.f;
+    int prev_e = 0;
+    for (int j = 0; j <= g.k; ++j) {
+        uint32_t top = 0;
+        int be = 0x7fffffff;
+        for (int i = 0, e = lane; e < g.E; ++i, e += 32) {
+            const uint32_t key = (taken >> i & 1u) || (grouped && !in_kept(g, kept, e)) ? 0u : order_key(v[e]);
+            if (key > top) {                                               // ascending experts: the first maximum wins
+                top = key;
+                be = e;
+            }
+        }
+        const uint32_t most = __reduce_max_sync(0xffffffffu, top);
+        if (!most) break;                                                  // no other expert can be chosen
+        const int e = (int)__reduce_min_sync(0xffffffffu, top == most ? (unsigned)be : 0x7fffffffu);
+        const float x = key_value(most);
+        if (!exact && j > 0 && x > -INFINITY && prev - x <= near0 + near1 * (fabsf(prev) + fabsf(x))) {
+            marked = true;
+            if (lane == 0) {
+                atomicOr(&todo[prev_e >> 5], 1u << (prev_e & 31));
+                atomicOr(&todo[e >> 5], 1u << (e & 31));
+            }
+            if (j == g.k)                                                  // whatever could displace the last choice, and a little more
+                for (int i = 0, o = lane; o < g.E; ++i, o += 32)
+                    if (!(taken >> i & 1u) && (!grouped || in_kept(g, kept, o)) && v[o] >= x - near0 - 2.f * near1 * fabsf(x)) atomicOr(&todo[o >> 5], 1u << (o & 31));
+        }
+        prev = x;
+        prev_e = e;
+        if (j == lane && j < g.k) mine = e;
+        if (lane == (e & 31)) taken |= 1u << (e >> 5);
+    }
+    __syncwarp();
+    return marked;
+}
+
 // What a warp needs in shared memory for a token's choice.
 template <int PER>
 struct __align__(16) ChoiceRoom {
@@ -226,14 +304,15 @@ __device__ __forceinline__ void choose_all(const GateArgs& g, ChoiceRoom<PER>& r
     __syncwarp();
 }
 
-// By one warp; lane l holds the PER experts from PER l on; `balance`: g.balance in shared memory, padded to 32 PER, or null; at most kFastChoices
-// choices.  `decided`: the groups are those of todo[kTodoKept].  True: nothing is written, and `todo` says what is to be done.
+// By one warp; lane l holds the PER experts from PER l on; `balance`: g.balance padded to 32 PER, or null; at most kFastChoices choices.
+// `mode`: GATE_NEW; GATE_DECIDED: the groups are those of todo[kTodoKept]; GATE_EXACT: and the exact logits of the experts marked in todo are in z64
+// (or z has them itself, z64 null).  True: nothing is written, and `todo` says what is to be done.
 // The choice itself: the k-th largest of the lanes' largest values is no more than the k-th largest value, so what is not below
 // it (by more than `near`) are all candidates, k and a few more; they go to a lane each, which counts those before its own.  (Instead
 // of k rounds of arg-max, which took twice the instructions.)
 template <int PER>
-__device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& room, const float* balance, float dz, float rel, int lane, bool decided,
-                                            int32_t* ids, float* weights) {
+__device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& room, const float* balance, float dz, float rel, int lane, int mode,
+                                            const double* z64, int32_t* ids, float* weights) {
     const bool grouped = g.top_groups < g.G, by_score = balance || (grouped && g.top2);
     float by[PER], other[PER];                                             // what orders the experts; scores where these are not it
     load_run<PER>(room.z + PER * lane, by);
@@ -294,15 +373,11 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
         __syncwarp();
     }
     int stage = odd ? GATE_ALL : GATE_EXPERTS;
-    unsigned kept = decided ? room.todo[kTodoKept] : 0xffffffffu;
-    if (lane < kTodoKept) room.todo[lane] = 0;
+    unsigned kept = mode == GATE_NEW ? 0xffffffffu : room.todo[kTodoKept];
+    if (mode != GATE_EXACT && lane < kTodoKept) room.todo[lane] = 0;
     __syncwarp();
     bool marked = false;
-    auto mark = [&](int e) {
-        atomicOr(&room.todo[e >> 5], 1u << (e & 31));
-        marked = true;
-    };
-    if (grouped && !decided && !odd) {
+    if (grouped && mode == GATE_NEW && !odd) {
         float a, b;
         if (g.log_run >= 0) {
             a = b = -INFINITY;
@@ -336,13 +411,8 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
         if (near > 0.f && high > -INFINITY && low - high <= near) {
             // the groups on the border, and of each the experts that may be its largest (two)
             const bool border = real && (keep ? value <= high + near : value >= low - near);
-            const float least = g.top2 && b > -INFINITY ? b : a, from = border ? least - near_v - 2.f * rel_v * fabsf(least) : INFINITY;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int e = PER * lane + i;
-                const float t = __shfl_sync(0xffffffffu, from, min(group_of(g, e), 31));
-                if (e < g.E && (by_score ? other[i] : by[i]) >= t) mark(e);
-            }
+            const float least = g.top2 && b > -INFINITY ? b : a;
+            mark_from(g, room.todo, by_score ? room.c : room.z, border ? least - near_v - 2.f * rel_v * fabsf(least) : INFINITY, lane);
             stage = GATE_GROUPS;
         }
     }
@@ -396,7 +466,13 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
             const float v = lane < n ? (balance ? room.c : room.z)[e] : -INFINITY;
             int before = 0, close = 0;
             float close_by = near;
-            if (exact) {
+            if (mode == GATE_EXACT) {
+                before = rank_exact(g, room.todo, room.z, z64, balance, v, e, n, dzs, mx, sum, lane);
+                if (before < 0) {
+                    marked = true;
+                    stage = GATE_ALL;
+                }
+            } else if (exact) {
 #pragma unroll 4
                 for (int j = 0; j < n; ++j) {
                     const float o = __shfl_sync(0xffffffffu, v, j);
@@ -419,9 +495,12 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
                 }
             }
             const bool chosen = lane < n && before < g.k;
-            if (!exact) {
+            if (!exact && mode != GATE_EXACT) {
                 const float last = __shfl_sync(0xffffffffu, v, __ffs(__ballot_sync(0xffffffffu, lane < n && before == g.k - 1)) - 1);
-                if (lane < n && (chosen ? close > 1 : v >= last - close_by)) mark(e);
+                if (lane < n && (chosen ? close > 1 : v >= last - close_by)) {
+                    atomicOr(&room.todo[e >> 5], 1u << (e & 31));
+                    marked = true;
+                }
             }
             if (!__any_sync(0xffffffffu, marked)) {
                 float s;
@@ -434,47 +513,17 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
                 }
                 stage = GATE_ALL;
             }
-        } else {                                                           // many equal values, or few logits that are not -infinity: k rounds
-            uint32_t key[PER];
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                const int e = PER * lane + i;
-                key[i] = e < g.E && (!grouped || in_kept(g, kept, e)) ? order_key(by[i]) : 0u;
-            }
-            float prev = 0.f;
-            int prev_e = 0, mine = 0;
-            for (int j = 0; j <= g.k; ++j) {
-                uint32_t top = 0;
-                int be = 0x7fffffff;
-#pragma unroll
-                for (int i = 0; i < PER; ++i)
-                    if (key[i] > top) {                                    // ascending experts: the first maximum wins
-                        top = key[i];
-                        be = PER * lane + i;
-                    }
-                const uint32_t most = __reduce_max_sync(0xffffffffu, top);
-                if (!most) break;                                          // no other expert can be chosen
-                const int e = (int)__reduce_min_sync(0xffffffffu, top == most ? (unsigned)be : 0x7fffffffu);
-                const float v = key_value(most);
-                if (!exact && j > 0 && v > -INFINITY && prev - v <= near0 + near1 * (fabsf(prev) + fabsf(v))) {
-                    if (lane == 0) mark(prev_e), mark(e);
-                    if (j == g.k)                                          // whatever could displace the last choice, and a little more
-#pragma unroll
-                        for (int i = 0; i < PER; ++i)
-                            if (key[i] && key_value(key[i]) >= v - near0 - 2.f * near1 * fabsf(v)) mark(PER * lane + i);
-                }
-                prev = v;
-                prev_e = e;
-                if (j == lane) mine = e;
-#pragma unroll
-                for (int i = 0; i < PER; ++i)
-                    if (PER * lane + i == e) key[i] = 0;
-            }
-            if (!__any_sync(0xffffffffu, marked)) {
+        } else if (mode == GATE_EXACT) {                                   // too many candidates for a lane each
+            marked = true;
+            stage = GATE_ALL;
+        } else {                                                           // many equal values, or few logits that are not -infinity
+            int at = -1;
+            marked = choose_rounds(g, room.todo, balance ? room.c : room.z, kept, near0, near1, lane, at);
+            if (!marked) {
                 float s;
-                if (choice_weight(g, room.z[mine], lane < g.k, mx, sum, s)) {
-                    if (lane < g.k) {
-                        ids[lane] = mine;
+                if (choice_weight(g, room.z[max(at, 0)], at >= 0, mx, sum, s)) {
+                    if (at >= 0) {
+                        ids[lane] = at;
                         weights[lane] = s;
                     }
                     return false;
@@ -496,29 +545,26 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
 
 // A marked expert's logit: from z64, or z itself where that is exact (z64 null).
 __device__ __forceinline__ double marked_logit(const double* z64, const float* z, int e) { return z64 ? z64[e] : (double)z[e]; }
-// The groups kept, from the exact logits of the marked experts, for choose_fast to go on from there; v [E]: room.
+// The groups kept, from the exact logits of the marked experts, for choose_fast to go on from there; v [E]: room, may be z64.
 template <int PER>
 static __device__ __noinline__ void choose_groups(const GateArgs& g, ChoiceRoom<PER>& room, const double* z64, double* v, int lane) {
-    float* z = room.z;
-    const float* c = room.c;
-    uint32_t* todo = room.todo;
     const bool by_score = g.balance || g.top2;
     float mx = -INFINITY, sum = 0.f;
-    if (!g.sigmoid && by_score) {                                          // as choose_fast: a common factor of all
-        for (int e = lane; e < g.E; e += 32) mx = fmaxf(mx, z[e]);
+    if (!g.sigmoid && by_score) {                                          // a common factor of all
+        for (int e = lane; e < g.E; e += 32) mx = fmaxf(mx, room.z[e]);
         mx = warp_max(mx);
-        for (int e = lane; e < g.E; e += 32) sum += expf(z[e] - mx);
+        for (int e = lane; e < g.E; e += 32) sum += expf(room.z[e] - mx);
         sum = warp_sum_f32(sum);
     }
-    for (int i = 0; i < PER; ++i) {
-        const int e = lane + 32 * i;
-        if (e >= g.E) break;
-        double x = by_score ? (double)c[e] : (double)z[e];
-        if (todo[i] >> lane & 1u) {
-            x = marked_logit(z64, z, e);
-            z[e] = (float)x;
-            if (by_score && x > -INFINITY)
-                x = (g.sigmoid ? 1.0 / (1.0 + exp(-x)) : exp(x - (double)mx) / (double)sum) + (g.balance ? (double)g.balance[e] : 0.0);
+    for (int e = lane; e < g.E; e += 32) {
+        const bool m = room.todo[e >> 5] >> (e & 31) & 1u;
+        double x = m ? marked_logit(z64, room.z, e) : (double)room.z[e];
+        if (by_score && x > -INFINITY) {
+            if (m)
+                x = g.sigmoid ? 1.0 / (1.0 + exp(-x)) : exp(x - (double)mx) / (double)sum;
+            else
+                x = (double)(g.sigmoid ? quick_sigmoid((float)x) : expf((float)x - mx) / sum);
+            if (g.balance) x += (double)g.balance[e];
         }
         v[e] = x;
     }
@@ -526,134 +572,25 @@ static __device__ __noinline__ void choose_groups(const GateArgs& g, ChoiceRoom<
     double a, b;
     two_largest(g, v, lane, a, b);
     const unsigned kept = kept_groups(g, g.top2 && b > -INFINITY ? a + b : a, lane);
-    if (lane == 0) todo[kTodoKept] = kept;
+    if (lane == 0) room.todo[kTodoKept] = kept;
     __syncwarp();
 }
 
-// The experts chosen again by one warp, from the exact logits of the marked ones.  What was not marked is far enough from everything
-// else to be ordered by its binary32 value.  False (a softmax with a bias only): p_e = exp(z_e - mx) / sum with a sum of logits that are off by dz
-// leaves c_a - c_b off by dz |p_a - p_b|, and that is not enough here.
+// After choose_fast's `true`, the marked logits being in z64 (room for all): the mode in which it goes on, or -1: the token is done.  The
+// logits in `room` are brought up to date.
 template <int PER>
-static __device__ __noinline__ bool choose_again(const GateArgs& g, ChoiceRoom<PER>& room, const double* z64, float dz, int lane, int32_t* ids, float* weights) {
-    float* z = room.z;
-    const float* c = room.c;
-    const uint32_t* todo = room.todo;
-    const bool grouped = g.top_groups < g.G, soft = !g.sigmoid && g.balance;
-    const unsigned kept = todo[kTodoKept];
-    unsigned long long key[PER];
-    float mx = -INFINITY, sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-        if (lane + 32 * i < g.E) mx = fmaxf(mx, z[lane + 32 * i]);
-    mx = warp_max(mx);
-    if (!g.sigmoid && (soft || !g.renorm)) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (lane + 32 * i < g.E) sum += expf(z[lane + 32 * i] - mx);
-        sum = warp_sum_f32(sum);
-    }
-    unsigned marked = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {                                        // lane l: experts l, l + 32, ...
-        const int e = lane + 32 * i;
-        key[i] = 0;
-        if (e < g.E) {
-            double v = g.balance ? (double)c[e] : (double)z[e];
-            if (todo[i] >> lane & 1u) {
-                const double x = marked_logit(z64, z, e);
-                v = x;
-                if (g.balance)
-                    v = x == -INFINITY ? x : (g.sigmoid ? 1.0 / (1.0 + exp(-x)) : exp(x - (double)mx) / (double)sum) + (double)g.balance[e];
-                z[e] = (float)x;
-                marked |= 1u << i;
-            }
-            if (!grouped || in_kept(g, kept, e)) key[i] = order_key(v);
-        }
-    }
-    int mine = 0;
-    double last = 0.0, last_p = 0.0;
-    bool last_marked = false;
-    for (int j = 0; j < g.k + (soft ? g.E : 0); ++j) {
-        unsigned long long best = 0;
-        int at = 0;
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (key[i] > best) {
-                best = key[i];
-                at = i;
-            }
-        const unsigned hi = __reduce_max_sync(0xffffffffu, (unsigned)(best >> 32));
-        if (!hi) break;
-        const unsigned lo = __reduce_max_sync(0xffffffffu, (unsigned)(best >> 32) == hi ? (unsigned)best : 0u);
-        const bool is = (unsigned)(best >> 32) == hi && (unsigned)best == lo;
-        const int e = (int)__reduce_min_sync(0xffffffffu, is ? (unsigned)(lane + 32 * at) : 0x7fffffffu);
-        if (soft) {
-            const unsigned long long top = (unsigned long long)hi << 32 | lo;
-            const double v = __longlong_as_double((long long)(top >> 63 ? top & 0x7fffffffffffffffull : ~top)), p = v - (double)g.balance[e];
-            const bool m = todo[e >> 5] >> (e & 31) & 1u;
-            // against the one before, and behind the last choice against that one, as long as the marked ones go on
-            if (j > 0 && m && last_marked && v > -INFINITY && last - v <= 1.1 * (double)dz * fabs(last_p - p) + 1e-12) return false;
-            if (j >= g.k && !m) break;
-            if (j < g.k) {
-                last = v;
-                last_p = p;
-                last_marked = m;
-            }
-        }
-        if (j < g.k && j == lane) mine = e;
-        if (lane == (e & 31))
-#pragma unroll
-            for (int i = 0; i < PER; ++i)
-                if (i == e >> 5) key[i] = 0;
-    }
-    __syncwarp();
-    float s;
-    const bool fits = choice_weight(g, z[mine], lane < g.k, mx, sum, s);
-    if (lane < g.k) {
-        ids[lane] = mine;
-        weights[lane] = s;
-    }
-    if (fits) return true;
-    // sigmoids of which nothing is left in binary32
-    const double x = lane < g.k ? (double)z[mine] : -INFINITY, d = 1.0 / (1.0 + exp(-x)), total = warp_sum_f64(lane < g.k ? d : 0.0);
-    if (lane < g.k) weights[lane] = total > 0.0 ? (float)(d / total * (double)g.scale) : 0.f;
-    return true;
-}
-
-// The choice values of a token whose logits are back in `room` (as choose_fast leaves them).
-template <int PER>
-static __device__ __noinline__ void choice_values(const GateArgs& g, ChoiceRoom<PER>& room, const float* balance, int lane) {
-    if (!balance && !(g.top_groups < g.G && g.top2)) return;
-    float mx = -INFINITY, sum = 0.f;
-    if (!g.sigmoid) {
-        for (int e = lane; e < g.E; e += 32) mx = fmaxf(mx, room.z[e]);
-        mx = warp_max(mx);
-        for (int e = lane; e < g.E; e += 32) sum += expf(room.z[e] - mx);
-        sum = warp_sum_f32(sum);
-    }
-    for (int e = lane; e < g.E; e += 32) {
-        const float v = room.z[e], s = g.sigmoid ? quick_sigmoid(v) : expf(v - mx) / sum;
-        room.c[e] = v == -INFINITY ? v : s + (balance ? balance[e] : 0.f);
-    }
-    __syncwarp();
-}
-// A step on from choose_fast's `true`, the marked logits being in z64 (room for all): true, and the token is done; or false, and todo says
-// which logits come next.
-template <int PER>
-static __device__ __noinline__ bool resolve(const GateArgs& g, ChoiceRoom<PER>& room, const float* balance, double* z64, float dz, float rel, int lane,
-                                        int32_t* ids, float* weights) {
+__device__ __forceinline__ int go_on(const GateArgs& g, ChoiceRoom<PER>& room, double* z64, int lane, int32_t* ids, float* weights) {
     const uint32_t stage = room.todo[kTodoStage];
-    if (stage == GATE_GROUPS) {
-        choose_groups<PER>(g, room, z64, z64, lane);
-        return !choose_fast<PER>(g, room, balance, dz, rel, lane, true, ids, weights);
-    }
     if (stage == GATE_ALL) {
         choose_exact(g, z64, reinterpret_cast<unsigned long long*>(room.z), lane, ids, weights);       // z and c
-        return true;
+        return -1;
     }
-    if (choose_again<PER>(g, room, z64, dz, lane, ids, weights)) return true;
-    choose_all<PER>(g, room, lane);
-    return false;
+    for (int b = 0; 32 * b < g.E; ++b)
+        if (room.todo[b] >> lane & 1u) room.z[32 * b + lane] = (float)z64[32 * b + lane];
+    __syncwarp();
+    if (stage == GATE_EXPERTS) return GATE_EXACT;
+    choose_groups<PER>(g, room, z64, z64, lane);
+    return GATE_DECIDED;
 }
 
 // ---- what the kernels share --------------------------------------------------------------------------------------------

@@ -18,7 +18,7 @@ namespace exmoe {
 
 namespace {
 
-constexpr int kTokens = 128, kStages = 4, kChain = 1, kDrainWarps = 16, kThreads = 32 * (4 + kDrainWarps);
+constexpr int kTokens = 128, kStages = 4, kChain = 2, kDrainWarps = 16, kThreads = 32 * (4 + kDrainWarps), kPad = 4;
 constexpr int kRowBytes = 128;                                             // 64 elements
 __device__ int g_gate_status;                                              // sticky: EXMOE_ERR_TIMEOUT
 
@@ -136,7 +136,7 @@ struct __align__(1024) Shared {
     union {
         unsigned char ring[kStages][kStage];                               // weights, then tokens; rows of 128 bytes, swizzled
         struct {
-            float part[kTokens][MT * 128];                                 // this CTA's part of the logits, read by the cluster
+            float part[kTokens][MT * 128 + kPad];                          // this CTA's part of the logits, read by the cluster; rows four banks apart
             Warp<PER> warp[kDrainWarps];
         } s;
     };
@@ -157,7 +157,7 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                const __nv_bfloat16* __restrict__ w_router, const float* __restrict__ bias, const float* addend, int T, int H,
                const __grid_constant__ GateArgs g, int CL, int32_t* ids, float* weights) {
     using S = Shared<MT, PER>;
-    constexpr int COLS = MT * kTokens / 4;                  // accumulator columns of a drain warp: a quarter of them, on its 32 lanes
+    constexpr int COLS = MT * 128 / 4;                      // accumulator columns of a drain warp: a quarter of them, on its 32 lanes
     extern __shared__ unsigned char raw[];
     S& sm = *reinterpret_cast<S*>(raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u));
     const int tid = threadIdx.x, lane = tid & 31, warp = warp_uniform(tid >> 5);
@@ -192,12 +192,12 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
 #pragma unroll
     for (int i = 0; i < COLS; ++i) acc[i] = 0.f;
     const int d = warp - 4, quarter = warp & 3;                            // drain warps: d of kDrainWarps
-    const int mt = MT == 2 ? d >> 3 : 0, col0 = (d >> 2) * COLS % kTokens; // experts mt * 128 + 32 quarter + lane, tokens col0 ..
+    const int col0 = (d >> 2) * COLS;                                      // token 32 quarter + lane, experts col0 ..
     bool ok = true;
     if (warp == 0) {
         // The ring unrolled, so that the MMAs' operands are constants away from two descriptors, and the next stage's barrier looked at
         // before this stage's MMAs: what stands between two MMAs is time that the tensor pipe may run dry.
-        constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(kTokens >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);
+constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(MT * 128 >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);   // N: experts
         static_assert(kStages % (2 * kChain) == 0, "a turn of the ring leaves off where it began");
         constexpr int kTurns = kStages / (2 * kChain);                     // of the two accumulators in a turn of the ring
         const uint64_t dw0 = make_desc_b(smem_u32(sm.ring[0])), dx0 = make_desc_b(smem_u32(sm.ring[0]) + MT * 128 * kRowBytes);
@@ -220,11 +220,9 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                 const bool seen = i0 + s + 1 < n && mbar_look_at(full + 8 * next, next ? turn : turn ^ 1);
                 if (elect_one()) {
 #pragma unroll
-                    for (int m = 0; m < MT; ++m)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)                        // K = 16: 32 bytes on
-                            mma_f16(tmem + (buf * MT + m) * kTokens, dw0 + (uint64_t)(s * S::kStage + m * 128 * kRowBytes + 32 * j >> 4),
-                                    dx0 + (uint64_t)(s * S::kStage + 32 * j >> 4), idesc, j > 0 || s % kChain > 0);
+                    for (int j = 0; j < 4; ++j)                            // K = 16: 32 bytes on
+                        mma_f16(tmem + buf * MT * 128, dx0 + (uint64_t)(s * S::kStage + 32 * j >> 4), dw0 + (uint64_t)(s * S::kStage + 32 * j >> 4), idesc,
+                                j > 0 || s % kChain > 0);
                     tc_commit_at(empty + 8 * s);
                     if (s % kChain == kChain - 1 || i0 + s == n - 1) tc_commit_at(acc_full + 8 * buf);
                 }
@@ -279,7 +277,7 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
             ok = mbar_wait_warp(acc_full + 8 * buf, (c >> 1) & 1, abort_flag, &g_gate_status);
             if (!ok) break;
             tc_fence_after();
-            const uint32_t at = tmem + ((uint32_t)(32 * quarter) << 16) + (buf * MT + mt) * kTokens + col0;
+            const uint32_t at = tmem + ((uint32_t)(32 * quarter) << 16) + buf * MT * 128 + col0;
 #pragma unroll
             for (int k = 0; k < COLS; k += 16) {
                 uint32_t r[16];
@@ -304,7 +302,8 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * MT * kTokens));
     if (warp >= 4) {
 #pragma unroll
-        for (int i = 0; i < COLS; ++i) sm.s.part[col0 + i][mt * 128 + 32 * quarter + lane] = acc[i];
+        for (int i = 0; i < COLS; i += 4)
+            *reinterpret_cast<float4*>(&sm.s.part[32 * quarter + lane][col0 + i]) = make_float4(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
         float w2 = 0.f;
 #pragma unroll
         for (int i = 0; i < kDrainWarps; ++i) w2 = fmaxf(w2, sm.w2_max[i]);
@@ -319,116 +318,117 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         const float* balance = g.balance ? sm.balance : nullptr;
         const float rel = bias || addend ? kAddedRel : 0.f;
         const int owned = kTokens / CL, chunks = H / 8;
-        for (int i = d; i < owned; i += kDrainWarps) {
-            const int tok = rank * owned + i;
-            const long long t = t0 + tok;
-            if (t >= T) break;
-            float size = 0.f;
-            load_logits<PER>(smem_u32(&sm.s.part[tok][0]), smem_u32(&sm.size[tok]), rank, CL, lane, room.z, size);
-            bool cancelled = false;
+        // Round 0: the CTA's tokens.  The rounds behind it: those that wait, done by the warps together: first the logits, then the choices.
+        for (int round = 0, n_tok = owned;; ++round) {
+            if (round > 0) {
+                for (int f = d; f < n_tok; f += kDrainWarps) {
+                    Waiting& w = sm.waiting[f];
+                    const unsigned es = w.token >= 0 && 32 * lane < g.E ? w.todo[lane] : 0u;   // a word per lane
+                    int before = __popc(es);
 #pragma unroll
-            for (int j = 0; j < PER; ++j) {
-                const int e = lane + 32 * j;
-                float v = -INFINITY;
-                if (e < g.E) {
-                    v = room.z[e];
-                    if (bias) v += bias[e];
-                    if (addend) {
-                        const float before = fabsf(v);
-                        v += addend[t * g.E + e];
-                        cancelled |= before > 2.f * fabsf(v) + 16.f;
+                    for (int m = 1; m < 32; m <<= 1) {
+                        const int o = __shfl_up_sync(0xffffffffu, before, m);
+                        if (lane >= m) before += o;
+                    }
+                    const int total = __shfl_sync(0xffffffffu, before, 31);
+                    int first = 0;
+                    if (lane == 0 && total) first = atomicAdd(&sm.n_items, total);
+                    first = __shfl_sync(0xffffffffu, first, 0);
+                    if (lane == 0) w.first = first + total <= kItems ? first : -1;
+                    int at = first + before - __popc(es);
+                    for (unsigned r = es; r; r &= r - 1, ++at)
+                        if (at < kItems) {
+                            sm.item_expert[at] = (unsigned short)(32 * lane + __ffs(r) - 1);
+                            sm.item_waiting[at] = (unsigned short)f;
+                        }
+                }
+                choosers_sync();
+                const int n_items = min(sm.n_items, kItems);
+                for (int j = d; j < n_items; j += kDrainWarps) {
+                    const long long t = t0 + sm.waiting[sm.item_waiting[j]].token;
+                    const int e = sm.item_expert[j];
+                    const double z = logit_f64(reinterpret_cast<const uint4*>(hidden + t * H), reinterpret_cast<const uint4*>(w_router + (size_t)e * H), chunks, lane);
+                    if (lane == 0) sm.item_z[j] = z + (bias ? (double)bias[e] : 0.0) + (addend ? (double)addend[t * g.E + e] : 0.0);
+                }
+                choosers_sync();
+                if (tid == 128) sm.n_items = 0;
+            }
+            bool open = false;
+            for (int f = d; f < n_tok; f += kDrainWarps) {
+                int tok = rank * owned + f, mode = GATE_NEW;
+                float dz = 0.f;
+                if (round == 0) {
+                    if (t0 + tok >= T) break;
+                    float size = 0.f;
+                    load_logits<PER>(smem_u32(&sm.s.part[tok][0]), smem_u32(&sm.size[tok]), rank, CL, lane, room.z, size);
+                    // the tensor cores' 2 x 21 per stage of a chain, an addition per chain, one per CTA; the norms are short by less than 2 %
+                    dz = 1.02f * (float)(42 * kChain + (blocks + kChain * CL - 1) / (kChain * CL) + 1 + CL) * 0x1p-24f * size + (addend ? 16.f * 0x1p-24f : 0.f);
+                    if (bias || addend || g.E < 32 * PER) {
+                        bool cancelled = false;
+#pragma unroll
+                        for (int j = 0; j < PER; ++j) {
+                            const int e = lane + 32 * j;
+                            float v = -INFINITY;
+                            if (e < g.E) {
+                                v = room.z[e];
+                                if (bias) v += bias[e];
+                                if (addend) {
+                                    const float before = fabsf(v);
+                                    v += addend[(size_t)(t0 + tok) * g.E + e];
+                                    cancelled |= before > 2.f * fabsf(v) + 16.f;
+                                }
+                            }
+                            room.z[e] = v;
+                        }
+                        if (__any_sync(0xffffffffu, cancelled)) dz = INFINITY;
+                        __syncwarp();
                     }
                 }
-                if (bias || addend || e >= g.E) room.z[e] = v;
-            }
-            __syncwarp();
-            // the tensor cores' 2 x 21 per stage of a chain, an addition per chain, one per CTA; the norms are short by less than 2 %
-            float dz = 1.02f * (float)(42 * kChain + (blocks + kChain * CL - 1) / (kChain * CL) + 1 + CL) * 0x1p-24f * size + (addend ? 16.f * 0x1p-24f : 0.f);
-            if (__any_sync(0xffffffffu, cancelled)) dz = INFINITY;
-            int32_t* ids_t = ids + t * g.k;
-            float* weights_t = weights + t * g.k;
-            if (!choose_fast<PER>(g, room, balance, dz, rel, lane, false, ids_t, weights_t)) continue;
-            int at = 0;
-            if (lane == 0) at = atomicAdd(&sm.n_waiting, 1);
-            at = __shfl_sync(0xffffffffu, at, 0);
-            if (lane < kTodoWords) sm.waiting[at].todo[lane] = room.todo[lane];
-            if (lane == 0) {
-                sm.waiting[at].token = tok;
-                sm.waiting[at].dz = dz;
-            }
-#pragma unroll
-            for (int j = 0; j < PER; ++j) sm.s.part[tok][lane + 32 * j] = room.z[lane + 32 * j];
-        }
-        cluster_arrive();                                                  // this warp has read the others' shared memory
-        choosers_sync();
-        // The tokens that wait are done by the warps together: first the logits, then the choices.
-        const int n_waiting = sm.n_waiting;
-        for (bool open = n_waiting > 0; open;) {
-            for (int f = d; f < n_waiting; f += kDrainWarps) {
                 Waiting& w = sm.waiting[f];
-                const unsigned es = w.token >= 0 && 32 * lane < g.E ? w.todo[lane] : 0u;       // a word per lane
-                int before = __popc(es);
-#pragma unroll
-                for (int m = 1; m < 32; m <<= 1) {
-                    const int o = __shfl_up_sync(0xffffffffu, before, m);
-                    if (lane >= m) before += o;
-                }
-                const int total = __shfl_sync(0xffffffffu, before, 31);
-                int first = 0;
-                if (lane == 0 && total) first = atomicAdd(&sm.n_items, total);
-                first = __shfl_sync(0xffffffffu, first, 0);
-                const bool fits = first + total <= kItems;
-                if (lane == 0) w.first = fits ? first : -1;
-                int at = first + before - __popc(es);
-                for (unsigned r = es; r; r &= r - 1, ++at)
-                    if (at < kItems) {
-                        sm.item_expert[at] = (unsigned short)(32 * lane + __ffs(r) - 1);
-                        sm.item_waiting[at] = (unsigned short)f;
+                if (round > 0) {
+                    tok = w.token;
+                    dz = w.dz;
+                    if (tok < 0) continue;
+                    if (w.first < 0) {                                     // no room for its logits: in the next round
+                        open = true;
+                        continue;
                     }
-            }
-            choosers_sync();
-            const int n_items = min(sm.n_items, kItems);
-            for (int j = d; j < n_items; j += kDrainWarps) {
-                const long long t = t0 + sm.waiting[sm.item_waiting[j]].token;
-                const int e = sm.item_expert[j];
-                const double z = logit_f64(reinterpret_cast<const uint4*>(hidden + t * H), reinterpret_cast<const uint4*>(w_router + (size_t)e * H), chunks, lane);
-                if (lane == 0) sm.item_z[j] = z + (bias ? (double)bias[e] : 0.0) + (addend ? (double)addend[t * g.E + e] : 0.0);
-            }
-            choosers_sync();
-            if (tid == 128) sm.n_items = 0;
-            open = false;
-            for (int f = d; f < n_waiting; f += kDrainWarps) {
-                Waiting& w = sm.waiting[f];
-                const int tok = w.token;
-                if (tok < 0) continue;
-                if (w.first < 0) {
-                    open = true;
-                    continue;
-                }
 #pragma unroll
-                for (int j = 0; j < PER; ++j) room.z[lane + 32 * j] = sm.s.part[tok][lane + 32 * j];
-                if (lane < kTodoWords) room.todo[lane] = w.todo[lane];
-                __syncwarp();
-                int j = w.first;
-                for (int b = 0; 32 * b < g.E; ++b)                         // the items are in ascending experts
-                    for (unsigned es = room.todo[b]; es; es &= es - 1, ++j)
-                        if (lane == 0) my.z64[32 * b + __ffs(es) - 1] = sm.item_z[j];
-                choice_values<PER>(g, room, balance, lane);
-                __syncwarp();
-                const long long t = t0 + tok;
-                const bool done = resolve<PER>(g, room, balance, my.z64, w.dz, rel, lane, ids + t * g.k, weights + t * g.k);
-                __syncwarp();
-                if (done) {
-                    if (lane == 0) w.token = -1;
-                } else {
-                    open = true;
-                    if (lane < kTodoWords) w.todo[lane] = room.todo[lane];
+                    for (int j = 0; j < PER; ++j) room.z[lane + 32 * j] = sm.s.part[tok][lane + 32 * j];
+                    if (lane < kTodoWords) room.todo[lane] = w.todo[lane];
+                    __syncwarp();
+                    int j = w.first;
+                    for (int b = 0; 32 * b < g.E; ++b)                     // the items are in ascending experts
+                        for (unsigned es = room.todo[b]; es; es &= es - 1, ++j)
+                            if (lane == 0) my.z64[32 * b + __ffs(es) - 1] = sm.item_z[j];
+                    __syncwarp();
+                }
+                int32_t* ids_t = ids + (size_t)(t0 + tok) * g.k;
+                float* weights_t = weights + (size_t)(t0 + tok) * g.k;
+                if (round > 0) mode = go_on<PER>(g, room, my.z64, lane, ids_t, weights_t);
+                const bool again = mode >= 0 && choose_fast<PER>(g, room, balance, dz, rel, lane, mode, my.z64, ids_t, weights_t);
+                if (again) {                                               // it waits; its logits go back to its row
+                    int at = f;
+                    if (round == 0) {
+                        if (lane == 0) at = atomicAdd(&sm.n_waiting, 1);
+                        at = __shfl_sync(0xffffffffu, at, 0);
+                    }
+                    if (lane < kTodoWords) sm.waiting[at].todo[lane] = room.todo[lane];
+                    if (lane == 0) {
+                        sm.waiting[at].token = tok;
+                        sm.waiting[at].dz = dz;
+                    }
 #pragma unroll
                     for (int j = 0; j < PER; ++j) sm.s.part[tok][lane + 32 * j] = room.z[lane + 32 * j];
+                    open = true;
+                } else if (round > 0 && lane == 0) {
+                    w.token = -1;
                 }
                 __syncwarp();
             }
-            open = choosers_or(open);
+            if (round == 0) cluster_arrive();                              // this warp has read the others' shared memory
+            if (!choosers_or(open)) break;
+            n_tok = sm.n_waiting;
         }
     } else {
         cluster_arrive();
