@@ -445,22 +445,20 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
         // the same for all pairs of candidates: these lie between the two
         const float near = near0 + (from > -INFINITY ? 2.f * near1 * fmaxf(fabsf(largest), fabsf(from)) : 0.f);
         if (!exact && !few) from -= near;
-        int mine = 0, n = 0, at = 0;                                       // candidates of this lane, of all, before this lane's
-        const unsigned lt = (1u << lane) - 1u;
+        unsigned mine = 0;                                                 // candidates of this lane, a bit each
         if (lane_in)
 #pragma unroll
-            for (int i = 0; i < PER; ++i) mine += by[i] >= from;
-        for (int c = 1;; ++c) {
-            const unsigned m = __ballot_sync(0xffffffffu, mine >= c);
+            for (int i = 0; i < PER; ++i) mine |= by[i] >= from ? 1u << i : 0u;
+        int n = 0, at = 0;                                                 // of all, before this lane's
+        const unsigned lt = (1u << lane) - 1u;
+        for (int c = __popc(mine);; --c) {
+            const unsigned m = __ballot_sync(0xffffffffu, c > 0);
             if (!m) break;
             n += __popc(m);
             at += __popc(m & lt);
         }
         if (n >= g.k && n <= 32 && from > -INFINITY) {
-            if (mine)
-#pragma unroll
-                for (int i = 0; i < PER; ++i)
-                    if (by[i] >= from) room.expert[at++] = PER * lane + i; // in ascending experts
+            for (; mine; mine &= mine - 1) room.expert[at++] = PER * lane + __ffs(mine) - 1;       // in ascending experts
             __syncwarp();
             const int e = lane < n ? room.expert[lane] : 0;
             const float v = lane < n ? (balance ? room.c : room.z)[e] : -INFINITY;

@@ -270,9 +270,15 @@ constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(MT *
             }
             __syncwarp();
             if (lane == 0) mbar_arrive_at(empty + 8 * s);
-            x2 += __low2float(a[0]) + __high2float(a[0]) + (__low2float(a[1]) + __high2float(a[1]));
+            // What is lost for the products of one MMA: 2 x 5.25 units of 2^-24 in it and in each that follows in its chain, an addition for each
+            // chain from its own on, one per CTA; with S_j the products of MMA j and loss = sum c_j S_j <= sqrt(sum c_j |x_j|^2) sqrt(sum c_j |w_j|^2).
+            auto cost = [&](int step) {
+                return 10.5f * (float)(4 * kChain - 4 * (i % kChain) - step) + (float)((n - 1) / kChain - c + 1 + CL);
+            };
+            x2 = fmaf(cost(u & 3), __low2float(a[0]) + __high2float(a[0]) + (__low2float(a[1]) + __high2float(a[1])), x2);
 #pragma unroll
-            for (int j = 0; j < WQ; ++j) w2 += __low2float(b[j]) + __high2float(b[j]);
+            for (int j = 0; j < WQ; j += 2)
+                w2 = fmaf(cost((MT == 2 ? 2 * (u & 1) : u & 3) + j / 2), __low2float(b[j]) + __high2float(b[j]) + (__low2float(b[j + 1]) + __high2float(b[j + 1])), w2);
             if (i % kChain < kChain - 1 && i < n - 1) continue;
             ok = mbar_wait_warp(acc_full + 8 * buf, (c >> 1) & 1, abort_flag, &g_gate_status);
             if (!ok) break;
@@ -307,7 +313,7 @@ constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(MT *
         float w2 = 0.f;
 #pragma unroll
         for (int i = 0; i < kDrainWarps; ++i) w2 = fmaxf(w2, sm.w2_max[i]);
-        const int u = tid - 128;                                           // |x| |w| of this part of K, the largest |w| of all experts
+        const int u = tid - 128;                                           // the bound for this part of K, with the largest |w| of all experts
         if ((u & 3) == 0) sm.size[u >> 2] = w2 < INFINITY ? sqrtf(x2) * sqrtf(w2) : INFINITY;
     }
     cluster_arrive();
@@ -361,8 +367,7 @@ constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(MT *
                     if (t0 + tok >= T) break;
                     float size = 0.f;
                     load_logits<PER>(smem_u32(&sm.s.part[tok][0]), smem_u32(&sm.size[tok]), rank, CL, lane, room.z, size);
-                    // the tensor cores' 2 x 21 per stage of a chain, an addition per chain, one per CTA; the norms are short by less than 2 %
-                    dz = 1.02f * (float)(42 * kChain + (blocks + kChain * CL - 1) / (kChain * CL) + 1 + CL) * 0x1p-24f * size + (addend ? 16.f * 0x1p-24f : 0.f);
+                    dz = 1.02f * 0x1p-24f * size + (addend ? 16.f * 0x1p-24f : 0.f);       // the norms are short by less than 2 %
                     if (bias || addend || g.E < 32 * PER) {
                         bool cancelled = false;
 #pragma unroll
