@@ -4,6 +4,7 @@
 
 #include "common.cuh"
 #include "frag.cuh"
+#include "mbar.cuh"
 
 namespace exmoe {
 
@@ -40,19 +41,32 @@ lora_plan_kernel(const int32_t* ids, int T, int n, int32_t* plan) {
     int32_t* perm = plan + LP_WORDS + 4 * plan_tiles(T, n);
     for (int i = tid; i < kPlanWarps * (n + 1); i += kPlanThreads) hist[i] = 0;
     if (tid == 0) bad = 0;
+    grid_dependency_wait();
+    grid_launch_dependents();
     __syncthreads();
     const int per = ((T + kPlanWarps - 1) / kPlanWarps + 31) & ~31;
     const int t_begin = min(T, warp * per), t_end = min(T, t_begin + per);
     int32_t* mine = hist + warp * (n + 1);
-    auto group_of = [&](int t) {
+    constexpr int KEPT = 8;                                                // of a lane's ids in registers: 8192 tokens
+    int kept[KEPT];
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i) kept[i] = t_begin + 32 * i + lane < t_end ? ids[t_begin + 32 * i + lane] : -1;
+    auto group_of = [&](int i, int t) {                                    // lane's token of step i
         if (t >= t_end) return n + 1;
-        const int id = ids[t];
+        int id = 0;
+        if (i < KEPT) {
+#pragma unroll
+            for (int j = 0; j < KEPT; ++j)
+                if (j == i) id = kept[j];
+        } else {
+            id = ids[t];
+        }
+        if (id < -1 || id >= n) bad = 1;
         return id >= 0 && id < n ? id : n;
     };
-    for (int t0 = t_begin; t0 < t_end; t0 += 32) {
-        const int b = group_of(t0 + lane);
+    for (int i = 0, t0 = t_begin; t0 < t_end; ++i, t0 += 32) {
+        const int b = group_of(i, t0 + lane);
         const unsigned same = __match_any_sync(0xffffffffu, b);
-        if (b == n && ids[t0 + lane] != -1) bad = 1;
         if (b <= n && !(same & lt)) mine[b] += __popc(same);
         __syncwarp();
     }
@@ -99,8 +113,8 @@ lora_plan_kernel(const int32_t* ids, int T, int n, int32_t* plan) {
     for (int b = tid; b <= n; b += kPlanThreads)
         for (int i = 0; i * most < count[b]; ++i)
             tiles[tile0[b] + i] = LoraTile{b < n ? b : -1, first[b] + i * most, min(most, count[b] - i * most), 0};
-    for (int t0 = t_begin; t0 < t_end; t0 += 32) {
-        const int b = group_of(t0 + lane);
+    for (int i = 0, t0 = t_begin; t0 < t_end; ++i, t0 += 32) {
+        const int b = group_of(i, t0 + lane);
         const unsigned same = __match_any_sync(0xffffffffu, b);
         if (b <= n) perm[first[b] + mine[b] + __popc(same & lt)] = t0 + lane;
         __syncwarp();
@@ -119,8 +133,9 @@ struct LoraArgs {
     int T, n, K, N, r;
 };
 // whether the plan is one for this call; a wrong one is reported and nothing else is done
-__device__ __forceinline__ bool plan_fits(const LoraArgs& p) {
-    if (p.plan[LP_MAGIC] == kPlanMagic && p.plan[LP_TOKENS] == p.T && p.plan[LP_ADAPTERS] == p.n) return true;
+__device__ __forceinline__ bool plan_fits(const LoraArgs& p, const int4& head) {
+    static_assert(LP_MAGIC == 0 && LP_TOKENS == 1 && LP_ADAPTERS == 2 && LP_TILES == 3, "the header's first words");
+    if (head.x == kPlanMagic && head.y == p.T && head.z == p.n) return true;
     if (blockIdx.x == 0 && threadIdx.x == 0) p.plan[LP_STATUS] = EXMOE_ERR_STATE;
     return false;
 }
@@ -130,12 +145,20 @@ __device__ __forceinline__ void cluster_arrive() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-__device__ __forceinline__ float ld_cluster(uint32_t addr, int rank) {     // a word of another CTA's shared memory
+__device__ __forceinline__ float4 ld_cluster(uint32_t addr, int rank) {    // of another CTA's shared memory
     uint32_t at;
-    float v;
+    float4 v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
     return v;
+}
+
+__device__ __forceinline__ void st_cluster(uint32_t addr, const float4& v, uint32_t bar, int rank) {      // and counts its bytes on that CTA's barrier
+    uint32_t at, b;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(b) : "r"(bar), "r"(rank));
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1,%2,%3,%4}, [%5];"
+                 ::"r"(at), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w), "r"(b) : "memory");
 }
 
 // Eight consecutive columns of a row of base or out.  `vec`: they are 16-byte aligned; `n`: how many of them there are.
@@ -217,12 +240,18 @@ template <> struct Cols<float> {
 template <typename O, int RP, int MB>
 struct LoraSmem {
     static constexpr int TM = 16 * MB, WN = RP / 16, WK = kLoraWarps / WN, PS = RP + 8, VS = RP + 8, SPLIT = sizeof(O) == 4 ? 3 : 2;
-    float sum[TM][RP];                                                     // this CTA's part of v, read by the cluster
+    alignas(16) float sum[TM][RP];                                                     // this CTA's part of v, read by the cluster
     union {
         float part[WK][TM][PS];                                            // the warps' parts
         __nv_bfloat16 v[SPLIT][TM][VS];                                    // v as BF16 numbers, largest first
     };
     long long token[TM];
+    // With few rows a CTA sends its part to the others instead of letting them fetch it: one way across the cluster instead of a
+    // barrier and two ways (T = 1, 16 x 2048 and 2048 x 16: 2800 cycles of 7100 -> see the kernel).
+    static constexpr bool PUSH = MB == 1;
+    alignas(16) float received[PUSH ? 8 : 1][PUSH ? TM : 1][RP];           // by rank
+    uint64_t arrived;
+    int abort_flag;
 };
 template <typename O, int RP, int MB>
 __global__ void __launch_bounds__(kLoraThreads, RP <= 64 ? 2 : 1)
@@ -236,10 +265,23 @@ lora_kernel(LoraArgs p, int CL) {
     grid_dependency_wait();
     grid_launch_dependents();
     const int at = (int)blockIdx.x / CL;
-    if (!plan_fits(p) || at >= p.plan[LP_TILES]) return;                   // the same for a whole cluster
-    const LoraTile tile = reinterpret_cast<const LoraTile*>(p.plan + LP_WORDS)[at];
+    const int4 head = load_behind_wait_cg(reinterpret_cast<const int4*>(p.plan));
+    const int4 entry = load_behind_wait_cg(reinterpret_cast<const int4*>(p.plan + LP_WORDS) + at);      // inside the plan, whatever it holds
+    if (!plan_fits(p, head) || at >= head.w) return;                       // the same for a whole cluster
+    const LoraTile tile{entry.x, entry.y, entry.z, entry.w};
     const int32_t* perm = p.plan + LP_WORDS + 4 * plan_tiles(p.T, p.n);
     const int nrows = tile.nrows, nmb = (nrows + 15) / 16;
+    const bool push = S::PUSH && CL > 1;
+    if (push) {
+        if (tid == 0 && tile.adapter >= 0) {
+            sm.abort_flag = 0;
+            mbar_init(&sm.arrived, 1);
+            asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+            mbar_expect_tx(&sm.arrived, CL * TM * RP * 4);
+        }
+        __syncthreads();
+        cluster_arrive();                                                  // this CTA can be sent to
+    }
     if (tid < TM) sm.token[tid] = perm[tile.row0 + min(tid, nrows - 1)];   // rows behind the last repeat it; they are not stored
     __syncthreads();
     const int n_blocks = (p.N + 31) / 32;
@@ -331,13 +373,29 @@ lora_kernel(LoraArgs p, int CL) {
     }
     __syncthreads();
     const int used = min(TM, 16 * nmb) * RP;
-    for (int i = tid; i < used; i += kLoraThreads) {
-        float s = 0.f;
+    for (int i = 4 * tid; i < used; i += 4 * kLoraThreads) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < WK; ++w) s += sm.part[w][i / RP][i % RP];
-        sm.sum[i / RP][i % RP] = s;
+        for (int w = 0; w < WK; ++w) {
+            const float4 o = *reinterpret_cast<const float4*>(&sm.part[w][i / RP][i % RP]);
+            v.x += o.x;
+            v.y += o.y;
+            v.z += o.z;
+            v.w += o.w;
+        }
+        *reinterpret_cast<float4*>(&sm.sum[0][0] + i) = v;
     }
-    if (CL > 1) cluster_arrive(); else __syncthreads();
+    if (push) {
+        cluster_wait();
+        for (int i = 4 * tid; i < used; i += 4 * kLoraThreads) {
+            const float4 v = *reinterpret_cast<const float4*>(&sm.sum[0][0] + i);        // its own
+            for (int r = 0; r < CL; ++r) st_cluster(smem_u32(&sm.received[S::PUSH ? rank : 0][0][0]) + 4 * i, v, smem_u32(&sm.arrived), r);
+        }
+    } else if (CL > 1) {
+        cluster_arrive();
+    } else {
+        __syncthreads();
+    }
     // in flight meanwhile: what the first columns need
     const float scale = p.scale[tile.adapter];
     constexpr int KB = RP / 16;
@@ -359,24 +417,46 @@ lora_kernel(LoraArgs p, int CL) {
         load_b(nb);
         load_base(nb);
     }
-    if (CL > 1) cluster_wait();
-    for (int i = tid; i < used; i += kLoraThreads) {
-        float v = 0.f;
-        if (CL > 1) {
-            const uint32_t addr = (uint32_t)__cvta_generic_to_shared(&sm.sum[0][0]) + 4 * i;
-            for (int r = 0; r < CL; ++r) v += ld_cluster(addr, r);
-        } else {
-            v = sm.sum[i / RP][i % RP];
+    if (push) {
+        // A peer that does not send (it never does not) would leave this call's rows unwritten and the plan's status at EXMOE_ERR_TIMEOUT.
+        if (!__syncthreads_and(mbar_wait(&sm.arrived, 0, &sm.abort_flag, p.plan + LP_STATUS))) {
+            cluster_arrive();                                              // nor may this CTA end while it can be sent to
+            cluster_wait();
+            return;
         }
+    } else if (CL > 1) {
+        cluster_wait();
+    }
+    for (int i = 4 * tid; i < used; i += 4 * kLoraThreads) {
+        float4 from[8];
+        const uint32_t addr = (uint32_t)__cvta_generic_to_shared(&sm.sum[0][0]) + 4 * i;
+#pragma unroll
+        for (int r = 0; r < 8; ++r)                                        // all in flight at once
+            if (r < CL)
+                from[r] = push ? *reinterpret_cast<const float4*>(&sm.received[S::PUSH ? r : 0][0][0] + i)
+                               : CL > 1 ? ld_cluster(addr, r) : *reinterpret_cast<const float4*>(&sm.sum[0][0] + i);
+        float v[4] = {from[0].x, from[0].y, from[0].z, from[0].w};
+#pragma unroll
+        for (int r = 1; r < 8; ++r)
+            if (r < CL) {
+                v[0] += from[r].x;
+                v[1] += from[r].y;
+                v[2] += from[r].z;
+                v[3] += from[r].w;
+            }
 #pragma unroll
         for (int n = 0; n < S::SPLIT; ++n) {
-            const __nv_bfloat16 h = __float2bfloat16(v);
-            sm.v[n][i / RP][i % RP] = h;
-            const float f = __bfloat162float(h);
-            v = fabsf(f) < INFINITY ? v - f : 0.f;                         // an infinity or NaN is all in the first
+            __nv_bfloat16 h[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                h[j] = __float2bfloat16(v[j]);
+                const float f = __bfloat162float(h[j]);
+                v[j] = fabsf(f) < INFINITY ? v[j] - f : 0.f;               // an infinity or NaN is all in the first
+            }
+            *reinterpret_cast<uint2*>(&sm.v[n][i / RP][i % RP]) = *reinterpret_cast<const uint2*>(h);
         }
     }
-    if (CL > 1) cluster_arrive();                                          // this CTA has read the others' shared memory
+    if (CL > 1 && !push) cluster_arrive();                                 // this CTA has read the others' shared memory
     __syncthreads();
     while (nb < n_blocks) {
         const int col = 32 * nb + 8 * c;
@@ -408,7 +488,7 @@ lora_kernel(LoraArgs p, int CL) {
             load_base(nb);
         }
     }
-    if (CL > 1) cluster_wait();
+    if (CL > 1 && !push) cluster_wait();
 }
 
 template <typename O, int RP, int MB>
@@ -491,8 +571,23 @@ extern "C" int exmoe_lora_plan(const int32_t* adapter_ids, int T, int num_adapte
     const size_t smem = 4 * (size_t)(kPlanWarps + 3) * (num_adapters + 1);
     static SmemOnce once;
     if (!allow_smem(lora_plan_kernel, 4 * (kPlanWarps + 3) * (kMaxAdapters + 1), once)) return EXMOE_ERR_CUDA;
-    lora_plan_kernel<<<1, kPlanThreads, smem, (cudaStream_t)stream>>>(adapter_ids, T, num_adapters, (int32_t*)plan);
-    if (cudaGetLastError() != cudaSuccess) return EXMOE_ERR_CUDA;
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = dim3(1);
+    lc.blockDim = dim3(kPlanThreads);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = (cudaStream_t)stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 1;
+#ifdef EXMOE_DISABLE_PDL
+    lc.numAttrs = 0;
+#endif
+    if (cudaLaunchKernelEx(&lc, lora_plan_kernel, adapter_ids, T, num_adapters, (int32_t*)plan) != cudaSuccess) {
+        cudaGetLastError();
+        return EXMOE_ERR_CUDA;
+    }
     count_launch();
     return EXMOE_OK;
 }
