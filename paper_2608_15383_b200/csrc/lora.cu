@@ -51,35 +51,54 @@ lora_plan_kernel(const int32_t* ids, int T, int n, int32_t* plan) {
     int kept[KEPT];
 #pragma unroll
     for (int i = 0; i < KEPT; ++i) kept[i] = t_begin + 32 * i + lane < t_end ? ids[t_begin + 32 * i + lane] : -1;
-    auto group_of = [&](int i, int t) {                                    // lane's token of step i
+    auto group_of = [&](int id, int t) {
         if (t >= t_end) return n + 1;
-        int id = 0;
-        if (i < KEPT) {
-#pragma unroll
-            for (int j = 0; j < KEPT; ++j)
-                if (j == i) id = kept[j];
-        } else {
-            id = ids[t];
-        }
         if (id < -1 || id >= n) bad = 1;
         return id >= 0 && id < n ? id : n;
     };
-    for (int i = 0, t0 = t_begin; t0 < t_end; ++i, t0 += 32) {
-        const int b = group_of(i, t0 + lane);
-        const unsigned same = __match_any_sync(0xffffffffu, b);
-        if (b <= n && !(same & lt)) mine[b] += __popc(same);
-        __syncwarp();
-    }
-    __syncthreads();
-    for (int b = tid; b <= n; b += kPlanThreads) {
-        int run = 0;
-        for (int w = 0; w < kPlanWarps; ++w) {
-            const int c = hist[w * (n + 1) + b];
-            hist[w * (n + 1) + b] = run;
-            run += c;
+    // Steps of 32 tokens.  Mostly all are of one adapter, where requests are long: then nothing is to be matched.
+    auto count_step = [&](int id, int t0) {
+        const int b = group_of(id, t0 + lane);
+        if (__all_sync(0xffffffffu, b == __shfl_sync(0xffffffffu, b, 0))) {
+            if (lane == 0) mine[b] += 32;
+        } else {
+            const unsigned same = __match_any_sync(0xffffffffu, b);
+            if (b <= n && !(same & lt)) mine[b] += __popc(same);
         }
-        count[b] = run;
+        __syncwarp();
+    };
+    auto place_step = [&](int id, int t0, int32_t* perm, const int32_t* first) {
+        const int b = group_of(id, t0 + lane);
+        if (__all_sync(0xffffffffu, b == __shfl_sync(0xffffffffu, b, 0))) {
+            const int at = mine[b];
+            perm[first[b] + at + lane] = t0 + lane;
+            __syncwarp();
+            if (lane == 0) mine[b] = at + 32;
+        } else {
+            const unsigned same = __match_any_sync(0xffffffffu, b);
+            if (b <= n) perm[first[b] + mine[b] + __popc(same & lt)] = t0 + lane;
+            __syncwarp();
+            if (b <= n && !(same & lt)) mine[b] += __popc(same);
+        }
+        __syncwarp();
+    };
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i)
+        if (t_begin + 32 * i < t_end) count_step(kept[i], t_begin + 32 * i);
+    for (int t0 = t_begin + 32 * KEPT; t0 < t_end; t0 += 32) count_step(t0 + lane < t_end ? ids[t0 + lane] : -1, t0);
+    __syncthreads();
+    for (int b = warp; b <= n; b += kPlanWarps) {                          // lane w: warp w's tokens of group b
+        const int c = hist[lane * (n + 1) + b];
+        int incl = c;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, incl, d);
+            if (lane >= d) incl += o;
+        }
+        hist[lane * (n + 1) + b] = incl - c;
+        if (lane == 31) count[b] = incl;
     }
+    static_assert(kPlanWarps == 32, "a lane per warp");
     __syncthreads();
     if (warp == 0) {
         int rows = 0, nt = 0;
@@ -110,17 +129,13 @@ lora_plan_kernel(const int32_t* ids, int T, int n, int32_t* plan) {
         }
     }
     __syncthreads();
-    for (int b = tid; b <= n; b += kPlanThreads)
-        for (int i = 0; i * most < count[b]; ++i)
+    for (int b = warp; b <= n; b += kPlanWarps)
+        for (int i = lane; i * most < count[b]; i += 32)
             tiles[tile0[b] + i] = LoraTile{b < n ? b : -1, first[b] + i * most, min(most, count[b] - i * most), 0};
-    for (int i = 0, t0 = t_begin; t0 < t_end; ++i, t0 += 32) {
-        const int b = group_of(i, t0 + lane);
-        const unsigned same = __match_any_sync(0xffffffffu, b);
-        if (b <= n) perm[first[b] + mine[b] + __popc(same & lt)] = t0 + lane;
-        __syncwarp();
-        if (b <= n && !(same & lt)) mine[b] += __popc(same);
-        __syncwarp();
-    }
+#pragma unroll
+    for (int i = 0; i < KEPT; ++i)
+        if (t_begin + 32 * i < t_end) place_step(kept[i], t_begin + 32 * i, perm, first);
+    for (int t0 = t_begin + 32 * KEPT; t0 < t_end; t0 += 32) place_step(t0 + lane < t_end ? ids[t0 + lane] : -1, t0, perm, first);
 }
 
 struct LoraArgs {
@@ -145,14 +160,6 @@ __device__ __forceinline__ void cluster_arrive() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-__device__ __forceinline__ float4 ld_cluster(uint32_t addr, int rank) {    // of another CTA's shared memory
-    uint32_t at;
-    float4 v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(at) : "memory");
-    return v;
-}
-
 __device__ __forceinline__ void st_cluster(uint32_t addr, const float4& v, uint32_t bar, int rank) {      // and counts its bytes on that CTA's barrier
     uint32_t at, b;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
@@ -246,16 +253,17 @@ struct LoraSmem {
         __nv_bfloat16 v[SPLIT][TM][VS];                                    // v as BF16 numbers, largest first
     };
     long long token[TM];
-    // With few rows a CTA sends its part to the others instead of letting them fetch it: one way across the cluster instead of a
-    // barrier and two ways (T = 1, 16 x 2048 and 2048 x 16: 2800 cycles of 7100 -> see the kernel).
-    static constexpr bool PUSH = MB == 1;
-    alignas(16) float received[PUSH ? 8 : 1][PUSH ? TM : 1][RP];           // by rank
-    uint64_t arrived;
+    uint64_t arrived[2];
     int abort_flag;
 };
+// The CTAs send each other their parts of v (st.async, counted by the receiver's barrier) instead of fetching them: a way across the cluster instead
+// of a barrier and two ways (one row of rank 16: 1200 cycles of the call's 5600; fetched, 2800 of 7100).  Up to kOneHop numbers for a CTA every CTA sends all of its part
+// to all; beyond, each adds up a CL-th of v and sends the sums (32 rows of rank 64, CL = 8: 64 KB for a CTA otherwise).  What a CTA
+// receives is behind LoraSmem: [rank][TM][RP], or [rank][CL-th] and v.
+constexpr int kOneHop = 4096;
 template <typename O, int RP, int MB>
 __global__ void __launch_bounds__(kLoraThreads, RP <= 64 ? 2 : 1)
-lora_kernel(LoraArgs p, int CL) {
+lora_kernel(LoraArgs p, int CL, bool one_hop) {
     using S = LoraSmem<O, RP, MB>;
     constexpr int TM = S::TM, WN = S::WN, WK = S::WK, U = MB == 1 ? 4 : MB == 2 ? 2 : 1;
     extern __shared__ __align__(16) unsigned char smem[];
@@ -271,16 +279,19 @@ lora_kernel(LoraArgs p, int CL) {
     const LoraTile tile{entry.x, entry.y, entry.z, entry.w};
     const int32_t* perm = p.plan + LP_WORDS + 4 * plan_tiles(p.T, p.n);
     const int nrows = tile.nrows, nmb = (nrows + 15) / 16;
-    const bool push = S::PUSH && CL > 1;
-    if (push) {
+    float* received = reinterpret_cast<float*>(smem + sizeof(S));
+    const int used = 16 * nmb * RP;                                        // numbers of v
+    if (CL > 1) {
         if (tid == 0 && tile.adapter >= 0) {
             sm.abort_flag = 0;
-            mbar_init(&sm.arrived, 1);
+            mbar_init(&sm.arrived[0], 1);
+            mbar_init(&sm.arrived[1], 1);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-            mbar_expect_tx(&sm.arrived, CL * TM * RP * 4);
+            mbar_expect_tx(&sm.arrived[0], (one_hop ? CL : 1) * used * 4);
+            mbar_expect_tx(&sm.arrived[1], used * 4);
         }
         __syncthreads();
-        cluster_arrive();                                                  // this CTA can be sent to
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // this CTA can be sent to
     }
     if (tid < TM) sm.token[tid] = perm[tile.row0 + min(tid, nrows - 1)];   // rows behind the last repeat it; they are not stored
     __syncthreads();
@@ -372,7 +383,6 @@ lora_kernel(LoraArgs p, int CL) {
                     *reinterpret_cast<float2*>(&sm.part[wk][16 * mb + 8 * h + q][16 * wn + 8 * j + 2 * c]) = make_float2(acc[mb][j][2 * h], acc[mb][j][2 * h + 1]);
     }
     __syncthreads();
-    const int used = min(TM, 16 * nmb) * RP;
     for (int i = 4 * tid; i < used; i += 4 * kLoraThreads) {
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
@@ -385,14 +395,18 @@ lora_kernel(LoraArgs p, int CL) {
         }
         *reinterpret_cast<float4*>(&sm.sum[0][0] + i) = v;
     }
-    if (push) {
+    const int slice = used / CL;                                           // two hops: what a CTA adds up
+    if (CL > 1) {
         cluster_wait();
-        for (int i = 4 * tid; i < used; i += 4 * kLoraThreads) {
-            const float4 v = *reinterpret_cast<const float4*>(&sm.sum[0][0] + i);        // its own
-            for (int r = 0; r < CL; ++r) st_cluster(smem_u32(&sm.received[S::PUSH ? rank : 0][0][0]) + 4 * i, v, smem_u32(&sm.arrived), r);
+        for (int i = 4 * tid; i < used; i += 4 * kLoraThreads) {           // its own again
+            const float4 v = *reinterpret_cast<const float4*>(&sm.sum[0][0] + i);
+            if (one_hop) {
+                for (int r = 0; r < CL; ++r) st_cluster(smem_u32(received + rank * TM * RP + i), v, smem_u32(&sm.arrived[0]), (rank + r) & (CL - 1));
+            } else {
+                const int to = i / slice;
+                st_cluster(smem_u32(received + (rank - to) * slice + i), v, smem_u32(&sm.arrived[0]), to);
+            }
         }
-    } else if (CL > 1) {
-        cluster_arrive();
     } else {
         __syncthreads();
     }
@@ -417,33 +431,48 @@ lora_kernel(LoraArgs p, int CL) {
         load_b(nb);
         load_base(nb);
     }
-    if (push) {
-        // A peer that does not send (it never does not) would leave this call's rows unwritten and the plan's status at EXMOE_ERR_TIMEOUT.
-        if (!__syncthreads_and(mbar_wait(&sm.arrived, 0, &sm.abort_flag, p.plan + LP_STATUS))) {
-            cluster_arrive();                                              // nor may this CTA end while it can be sent to
-            cluster_wait();
-            return;
-        }
-    } else if (CL > 1) {
+    // A peer that does not send (none does that) would leave this call's rows unwritten and the plan's status at EXMOE_ERR_TIMEOUT.
+    auto joined = [&](int hop) {
+        if (__syncthreads_and(mbar_wait(&sm.arrived[hop], 0, &sm.abort_flag, p.plan + LP_STATUS))) return true;
+        cluster_arrive();                                                  // nor may this CTA end while it can be sent to
         cluster_wait();
-    }
-    for (int i = 4 * tid; i < used; i += 4 * kLoraThreads) {
-        float4 from[8];
-        const uint32_t addr = (uint32_t)__cvta_generic_to_shared(&sm.sum[0][0]) + 4 * i;
+        return false;
+    };
+    auto add_parts = [&](const float* at, int stride) {                    // by rank; all in flight at once
+        float4 from[8], v;
 #pragma unroll
-        for (int r = 0; r < 8; ++r)                                        // all in flight at once
-            if (r < CL)
-                from[r] = push ? *reinterpret_cast<const float4*>(&sm.received[S::PUSH ? r : 0][0][0] + i)
-                               : CL > 1 ? ld_cluster(addr, r) : *reinterpret_cast<const float4*>(&sm.sum[0][0] + i);
-        float v[4] = {from[0].x, from[0].y, from[0].z, from[0].w};
+        for (int r = 0; r < 8; ++r)
+            if (r < CL) from[r] = *reinterpret_cast<const float4*>(at + r * stride);
+        v = from[0];
 #pragma unroll
         for (int r = 1; r < 8; ++r)
             if (r < CL) {
-                v[0] += from[r].x;
-                v[1] += from[r].y;
-                v[2] += from[r].z;
-                v[3] += from[r].w;
+                v.x += from[r].x;
+                v.y += from[r].y;
+                v.z += from[r].z;
+                v.w += from[r].w;
             }
+        return v;
+    };
+    if (CL > 1) {
+        if (!joined(0)) return;
+        if (!one_hop) {
+            for (int i = 4 * tid; i < slice; i += 4 * kLoraThreads) {
+                const float4 v = add_parts(received + i, slice);
+                for (int r = 0; r < CL; ++r) st_cluster(smem_u32(received + TM * RP + rank * slice + i), v, smem_u32(&sm.arrived[1]), (rank + r) & (CL - 1));
+            }
+            if (!joined(1)) return;
+        }
+    }
+    for (int i = 4 * tid; i < used; i += 4 * kLoraThreads) {
+        float4 all;
+        if (CL == 1)
+            all = *reinterpret_cast<const float4*>(&sm.sum[0][0] + i);
+        else if (one_hop)
+            all = add_parts(received + i, TM * RP);
+        else
+            all = *reinterpret_cast<const float4*>(received + TM * RP + i);
+        float v[4] = {all.x, all.y, all.z, all.w};
 #pragma unroll
         for (int n = 0; n < S::SPLIT; ++n) {
             __nv_bfloat16 h[4];
@@ -456,7 +485,6 @@ lora_kernel(LoraArgs p, int CL) {
             *reinterpret_cast<uint2*>(&sm.v[n][i / RP][i % RP]) = *reinterpret_cast<const uint2*>(h);
         }
     }
-    if (CL > 1 && !push) cluster_arrive();                                 // this CTA has read the others' shared memory
     __syncthreads();
     while (nb < n_blocks) {
         const int col = 32 * nb + 8 * c;
@@ -488,7 +516,6 @@ lora_kernel(LoraArgs p, int CL) {
             load_base(nb);
         }
     }
-    if (CL > 1 && !push) cluster_wait();
 }
 
 template <typename O, int RP, int MB>
@@ -496,11 +523,15 @@ int launch_lora(const LoraArgs& p, int tiles, int CL, cudaStream_t st) {
     using S = LoraSmem<O, RP, MB>;
     static SmemOnce once;
     const auto kern = lora_kernel<O, RP, MB>;
-    if (!allow_smem(kern, (int)sizeof(S), once)) return EXMOE_ERR_CUDA;
+    const bool one_hop = CL * S::TM * RP <= kOneHop;
+    constexpr int most = (int)sizeof(S) + std::max(kOneHop, 2 * S::TM * RP) * 4;
+    static_assert(sizeof(S) % 16 == 0 && most <= (RP <= 64 ? 112 : 224) * 1024, "shared memory, of a second CTA too");
+    if (!allow_smem(kern, most, once)) return EXMOE_ERR_CUDA;
+    const size_t smem = sizeof(S) + (CL == 1 ? 0 : one_hop ? CL : 2) * S::TM * RP * 4;
     cudaLaunchConfig_t lc{};
     lc.gridDim = dim3((unsigned)(tiles * CL));
     lc.blockDim = dim3(kLoraThreads);
-    lc.dynamicSmemBytes = sizeof(S);
+    lc.dynamicSmemBytes = smem;
     lc.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -514,7 +545,7 @@ int launch_lora(const LoraArgs& p, int tiles, int CL, cudaStream_t st) {
     lc.attrs = attr + 1;
     --lc.numAttrs;
 #endif
-    if (cudaLaunchKernelEx(&lc, kern, p, CL) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&lc, kern, p, CL, one_hop) != cudaSuccess) {
         cudaGetLastError();
         return EXMOE_ERR_CUDA;
     }
