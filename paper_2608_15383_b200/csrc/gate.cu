@@ -107,7 +107,8 @@ struct __align__(16) FewRoom {
     float balance[32 * PER];
     double z64[32 * PER];
 };
-constexpr int kFewCluster = 8, kFewFour = 48;                              // four tokens per cluster from here on
+// Four tokens per cluster from here on: 16 tokens one / four 6.6 / 7.0, 32 tokens 9.1 / 7.9 us (64 experts of 2048); 15.7 / 19.1 and 22.3 / 19.1 (256 of 4096).
+constexpr int kFewCluster = 8, kFewFour = 24;
 template <int TB, int PER>
 __global__ void __launch_bounds__(kGateThreads)
 gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w_router, const float* __restrict__ bias, const float* addend, int T, int H,
@@ -258,7 +259,15 @@ int check_gate(const exmoe_shape* shape, const exmoe_gate* gate, int T, GateArgs
     return EXMOE_OK;
 }
 
-constexpr int kManyTokens = 64, kManyExperts = 256;                        // tensor cores from here on, up to there
+// From how many tokens on the tensor cores (at most 256 experts) are faster than four tokens per cluster, by the size of the router's matrix.
+// us, four / tensor cores, means of four batches: 16 experts of d_model 512: 256 tokens 10.0 / 11.1, 384: 13.7 / 11.1.   64 of 2048: 192 13.2 / 14.0,
+// 256: 16.7 / 14.3.   128 of 2048: 128 15.5 / 18.0, 192: 19.8 / 18.8.   256 of 1024: 128 15.3 / 18.5, 192: 21.0 / 18.5.   64 of 4096: 128 14.3 / 16.8,
+// 192: 18.2 / 16.9.   256 of 4096: 64 27.1 / 26.8, 96: 30.2 / 28.7.
+constexpr int kManyExperts = 256;
+constexpr int many_tokens(int E, int H) {
+    const long long n = (long long)E * H;
+    return n <= 1 << 14 ? 288 : n <= 3 << 16 ? 200 : n <= 1 << 19 ? 160 : 72;
+}
 
 // A call's kernels by the number of experts: what choose_fast holds per lane.
 template <int TB, int PER>
@@ -308,7 +317,7 @@ extern "C" int exmoe_route_gated(const exmoe_shape* shape, const exmoe_gate* gat
     g.balance = balance;
     const __nv_bfloat16 *x = (const __nv_bfloat16*)hidden_bf16, *w = (const __nv_bfloat16*)router_bf16;
     cudaStream_t st = (cudaStream_t)stream;
-    if (g.E <= kManyExperts && g.k <= kFastChoices && T >= kManyTokens && H >= 64) return launch_gate_tc(x, w, bias, addend, T, H, g, topk_ids, topk_weights, st);
+    if (g.E <= kManyExperts && g.k <= kFastChoices && T >= many_tokens(g.E, H) && H >= 64) return launch_gate_tc(x, w, bias, addend, T, H, g, topk_ids, topk_weights, st);
     if (g.E <= kFastExperts && g.k <= kFastChoices && sizeof(FewRoom<16>) + 8 * (size_t)H <= (size_t)kGateSmemMax)
         return T < kFewFour ? launch_few<1>(x, w, bias, addend, T, H, g, topk_ids, topk_weights, st) : launch_few<4>(x, w, bias, addend, T, H, g, topk_ids, topk_weights, st);
     static SmemOnce once;
