@@ -95,9 +95,10 @@ gate_logits_kernel(const Z* logits, long long ld, int T, const __grid_constant__
 
 
 // ---- few tokens: a cluster of eight CTAs shares the experts of TB tokens -----------------------------------------------
-// As many warps as a 64-expert router has rows, so that a row's 4 KB are in flight at once.  Logits in binary32: chains of 8 products,
-// H / 256 + 1 chunks of a lane, a tree over the lanes: each addition off by 2^-24 of what is summed, so by
-// (8 + H / 256 + 1 + 5) 2^-24 |x| |w| together; bias and addend are off by 2^-24 of the sum before and of the logit (where the
+// As many warps as a 64-expert router has rows, so that a row's 4 KB are in flight at once.  Logits in binary32: chains of four products, two
+// to a chunk, a lane's H / 256 chunks one after another, a tree over the lanes.  Each addition is off by 2^-24 of what is summed, so
+// the products of chunk j count 4 + 1 + (chunks - j) + 5 times: sum c_j S_j <= sqrt(sum c_j |x_j|^2) sqrt(sum c_j |w_j|^2) such units.  Bias and
+// addend are off by 2^-24 of the sum before and of the logit (where the
 // former is larger than twice the latter + 16, all logits are computed again).  They travel through the cluster's shared
 // memory to the CTA that owns the token (i % 8), whose first warp chooses; where that rests on less than the bound, its warps
 // compute the logits that matter once more in binary64.
@@ -148,14 +149,15 @@ gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w
     }
     __syncthreads();
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");  // every CTA runs: its memory may be written
+    const int nj = (chunks + 31) / 32;
+    auto cost = [&](int j) { return (float)(10 + nj - j); };
     {
-        float x2 = 0.f;                                                    // |x|^2 of the token that this CTA owns
+        float x2 = 0.f;                                                    // sum c |x|^2 of the token that this CTA owns
         if (rank < n_tok)
-            for (int i = tid; i < chunks; i += kGateThreads) x2 += square8(xs[(size_t)rank * chunks + i]);
+            for (int i = tid; i < chunks; i += kGateThreads) x2 = fmaf(cost(i >> 5), square8(xs[(size_t)rank * chunks + i]), x2);
         x2 = warp_sum_f32(x2);
         if (lane == 0) x2_of[warp] = x2;
     }
-    const int nj = (chunks + 31) / 32;
     bool joined = false;
     float w2_top = 0.f;
     for (int e = gw; e < g.E; e += kFewCluster * kGateWarps) {
@@ -170,7 +172,7 @@ gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w
                 const int i = lane + 32 * (j0 + j);
                 float w[8];
                 unpack8(raw[j], w);
-                w2 += dot8(w, w);
+                w2 = fmaf(cost(j0 + j), dot8(w, w), w2);
 #pragma unroll
                 for (int t = 0; t < TB; ++t) {
                     float x[8];
@@ -213,7 +215,7 @@ gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w
 #pragma unroll
         for (int i = 0; i < kGateWarps; ++i) x2 += x2_of[i];
         // the norms come out of binary32 sums, short by less than 1 %
-        dz = 1.01f * (float)(14 + (H + 255) / 256) * 0x1p-24f * sqrtf(x2) * sqrtf(w2) + (addend ? 16.f * 0x1p-24f : 0.f);
+        dz = 1.01f * 0x1p-24f * sqrtf(x2) * sqrtf(w2) + (addend ? 16.f * 0x1p-24f : 0.f);
         if (cancelled) dz = INFINITY;
     }
     const float* balance = g.balance ? sm.balance : nullptr;

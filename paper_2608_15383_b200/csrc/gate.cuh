@@ -603,11 +603,14 @@ __device__ __forceinline__ void unpack8(const uint4& a, float (&x)[8]) {
         x[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
     }
 }
-__device__ __forceinline__ float dot8(const float (&w)[8], const float (&x)[8]) {
-    float d = 0.f;
+__device__ __forceinline__ float dot8(const float (&w)[8], const float (&x)[8]) {        // two chains of four
+    float d = 0.f, e = 0.f;
 #pragma unroll
-    for (int n = 0; n < 8; ++n) d = fmaf(w[n], x[n], d);
-    return d;
+    for (int n = 0; n < 4; ++n) {
+        d = fmaf(w[n], x[n], d);
+        e = fmaf(w[n + 4], x[n + 4], e);
+    }
+    return d + e;
 }
 __device__ __forceinline__ float square8(const uint4& a) {
     float x[8];
