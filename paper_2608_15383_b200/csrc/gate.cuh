@@ -593,6 +593,9 @@ __device__ __forceinline__ int go_on(const GateArgs& g, ChoiceRoom<PER>& room, d
 
 // ---- what the kernels share --------------------------------------------------------------------------------------------
 constexpr int kGateSmemMax = 200 * 1024, kSms = 148;
+// Squares below 2^-149 are lost from a norm; where one has come out so small that this matters, it is taken to be this.  A row of zeros, whose
+// logits are exact, is then told by its logits.
+constexpr float kLeastSquare = 1e-30f, kZeroRow = 1e-12f;
 constexpr float kAddedRel = 3.f * 0x1p-24f;                                // bias and addend: 2^-24 (|sum before| + |z|), with |sum before| <= 2 |z| + 16
 
 __device__ __forceinline__ void unpack8(const uint4& a, float (&x)[8]) {

@@ -314,7 +314,7 @@ constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(MT *
 #pragma unroll
         for (int i = 0; i < kDrainWarps; ++i) w2 = fmaxf(w2, sm.w2_max[i]);
         const int u = tid - 128;                                           // the bound for this part of K, with the largest |w| of all experts
-        if ((u & 3) == 0) sm.size[u >> 2] = w2 < INFINITY ? sqrtf(x2) * sqrtf(w2) : INFINITY;
+        if ((u & 3) == 0) sm.size[u >> 2] = w2 < INFINITY ? sqrtf(fmaxf(x2, kLeastSquare)) * sqrtf(fmaxf(w2, kLeastSquare)) : INFINITY;
     }
     cluster_arrive();
     cluster_wait();
@@ -367,6 +367,11 @@ constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(MT *
                     if (t0 + tok >= T) break;
                     float size = 0.f;
                     load_logits<PER>(smem_u32(&sm.s.part[tok][0]), smem_u32(&sm.size[tok]), rank, CL, lane, room.z, size);
+                    if (size < kZeroRow) {                                 // a row of zeros
+                        bool any = false;
+                        for (int e = lane; e < g.E; e += 32) any |= room.z[e] != 0.f;
+                        if (!__any_sync(0xffffffffu, any)) size = 0.f;
+                    }
                     dz = 1.02f * 0x1p-24f * size + (addend ? 16.f * 0x1p-24f : 0.f);       // the norms are short by less than 2 %
                     if (bias || addend || g.E < 32 * PER) {
                         bool cancelled = false;

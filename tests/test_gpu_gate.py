@@ -92,7 +92,7 @@ def test_near_ties_are_decided_as_in_64_bits(B, g, H, E, k, T):
 
 def test_logits_bias_addend_masks_and_nan(B):
     s = shape(512, 24, 4)
-    for T in (7, 280):
+    for T in (7, 280, 300):                                                # the last on the tensor cores
         hidden, w = synth.hidden_states(s, T, 8), synth.router_weights(s, 9)
         g = torch.Generator().manual_seed(T)
         bias, addend = torch.randn(24, generator=g), torch.randn(T, 24, generator=g)
@@ -192,6 +192,55 @@ def test_streams_and_graphs(B, T):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(ids, want[i][0]) and torch.equal(weights, want[i][1])
+
+
+@pytest.mark.parametrize("H,E,k,T", [(128, 16, 4, 20000), (64, 256, 8, 19100), (72, 100, 7, 1000), (64, 512, 32, 300), (64, 513, 5, 60), (64, 300, 33, 40), (8, 40, 2, 500),
+                                     (4096, 256, 32, 200), (2048, 512, 8, 30), (104, 65, 1, 290)])
+def test_sizes_at_the_edges_of_the_kernels(B, H, E, k, T):
+    """Beyond 148 tiles of 128 tokens, K not a multiple of the stages' 64, the largest numbers of experts and choices of each kernel, one more than these."""
+    s = shape(H, E, k)
+    hidden, w = synth.hidden_states(s, T, 6), synth.router_weights(s, 7)
+    check_gated(B, s, B.Gate(renormalise=True), hidden, w)
+    check_gated(B, s, B.Gate(score="sigmoid"), hidden, w, balance=torch.randn(E, generator=torch.Generator().manual_seed(3)) * 0.02)
+
+
+@pytest.mark.parametrize("T", [3, 40, 300])
+@pytest.mark.parametrize("E", [40, 256])
+def test_every_token_is_a_tie(B, E, T):
+    """Equal rows of the router's matrix, rows of zeros, and rows so small that their squares are lost: ties by the lower id, near-ties in 64 bits."""
+    s = shape(128, E, 8)
+    hidden, w = synth.hidden_states(s, T, 1), synth.router_weights(s, 2)
+    for kw in (dict(), dict(score="sigmoid", num_groups=4, top_groups=2, group_score="top2", renormalise=True)):
+        gate = B.Gate(**kw)
+        for balance in (None, torch.zeros(E)):
+            same = w[:1].repeat(E, 1)
+            ids, _ = check_gated(B, s, gate, hidden, same, balance=balance)
+            assert (ids.cpu() == torch.arange(8)).all()
+            zeros = hidden.clone()
+            zeros[::2] = 0
+            check_gated(B, s, gate, zeros, w, balance=balance)
+            check_gated(B, s, gate, hidden, torch.zeros_like(w), balance=balance)
+    tiny = (hidden.float() * 2.0 ** -66).to(torch.bfloat16)
+    close = w.clone()
+    close[1::2] = close[::2]
+    close[1::2, 5] = (close[::2, 5].float() * (1 + 2.0 ** -7)).to(torch.bfloat16)
+    check_gated(B, s, B.Gate(), tiny, close)
+
+
+def test_calls_at_once_on_several_streams(B):
+    s, gate = shape(512, 64, 8), B.Gate(score="sigmoid", num_groups=4, top_groups=2, renormalise=True)
+    w = synth.router_weights(s, 1).cuda()
+    batches = [synth.hidden_states(s, T, 60 + T).cuda() for T in (1, 30, 300, 700)]
+    want = [B.exmoe_route_gated(s, gate, h, w) for h in batches]
+    streams = [torch.cuda.Stream() for _ in batches]
+    for st in streams:
+        st.wait_stream(torch.cuda.current_stream())
+    for _ in range(5):
+        got = [B.exmoe_route_gated(s, gate, h, w, stream=st) for h, st in zip(batches, streams)]
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    assert B.exmoe_gate_status() == B.EXMOE_OK
 
 
 def test_empty_calls_and_refusals(B):
