@@ -76,6 +76,29 @@ def test_adapters_match_oracle(B, T, n, r, K, N, dtype):
         assert B.exmoe_lora_plan_status(plan) == B.EXMOE_OK
 
 
+@pytest.mark.parametrize("T,n,r,K,N", [(1300, 2, 64, 256, 264), (1500, 3, 128, 392, 200), (1200, 200, 32, 128, 72), (600, 1, 128, 520, 1), (650, 40, 64, 64, 130),
+                                       (8, 1024, 128, 8, 1000), (3000, 5, 24, 1032, 33), (1, 1, 128, 4096, 4096), (5000, 1, 16, 4096, 16)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_every_rank_with_every_tile(B, T, n, r, K, N, dtype):
+    """Tiles of 16, 32 and 64 rows with ranks of each kernel, clusters of one to eight CTAs, K and N of less than a step."""
+    x, a, b, scale, ids, y = inputs(T, n, r, K, N, T + N, dtype)
+    rows = list(range(0, T, 1 + T // 300)) + [T - 1]
+    check(B.exmoe_lora(B.exmoe_lora_plan(ids, n), x, a, b, scale, base=y), x, a, b, scale, ids, y, rows)
+
+
+def test_rows_far_apart(B):
+    """Rows of x, base and out 2^30 bytes apart: offsets beyond 32 bits."""
+    T, n, r, K, N = 5, 2, 8, 64, 40
+    x, a, b, scale, ids, y = inputs(T, n, r, K, N, 4, ids=torch.tensor([1, 0, -1, 1, 0]))
+    big = torch.empty(T << 29, dtype=torch.bfloat16, device="cuda")
+    far = [big[at:].as_strided((T, w), (1 << 29, 1)) for at, w in ((0, K), (64, N), (128, N))]
+    far[0].copy_(x)
+    far[1].copy_(y)
+    far[2].fill_(7.0)
+    out = B.exmoe_lora(B.exmoe_lora_plan(ids, n), far[0], a, b, scale, base=far[1], out=far[2])
+    assert torch.equal(out, B.exmoe_lora(B.exmoe_lora_plan(ids, n), x, a, b, scale, base=y))
+
+
 @pytest.mark.parametrize("T,n,r,K,N", [(3, 2, 16, 256, 136), (40, 6, 8, 512, 77), (150, 2, 64, 1024, 1024), (600, 9, 16, 640, 384)])
 def test_results_depend_on_the_own_row_only(B, T, n, r, K, N):
     """In another order, and with other rows and adapters around them: the same bits.  Alone: the same value."""
