@@ -263,16 +263,16 @@ struct LoraSmem {
 constexpr int kOneHop = 4096;
 template <typename O, int RP, int MB>
 __global__ void __launch_bounds__(kLoraThreads, RP <= 64 ? 2 : 1)
-lora_kernel(LoraArgs p, int CL, bool one_hop) {
+lora_kernel(LoraArgs p, int log_cl, bool one_hop) {
     using S = LoraSmem<O, RP, MB>;
     constexpr int TM = S::TM, WN = S::WN, WK = S::WK, U = MB == 1 ? 4 : MB == 2 ? 2 : 1;
     extern __shared__ __align__(16) unsigned char smem[];
     S& sm = *reinterpret_cast<S*>(smem);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, q = lane >> 2, c = lane & 3;
-    const int rank = (int)blockIdx.x % CL;
+    const int CL = 1 << log_cl, rank = (int)blockIdx.x & (CL - 1);
     grid_dependency_wait();
     grid_launch_dependents();
-    const int at = (int)blockIdx.x / CL;
+    const int at = (int)blockIdx.x >> log_cl;
     const int4 head = load_behind_wait_cg(reinterpret_cast<const int4*>(p.plan));
     const int4 entry = load_behind_wait_cg(reinterpret_cast<const int4*>(p.plan + LP_WORDS) + at);      // inside the plan, whatever it holds
     if (!plan_fits(p, head) || at >= head.w) return;                       // the same for a whole cluster
@@ -323,7 +323,7 @@ lora_kernel(LoraArgs p, int CL, bool one_hop) {
     }
     {   // shrink
         const int wn = warp % WN, wk = warp / WN;
-        const int steps = (p.K + 31) / 32, s_end = (int)((long long)steps * (rank + 1) / CL);
+        const int steps = (p.K + 31) / 32, s_end = steps * (rank + 1) >> log_cl;
         const uint4 *xrow[MB][2], *arow[2];
 #pragma unroll
         for (int mb = 0; mb < MB; ++mb)
@@ -343,7 +343,7 @@ lora_kernel(LoraArgs p, int CL, bool one_hop) {
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[mb][j][i] = 0.f;
-        for (int s0 = (int)((long long)steps * rank / CL) + wk; s0 < s_end; s0 += U * WK) {
+        for (int s0 = (steps * rank >> log_cl) + wk; s0 < s_end; s0 += U * WK) {
             uint4 xv[U][MB][2], av[U][2];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -395,13 +395,15 @@ lora_kernel(LoraArgs p, int CL, bool one_hop) {
         }
         *reinterpret_cast<float4*>(&sm.sum[0][0] + i) = v;
     }
-    const int slice = used / CL;                                           // two hops: what a CTA adds up
+    const int slice = used >> log_cl;                                           // two hops: what a CTA adds up
     if (CL > 1) {
         cluster_wait();
         for (int i = 4 * tid; i < used; i += 4 * kLoraThreads) {           // its own again
             const float4 v = *reinterpret_cast<const float4*>(&sm.sum[0][0] + i);
             if (one_hop) {
-                for (int r = 0; r < CL; ++r) st_cluster(smem_u32(received + rank * TM * RP + i), v, smem_u32(&sm.arrived[0]), (rank + r) & (CL - 1));
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    if (r < CL) st_cluster(smem_u32(received + rank * TM * RP + i), v, smem_u32(&sm.arrived[0]), (rank + r) & (CL - 1));
             } else {
                 const int to = i / slice;
                 st_cluster(smem_u32(received + (rank - to) * slice + i), v, smem_u32(&sm.arrived[0]), to);
@@ -459,7 +461,9 @@ lora_kernel(LoraArgs p, int CL, bool one_hop) {
         if (!one_hop) {
             for (int i = 4 * tid; i < slice; i += 4 * kLoraThreads) {
                 const float4 v = add_parts(received + i, slice);
-                for (int r = 0; r < CL; ++r) st_cluster(smem_u32(received + TM * RP + rank * slice + i), v, smem_u32(&sm.arrived[1]), (rank + r) & (CL - 1));
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    if (r < CL) st_cluster(smem_u32(received + TM * RP + rank * slice + i), v, smem_u32(&sm.arrived[1]), (rank + r) & (CL - 1));
             }
             if (!joined(1)) return;
         }
@@ -545,7 +549,7 @@ int launch_lora(const LoraArgs& p, int tiles, int CL, cudaStream_t st) {
     lc.attrs = attr + 1;
     --lc.numAttrs;
 #endif
-    if (cudaLaunchKernelEx(&lc, kern, p, CL, one_hop) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&lc, kern, p, CL == 8 ? 3 : CL == 4 ? 2 : CL == 2 ? 1 : 0, one_hop) != cudaSuccess) {
         cudaGetLastError();
         return EXMOE_ERR_CUDA;
     }
