@@ -226,7 +226,7 @@ typedef struct {
  *                  (exmoe_lora), noise, or -infinity for experts it may not use
  *   balance      : dev, float32 [E], or NULL
  *   topk_ids     : dev, int32 [T, k]                      topk_weights : dev, float32 [T, k]
- * Limits as exmoe_route's: d_model a multiple of 8, num_experts <= 4096, 2 * d_model + 16 * num_experts <= 204,800 bytes.
+ * Limits as exmoe_route's: d_model a multiple of 8, num_experts <= 4096, 2 * d_model + 16 * num_experts <= 204,800 bytes; and T <= 2^29.
  * Asynchronous on `stream`; allocates nothing; T = 0 is a no-op.  EXMOE_ERR_SHAPE / EXMOE_ERR_ARG before any work is queued. */
 int exmoe_route_gated(const exmoe_shape* shape, const exmoe_gate* gate, const void* hidden_bf16, const void* router_bf16,
                       const float* bias, const float* addend, const float* balance, int T, int32_t* topk_ids,
@@ -239,8 +239,8 @@ int exmoe_gate_logits(const exmoe_shape* shape, const exmoe_gate* gate, const vo
                       const float* balance, int T, int32_t* topk_ids, float* topk_weights, void* stream);
 
 /* Sticky device-side status of exmoe_route_gated on the current device: synchronises it, returns EXMOE_OK, or EXMOE_ERR_TIMEOUT if a
- * bounded wait of the tensor-core form expired since the previous call of this function (the tokens of its cluster were then left
- * unwritten), and clears it. */
+ * bounded wait of the tensor-core form expired since the previous call of this function (what that call wrote is then not to be
+ * used), and clears it. */
 int exmoe_gate_status(void);
 
 /* Low-rank adapters of many requests beside a projection that all of them share (the paper has none; packed int4 weights cannot
@@ -250,8 +250,8 @@ int exmoe_gate_status(void);
  * Products are summed in binary32 and rounded once, to the type of `out`. */
 typedef struct {
     int num_adapters;   /* n, 1 .. 1024 */
-    int d_in;           /* K, a multiple of 8 */
-    int d_out;          /* N */
+    int d_in;           /* K, a multiple of 8, at most 2^30 */
+    int d_out;          /* N, at most 2^30 */
     int rank;           /* r, a multiple of 8, at most 128; adapters of smaller rank are padded with zeros */
 } exmoe_lora_shape;
 
@@ -259,7 +259,7 @@ typedef struct {
  *   adapter_ids : dev, int32 [T], -1: no adapter; any order, any repeats.  Another id outside [0, n) counts as none and is
  *                 reported by exmoe_lora_plan_status
  *   plan        : dev, exmoe_lora_plan_bytes(T, n) bytes, 16-byte aligned, written here
- * Asynchronous on `stream`; a plan of T = 0 tokens is one too. */
+ * Asynchronous on `stream`; a plan of T = 0 tokens is one too; T <= 2^29. */
 int exmoe_lora_plan_bytes(int T, int num_adapters, size_t* bytes);
 int exmoe_lora_plan(const int32_t* adapter_ids, int T, int num_adapters, void* plan, void* stream);
 /* What the device found in a plan's ids or in its use (synchronises the device): EXMOE_OK, EXMOE_ERR_BAD_ADAPTER_ID, or
@@ -268,7 +268,8 @@ int exmoe_lora_plan(const int32_t* adapter_ids, int T, int num_adapters, void* p
 int exmoe_lora_plan_status(const void* plan);
 
 /* One projection's adapters.
- *   plan  : dev, from exmoe_lora_plan for the same T and num_adapters
+ *   plan  : dev, from exmoe_lora_plan for the same T and num_adapters; at least exmoe_lora_plan_bytes(T, num_adapters) bytes
+ *           whatever it was written for
  *   x     : dev, BF16 [T, K], rows ld_x elements apart (a multiple of 8), 16-byte aligned
  *   a, b  : dev, BF16 [n, r, K] and [n, N, r], 16-byte aligned        scale : dev, float32 [n]
  *   base  : dev, [T, N] of `type`, rows ld_base elements apart, or NULL for zeros

@@ -258,6 +258,8 @@ def exmoe_lora_plan(adapter_ids, num_adapters, plan=None, stream=None):
 
 def exmoe_lora_plan_status(plan):
     """EXMOE_OK, EXMOE_ERR_BAD_ADAPTER_ID or EXMOE_ERR_STATE: what the device found in the plan's ids or its use (synchronises)."""
+    if plan.numel() < 16 or plan.device.index != torch.cuda.current_device():      # shorter than any plan's header
+        raise ValueError("plan: need one of exmoe_lora_plan on the current CUDA device")
     return int(lib().exmoe_lora_plan_status(_dev(plan, torch.int32, "plan")))
 
 

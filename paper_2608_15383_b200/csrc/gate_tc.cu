@@ -1,13 +1,22 @@
 // The gate on many tokens: the logits as a GEMM on tcgen05, then the choice, in one kernel.
 //
-// A cluster of CL CTAs takes 128 tokens; each multiplies a CL-th of K: weights of all experts (up to MT x 128 rows, the MMA's M) and
-// tokens (N = 128) come by TMA into a ring of 64-wide stages, and a stage's four MMAs of K = 16 start from zero.  An MMA truncates:
-// every product to 2^-25 of the largest one's (and the accumulator's) binade, the result to 24 bits; four of them one after
-// another lose at most 4 (17 / 4 + 1) units of 2^-23 of S = sum |x_i w_i|, while the 64 MMAs of 1024 elements, each truncating what the
-// ones before have summed, would lose as many times more.  So sixteen warps take every stage's accumulator out of tensor memory, which
-// has two of them, and add it to binary32 sums in registers, behind the MMAs of the next stage; they also add up |x|^2 and |w|^2
-// from the stages' tiles.  The partial logits go to shared memory, the CTA that owns a token adds the CL parts, and a warp makes its
-// choice (gate.cuh), with the logits that decide computed again in binary64 where they are closer than the bound.
+// A cluster of CL CTAs (as many, up to eight, as 148 SMs have room for) takes 128 tokens, the MMA's M; each multiplies a CL-th of K by
+// all experts, its N = MT x 128.  Tokens and weights come by TMA into a ring of kStages 64-wide stages.
+//   Rounding.  An MMA truncates: every product to 2^-25 of the binade of the largest one (or of the accumulator), its result to 24 bits; at
+// most 17 / 4 + 1 = 5.25 units of 2^-23 of the magnitudes summed so far.  In one chain over K, each MMA would lose that much of all that
+// the ones before have summed, H / 16 times.  So only kChain stages (8 MMAs) make a chain that starts from zero; sixteen warps take its
+// accumulator out of tensor memory, which has two of them, and add it to binary32 sums in registers behind the next chain's MMAs.
+// What is left is bounded in the units that decide (`cost` below): the products of an MMA count once for it and each that follows in its
+// chain, and once for every addition behind that, and with weighted norms, summed by the same warps from the stages' tiles, Cauchy's
+// inequality gives dz = 2^-24 sqrt(sum c |x|^2) sqrt(sum c |w|^2).  With chains of one stage the main loop took 50 thousand cycles instead of 40
+// (gate below; twice as many drains), and the bounds of longer ones mark more.
+//   Choice.  The partial logits go to shared memory; the CTA that owns a token (128 / CL each) adds the CL parts, and a warp chooses
+// (gate.cuh).  Where a decision rests on less than the bound, the token waits; behind the others, all sixteen warps compute the logits that
+// matter in binary64, a warp per logit, and its choice goes on.
+//   What bounds it, at 8192 tokens of d_model 4096, 256 experts, 8 of 4 of 8 groups by the two largest, sigmoid with a balance bias (64
+// clusters of two): 64 us replayed from a graph, of 97 thousand cycles per CTA 38 in the main loop, 30 in its 64 tokens' choices, 19 in
+// the near-ties, the rest in start and exchange.  The main loop runs at the rate of shared memory (TMA in, MMAs and norms out: 128 bytes a
+// cycle; the tensor pipe is busy for 15 % of the kernel), the choices at that of instructions.  The bytes alone would take 10.8 us.
 #include <algorithm>
 
 #include "gate.cuh"
@@ -105,6 +114,11 @@ __device__ __forceinline__ void square(__nv_bfloat162& sum, const uint4& v) {
     }
 }
 
+__device__ __forceinline__ void in_flight_end(uint32_t bar, uint32_t parity) {
+    const long long t0 = clock64();
+    while (!mbar_try_at(bar, parity) && clock64() - t0 < kWaitBudget) {}
+}
+
 // the choosing warps' barrier
 __device__ __forceinline__ void choosers_sync() {
     __syncwarp();
@@ -146,7 +160,7 @@ struct __align__(1024) Shared {
     Waiting waiting[kTokens];
     double item_z[kItems];                                                 // logits to compute again
     unsigned short item_expert[kItems], item_waiting[kItems];
-    uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2];
+    uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], drained;
     uint32_t tmem;
     int abort_flag;
 };
@@ -172,6 +186,7 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
             mbar_init(&sm.acc_full[b], 1);
             mbar_init(&sm.acc_empty[b], kDrainWarps);
         }
+        mbar_init(&sm.drained, 1);
         sm.abort_flag = 0;
         sm.n_waiting = sm.n_items = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -197,7 +212,7 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     if (warp == 0) {
         // The ring unrolled, so that the MMAs' operands are constants away from two descriptors, and the next stage's barrier looked at
         // before this stage's MMAs: what stands between two MMAs is time that the tensor pipe may run dry.
-constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(MT * 128 >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);   // N: experts
+        constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(MT * 128 >> 3) << 17) | ((uint32_t)(BM >> 4) << 24);   // N: experts
         static_assert(kStages % (2 * kChain) == 0, "a turn of the ring leaves off where it began");
         constexpr int kTurns = kStages / (2 * kChain);                     // of the two accumulators in a turn of the ring
         const uint64_t dw0 = make_desc_b(smem_u32(sm.ring[0])), dx0 = make_desc_b(smem_u32(sm.ring[0]) + MT * 128 * kRowBytes);
@@ -230,8 +245,14 @@ constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(MT *
                 ready = __all_sync(0xffffffffu, seen);
             }
         }
+        if (!ok) {                                                         // given up: the MMAs in flight end before their operands' memory is used again
+            if (elect_one()) tc_commit_at(smem_u32(&sm.drained));
+            __syncwarp();
+            in_flight_end(smem_u32(&sm.drained), 0);
+        }
     } else if (warp == 1) {
-        for (int i = 0; i < n; ++i) {
+        int i = 0;
+        for (; i < n; ++i) {
             const int s = i % kStages;
             if (i >= kStages) ok = mbar_wait_warp(empty + 8 * s, (i / kStages - 1) & 1, abort_flag, &g_gate_status);
             if (!ok) break;
@@ -242,6 +263,7 @@ constexpr uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(MT *
             }
             __syncwarp();
         }
+        for (int j = max(0, i - kStages); j < i; ++j) in_flight_end(full + 8 * (j % kStages), (j / kStages) & 1);   // and so do the copies
     } else if (warp < 4) {
         for (int e = tid - 64; e < 32 * PER; e += 64) sm.balance[e] = g.balance && e < g.E ? g.balance[e] : 0.f;
     } else {

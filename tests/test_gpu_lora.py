@@ -189,6 +189,11 @@ def test_a_plan_serves_its_own_sizes_only(B):
     assert B.exmoe_lora(empty, x[:0], a, b, scale).shape == (0, 32) and B.exmoe_lora_plan_status(empty) == B.EXMOE_OK
 
 
+def test_status_of_what_is_no_plan_is_refused(B):
+    with pytest.raises(ValueError, match="plan"):
+        B.exmoe_lora_plan_status(torch.zeros(15, dtype=torch.int32, device="cuda"))
+
+
 def test_refusals(B):
     x, a, b, scale, ids, y = inputs(10, 4, 8, 64, 32, 1)
     plan = B.exmoe_lora_plan(ids, 4)

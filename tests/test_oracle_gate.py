@@ -148,6 +148,21 @@ def test_adapter_refusals(B):
         assert lora(base=p + 5 * MB + 128, ld_base=64, out=p + 5 * MB + 128 + shift, ld_out=64, shape=(4, 64, 34, 8)) == B.EXMOE_ERR_ARG, shift
 
 
+def test_sizes_beyond_32_bits_are_refused(B):
+    """Row and column counts whose rounding up or grid would pass 32 bits; nothing is read."""
+    from ctypes import byref, c_size_t
+    L, p, many = B.lib(), 1 << 30, (1 << 29) + 1
+    gate = byref(B.exmoe_gate(0, 1, 1, 0, 0, 1.0))
+    assert L.exmoe_route_gated(byref(B.exmoe_shape(8, 128, 8, 2, 128)), gate, p, p, None, None, None, many, p, p, None) == B.EXMOE_ERR_ARG
+    assert L.exmoe_gate_logits(byref(B.exmoe_shape(0, 0, 8, 2, 0)), gate, p, 0, 8, None, many, p, p, None) == B.EXMOE_ERR_ARG
+    n = c_size_t()
+    assert L.exmoe_lora_plan_bytes(many, 4, byref(n)) == L.exmoe_lora_plan(p, many, 4, p, None) == B.EXMOE_ERR_ARG
+    assert L.exmoe_lora_plan_bytes(many - 1, 1024, byref(n)) == B.EXMOE_OK and n.value == 4 * (16 + 4 * ((many - 1) // 64 + 1025) + many - 1)
+    for shape, T, want in (((1, 8, 8, 8), many, B.EXMOE_ERR_ARG), ((1, (1 << 30) + 8, 8, 8), 1, B.EXMOE_ERR_SHAPE), ((1, 8, (1 << 30) + 1, 8), 1, B.EXMOE_ERR_SHAPE)):
+        ld = max(shape[1:3])
+        assert L.exmoe_lora(byref(B.exmoe_lora_shape(*shape)), p, p, ld, p, p, p, T, None, 0, p + (1 << 40), ld, 1, None) == want, shape
+
+
 def test_binding_refuses_host_tensors(B):
     z = torch.zeros((2, 8))
     shape, g = SimpleNamespace(d_model=64, d_ff=128, num_experts=8, top_k=2), B.Gate()
