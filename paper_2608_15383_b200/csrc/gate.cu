@@ -78,15 +78,18 @@ gate_logits_kernel(const Z* logits, long long ld, int T, const __grid_constant__
         __syncwarp();
         z64 = reinterpret_cast<double*>(mine + sizeof(ChoiceRoom<PER>));
         key = reinterpret_cast<double*>(room.z);                           // z and c
-        for (int mode = GATE_NEW;;) {
-            if (!choose_fast<PER>(g, room, balance, 0.f, 0.f, lane, mode, nullptr, ids + t * g.k, weights + t * g.k)) return;
-            if (room.todo[kTodoStage] == GATE_ALL) break;
-            mode = GATE_EXACT;
-            if (room.todo[kTodoStage] == GATE_GROUPS) {
+        bool all = false;                                                  // everything in binary64 after all
+        for (int mode = GATE_NEW; choose_fast<PER>(g, room, balance, 0.f, 0.f, lane, mode, ids + t * g.k, weights + t * g.k); mode = GATE_DECIDED) {
+            const uint32_t stage = room.todo[kTodoStage];
+            if (stage == GATE_GROUPS) {
                 choose_groups<PER>(g, room, nullptr, z64, lane);
-                mode = GATE_DECIDED;
+                continue;
             }
+            if (stage == GATE_EXPERTS && finish_choice<PER>(g, room, nullptr, 0.f, 0.f, lane, ids + t * g.k, weights + t * g.k)) return;
+            all = true;
+            break;
         }
+        if (!all) return;
         __syncwarp();
     } else {
         if (t >= (size_t)T) return;
@@ -234,7 +237,7 @@ gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w
     int32_t* ids_t = ids + t * g.k;
     float* weights_t = weights + t * g.k;
     for (int mode = GATE_NEW;;) {
-        const bool open = warp == 0 && mode >= 0 && choose_fast<PER>(g, room, balance, dz, rel, lane, mode, sm.z64, ids_t, weights_t);
+        const bool open = warp == 0 && (mode == GATE_WAITS || (mode != GATE_DONE && choose_fast<PER>(g, room, balance, dz, rel, lane, mode, ids_t, weights_t)));
         if (!__syncthreads_or(open)) return;
         int item = 0;
         for (int b = 0; 32 * b < g.E; ++b)
@@ -245,7 +248,7 @@ gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w
                 if (lane == 0) sm.z64[e] = v + (bias ? (double)bias[e] : 0.0) + (addend ? (double)addend[t * g.E + e] : 0.0);
             }
         __syncthreads();
-        if (warp == 0) mode = go_on<PER>(g, room, sm.z64, lane, ids_t, weights_t);
+        if (warp == 0) mode = go_on<PER>(g, room, sm.z64, dz, rel, lane, ids_t, weights_t);
     }
 }
 

@@ -21,7 +21,7 @@ constexpr int kFastExperts = 512, kFastChoices = 32;                       // wh
 // What it leaves where it cannot decide: a bit per expert whose logit decides, the groups kept, and what is to be done with these logits
 constexpr int kTodoKept = kFastExperts / 32, kTodoStage = kTodoKept + 1, kTodoWords = kTodoKept + 2;
 enum { GATE_EXPERTS = 0, GATE_ALL = 1, GATE_GROUPS = 2 };
-enum { GATE_NEW = 0, GATE_DECIDED = 1, GATE_EXACT = 2 };                   // how a choice begins
+enum { GATE_NEW = 0, GATE_DECIDED = 1, GATE_DONE = -1, GATE_WAITS = -2 };  // how a choice begins, and what go_on says besides
 
 // Doubles as integers of the same order: 0 is left for an expert that cannot be chosen, 1 is a NaN, -infinity follows; zeros of both signs are equal.
 __device__ __forceinline__ unsigned long long order_key(double v) {
@@ -160,6 +160,8 @@ __device__ __forceinline__ float sigmoid(float z) {
     const float e = expf(-fabsf(z));
     return (z >= 0.f ? 1.f : e) / (1.f + e);
 }
+// rel: |z| s (1 - s) < 0.23 for a sigmoid; in a softmax logits 100 below the largest have no part
+__device__ __forceinline__ float bound_of(const GateArgs& g, float dz, float rel, float mx) { return dz + (g.sigmoid ? rel : rel * (fabsf(mx) + 100.f)); }
 __device__ __forceinline__ float quick_sigmoid(float z) { return __fdividef(1.f, 1.f + __expf(-z)); }
 // exp(z - top): the rounding of the difference, 2^-24 of it, is put back
 __device__ __forceinline__ float exp_below(float z, float top) {
@@ -199,39 +201,11 @@ static __device__ __noinline__ void mark_from(const GateArgs& g, uint32_t* todo,
     }
     __syncwarp();
 }
-// Candidates (expert e with value v in lanes 0 .. n - 1) before this lane's, the marked ones by their exact logits; the others are far
-// enough from everything to be ordered by v.  -1 in all lanes: that does not decide.  It may not for a softmax with a bias: p_e = exp(z_e -
-// mx) / sum with a sum of logits that are off by dz leaves c_a - c_b off by dz |p_a - p_b|.
-static __device__ __noinline__ int rank_exact(const GateArgs& g, const uint32_t* todo, const float* z, const double* z64, const float* balance, float v, int e,
-                                              int n, float dz, float mx, float sum, int lane) {
-    const bool m = lane < n && (todo[e >> 5] >> (e & 31) & 1u), soft = balance && !g.sigmoid;
-    const double b = balance && lane < n ? (double)balance[e] : 0.0;
-    double w = (double)v;
-    if (m) {
-        const double x = z64 ? z64[e] : (double)z[e];
-        w = x;
-        if (balance) w = x == -INFINITY ? x : (g.sigmoid ? 1.0 / (1.0 + exp(-x)) : exp(x - (double)mx) / (double)sum) + b;
-    }
-    int before = 0;
-    bool unsure = false;
-    for (int j = 0; j < n; ++j) {
-        const double o = __shfl_sync(0xffffffffu, w, j);
-        before += o > w || (o == w && j < lane);
-        if (soft) {
-            const double ob = __shfl_sync(0xffffffffu, b, j);
-            const bool om = __shfl_sync(0xffffffffu, m, j);
-            unsure |= m && om && j != lane && w > -INFINITY && o > -INFINITY && fabs(o - w) <= 1.1 * (double)dz * fabs((o - ob) - (w - b)) + 1e-12;
-        }
-    }
-    return __any_sync(0xffffffffu, unsure && before <= g.k) ? -1 : before;
-}
-// k rounds of arg-max over v [E]: lane j gets the j-th choice (-1: none).  True: near-ties were marked instead.
-static __device__ __noinline__ bool choose_rounds(const GateArgs& g, uint32_t* todo, const float* v, unsigned kept, float near0, float near1, int lane, int& mine) {
+// k rounds of arg-max over v [E]: lane j gets the j-th choice (-1: none).  False: two of them, or the last and the next, are too close.
+static __device__ __noinline__ bool choose_rounds(const GateArgs& g, const float* v, unsigned kept, float near0, float near1, int lane, int& mine) {
     const bool grouped = g.top_groups < g.G, exact = near0 == 0.f;
     unsigned taken = 0;                                                    // of experts lane, lane + 32, ...
-    bool marked = false;
     float prev = 0.f;
-    int prev_e = 0;
     for (int j = 0; j <= g.k; ++j) {
         uint32_t top = 0;
         int be = 0x7fffffff;
@@ -246,25 +220,22 @@ static __device__ __noinline__ bool choose_rounds(const GateArgs& g, uint32_t* t
         if (!most) break;                                                  // no other expert can be chosen
         const int e = (int)__reduce_min_sync(0xffffffffu, top == most ? (unsigned)be : 0x7fffffffu);
         const float x = key_value(most);
-        if (!exact && j > 0 && x > -INFINITY && prev - x <= near0 + near1 * (fabsf(prev) + fabsf(x))) {
-            marked = true;
-            if (lane == 0) {
-                atomicOr(&todo[prev_e >> 5], 1u << (prev_e & 31));
-                atomicOr(&todo[e >> 5], 1u << (e & 31));
-            }
-            if (j == g.k)                                                  // whatever could displace the last choice, and a little more
-                for (int i = 0, o = lane; o < g.E; ++i, o += 32)
-                    if (!(taken >> i & 1u) && (!grouped || in_kept(g, kept, o)) && v[o] >= x - near0 - 2.f * near1 * fabsf(x)) atomicOr(&todo[o >> 5], 1u << (o & 31));
-        }
+        if (!exact && j > 0 && x > -INFINITY && prev - x <= near0 + near1 * (fabsf(prev) + fabsf(x))) return false;
         prev = x;
-        prev_e = e;
         if (j == lane && j < g.k) mine = e;
         if (lane == (e & 31)) taken |= 1u << (e >> 5);
     }
-    __syncwarp();
-    return marked;
+    return true;
 }
 
+// The candidates among which GATE_EXPERTS marks the near-ties, for finish_choice: expert | rank << 9, the largest logit of all, and the sum of
+// the exponentials below it.
+struct Picks {
+    unsigned short at[32];
+    int n;
+    float mx, sum;
+};
+static_assert(kFastExperts <= 512 && kFastChoices <= 32, "a candidate's sixteen bits");
 // What a warp needs in shared memory for a token's choice.
 template <int PER>
 struct __align__(16) ChoiceRoom {
@@ -272,6 +243,7 @@ struct __align__(16) ChoiceRoom {
     float c[32 * PER];                                                     // choice values
     int expert[32];                                                        // candidates
     uint32_t todo[kTodoWords];
+    Picks picks;
 };
 template <int PER>
 __device__ __forceinline__ void load_run(const float* p, float (&v)[PER]) {
@@ -305,14 +277,13 @@ __device__ __forceinline__ void choose_all(const GateArgs& g, ChoiceRoom<PER>& r
 }
 
 // By one warp; lane l holds the PER experts from PER l on; `balance`: g.balance padded to 32 PER, or null; at most kFastChoices choices.
-// `mode`: GATE_NEW; GATE_DECIDED: the groups are those of todo[kTodoKept]; GATE_EXACT: and the exact logits of the experts marked in todo are in z64
-// (or z has them itself, z64 null).  True: nothing is written, and `todo` says what is to be done.
+// `mode`: GATE_NEW; GATE_DECIDED: the groups are those of todo[kTodoKept].  True: nothing is written, and `todo` says what is to be done.
 // The choice itself: the k-th largest of the lanes' largest values is no more than the k-th largest value, so what is not below
 // it (by more than `near`) are all candidates, k and a few more; they go to a lane each, which counts those before its own.  (Instead
 // of k rounds of arg-max, which took twice the instructions.)
 template <int PER>
 __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& room, const float* balance, float dz, float rel, int lane, int mode,
-                                            const double* z64, int32_t* ids, float* weights) {
+                                            int32_t* ids, float* weights) {
     const bool grouped = g.top_groups < g.G, by_score = balance || (grouped && g.top2);
     float by[PER], other[PER];                                             // what orders the experts; scores where these are not it
     load_run<PER>(room.z + PER * lane, by);
@@ -323,8 +294,7 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
         any += by[i];                                                      // a NaN where there is one, or infinities of both signs
     }
     mx = warp_max(mx);
-    // rel: |z| s (1 - s) < 0.23 for a sigmoid; in a softmax logits 100 below the largest have no part
-    const float dzs = dz + (g.sigmoid ? rel : rel * (fabsf(mx) + 100.f));
+    const float dzs = bound_of(g, dz, rel, mx);
     bool odd = __any_sync(0xffffffffu, any != any) || !(fabsf(mx) < INFINITY) || !(dzs <= 0.05f);
     // quick_sigmoid is within 3.5e-7 of the true one (__expf's argument off by 2^-23 |z|, its result by 2^-22 of itself, each times s (1 - s); the quotient
     // by 2^-22 s), a probability (an argument off by 2^-24 of itself, p |argument| < 0.37; up to 25 roundings in exponentials, sum and
@@ -374,7 +344,7 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
     }
     int stage = odd ? GATE_ALL : GATE_EXPERTS;
     unsigned kept = mode == GATE_NEW ? 0xffffffffu : room.todo[kTodoKept];
-    if (mode != GATE_EXACT && lane < kTodoKept) room.todo[lane] = 0;
+    if (lane < kTodoKept) room.todo[lane] = 0;
     __syncwarp();
     bool marked = false;
     if (grouped && mode == GATE_NEW && !odd) {
@@ -464,13 +434,7 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
             const float v = lane < n ? (balance ? room.c : room.z)[e] : -INFINITY;
             int before = 0, close = 0;
             float close_by = near;
-            if (mode == GATE_EXACT) {
-                before = rank_exact(g, room.todo, room.z, z64, balance, v, e, n, dzs, mx, sum, lane);
-                if (before < 0) {
-                    marked = true;
-                    stage = GATE_ALL;
-                }
-            } else if (exact) {
+            if (exact) {
 #pragma unroll 4
                 for (int j = 0; j < n; ++j) {
                     const float o = __shfl_sync(0xffffffffu, v, j);
@@ -493,7 +457,7 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
                 }
             }
             const bool chosen = lane < n && before < g.k;
-            if (!exact && mode != GATE_EXACT) {
+            if (!exact) {
                 const float last = __shfl_sync(0xffffffffu, v, __ffs(__ballot_sync(0xffffffffu, lane < n && before == g.k - 1)) - 1);
                 if (lane < n && (chosen ? close > 1 : v >= last - close_by)) {
                     atomicOr(&room.todo[e >> 5], 1u << (e & 31));
@@ -510,14 +474,17 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
                     return false;
                 }
                 stage = GATE_ALL;
+            } else {
+                room.picks.at[lane] = (unsigned short)(e | before << 9);
+                if (lane == 0) {
+                    room.picks.n = n;
+                    room.picks.mx = mx;
+                    room.picks.sum = sum;
+                }
             }
-        } else if (mode == GATE_EXACT) {                                   // too many candidates for a lane each
-            marked = true;
-            stage = GATE_ALL;
         } else {                                                           // many equal values, or few logits that are not -infinity
             int at = -1;
-            marked = choose_rounds(g, room.todo, balance ? room.c : room.z, kept, near0, near1, lane, at);
-            if (!marked) {
+            if (choose_rounds(g, balance ? room.c : room.z, kept, near0, near1, lane, at)) {
                 float s;
                 if (choice_weight(g, room.z[max(at, 0)], at >= 0, mx, sum, s)) {
                     if (at >= 0) {
@@ -526,8 +493,8 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
                     }
                     return false;
                 }
-                stage = GATE_ALL;
             }
+            stage = GATE_ALL;
         }
     }
     if (!g.sigmoid && balance && stage == GATE_GROUPS) stage = GATE_ALL;   // a softmax with a bias: all logits enter every choice value
@@ -574,19 +541,61 @@ static __device__ __noinline__ void choose_groups(const GateArgs& g, ChoiceRoom<
     __syncwarp();
 }
 
-// After choose_fast's `true`, the marked logits being in z64 (room for all): the mode in which it goes on, or -1: the token is done.  The
-// logits in `room` are brought up to date.
+// The choice among the candidates, whose marked ones' logits are exact in z64 (or z, z64 null), z being up to date: each keeps its rank among the unmarked
+// ones, from which it is far enough, and the marked ones are ranked among themselves.  False: that does not decide, and everything is to be computed again.
+// It may not for a softmax with a bias: p_e = exp(z_e - mx) / sum with a sum of logits that are off by dz leaves c_a - c_b off by dz |p_a - p_b|.
+// (The whole of choose_fast once more took 10 thousand cycles of gate_8192 where this takes a third.)
 template <int PER>
-__device__ __forceinline__ int go_on(const GateArgs& g, ChoiceRoom<PER>& room, double* z64, int lane, int32_t* ids, float* weights) {
+static __device__ __noinline__ bool finish_choice(const GateArgs& g, ChoiceRoom<PER>& room, const double* z64, float dz, float rel, int lane, int32_t* ids, float* weights) {
+    const int n = room.picks.n, e = lane < n ? room.picks.at[lane] & 511 : 0, was = lane < n ? room.picks.at[lane] >> 9 : 32;
+    const float mx = room.picks.mx, sum = room.picks.sum;
+    const bool m = lane < n && (room.todo[e >> 5] >> (e & 31) & 1u), soft = g.balance && !g.sigmoid;
+    double w = 0.0, b = 0.0;
+    if (m) {
+        w = marked_logit(z64, room.z, e);
+        if (g.balance) {
+            b = (double)g.balance[e];
+            w = w == -INFINITY ? w : (g.sigmoid ? 1.0 / (1.0 + exp(-w)) : exp(w - (double)mx) / (double)sum) + b;
+        }
+    }
+    int before = was;
+    bool unsure = false;
+    for (unsigned left = __ballot_sync(0xffffffffu, m); left; left &= left - 1) {
+        const int j = __ffs(left) - 1;                                     // ascending experts
+        const double o = __shfl_sync(0xffffffffu, w, j);
+        const int o_was = __shfl_sync(0xffffffffu, was, j);
+        if (m) before += (int)(o > w || (o == w && j < lane)) - (int)(o_was < was);
+        if (soft) {
+            const double ob = __shfl_sync(0xffffffffu, b, j);
+            unsure |= m && j != lane && w > -INFINITY && o > -INFINITY && fabs(o - w) <= 1.1 * (double)bound_of(g, dz, rel, mx) * fabs((o - ob) - (w - b)) + 1e-12;
+        }
+    }
+    const bool chosen = lane < n && before < g.k;
+    float s = 0.f;
+    if (!__any_sync(0xffffffffu, unsure && before <= g.k) && choice_weight(g, room.z[e], chosen, mx, sum, s)) {
+        if (chosen) {
+            ids[before] = e;
+            weights[before] = s;
+        }
+        return true;
+    }
+    if (lane == 0) room.todo[kTodoStage] = GATE_ALL;
+    choose_all<PER>(g, room, lane);
+    return false;
+}
+// After choose_fast's `true`, the marked logits being in z64 (room for all): the mode in which it goes on, GATE_DONE, or GATE_WAITS for what
+// is marked now.  The logits in `room` are brought up to date.
+template <int PER>
+__device__ __forceinline__ int go_on(const GateArgs& g, ChoiceRoom<PER>& room, double* z64, float dz, float rel, int lane, int32_t* ids, float* weights) {
     const uint32_t stage = room.todo[kTodoStage];
     if (stage == GATE_ALL) {
         choose_exact(g, z64, reinterpret_cast<unsigned long long*>(room.z), lane, ids, weights);       // z and c
-        return -1;
+        return GATE_DONE;
     }
     for (int b = 0; 32 * b < g.E; ++b)
         if (room.todo[b] >> lane & 1u) room.z[32 * b + lane] = (float)z64[32 * b + lane];
     __syncwarp();
-    if (stage == GATE_EXPERTS) return GATE_EXACT;
+    if (stage == GATE_EXPERTS) return finish_choice<PER>(g, room, z64, dz, rel, lane, ids, weights) ? GATE_DONE : GATE_WAITS;
     choose_groups<PER>(g, room, z64, z64, lane);
     return GATE_DECIDED;
 }

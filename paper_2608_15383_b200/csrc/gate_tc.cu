@@ -137,12 +137,15 @@ struct Warp {                                                              // a 
     ChoiceRoom<PER> room;
     double z64[32 * PER];                                                  // logits computed again
 };
-constexpr int kItems = 1024;
+constexpr int kTodoUsed = 10;
+__device__ __forceinline__ int todo_at(int i) { return i < 8 ? i : kTodoKept + i - 8; }
+constexpr int kItems = 512;                                               // two tokens with all of their logits
 // A token that waits for logits to be computed again; its logits are back in its row of `part`, which no other CTA reads.
 struct Waiting {
     int token, first;                                                      // in the tile; first item, -1: no room for it in this round
     float dz;
-    uint32_t todo[kTodoWords];
+    uint32_t todo[kTodoUsed];                                              // the words of 256 experts, kTodoKept, kTodoStage
+    Picks picks;
 };
 template <int MT, int PER>
 struct __align__(1024) Shared {
@@ -427,7 +430,13 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                     }
 #pragma unroll
                     for (int j = 0; j < PER; ++j) room.z[lane + 32 * j] = sm.s.part[tok][lane + 32 * j];
-                    if (lane < kTodoWords) room.todo[lane] = w.todo[lane];
+                    if (lane < kTodoUsed) room.todo[todo_at(lane)] = w.todo[lane];
+                    room.picks.at[lane] = w.picks.at[lane];
+                    if (lane == 0) {
+                        room.picks.n = w.picks.n;
+                        room.picks.mx = w.picks.mx;
+                        room.picks.sum = w.picks.sum;
+                    }
                     __syncwarp();
                     int j = w.first;
                     for (int b = 0; 32 * b < g.E; ++b)                     // the items are in ascending experts
@@ -437,16 +446,20 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                 }
                 int32_t* ids_t = ids + (size_t)(t0 + tok) * g.k;
                 float* weights_t = weights + (size_t)(t0 + tok) * g.k;
-                if (round > 0) mode = go_on<PER>(g, room, my.z64, lane, ids_t, weights_t);
-                const bool again = mode >= 0 && choose_fast<PER>(g, room, balance, dz, rel, lane, mode, my.z64, ids_t, weights_t);
+                if (round > 0) mode = go_on<PER>(g, room, my.z64, dz, rel, lane, ids_t, weights_t);
+                const bool again = mode == GATE_WAITS || (mode != GATE_DONE && choose_fast<PER>(g, room, balance, dz, rel, lane, mode, ids_t, weights_t));
                 if (again) {                                               // it waits; its logits go back to its row
                     int at = f;
                     if (round == 0) {
                         if (lane == 0) at = atomicAdd(&sm.n_waiting, 1);
                         at = __shfl_sync(0xffffffffu, at, 0);
                     }
-                    if (lane < kTodoWords) sm.waiting[at].todo[lane] = room.todo[lane];
+                    if (lane < kTodoUsed) sm.waiting[at].todo[lane] = room.todo[todo_at(lane)];
+                    sm.waiting[at].picks.at[lane] = room.picks.at[lane];
                     if (lane == 0) {
+                        sm.waiting[at].picks.n = room.picks.n;
+                        sm.waiting[at].picks.mx = room.picks.mx;
+                        sm.waiting[at].picks.sum = room.picks.sum;
                         sm.waiting[at].token = tok;
                         sm.waiting[at].dz = dz;
                     }
