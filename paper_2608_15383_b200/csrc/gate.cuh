@@ -629,31 +629,71 @@ __device__ __forceinline__ float square8(const uint4& a) {
     unpack8(a, x);
     return dot8(x, x);
 }
-// A logit by one warp in binary64; products of BF16 values are exact in binary32.
-static __device__ __noinline__ double logit_f64(const uint4* x, const uint4* w, int chunks, int lane) {
-    constexpr int U = 8;                                                   // chunks in flight, sums side by side
-    double s[U] = {};
-    for (int i0 = 0; i0 < chunks; i0 += 32 * U) {
-        uint4 wv[U], xv[U];
+// A logit, or what chunks `from` .. `to` - 1 of eight numbers add to it, by one warp in binary64; products of BF16 values are exact in
+// binary32.  Conversions to binary64 bound it (16 a cycle and SM).
+static __device__ __noinline__ double logit_f64(const uint4* x, const uint4* w, int from, int to, int lane) {
+    constexpr int U = 2;                                                   // chunks at a time (little code: it is mostly cold), the next ones in flight
+    double s[4 * U] = {};
+    uint4 wv[U], xv[U];
+    auto fetch = [&](int i0) {
 #pragma unroll
         for (int j = 0; j < U; ++j) {
             const int i = i0 + 32 * j + lane;
             wv[j] = xv[j] = make_uint4(0, 0, 0, 0);
-            if (i < chunks) {
+            if (i < to) {
                 wv[j] = w[i];
                 xv[j] = x[i];
             }
         }
+    };
+    fetch(from);
+#pragma unroll 1
+    for (int i0 = from; i0 < to; i0 += 32 * U) {
+        float p[U][8];
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const uint32_t a[4] = {wv[j].x, wv[j].y, wv[j].z, wv[j].w}, b[4] = {xv[j].x, xv[j].y, xv[j].z, xv[j].w};
+#pragma unroll
+            for (int n = 0; n < 4; ++n) {
+                p[j][2 * n] = __uint_as_float(a[n] << 16) * __uint_as_float(b[n] << 16);
+                p[j][2 * n + 1] = __uint_as_float(a[n] & 0xffff0000u) * __uint_as_float(b[n] & 0xffff0000u);
+            }
+        }
+        fetch(i0 + 32 * U);
 #pragma unroll
         for (int n = 0; n < 8; ++n)
 #pragma unroll
-            for (int j = 0; j < U; ++j) {
-                const uint32_t a = n < 2 ? wv[j].x : n < 4 ? wv[j].y : n < 6 ? wv[j].z : wv[j].w, b = n < 2 ? xv[j].x : n < 4 ? xv[j].y : n < 6 ? xv[j].z : xv[j].w;
-                s[j] += (double)(n & 1 ? __uint_as_float(a & 0xffff0000u) * __uint_as_float(b & 0xffff0000u) : __uint_as_float(a << 16) * __uint_as_float(b << 16));
-            }
+            for (int j = 0; j < U; ++j) s[4 * j + n % 4] += (double)p[j][n];
     }
-    return warp_sum_f64(((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7])));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) s[j] += s[4 + j];
+    return warp_sum_f64((s[0] + s[1]) + (s[2] + s[3]));
 }
+// Into how many parts (a power of two, up to eight) the warps of a CTA share the sums of `items` logits: no more than `most` parts in all.
+__device__ __forceinline__ int log_parts(int items, int most) {
+    return items * 8 <= most ? 3 : items * 4 <= most ? 2 : items * 2 <= most ? 1 : 0;
+}
+// The marked experts, words of 32: how many there are up to a lane's word, and expert number `i` of them.
+struct Marked {
+    unsigned word;
+    int up_to;
+    __device__ __forceinline__ Marked(const uint32_t* todo, int words, int lane) {
+        word = lane < words ? todo[lane] : 0u;
+        up_to = __popc(word);
+#pragma unroll
+        for (int m = 1; m < 32; m <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, up_to, m);
+            if (lane >= m) up_to += o;
+        }
+    }
+    __device__ __forceinline__ int count() const { return __shfl_sync(0xffffffffu, up_to, 31); }
+    __device__ __forceinline__ int expert(int i) const {                   // the same i in all lanes
+        const int at = __ffs(__ballot_sync(0xffffffffu, up_to > i)) - 1;
+        unsigned es = __shfl_sync(0xffffffffu, word, at);
+        for (int skip = i - (__shfl_sync(0xffffffffu, up_to, at) - __popc(es)); skip > 0; --skip) es &= es - 1;
+        return 32 * at + __ffs(es) - 1;
+    }
+};
 
 // every form is a programmatic dependent of the kernel before it in the stream (it waits for it before it reads anything)
 template <typename... P, typename... A>

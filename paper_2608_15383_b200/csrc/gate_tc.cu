@@ -139,10 +139,11 @@ struct Warp {                                                              // a 
 };
 constexpr int kTodoUsed = 10;
 __device__ __forceinline__ int todo_at(int i) { return i < 8 ? i : kTodoKept + i - 8; }
+constexpr int kParts = 2 * kDrainWarps;
 constexpr int kItems = 512;                                               // two tokens with all of their logits
 // A token that waits for logits to be computed again; its logits are back in its row of `part`, which no other CTA reads.
 struct Waiting {
-    int token, first;                                                      // in the tile; first item, -1: no room for it in this round
+    int token, first;                                                      // in the tile; first item | how many << 16, -1: no room for them in this round
     float dz;
     uint32_t todo[kTodoUsed];                                              // the words of 256 experts, kTodoKept, kTodoStage
     Picks picks;
@@ -350,24 +351,18 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         const float rel = bias || addend ? kAddedRel : 0.f;
         const int owned = kTokens / CL, chunks = H / 8;
         // Round 0: the CTA's tokens.  The rounds behind it: those that wait, done by the warps together: first the logits, then the choices.
-        for (int round = 0, n_tok = owned;; ++round) {
+        for (int round = 0, n_tok = owned, log_p = 0;; ++round) {
             if (round > 0) {
                 for (int f = d; f < n_tok; f += kDrainWarps) {
                     Waiting& w = sm.waiting[f];
-                    const unsigned es = w.token >= 0 && 32 * lane < g.E ? w.todo[lane] : 0u;   // a word per lane
-                    int before = __popc(es);
-#pragma unroll
-                    for (int m = 1; m < 32; m <<= 1) {
-                        const int o = __shfl_up_sync(0xffffffffu, before, m);
-                        if (lane >= m) before += o;
-                    }
-                    const int total = __shfl_sync(0xffffffffu, before, 31);
+                    const Marked marked(w.todo, w.token >= 0 ? (g.E + 31) / 32 : 0, lane);   // a word per lane
+                    const int total = marked.count();
                     int first = 0;
                     if (lane == 0 && total) first = atomicAdd(&sm.n_items, total);
                     first = __shfl_sync(0xffffffffu, first, 0);
-                    if (lane == 0) w.first = first + total <= kItems ? first : -1;
-                    int at = first + before - __popc(es);
-                    for (unsigned r = es; r; r &= r - 1, ++at)
+                    if (lane == 0) w.first = first + total <= kItems ? first | total << 16 : -1;
+                    int at = first + marked.up_to - __popc(marked.word);
+                    for (unsigned r = marked.word; r; r &= r - 1, ++at)
                         if (at < kItems) {
                             sm.item_expert[at] = (unsigned short)(32 * lane + __ffs(r) - 1);
                             sm.item_waiting[at] = (unsigned short)f;
@@ -375,11 +370,16 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                 }
                 choosers_sync();
                 const int n_items = min(sm.n_items, kItems);
-                for (int j = d; j < n_items; j += kDrainWarps) {
+                log_p = log_parts(n_items, kParts);
+                for (int u = d; u < n_items << log_p; u += kDrainWarps) {
+                    const int j = u >> log_p, part = u & ((1 << log_p) - 1), e = sm.item_expert[j];
                     const long long t = t0 + sm.waiting[sm.item_waiting[j]].token;
-                    const int e = sm.item_expert[j];
-                    const double z = logit_f64(reinterpret_cast<const uint4*>(hidden + t * H), reinterpret_cast<const uint4*>(w_router + (size_t)e * H), chunks, lane);
-                    if (lane == 0) sm.item_z[j] = z + (bias ? (double)bias[e] : 0.0) + (addend ? (double)addend[t * g.E + e] : 0.0);
+                    const float b = bias && part == 0 ? bias[e] : 0.f, add = addend && part == 0 ? addend[(size_t)t * g.E + e] : 0.f;
+                    double z = logit_f64(reinterpret_cast<const uint4*>(hidden + t * H), reinterpret_cast<const uint4*>(w_router + (size_t)e * H), chunks * part >> log_p,
+                                         chunks * (part + 1) >> log_p, lane);
+                    z += (double)b;
+                    z += (double)add;
+                    if (lane == 0) sm.item_z[u] = z;
                 }
                 choosers_sync();
                 if (tid == 128) sm.n_items = 0;
@@ -438,10 +438,12 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                         room.picks.sum = w.picks.sum;
                     }
                     __syncwarp();
-                    int j = w.first;
-                    for (int b = 0; 32 * b < g.E; ++b)                     // the items are in ascending experts
-                        for (unsigned es = room.todo[b]; es; es &= es - 1, ++j)
-                            if (lane == 0) my.z64[32 * b + __ffs(es) - 1] = sm.item_z[j];
+                    const int first = w.first & 0xffff, count = w.first >> 16;
+                    for (int j = first + lane; j < first + count; j += 32) {
+                        double z = sm.item_z[j << log_p];
+                        for (int p = 1; p < 1 << log_p; ++p) z += sm.item_z[(j << log_p) + p];
+                        my.z64[sm.item_expert[j]] = z;
+                    }
                     __syncwarp();
                 }
                 int32_t* ids_t = ids + (size_t)(t0 + tok) * g.k;
