@@ -202,20 +202,25 @@ static __device__ __noinline__ void mark_from(const GateArgs& g, uint32_t* todo,
     __syncwarp();
 }
 // k rounds of arg-max over v [E]: lane j gets the j-th choice (-1: none).  False: two of them, or the last and the next, are too close.
+template <int PER>
 static __device__ __noinline__ bool choose_rounds(const GateArgs& g, const float* v, unsigned kept, float near0, float near1, int lane, int& mine) {
     const bool grouped = g.top_groups < g.G, exact = near0 == 0.f;
-    unsigned taken = 0;                                                    // of experts lane, lane + 32, ...
+    uint32_t key[PER];                                                     // of experts lane, lane + 32, ...
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int e = lane + 32 * i;
+        key[i] = e < g.E && (!grouped || in_kept(g, kept, e)) ? order_key(v[e]) : 0u;
+    }
     float prev = 0.f;
     for (int j = 0; j <= g.k; ++j) {
         uint32_t top = 0;
         int be = 0x7fffffff;
-        for (int i = 0, e = lane; e < g.E; ++i, e += 32) {
-            const uint32_t key = (taken >> i & 1u) || (grouped && !in_kept(g, kept, e)) ? 0u : order_key(v[e]);
-            if (key > top) {                                               // ascending experts: the first maximum wins
-                top = key;
-                be = e;
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (key[i] > top) {                                            // ascending experts: the first maximum wins
+                top = key[i];
+                be = lane + 32 * i;
             }
-        }
         const uint32_t most = __reduce_max_sync(0xffffffffu, top);
         if (!most) break;                                                  // no other expert can be chosen
         const int e = (int)__reduce_min_sync(0xffffffffu, top == most ? (unsigned)be : 0x7fffffffu);
@@ -223,7 +228,9 @@ static __device__ __noinline__ bool choose_rounds(const GateArgs& g, const float
         if (!exact && j > 0 && x > -INFINITY && prev - x <= near0 + near1 * (fabsf(prev) + fabsf(x))) return false;
         prev = x;
         if (j == lane && j < g.k) mine = e;
-        if (lane == (e & 31)) taken |= 1u << (e >> 5);
+#pragma unroll
+        for (int i = 0; i < PER; ++i)
+            if (e == lane + 32 * i) key[i] = 0u;
     }
     return true;
 }
@@ -484,7 +491,7 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
             }
         } else {                                                           // many equal values, or few logits that are not -infinity
             int at = -1;
-            if (choose_rounds(g, balance ? room.c : room.z, kept, near0, near1, lane, at)) {
+            if (choose_rounds<PER>(g, balance ? room.c : room.z, kept, near0, near1, lane, at)) {
                 float s;
                 if (choice_weight(g, room.z[max(at, 0)], at >= 0, mx, sum, s)) {
                     if (at >= 0) {
