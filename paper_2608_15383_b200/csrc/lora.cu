@@ -30,8 +30,12 @@ __host__ __device__ inline int plan_tiles(int T, int n) {                  // mo
     return T / tile_rows(T) + groups;
 }
 
-// A counting sort by one CTA: a warp's tokens in steps of 32, the warps' counts per group summed over the warps, ranks inside a step by matching.  It is
-// bound by the latency of those steps: 2.2 us for few tokens, 6 for 8192 (once per step of all layers).
+// A counting sort by one CTA.  A warp takes a run of tokens in steps of 32 and counts its tokens of each group; a thread per group adds up the warps'
+// counts; a scan over the groups gives their first rows and tiles; then every warp places its tokens behind those of the warps before it.
+// Which lanes of a step have the same group comes from a ballot for each bit of its number (`match` takes 10 cycles for each value that
+// differs) unless all have.  us, replayed from a graph, 16 adapters and long requests / 256 adapters, each token another: 64 tokens 2.6 / 2.9, 1024
+// 3.2 / 4.4, 8192 5.8 / 17.0 (`match`: 26); 1000 adapters, 64 tokens 3.5 (a warp per group over the warps' counts: 16.9).  Bound by the steps'
+// instructions, 50 in each of the two passes where requests are long; once per step of all layers.
 __global__ void __launch_bounds__(kPlanThreads)
 lora_plan_kernel(const int32_t* ids, int T, int n, int32_t* plan) {
     extern __shared__ int32_t sm[];
@@ -39,108 +43,142 @@ lora_plan_kernel(const int32_t* ids, int T, int n, int32_t* plan) {
     int32_t* count = hist + kPlanWarps * (n + 1);                          // [n + 1]
     int32_t* first = count + n + 1;                                        // [n + 1] first row of a group
     int32_t* tile0 = first + n + 1;                                        // [n + 1] its first tile
-    __shared__ int bad;
+    __shared__ int bad, rows_of[kPlanWarps], tiles_of[kPlanWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, most = tile_rows(T);
     const unsigned lt = (1u << lane) - 1u;
     LoraTile* tiles = reinterpret_cast<LoraTile*>(plan + LP_WORDS);
     int32_t* perm = plan + LP_WORDS + 4 * plan_tiles(T, n);
-    for (int i = tid; i < kPlanWarps * (n + 1); i += kPlanThreads) hist[i] = 0;
+    const int per = ((T + kPlanWarps - 1) / kPlanWarps + 31) & ~31, warps = per ? (T + per - 1) / per : 0;   // tokens of a warp, warps that have some
+    for (int i = tid; i < warps * (n + 1); i += kPlanThreads) hist[i] = 0;
     if (tid == 0) bad = 0;
     grid_dependency_wait();
     grid_launch_dependents();
     __syncthreads();
-    const int per = ((T + kPlanWarps - 1) / kPlanWarps + 31) & ~31;
-    const int t_begin = min(T, warp * per), t_end = min(T, t_begin + per);
+    const int t_begin = min(T, warp * per), t_end = min(T, t_begin + per), bits = 32 - __clz(n);
     int32_t* mine = hist + warp * (n + 1);
-    constexpr int KEPT = 8;                                                // of a lane's ids in registers: 8192 tokens
+    constexpr int KEPT = 8;                                                // steps whose ids, then groups, are in registers: 8192 tokens
     int kept[KEPT];
+    unsigned same[KEPT];                                                   // lanes of the same group
 #pragma unroll
     for (int i = 0; i < KEPT; ++i) kept[i] = t_begin + 32 * i + lane < t_end ? ids[t_begin + 32 * i + lane] : -1;
-    auto group_of = [&](int id, int t) {
-        if (t >= t_end) return n + 1;
+    auto look_at = [&](int id, bool in, int& group, unsigned& same) {
         if (id < -1 || id >= n) bad = 1;
-        return id >= 0 && id < n ? id : n;
-    };
-    // Steps of 32 tokens.  Mostly all are of one adapter, where requests are long: then nothing is to be matched.
-    auto count_step = [&](int id, int t0) {
-        const int b = group_of(id, t0 + lane);
-        if (__all_sync(0xffffffffu, b == __shfl_sync(0xffffffffu, b, 0))) {
-            if (lane == 0) mine[b] += 32;
-        } else {
-            const unsigned same = __match_any_sync(0xffffffffu, b);
-            if (b <= n && !(same & lt)) mine[b] += __popc(same);
+        group = id >= 0 && id < n ? id : n;
+        same = 0xffffffffu;
+        const int of_first = __shfl_sync(0xffffffffu, group, 0);
+        if (__all_sync(0xffffffffu, in && group == of_first)) return;      // mostly, where requests are long
+        const unsigned valid = __ballot_sync(0xffffffffu, in);
+        unsigned other = 0u;
+#pragma unroll 4
+        for (int b = 0; b < bits; ++b) {
+            const unsigned m = __ballot_sync(0xffffffffu, group >> b & 1);
+            other |= m ^ (unsigned)-(group >> b & 1);
         }
+        same = valid & ~other;
+    };
+    auto count_step = [&](int group, unsigned same, bool in) {
+        if (in && !(same & lt)) mine[group] += __popc(same);
         __syncwarp();
     };
-    auto place_step = [&](int id, int t0, int32_t* perm, const int32_t* first) {
-        const int b = group_of(id, t0 + lane);
-        if (__all_sync(0xffffffffu, b == __shfl_sync(0xffffffffu, b, 0))) {
-            const int at = mine[b];
-            perm[first[b] + at + lane] = t0 + lane;
-            __syncwarp();
-            if (lane == 0) mine[b] = at + 32;
-        } else {
-            const unsigned same = __match_any_sync(0xffffffffu, b);
-            if (b <= n) perm[first[b] + mine[b] + __popc(same & lt)] = t0 + lane;
-            __syncwarp();
-            if (b <= n && !(same & lt)) mine[b] += __popc(same);
-        }
+    auto place_step = [&](int group, unsigned same, int t0, bool in) {
+        if (in) perm[first[group] + mine[group] + __popc(same & lt)] = t0 + lane;
         __syncwarp();
+        count_step(group, same, in);
     };
 #pragma unroll
-    for (int i = 0; i < KEPT; ++i)
-        if (t_begin + 32 * i < t_end) count_step(kept[i], t_begin + 32 * i);
-    for (int t0 = t_begin + 32 * KEPT; t0 < t_end; t0 += 32) count_step(t0 + lane < t_end ? ids[t0 + lane] : -1, t0);
+    for (int i = 0; i < KEPT; ++i) {
+        const int t0 = t_begin + 32 * i;
+        if (t0 >= t_end) break;
+        look_at(kept[i], t0 + lane < t_end, kept[i], same[i]);
+        count_step(kept[i], same[i], t0 + lane < t_end);
+    }
+    for (int t0 = t_begin + 32 * KEPT; t0 < t_end; t0 += 32) {
+        int group;
+        unsigned like;
+        look_at(t0 + lane < t_end ? ids[t0 + lane] : -1, t0 + lane < t_end, group, like);
+        count_step(group, like, t0 + lane < t_end);
+    }
     __syncthreads();
-    for (int b = warp; b <= n; b += kPlanWarps) {                          // lane w: warp w's tokens of group b
-        const int c = hist[lane * (n + 1) + b];
-        int incl = c;
+    int rows = 0;                                                          // of group tid
+    for (int b = tid; b <= n; b += kPlanThreads) {
+        int sum = 0;
+        for (int w0 = 0; w0 < warps; w0 += 8) {
+            int c[8];
+#pragma unroll
+            for (int w = 0; w < 8; ++w) c[w] = w0 + w < warps ? hist[(w0 + w) * (n + 1) + b] : 0;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) {
+                if (w0 + w < warps) hist[(w0 + w) * (n + 1) + b] = sum;
+                sum += c[w];
+            }
+        }
+        count[b] = sum;
+        if (b < n) rows = b == tid ? sum : rows;
+    }
+    static_assert(kMaxAdapters <= kPlanThreads && kPlanWarps == 32, "a thread per adapter, a lane per warp");
+    int ir = rows, it = (rows + most - 1) / most;
+    const int nt_mine = it;
+    auto scan = [&](int& r, int& t) {                                      // sums up to this lane's
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
-            const int o = __shfl_up_sync(0xffffffffu, incl, d);
-            if (lane >= d) incl += o;
-        }
-        hist[lane * (n + 1) + b] = incl - c;
-        if (lane == 31) count[b] = incl;
-    }
-    static_assert(kPlanWarps == 32, "a lane per warp");
-    __syncthreads();
-    if (warp == 0) {
-        int rows = 0, nt = 0;
-        for (int b0 = 0; b0 <= n; b0 += 32) {
-            const int c = b0 + lane <= n ? count[b0 + lane] : 0, tl = (c + most - 1) / most;
-            int ic = c, it = tl;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int oc = __shfl_up_sync(0xffffffffu, ic, d), ot = __shfl_up_sync(0xffffffffu, it, d);
-                if (lane >= d) {
-                    ic += oc;
-                    it += ot;
-                }
+            const int o = __shfl_up_sync(0xffffffffu, r, d), p = __shfl_up_sync(0xffffffffu, t, d);
+            if (lane >= d) {
+                r += o;
+                t += p;
             }
-            if (b0 + lane <= n) {
-                first[b0 + lane] = rows + ic - c;
-                tile0[b0 + lane] = nt + it - tl;
-            }
-            rows += __shfl_sync(0xffffffffu, ic, 31);
-            nt += __shfl_sync(0xffffffffu, it, 31);
         }
-        if (lane == 0) {
-            plan[LP_MAGIC] = kPlanMagic;
-            plan[LP_TOKENS] = T;
-            plan[LP_ADAPTERS] = n;
-            plan[LP_TILES] = nt;
-            plan[LP_STATUS] = bad ? EXMOE_ERR_BAD_ADAPTER_ID : EXMOE_OK;
-        }
+    };
+    scan(ir, it);
+    if (lane == 31) {
+        rows_of[warp] = ir;
+        tiles_of[warp] = it;
     }
     __syncthreads();
-    for (int b = warp; b <= n; b += kPlanWarps)
-        for (int i = lane; i * most < count[b]; i += 32)
-            tiles[tile0[b] + i] = LoraTile{b < n ? b : -1, first[b] + i * most, min(most, count[b] - i * most), 0};
+    int wr = rows_of[lane], wt = tiles_of[lane];
+    scan(wr, wt);
+    const int rows_all = __shfl_sync(0xffffffffu, wr, 31), tiles_all = __shfl_sync(0xffffffffu, wt, 31);
+    const int r0 = __shfl_sync(0xffffffffu, wr, (warp + 31) & 31), q0 = __shfl_sync(0xffffffffu, wt, (warp + 31) & 31);
+    if (tid < n) {
+        first[tid] = (warp ? r0 : 0) + ir - rows;
+        tile0[tid] = (warp ? q0 : 0) + it - nt_mine;
+    }
+    if (tid == 0) {                                                        // the tokens without an adapter come last
+        first[n] = rows_all;
+        tile0[n] = tiles_all;
+    }
+    const int nt = tiles_all + (T - rows_all + most - 1) / most;
+    if (tid == 0) {
+        plan[LP_MAGIC] = kPlanMagic;
+        plan[LP_TOKENS] = T;
+        plan[LP_ADAPTERS] = n;
+        plan[LP_TILES] = nt;
+        plan[LP_STATUS] = bad ? EXMOE_ERR_BAD_ADAPTER_ID : EXMOE_OK;
+    }
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < KEPT; ++i)
-        if (t_begin + 32 * i < t_end) place_step(kept[i], t_begin + 32 * i, perm, first);
-    for (int t0 = t_begin + 32 * KEPT; t0 < t_end; t0 += 32) place_step(t0 + lane < t_end ? ids[t0 + lane] : -1, t0, perm, first);
+    for (int i = 0; i < KEPT; ++i) {
+        const int t0 = t_begin + 32 * i;
+        if (t0 >= t_end) break;
+        place_step(kept[i], same[i], t0, t0 + lane < t_end);
+    }
+    for (int t0 = t_begin + 32 * KEPT; t0 < t_end; t0 += 32) {
+        int group;
+        unsigned like;
+        look_at(t0 + lane < t_end ? ids[t0 + lane] : -1, t0 + lane < t_end, group, like);
+        place_step(group, like, t0, t0 + lane < t_end);
+    }
+    for (int i = tid; i < nt; i += kPlanThreads) {
+        int b = 0, above = n + 1;                                          // the last group whose first tile is not behind this one: the others have none
+        while (above - b > 1) {
+            const int m = (b + above) / 2;
+            if (tile0[m] <= i)
+                b = m;
+            else
+                above = m;
+        }
+        const int row = (i - tile0[b]) * most;
+        tiles[i] = LoraTile{b < n ? b : -1, first[b] + row, min(most, count[b] - row), 0};
+    }
 }
 
 struct LoraArgs {
