@@ -85,7 +85,7 @@ gate_logits_kernel(const Z* logits, long long ld, int T, const __grid_constant__
                 choose_groups<PER>(g, room, nullptr, z64, lane);
                 continue;
             }
-            if (stage == GATE_EXPERTS && finish_choice<PER>(g, room, nullptr, 0.f, 0.f, lane, ids + t * g.k, weights + t * g.k)) return;
+            if (stage == GATE_EXPERTS && finish_choice<PER>(g, room, balance, nullptr, 0.f, 0.f, lane, ids + t * g.k, weights + t * g.k)) return;
             all = true;
             break;
         }
@@ -248,7 +248,7 @@ gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w
                 if (lane == 0) sm.z64[e] = v + (bias ? (double)bias[e] : 0.0) + (addend ? (double)addend[t * g.E + e] : 0.0);
             }
         __syncthreads();
-        if (warp == 0) mode = go_on<PER>(g, room, sm.z64, dz, rel, lane, ids_t, weights_t);
+        if (warp == 0) mode = go_on<PER>(g, room, balance, sm.z64, dz, rel, lane, ids_t, weights_t);
     }
 }
 

@@ -553,15 +553,15 @@ static __device__ __noinline__ void choose_groups(const GateArgs& g, ChoiceRoom<
 // It may not for a softmax with a bias: p_e = exp(z_e - mx) / sum with a sum of logits that are off by dz leaves c_a - c_b off by dz |p_a - p_b|.
 // (The whole of choose_fast once more took 10 thousand cycles of gate_8192 where this takes a third.)
 template <int PER>
-static __device__ __noinline__ bool finish_choice(const GateArgs& g, ChoiceRoom<PER>& room, const double* z64, float dz, float rel, int lane, int32_t* ids, float* weights) {
+static __device__ __noinline__ bool finish_choice(const GateArgs& g, ChoiceRoom<PER>& room, const float* balance, const double* z64, float dz, float rel, int lane, int32_t* ids, float* weights) {
     const int n = room.picks.n, e = lane < n ? room.picks.at[lane] & 511 : 0, was = lane < n ? room.picks.at[lane] >> 9 : 32;
     const float mx = room.picks.mx, sum = room.picks.sum;
-    const bool m = lane < n && (room.todo[e >> 5] >> (e & 31) & 1u), soft = g.balance && !g.sigmoid;
+    const bool m = lane < n && (room.todo[e >> 5] >> (e & 31) & 1u), soft = balance && !g.sigmoid;
     double w = 0.0, b = 0.0;
     if (m) {
         w = marked_logit(z64, room.z, e);
-        if (g.balance) {
-            b = (double)g.balance[e];
+        if (balance) {
+            b = (double)balance[e];
             w = w == -INFINITY ? w : (g.sigmoid ? 1.0 / (1.0 + exp(-w)) : exp(w - (double)mx) / (double)sum) + b;
         }
     }
@@ -593,7 +593,7 @@ static __device__ __noinline__ bool finish_choice(const GateArgs& g, ChoiceRoom<
 // After choose_fast's `true`, the marked logits being in z64 (room for all): the mode in which it goes on, GATE_DONE, or GATE_WAITS for what
 // is marked now.  The logits in `room` are brought up to date.
 template <int PER>
-__device__ __forceinline__ int go_on(const GateArgs& g, ChoiceRoom<PER>& room, double* z64, float dz, float rel, int lane, int32_t* ids, float* weights) {
+__device__ __forceinline__ int go_on(const GateArgs& g, ChoiceRoom<PER>& room, const float* balance, double* z64, float dz, float rel, int lane, int32_t* ids, float* weights) {
     const uint32_t stage = room.todo[kTodoStage];
     if (stage == GATE_ALL) {
         choose_exact(g, z64, reinterpret_cast<unsigned long long*>(room.z), lane, ids, weights);       // z and c
@@ -602,7 +602,7 @@ __device__ __forceinline__ int go_on(const GateArgs& g, ChoiceRoom<PER>& room, d
     for (int b = 0; 32 * b < g.E; ++b)
         if (room.todo[b] >> lane & 1u) room.z[32 * b + lane] = (float)z64[32 * b + lane];
     __syncwarp();
-    if (stage == GATE_EXPERTS) return finish_choice<PER>(g, room, z64, dz, rel, lane, ids, weights) ? GATE_DONE : GATE_WAITS;
+    if (stage == GATE_EXPERTS) return finish_choice<PER>(g, room, balance, z64, dz, rel, lane, ids, weights) ? GATE_DONE : GATE_WAITS;
     choose_groups<PER>(g, room, z64, z64, lane);
     return GATE_DECIDED;
 }
@@ -680,7 +680,7 @@ static __device__ __noinline__ double logit_f64(const uint4* x, const uint4* w, 
 __device__ __forceinline__ int log_parts(int items, int most) {
     return items * 8 <= most ? 3 : items * 4 <= most ? 2 : items * 2 <= most ? 1 : 0;
 }
-// The marked experts, words of 32: how many there are up to a lane's word, and expert number `i` of them.
+// The marked experts, a word of 32 per lane, and how many there are up to it.
 struct Marked {
     unsigned word;
     int up_to;
@@ -694,12 +694,6 @@ struct Marked {
         }
     }
     __device__ __forceinline__ int count() const { return __shfl_sync(0xffffffffu, up_to, 31); }
-    __device__ __forceinline__ int expert(int i) const {                   // the same i in all lanes
-        const int at = __ffs(__ballot_sync(0xffffffffu, up_to > i)) - 1;
-        unsigned es = __shfl_sync(0xffffffffu, word, at);
-        for (int skip = i - (__shfl_sync(0xffffffffu, up_to, at) - __popc(es)); skip > 0; --skip) es &= es - 1;
-        return 32 * at + __ffs(es) - 1;
-    }
 };
 
 // every form is a programmatic dependent of the kernel before it in the stream (it waits for it before it reads anything)

@@ -448,7 +448,7 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                 }
                 int32_t* ids_t = ids + (size_t)(t0 + tok) * g.k;
                 float* weights_t = weights + (size_t)(t0 + tok) * g.k;
-                if (round > 0) mode = go_on<PER>(g, room, my.z64, dz, rel, lane, ids_t, weights_t);
+                if (round > 0) mode = go_on<PER>(g, room, balance, my.z64, dz, rel, lane, ids_t, weights_t);
                 const bool again = mode == GATE_WAITS || (mode != GATE_DONE && choose_fast<PER>(g, room, balance, dz, rel, lane, mode, ids_t, weights_t));
                 if (again) {                                               // it waits; its logits go back to its row
                     int at = f;

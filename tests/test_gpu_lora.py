@@ -174,6 +174,17 @@ def test_plan_of_many_tokens_and_adapters(B):
         check(out, x, a, b, scale, ids, y, rows)
 
 
+@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 1023, 1024])
+@pytest.mark.parametrize("T", [1, 33, 1023, 1025, 8193])
+def test_plan_at_its_edges(B, T, n):
+    """Steps of 32 tokens, 32 warps, 1024 threads and the steps kept in registers, each with one more and one less; ids in any order and in runs."""
+    x, a, b, scale, ids, y = inputs(T, n, 8, 64, 40, 3 * n + T)
+    for order in (ids, ids.sort().values):
+        plan = B.exmoe_lora_plan(order, n)
+        check(B.exmoe_lora(plan, x, a, b, scale, base=y), x, a, b, scale, order, y, sorted({*range(0, T, max(1, T // 40)), T - 1}))
+        assert B.exmoe_lora_plan_status(plan) == B.EXMOE_OK
+
+
 def test_a_plan_serves_its_own_sizes_only(B):
     x, a, b, scale, ids, y = inputs(10, 4, 8, 64, 32, 1)
     plan = B.exmoe_lora_plan(ids, 4)
