@@ -40,7 +40,8 @@ gate_token_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__
 }
 
 // One warp per token: the latency of a row's loads, then the choice's instructions.  16 tokens of 64 experts 2.4 us (replayed from a graph), 8191 BF16
-// rows of 256 experts, 8 of 3 of 8 groups, 8.8 us, of which the bytes would take 0.7.  Longer-lived warps that take several tokens each lost (a choice's
+// rows of 256 experts, 8 of 3 of 8 groups, 8.8 us (818 instructions a token, 6 us of issue), of which the bytes would take 0.7; 16-byte loads instead of 2-byte ones
+// changed nothing.  Longer-lived warps that take several tokens each lost (a choice's
 // latency is then in the open).  PER: experts per lane of choose_fast, 0: all in binary64.  Shared memory, per warp: logits_room(), and the balance
 // bias where choose_fast reads it.
 template <int PER>
@@ -110,14 +111,14 @@ gate_logits_kernel(const Z* logits, long long ld, int T, const __grid_constant__
 // former is larger than twice the latter + 16, all logits are computed again).  They travel through the cluster's shared
 // memory to the CTA that owns the token (i % 8), whose first warp chooses; where that rests on less than the bound, its warps
 // compute the logits that matter once more in binary64.  What bounds it is the chain of latencies: weights from memory, sums, the
-// exchange in the cluster, the choice.  64 experts of 2048, replayed from a graph: one token 5.1 us, 37 tokens 6.1, or 9.3 with a near-tie.
+// exchange in the cluster, the choice.  64 experts of 2048, replayed from a graph: one token 4.9 us, 37 tokens 6.2, or 9.0 with a near-tie.
 template <int PER>
 struct __align__(16) FewRoom {
     ChoiceRoom<PER> room;
     float balance[32 * PER];
     double z64[32 * PER];
 };
-// Four tokens per cluster from here on: 16 tokens one / four 6.6 / 7.0, 32 tokens 9.1 / 7.9 us (64 experts of 2048); 15.7 / 19.1 and 22.3 / 19.1 (256 of 4096).
+// Four tokens per cluster from here on: 16 tokens one / four 5.9 / 6.4, 32 tokens 8.6 / 7.2 us (64 experts of 2048); 16.1 / 19.2 and 23.5 / 19.2 (256 of 4096).
 constexpr int kFewCluster = 8, kFewFour = 24;
 template <int TB, int PER>
 __global__ void __launch_bounds__(kGateThreads, 2)                         // else the compiler may take 80 registers, and fewer loads are in flight: 37 tokens 6.1 -> 7.4 us
@@ -276,13 +277,13 @@ int check_gate(const exmoe_shape* shape, const exmoe_gate* gate, int T, GateArgs
 }
 
 // From how many tokens on the tensor cores (at most 256 experts) are faster than four tokens per cluster, by the size of the router's matrix.
-// us, four / tensor cores, means of four batches: 16 experts of d_model 512: 256 tokens 10.0 / 11.1, 384: 13.7 / 11.1.   64 of 2048: 192 13.2 / 14.0,
-// 256: 16.7 / 14.3.   128 of 2048: 128 15.5 / 18.0, 192: 19.8 / 18.8.   256 of 1024: 128 15.3 / 18.5, 192: 21.0 / 18.5.   64 of 4096: 128 14.3 / 16.8,
-// 192: 18.2 / 16.9.   256 of 4096: 64 27.1 / 26.8, 96: 30.2 / 28.7.
+// us, four / tensor cores, means of four batches: 16 experts of d_model 512: 256 tokens 10.2 / 10.9, 384: 13.9 / 10.9.   64 of 2048: 128 9.1 / 12.0,
+// 192: 13.7 / 12.8.   128 of 2048: 128 14.8 / 17.1, 192: 20.0 / 18.1.   256 of 1024: 128 14.9 / 16.9, 192: 20.9 / 16.9.   64 of 4096: 128 14.0 / 14.7,
+// 192: 18.2 / 14.7.   256 of 4096: 48 19.5 / 21.4, 64: 26.7 / 24.5.
 constexpr int kManyExperts = 256;
 constexpr int many_tokens(int E, int H) {
     const long long n = (long long)E * H;
-    return n <= 1 << 14 ? 288 : n <= 3 << 16 ? 200 : n <= 1 << 19 ? 160 : 72;
+    return n <= 1 << 14 ? 288 : n <= 3 << 16 ? 176 : n <= 1 << 19 ? 150 : 56;
 }
 
 // A call's kernels by the number of experts: what choose_fast holds per lane.

@@ -14,9 +14,11 @@
 // (gate.cuh).  Where a decision rests on less than the bound, the token waits; behind the others, all sixteen warps compute the logits that
 // matter in binary64, a warp per logit, and its choice goes on.
 //   What bounds it, at 8192 tokens of d_model 4096, 256 experts, 8 of 4 of 8 groups by the two largest, sigmoid with a balance bias (64
-// clusters of two): 64 us replayed from a graph, of 97 thousand cycles per CTA 38 in the main loop, 30 in its 64 tokens' choices, 19 in
-// the near-ties, the rest in start and exchange.  The main loop runs at the rate of shared memory (TMA in, MMAs and norms out: 128 bytes a
-// cycle; the tensor pipe is busy for 15 % of the kernel), the choices at that of instructions.  The bytes alone would take 10.8 us.
+// clusters of two): 58.8 us replayed from a graph, of 91 thousand cycles per CTA (106 in the last) 38 in the main loop, 31 in its 64 tokens' exchange and
+// choices, 17 in the near-ties (3 tokens, 8 logits), the rest in barriers.  The main loop runs at the rate of shared memory (a stage's 48 KB come in by TMA and
+// go out to the MMAs and to the norms: 1,150 cycles at 128 bytes each; the tensor pipe is busy for 17 % of the kernel), the choices at that of
+// instructions, the near-ties at the latency of code that few tokens run.  The bytes alone would take 10.8 us.  With eight CTAs per cluster (up to 2048 tokens) the
+// exchange takes 9 of 40 thousand cycles.
 #include <algorithm>
 
 #include "gate.cuh"
