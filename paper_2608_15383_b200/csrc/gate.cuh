@@ -303,11 +303,6 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
     mx = warp_max(mx);
     const float dzs = bound_of(g, dz, rel, mx);
     bool odd = __any_sync(0xffffffffu, any != any) || !(fabsf(mx) < INFINITY) || !(dzs <= 0.05f);
-    // quick_sigmoid is within 3.5e-7 of the true one (__expf's argument off by 2^-23 |z|, its result by 2^-22 of itself, each times s (1 - s); the quotient
-    // by 2^-22 s), a probability (an argument off by 2^-24 of itself, p |argument| < 0.37; up to 25 roundings in exponentials, sum and
-    // quotient) within 2e-6; c itself rounds once more
-    const float score_near = (g.sigmoid ? 2.f * 0.26f : 2.f * 0.55f) * dzs + (g.sigmoid ? 7e-7f : 4e-6f);
-    const float near0 = balance ? score_near : 2.f * dz, near1 = balance ? 1.2e-7f : rel;                // near = near0 + near1 (|a| + |b|)
     float sum = 1.f;
     // branches around loops that all lanes take alike, not choices per expert: both sides of these would be computed
     if (!odd && !g.sigmoid && (by_score || !g.renorm)) {
@@ -320,14 +315,21 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
             for (int i = 0; i < n; ++i) part[i] += part[i + n];
         sum = warp_sum_f32(part[0]);
     }
+    // quick_sigmoid is within 3.5e-7 of the true one (__expf's argument off by 2^-23 |z|, its result by 2^-22 of itself, each times s (1 - s); the quotient
+    // by 2^-22 s), a probability p = p_max exp(-a) (a off by 2^-24 of itself, a exp(-a) < 0.37; up to 25 roundings in exponentials, sum and quotient) within
+    // 2e-6 p_max; c itself rounds once more.  s (1 - s) is no more than 1/4, in a softmax no more than p_max either: with a hundred experts values
+    // lie p_max / 10 and less apart, and 1/4 would have most tokens' logits computed again.
+    const float p_max = 1.f / sum;
+    const float slope_near = g.sigmoid ? 2.f * 0.26f : 2.f * 2.2f * fminf(0.25f, p_max), round_near = g.sigmoid ? 7e-7f : 4e-6f * p_max;
+    const float score_near = slope_near * dzs + round_near;
+    const float near0 = balance ? score_near : 2.f * dz, near1 = balance ? 1.2e-7f : rel;                // near = near0 + near1 (|a| + |b|)
     if (!odd && by_score) {
         if (g.sigmoid) {
 #pragma unroll
             for (int i = 0; i < PER; ++i) other[i] = quick_sigmoid(by[i]);
         } else {
-            const float inv = 1.f / sum;
 #pragma unroll
-            for (int i = 0; i < PER; ++i) other[i] *= inv;
+            for (int i = 0; i < PER; ++i) other[i] *= p_max;
         }
         if (balance) {
             float bias[PER];
@@ -454,7 +456,7 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
                         const float p = g.sigmoid ? quick_sigmoid(room.z[e]) : expf(room.z[e] - mx) / sum;
                         slope = (g.sigmoid ? p : 2.f * p) * (1.f - p);
                     }
-                    close_by = near - near0 + 2.f * 1.06f * dzs * (warp_max(slope) + 1e-5f) + score_near - (g.sigmoid ? 2.f * 0.26f : 2.f * 0.55f) * dzs;
+                    close_by = near - near0 + 2.f * 1.06f * dzs * (warp_max(slope) + 1e-5f * (g.sigmoid ? 1.f : p_max)) + round_near;
                 }
 #pragma unroll 4
                 for (int j = 0; j < n; ++j) {
