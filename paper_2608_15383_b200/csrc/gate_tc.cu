@@ -145,7 +145,7 @@ constexpr int kParts = 2 * kDrainWarps;
 constexpr int kItems = 512;                                               // two tokens with all of their logits
 // A token that waits for logits to be computed again; its logits are back in its row of `part`, which no other CTA reads.
 struct Waiting {
-    int token, first;                                                      // in the tile; first item | how many << 16, -1: no room for them in this round
+    int token, first;                                                      // in the tile; first item | how many << 16, -1: there was no room for them
     float dz;
     uint32_t todo[kTodoUsed];                                              // the words of 256 experts, kTodoKept, kTodoStage
     Picks picks;
