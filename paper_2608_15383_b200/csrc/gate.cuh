@@ -552,8 +552,12 @@ static __device__ __noinline__ void choose_groups(const GateArgs& g, ChoiceRoom<
 
 // The choice among the candidates, whose marked ones' logits are exact in z64 (or z, z64 null), z being up to date: each keeps its rank among the unmarked
 // ones, from which it is far enough, and the marked ones are ranked among themselves.  False: that does not decide, and everything is to be computed again.
-// It may not for a softmax with a bias: p_e = exp(z_e - mx) / sum with a sum of logits that are off by dz leaves c_a - c_b off by dz |p_a - p_b|.
+// It may not for a softmax with a bias: p_e = exp(z_e - mx) / sum with a sum of logits that are off by dz, which is itself off by kSumRel (below)
+// of itself, leaves c_a - c_b off by (dz + kSumRel) |p_a - p_b|: also where the logits are exact, as given ones are.
 // (The whole of choose_fast once more took 10 thousand cycles of gate_8192 where this takes a third.)
+// kSumRel: choose_fast's sum in units of 2^-24: expf 4, its argument (in the mean over the probabilities, up to ln 512 of them) 6.3, 4 additions in a lane and 5
+// over the lanes: 19.3, or 1.2e-6.
+constexpr double kSumRel = 2e-6;
 template <int PER>
 static __device__ __noinline__ bool finish_choice(const GateArgs& g, ChoiceRoom<PER>& room, const float* balance, const double* z64, float dz, float rel, int lane, int32_t* ids, float* weights) {
     const int n = room.picks.n, e = lane < n ? room.picks.at[lane] & 511 : 0, was = lane < n ? room.picks.at[lane] >> 9 : 32;
@@ -576,7 +580,7 @@ static __device__ __noinline__ bool finish_choice(const GateArgs& g, ChoiceRoom<
         if (m) before += (int)(o > w || (o == w && j < lane)) - (int)(o_was < was);
         if (soft) {
             const double ob = __shfl_sync(0xffffffffu, b, j);
-            unsure |= m && j != lane && w > -INFINITY && o > -INFINITY && fabs(o - w) <= 1.1 * (double)bound_of(g, dz, rel, mx) * fabs((o - ob) - (w - b)) + 1e-12;
+            unsure |= m && j != lane && w > -INFINITY && o > -INFINITY && fabs(o - w) <= (1.1 * (double)bound_of(g, dz, rel, mx) + kSumRel) * fabs((o - ob) - (w - b)) + 1e-12;
         }
     }
     const bool chosen = lane < n && before < g.k;
