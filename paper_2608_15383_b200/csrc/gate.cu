@@ -224,13 +224,9 @@ gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w
         w2 = warp_max(w2);
 #pragma unroll
         for (int i = 0; i < kGateWarps; ++i) x2 += x2_of[i];
+        if (x2 == 0.f && any_number(xs + (size_t)rank * chunks, chunks, lane, 32)) x2 = kLeastSquare;
         // the norms come out of binary32 sums, short by less than 1 %
-        dz = 1.01f * 0x1p-24f * sqrtf(fmaxf(x2, kLeastSquare)) * sqrtf(fmaxf(w2, kLeastSquare)) + (addend ? 16.f * 0x1p-24f : 0.f);
-        if (dz < kZeroRow && !bias && !addend) {                           // a row of zeros
-            bool any = false;
-            for (int e = lane; e < g.E; e += 32) any |= z[e] != 0.f;
-            if (!__any_sync(0xffffffffu, any)) dz = 0.f;
-        }
+        dz = 1.01f * 0x1p-24f * sqrtf(least_of(x2)) * sqrtf(fmaxf(w2, kLeastSquare)) + (addend ? 16.f * 0x1p-24f : 0.f);
         if (cancelled) dz = INFINITY;
     }
     const float* balance = g.balance ? sm.balance : nullptr;

@@ -615,9 +615,21 @@ __device__ __forceinline__ int go_on(const GateArgs& g, ChoiceRoom<PER>& room, c
 
 // ---- what the kernels share --------------------------------------------------------------------------------------------
 constexpr int kGateSmemMax = 200 * 1024, kSms = 148;
-// Squares below 2^-149 are lost from a norm; where one has come out so small that this matters, it is taken to be this.  A row of zeros, whose
-// logits are exact, is then told by its logits.
-constexpr float kLeastSquare = 1e-30f, kZeroRow = 1e-12f;
+// Squares below 2^-149 are lost from a norm; where one has come out so small that this matters, it is taken to be this.  A row of zeros, or a
+// router of zeros, has exact logits and a bound of 0; where a norm has come out as 0, the numbers tell (logits that all come out as 0 do not: sums may
+// cancel).  The form for few tokens does not look at the router's: computing all logits again is quicker there than reading it once more.
+constexpr float kLeastSquare = 1e-30f;
+__device__ __forceinline__ float least_of(float sum) { return sum == 0.f ? 0.f : fmaxf(sum, kLeastSquare); }
+// Whether one of chunks lane, lane + step, ... of eight BF16 numbers is not all zeros, for any lane of the warp.
+__device__ __forceinline__ bool any_number(const uint4* p, int chunks, int lane, int step) {
+    bool any = false;
+#pragma unroll 1
+    for (int i = lane; i < chunks; i += step) {
+        const uint4 v = p[i];
+        any |= ((v.x | v.y | v.z | v.w) & 0x7fff7fffu) != 0u;
+    }
+    return __any_sync(0xffffffffu, any);
+}
 constexpr float kAddedRel = 3.f * 0x1p-24f;                                // bias and addend: 2^-24 (|sum before| + |z|), with |sum before| <= 2 |z| + 16
 
 __device__ __forceinline__ void unpack8(const uint4& a, float (&x)[8]) {

@@ -341,8 +341,19 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         float w2 = 0.f;
 #pragma unroll
         for (int i = 0; i < kDrainWarps; ++i) w2 = fmaxf(w2, sm.w2_max[i]);
-        const int u = tid - 128;                                           // the bound for this part of K, with the largest |w| of all experts
-        if ((u & 3) == 0) sm.size[u >> 2] = w2 < INFINITY ? sqrtf(fmaxf(x2, kLeastSquare)) * sqrtf(fmaxf(w2, kLeastSquare)) : INFINITY;
+        const int c0 = 8 * kb0, chunks = min(8 * n, H / 8 - c0);           // this part of K
+        if (w2 == 0.f) {                                                   // the same for all warps
+            bool any = false;
+            for (int e = d; e < g.E && !any; e += kDrainWarps) any = any_number(reinterpret_cast<const uint4*>(w_router + (size_t)e * H) + c0, chunks, lane, 32);
+            w2 = choosers_or(any) ? kLeastSquare : 0.f;
+        }
+        const int u = tid - 128;                                           // the bound for this part, with the largest |w| of all experts
+        for (unsigned rows = __ballot_sync(0xffffffffu, x2 == 0.f) & 0x11111111u; rows; rows &= rows - 1) {
+            const int from = __ffs(rows) - 1;
+            const long long t = t0 + ((u & ~31) + from >> 2);
+            if (t < T && any_number(reinterpret_cast<const uint4*>(hidden + t * H) + c0, chunks, lane, 32) && lane == from) x2 = kLeastSquare;
+        }
+        if ((u & 3) == 0) sm.size[u >> 2] = w2 < INFINITY ? sqrtf(least_of(x2)) * sqrtf(least_of(w2)) : INFINITY;
     }
     cluster_arrive();
     cluster_wait();
@@ -394,11 +405,6 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                     if (t0 + tok >= T) break;
                     float size = 0.f;
                     load_logits<PER>(smem_u32(&sm.s.part[tok][0]), smem_u32(&sm.size[tok]), rank, CL, lane, room.z, size);
-                    if (size < kZeroRow) {                                 // a row of zeros
-                        bool any = false;
-                        for (int e = lane; e < g.E; e += 32) any |= room.z[e] != 0.f;
-                        if (!__any_sync(0xffffffffu, any)) size = 0.f;
-                    }
                     dz = 1.02f * 0x1p-24f * size + (addend ? 16.f * 0x1p-24f : 0.f);       // the norms are short by less than 2 %
                     if (bias || addend || g.E < 32 * PER) {
                         bool cancelled = false;

@@ -86,3 +86,25 @@ def test_softmax_with_balance_bias_on_hidden_rows_of_small_norm(B, T):
         ids, _ = B.exmoe_route_gated(shape(H, E, 1), B.Gate(), x.cuda(), w.cuda(), balance=torch.from_numpy(balance).cuda())
         ref, _ = ogate.choose_token(z, B.Gate(), 1, balance)
         assert (ids.cpu().numpy() == ref).all(), (i, gap)
+
+
+@pytest.mark.parametrize("E,T", [(128, 1), (128, 30), (100, 3), (128, 300), (60, 700)])
+def test_rows_of_tiny_norm_whose_sums_cancel(B, E, T):
+    """Logits that come out as 0 in binary32 and are not: c - c + w_e 2^-100, c = 2^-60.  Only a row of zeros, or a router of zeros, has logits that are 0 by themselves."""
+    H, k = 64, min(8, E)
+    order = torch.from_numpy(np.random.default_rng(E).permutation(128)[:E])
+    w = torch.zeros(E, H)
+    w[:, 0] = w[:, 2] = 1.0
+    w[:, 1] = 1.0 + order / 128.0
+    x = torch.zeros(T, H)
+    x[:, 0], x[:, 1], x[:, 2] = 2.0 ** -60, 2.0 ** -100, -2.0 ** -60
+    if T > 1:
+        x[T // 2] = 0.0
+    for kw in (dict(), dict(score="sigmoid", renormalise=True)):
+        hidden, router, gate = x.to(torch.bfloat16), w.to(torch.bfloat16), B.Gate(**kw)
+        ids, weights = B.exmoe_route_gated(shape(H, E, k), gate, hidden.cuda(), router.cuda())
+        ref, ref_w = ogate.choose(ogate.logits(hidden.double().numpy(), router.double().numpy()), gate, k)
+        assert np.array_equal(ids.cpu().numpy(), ref)
+        np.testing.assert_allclose(weights.cpu().numpy(), ref_w, rtol=WEIGHT)
+        ids, _ = B.exmoe_route_gated(shape(H, E, k), gate, hidden.cuda(), torch.zeros_like(router).cuda())
+        assert (ids.cpu() == torch.arange(k)).all()
