@@ -32,7 +32,7 @@ gate_token_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__
     for (int i = tid; i < chunks; i += kGateThreads) xs[i] = xrow[i];
     __syncthreads();
     for (int e = warp; e < g.E; e += kGateWarps) {
-        const double s = logit_f64(xs, reinterpret_cast<const uint4*>(w_router + (size_t)e * H), 0, chunks, lane);
+        const double s = logit_f64<true>(xs, reinterpret_cast<const uint4*>(w_router + (size_t)e * H), 0, chunks, lane);
         if (lane == 0) z[e] = s + (bias ? (double)bias[e] : 0.0) + (addend ? (double)addend[t * g.E + e] : 0.0);
     }
     __syncthreads();
@@ -241,7 +241,7 @@ gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w
             for (unsigned es = room.todo[b]; es; es &= es - 1, ++item) {
                 if (item % kGateWarps != warp) continue;
                 const int e = 32 * b + __ffs(es) - 1;
-                const double v = logit_f64(xs + (size_t)rank * chunks, reinterpret_cast<const uint4*>(w_router + (size_t)e * H), 0, chunks, lane);
+                const double v = logit_f64<true>(xs + (size_t)rank * chunks, reinterpret_cast<const uint4*>(w_router + (size_t)e * H), 0, chunks, lane);
                 if (lane == 0) sm.z64[e] = v + (bias ? (double)bias[e] : 0.0) + (addend ? (double)addend[t * g.E + e] : 0.0);
             }
         __syncthreads();

@@ -615,10 +615,11 @@ __device__ __forceinline__ int go_on(const GateArgs& g, ChoiceRoom<PER>& room, c
 
 // ---- what the kernels share --------------------------------------------------------------------------------------------
 constexpr int kGateSmemMax = 200 * 1024, kSms = 148;
-// Squares below 2^-149 are lost from a norm; where one has come out so small that this matters, it is taken to be this.  A row of zeros, or a
+// Squares below 2^-149 are lost from a norm, and products below 2^-126 may be from a logit; where a norm has come out so small that this matters, it is taken
+// to be this: 2^-24 of two such norms' product is more than 102,400 products of 2^-126.  A row of zeros, or a
 // router of zeros, has exact logits and a bound of 0; where a norm has come out as 0, the numbers tell (logits that all come out as 0 do not: sums may
 // cancel).  The form for few tokens does not look at the router's: computing all logits again is quicker there than reading it once more.
-constexpr float kLeastSquare = 1e-30f;
+constexpr float kLeastSquare = 1e-25f;
 __device__ __forceinline__ float least_of(float sum) { return sum == 0.f ? 0.f : fmaxf(sum, kLeastSquare); }
 // Whether one of chunks lane, lane + step, ... of eight BF16 numbers is not all zeros, for any lane of the warp.
 __device__ __forceinline__ bool any_number(const uint4* p, int chunks, int lane, int step) {
@@ -654,8 +655,25 @@ __device__ __forceinline__ float square8(const uint4& a) {
     unpack8(a, x);
     return dot8(x, x);
 }
-// A logit, or what chunks `from` .. `to` - 1 of eight numbers add to it, by one warp in binary64; products of BF16 values are exact in
-// binary32.  Conversions to binary64 bound it (16 a cycle and SM).
+// What chunks `from` .. `to` - 1 of eight numbers add to a logit, by one warp in binary64.
+static __device__ __noinline__ double logit_wide(const uint4* x, const uint4* w, int from, int to, int lane) {
+    double s = 0.0;
+#pragma unroll 1
+    for (int i = from + lane; i < to; i += 32) {
+        float a[8], b[8];
+        unpack8(w[i], a);
+        unpack8(x[i], b);
+#pragma unroll
+        for (int n = 0; n < 8; ++n) s += (double)a[n] * (double)b[n];
+    }
+    return warp_sum_f64(s);
+}
+// Products of BF16 values are exact in binary32 between 2^-126 and 2^128.  Above, a sum of them is an infinity or a NaN; below, they are off by 2^-150, which a
+// sum of 2^-66 and more does not hold.
+__device__ __forceinline__ bool needs_wide(double s) { return !(fabs(s) >= 0x1p-66 && fabs(s) < (double)INFINITY); }
+// The same with products in binary32; WIDE: by logit_wide where the sum needs it, otherwise the caller sees to that.  Conversions to binary64 bound it (16 a cycle
+// and SM), half as many as there.
+template <bool WIDE>
 static __device__ __noinline__ double logit_f64(const uint4* x, const uint4* w, int from, int to, int lane) {
     constexpr int U = 2;                                                   // chunks at a time (little code: it is mostly cold), the next ones in flight
     double s[4 * U] = {};
@@ -692,7 +710,8 @@ static __device__ __noinline__ double logit_f64(const uint4* x, const uint4* w, 
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) s[j] += s[4 + j];
-    return warp_sum_f64((s[0] + s[1]) + (s[2] + s[3]));
+    const double sum = warp_sum_f64((s[0] + s[1]) + (s[2] + s[3]));
+    return WIDE && needs_wide(sum) ? logit_wide(x, w, from, to, lane) : sum;
 }
 // Into how many parts (a power of two, up to eight) the warps of a CTA share the sums of `items` logits: no more than `most` parts in all.
 __device__ __forceinline__ int log_parts(int items, int most) {

@@ -162,7 +162,7 @@ struct __align__(1024) Shared {
     };
     float size[kTokens], balance[32 * PER];
     float w2_max[kDrainWarps];
-    int n_waiting, n_items;
+    int n_waiting, n_items, wide;
     Waiting waiting[kTokens];
     double item_z[kItems];                                                 // logits to compute again
     unsigned short item_expert[kItems], item_waiting[kItems];
@@ -194,7 +194,7 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         }
         mbar_init(&sm.drained, 1);
         sm.abort_flag = 0;
-        sm.n_waiting = sm.n_items = 0;
+        sm.n_waiting = sm.n_items = sm.wide = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {
@@ -384,17 +384,23 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                 choosers_sync();
                 const int n_items = min(sm.n_items, kItems);
                 log_p = log_parts(n_items, kParts);
-                for (int u = d; u < n_items << log_p; u += kDrainWarps) {
-                    const int j = u >> log_p, part = u & ((1 << log_p) - 1), e = sm.item_expert[j];
-                    const long long t = t0 + sm.waiting[sm.item_waiting[j]].token;
-                    const float b = bias && part == 0 ? bias[e] : 0.f, add = addend && part == 0 ? addend[(size_t)t * g.E + e] : 0.f;
-                    double z = logit_f64(reinterpret_cast<const uint4*>(hidden + t * H), reinterpret_cast<const uint4*>(w_router + (size_t)e * H), chunks * part >> log_p,
-                                         chunks * (part + 1) >> log_p, lane);
-                    z += (double)b;
-                    z += (double)add;
-                    if (lane == 0) sm.item_z[u] = z;
+                // once more with logit_wide where one of the sums needs it (from then on in every round)
+                for (bool wide = false;; wide = true) {
+                    for (int u = d; u < n_items << log_p; u += kDrainWarps) {
+                        const int j = u >> log_p, part = u & ((1 << log_p) - 1), e = sm.item_expert[j];
+                        const long long t = t0 + sm.waiting[sm.item_waiting[j]].token;
+                        const float b = bias && part == 0 ? bias[e] : 0.f, add = addend && part == 0 ? addend[(size_t)t * g.E + e] : 0.f;
+                        const uint4 *x = reinterpret_cast<const uint4*>(hidden + t * H), *w = reinterpret_cast<const uint4*>(w_router + (size_t)e * H);
+                        const int from = chunks * part >> log_p, to = chunks * (part + 1) >> log_p;
+                        double z = wide ? logit_wide(x, w, from, to, lane) : logit_f64<false>(x, w, from, to, lane);
+                        if (lane == 0 && !wide && needs_wide(z)) sm.wide = 1;
+                        z += (double)b;
+                        z += (double)add;
+                        if (lane == 0) sm.item_z[u] = z;
+                    }
+                    choosers_sync();
+                    if (wide || !sm.wide) break;
                 }
-                choosers_sync();
                 if (tid == 128) sm.n_items = 0;
             }
             bool open = false;

@@ -108,3 +108,27 @@ def test_rows_of_tiny_norm_whose_sums_cancel(B, E, T):
         np.testing.assert_allclose(weights.cpu().numpy(), ref_w, rtol=WEIGHT)
         ids, _ = B.exmoe_route_gated(shape(H, E, k), gate, hidden.cuda(), torch.zeros_like(router).cuda())
         assert (ids.cpu() == torch.arange(k)).all()
+
+
+@pytest.mark.parametrize("E,T", [(16, 1), (16, 30), (16, 300), (600, 2)])
+@pytest.mark.parametrize("hidden_at,router_at", [(70, 60), (100, 100), (-70, -70), (-80, -60), (-100, -30), (-63, -63), (-120, -120)])
+def test_products_beyond_binary32(B, E, T, hidden_at, router_at):
+    """Products of BF16 numbers that binary32 holds as an infinity, as a subnormal number, or as zero."""
+    H, k = 64, 5
+    rng = np.random.default_rng(E + T)
+    x = torch.from_numpy(rng.uniform(1, 2, (T, H)) * rng.choice([-1, 1], (T, H)) * 2.0 ** hidden_at).to(torch.bfloat16)
+    w = torch.from_numpy(rng.uniform(1, 2, (E, H)) * rng.choice([-1, 1], (E, H)) * 2.0 ** router_at).to(torch.bfloat16)
+    x[0, 1::2] = 0.0
+    z = ogate.logits(x.double().numpy(), w.double().numpy())
+    for kw in (dict(), dict(score="sigmoid", renormalise=True), dict(renormalise=True, num_groups=2)):
+        gate = B.Gate(**kw)
+        ids, weights = B.exmoe_route_gated(shape(H, E, k), gate, x.cuda(), w.cuda())
+        ref, ref_w = ogate.choose(z, gate, k)
+        assert np.array_equal(ids.cpu().numpy(), ref)
+        np.testing.assert_allclose(weights.cpu().numpy(), ref_w, rtol=WEIGHT, atol=2.0 ** -126)
+    mask = torch.zeros(T, E)
+    mask[torch.from_numpy(rng.random((T, E)) < 0.3)] = -np.inf
+    ids, weights = B.exmoe_route_gated(shape(H, E, k), B.Gate(), x.cuda(), w.cuda(), addend=mask.cuda())
+    ref, ref_w = ogate.choose(z + mask.double().numpy(), B.Gate(), k)
+    assert np.array_equal(ids.cpu().numpy(), ref)
+    np.testing.assert_allclose(weights.cpu().numpy(), ref_w, rtol=WEIGHT, atol=2.0 ** -126)
