@@ -524,6 +524,7 @@ lora_kernel(LoraArgs p, int log_cl, bool one_hop) {
         else
             all = *reinterpret_cast<const float4*>(received + TM * RP + i);
         float v[4] = {all.x, all.y, all.z, all.w};
+        if (i % RP >= p.r) v[0] = v[1] = v[2] = v[3] = 0.f;                // behind the rank: an infinity in x made 0 x infinity of the zeros there
 #pragma unroll
         for (int n = 0; n < S::SPLIT; ++n) {
             __nv_bfloat16 h[4];
