@@ -700,7 +700,7 @@ extern "C" int exmoe_lora(const exmoe_lora_shape* shape, void* plan, const void*
     size_t plan_size = 0;
     exmoe_lora_plan_bytes(T, n, &plan_size);
     const Range o = range(out, T, ld_out, N, es), bs = range(base, T, ld_base, N, es);
-    if ((!(base == out && ld_base == ld_out) && overlap(o, bs)) || overlap(o, range(x, T, ld_x, K, 2)) || overlap(o, range(a, 1, 0, (long long)n * r * K, 2)) ||
+    if ((!(base == out && (ld_base == ld_out || T == 1)) && overlap(o, bs)) || overlap(o, range(x, T, ld_x, K, 2)) || overlap(o, range(a, 1, 0, (long long)n * r * K, 2)) ||
         overlap(o, range(b, 1, 0, (long long)n * r * N, 2)) || overlap(o, range(scale, 1, 0, n, 4)) || overlap(o, range(plan, 1, 0, (long long)plan_size, 1)))
         return EXMOE_ERR_ARG;
     const LoraArgs args{(int32_t*)plan, (const __nv_bfloat16*)x, (const __nv_bfloat16*)a, (const __nv_bfloat16*)b, scale, base, out,

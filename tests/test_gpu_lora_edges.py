@@ -43,3 +43,16 @@ def test_infinities_as_the_definition_gives_them(B, r, T, dtype):
     assert np.isinf(ref).any() and np.isnan(ref[:, 1::2]).any()
     assert np.array_equal(np.isnan(out), np.isnan(ref))
     assert np.array_equal(np.where(np.isinf(out), np.sign(out), 0), np.where(np.isinf(ref), np.sign(ref), 0))
+
+
+def test_one_row_in_place_whatever_its_distance_to_the_next(B):
+    """A single row has no row behind it: base and out are the same where their addresses are."""
+    g = torch.Generator().manual_seed(1)
+    n, r, K, N = 2, 8, 64, 40
+    x, a, b, scale = normal(g, 1.0, 1, K).cuda(), normal(g, 0.1, n, r, K).cuda(), normal(g, 0.1, n, N, r).cuda(), torch.ones(n, device="cuda")
+    wide = normal(g, 1.0, 1, 2 * N).cuda()
+    plan = B.exmoe_lora_plan(torch.zeros(1, dtype=torch.int32, device="cuda"), n)
+    want = B.exmoe_lora(plan, x, a, b, scale, base=wide[:, :N])
+    out = wide.as_strided((1, N), (N, 1))
+    assert B.exmoe_lora(plan, x, a, b, scale, base=wide[:, :N], out=out) is out
+    assert torch.equal(out, want)
