@@ -226,6 +226,7 @@ typedef struct {
  *                  (exmoe_lora), noise, or -infinity for experts it may not use
  *   balance      : dev, float32 [E], or NULL
  *   topk_ids     : dev, int32 [T, k]                      topk_weights : dev, float32 [T, k]
+ * Every pointer, here and below, at least aligned to its type (EXMOE_ERR_ARG).
  * Limits as exmoe_route's: d_model a multiple of 8, num_experts <= 4096, 2 * d_model + 16 * num_experts <= 204,800 bytes; and T <= 2^29.
  * Asynchronous on `stream`; allocates nothing; T = 0 is a no-op.  EXMOE_ERR_SHAPE / EXMOE_ERR_ARG before any work is queued. */
 int exmoe_route_gated(const exmoe_shape* shape, const exmoe_gate* gate, const void* hidden_bf16, const void* router_bf16,

@@ -98,6 +98,10 @@ constexpr int kPairMaxPairs = 32;
 constexpr int kSmallMaxPairs = EXMOE_SMALL_MAX_PAIRS;
 constexpr int kSmallMaxSlots = 1024;
 
+// whether all addresses are multiples of `bytes`, a power of two
+template <typename... P>
+inline bool aligned(size_t bytes, const P*... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) & (bytes - 1)) == 0; }
+
 // launch accounting (exmoe_launch_count)
 void count_launch(int n = 1);
 

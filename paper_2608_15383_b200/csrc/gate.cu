@@ -326,7 +326,7 @@ extern "C" int exmoe_route_gated(const exmoe_shape* shape, const exmoe_gate* gat
     if (H <= 0 || H % 8 || 2 * (size_t)H + 16 * (size_t)g.E > (size_t)kGateSmemMax) return EXMOE_ERR_SHAPE;
     if (T == 0) return EXMOE_OK;
     if (!hidden_bf16 || !router_bf16 || !topk_ids || !topk_weights) return EXMOE_ERR_ARG;
-    if ((reinterpret_cast<uintptr_t>(hidden_bf16) | reinterpret_cast<uintptr_t>(router_bf16)) & 15) return EXMOE_ERR_ARG;
+    if (!aligned(16, hidden_bf16, router_bf16) || !aligned(4, bias, addend, balance, topk_ids, topk_weights)) return EXMOE_ERR_ARG;
     g.balance = balance;
     const __nv_bfloat16 *x = (const __nv_bfloat16*)hidden_bf16, *w = (const __nv_bfloat16*)router_bf16;
     cudaStream_t st = (cudaStream_t)stream;
@@ -345,6 +345,7 @@ extern "C" int exmoe_gate_logits(const exmoe_shape* shape, const exmoe_gate* gat
     if ((type != EXMOE_F32 && type != EXMOE_BF16) || row_stride < 0 || (T > 1 && row_stride < g.E)) return EXMOE_ERR_ARG;
     if (T == 0) return EXMOE_OK;
     if (!logits || !topk_ids || !topk_weights) return EXMOE_ERR_ARG;
+    if (!aligned(type == EXMOE_F32 ? 4 : 2, logits) || !aligned(4, balance, topk_ids, topk_weights)) return EXMOE_ERR_ARG;
     g.balance = balance;
     cudaStream_t st = (cudaStream_t)stream;
     return type == EXMOE_F32 ? launch_logits((const float*)logits, row_stride, T, g, topk_ids, topk_weights, st)

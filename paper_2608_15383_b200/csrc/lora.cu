@@ -650,7 +650,7 @@ extern "C" int exmoe_lora_plan_bytes(int T, int num_adapters, size_t* bytes) {
 extern "C" int exmoe_lora_plan(const int32_t* adapter_ids, int T, int num_adapters, void* plan, void* stream) {
     const int rc = check_plan(T, num_adapters);
     if (rc) return rc;
-    if ((!adapter_ids && T) || !plan || (reinterpret_cast<uintptr_t>(plan) & 15)) return EXMOE_ERR_ARG;
+    if ((!adapter_ids && T) || !plan || !aligned(4, adapter_ids) || !aligned(16, plan)) return EXMOE_ERR_ARG;
     const size_t smem = 4 * (size_t)(kPlanWarps + 3) * (num_adapters + 1);
     static SmemOnce once;
     if (!allow_smem(lora_plan_kernel, 4 * (kPlanWarps + 3) * (kMaxAdapters + 1), once)) return EXMOE_ERR_CUDA;
@@ -691,9 +691,8 @@ extern "C" int exmoe_lora(const exmoe_lora_shape* shape, void* plan, const void*
     if (T == 0) return EXMOE_OK;
     if (!plan || !x || !a || !b || !scale || !out) return EXMOE_ERR_ARG;
     if (ld_x < K || ld_x % 8 || ld_out < N || (base && ld_base < N)) return EXMOE_ERR_ARG;
-    if ((reinterpret_cast<uintptr_t>(plan) | reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(a) | reinterpret_cast<uintptr_t>(b)) & 15)
-        return EXMOE_ERR_ARG;
     const long long es = type == EXMOE_F32 ? 4 : 2;
+    if (!aligned(16, plan, x, a, b) || !aligned(4, scale) || !aligned(es, base, out)) return EXMOE_ERR_ARG;
     auto range = [](const void* p, long long rows, long long ld, long long width, long long es) {
         return Range{reinterpret_cast<uintptr_t>(p), rows, ld * es, width * es};
     };
