@@ -263,9 +263,9 @@ typedef struct {
  * Asynchronous on `stream`; a plan of T = 0 tokens is one too; T <= 2^29. */
 int exmoe_lora_plan_bytes(int T, int num_adapters, size_t* bytes);
 int exmoe_lora_plan(const int32_t* adapter_ids, int T, int num_adapters, void* plan, void* stream);
-/* What the device found in a plan's ids or in its use (synchronises the device): EXMOE_OK, EXMOE_ERR_BAD_ADAPTER_ID, or
- * EXMOE_ERR_STATE where exmoe_lora was called with a T or a number of adapters that are not the plan's (its outputs were then left as
- * they were). */
+/* What the device found in a plan's ids or in its use (synchronises the device): EXMOE_OK, EXMOE_ERR_BAD_ADAPTER_ID, EXMOE_ERR_STATE where exmoe_lora was
+ * called with a T or a number of adapters that are not the plan's (its outputs were then left as they were), or EXMOE_ERR_TIMEOUT where a bounded wait of exmoe_lora
+ * expired (some of its outputs may then be left as they were).  The plan keeps it until it is made anew. */
 int exmoe_lora_plan_status(const void* plan);
 
 /* One projection's adapters.
@@ -381,6 +381,14 @@ int exmoe_debug_read_slot(exmoe_cache* cache, int layer, int slot, void* host_ou
  * barrier that nothing completes.  *gave_up gets bit 0 = the wait returned "expired", bit 1 = the abort flag was
  * raised; exmoe_status() then reports EXMOE_ERR_TIMEOUT.  Synchronous. */
 int exmoe_debug_wait_timeout(exmoe_cache* cache, long long budget_cycles, int* gave_up);
+/* The same of the kernels of the gate and of the adapters that wait: one call of exmoe_route_gated's tensor-core form (E <= 64, d_model >= 1024, no bias, addend or
+ * balance) and one of exmoe_lora (BF16, no base, rows without gaps, rank <= 64, T < 592, few enough tiles for clusters) with a barrier that nothing completes and a
+ * budget of 2,000,000 ticks.  exmoe_gate_status and exmoe_lora_plan_status then report EXMOE_ERR_TIMEOUT; what was written is not to be used.  Asynchronous on `stream`;
+ * EXMOE_ERR_SHAPE for other sizes. */
+int exmoe_debug_gate_timeout(const exmoe_shape* shape, const exmoe_gate* gate, const void* hidden_bf16, const void* router_bf16, int T, int32_t* topk_ids,
+                             float* topk_weights, void* stream);
+int exmoe_debug_lora_timeout(const exmoe_lora_shape* shape, void* plan, const void* x, const void* a, const void* b, const float* scale, int T, void* out,
+                             void* stream);
 
 /* Counters of one layer's cache (Sec. 4.2: hit rate and transferred bytes are reported per configuration).  Synchronises. */
 int exmoe_cache_stats(exmoe_cache* cache, int layer, exmoe_stats* out);

@@ -77,6 +77,8 @@ _SIGNATURES = {
     "exmoe_lora_plan_status": (c_int, [c_void_p]),
     "exmoe_lora": (c_int, [POINTER(exmoe_lora_shape), c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int, c_void_p,
                            c_int64, c_void_p, c_int64, c_int, c_void_p]),
+    "exmoe_debug_gate_timeout": (c_int, [POINTER(exmoe_shape), POINTER(exmoe_gate), c_void_p, c_void_p, c_int] + [c_void_p] * 3),
+    "exmoe_debug_lora_timeout": (c_int, [POINTER(exmoe_lora_shape)] + [c_void_p] * 5 + [c_int, c_void_p, c_void_p]),
     "exmoe_cache_get_state": (c_int, [c_void_p, c_int, c_void_p, c_void_p, c_void_p, c_void_p]),
     "exmoe_debug_last_plan": (c_int, [c_void_p, c_int] + [c_void_p] * 9),
     "exmoe_debug_last_path": (c_int, [c_void_p]),
@@ -257,7 +259,7 @@ def exmoe_lora_plan(adapter_ids, num_adapters, plan=None, stream=None):
 
 
 def exmoe_lora_plan_status(plan):
-    """EXMOE_OK, EXMOE_ERR_BAD_ADAPTER_ID or EXMOE_ERR_STATE: what the device found in the plan's ids or its use (synchronises)."""
+    """EXMOE_OK, EXMOE_ERR_BAD_ADAPTER_ID, EXMOE_ERR_STATE or EXMOE_ERR_TIMEOUT: what the device found in the plan's ids or its use (synchronises)."""
     if plan.numel() < 16 or plan.device.index != torch.cuda.current_device():      # shorter than any plan's header
         raise ValueError("plan: need one of exmoe_lora_plan on the current CUDA device")
     return int(lib().exmoe_lora_plan_status(_dev(plan, torch.int32, "plan")))

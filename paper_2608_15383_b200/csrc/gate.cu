@@ -337,6 +337,18 @@ extern "C" int exmoe_route_gated(const exmoe_shape* shape, const exmoe_gate* gat
     return launch(gate_token_kernel, (unsigned)T, kGateThreads, 1, 2 * (size_t)H + 16 * (size_t)g.E, once, st, x, w, bias, addend, H, g, topk_ids, topk_weights);
 }
 
+extern "C" int exmoe_debug_gate_timeout(const exmoe_shape* shape, const exmoe_gate* gate, const void* hidden_bf16, const void* router_bf16, int T, int32_t* topk_ids,
+                                       float* topk_weights, void* stream) {
+    GateArgs g;
+    const int rc = check_gate(shape, gate, T, &g);
+    if (rc) return rc;
+    const int H = shape->d_model;
+    if (g.E > 64 || g.k > kFastChoices || H % 8 || H < 1024 || 2 * (size_t)H + 16 * (size_t)g.E > (size_t)kGateSmemMax) return EXMOE_ERR_SHAPE;
+    if (T == 0 || !hidden_bf16 || !router_bf16 || !topk_ids || !topk_weights) return EXMOE_ERR_ARG;
+    if (!aligned(16, hidden_bf16, router_bf16) || !aligned(4, topk_ids, topk_weights)) return EXMOE_ERR_ARG;
+    return launch_gate_tc_stuck((const __nv_bfloat16*)hidden_bf16, (const __nv_bfloat16*)router_bf16, T, H, g, topk_ids, topk_weights, (cudaStream_t)stream);
+}
+
 extern "C" int exmoe_gate_logits(const exmoe_shape* shape, const exmoe_gate* gate, const void* logits, int type, int64_t row_stride,
                                  const float* balance, int T, int32_t* topk_ids, float* topk_weights, void* stream) {
     GateArgs g;

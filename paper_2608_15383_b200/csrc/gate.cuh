@@ -765,5 +765,6 @@ int launch(void (*kern)(P...), unsigned ctas, int threads, int cluster, size_t s
 // Many tokens, at most 256 experts: the logits on tensor cores (gate_tc.cu).
 int launch_gate_tc(const __nv_bfloat16* x, const __nv_bfloat16* w, const float* bias, const float* addend, int T, int H, const GateArgs& g, int32_t* ids,
                    float* weights, cudaStream_t st);
+int launch_gate_tc_stuck(const __nv_bfloat16* x, const __nv_bfloat16* w, int T, int H, const GateArgs& g, int32_t* ids, float* weights, cudaStream_t st);
 
 }  // namespace exmoe

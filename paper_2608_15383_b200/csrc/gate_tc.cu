@@ -116,9 +116,9 @@ __device__ __forceinline__ void square(__nv_bfloat162& sum, const uint4& v) {
     }
 }
 
-__device__ __forceinline__ void in_flight_end(uint32_t bar, uint32_t parity) {
+__device__ __forceinline__ void in_flight_end(uint32_t bar, uint32_t parity, long long budget) {
     const long long t0 = clock64();
-    while (!mbar_try_at(bar, parity) && clock64() - t0 < kWaitBudget) {}
+    while (!mbar_try_at(bar, parity) && clock64() - t0 < budget) {}
 }
 
 // the choosing warps' barrier
@@ -171,12 +171,14 @@ struct __align__(1024) Shared {
     int abort_flag;
 };
 
-template <int MT, int PER>
+// STUCK (exmoe_debug_gate_timeout): the second stage's barrier asks for an arrival that nobody makes.
+template <int MT, int PER, bool STUCK>
 __global__ void __launch_bounds__(kThreads, 1)
 gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x, const __nv_bfloat16* hidden,
                const __nv_bfloat16* __restrict__ w_router, const float* __restrict__ bias, const float* addend, int T, int H,
                const __grid_constant__ GateArgs g, int CL, int32_t* ids, float* weights) {
     using S = Shared<MT, PER>;
+    constexpr long long budget = STUCK ? kWaitBudgetTest : kWaitBudget;
     constexpr int COLS = MT * 128 / 4;                      // accumulator columns of a drain warp: a quarter of them, on its 32 lanes
     extern __shared__ unsigned char raw[];
     S& sm = *reinterpret_cast<S*>(raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u));
@@ -185,7 +187,7 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     volatile int* abort_flag = &sm.abort_flag;
     if (tid == 0) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(&sm.full[s], 1);
+            mbar_init(&sm.full[s], STUCK && s == 1 ? 2 : 1);
             mbar_init(&sm.empty[s], 1 + kDrainWarps);                      // the MMAs and the warps that add up the squares
         }
         for (int b = 0; b < 2; ++b) {
@@ -230,11 +232,11 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                 if (i0 + s >= n) break;
                 const int buf = s / kChain & 1, use = s / (2 * kChain), next = (s + 1) % kStages;
                 if (s % kChain == 0 && (i0 > 0 || use > 0)) {              // the accumulator's use number i0 / kStages * kTurns + use
-                    ok = mbar_wait_warp(acc_empty + 8 * buf, (kTurns % 2 ? turn + use + 1 : use + 1) & 1, abort_flag, &g_gate_status);
+                    ok = mbar_wait_warp(acc_empty + 8 * buf, (kTurns % 2 ? turn + use + 1 : use + 1) & 1, abort_flag, &g_gate_status, budget);
                     if (!ok) break;
                 }
                 if (!ready) {
-                    ok = mbar_wait_warp(full + 8 * s, turn, abort_flag, &g_gate_status);
+                    ok = mbar_wait_warp(full + 8 * s, turn, abort_flag, &g_gate_status, budget);
                     if (!ok) break;
                 }
                 tc_fence_after();
@@ -254,13 +256,13 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         if (!ok) {                                                         // given up: the MMAs in flight end before their operands' memory is used again
             if (elect_one()) tc_commit_at(smem_u32(&sm.drained));
             __syncwarp();
-            in_flight_end(smem_u32(&sm.drained), 0);
+            in_flight_end(smem_u32(&sm.drained), 0, budget);
         }
     } else if (warp == 1) {
         int i = 0;
         for (; i < n; ++i) {
             const int s = i % kStages;
-            if (i >= kStages) ok = mbar_wait_warp(empty + 8 * s, (i / kStages - 1) & 1, abort_flag, &g_gate_status);
+            if (i >= kStages) ok = mbar_wait_warp(empty + 8 * s, (i / kStages - 1) & 1, abort_flag, &g_gate_status, budget);
             if (!ok) break;
             if (elect_one()) {
                 mbar_expect_tx(&sm.full[s], S::kStage);
@@ -269,7 +271,7 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
             }
             __syncwarp();
         }
-        for (int j = max(0, i - kStages); j < i; ++j) in_flight_end(full + 8 * (j % kStages), (j / kStages) & 1);   // and so do the copies
+        for (int j = max(0, i - kStages); j < i; ++j) in_flight_end(full + 8 * (j % kStages), (j / kStages) & 1, budget);   // and so do the copies
     } else if (warp < 4) {
         for (int e = tid - 64; e < 32 * PER; e += 64) sm.balance[e] = g.balance && e < g.E ? g.balance[e] : 0.f;
     } else {
@@ -279,7 +281,7 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         float w2 = 0.f;
         for (int i = 0; i < n; ++i) {
             const int s = i % kStages, c = i / kChain, buf = c & 1;
-            ok = mbar_wait_warp(full + 8 * s, (i / kStages) & 1, abort_flag, &g_gate_status);
+            ok = mbar_wait_warp(full + 8 * s, (i / kStages) & 1, abort_flag, &g_gate_status, budget);
             if (!ok) break;
             const __nv_bfloat162 zero(__float2bfloat16(0.f), __float2bfloat16(0.f));
             __nv_bfloat162 a[2] = {zero, zero}, b[WQ];
@@ -308,7 +310,7 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
             for (int j = 0; j < WQ; j += 2)
                 w2 = fmaf(cost((MT == 2 ? 2 * (u & 1) : u & 3) + j / 2), __low2float(b[j]) + __high2float(b[j]) + (__low2float(b[j + 1]) + __high2float(b[j + 1])), w2);
             if (i % kChain < kChain - 1 && i < n - 1) continue;
-            ok = mbar_wait_warp(acc_full + 8 * buf, (c >> 1) & 1, abort_flag, &g_gate_status);
+            ok = mbar_wait_warp(acc_full + 8 * buf, (c >> 1) & 1, abort_flag, &g_gate_status, budget);
             if (!ok) break;
             tc_fence_after();
             const uint32_t at = tmem + ((uint32_t)(32 * quarter) << 16) + buf * MT * 128 + col0;
@@ -497,7 +499,7 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
     cluster_wait();                                                        // nobody reads this CTA's shared memory any more
 }
 
-template <int MT, int PER>
+template <int MT, int PER, bool STUCK = false>
 int launch_tc(const __nv_bfloat16* x, const __nv_bfloat16* w, const float* bias, const float* addend, int T, int H, const GateArgs& g, int32_t* ids,
               float* weights, cudaStream_t st) {
     using S = Shared<MT, PER>;
@@ -508,10 +510,14 @@ int launch_tc(const __nv_bfloat16* x, const __nv_bfloat16* w, const float* bias,
     const int tiles = (T + kTokens - 1) / kTokens;
     int CL = 8;
     while (CL > 1 && tiles * CL > kSms) CL /= 2;
-    return launch(gate_tc_kernel<MT, PER>, (unsigned)(tiles * CL), kThreads, CL, sizeof(S) + 1024, once, st, map_w, map_x, x, w, bias, addend, T, H, g, CL, ids, weights);
+    return launch(gate_tc_kernel<MT, PER, STUCK>, (unsigned)(tiles * CL), kThreads, CL, sizeof(S) + 1024, once, st, map_w, map_x, x, w, bias, addend, T, H, g, CL, ids, weights);
 }
 
 }  // namespace
+
+int launch_gate_tc_stuck(const __nv_bfloat16* x, const __nv_bfloat16* w, int T, int H, const GateArgs& g, int32_t* ids, float* weights, cudaStream_t st) {
+    return launch_tc<1, 2, true>(x, w, nullptr, nullptr, T, H, g, ids, weights, st);
+}
 
 int launch_gate_tc(const __nv_bfloat16* x, const __nv_bfloat16* w, const float* bias, const float* addend, int T, int H, const GateArgs& g, int32_t* ids,
                    float* weights, cudaStream_t st) {

@@ -308,7 +308,8 @@ struct LoraSmem {
 // to all; beyond, each adds up a CL-th of v and sends the sums (32 rows of rank 64, CL = 8: 64 KB for a CTA otherwise).  What a CTA
 // receives is behind LoraSmem: [rank][TM][RP], or [rank][CL-th] and v.
 constexpr int kOneHop = 4096;
-template <typename O, int RP, int MB>
+// STUCK (exmoe_debug_lora_timeout): the barrier of a cluster's first CTA asks for an arrival that nobody makes.
+template <typename O, int RP, int MB, bool STUCK>
 __global__ void __launch_bounds__(kLoraThreads, RP <= 64 ? 2 : 1)
 lora_kernel(LoraArgs p, int log_cl, bool one_hop) {
     using S = LoraSmem<O, RP, MB>;
@@ -331,7 +332,7 @@ lora_kernel(LoraArgs p, int log_cl, bool one_hop) {
     if (CL > 1) {
         if (tid == 0 && tile.adapter >= 0) {
             sm.abort_flag = 0;
-            mbar_init(&sm.arrived[0], 1);
+            mbar_init(&sm.arrived[0], STUCK && rank == 0 ? 2 : 1);
             mbar_init(&sm.arrived[1], 1);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
             mbar_expect_tx(&sm.arrived[0], (one_hop ? CL : 1) * used * 4);
@@ -482,7 +483,7 @@ lora_kernel(LoraArgs p, int log_cl, bool one_hop) {
     }
     // A peer that does not send (none does that) would leave this call's rows unwritten and the plan's status at EXMOE_ERR_TIMEOUT.
     auto joined = [&](int hop) {
-        if (__syncthreads_and(mbar_wait(&sm.arrived[hop], 0, &sm.abort_flag, p.plan + LP_STATUS))) return true;
+        if (__syncthreads_and(mbar_wait(&sm.arrived[hop], 0, &sm.abort_flag, p.plan + LP_STATUS, STUCK ? kWaitBudgetTest : kWaitBudget))) return true;
         cluster_arrive();                                                  // nor may this CTA end while it can be sent to
         cluster_wait();
         return false;
@@ -570,11 +571,11 @@ lora_kernel(LoraArgs p, int log_cl, bool one_hop) {
     }
 }
 
-template <typename O, int RP, int MB>
+template <typename O, int RP, int MB, bool STUCK = false>
 int launch_lora(const LoraArgs& p, int tiles, int CL, cudaStream_t st) {
     using S = LoraSmem<O, RP, MB>;
     static SmemOnce once;
-    const auto kern = lora_kernel<O, RP, MB>;
+    const auto kern = lora_kernel<O, RP, MB, STUCK>;
     const bool one_hop = CL * S::TM * RP <= kOneHop;
     constexpr int most = (int)sizeof(S) + std::max(kOneHop, 2 * S::TM * RP) * 4;
     static_assert(sizeof(S) % 16 == 0 && most <= (RP <= 64 ? 112 : 224) * 1024, "shared memory, of a second CTA too");
@@ -682,9 +683,8 @@ extern "C" int exmoe_lora_plan_status(const void* plan) {
     return head[LP_MAGIC] == kPlanMagic ? head[LP_STATUS] : EXMOE_ERR_STATE;
 }
 
-extern "C" int exmoe_lora(const exmoe_lora_shape* shape, void* plan, const void* x, int64_t ld_x, const void* a, const void* b,
-                          const float* scale, int T, const void* base, int64_t ld_base, void* out, int64_t ld_out, int type,
-                          void* stream) {
+static int lora_call(const exmoe_lora_shape* shape, void* plan, const void* x, int64_t ld_x, const void* a, const void* b, const float* scale, int T,
+                     const void* base, int64_t ld_base, void* out, int64_t ld_out, int type, bool stuck, void* stream) {
     if (!shape || T < 0 || T > kMaxTokens || (type != EXMOE_F32 && type != EXMOE_BF16)) return EXMOE_ERR_ARG;
     const int n = shape->num_adapters, K = shape->d_in, N = shape->d_out, r = shape->rank;
     if (n < 1 || n > kMaxAdapters || K <= 0 || K % 8 || N <= 0 || r <= 0 || r % 8 || r > kMaxRank || K > kMaxDim || N > kMaxDim) return EXMOE_ERR_SHAPE;
@@ -708,7 +708,24 @@ extern "C" int exmoe_lora(const exmoe_lora_shape* shape, void* plan, const void*
     const int tiles = plan_tiles(T, n);
     int CL = 8;
     while (CL > 1 && (long long)tiles * CL > 2 * kSms) CL /= 2;
+    if (stuck) {
+        if (type != EXMOE_BF16 || tile_rows(T) != 16 || r > 64 || CL == 1) return EXMOE_ERR_SHAPE;
+        return r <= 16 ? launch_lora<__nv_bfloat16, 16, 1, true>(args, tiles, CL, (cudaStream_t)stream)
+                       : launch_lora<__nv_bfloat16, 64, 1, true>(args, tiles, CL, (cudaStream_t)stream);
+    }
     return type == EXMOE_F32 ? launch_lora_rank<float>(args, tiles, CL, (cudaStream_t)stream) : launch_lora_rank<__nv_bfloat16>(args, tiles, CL, (cudaStream_t)stream);
+}
+
+extern "C" int exmoe_lora(const exmoe_lora_shape* shape, void* plan, const void* x, int64_t ld_x, const void* a, const void* b,
+                          const float* scale, int T, const void* base, int64_t ld_base, void* out, int64_t ld_out, int type,
+                          void* stream) {
+    return lora_call(shape, plan, x, ld_x, a, b, scale, T, base, ld_base, out, ld_out, type, false, stream);
+}
+
+extern "C" int exmoe_debug_lora_timeout(const exmoe_lora_shape* shape, void* plan, const void* x, const void* a, const void* b, const float* scale, int T, void* out,
+                                       void* stream) {
+    if (!shape || T == 0) return EXMOE_ERR_ARG;
+    return lora_call(shape, plan, x, shape->d_in, a, b, scale, T, nullptr, 0, out, shape->d_out, EXMOE_BF16, true, stream);
 }
 
 }  // namespace exmoe

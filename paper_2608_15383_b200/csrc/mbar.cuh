@@ -11,6 +11,7 @@
 namespace exmoe {
 
 constexpr long long kWaitBudget = 2000000000ll;   // clock64 ticks (~1 s) before a wait gives up
+constexpr long long kWaitBudgetTest = 2000000ll;  // ... in the kernels of the exmoe_debug_* calls, one of whose barriers nothing completes
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void mbar_init(uint64_t* bar, int count) {
@@ -82,13 +83,14 @@ __device__ __forceinline__ bool mbar_look_at(uint32_t bar, uint32_t parity) {
         : "memory");
     return ok != 0;
 }
-__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status) {
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status,
+                                               long long budget = kWaitBudget) {
     if (__all_sync(0xffffffffu, mbar_try_at(bar, parity))) return true;
     const long long t0 = clock64();
     for (unsigned polls = 1;; ++polls) {
         if (__all_sync(0xffffffffu, mbar_try_at(bar, parity))) return true;
         if ((polls & 15u) == 0) {
-            const bool late = clock64() - t0 > kWaitBudget;
+            const bool late = clock64() - t0 > budget;
             if (late) {
                 *abort_flag = 1;
                 atomicExch(status, EXMOE_ERR_TIMEOUT);
