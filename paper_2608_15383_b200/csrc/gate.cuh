@@ -172,7 +172,7 @@ __device__ __forceinline__ float exp_below(float z, float top) {
 }
 
 // The weight of a chosen expert's logit, by the lanes that hold one (`chosen`); mx: the largest logit of all, sum: of the exponentials below
-// it.  False: too small for binary32.
+// it.  False: too small for binary32, which holds a sigmoid of 2^-126 and less with few bits or none; beside a sum of 1e-8 and more that is nothing.
 __device__ __forceinline__ bool choice_weight(const GateArgs& g, float z, bool chosen, float mx, float sum, float& s) {
     if (g.sigmoid) {
         s = sigmoid(z);
@@ -183,7 +183,7 @@ __device__ __forceinline__ bool choice_weight(const GateArgs& g, float z, bool c
     }
     if (g.renorm) {
         const float total = warp_sum_f32(chosen ? s : 0.f);
-        if (g.sigmoid && total < 1e-30f) return false;                     // nothing left, or nearly
+        if (g.sigmoid && total < 1e-8f) return false;                      // nothing left, or nearly
         s = total > 0.f ? s / total : 0.f;
     }
     s *= g.scale;

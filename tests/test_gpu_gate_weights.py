@@ -45,3 +45,18 @@ def test_weights(B, H, E, k, T, kw):
     ref, ref_w = ogate.choose(ogate.logits(hidden.double().numpy(), w.double().numpy()), gate, k)
     assert np.array_equal(ids.cpu().numpy(), ref)
     np.testing.assert_allclose(weights.cpu().numpy(), ref_w, rtol=2 * logit_error(T, H, E) + 28 * UNIT)
+
+
+@pytest.mark.parametrize("E,k", [(8, 8), (40, 5), (100, 9), (256, 32), (500, 16)])
+def test_sigmoids_below_binary32_are_renormalised(B, E, k):
+    """Sigmoids that binary32 holds as subnormal numbers or as 0 have weights relative to the largest of them.  Exponentials (2^-22 each), a sum of 32 and a quotient in binary32,
+    or all in binary64: below 48 units."""
+    g = torch.Generator().manual_seed(E)
+    z = torch.stack([-low - torch.rand(E, generator=g) * span for low in (0.0, 10.0, 17.0, 19.0, 40.0, 62.0, 85.0, 95.0, 150.0, 600.0) for span in (1.0, 30.0, 80.0)])
+    for dtype in (torch.float32, torch.bfloat16):
+        for kw in (dict(), dict(num_groups=2 if E % 2 == 0 and 2 * k <= E else 1)):
+            gate = B.Gate(score="sigmoid", renormalise=True, scale=2.5, **kw)
+            ids, w = B.exmoe_gate_logits(SimpleNamespace(num_experts=E, top_k=k), gate, z.to(dtype).cuda())
+            ref, ref_w = ogate.choose(z.to(dtype).double().numpy(), gate, k)
+            assert np.array_equal(ids.cpu().numpy(), ref)
+            np.testing.assert_allclose(w.cpu().numpy(), ref_w, rtol=48 * UNIT, atol=1e-30)
