@@ -205,7 +205,9 @@ int exmoe_route(const exmoe_shape* shape, const void* hidden_bf16, const void* r
  *   experts      the k largest c_e of these groups, in descending order, equal values by ascending id
  *   weights      s_e of the chosen, divided by their sum if `renormalise` is set, times `weight_scale`
  * Everything is decided as in binary64 (experts without a balance bias by z_e itself, of which s_e is a monotone function), whatever the
- * number of tokens; weights are binary32.  A logit of -infinity switches its expert off: score 0, chosen after all others of the kept
+ * number of tokens.  Weights are binary32, within a few roundings of their logits'; logits of hidden states are binary32 sums there (for
+ * hidden states of N(0, 1) weights are within 5e-6 of themselves for few tokens, 1e-4 on tensor cores), and binary64's for a token whose sums' bound, no more than
+ * 2^-24 (100 + d_model / 128) |h| |W_e|, passes 0.05.  A logit of -infinity switches its expert off: score 0, chosen after all others of the kept
  * groups, absent from its group's value.  A token without any expert left gets the first k of the first groups, with weights of
  * zero.  A NaN logit comes behind those; with softmax it makes the token's weights NaN. */
 enum { EXMOE_SCORE_SOFTMAX = 0, EXMOE_SCORE_SIGMOID = 1 };
@@ -248,7 +250,8 @@ int exmoe_gate_status(void);
  * take an adapter in, and the requests of a batch bring different ones).  For token t with adapter a:
  *   out_t = base_t + scale_a * B_a (A_a x_t)
  * with base what the shared projection gave: a BF16 projection, the sparse block's output, or the router's logits in float32.
- * Products are summed in binary32 and rounded once, to the type of `out`. */
+ * Products are summed in binary32 and rounded once, to the type of `out`.  Infinities in x, base and a are carried as in the formula;
+ * where b has one, its column is infinite or NaN. */
 typedef struct {
     int num_adapters;   /* n, 1 .. 1024 */
     int d_in;           /* K, a multiple of 8, at most 2^30 */

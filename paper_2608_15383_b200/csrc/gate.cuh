@@ -450,7 +450,9 @@ __device__ __forceinline__ bool choose_fast(const GateArgs& g, ChoiceRoom<PER>& 
                     before += o > v || (o == v && j < lane);
                 }
             } else {
-                if (balance) {                                             // the candidates' own slopes: they lie where a sigmoid is flat
+                // The candidates' own slopes: they lie where a sigmoid is flat.  A logit of z is off by dz + rel |z| where this has dz + rel: what
+                // 2 rel (|z| - 1.06) s (1 - s) lacks is below 3.7e-8, and round_near is 7.3e-8 and more above what two quick_sigmoids need at any z.
+                if (balance) {
                     float slope = 0.f;
                     if (lane < n) {
                         const float p = g.sigmoid ? quick_sigmoid(room.z[e]) : expf(room.z[e] - mx) / sum;
