@@ -226,11 +226,11 @@ gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w
         for (int i = 0; i < kGateWarps; ++i) x2 += x2_of[i];
         if (x2 == 0.f && any_number(xs + (size_t)rank * chunks, chunks, lane, 32)) x2 = kLeastSquare;
         // the norms come out of binary32 sums, short by less than 1 %
-        dz = 1.01f * 0x1p-24f * sqrtf(least_of(x2)) * sqrtf(fmaxf(w2, kLeastSquare)) + (addend ? 16.f * 0x1p-24f : 0.f);
+        dz = x2 == 0.f && !(bias && addend) ? 0.f : 1.01f * 0x1p-24f * sqrtf(least_of(x2)) * sqrtf(fmaxf(w2, kLeastSquare)) + (addend ? 16.f * 0x1p-24f : 0.f);
         if (cancelled) dz = INFINITY;
     }
     const float* balance = g.balance ? sm.balance : nullptr;
-    const float rel = bias || addend ? kAddedRel : 0.f;
+    const float rel = (bias || addend) && dz > 0.f ? kAddedRel : 0.f;
     int32_t* ids_t = ids + t * g.k;
     float* weights_t = weights + t * g.k;
     for (int mode = GATE_NEW;;) {

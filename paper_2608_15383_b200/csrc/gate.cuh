@@ -633,7 +633,8 @@ __device__ __forceinline__ bool any_number(const uint4* p, int chunks, int lane,
     }
     return __any_sync(0xffffffffu, any);
 }
-constexpr float kAddedRel = 3.f * 0x1p-24f;                                // bias and addend: 2^-24 (|sum before| + |z|), with |sum before| <= 2 |z| + 16
+// Bias and addend: 2^-24 (|sum before| + |z|), with |sum before| <= 2 |z| + 16.  The logits of a row of zeros are its bias or its addend, exact unless it has both.
+constexpr float kAddedRel = 3.f * 0x1p-24f;
 
 __device__ __forceinline__ void unpack8(const uint4& a, float (&x)[8]) {
     const uint32_t r[4] = {a.x, a.y, a.z, a.w};

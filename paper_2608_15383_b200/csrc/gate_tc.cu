@@ -363,7 +363,7 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
         Warp<PER>& my = sm.s.warp[d];
         ChoiceRoom<PER>& room = my.room;
         const float* balance = g.balance ? sm.balance : nullptr;
-        const float rel = bias || addend ? kAddedRel : 0.f;
+        const float added = bias || addend ? kAddedRel : 0.f;
         const int owned = kTokens / CL, chunks = H / 8;
         // Round 0: the CTA's tokens.  The rounds behind it: those that wait, done by the warps together: first the logits, then the choices.
         for (int round = 0, n_tok = owned, log_p = 0;; ++round) {
@@ -413,7 +413,7 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                     if (t0 + tok >= T) break;
                     float size = 0.f;
                     load_logits<PER>(smem_u32(&sm.s.part[tok][0]), smem_u32(&sm.size[tok]), rank, CL, lane, room.z, size);
-                    dz = 1.02f * 0x1p-24f * size + (addend ? 16.f * 0x1p-24f : 0.f);       // the norms are short by less than 2 %
+                    dz = 1.02f * 0x1p-24f * size + (addend && (bias || size > 0.f) ? 16.f * 0x1p-24f : 0.f);       // the norms are short by less than 2 %
                     if (bias || addend || g.E < 32 * PER) {
                         bool cancelled = false;
 #pragma unroll
@@ -462,6 +462,7 @@ gate_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant_
                     }
                     __syncwarp();
                 }
+                const float rel = dz > 0.f ? added : 0.f;
                 int32_t* ids_t = ids + (size_t)(t0 + tok) * g.k;
                 float* weights_t = weights + (size_t)(t0 + tok) * g.k;
                 if (round > 0) mode = go_on<PER>(g, room, balance, my.z64, dz, rel, lane, ids_t, weights_t);

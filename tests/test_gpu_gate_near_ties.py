@@ -132,3 +132,20 @@ def test_products_beyond_binary32(B, E, T, hidden_at, router_at):
     ref, ref_w = ogate.choose(z + mask.double().numpy(), B.Gate(), k)
     assert np.array_equal(ids.cpu().numpy(), ref)
     np.testing.assert_allclose(weights.cpu().numpy(), ref_w, rtol=WEIGHT, atol=2.0 ** -126)
+
+
+@pytest.mark.parametrize("E,T", [(64, 5), (64, 40), (256, 300)])
+def test_rows_of_zeros_with_bias_or_addend(B, E, T):
+    """A padded row's logits are its bias or its addend, or the sum of both in 64 bits: ties and neighbours of one binary32 step."""
+    H, k = 256, 8
+    g = torch.Generator().manual_seed(E + T)
+    x, w = torch.randn(T, H, generator=g).to(torch.bfloat16), (torch.randn(E, H, generator=g) * 0.02).to(torch.bfloat16)
+    x[1::2] = 0.0
+    one = torch.full((E,), 1.0)
+    one[::3] += 2.0 ** -23
+    for bias, addend in ((one, None), (None, torch.zeros(T, E)), (None, one.flip(0).repeat(T, 1)), (one, torch.zeros(T, E)), (one * 2.0 ** -30, one.repeat(T, 1))):
+        for gate in (B.Gate(), B.Gate(score="sigmoid", num_groups=4, top_groups=2, group_score="top2", renormalise=True)):
+            cuda = lambda v: None if v is None else v.cuda()
+            ids, _ = B.exmoe_route_gated(shape(H, E, k), gate, x.cuda(), w.cuda(), bias=cuda(bias), addend=cuda(addend))
+            z = ogate.logits(x.double().numpy(), w.double().numpy(), None if bias is None else bias.double().numpy(), None if addend is None else addend.double().numpy())
+            assert np.array_equal(ids.cpu().numpy(), ogate.choose(z, gate, k)[0])
