@@ -185,7 +185,7 @@ def _run_own(state):
         return binding.exmoe_balance_loss(state["shape"], state["gate"], state["logits"], state["ids"], mask=state["mask"], offsets=state["offsets"])
     return binding.exmoe_gate_backward(state["shape"], state["gate"], state["logits"], state["ids"], d_weights=state["d_weights"], d_losses=state["d_losses"],
                                        counts=state["counts"] if case["losses"] else None, kept=state["kept"] if case["losses"] else None,
-                                       mask=state["mask"] if case["losses"] else None, offsets=state["offsets"] if case["losses"] else None)
+                                       mask=state["mask"], offsets=state["offsets"] if case["losses"] else None)
 
 
 def _activate(v, activation):
@@ -255,17 +255,17 @@ def run(state):
         z_loss = (lse.double().squeeze(1) ** 2 * keep).sum() / n.sum().clamp(min=1)
         return torch.stack([balance, z_loss]).float(), counts, sums.float(), kept
     dz = torch.zeros_like(z)
+    _, _, of, keep = _counts(ids, offsets, mask, E)
     if case["losses"]:
         counts, kept = state["counts"].double(), state["kept"].double()
         factor = state["d_losses"][0] * E / (k * (kept > 0).sum().clamp(min=1) * kept.clamp(min=1) ** 2)
-        _, _, of, keep = _counts(ids, offsets, mask, E)
         G = (factor[:, None] * counts).float()[of] * keep[:, None]
         G = G - (q * G).sum(1, keepdim=True)
         dz = s * (1 - s) * G / total if sigmoid else q * G
         dz = dz + (2 * state["d_losses"][1] / kept.sum().clamp(min=1)).float() * lse * p * keep[:, None]
     if case["weights"]:
         chosen = s.gather(1, ids)
-        d = state["d_weights"] * case["scale"]
+        d = state["d_weights"] * case["scale"] * keep[:, None]
         if case["renormalise"]:
             w, t = _normalised(chosen)
             d = (d - (w * d).sum(1, keepdim=True)) / t
@@ -345,7 +345,7 @@ def exact(case, seed):
                 ds[rows] = (f - q[rows] @ f[:, None]) / total[rows]
         direct[keep] = d[1] * 2 * lse[keep, None] * p[keep] / max(kept.sum(), 1)
     if case["weights"]:
-        d = _numpy(state["d_weights"]) * case["scale"]
+        d = np.where(keep[:, None], _numpy(state["d_weights"]) * case["scale"], 0.0)
         if case["renormalise"]:
             c = np.take_along_axis(s, ids, 1)
             t = c.sum(1, keepdims=True)
