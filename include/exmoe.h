@@ -246,6 +246,65 @@ int exmoe_gate_logits(const exmoe_shape* shape, const exmoe_gate* gate, const vo
  * used), and clears it. */
 int exmoe_gate_status(void);
 
+/* How evenly a gate uses its experts, per sequence, and the two losses it is trained with.  With z the logits, ids the choice, and q the scores of a
+ * token over all experts (softmax(z), or sigmoids divided by their sum):
+ *   counts_se   how often expert e was chosen by the tokens of sequence s that count; counts of tokens in use drive the balance bias
+ *   sums_se     the sum of these tokens' q_e                         kept_s   how many they are (T_s)
+ *   losses[0]   balance loss: the mean over the sequences with T_s > 0 of E / (k T_s^2) sum_e counts_se sums_se (1 where all experts are used alike)
+ *   losses[1]   z loss: the mean over all tokens that count of (log sum_e exp z_e)^2, of the logits whatever the scores are
+ * Losses without any token that counts are 0.  A token all of whose logits are -infinity has scores and logarithm 0.  An id outside [0, E) is not counted.
+ *   logits       : dev, float32 or BF16 (`type`) [T, E], rows `row_stride` elements apart     topk_ids : dev, int32 [T, k]
+ *   mask         : dev, one byte per token, or NULL: 0 for padding.  What a masked token's row and ids hold does not matter
+ *   offsets      : dev, int32 [num_sequences + 1], ascending in [0, T], or NULL for one sequence of all tokens: sequence s is the tokens
+ *                  [offsets[s], offsets[s + 1]), which may be none; tokens outside all of them count nowhere.  With offsets that do not ascend in
+ *                  [0, T] both losses are NaN and the other outputs are not to be used
+ *   losses       : dev, float32 [2]        counts : dev, int32 [S, E]        score_sums : dev, float32 [S, E]        kept : dev, int32 [S]
+ *   scratch      : dev, exmoe_balance_scratch_bytes(), 8-byte aligned; calls that may overlap need one each
+ * All outputs are fully overwritten and overlap nothing.  Uses num_experts (<= 4096), top_k, and of the gate score (the whole gate is checked).  Sums are binary32 in a
+ * fixed order: the same call gives the same bits.  Asynchronous on `stream`; allocates nothing. */
+int exmoe_balance_scratch_bytes(const exmoe_shape* shape, int T, size_t* bytes);
+int exmoe_balance_loss(const exmoe_shape* shape, const exmoe_gate* gate, const void* logits, int type, int64_t row_stride, const int32_t* topk_ids,
+                       const uint8_t* mask, const int32_t* offsets, int num_sequences, int T, float* losses, int32_t* counts, float* score_sums,
+                       int32_t* kept, void* scratch, void* stream);
+
+/* The gradient on the logits of the gate's mixture weights and of both losses (the choice itself, and the balance bias, have none):
+ *   d_logits = d_weights . d weights / d z + d_losses . d losses / d z
+ * with counts held fixed, as the balance loss is meant.
+ *   logits, type, row_stride, topk_ids, mask, offsets, num_sequences : as above; topk_ids may be NULL without d_weights.  A masked token's gradient
+ *                  is zero.  An id outside [0, E) has no weight, an expert that a token names twice both of them
+ *   d_weights    : dev, float32 [T, k], or NULL        d_losses : dev, float32 [2], or NULL
+ *   counts, kept : dev, of exmoe_balance_loss (or summed over the processes of a job); needed with d_losses
+ *   d_logits     : dev, [T, E] of `type`, rows d_row_stride elements apart, fully overwritten; overlaps no input (EXMOE_ERR_ARG)
+ * Uses of the gate score, renormalise and weight_scale.  Asynchronous on `stream`; allocates nothing; T = 0 is a no-op. */
+int exmoe_gate_backward(const exmoe_shape* shape, const exmoe_gate* gate, const void* logits, int type, int64_t row_stride, const int32_t* topk_ids,
+                        const float* d_weights, const float* d_losses, const int32_t* counts, const int32_t* kept, const uint8_t* mask,
+                        const int32_t* offsets, int num_sequences, int T, void* d_logits, int64_t d_row_stride, void* stream);
+
+/* A dense product with its epilogue (the paper keeps the model's dense parts; these are the ones that stand around a sparse block: a projection that
+ * adapters go beside, a router's logits, an expert that all tokens share):
+ *   out_t = residual_t + act(W x_t + bias)                       or, with a second matrix,
+ *   out_t = residual_t + act(W x_t + bias) * (W_up x_t + bias_up)
+ * Products are summed in binary32, the epilogue is binary32, and the result is rounded once, to the type of `out`.  (In which order and how often the sums
+ * are rounded depends on T, K and N.) */
+enum { EXMOE_ACT_NONE = 0, EXMOE_ACT_RELU = 1, EXMOE_ACT_GELU = 2 /* v Phi(v) */, EXMOE_ACT_GELU_TANH = 3, EXMOE_ACT_SILU = 4 };
+typedef struct {
+    int d_in;           /* K, a multiple of 8, at most 2^30 */
+    int d_out;          /* N, at most 2^30 */
+    int activation;     /* EXMOE_ACT_* */
+} exmoe_linear_shape;
+
+/* x             : dev, BF16 [T, K], rows ld_x elements apart (a multiple of 8), 16-byte aligned
+ * w, w_up       : dev, BF16 [N, K], rows ld_w, ld_w_up elements apart (multiples of 8), 16-byte aligned; w_up may be NULL
+ * bias, bias_up : dev, float32 [N], or NULL; bias_up needs w_up
+ * residual      : dev, [T, N] of `type`, rows ld_residual elements apart, or NULL for zeros
+ * out           : dev, [T, N] of `type`, rows ld_out elements apart, fully overwritten; may be `residual` itself with the same rows and otherwise
+ *                 overlaps none of the inputs (EXMOE_ERR_ARG)
+ * type          : EXMOE_F32 or EXMOE_BF16, of residual and out
+ * T <= 2^29.  Asynchronous on `stream`; allocates nothing; T = 0 is a no-op.  EXMOE_ERR_SHAPE / EXMOE_ERR_ARG before any work is queued. */
+int exmoe_linear(const exmoe_linear_shape* shape, const void* x, int64_t ld_x, const void* w, int64_t ld_w, const float* bias, const void* w_up,
+                 int64_t ld_w_up, const float* bias_up, int T, const void* residual, int64_t ld_residual, void* out, int64_t ld_out, int type,
+                 void* stream);
+
 /* Low-rank adapters of many requests beside a projection that all of them share (the paper has none; packed int4 weights cannot
  * take an adapter in, and the requests of a batch bring different ones).  For token t with adapter a:
  *   out_t = base_t + scale_a * B_a (A_a x_t)

@@ -55,6 +55,10 @@ class exmoe_lora_shape(ctypes.Structure):
     _fields_ = [("num_adapters", c_int), ("d_in", c_int), ("d_out", c_int), ("rank", c_int)]
 
 
+class exmoe_linear_shape(ctypes.Structure):
+    _fields_ = [("d_in", c_int), ("d_out", c_int), ("activation", c_int)]
+
+
 _SIGNATURES = {
     "exmoe_strerror": (c_char_p, [c_int]),
     "exmoe_packed_bytes": (c_int, [POINTER(exmoe_shape), POINTER(c_size_t)]),
@@ -72,6 +76,11 @@ _SIGNATURES = {
     "exmoe_route_gated": (c_int, [POINTER(exmoe_shape), POINTER(exmoe_gate)] + [c_void_p] * 5 + [c_int] + [c_void_p] * 3),
     "exmoe_gate_logits": (c_int, [POINTER(exmoe_shape), POINTER(exmoe_gate), c_void_p, c_int, c_int64, c_void_p, c_int] + [c_void_p] * 3),
     "exmoe_gate_status": (c_int, []),
+    "exmoe_balance_scratch_bytes": (c_int, [POINTER(exmoe_shape), c_int, POINTER(c_size_t)]),
+    "exmoe_balance_loss": (c_int, [POINTER(exmoe_shape), POINTER(exmoe_gate), c_void_p, c_int, c_int64, c_void_p, c_void_p, c_void_p, c_int, c_int] + [c_void_p] * 6),
+    "exmoe_gate_backward": (c_int, [POINTER(exmoe_shape), POINTER(exmoe_gate), c_void_p, c_int, c_int64] + [c_void_p] * 7 + [c_int, c_int, c_void_p, c_int64, c_void_p]),
+    "exmoe_linear": (c_int, [POINTER(exmoe_linear_shape), c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_int, c_void_p, c_int64,
+                             c_void_p, c_int64, c_int, c_void_p]),
     "exmoe_lora_plan_bytes": (c_int, [c_int, c_int, POINTER(c_size_t)]),
     "exmoe_lora_plan": (c_int, [c_void_p, c_int, c_int, c_void_p, c_void_p]),
     "exmoe_lora_plan_status": (c_int, [c_void_p]),
@@ -134,7 +143,8 @@ def _serving():
         spec.loader.exec_module(native)
         native.set_entry_points(*(ctypes.cast(getattr(lib(), name), c_void_p).value for name in
                                   ("exmoe_route", "exmoe_moe_forward", "exmoe_moe_forward_host", "exmoe_route_gated", "exmoe_gate_logits",
-                                   "exmoe_lora_plan_bytes", "exmoe_lora_plan", "exmoe_lora")))
+                                   "exmoe_lora_plan_bytes", "exmoe_lora_plan", "exmoe_lora", "exmoe_balance_scratch_bytes", "exmoe_balance_loss",
+                                   "exmoe_gate_backward", "exmoe_linear")))
         _native = native
     return _native
 
@@ -247,6 +257,35 @@ def exmoe_gate_logits(shape, gate, logits, balance=None, topk_ids=None, topk_wei
     r = (_native or _serving()).gate_logits(shape, gate, logits, balance, topk_ids, topk_weights, stream)
     if r.__class__ is int:
         raise ExmoeError(r, "exmoe_gate_logits")
+    return r
+
+
+def exmoe_balance_loss(shape, gate, logits, topk_ids, mask=None, offsets=None, out=None, stream=None):
+    """How evenly the gate's choice topk_ids (int32 [T, k]) from logits (fp32 or BF16 [T, E], rows may be apart) uses the experts, in sequences
+    offsets[s] .. offsets[s + 1] (int32 [S + 1]; None: one of all tokens) of the tokens that mask (bool [T]) keeps.  Returns (losses fp32 [2]: balance
+    loss, z loss; counts int32 [S, E]; score sums fp32 [S, E]; kept tokens int32 [S]), or fills the four tensors in `out`."""
+    r = (_native or _serving()).balance_loss(shape, gate, logits, topk_ids, mask, offsets, out, stream)
+    if r.__class__ is int:
+        raise ExmoeError(r, "exmoe_balance_loss")
+    return r
+
+
+def exmoe_gate_backward(shape, gate, logits, topk_ids=None, d_weights=None, d_losses=None, counts=None, kept=None, mask=None, offsets=None, out=None, stream=None):
+    """The gradient on the logits [T, E], of their type, from the mixture weights' (d_weights fp32 [T, k]) and from both losses' (d_losses fp32 [2],
+    with the counts and kept tokens that exmoe_balance_loss gave)."""
+    r = (_native or _serving()).gate_backward(shape, gate, logits, topk_ids, d_weights, d_losses, counts, kept, mask, offsets, out, stream)
+    if r.__class__ is int:
+        raise ExmoeError(r, "exmoe_gate_backward")
+    return r
+
+
+def exmoe_linear(x, w, bias=None, w_up=None, bias_up=None, activation="none", residual=None, out=None, out_dtype=None, stream=None):
+    """residual + act(x W^T + bias), or residual + act(x W^T + bias) * (x W_up^T + bias_up): x BF16 [T, K], w and w_up BF16 [N, K], biases fp32 [N];
+    activation "none", "relu", "gelu", "gelu_tanh" or "silu"; residual and out fp32 or BF16 [T, N] (`out_dtype` where neither is given, BF16 by
+    default).  Rows of all matrices may be apart; out may be residual."""
+    r = (_native or _serving()).linear(x, w, bias, w_up, bias_up, activation, residual, out, out_dtype, stream)
+    if r.__class__ is int:
+        raise ExmoeError(r, "exmoe_linear")
     return r
 
 

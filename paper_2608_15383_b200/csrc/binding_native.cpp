@@ -27,6 +27,10 @@ decltype(&exmoe_gate_logits) g_gate_logits = nullptr;
 decltype(&exmoe_lora_plan_bytes) g_lora_plan_bytes = nullptr;
 decltype(&exmoe_lora_plan) g_lora_plan = nullptr;
 decltype(&exmoe_lora) g_lora = nullptr;
+decltype(&exmoe_balance_scratch_bytes) g_balance_scratch_bytes = nullptr;
+decltype(&exmoe_balance_loss) g_balance_loss = nullptr;
+decltype(&exmoe_gate_backward) g_gate_backward = nullptr;
+decltype(&exmoe_linear) g_linear = nullptr;
 
 PyObject *s_d_model, *s_d_ff, *s_experts, *s_top_k, *s_group, *s_cuda_stream;
 PyObject *s_score, *s_num_groups, *s_top_groups, *s_group_score, *s_renormalise, *s_scale;
@@ -378,6 +382,19 @@ PyObject* lora_plan(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// The type of a result [T, N]: that of the tensors given, or of `out_dtype`, BF16 by default.
+bool result_type(PyObject* like, PyObject* asked, const char* same, at::ScalarType* dt) {
+    *dt = at::kBFloat16;
+    if (like != Py_None) {
+        if (THPVariable_Check(like)) *dt = THPVariable_Unpack(like).scalar_type();
+        if (asked != Py_None && (!THPDtype_Check(asked) || reinterpret_cast<THPDtype*>(asked)->scalar_type != *dt)) return wrong("out_dtype", same);
+    } else if (asked != Py_None) {
+        if (!THPDtype_Check(asked)) return wrong("out_dtype", "a torch.dtype");
+        *dt = reinterpret_cast<THPDtype*>(asked)->scalar_type;
+    }
+    return *dt == at::kFloat || *dt == at::kBFloat16 || wrong("out_dtype", "torch.float32 or torch.bfloat16");
+}
+
 // lora(plan, x, a, b, scale, base, out, out_dtype, stream) -> out
 PyObject* lora(PyObject*, PyObject* const* a, Py_ssize_t n) {
     if (n != 9) return PyErr_Format(PyExc_TypeError, "lora: 9 arguments");
@@ -398,16 +415,8 @@ PyObject* lora(PyObject*, PyObject* const* a, Py_ssize_t n) {
         int rc = g_lora_plan_bytes(T, na, &bytes);
         if (rc) return PyLong_FromLong(rc);
         if (p->dim() != 1 || p->size(0) != (int64_t)bytes / 4) return wrong("plan", "one of as many tokens and adapters"), nullptr;
-        at::ScalarType dt = at::kBFloat16;
-        PyObject* like = a[5] != Py_None ? a[5] : a[6];
-        if (like != Py_None) {
-            if (THPVariable_Check(like)) dt = THPVariable_Unpack(like).scalar_type();
-            if (a[7] != Py_None && (!THPDtype_Check(a[7]) || reinterpret_cast<THPDtype*>(a[7])->scalar_type != dt)) return wrong("out_dtype", "the type of base and out"), nullptr;
-        } else if (a[7] != Py_None) {
-            if (!THPDtype_Check(a[7])) return wrong("out_dtype", "a torch.dtype"), nullptr;
-            dt = reinterpret_cast<THPDtype*>(a[7])->scalar_type;
-        }
-        if (dt != at::kFloat && dt != at::kBFloat16) return wrong("out_dtype", "torch.float32 or torch.bfloat16"), nullptr;
+        at::ScalarType dt;
+        if (!result_type(a[5] != Py_None ? a[5] : a[6], a[7], "the type of base and out", &dt)) return nullptr;
         constexpr const char* kRows = "a CUDA matrix [T, d_out] of torch.float32 or torch.bfloat16 with rows of consecutive elements";
         if (a[5] != Py_None && (!(base = rows(a[5], dt, "base", kRows)) || !sized(*base, {T, N}, "base", kRows))) return nullptr;
         if (a[6] != Py_None && (!(o = rows(a[6], dt, "out", kRows)) || !sized(*o, {T, N}, "out", kRows))) return nullptr;
@@ -427,9 +436,167 @@ PyObject* lora(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// The logits of a gate's losses and gradients, and what goes with them: the choice, the mask, the sequences.
+struct LossInputs {
+    exmoe_shape s;
+    exmoe_gate g;
+    bool bf16;
+    int T, S = 1;
+    const at::Tensor *z, *ids = nullptr, *mask = nullptr, *offsets = nullptr;
+    bool init(PyObject* shape, PyObject* gate, PyObject* logits, PyObject* i, PyObject* m, PyObject* off) {
+        if (!gate_shape_of(shape, &s, false) || !gate_of(gate, &g)) return false;
+        bf16 = THPVariable_Check(logits) && THPVariable_Unpack(logits).scalar_type() == at::kBFloat16;
+        z = rows(logits, bf16 ? at::kBFloat16 : at::kFloat, "logits", "a CUDA matrix of torch.float32 or torch.bfloat16 with rows of consecutive elements");
+        if (!z) return false;
+        if (z->size(1) != s.num_experts) return wrong("logits", "[T, num_experts]");
+        if (!int32_of(z->size(0), &T, "logits") || !here(*z, "logits")) return false;
+        if (i != Py_None && (!(ids = tensor(i, at::kInt, true, "topk_ids", kI32)) || !sized(*ids, {T, s.top_k}, "topk_ids", "[T, top_k]") || !here(*ids, "topk_ids"))) return false;
+        if (m != Py_None) {
+            mask = THPVariable_Check(m) ? &THPVariable_Unpack(m) : nullptr;
+            if (!mask || !mask->is_cuda() || mask->scalar_type() != at::kBool || !mask->is_contiguous()) return wrong("mask", "a contiguous CUDA tensor of torch.bool");
+            if (!sized(*mask, {T}, "mask", "[T]") || !here(*mask, "mask")) return false;
+        }
+        if (off != Py_None) {
+            if (!(offsets = tensor(off, at::kInt, true, "offsets", kI32)) || !here(*offsets, "offsets")) return false;
+            if (offsets->dim() != 1 || offsets->size(0) < 2) return wrong("offsets", "[S + 1] of one sequence or more");
+            if (!int32_of(offsets->size(0) - 1, &S, "offsets")) return false;
+        }
+        return true;
+    }
+    int type() const { return bf16 ? EXMOE_BF16 : EXMOE_F32; }
+    const int32_t* ids_data() const { return ids ? static_cast<const int32_t*>(ids->data_ptr()) : nullptr; }
+    const uint8_t* mask_data() const { return mask ? static_cast<const uint8_t*>(mask->data_ptr()) : nullptr; }
+    const int32_t* offsets_data() const { return offsets ? static_cast<const int32_t*>(offsets->data_ptr()) : nullptr; }
+};
+
+// balance_loss(shape, gate, logits, topk_ids, mask, offsets, out, stream) -> (losses, counts, score_sums, kept)
+PyObject* balance_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 8) return PyErr_Format(PyExc_TypeError, "balance_loss: 8 arguments");
+    return guarded([&]() -> PyObject* {
+        LossInputs in;
+        if (!in.init(a[0], a[1], a[2], a[3], a[4], a[5])) return nullptr;
+        if (!in.ids) return bad_tensor("topk_ids", true, kI32);
+        size_t bytes = 0;
+        int rc = g_balance_scratch_bytes(&in.s, in.T, &bytes);
+        if (rc) return PyLong_FromLong(rc);
+        const int64_t S = in.S, E = in.s.num_experts;
+        at::Tensor o[4];
+        const at::ScalarType types[4] = {at::kFloat, at::kInt, at::kFloat, at::kInt};
+        const std::vector<int64_t> sizes[4] = {{2}, {S, E}, {S, E}, {S}};
+        if (a[6] != Py_None) {
+            if (!PyTuple_Check(a[6]) || PyTuple_GET_SIZE(a[6]) != 4) return wrong("out", "a tuple (losses, counts, score_sums, kept)"), nullptr;
+            static const char* const names[4] = {"losses", "counts", "score_sums", "kept"};
+            static const char* const need[4] = {"[2]", "[S, num_experts]", "[S, num_experts]", "[S]"};
+            for (int i = 0; i < 4; ++i) {
+                const at::Tensor* t = tensor(PyTuple_GET_ITEM(a[6], i), types[i], true, names[i], types[i] == at::kInt ? kI32 : kF32);
+                if (!t || !sized(*t, sizes[i], names[i], need[i]) || !here(*t, names[i])) return nullptr;
+                o[i] = *t;
+            }
+        }
+        void* st;
+        if (!stream_of(a[7], &st)) return nullptr;
+        const OnStream on(a[7], st);
+        if (a[6] == Py_None)
+            for (int i = 0; i < 4; ++i) o[i] = empty_on(*in.z, sizes[i], types[i]);
+        const at::Tensor scratch = empty_on(*in.z, {(int64_t)bytes}, at::kByte);
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_balance_loss(&in.s, &in.g, in.z->data_ptr(), in.type(), pitch(*in.z), in.ids_data(), in.mask_data(), in.offsets_data(), in.S, in.T,
+                            static_cast<float*>(o[0].data_ptr()), static_cast<int32_t*>(o[1].data_ptr()), static_cast<float*>(o[2].data_ptr()),
+                            static_cast<int32_t*>(o[3].data_ptr()), scratch.data_ptr(), st);
+        Py_END_ALLOW_THREADS
+        if (rc) return PyLong_FromLong(rc);
+        if (a[6] != Py_None) return Py_NewRef(a[6]);
+        PyObject* r = PyTuple_New(4);
+        for (int i = 0; r && i < 4; ++i) PyTuple_SET_ITEM(r, i, THPVariable_Wrap(std::move(o[i])));
+        return r;
+    });
+}
+
+// gate_backward(shape, gate, logits, topk_ids, d_weights, d_losses, counts, kept, mask, offsets, out, stream) -> d_logits
+PyObject* gate_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 12) return PyErr_Format(PyExc_TypeError, "gate_backward: 12 arguments");
+    return guarded([&]() -> PyObject* {
+        LossInputs in;
+        if (!in.init(a[0], a[1], a[2], a[3], a[8], a[9])) return nullptr;
+        bool ok = true;
+        const at::Tensor* dw = optional_f32(a[4], {in.T, in.s.top_k}, "d_weights", "[T, top_k]", &ok);
+        if (!ok) return nullptr;
+        if (dw && !in.ids) return bad_tensor("topk_ids", true, kI32);
+        const at::Tensor* dl = optional_f32(a[5], {2}, "d_losses", "[2]", &ok);
+        if (!ok) return nullptr;
+        const at::Tensor *counts = nullptr, *kept = nullptr, *o = nullptr;
+        if (dl) {
+            if (!(counts = tensor(a[6], at::kInt, true, "counts", kI32)) || !sized(*counts, {in.S, in.s.num_experts}, "counts", "[S, num_experts]") || !here(*counts, "counts")) return nullptr;
+            if (!(kept = tensor(a[7], at::kInt, true, "kept", kI32)) || !sized(*kept, {in.S}, "kept", "[S]") || !here(*kept, "kept")) return nullptr;
+        }
+        const at::ScalarType dt = in.bf16 ? at::kBFloat16 : at::kFloat;
+        constexpr const char* kNeed = "a CUDA matrix [T, num_experts] of the logits' type with rows of consecutive elements";
+        if (a[10] != Py_None && (!(o = rows(a[10], dt, "out", kNeed)) || !sized(*o, {in.T, in.s.num_experts}, "out", kNeed) || !here(*o, "out"))) return nullptr;
+        void* st;
+        if (!stream_of(a[11], &st)) return nullptr;
+        const OnStream on(a[11], st);
+        at::Tensor out = o ? *o : empty_on(*in.z, {in.T, in.s.num_experts}, dt);
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_gate_backward(&in.s, &in.g, in.z->data_ptr(), in.type(), pitch(*in.z), in.ids_data(), data_of(dw), data_of(dl),
+                             counts ? static_cast<const int32_t*>(counts->data_ptr()) : nullptr, kept ? static_cast<const int32_t*>(kept->data_ptr()) : nullptr,
+                             in.mask_data(), in.offsets_data(), in.S, in.T, out.data_ptr(), pitch(out), st);
+        Py_END_ALLOW_THREADS
+        if (rc) return PyLong_FromLong(rc);
+        return o ? Py_NewRef(a[10]) : THPVariable_Wrap(std::move(out));
+    });
+}
+
+bool activation_of(PyObject* o, int* v) {
+    if (!PyUnicode_Check(o)) return to_int(o, v);
+    static const char* const names[] = {"none", "relu", "gelu", "gelu_tanh", "silu"};
+    for (*v = 0; *v < 5; ++*v)
+        if (PyUnicode_CompareWithASCIIString(o, names[*v]) == 0) return true;
+    PyErr_SetString(PyExc_ValueError, "activation: 'none', 'relu', 'gelu', 'gelu_tanh' or 'silu'");
+    return false;
+}
+
+// linear(x, w, bias, w_up, bias_up, activation, residual, out, out_dtype, stream) -> out
+PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    if (n != 10) return PyErr_Format(PyExc_TypeError, "linear: 10 arguments");
+    return guarded([&]() -> PyObject* {
+        constexpr const char* kMatrix = "a CUDA matrix of torch.bfloat16 with rows of consecutive elements";
+        const at::Tensor *x, *w, *up = nullptr, *res = nullptr, *o = nullptr;
+        if (!(x = rows(a[0], at::kBFloat16, "x", kMatrix)) || !(w = rows(a[1], at::kBFloat16, "w", kMatrix))) return nullptr;
+        int T, K, N, act;
+        if (!int32_of(x->size(0), &T, "x") || !int32_of(w->size(0), &N, "w") || !int32_of(w->size(1), &K, "w")) return nullptr;
+        if (x->size(1) != K) return wrong("x", "[T, d_in]"), nullptr;
+        if (a[3] != Py_None && (!(up = rows(a[3], at::kBFloat16, "w_up", kMatrix)) || !sized(*up, {N, K}, "w_up", "as many rows and columns as w"))) return nullptr;
+        bool ok = true;
+        const at::Tensor* b = optional_f32(a[2], {N}, "bias", "[d_out]", &ok);
+        if (!ok) return nullptr;
+        const at::Tensor* bu = optional_f32(a[4], {N}, "bias_up", "[d_out]", &ok);
+        if (!ok) return nullptr;
+        if (bu && !up) return wrong("bias_up", "w_up"), nullptr;
+        at::ScalarType dt;
+        if (!activation_of(a[5], &act) || !result_type(a[6] != Py_None ? a[6] : a[7], a[8], "the type of residual and out", &dt)) return nullptr;
+        constexpr const char* kRows = "a CUDA matrix [T, d_out] of torch.float32 or torch.bfloat16 with rows of consecutive elements";
+        if (a[6] != Py_None && (!(res = rows(a[6], dt, "residual", kRows)) || !sized(*res, {T, N}, "residual", kRows))) return nullptr;
+        if (a[7] != Py_None && (!(o = rows(a[7], dt, "out", kRows)) || !sized(*o, {T, N}, "out", kRows))) return nullptr;
+        if (!here(*x, "x") || !here(*w, "w") || (up && !here(*up, "w_up")) || (res && !here(*res, "residual")) || (o && !here(*o, "out"))) return nullptr;
+        void* st;
+        if (!stream_of(a[9], &st)) return nullptr;
+        const OnStream on(a[9], st);
+        at::Tensor out = o ? *o : empty_on(*x, {T, N}, dt);
+        const exmoe_linear_shape s{K, N, act};
+        int rc;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_linear(&s, x->data_ptr(), pitch8(*x), w->data_ptr(), pitch8(*w), data_of(b), up ? up->data_ptr() : nullptr, up ? pitch8(*up) : 0, data_of(bu), T,
+                      res ? res->data_ptr() : nullptr, res ? pitch(*res) : 0, out.data_ptr(), pitch(out), dt == at::kFloat ? EXMOE_F32 : EXMOE_BF16, st);
+        Py_END_ALLOW_THREADS
+        if (rc) return PyLong_FromLong(rc);
+        return o ? Py_NewRef(a[7]) : THPVariable_Wrap(std::move(out));
+    });
+}
+
 // set_entry_points(addresses in the loaded libexmoe.so, in the order of binding.py's list)
 PyObject* set_entry_points(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 8) return PyErr_Format(PyExc_TypeError, "set_entry_points: 8 addresses");
+    if (n != 12) return PyErr_Format(PyExc_TypeError, "set_entry_points: 12 addresses");
     g_route = reinterpret_cast<decltype(g_route)>(PyLong_AsVoidPtr(a[0]));
     g_forward = reinterpret_cast<decltype(g_forward)>(PyLong_AsVoidPtr(a[1]));
     g_forward_host = reinterpret_cast<decltype(g_forward_host)>(PyLong_AsVoidPtr(a[2]));
@@ -438,6 +605,10 @@ PyObject* set_entry_points(PyObject*, PyObject* const* a, Py_ssize_t n) {
     g_lora_plan_bytes = reinterpret_cast<decltype(g_lora_plan_bytes)>(PyLong_AsVoidPtr(a[5]));
     g_lora_plan = reinterpret_cast<decltype(g_lora_plan)>(PyLong_AsVoidPtr(a[6]));
     g_lora = reinterpret_cast<decltype(g_lora)>(PyLong_AsVoidPtr(a[7]));
+    g_balance_scratch_bytes = reinterpret_cast<decltype(g_balance_scratch_bytes)>(PyLong_AsVoidPtr(a[8]));
+    g_balance_loss = reinterpret_cast<decltype(g_balance_loss)>(PyLong_AsVoidPtr(a[9]));
+    g_gate_backward = reinterpret_cast<decltype(g_gate_backward)>(PyLong_AsVoidPtr(a[10]));
+    g_linear = reinterpret_cast<decltype(g_linear)>(PyLong_AsVoidPtr(a[11]));
     if (PyErr_Occurred()) return nullptr;
     Py_RETURN_NONE;
 }
@@ -450,6 +621,9 @@ PyMethodDef methods[] = {
     {"gate_logits", reinterpret_cast<PyCFunction>(gate_logits), METH_FASTCALL, nullptr},
     {"lora_plan", reinterpret_cast<PyCFunction>(lora_plan), METH_FASTCALL, nullptr},
     {"lora", reinterpret_cast<PyCFunction>(lora), METH_FASTCALL, nullptr},
+    {"balance_loss", reinterpret_cast<PyCFunction>(balance_loss), METH_FASTCALL, nullptr},
+    {"gate_backward", reinterpret_cast<PyCFunction>(gate_backward), METH_FASTCALL, nullptr},
+    {"linear", reinterpret_cast<PyCFunction>(linear), METH_FASTCALL, nullptr},
     {"set_entry_points", reinterpret_cast<PyCFunction>(set_entry_points), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_exmoe_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -102,6 +102,21 @@ constexpr int kSmallMaxSlots = 1024;
 template <typename... P>
 inline bool aligned(size_t bytes, const P*... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) & (bytes - 1)) == 0; }
 
+// [rows, cols] elements of `es` bytes, rows `ld` elements apart: do two such ranges share a byte?  Column ranges of the same wider rows do not.
+struct Range { uintptr_t at; long long rows, pitch, width; };
+inline Range range_of(const void* p, long long rows, long long ld, long long cols, long long es) {
+    return Range{reinterpret_cast<uintptr_t>(p), rows, ld * es, cols * es};
+}
+inline bool overlap(const Range& a, const Range& b) {
+    if (!a.at || !b.at || a.rows <= 0 || b.rows <= 0) return false;
+    const uintptr_t a_end = a.at + (a.rows - 1) * a.pitch + a.width, b_end = b.at + (b.rows - 1) * b.pitch + b.width;
+    if (a_end <= b.at || b_end <= a.at) return false;
+    if (a.pitch != b.pitch || a.rows == 1 || b.rows == 1) return true;
+    const long long d = (long long)((b.at > a.at ? b.at - a.at : a.at - b.at) % (uintptr_t)a.pitch);   // column distance
+    const Range &lo = b.at > a.at ? a : b, &hi = b.at > a.at ? b : a;
+    return !(d >= lo.width && d + hi.width <= a.pitch);
+}
+
 // launch accounting (exmoe_launch_count)
 void count_launch(int n = 1);
 

@@ -249,29 +249,6 @@ gate_few_kernel(const __nv_bfloat16* hidden, const __nv_bfloat16* __restrict__ w
     }
 }
 
-int check_gate(const exmoe_shape* shape, const exmoe_gate* gate, int T, GateArgs* a) {
-    if (!shape || !gate || T < 0 || T > kMaxTokens) return EXMOE_ERR_ARG;
-    if ((gate->score != EXMOE_SCORE_SOFTMAX && gate->score != EXMOE_SCORE_SIGMOID) ||
-        (gate->group_score != EXMOE_GROUP_MAX && gate->group_score != EXMOE_GROUP_TOP2) || (gate->renormalise != 0 && gate->renormalise != 1))
-        return EXMOE_ERR_ARG;
-    if (shape->num_experts <= 0 || shape->num_experts > 4096 || shape->top_k <= 0) return EXMOE_ERR_SHAPE;
-    if (gate->num_groups < 1 || gate->num_groups > 32 || shape->num_experts % gate->num_groups || gate->top_groups < 1 ||
-        gate->top_groups > gate->num_groups)
-        return EXMOE_ERR_SHAPE;
-    const int size = shape->num_experts / gate->num_groups;
-    if (shape->top_k > gate->top_groups * size) return EXMOE_ERR_SHAPE;
-    int log_lanes = 5;
-    while (gate->num_groups << log_lanes > 32) --log_lanes;
-    *a = GateArgs{shape->num_experts, shape->top_k, gate->num_groups, size, gate->top_groups, gate->score == EXMOE_SCORE_SIGMOID,
-                  gate->group_score == EXMOE_GROUP_TOP2, gate->renormalise != 0, gate->weight_scale, nullptr, 1 << log_lanes, log_lanes, (size + (1 << log_lanes) - 1) >> log_lanes, -1, 1.f / (float)size};
-    if (shape->num_experts <= kFastExperts) {                              // choose_fast's run of a lane
-        const int run = shape->num_experts <= 64 ? 2 : shape->num_experts <= 128 ? 4 : shape->num_experts <= 256 ? 8 : 16;
-        for (int l = 0; l <= 5; ++l)
-            if (run << l == size) a->log_run = l;
-    }
-    return EXMOE_OK;
-}
-
 // From how many tokens on the tensor cores (at most 256 experts) are faster than four tokens per cluster, by the size of the router's matrix.
 // us, four / tensor cores, means of four batches: 16 experts of d_model 512: 256 tokens 10.2 / 10.9, 384: 13.9 / 10.9.   64 of 2048: 128 9.1 / 12.0,
 // 192: 13.7 / 12.8.   128 of 2048: 128 14.8 / 17.1, 192: 20.0 / 18.1.   256 of 1024: 128 14.9 / 16.9, 192: 20.9 / 16.9.   64 of 4096: 128 14.0 / 14.7,
@@ -315,6 +292,29 @@ int launch_logits(const Z* z, long long ld, int T, const GateArgs& g, int32_t* i
 }
 
 }  // namespace
+
+int check_gate(const exmoe_shape* shape, const exmoe_gate* gate, int T, GateArgs* a) {
+    if (!shape || !gate || T < 0 || T > kMaxTokens) return EXMOE_ERR_ARG;
+    if ((gate->score != EXMOE_SCORE_SOFTMAX && gate->score != EXMOE_SCORE_SIGMOID) ||
+        (gate->group_score != EXMOE_GROUP_MAX && gate->group_score != EXMOE_GROUP_TOP2) || (gate->renormalise != 0 && gate->renormalise != 1))
+        return EXMOE_ERR_ARG;
+    if (shape->num_experts <= 0 || shape->num_experts > 4096 || shape->top_k <= 0) return EXMOE_ERR_SHAPE;
+    if (gate->num_groups < 1 || gate->num_groups > 32 || shape->num_experts % gate->num_groups || gate->top_groups < 1 ||
+        gate->top_groups > gate->num_groups)
+        return EXMOE_ERR_SHAPE;
+    const int size = shape->num_experts / gate->num_groups;
+    if (shape->top_k > gate->top_groups * size) return EXMOE_ERR_SHAPE;
+    int log_lanes = 5;
+    while (gate->num_groups << log_lanes > 32) --log_lanes;
+    *a = GateArgs{shape->num_experts, shape->top_k, gate->num_groups, size, gate->top_groups, gate->score == EXMOE_SCORE_SIGMOID,
+                  gate->group_score == EXMOE_GROUP_TOP2, gate->renormalise != 0, gate->weight_scale, nullptr, 1 << log_lanes, log_lanes, (size + (1 << log_lanes) - 1) >> log_lanes, -1, 1.f / (float)size};
+    if (shape->num_experts <= kFastExperts) {                              // choose_fast's run of a lane
+        const int run = shape->num_experts <= 64 ? 2 : shape->num_experts <= 128 ? 4 : shape->num_experts <= 256 ? 8 : 16;
+        for (int l = 0; l <= 5; ++l)
+            if (run << l == size) a->log_run = l;
+    }
+    return EXMOE_OK;
+}
 
 extern "C" int exmoe_route_gated(const exmoe_shape* shape, const exmoe_gate* gate, const void* hidden_bf16, const void* router_bf16,
                                  const float* bias, const float* addend, const float* balance, int T, int32_t* topk_ids,

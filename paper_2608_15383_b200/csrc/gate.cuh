@@ -765,6 +765,7 @@ int launch(void (*kern)(P...), unsigned ctas, int threads, int cluster, size_t s
     return EXMOE_OK;
 }
 
+int check_gate(const exmoe_shape* shape, const exmoe_gate* gate, int T, GateArgs* a);      // EXMOE_OK and `a`, or what is wrong with them
 // Many tokens, at most 256 experts: the logits on tensor cores (gate_tc.cu).
 int launch_gate_tc(const __nv_bfloat16* x, const __nv_bfloat16* w, const float* bias, const float* addend, int T, int H, const GateArgs& g, int32_t* ids,
                    float* weights, cudaStream_t st);

@@ -1,0 +1,165 @@
+// Products with an epilogue (exmoe_linear): out = residual + act(x W^T + bias), or residual + act(x W^T + bias) * (x U^T + bias_up).
+#include <algorithm>
+
+#include "common.cuh"
+#include "frag.cuh"
+#include "gate.cuh"
+
+namespace exmoe {
+
+namespace {
+
+constexpr int kMaxTokens = 1 << 29, kMaxDim = 1 << 30;
+
+struct LinearArgs {
+    const __nv_bfloat16 *x, *w, *w_up;   // w_up: null without a second factor
+    const float *bias, *bias_up;         // or null
+    const void* residual;                // or null
+    void* out;
+    long long ld_x, ld_w, ld_up, ld_res, ld_out;
+    int T, K, N, act;
+};
+
+__device__ __forceinline__ float activate(float v, int act) {
+    switch (act) {
+        case EXMOE_ACT_RELU: return v < 0.f ? 0.f : v;                     // a NaN stays one
+        case EXMOE_ACT_GELU: return v * normcdff(v);
+        case EXMOE_ACT_GELU_TANH: {                                        // (1 + tanh y) / 2 = 1 / (1 + exp(-2 y))
+            const float y = 0.7978845608028654f * fmaf(0.044715f * v * v, v, v);
+            return __fdividef(v, 1.f + __expf(-2.f * y));
+        }
+        case EXMOE_ACT_SILU: return __fdividef(v, 1.f + __expf(-v));
+        default: return v;
+    }
+}
+template <typename O> __device__ __forceinline__ float load_out(const void* p, long long at);
+template <> __device__ __forceinline__ float load_out<float>(const void* p, long long at) { return static_cast<const float*>(p)[at]; }
+template <> __device__ __forceinline__ float load_out<__nv_bfloat16>(const void* p, long long at) { return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[at]); }
+__device__ __forceinline__ void store_out(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store_out(__nv_bfloat16* p, float v) { *p = __float2bfloat16(v); }
+
+// Few tokens.  A CTA takes 16 rows of W (8 of W and 8 of U: the two factors meet in one lane) and 8 NT tokens; its warps split K.
+// Weights are the MMA's rows: a lane's 16 bytes of a row are k = 8 c .. 8 c + 7 of every 32, the k that two MMAs take from it, and the
+// tokens are read in the same order.
+constexpr int kFewThreads = 256, kFewWarps = kFewThreads / 32, kFewAhead = 4;
+
+template <typename O, int NT, bool GATED>
+__global__ void __launch_bounds__(kFewThreads)
+linear_few_kernel(const __grid_constant__ LinearArgs a) {
+    __shared__ float part[kFewWarps][NT][16][9];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
+    const int rows = GATED ? 8 : 16;
+    const long long n0 = (long long)blockIdx.x * rows, t0 = (long long)blockIdx.y * 8 * NT;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const uint4 zero = make_uint4(0, 0, 0, 0);
+    const bool row_a = n0 + g < a.N, row_b = GATED ? row_a : n0 + 8 + g < a.N;
+    const __nv_bfloat16* wa = a.w + (n0 + g) * a.ld_w + 8 * c;
+    const __nv_bfloat16* wb = GATED ? a.w_up + (n0 + g) * a.ld_up + 8 * c : a.w + (n0 + 8 + g) * a.ld_w + 8 * c;
+    float acc[NT][4];
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+    const int blocks = (a.K + 31) / 32;
+    for (int b0 = warp; b0 < blocks; b0 += kFewWarps * kFewAhead) {
+        uint4 va[kFewAhead], vb[kFewAhead], vx[kFewAhead][NT];
+#pragma unroll
+        for (int u = 0; u < kFewAhead; ++u) {
+            const int k = (b0 + u * kFewWarps) * 32;
+            const bool in = k + 8 * c < a.K;
+            va[u] = in && row_a ? *reinterpret_cast<const uint4*>(wa + k) : zero;
+            vb[u] = in && row_b ? *reinterpret_cast<const uint4*>(wb + k) : zero;
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                const long long t = t0 + 8 * i + g;
+                vx[u][i] = in && t < a.T ? *reinterpret_cast<const uint4*>(a.x + t * a.ld_x + 8 * c + k) : zero;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kFewAhead; ++u)
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                mma_m16n8k16(acc[i], va[u].x, vb[u].x, va[u].y, vb[u].y, vx[u][i].x, vx[u][i].y);
+                mma_m16n8k16(acc[i], va[u].z, vb[u].z, va[u].w, vb[u].w, vx[u][i].z, vx[u][i].w);
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        part[warp][i][g][2 * c] = acc[i][0];
+        part[warp][i][g][2 * c + 1] = acc[i][1];
+        part[warp][i][8 + g][2 * c] = acc[i][2];
+        part[warp][i][8 + g][2 * c + 1] = acc[i][3];
+    }
+    __syncthreads();
+    for (int i = tid; i < NT * 8 * rows; i += kFewThreads) {
+        const int r = i % rows, tt = i / rows, nt = tt >> 3, col = tt & 7;
+        const long long n = n0 + r, t = t0 + tt;
+        if (n >= a.N || t >= a.T) continue;
+        float v = 0.f, u = 0.f;
+#pragma unroll
+        for (int w = 0; w < kFewWarps; ++w) {
+            v += part[w][nt][r][col];
+            if (GATED) u += part[w][nt][8 + r][col];
+        }
+        v = activate(v + (a.bias ? a.bias[n] : 0.f), a.act);
+        if (GATED) v *= u + (a.bias_up ? a.bias_up[n] : 0.f);
+        if (a.residual) v += load_out<O>(a.residual, t * a.ld_res + n);
+        store_out(static_cast<O*>(a.out) + t * a.ld_out + n, v);
+    }
+}
+
+template <typename O, int NT, bool GATED>
+int launch_few(const LinearArgs& a, cudaStream_t st) {
+    constexpr int rows = GATED ? 8 : 16;
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = dim3((unsigned)((a.N + rows - 1) / rows), (unsigned)((a.T + 8 * NT - 1) / (8 * NT)));
+    lc.blockDim = dim3(kFewThreads);
+    lc.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 1;
+#ifdef EXMOE_DISABLE_PDL
+    lc.numAttrs = 0;
+#endif
+    if (cudaLaunchKernelEx(&lc, linear_few_kernel<O, NT, GATED>, a) != cudaSuccess) {
+        cudaGetLastError();
+        return EXMOE_ERR_CUDA;
+    }
+    count_launch();
+    return EXMOE_OK;
+}
+template <typename O, bool GATED>
+int launch_linear(const LinearArgs& a, cudaStream_t st) {
+    return a.T <= 8 ? launch_few<O, 1, GATED>(a, st) : launch_few<O, 2, GATED>(a, st);
+}
+
+}  // namespace
+
+extern "C" int exmoe_linear(const exmoe_linear_shape* shape, const void* x, int64_t ld_x, const void* w, int64_t ld_w, const float* bias, const void* w_up,
+                            int64_t ld_w_up, const float* bias_up, int T, const void* residual, int64_t ld_residual, void* out, int64_t ld_out, int type,
+                            void* stream) {
+    if (!shape || T < 0 || T > kMaxTokens || (type != EXMOE_F32 && type != EXMOE_BF16)) return EXMOE_ERR_ARG;
+    const int K = shape->d_in, N = shape->d_out;
+    if (shape->activation < EXMOE_ACT_NONE || shape->activation > EXMOE_ACT_SILU) return EXMOE_ERR_ARG;
+    if (K <= 0 || K % 8 || N <= 0 || K > kMaxDim || N > kMaxDim) return EXMOE_ERR_SHAPE;
+    if (T == 0) return EXMOE_OK;
+    if (!x || !w || !out || (bias_up && !w_up)) return EXMOE_ERR_ARG;
+    if (ld_x < K || ld_x % 8 || ld_w < K || ld_w % 8 || (w_up && (ld_w_up < K || ld_w_up % 8)) || ld_out < N || (residual && ld_residual < N)) return EXMOE_ERR_ARG;
+    const long long es = type == EXMOE_F32 ? 4 : 2;
+    if (!aligned(16, x, w, w_up) || !aligned(4, bias, bias_up) || !aligned(es, residual, out)) return EXMOE_ERR_ARG;
+    const Range o = range_of(out, T, ld_out, N, es);
+    if ((!(residual == out && (ld_residual == ld_out || T == 1)) && overlap(o, range_of(residual, T, ld_residual, N, es))) || overlap(o, range_of(x, T, ld_x, K, 2)) ||
+        overlap(o, range_of(w, N, ld_w, K, 2)) || overlap(o, range_of(w_up, N, ld_w_up, K, 2)) || overlap(o, range_of(bias, 1, 0, N, 4)) ||
+        overlap(o, range_of(bias_up, 1, 0, N, 4)))
+        return EXMOE_ERR_ARG;
+    const LinearArgs a{(const __nv_bfloat16*)x, (const __nv_bfloat16*)w, (const __nv_bfloat16*)w_up, bias, bias_up, residual, out, ld_x, ld_w, ld_w_up,
+                       ld_residual, ld_out, T, K, N, shape->activation};
+    cudaStream_t st = (cudaStream_t)stream;
+    if (type == EXMOE_F32) return w_up ? launch_linear<float, true>(a, st) : launch_linear<float, false>(a, st);
+    return w_up ? launch_linear<__nv_bfloat16, true>(a, st) : launch_linear<__nv_bfloat16, false>(a, st);
+}
+
+}  // namespace exmoe

@@ -626,18 +626,6 @@ int check_plan(int T, int n) {
     return n < 1 || n > kMaxAdapters ? EXMOE_ERR_SHAPE : EXMOE_OK;
 }
 
-// [rows, cols] elements of `es` bytes, rows `ld` elements apart: do two such ranges share a byte?  Column ranges of the same wider rows do not.
-struct Range { uintptr_t at; long long rows, pitch, width; };
-bool overlap(const Range& a, const Range& b) {
-    if (!a.at || !b.at || a.rows <= 0 || b.rows <= 0) return false;
-    const uintptr_t a_end = a.at + (a.rows - 1) * a.pitch + a.width, b_end = b.at + (b.rows - 1) * b.pitch + b.width;
-    if (a_end <= b.at || b_end <= a.at) return false;
-    if (a.pitch != b.pitch || a.rows == 1 || b.rows == 1) return true;
-    const long long d = (long long)((b.at > a.at ? b.at - a.at : a.at - b.at) % (uintptr_t)a.pitch);   // column distance
-    const Range &lo = b.at > a.at ? a : b, &hi = b.at > a.at ? b : a;
-    return !(d >= lo.width && d + hi.width <= a.pitch);
-}
-
 }  // namespace
 
 extern "C" int exmoe_lora_plan_bytes(int T, int num_adapters, size_t* bytes) {
@@ -693,14 +681,11 @@ static int lora_call(const exmoe_lora_shape* shape, void* plan, const void* x, i
     if (ld_x < K || ld_x % 8 || ld_out < N || (base && ld_base < N)) return EXMOE_ERR_ARG;
     const long long es = type == EXMOE_F32 ? 4 : 2;
     if (!aligned(16, plan, x, a, b) || !aligned(4, scale) || !aligned(es, base, out)) return EXMOE_ERR_ARG;
-    auto range = [](const void* p, long long rows, long long ld, long long width, long long es) {
-        return Range{reinterpret_cast<uintptr_t>(p), rows, ld * es, width * es};
-    };
     size_t plan_size = 0;
     exmoe_lora_plan_bytes(T, n, &plan_size);
-    const Range o = range(out, T, ld_out, N, es), bs = range(base, T, ld_base, N, es);
-    if ((!(base == out && (ld_base == ld_out || T == 1)) && overlap(o, bs)) || overlap(o, range(x, T, ld_x, K, 2)) || overlap(o, range(a, 1, 0, (long long)n * r * K, 2)) ||
-        overlap(o, range(b, 1, 0, (long long)n * r * N, 2)) || overlap(o, range(scale, 1, 0, n, 4)) || overlap(o, range(plan, 1, 0, (long long)plan_size, 1)))
+    const Range o = range_of(out, T, ld_out, N, es), bs = range_of(base, T, ld_base, N, es);
+    if ((!(base == out && (ld_base == ld_out || T == 1)) && overlap(o, bs)) || overlap(o, range_of(x, T, ld_x, K, 2)) || overlap(o, range_of(a, 1, 0, (long long)n * r * K, 2)) ||
+        overlap(o, range_of(b, 1, 0, (long long)n * r * N, 2)) || overlap(o, range_of(scale, 1, 0, n, 4)) || overlap(o, range_of(plan, 1, 0, (long long)plan_size, 1)))
         return EXMOE_ERR_ARG;
     const LoraArgs args{(int32_t*)plan, (const __nv_bfloat16*)x, (const __nv_bfloat16*)a, (const __nv_bfloat16*)b, scale, base, out,
                         ld_x, ld_base, ld_out, T, n, K, N, r};
