@@ -305,6 +305,10 @@ int exmoe_linear(const exmoe_linear_shape* shape, const void* x, int64_t ld_x, c
                  int64_t ld_w_up, const float* bias_up, int T, const void* residual, int64_t ld_residual, void* out, int64_t ld_out, int type,
                  void* stream);
 
+/* Sticky device-side status of exmoe_linear on the current device: synchronises it, returns EXMOE_OK, or EXMOE_ERR_TIMEOUT if a bounded wait of its
+ * tensor-core kernels expired since the previous call of this function (what that call wrote is then not to be used), and clears it. */
+int exmoe_linear_status(void);
+
 /* Low-rank adapters of many requests beside a projection that all of them share (the paper has none; packed int4 weights cannot
  * take an adapter in, and the requests of a batch bring different ones).  For token t with adapter a:
  *   out_t = base_t + scale_a * B_a (A_a x_t)

@@ -81,6 +81,7 @@ _SIGNATURES = {
     "exmoe_gate_backward": (c_int, [POINTER(exmoe_shape), POINTER(exmoe_gate), c_void_p, c_int, c_int64] + [c_void_p] * 7 + [c_int, c_int, c_void_p, c_int64, c_void_p]),
     "exmoe_linear": (c_int, [POINTER(exmoe_linear_shape), c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_void_p, c_int64, c_void_p, c_int, c_void_p, c_int64,
                              c_void_p, c_int64, c_int, c_void_p]),
+    "exmoe_linear_status": (c_int, []),
     "exmoe_lora_plan_bytes": (c_int, [c_int, c_int, POINTER(c_size_t)]),
     "exmoe_lora_plan": (c_int, [c_void_p, c_int, c_int, c_void_p, c_void_p]),
     "exmoe_lora_plan_status": (c_int, [c_void_p]),
@@ -287,6 +288,11 @@ def exmoe_linear(x, w, bias=None, w_up=None, bias_up=None, activation="none", re
     if r.__class__ is int:
         raise ExmoeError(r, "exmoe_linear")
     return r
+
+
+def exmoe_linear_status():
+    """EXMOE_OK, or EXMOE_ERR_TIMEOUT if a bounded wait of exmoe_linear expired since the last call (synchronises, clears)."""
+    return int(lib().exmoe_linear_status())
 
 
 def exmoe_lora_plan(adapter_ids, num_adapters, plan=None, stream=None):

@@ -3,40 +3,13 @@
 
 #include "common.cuh"
 #include "frag.cuh"
-#include "gate.cuh"
+#include "linear.cuh"
 
 namespace exmoe {
 
 namespace {
 
 constexpr int kMaxTokens = 1 << 29, kMaxDim = 1 << 30;
-
-struct LinearArgs {
-    const __nv_bfloat16 *x, *w, *w_up;   // w_up: null without a second factor
-    const float *bias, *bias_up;         // or null
-    const void* residual;                // or null
-    void* out;
-    long long ld_x, ld_w, ld_up, ld_res, ld_out;
-    int T, K, N, act;
-};
-
-__device__ __forceinline__ float activate(float v, int act) {
-    switch (act) {
-        case EXMOE_ACT_RELU: return v < 0.f ? 0.f : v;                     // a NaN stays one
-        case EXMOE_ACT_GELU: return v * normcdff(v);
-        case EXMOE_ACT_GELU_TANH: {                                        // (1 + tanh y) / 2 = 1 / (1 + exp(-2 y))
-            const float y = 0.7978845608028654f * fmaf(0.044715f * v * v, v, v);
-            return __fdividef(v, 1.f + __expf(-2.f * y));
-        }
-        case EXMOE_ACT_SILU: return __fdividef(v, 1.f + __expf(-v));
-        default: return v;
-    }
-}
-template <typename O> __device__ __forceinline__ float load_out(const void* p, long long at);
-template <> __device__ __forceinline__ float load_out<float>(const void* p, long long at) { return static_cast<const float*>(p)[at]; }
-template <> __device__ __forceinline__ float load_out<__nv_bfloat16>(const void* p, long long at) { return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[at]); }
-__device__ __forceinline__ void store_out(float* p, float v) { *p = v; }
-__device__ __forceinline__ void store_out(__nv_bfloat16* p, float v) { *p = __float2bfloat16(v); }
 
 // Few tokens.  A CTA takes 16 rows of W (8 of W and 8 of U: the two factors meet in one lane) and 8 NT tokens; its warps split K.
 // Weights are the MMA's rows: a lane's 16 bytes of a row are k = 8 c .. 8 c + 7 of every 32, the k that two MMAs take from it, and the
@@ -131,8 +104,10 @@ int launch_few(const LinearArgs& a, cudaStream_t st) {
     count_launch();
     return EXMOE_OK;
 }
+// Tokens that the form for few takes: four times eight would hold four weights' fragments per 16 bytes of them.
+constexpr int kFewTokens = 16;
 template <typename O, bool GATED>
-int launch_linear(const LinearArgs& a, cudaStream_t st) {
+int launch_few_tokens(const LinearArgs& a, cudaStream_t st) {
     return a.T <= 8 ? launch_few<O, 1, GATED>(a, st) : launch_few<O, 2, GATED>(a, st);
 }
 
@@ -158,8 +133,9 @@ extern "C" int exmoe_linear(const exmoe_linear_shape* shape, const void* x, int6
     const LinearArgs a{(const __nv_bfloat16*)x, (const __nv_bfloat16*)w, (const __nv_bfloat16*)w_up, bias, bias_up, residual, out, ld_x, ld_w, ld_w_up,
                        ld_residual, ld_out, T, K, N, shape->activation};
     cudaStream_t st = (cudaStream_t)stream;
-    if (type == EXMOE_F32) return w_up ? launch_linear<float, true>(a, st) : launch_linear<float, false>(a, st);
-    return w_up ? launch_linear<__nv_bfloat16, true>(a, st) : launch_linear<__nv_bfloat16, false>(a, st);
+    if (T > kFewTokens) return launch_linear_tc(a, type, st);
+    if (type == EXMOE_F32) return w_up ? launch_few_tokens<float, true>(a, st) : launch_few_tokens<float, false>(a, st);
+    return w_up ? launch_few_tokens<__nv_bfloat16, true>(a, st) : launch_few_tokens<__nv_bfloat16, false>(a, st);
 }
 
 }  // namespace exmoe

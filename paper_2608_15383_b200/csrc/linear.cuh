@@ -1,0 +1,37 @@
+// What the kernels of exmoe_linear share: arguments, activations, access to results.
+#pragma once
+#include "common.cuh"
+
+namespace exmoe {
+
+struct LinearArgs {
+    const __nv_bfloat16 *x, *w, *w_up;   // w_up: null without a second factor
+    const float *bias, *bias_up;         // or null
+    const void* residual;                // or null
+    void* out;
+    long long ld_x, ld_w, ld_up, ld_res, ld_out;
+    int T, K, N, act;
+};
+
+__device__ __forceinline__ float activate(float v, int act) {
+    switch (act) {
+        case EXMOE_ACT_RELU: return v < 0.f ? 0.f : v;                     // a NaN stays one
+        case EXMOE_ACT_GELU: return v * normcdff(v);
+        case EXMOE_ACT_GELU_TANH: {                                        // (1 + tanh y) / 2 = 1 / (1 + exp(-2 y))
+            const float y = 0.7978845608028654f * fmaf(0.044715f * v * v, v, v);
+            return __fdividef(v, 1.f + __expf(-2.f * y));
+        }
+        case EXMOE_ACT_SILU: return __fdividef(v, 1.f + __expf(-v));
+        default: return v;
+    }
+}
+template <typename O> __device__ __forceinline__ float load_out(const void* p, long long at);
+template <> __device__ __forceinline__ float load_out<float>(const void* p, long long at) { return static_cast<const float*>(p)[at]; }
+template <> __device__ __forceinline__ float load_out<__nv_bfloat16>(const void* p, long long at) { return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[at]); }
+__device__ __forceinline__ void store_out(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store_out(__nv_bfloat16* p, float v) { *p = __float2bfloat16(v); }
+
+// More than a few tokens, on tensor cores (linear_tc.cu).
+int launch_linear_tc(const LinearArgs& a, int type, cudaStream_t st);
+
+}  // namespace exmoe

@@ -1,0 +1,312 @@
+// exmoe_linear on tcgen05: D = W X^T with the weights' rows as the MMA's M and the tokens as its N, so that a warp's lanes hold consecutive
+// outputs of one token: they are read and written in runs of 32 whatever the rows' distances and alignment are.
+//
+// Two forms.  `linear_split_kernel`: a tile of 128 rows by up to 128 tokens per cluster of CL CTAs, which split K and add their parts through
+// the cluster's shared memory in a fixed order.  `linear_pair_kernel`: persistent pairs of CTAs (cta_group::2), 256 rows by up to 256 tokens.
+// Both: TMA into a ring of 64-wide stages with the 128-byte swizzle, one warp issuing the MMAs; chains of kChain stages (32 MMAs) that start from zero in one of
+// two accumulators, and warps that take them out of tensor memory and add them to binary32 sums in registers.  An MMA truncates what it adds
+// (a few units of 2^-24 of all that its chain has summed): over a whole K of thousands that would show in a binary32 result.
+//
+// With a second matrix a tile's 128 rows are 64 of W and the same 64 of U: a row's two factors are 64 lanes of tensor memory apart and meet in shared memory.
+#include <algorithm>
+
+#include "common.cuh"
+#include "frag.cuh"
+#include "linear.cuh"
+#include "mbar.cuh"
+#include "tc.cuh"
+
+namespace exmoe {
+
+namespace {
+
+constexpr int kSms = 148;
+constexpr int kChain = 8;                                                  // stages
+constexpr int kABytes = BM * 128;                                          // weights of a stage: 128 rows of 64 elements
+__device__ int g_linear_status;                                            // sticky: EXMOE_ERR_TIMEOUT
+
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr));
+}
+__device__ __forceinline__ void cluster_arrive() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t at_rank(uint32_t addr, int rank) {
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+    return at;
+}
+__device__ __forceinline__ void in_flight_end(uint32_t bar, uint32_t parity) {
+    const long long t0 = clock64();
+    while (!mbar_try_at(bar, parity) && clock64() - t0 < kWaitBudget) {}
+}
+// Takes up to 64 columns of a chain's accumulator (this warp's lanes) into acc: in pieces of 8, `cols` of them in use.
+__device__ __forceinline__ void drain(uint32_t at, int cols, bool first, float (&acc)[64]) {
+#pragma unroll
+    for (int c = 0; c < 64; c += 16) {
+        if (c < cols) {
+            uint32_t r[8], s[8];
+            tmem_ld8(at + c, r);
+            if (c + 8 < cols) tmem_ld8(at + c + 8, s);
+            tc_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[c + i] = first ? __uint_as_float(r[i]) : acc[c + i] + __uint_as_float(r[i]);
+            if (c + 8 < cols) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[c + 8 + i] = first ? __uint_as_float(s[i]) : acc[c + 8 + i] + __uint_as_float(s[i]);
+            }
+        }
+    }
+}
+
+// ---- one CTA per tile part -----------------------------------------------------------------------------------------
+constexpr int kSplitStages = 6, kSplitThreads = 32 * 12, kSplitTokens = 128;
+struct __align__(1024) SplitShared {
+    union {
+        unsigned char ring[kSplitStages][kABytes + kSplitTokens * 128];
+        float part[kSplitTokens][BM];                                      // this CTA's part of the tile
+    };
+    uint64_t full[kSplitStages], empty[kSplitStages], acc_full[2], acc_empty[2], drained;
+    uint32_t tmem;
+    int abort_flag;
+};
+
+__device__ __forceinline__ void mma_one(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+
+template <typename O, bool GATED>
+__global__ void __launch_bounds__(kSplitThreads, 1)
+linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_u, const __grid_constant__ CUtensorMap map_x,
+                    const __grid_constant__ LinearArgs a, int BN, int CL, int row_tiles) {
+    extern __shared__ unsigned char raw[];
+    SplitShared& sm = *reinterpret_cast<SplitShared*>(raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u));
+    constexpr int kRows = GATED ? BM / 2 : BM;                             // outputs of a tile
+    const int tid = threadIdx.x, lane = tid & 31, warp = warp_uniform(tid >> 5);
+    const int rank = (int)blockIdx.x % CL, tile = (int)blockIdx.x / CL;
+    const int n0 = tile % row_tiles * kRows, t0 = tile / row_tiles * BN;
+    volatile int* abort_flag = &sm.abort_flag;
+    if (tid == 0) {
+        for (int s = 0; s < kSplitStages; ++s) {
+            mbar_init(&sm.full[s], 1);
+            mbar_init(&sm.empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&sm.acc_full[b], 1);
+            mbar_init(&sm.acc_empty[b], 8);
+        }
+        mbar_init(&sm.drained, 1);
+        sm.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem)), "r"(2 * kSplitTokens));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sm.tmem;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int blocks = (a.K + 63) / 64, kb0 = (int)((long long)blocks * rank / CL), n = (int)((long long)blocks * (rank + 1) / CL) - kb0;
+    const uint32_t stage_bytes = (uint32_t)(kABytes + BN * 128);
+    const uint32_t full = smem_u32(sm.full), empty = smem_u32(sm.empty), acc_full = smem_u32(sm.acc_full), acc_empty = smem_u32(sm.acc_empty);
+    bool ok = true;
+    if (warp == 0) {
+        int i = 0;
+        for (; i < n; ++i) {
+            const int s = i % kSplitStages;
+            if (i >= kSplitStages) ok = mbar_wait_warp(empty + 8 * s, (i / kSplitStages - 1) & 1, abort_flag, &g_linear_status);
+            if (!ok) break;
+            if (elect_one()) {
+                const uint32_t at = smem_u32(sm.ring[s]);
+                const int k = (kb0 + i) * 64;
+                mbar_expect_tx(&sm.full[s], stage_bytes);
+                tma_load_2d(at, &map_w, k, n0, &sm.full[s]);
+                if (GATED) tma_load_2d(at + kABytes / 2, &map_u, k, n0, &sm.full[s]);
+                tma_load_2d(at + kABytes, &map_x, k, t0, &sm.full[s]);
+            }
+            __syncwarp();
+        }
+        if (!ok)
+            for (int j = max(0, i - kSplitStages); j < i; ++j) in_flight_end(full + 8 * (j % kSplitStages), (j / kSplitStages) & 1);
+    } else if (warp == 1) {
+        const uint32_t idesc = make_idesc(BN);
+        const uint64_t da0 = make_desc_b(smem_u32(sm.ring[0])), db0 = make_desc_b(smem_u32(sm.ring[0]) + kABytes);
+        for (int i = 0; i < n; ++i) {
+            const int s = i % kSplitStages, c = i / kChain, buf = c & 1;
+            if (i % kChain == 0 && c >= 2) ok = mbar_wait_warp(acc_empty + 8 * buf, (c / 2 - 1) & 1, abort_flag, &g_linear_status);
+            if (ok) ok = mbar_wait_warp(full + 8 * s, (i / kSplitStages) & 1, abort_flag, &g_linear_status);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint64_t off = (uint64_t)(s * (kABytes + kSplitTokens * 128) >> 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)                                // K = 16: 32 bytes on
+                    mma_one(tmem + buf * kSplitTokens, da0 + off + 2 * j, db0 + off + 2 * j, idesc, j > 0 || i % kChain > 0);
+                tc_commit_at(empty + 8 * s);
+                if (i % kChain == kChain - 1 || i == n - 1) tc_commit_at(acc_full + 8 * buf);
+            }
+            __syncwarp();
+        }
+        if (!ok) {                                                         // given up: the MMAs in flight end before their operands' memory is used again
+            if (elect_one()) tc_commit_at(smem_u32(&sm.drained));
+            __syncwarp();
+            in_flight_end(smem_u32(&sm.drained), 0);
+        }
+    }
+    float acc[64];
+    const int quarter = warp & 3, half = (warp - 4) >> 2, cw = BN / 2;     // drain warps: half of the columns, on their 32 lanes
+    if (warp >= 4) {
+        const int chains = (n + kChain - 1) / kChain;
+        if (chains == 0)
+#pragma unroll
+            for (int i = 0; i < 64; ++i) acc[i] = 0.f;
+        for (int c = 0; c < chains; ++c) {
+            const int buf = c & 1;
+            ok = mbar_wait_warp(acc_full + 8 * buf, (c >> 1) & 1, abort_flag, &g_linear_status);
+            if (!ok) break;
+            tc_fence_after();
+            drain(tmem + ((uint32_t)(32 * quarter) << 16) + buf * kSplitTokens + half * cw, cw, c == 0, acc);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_at(acc_empty + 8 * buf);
+        }
+    }
+    __syncthreads();                                                       // the ring has been read (or is given up), the accumulators too
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kSplitTokens));
+    if (warp >= 4) {
+#pragma unroll
+        for (int i = 0; i < 64; ++i)
+            if (i < cw) sm.part[half * cw + i][32 * quarter + lane] = acc[i];
+    }
+    if (CL > 1) {
+        cluster_arrive();
+        cluster_wait();
+    } else {
+        __syncthreads();
+    }
+    if (warp >= 4) {
+        // a CTA finishes a CL-th of the tile's tokens; a thread one output of every (256 / kRows)-th of them, four at a time
+        const int u = tid - 128, row = u % kRows, share = (BN + CL - 1) / CL, c_end = min(BN, (rank + 1) * share), nn = n0 + row;
+        constexpr int kStep = 256 / kRows;
+        const float bias = a.bias && nn < a.N ? a.bias[nn] : 0.f, bias_up = GATED && a.bias_up && nn < a.N ? a.bias_up[nn] : 0.f;
+        const uint32_t part = smem_u32(sm.part);
+        for (int c0 = rank * share + u / kRows; c0 < c_end && nn < a.N; c0 += 4 * kStep) {
+            float v[4], up[4], res[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int c = c0 + i * kStep;
+                const long long t = t0 + c;
+                v[i] = up[i] = res[i] = 0.f;
+                if (c < c_end && t < a.T && a.residual) res[i] = load_out<O>(a.residual, t * a.ld_res + nn);
+            }
+            for (int p = 0; p < CL; ++p) {
+                const uint32_t from = at_rank(part, p);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int c = min(c0 + i * kStep, c_end - 1);
+                    float g;
+                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(g) : "r"(from + 4 * (c * BM + row)) : "memory");
+                    v[i] += g;
+                    if (GATED) {
+                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(g) : "r"(from + 4 * (c * BM + BM / 2 + row)) : "memory");
+                        up[i] += g;
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int c = c0 + i * kStep;
+                const long long t = t0 + c;
+                if (c >= c_end || t >= a.T) continue;
+                float y = activate(v[i] + bias, a.act);
+                if (GATED) y *= up[i] + bias_up;
+                store_out(static_cast<O*>(a.out) + t * a.ld_out + nn, y + res[i]);
+            }
+        }
+    }
+    if (CL > 1) {
+        cluster_arrive();                                                  // nobody reads this CTA's shared memory any more
+        cluster_wait();
+    }
+}
+
+template <typename O, bool GATED>
+int launch_split(const LinearArgs& a, int BN, int CL, cudaStream_t st) {
+    constexpr int kRows = GATED ? BM / 2 : BM;
+    alignas(64) CUtensorMap mw, mu, mx;
+    if (encode_map(&mw, a.w, a.N, a.K, a.ld_w, kRows) || encode_map(&mu, GATED ? a.w_up : a.w, a.N, a.K, GATED ? a.ld_up : a.ld_w, kRows) ||
+        encode_map(&mx, a.x, a.T, a.K, a.ld_x, BN))
+        return EXMOE_ERR_CUDA;
+    static SmemOnce once;
+    const auto kern = linear_split_kernel<O, GATED>;
+    constexpr int smem = (int)sizeof(SplitShared) + 1024;
+    static_assert(smem <= 227 * 1024, "shared memory");
+    if (!allow_smem(kern, smem, once)) return EXMOE_ERR_CUDA;
+    const int row_tiles = (a.N + kRows - 1) / kRows;
+    const long long ctas = (long long)row_tiles * ((a.T + BN - 1) / BN) * CL;
+    if (ctas > INT32_MAX) return EXMOE_ERR_SHAPE;
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = dim3((unsigned)ctas);
+    lc.blockDim = dim3(kSplitThreads);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)CL;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 2;
+#ifdef EXMOE_DISABLE_PDL
+    lc.attrs = attr + 1;
+    --lc.numAttrs;
+#endif
+    if (cudaLaunchKernelEx(&lc, kern, mw, mu, mx, a, BN, CL, row_tiles) != cudaSuccess) {
+        cudaGetLastError();
+        return EXMOE_ERR_CUDA;
+    }
+    count_launch();
+    return EXMOE_OK;
+}
+
+template <typename O, bool GATED>
+int launch_tc(const LinearArgs& a, cudaStream_t st) {
+    const int row_tiles = (a.N + (GATED ? 63 : 127)) / (GATED ? 64 : 128), blocks = (a.K + 63) / 64;
+    int BN = 128;
+    if (a.T <= 128) BN = (a.T + 31) / 32 * 32;
+    const long long tiles = (long long)row_tiles * ((a.T + BN - 1) / BN);
+    int CL = 8;
+    while (CL > 1 && (tiles * CL > kSms || blocks < 2 * CL)) CL /= 2;
+    return launch_split<O, GATED>(a, BN, CL, st);
+}
+
+}  // namespace
+
+int launch_linear_tc(const LinearArgs& a, int type, cudaStream_t st) {
+    if (type == EXMOE_F32) return a.w_up ? launch_tc<float, true>(a, st) : launch_tc<float, false>(a, st);
+    return a.w_up ? launch_tc<__nv_bfloat16, true>(a, st) : launch_tc<__nv_bfloat16, false>(a, st);
+}
+
+extern "C" int exmoe_linear_status(void) {
+    int v = 0;
+    const int zero = 0;
+    if (cudaDeviceSynchronize() != cudaSuccess || cudaMemcpyFromSymbol(&v, g_linear_status, sizeof v) != cudaSuccess ||
+        (v && cudaMemcpyToSymbol(g_linear_status, &zero, sizeof zero) != cudaSuccess))
+        return EXMOE_ERR_CUDA;
+    return v;
+}
+
+}  // namespace exmoe

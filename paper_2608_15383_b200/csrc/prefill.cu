@@ -844,7 +844,8 @@ size_t prefill_scratch_bytes(int max_pairs, int num_experts) {
 static_assert(sizeof(CUtensorMap) == 128, "PrefillMaps mirrors CUtensorMap objects");
 
 // 2-D row-major BF16 matrix [rows, cols] -> tensor map with a 64-column x `box_rows`-row box, 128-byte swizzle
-int encode_map(CUtensorMap* out, const void* base, int rows, int cols, int box_rows) {
+int encode_map(CUtensorMap* out, const void* base, int rows, int cols, int box_rows) { return encode_map(out, base, rows, cols, cols, box_rows); }
+int encode_map(CUtensorMap* out, const void* base, int rows, int cols, long long ld, int box_rows) {
     typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -856,7 +857,7 @@ int encode_map(CUtensorMap* out, const void* base, int rows, int cols, int box_r
         fn = reinterpret_cast<EncodeFn>(p);
     }
     const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    const cuuint64_t strides[1] = {(cuuint64_t)cols * 2};
+    const cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
     const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
     const cuuint32_t estr[2] = {1, 1};
     const CUresult rc = fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims, strides, box, estr,

@@ -49,6 +49,7 @@ __device__ __forceinline__ uint64_t make_desc_b(uint32_t saddr) {            // 
     return d;
 }
 int encode_map(CUtensorMap* out, const void* base, int rows, int cols, int box_rows);     // host; EXMOE_OK or EXMOE_ERR_CUDA
+int encode_map(CUtensorMap* out, const void* base, int rows, int cols, long long ld, int box_rows);    // rows `ld` elements apart
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {
     asm volatile(
         "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
