@@ -282,9 +282,288 @@ int launch_split(const LinearArgs& a, int BN, int CL, cudaStream_t st) {
     return EXMOE_OK;
 }
 
+// ---- pairs of CTAs ---------------------------------------------------------------------------------------------------
+// 256 rows (128 in each CTA; 64 of W and 64 of U) by BN tokens (half of their operand in each CTA).  Both CTAs load; the first one's barriers count the bytes of both, its
+// second warp issues the pair's MMAs, whose commits arrive in both.  16 warps of each CTA drain its half of the accumulators and finish the tile
+// while the next one's chains run.
+constexpr int kPairThreads = 32 * 20, kPairTokens = 256, kDrainWarps = 16;
+constexpr int kPairStage = kABytes + kPairTokens / 2 * 128;
+template <bool GATED>
+struct __align__(1024) PairShared {
+    static constexpr int kStages = GATED ? 5 : 6;
+    unsigned char ring[kStages][kPairStage];
+    float meet[GATED ? kDrainWarps : 1][GATED ? 4 : 1][8][32];             // the factors that a warp's partner needs
+    uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2], drained;
+    uint32_t tmem;
+    int abort_flag;
+};
+
+__device__ __forceinline__ void mma_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void commit_pair(uint32_t bar) {                // arrives at this barrier in both CTAs
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((unsigned short)3) : "memory");
+}
+__device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {    // `bar` may be the other CTA's
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void two_warps_sync(int barrier) {
+    __syncwarp();
+    asm volatile("barrier.cta.sync.aligned %0, 64;" ::"r"(barrier) : "memory");
+}
+
+// Finishes eight tokens from t on of output nn: v their sums, bias included; up the second factor.
+template <typename O, bool GATED>
+__device__ __forceinline__ void finish8(const LinearArgs& a, long long t, int nn, float (&v)[8], const float (&up)[8]) {
+    float res[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) res[i] = a.residual && t + i < a.T ? load_out<O>(a.residual, (t + i) * a.ld_res + nn) : 0.f;
+    switch (a.act) {
+        case EXMOE_ACT_RELU:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_RELU);
+            break;
+        case EXMOE_ACT_GELU:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_GELU);
+            break;
+        case EXMOE_ACT_GELU_TANH:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_GELU_TANH);
+            break;
+        case EXMOE_ACT_SILU:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_SILU);
+            break;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (t + i < a.T) store_out(static_cast<O*>(a.out) + (t + i) * a.ld_out + nn, (GATED ? v[i] * up[i] : v[i]) + res[i]);
+}
+
+template <typename O, bool GATED>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
+linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_u, const __grid_constant__ CUtensorMap map_x,
+                   const __grid_constant__ LinearArgs a, int BN, int row_tiles, int tiles) {
+    using S = PairShared<GATED>;
+    extern __shared__ unsigned char raw[];
+    S& sm = *reinterpret_cast<S*>(raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u));
+    constexpr int kRows = GATED ? BM / 2 : BM;                             // outputs of a CTA's half of a tile
+    const int tid = threadIdx.x, lane = tid & 31, warp = warp_uniform(tid >> 5);
+    const int rank = (int)blockIdx.x & 1, pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
+    volatile int* abort_flag = &sm.abort_flag;
+    if (tid == 0) {
+        for (int s = 0; s < S::kStages; ++s) {
+            mbar_init(&sm.full[s], 1);
+            mbar_init(&sm.empty[s], 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(&sm.acc_full[b], 1);
+            mbar_init(&sm.acc_empty[b], 2 * kDrainWarps);
+        }
+        mbar_init(&sm.drained, 1);
+        sm.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem)), "r"(2 * kPairTokens));
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::);
+    }
+    tc_fence_before();
+    cluster_arrive();
+    cluster_wait();
+    tc_fence_after();
+    const uint32_t tmem = sm.tmem;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int blocks = (a.K + 63) / 64, chains = (blocks + kChain - 1) / kChain;
+    const uint32_t full = smem_u32(sm.full), empty = smem_u32(sm.empty), acc_full = smem_u32(sm.acc_full), acc_empty = smem_u32(sm.acc_empty);
+    const uint32_t ring = smem_u32(sm.ring[0]);
+    bool ok = true;
+    if (warp == 0) {
+        const uint32_t first_full = at_rank(full, 0);
+        int s = 0, turn = 0;                                               // stage, turns of the ring
+        for (int tile = pair; tile < tiles && ok; tile += pairs) {
+            const int n0 = (tile % row_tiles * 2 + rank) * kRows, t0 = tile / row_tiles * BN + rank * (BN / 2);
+            for (int i = 0; i < blocks; ++i) {
+                if (turn > 0) ok = mbar_wait_warp(empty + 8 * s, (turn - 1) & 1, abort_flag, &g_linear_status);
+                if (!ok) break;
+                if (elect_one()) {
+                    const uint32_t at = ring + s * kPairStage, bar = first_full + 8 * s;
+                    if (rank == 0) mbar_expect_tx(&sm.full[s], 2 * (uint32_t)(kABytes + BN / 2 * 128));
+                    tma_load_pair(at, &map_w, i * 64, n0, bar);
+                    if (GATED) tma_load_pair(at + kABytes / 2, &map_u, i * 64, n0, bar);
+                    tma_load_pair(at + kABytes, &map_x, i * 64, t0, bar);
+                }
+                __syncwarp();
+                if (++s == S::kStages) {
+                    s = 0;
+                    ++turn;
+                }
+            }
+        }
+        if (!ok && rank == 0)                                              // the copies in flight end (the other CTA's are counted here too)
+            for (int j = 0; j < S::kStages; ++j)
+                if (turn > 0 || j < s) in_flight_end(full + 8 * j, (j < s ? turn : turn - 1) & 1);
+    } else if (warp == 1 && rank == 0) {
+        const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(2 * BM >> 4) << 24);
+        const uint64_t da0 = make_desc_b(ring), db0 = make_desc_b(ring + kABytes);
+        int s = 0, chain = 0;
+        uint32_t turn = 0;
+        for (int tile = pair; tile < tiles && ok; tile += pairs) {
+            for (int i = 0; i < blocks; ++i) {
+                const int buf = chain & 1;
+                if (i % kChain == 0 && chain >= 2) ok = mbar_wait_warp(acc_empty + 8 * buf, (chain / 2 - 1) & 1, abort_flag, &g_linear_status);
+                if (ok) ok = mbar_wait_warp(full + 8 * s, turn, abort_flag, &g_linear_status);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t off = (uint64_t)(s * kPairStage >> 4);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)                            // K = 16: 32 bytes on
+                        mma_pair(tmem + buf * kPairTokens, da0 + off + 2 * j, db0 + off + 2 * j, idesc, j > 0 || i % kChain > 0);
+                    commit_pair(empty + 8 * s);
+                    if (i % kChain == kChain - 1 || i == blocks - 1) commit_pair(acc_full + 8 * buf);
+                }
+                __syncwarp();
+                if (i % kChain == kChain - 1 || i == blocks - 1) ++chain;
+                if (++s == S::kStages) {
+                    s = 0;
+                    turn ^= 1;
+                }
+            }
+        }
+        if (!ok) {                                                         // the MMAs in flight end
+            if (elect_one()) asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(&sm.drained)) : "memory");
+            __syncwarp();
+            in_flight_end(smem_u32(&sm.drained), 0);
+        }
+    } else if (warp >= 4) {
+        const int d = warp - 4, quarter = warp & 3, group = d >> 2, cw = BN / 4;   // a quarter of the columns, on the warp's 32 lanes
+        const bool is_up = GATED && quarter >= 2;
+        const uint32_t my_empty = at_rank(acc_empty, 0);
+        int chain = 0;
+        for (int tile = pair; tile < tiles; tile += pairs) {               // (a warp that has given up stores nothing, but keeps its appointments)
+            float acc[64];
+            for (int c = 0; c < chains && ok; ++c, ++chain) {
+                const int buf = chain & 1;
+                ok = mbar_wait_warp(acc_full + 8 * buf, (chain >> 1) & 1, abort_flag, &g_linear_status);
+                if (!ok) break;
+                tc_fence_after();
+                drain(tmem + ((uint32_t)(32 * quarter) << 16) + buf * kPairTokens + group * cw, cw, c == 0, acc);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) arrive_cluster(my_empty + 8 * buf);
+            }
+            const int nn = (tile % row_tiles * 2 + rank) * kRows + (GATED ? 32 * (quarter & 1) : 32 * quarter) + lane;
+            const long long t0 = (long long)(tile / row_tiles) * BN + group * cw;
+            const bool in = ok && nn < a.N;
+            const float bias = in && (is_up ? a.bias_up : a.bias) ? (is_up ? a.bias_up : a.bias)[nn] : 0.f;
+#pragma unroll
+            for (int i = 0; i < 64; ++i) acc[i] += bias;
+            if constexpr (GATED) {
+                // lanes of W keep the even runs of eight tokens and send their factor of the odd ones, lanes of U the other way round
+                const int partner = d ^ 2, barrier = 1 + (d & 1) + 2 * group;
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    if (8 * c < cw && ((c & 1) != 0) != is_up)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) sm.meet[d][c >> 1][i][lane] = acc[8 * c + i];
+                two_warps_sync(barrier);
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    if (8 * c < cw && ((c & 1) != 0) == is_up) {
+                        float mine[8], other[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float o = sm.meet[partner][c >> 1][i][lane];
+                            mine[i] = is_up ? o : acc[8 * c + i];
+                            other[i] = is_up ? acc[8 * c + i] : o;
+                        }
+                        if (in) finish8<O, true>(a, t0 + 8 * c, nn, mine, other);
+                    }
+                two_warps_sync(barrier);
+            } else if (in) {
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    if (8 * c < cw) {
+                        float v[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] = acc[8 * c + i];
+                        finish8<O, false>(a, t0 + 8 * c, nn, v, v);
+                    }
+            }
+        }
+    }
+    tc_fence_before();
+    cluster_arrive();                                                      // neither CTA's memory nor barriers are in use any more
+    cluster_wait();
+    tc_fence_after();
+    if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kPairTokens));
+}
+
+template <typename O, bool GATED>
+int launch_pair(const LinearArgs& a, int BN, cudaStream_t st) {
+    using S = PairShared<GATED>;
+    constexpr int kRows = GATED ? BM / 2 : BM;
+    alignas(64) CUtensorMap mw, mu, mx;
+    if (encode_map(&mw, a.w, a.N, a.K, a.ld_w, kRows) || encode_map(&mu, GATED ? a.w_up : a.w, a.N, a.K, GATED ? a.ld_up : a.ld_w, kRows) ||
+        encode_map(&mx, a.x, a.T, a.K, a.ld_x, BN / 2))
+        return EXMOE_ERR_CUDA;
+    static SmemOnce once;
+    const auto kern = linear_pair_kernel<O, GATED>;
+    constexpr int smem = (int)sizeof(S) + 1024;
+    static_assert(smem <= 227 * 1024, "shared memory");
+    if (!allow_smem(kern, smem, once)) return EXMOE_ERR_CUDA;
+    const int row_tiles = (a.N + 2 * kRows - 1) / (2 * kRows);
+    const long long tiles = (long long)row_tiles * ((a.T + BN - 1) / BN);
+    if (tiles > INT32_MAX) return EXMOE_ERR_SHAPE;
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = dim3(2 * (unsigned)std::min<long long>(tiles, kSms / 2));
+    lc.blockDim = dim3(kPairThreads);
+    lc.dynamicSmemBytes = smem;
+    lc.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = attr;
+    lc.numAttrs = 1;
+#ifdef EXMOE_DISABLE_PDL
+    lc.numAttrs = 0;
+#endif
+    if (cudaLaunchKernelEx(&lc, kern, mw, mu, mx, a, BN, row_tiles, (int)tiles) != cudaSuccess) {
+        cudaGetLastError();
+        return EXMOE_ERR_CUDA;
+    }
+    count_launch();
+    return EXMOE_OK;
+}
+
 template <typename O, bool GATED>
 int launch_tc(const LinearArgs& a, cudaStream_t st) {
     const int row_tiles = (a.N + (GATED ? 63 : 127)) / (GATED ? 64 : 128), blocks = (a.K + 63) / 64;
+    const long long pair_rows = (row_tiles + 1) / 2;
+    if (pair_rows * ((a.T + 255) / 256) >= kSms / 4) {
+        int best = 256;
+        long long least = INT64_MAX;
+        for (int BN = 256; BN >= 96; BN -= 32) {
+            const long long rounds = (pair_rows * ((a.T + BN - 1) / BN) + kSms / 2 - 1) / (kSms / 2), cost = rounds * (blocks * (long long)(256 + BN) + 1500);
+            if (cost < least) {
+                least = cost;
+                best = BN;
+            }
+        }
+        return launch_pair<O, GATED>(a, best, st);
+    }
     int BN = 128;
     if (a.T <= 128) BN = (a.T + 31) / 32 * 32;
     const long long tiles = (long long)row_tiles * ((a.T + BN - 1) / BN);

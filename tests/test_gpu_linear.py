@@ -85,7 +85,18 @@ def test_products_match_oracle(B, T, K, N, dtype, gated):
         check(out, i, act, some_rows(T))
 
 
-@pytest.mark.parametrize("T", [1, 12, 40, 200, 600])
+@pytest.mark.parametrize("T,K,N", [(4097, 72, 700), (9000, 64, 300), (2600, 576, 1290), (1100, 1096, 4000), (3300, 512, 2049), (20000, 8, 257), (5000, 2048, 1000)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("gated", [False, True])
+def test_many_tokens(B, T, K, N, dtype, gated):
+    """Calls that fill the chip with tiles of 256 x 256, partly empty ones at both edges."""
+    for act, bias in (("silu", True), ("none", False)):
+        i = inputs(T, K, N, T + N, gated, bias, bias, dtype)
+        check(B.exmoe_linear(**i, activation=act, out_dtype=dtype), i, act, some_rows(T))
+    assert B.exmoe_linear_status() == B.EXMOE_OK
+
+
+@pytest.mark.parametrize("T", [1, 12, 40, 200, 600, 12000])
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("gated", [False, True])
 def test_every_activation(B, T, act, gated):
