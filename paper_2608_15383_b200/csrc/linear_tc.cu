@@ -321,34 +321,45 @@ __device__ __forceinline__ void two_warps_sync(int barrier) {
     asm volatile("barrier.cta.sync.aligned %0, 64;" ::"r"(barrier) : "memory");
 }
 
-// Finishes eight tokens from t on of output nn: v their sums, bias included; up the second factor.
-template <typename O, bool GATED>
-__device__ __forceinline__ void finish8(const LinearArgs& a, long long t, int nn, float (&v)[8], const float (&up)[8]) {
-    float res[8];
+// What a lane finishes: its output of a run of tokens, eight at a time.
+template <typename O>
+struct Lane {
+    const O* res;                                                          // of the first token; null without one
+    O* out;
+    long long ld_res, ld_out;
+    int left, act;                                                         // tokens of the run that exist (none: nothing is read or written)
+    // residuals of the eight tokens from `c` on
+    __device__ __forceinline__ void load(int c, O (&r)[8]) const {
+        const O* p = res + c * ld_res;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) res[i] = a.residual && t + i < a.T ? load_out<O>(a.residual, (t + i) * a.ld_res + nn) : 0.f;
-    switch (a.act) {
-        case EXMOE_ACT_RELU:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_RELU);
-            break;
-        case EXMOE_ACT_GELU:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_GELU);
-            break;
-        case EXMOE_ACT_GELU_TANH:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_GELU_TANH);
-            break;
-        case EXMOE_ACT_SILU:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_SILU);
-            break;
+        for (int i = 0; i < 8; ++i, p += ld_res) r[i] = res && c + i < left ? *p : O(0.f);
     }
+    template <bool GATED>
+    __device__ __forceinline__ void store(int c, float (&v)[8], const float (&up)[8], const O (&r)[8]) const {
+        switch (act) {
+            case EXMOE_ACT_RELU:
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (t + i < a.T) store_out(static_cast<O*>(a.out) + (t + i) * a.ld_out + nn, (GATED ? v[i] * up[i] : v[i]) + res[i]);
-}
+                for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_RELU);
+                break;
+            case EXMOE_ACT_GELU:
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_GELU);
+                break;
+            case EXMOE_ACT_GELU_TANH:
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_GELU_TANH);
+                break;
+            case EXMOE_ACT_SILU:
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_SILU);
+                break;
+        }
+        O* p = out + c * ld_out;
+#pragma unroll
+        for (int i = 0; i < 8; ++i, p += ld_out)
+            if (c + i < left) store_out(p, (GATED ? v[i] * up[i] : v[i]) + (float)r[i]);
+    }
+};
 
 template <typename O, bool GATED>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
@@ -385,7 +396,10 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     const uint32_t tmem = sm.tmem;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int blocks = (a.K + 63) / 64, chains = (blocks + kChain - 1) / kChain;
+    // In front of a BF16 result the whole K is one chain, which stays in tensor memory until it is finished: what truncation takes (K / 16 MMAs,
+    // 2^-8 of a BF16 step each at most) does not show.
+    constexpr bool kChained = sizeof(O) == 4;
+    const int blocks = (a.K + 63) / 64, per_chain = kChained ? kChain : blocks, chains = (blocks + per_chain - 1) / per_chain;
     const uint32_t full = smem_u32(sm.full), empty = smem_u32(sm.empty), acc_full = smem_u32(sm.acc_full), acc_empty = smem_u32(sm.acc_empty);
     const uint32_t ring = smem_u32(sm.ring[0]);
     bool ok = true;
@@ -417,25 +431,27 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     } else if (warp == 1 && rank == 0) {
         const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(BN >> 3) << 17) | ((uint32_t)(2 * BM >> 4) << 24);
         const uint64_t da0 = make_desc_b(ring), db0 = make_desc_b(ring + kABytes);
-        int s = 0, chain = 0;
+        int s = 0, chain = 0, in_chain = 0;
         uint32_t turn = 0;
         for (int tile = pair; tile < tiles && ok; tile += pairs) {
             for (int i = 0; i < blocks; ++i) {
                 const int buf = chain & 1;
-                if (i % kChain == 0 && chain >= 2) ok = mbar_wait_warp(acc_empty + 8 * buf, (chain / 2 - 1) & 1, abort_flag, &g_linear_status);
+                if (in_chain == 0 && chain >= 2) ok = mbar_wait_warp(acc_empty + 8 * buf, (chain / 2 - 1) & 1, abort_flag, &g_linear_status);
                 if (ok) ok = mbar_wait_warp(full + 8 * s, turn, abort_flag, &g_linear_status);
                 if (!ok) break;
                 tc_fence_after();
+                const bool ends = in_chain == per_chain - 1 || i == blocks - 1;
                 if (elect_one()) {
                     const uint64_t off = (uint64_t)(s * kPairStage >> 4);
 #pragma unroll
                     for (int j = 0; j < 4; ++j)                            // K = 16: 32 bytes on
-                        mma_pair(tmem + buf * kPairTokens, da0 + off + 2 * j, db0 + off + 2 * j, idesc, j > 0 || i % kChain > 0);
+                        mma_pair(tmem + buf * kPairTokens, da0 + off + 2 * j, db0 + off + 2 * j, idesc, j > 0 || in_chain > 0);
                     commit_pair(empty + 8 * s);
-                    if (i % kChain == kChain - 1 || i == blocks - 1) commit_pair(acc_full + 8 * buf);
+                    if (ends) commit_pair(acc_full + 8 * buf);
                 }
                 __syncwarp();
-                if (i % kChain == kChain - 1 || i == blocks - 1) ++chain;
+                in_chain = ends ? 0 : in_chain + 1;
+                chain += ends;
                 if (++s == S::kStages) {
                     s = 0;
                     turn ^= 1;
@@ -451,57 +467,92 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
         const int d = warp - 4, quarter = warp & 3, group = d >> 2, cw = BN / 4;   // a quarter of the columns, on the warp's 32 lanes
         const bool is_up = GATED && quarter >= 2;
         const uint32_t my_empty = at_rank(acc_empty, 0);
+        const uint32_t lanes = tmem + ((uint32_t)(32 * quarter) << 16) + group * cw;
         int chain = 0;
         for (int tile = pair; tile < tiles; tile += pairs) {               // (a warp that has given up stores nothing, but keeps its appointments)
-            float acc[64];
+            const int nn = (tile % row_tiles * 2 + rank) * kRows + (GATED ? 32 * (quarter & 1) : 32 * quarter) + lane;
+            const long long t0 = (long long)(tile / row_tiles) * BN + group * cw;
+            const bool in = nn < a.N;
+            const float bias = in && (is_up ? a.bias_up : a.bias) ? (is_up ? a.bias_up : a.bias)[nn] : 0.f;
+            Lane<O> to{a.residual ? static_cast<const O*>(a.residual) + t0 * a.ld_res + nn : nullptr, static_cast<O*>(a.out) + t0 * a.ld_out + nn,
+                       a.ld_res, a.ld_out, in ? (int)max(0ll, min((long long)cw, a.T - t0)) : 0, a.act};
+            // The runs of eight tokens that this warp finishes: with a second factor lanes of W the even ones, lanes of U the odd ones.
+            // Residuals are on their way two runs ahead (one where the sums take the registers), the first ones before the tile's sums are there.
+            constexpr int kRuns = GATED ? 4 : 8, kAhead = kChained ? 1 : 2, kStep = GATED ? 2 : 1;
+            const int c_first = GATED && is_up ? 8 : 0;
+            O res[kAhead + 1][8];
+#pragma unroll
+            for (int r = 0; r < kAhead; ++r) to.load(c_first + 8 * kStep * r, res[r]);
+            float acc[kChained ? 64 : 1];
+            int buf = chain & 1;
             for (int c = 0; c < chains && ok; ++c, ++chain) {
-                const int buf = chain & 1;
+                buf = chain & 1;
                 ok = mbar_wait_warp(acc_full + 8 * buf, (chain >> 1) & 1, abort_flag, &g_linear_status);
                 if (!ok) break;
                 tc_fence_after();
-                drain(tmem + ((uint32_t)(32 * quarter) << 16) + buf * kPairTokens + group * cw, cw, c == 0, acc);
+                if constexpr (kChained) {
+                    drain(lanes + buf * kPairTokens, cw, c == 0, acc);
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) arrive_cluster(my_empty + 8 * buf);
+                }
+            }
+            if (!ok) to.left = 0;
+            const auto sums = [&](int c, float (&v)[8]) {                  // eight columns from c on, bias included
+                if constexpr (kChained) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = acc[c + i] + bias;
+                } else {
+                    uint32_t r[8];
+                    tmem_ld8(lanes + buf * kPairTokens + c, r);
+                    tc_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]) + bias;
+                }
+            };
+            const int partner = d ^ 2, barrier = 1 + (d & 1) + 2 * group;
+            if constexpr (GATED) {
+#pragma unroll
+                for (int c = 0; c < 64; c += 8)
+                    if (c < cw && ((c & 8) != 0) != is_up) {
+                        float v[8];
+                        sums(c, v);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) sm.meet[d][c >> 4][i][lane] = v[i];
+                    }
+                two_warps_sync(barrier);
+            }
+#pragma unroll
+            for (int r = 0; r < kRuns; ++r) {
+                const int c = c_first + 8 * kStep * r;
+                if (c < cw) {
+                    if (r + kAhead < kRuns) to.load(c + 8 * kStep * kAhead, res[(r + kAhead) % (kAhead + 1)]);
+                    float v[8], other[8];
+                    if constexpr (GATED) {
+                        if constexpr (kChained) {                          // (indices known to the compiler)
+                            if (is_up) sums(16 * r + 8, v);
+                            else sums(16 * r, v);
+                        } else {
+                            sums(c, v);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float o = sm.meet[partner][r][i][lane];
+                            other[i] = is_up ? v[i] : o;
+                            v[i] = is_up ? o : v[i];
+                        }
+                    } else {
+                        sums(8 * r, v);
+                    }
+                    to.template store<GATED>(c, v, other, res[r % (kAhead + 1)]);
+                }
+            }
+            if constexpr (!kChained) {
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) arrive_cluster(my_empty + 8 * buf);
             }
-            const int nn = (tile % row_tiles * 2 + rank) * kRows + (GATED ? 32 * (quarter & 1) : 32 * quarter) + lane;
-            const long long t0 = (long long)(tile / row_tiles) * BN + group * cw;
-            const bool in = ok && nn < a.N;
-            const float bias = in && (is_up ? a.bias_up : a.bias) ? (is_up ? a.bias_up : a.bias)[nn] : 0.f;
-#pragma unroll
-            for (int i = 0; i < 64; ++i) acc[i] += bias;
-            if constexpr (GATED) {
-                // lanes of W keep the even runs of eight tokens and send their factor of the odd ones, lanes of U the other way round
-                const int partner = d ^ 2, barrier = 1 + (d & 1) + 2 * group;
-#pragma unroll
-                for (int c = 0; c < 8; ++c)
-                    if (8 * c < cw && ((c & 1) != 0) != is_up)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) sm.meet[d][c >> 1][i][lane] = acc[8 * c + i];
-                two_warps_sync(barrier);
-#pragma unroll
-                for (int c = 0; c < 8; ++c)
-                    if (8 * c < cw && ((c & 1) != 0) == is_up) {
-                        float mine[8], other[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float o = sm.meet[partner][c >> 1][i][lane];
-                            mine[i] = is_up ? o : acc[8 * c + i];
-                            other[i] = is_up ? acc[8 * c + i] : o;
-                        }
-                        if (in) finish8<O, true>(a, t0 + 8 * c, nn, mine, other);
-                    }
-                two_warps_sync(barrier);
-            } else if (in) {
-#pragma unroll
-                for (int c = 0; c < 8; ++c)
-                    if (8 * c < cw) {
-                        float v[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) v[i] = acc[8 * c + i];
-                        finish8<O, false>(a, t0 + 8 * c, nn, v, v);
-                    }
-            }
+            if constexpr (GATED) two_warps_sync(barrier);
         }
     }
     tc_fence_before();
