@@ -321,45 +321,66 @@ __device__ __forceinline__ void two_warps_sync(int barrier) {
     asm volatile("barrier.cta.sync.aligned %0, 64;" ::"r"(barrier) : "memory");
 }
 
-// What a lane finishes: its output of a run of tokens, eight at a time.
+// Eight tokens of a warp's 32 outputs: read, finished, written.  Addresses are a base that all lanes share and 32 bits of a lane's own: steps from token
+// to token are then uniform instructions, and a call without residuals or with whole runs has none of their predicates (21 instructions per element
+// otherwise, and a product of K = 512 takes twice as long as its MMAs).
 template <typename O>
-struct Lane {
-    const O* res;                                                          // of the first token; null without one
-    O* out;
-    long long ld_res, ld_out;
-    int left, act;                                                         // tokens of the run that exist (none: nothing is read or written)
-    // residuals of the eight tokens from `c` on
+struct Outputs {
+    const char* res;                                                       // of the first token's first output; null without one
+    char* out;
+    long long res_step, out_step;                                          // bytes from token to token
+    int left, act;                                                         // tokens that exist
+    uint32_t lane_at;                                                      // bytes
+    bool in;                                                               // this lane's output exists
     __device__ __forceinline__ void load(int c, O (&r)[8]) const {
-        const O* p = res + c * ld_res;
+        if (!res || !in) return;
+        const char* p = res + c * res_step;
+        if (c + 8 <= left) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i, p += ld_res) r[i] = res && c + i < left ? *p : O(0.f);
-    }
-    template <bool GATED>
-    __device__ __forceinline__ void store(int c, float (&v)[8], const float (&up)[8], const O (&r)[8]) const {
-        switch (act) {
-            case EXMOE_ACT_RELU:
+            for (int i = 0; i < 8; ++i, p += res_step) r[i] = *reinterpret_cast<const O*>(p + lane_at);
+        } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_RELU);
-                break;
-            case EXMOE_ACT_GELU:
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_GELU);
-                break;
-            case EXMOE_ACT_GELU_TANH:
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_GELU_TANH);
-                break;
-            case EXMOE_ACT_SILU:
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_SILU);
-                break;
+            for (int i = 0; i < 8; ++i, p += res_step)
+                if (c + i < left) r[i] = *reinterpret_cast<const O*>(p + lane_at);
         }
-        O* p = out + c * ld_out;
+    }
+    __device__ __forceinline__ void store(int c, float (&v)[8], const O (&r)[8]) const {
+        if (!in) return;
+        if (res) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i, p += ld_out)
-            if (c + i < left) store_out(p, (GATED ? v[i] * up[i] : v[i]) + (float)r[i]);
+            for (int i = 0; i < 8; ++i) v[i] += (float)r[i];
+        }
+        char* p = out + c * out_step;
+        if (c + 8 <= left) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i, p += out_step) store_out(reinterpret_cast<O*>(p + lane_at), v[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i, p += out_step)
+                if (c + i < left) store_out(reinterpret_cast<O*>(p + lane_at), v[i]);
+        }
     }
 };
+__device__ __forceinline__ void activate8(float (&v)[8], int act) {
+    switch (act) {
+        case EXMOE_ACT_RELU:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_RELU);
+            break;
+        case EXMOE_ACT_GELU:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_GELU);
+            break;
+        case EXMOE_ACT_GELU_TANH:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_GELU_TANH);
+            break;
+        case EXMOE_ACT_SILU:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_SILU);
+            break;
+    }
+}
 
 template <typename O, bool GATED>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
@@ -470,15 +491,16 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
         const uint32_t lanes = tmem + ((uint32_t)(32 * quarter) << 16) + group * cw;
         int chain = 0;
         for (int tile = pair; tile < tiles; tile += pairs) {               // (a warp that has given up stores nothing, but keeps its appointments)
-            const int nn = (tile % row_tiles * 2 + rank) * kRows + (GATED ? 32 * (quarter & 1) : 32 * quarter) + lane;
+            const int n0 = (tile % row_tiles * 2 + rank) * kRows + 32 * (GATED ? quarter & 1 : quarter), nn = n0 + lane;
             const long long t0 = (long long)(tile / row_tiles) * BN + group * cw;
-            const bool in = nn < a.N;
-            const float bias = in && (is_up ? a.bias_up : a.bias) ? (is_up ? a.bias_up : a.bias)[nn] : 0.f;
-            Lane<O> to{a.residual ? static_cast<const O*>(a.residual) + t0 * a.ld_res + nn : nullptr, static_cast<O*>(a.out) + t0 * a.ld_out + nn,
-                       a.ld_res, a.ld_out, in ? (int)max(0ll, min((long long)cw, a.T - t0)) : 0, a.act};
+            const float* b = is_up ? a.bias_up : a.bias;
+            const float bias = b && nn < a.N ? b[nn] : 0.f;
+            Outputs<O> to{a.residual ? static_cast<const char*>(a.residual) + (t0 * a.ld_res + n0) * (int)sizeof(O) : nullptr,
+                          static_cast<char*>(a.out) + (t0 * a.ld_out + n0) * (int)sizeof(O), a.ld_res * (int)sizeof(O), a.ld_out * (int)sizeof(O),
+                          (int)max(0ll, min((long long)cw, a.T - t0)), a.act, lane * (uint32_t)sizeof(O), nn < a.N};
             // The runs of eight tokens that this warp finishes: with a second factor lanes of W the even ones, lanes of U the odd ones.
             // Residuals are on their way two runs ahead (one where the sums take the registers), the first ones before the tile's sums are there.
-            constexpr int kRuns = GATED ? 4 : 8, kAhead = kChained ? 1 : 2, kStep = GATED ? 2 : 1;
+            constexpr int kRuns = GATED ? 4 : 8, kAhead = kChained ? 0 : 2, kStep = GATED ? 2 : 1;
             const int c_first = GATED && is_up ? 8 : 0;
             O res[kAhead + 1][8];
 #pragma unroll
@@ -497,7 +519,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
                     if (lane == 0) arrive_cluster(my_empty + 8 * buf);
                 }
             }
-            if (!ok) to.left = 0;
+            if (!ok) to.in = false;
             const auto sums = [&](int c, float (&v)[8]) {                  // eight columns from c on, bias included
                 if constexpr (kChained) {
 #pragma unroll
@@ -527,8 +549,9 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
                 const int c = c_first + 8 * kStep * r;
                 if (c < cw) {
                     if (r + kAhead < kRuns) to.load(c + 8 * kStep * kAhead, res[(r + kAhead) % (kAhead + 1)]);
-                    float v[8], other[8];
+                    float v[8];
                     if constexpr (GATED) {
+                        float other[8];
                         if constexpr (kChained) {                          // (indices known to the compiler)
                             if (is_up) sums(16 * r + 8, v);
                             else sums(16 * r, v);
@@ -541,10 +564,14 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
                             other[i] = is_up ? v[i] : o;
                             v[i] = is_up ? o : v[i];
                         }
+                        activate8(v, a.act);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] *= other[i];
                     } else {
                         sums(8 * r, v);
+                        activate8(v, a.act);
                     }
-                    to.template store<GATED>(c, v, other, res[r % (kAhead + 1)]);
+                    to.store(c, v, res[r % (kAhead + 1)]);
                 }
             }
             if constexpr (!kChained) {
