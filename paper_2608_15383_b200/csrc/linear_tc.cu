@@ -30,6 +30,12 @@ __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8]) {
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
                  : "r"(taddr));
 }
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const float* v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"
+                 ::"r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])), "r"(__float_as_uint(v[4])),
+                 "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7])), "r"(taddr)
+                 : "memory");
+}
 __device__ __forceinline__ void cluster_arrive() {
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -314,7 +320,7 @@ __device__ __forceinline__ void tma_load_pair(uint32_t dst, const CUtensorMap* m
                  ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");     // (released to the cluster it would wait for the stores before it)
 }
 __device__ __forceinline__ void two_warps_sync(int barrier) {
     __syncwarp();
@@ -382,16 +388,25 @@ __device__ __forceinline__ void activate8(float (&v)[8], int act) {
     }
 }
 
+// The pairs work side by side on tiles of kGroup rows of tiles and as many columns as it takes: what they read at a time is then few weights and few
+// tokens (8192 x 8192 -> 8192 outputs: TODO us instead of 805 along whole columns).
+constexpr int kGroup = 8;
+struct TileAt { int row, token; };
+__device__ __forceinline__ TileAt tile_at(int tile, int row_tiles, int token_tiles) {
+    const int group = tile / (kGroup * token_tiles), in_group = tile - group * kGroup * token_tiles, rows = min(kGroup, row_tiles - group * kGroup);
+    return {group * kGroup + in_group % rows, in_group / rows};
+}
+
 template <typename O, bool GATED>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_u, const __grid_constant__ CUtensorMap map_x,
-                   const __grid_constant__ LinearArgs a, int BN, int row_tiles, int tiles) {
+                   const __grid_constant__ LinearArgs a, int BN, int row_tiles, int token_tiles) {
     using S = PairShared<GATED>;
     extern __shared__ unsigned char raw[];
     S& sm = *reinterpret_cast<S*>(raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u));
     constexpr int kRows = GATED ? BM / 2 : BM;                             // outputs of a CTA's half of a tile
     const int tid = threadIdx.x, lane = tid & 31, warp = warp_uniform(tid >> 5);
-    const int rank = (int)blockIdx.x & 1, pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1;
+    const int rank = (int)blockIdx.x & 1, pair = (int)blockIdx.x >> 1, pairs = (int)gridDim.x >> 1, tiles = row_tiles * token_tiles;
     volatile int* abort_flag = &sm.abort_flag;
     if (tid == 0) {
         for (int s = 0; s < S::kStages; ++s) {
@@ -428,7 +443,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
         const uint32_t first_full = at_rank(full, 0);
         int s = 0, turn = 0;                                               // stage, turns of the ring
         for (int tile = pair; tile < tiles && ok; tile += pairs) {
-            const int n0 = (tile % row_tiles * 2 + rank) * kRows, t0 = tile / row_tiles * BN + rank * (BN / 2);
+            const TileAt at_tile = tile_at(tile, row_tiles, token_tiles);
+            const int n0 = (at_tile.row * 2 + rank) * kRows, t0 = at_tile.token * BN + rank * (BN / 2);
             for (int i = 0; i < blocks; ++i) {
                 if (turn > 0) ok = mbar_wait_warp(empty + 8 * s, (turn - 1) & 1, abort_flag, &g_linear_status);
                 if (!ok) break;
@@ -484,6 +500,23 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
             __syncwarp();
             in_flight_end(smem_u32(&sm.drained), 0);
         }
+    } else if (warp == 3 && a.residual) {
+        // the residuals of a tile come into L2 while its MMAs run
+        int chain = 0;
+        for (int tile = pair; tile < tiles && ok; tile += pairs) {
+            const TileAt at_tile = tile_at(tile, row_tiles, token_tiles);
+            const int n0 = (at_tile.row * 2 + rank) * kRows, n1 = min(n0 + kRows, a.N) - 1;
+            const long long t0 = (long long)at_tile.token * BN, t1 = min(t0 + BN, (long long)a.T);
+            for (long long t = t0 + lane; t < t1 && n0 <= n1; t += 32) {
+                const O* row = static_cast<const O*>(a.residual) + t * a.ld_res;
+#pragma unroll
+                for (int i = 0; i <= kRows * (int)sizeof(O) / 128; ++i)
+                    asm volatile("prefetch.global.L2 [%0];" ::"l"(row + min(n0 + i * (128 / (int)sizeof(O)), n1)));
+            }
+            // no further ahead than the drain warps and one tile
+            if (tile != pair)
+                for (int c = 0; c < chains && ok; ++c, ++chain) ok = mbar_wait_warp(acc_full + 8 * (chain & 1), (chain >> 1) & 1, abort_flag, &g_linear_status);
+        }
     } else if (warp >= 4) {
         const int d = warp - 4, quarter = warp & 3, group = d >> 2, cw = BN / 4;   // a quarter of the columns, on the warp's 32 lanes
         const bool is_up = GATED && quarter >= 2;
@@ -491,94 +524,95 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
         const uint32_t lanes = tmem + ((uint32_t)(32 * quarter) << 16) + group * cw;
         int chain = 0;
         for (int tile = pair; tile < tiles; tile += pairs) {               // (a warp that has given up stores nothing, but keeps its appointments)
-            const int n0 = (tile % row_tiles * 2 + rank) * kRows + 32 * (GATED ? quarter & 1 : quarter), nn = n0 + lane;
-            const long long t0 = (long long)(tile / row_tiles) * BN + group * cw;
+            const TileAt at_tile = tile_at(tile, row_tiles, token_tiles);
+            const int n0 = (at_tile.row * 2 + rank) * kRows + 32 * (GATED ? quarter & 1 : quarter), nn = n0 + lane;
+            const long long t0 = (long long)at_tile.token * BN + group * cw;
             const float* b = is_up ? a.bias_up : a.bias;
             const float bias = b && nn < a.N ? b[nn] : 0.f;
             Outputs<O> to{a.residual ? static_cast<const char*>(a.residual) + (t0 * a.ld_res + n0) * (int)sizeof(O) : nullptr,
                           static_cast<char*>(a.out) + (t0 * a.ld_out + n0) * (int)sizeof(O), a.ld_res * (int)sizeof(O), a.ld_out * (int)sizeof(O),
                           (int)max(0ll, min((long long)cw, a.T - t0)), a.act, lane * (uint32_t)sizeof(O), nn < a.N};
-            // The runs of eight tokens that this warp finishes: with a second factor lanes of W the even ones, lanes of U the odd ones.
-            // Residuals are on their way two runs ahead (one where the sums take the registers), the first ones before the tile's sums are there.
-            constexpr int kRuns = GATED ? 4 : 8, kAhead = kChained ? 0 : 2, kStep = GATED ? 2 : 1;
+            // The runs of eight tokens that this warp finishes: with a second factor lanes of W the even ones, lanes of U the odd ones.  Residuals are
+            // requested two of them ahead, the first ones before the tile's sums are there.
+            constexpr int kStep = GATED ? 16 : 8;
             const int c_first = GATED && is_up ? 8 : 0;
-            O res[kAhead + 1][8];
-#pragma unroll
-            for (int r = 0; r < kAhead; ++r) to.load(c_first + 8 * kStep * r, res[r]);
-            float acc[kChained ? 64 : 1];
+            O res[2][8];
+            if (c_first < cw) to.load(c_first, res[0]);
+            if (c_first + kStep < cw) to.load(c_first + kStep, res[1]);
             int buf = chain & 1;
-            for (int c = 0; c < chains && ok; ++c, ++chain) {
-                buf = chain & 1;
-                ok = mbar_wait_warp(acc_full + 8 * buf, (chain >> 1) & 1, abort_flag, &g_linear_status);
-                if (!ok) break;
-                tc_fence_after();
-                if constexpr (kChained) {
+            if (kChained && chains > 1) {
+                // the chains' sums go back to where the last one was
+                float acc[64];
+                for (int c = 0; c < chains && ok; ++c, ++chain) {
+                    buf = chain & 1;
+                    ok = mbar_wait_warp(acc_full + 8 * buf, (chain >> 1) & 1, abort_flag, &g_linear_status);
+                    if (!ok) break;
+                    tc_fence_after();
                     drain(lanes + buf * kPairTokens, cw, c == 0, acc);
+                    if (c == chains - 1) break;
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) arrive_cluster(my_empty + 8 * buf);
                 }
+                if (ok) {
+#pragma unroll
+                    for (int c = 0; c < 64; c += 8)
+                        if (c < cw) tmem_st8(lanes + buf * kPairTokens + c, acc + c);
+                    asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                }
+                ++chain;
+            } else {
+                if (ok) ok = mbar_wait_warp(acc_full + 8 * buf, (chain >> 1) & 1, abort_flag, &g_linear_status);
+                tc_fence_after();
+                ++chain;
             }
             if (!ok) to.in = false;
             const auto sums = [&](int c, float (&v)[8]) {                  // eight columns from c on, bias included
-                if constexpr (kChained) {
+                uint32_t r[8];
+                tmem_ld8(lanes + buf * kPairTokens + c, r);
+                tc_wait_ld();
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = acc[c + i] + bias;
-                } else {
-                    uint32_t r[8];
-                    tmem_ld8(lanes + buf * kPairTokens + c, r);
-                    tc_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]) + bias;
-                }
+                for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]) + bias;
             };
             const int partner = d ^ 2, barrier = 1 + (d & 1) + 2 * group;
             if constexpr (GATED) {
+#pragma unroll 1
+                for (int c = 8 - c_first; c < cw; c += 16) {
+                    float v[8];
+                    sums(c, v);
 #pragma unroll
-                for (int c = 0; c < 64; c += 8)
-                    if (c < cw && ((c & 8) != 0) != is_up) {
-                        float v[8];
-                        sums(c, v);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) sm.meet[d][c >> 4][i][lane] = v[i];
-                    }
+                    for (int i = 0; i < 8; ++i) sm.meet[d][c >> 4][i][lane] = v[i];
+                }
                 two_warps_sync(barrier);
             }
+            const auto finish = [&](int c, O (&r)[8]) {
+                float v[8];
+                sums(c, v);
+                if constexpr (GATED) {
+                    float other[8];
 #pragma unroll
-            for (int r = 0; r < kRuns; ++r) {
-                const int c = c_first + 8 * kStep * r;
-                if (c < cw) {
-                    if (r + kAhead < kRuns) to.load(c + 8 * kStep * kAhead, res[(r + kAhead) % (kAhead + 1)]);
-                    float v[8];
-                    if constexpr (GATED) {
-                        float other[8];
-                        if constexpr (kChained) {                          // (indices known to the compiler)
-                            if (is_up) sums(16 * r + 8, v);
-                            else sums(16 * r, v);
-                        } else {
-                            sums(c, v);
-                        }
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float o = sm.meet[partner][r][i][lane];
-                            other[i] = is_up ? v[i] : o;
-                            v[i] = is_up ? o : v[i];
-                        }
-                        activate8(v, a.act);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) v[i] *= other[i];
-                    } else {
-                        sums(8 * r, v);
-                        activate8(v, a.act);
+                    for (int i = 0; i < 8; ++i) {
+                        const float o = sm.meet[partner][c >> 4][i][lane];
+                        other[i] = is_up ? v[i] : o;
+                        v[i] = is_up ? o : v[i];
                     }
-                    to.store(c, v, res[r % (kAhead + 1)]);
+                    activate8(v, a.act);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] *= other[i];
+                } else {
+                    activate8(v, a.act);
                 }
+                to.store(c, v, r);
+                if (c + 2 * kStep < cw) to.load(c + 2 * kStep, r);
+            };
+#pragma unroll 1
+            for (int c = c_first; c < cw; c += 2 * kStep) {
+                finish(c, res[0]);
+                if (c + kStep < cw) finish(c + kStep, res[1]);
             }
-            if constexpr (!kChained) {
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) arrive_cluster(my_empty + 8 * buf);
-            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) arrive_cluster(my_empty + 8 * buf);
             if constexpr (GATED) two_warps_sync(barrier);
         }
     }
@@ -618,7 +652,7 @@ int launch_pair(const LinearArgs& a, int BN, cudaStream_t st) {
 #ifdef EXMOE_DISABLE_PDL
     lc.numAttrs = 0;
 #endif
-    if (cudaLaunchKernelEx(&lc, kern, mw, mu, mx, a, BN, row_tiles, (int)tiles) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&lc, kern, mw, mu, mx, a, BN, row_tiles, (a.T + BN - 1) / BN) != cudaSuccess) {
         cudaGetLastError();
         return EXMOE_ERR_CUDA;
     }
