@@ -14,19 +14,24 @@ constexpr int kMaxTokens = 1 << 29, kMaxDim = 1 << 30;
 // Few tokens.  A CTA takes 16 rows of W (8 of W and 8 of U: the two factors meet in one lane) and 8 NT tokens; its warps split K.
 // Weights are the MMA's rows: a lane's 16 bytes of a row are k = 8 c .. 8 c + 7 of every 32, the k that two MMAs take from it, and the
 // tokens are read in the same order.
-constexpr int kFewThreads = 256, kFewWarps = kFewThreads / 32, kFewAhead = 4;
+constexpr int kFewThreads = 256, kFewWarps = kFewThreads / 32;
 
 template <typename O, int NT, bool GATED>
-__global__ void __launch_bounds__(kFewThreads)
-linear_few_kernel(const __grid_constant__ LinearArgs a) {
+__global__ void __launch_bounds__(kFewThreads, 2)
+linear_few_kernel(const __grid_constant__ LinearArgs a, int rows) {
+    constexpr int kFewAhead = NT == 1 ? 8 : 4;
     __shared__ float part[kFewWarps][NT][16][9];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
-    const int rows = GATED ? 8 : 16;
     const long long n0 = (long long)blockIdx.x * rows, t0 = (long long)blockIdx.y * 8 * NT;
+    const int n_rows = (int)min((long long)rows, a.N - n0);
+    if (tid < (GATED ? 2 : 1) * n_rows) {                                  // into L2, before the wait (the kernel in front may be writing them: L2 has what it writes)
+        const __nv_bfloat16* row = tid < n_rows ? a.w + (n0 + tid) * a.ld_w : a.w_up + (n0 + tid - n_rows) * a.ld_up;
+        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(row), "r"(2 * min(a.K, 1 << 19)) : "memory");
+    }
     grid_dependency_wait();
     grid_launch_dependents();
     const uint4 zero = make_uint4(0, 0, 0, 0);
-    const bool row_a = n0 + g < a.N, row_b = GATED ? row_a : n0 + 8 + g < a.N;
+    const bool row_a = g < n_rows, row_b = GATED ? row_a : 8 + g < n_rows;
     const __nv_bfloat16* wa = a.w + (n0 + g) * a.ld_w + 8 * c;
     const __nv_bfloat16* wb = GATED ? a.w_up + (n0 + g) * a.ld_up + 8 * c : a.w + (n0 + 8 + g) * a.ld_w + 8 * c;
     float acc[NT][4];
@@ -65,10 +70,10 @@ linear_few_kernel(const __grid_constant__ LinearArgs a) {
         part[warp][i][8 + g][2 * c + 1] = acc[i][3];
     }
     __syncthreads();
-    for (int i = tid; i < NT * 8 * rows; i += kFewThreads) {
-        const int r = i % rows, tt = i / rows, nt = tt >> 3, col = tt & 7;
+    for (int i = tid; i < NT * 8 * n_rows; i += kFewThreads) {
+        const int r = i % n_rows, tt = i / n_rows, nt = tt >> 3, col = tt & 7;
         const long long n = n0 + r, t = t0 + tt;
-        if (n >= a.N || t >= a.T) continue;
+        if (t >= a.T) continue;
         float v = 0.f, u = 0.f;
 #pragma unroll
         for (int w = 0; w < kFewWarps; ++w) {
@@ -84,7 +89,9 @@ linear_few_kernel(const __grid_constant__ LinearArgs a) {
 
 template <typename O, int NT, bool GATED>
 int launch_few(const LinearArgs& a, cudaStream_t st) {
-    constexpr int rows = GATED ? 8 : 16;
+    // as many rows, up to 16 (8 of each matrix), as spread evenly over the SMs
+    constexpr int most = GATED ? 8 : 16;
+    const long long turns = (a.N + most * 148ll - 1) / (most * 148ll), rows = (a.N + 148 * turns - 1) / (148 * turns);
     cudaLaunchConfig_t lc{};
     lc.gridDim = dim3((unsigned)((a.N + rows - 1) / rows), (unsigned)((a.T + 8 * NT - 1) / (8 * NT)));
     lc.blockDim = dim3(kFewThreads);
@@ -97,7 +104,7 @@ int launch_few(const LinearArgs& a, cudaStream_t st) {
 #ifdef EXMOE_DISABLE_PDL
     lc.numAttrs = 0;
 #endif
-    if (cudaLaunchKernelEx(&lc, linear_few_kernel<O, NT, GATED>, a) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&lc, linear_few_kernel<O, NT, GATED>, a, (int)rows) != cudaSuccess) {
         cudaGetLastError();
         return EXMOE_ERR_CUDA;
     }

@@ -31,6 +31,27 @@ __device__ __forceinline__ float activate(float v, int act) {
         default: return v;
     }
 }
+__device__ __forceinline__ void activate8(float (&v)[8], int act) {
+    switch (act) {
+        case EXMOE_ACT_RELU:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_RELU);
+            break;
+        case EXMOE_ACT_GELU:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_GELU);
+            break;
+        case EXMOE_ACT_GELU_TANH:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_GELU_TANH);
+            break;
+        case EXMOE_ACT_SILU:
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_SILU);
+            break;
+    }
+}
+
 template <typename O> __device__ __forceinline__ float load_out(const void* p, long long at);
 template <> __device__ __forceinline__ float load_out<float>(const void* p, long long at) { return static_cast<const float*>(p)[at]; }
 template <> __device__ __forceinline__ float load_out<__nv_bfloat16>(const void* p, long long at) { return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[at]); }

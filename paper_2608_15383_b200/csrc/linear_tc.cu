@@ -69,17 +69,18 @@ __device__ __forceinline__ void drain(uint32_t at, int cols, bool first, float (
     }
 }
 
-// ---- one CTA per tile part -----------------------------------------------------------------------------------------
-constexpr int kSplitStages = 6, kSplitThreads = 32 * 12, kSplitTokens = 128;
-struct __align__(1024) SplitShared {
-    union {
-        unsigned char ring[kSplitStages][kABytes + kSplitTokens * 128];
-        float part[kSplitTokens][BM];                                      // this CTA's part of the tile
-    };
-    uint64_t full[kSplitStages], empty[kSplitStages], acc_full[2], acc_empty[2], drained;
+// ---- clusters that split K -------------------------------------------------------------------------------------------
+// 128 rows by up to 64 tokens; a CTA takes a CL-th of K.  Two CTAs fit an SM, so that one loads while another finishes, and so that the next call's can
+// be set up while this one's are at work.  The weights are requested into L2 before the wait for the kernel in front (which may still be writing them: L2 has
+// what it writes), and read behind it.
+constexpr int kSplitThreads = 256, kSplitTokens = 64, kSplitDrain = 4, kSplitRoom = 104 * 1024;
+__host__ __device__ constexpr int split_stages(int BN) { return kSplitRoom / (kABytes + BN * 128); }
+struct SplitShared {                                                       // behind the ring, which then holds the CTA's part of the tile: float [BN][BM]
+    uint64_t full[8], empty[8], acc_full[2], acc_empty[2], drained;
     uint32_t tmem;
     int abort_flag;
 };
+static_assert(kSplitTokens * BM * 4 <= kSplitRoom && split_stages(16) <= 8, "room");
 
 __device__ __forceinline__ void mma_one(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
@@ -89,32 +90,113 @@ __device__ __forceinline__ void mma_one(uint32_t d_tmem, uint64_t a_desc, uint64
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
+__device__ __forceinline__ void prefetch_2d(const CUtensorMap* map, int x, int y) {
+    asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y) : "memory");
+}
 
-template <typename O, bool GATED>
-__global__ void __launch_bounds__(kSplitThreads, 1)
+// The CTA's share of the tile's tokens, summed over the cluster in order and finished: a thread has one output of every (256 / kRows)-th token, eight at a time.
+// before: the residuals of the first eight, requested before the others' parts were there.
+template <typename O, bool GATED, int CL>
+struct Finish {
+    static constexpr int kRows = GATED ? BM / 2 : BM, kEvery = kSplitThreads / kRows;
+    const LinearArgs& a;
+    int nn, row, c0, c_end;
+    long long t0;
+    O res[8];
+    __device__ __forceinline__ Finish(const LinearArgs& args, int n0, long long tile_t0, int rank, int BN, int tid) : a(args), t0(tile_t0) {
+        const int share = (BN + CL - 1) / CL;
+        row = tid % kRows;
+        nn = n0 + row;
+        c0 = rank * share + tid / kRows;
+        c_end = (int)min((long long)min(BN, (rank + 1) * share), a.T - t0);
+        if (nn >= a.N) c_end = 0;
+        load(c0);
+    }
+    __device__ __forceinline__ void load(int from) {
+        if (!a.residual) return;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (from + i * kEvery < c_end) res[i] = static_cast<const O*>(a.residual)[(t0 + from + i * kEvery) * a.ld_res + nn];
+    }
+    __device__ __forceinline__ void operator()(uint32_t part) {
+        if (c0 >= c_end) return;
+        const float bias = a.bias ? a.bias[nn] : 0.f, bias_up = GATED && a.bias_up ? a.bias_up[nn] : 0.f;
+        uint32_t from[CL];
+#pragma unroll
+        for (int p = 0; p < CL; ++p) from[p] = (CL > 1 ? at_rank(part, p) : part) + 4 * row;
+        constexpr int kBatch = CL * (GATED ? 2 : 1) > 4 ? 4 : 8;           // loads in flight: at most 64
+        for (int c = c0; c < c_end; c += 8 * kEvery) {
+            float v[8], up[8];
+#pragma unroll
+            for (int b = 0; b < 8; b += kBatch) {
+                float g[CL][kBatch], u[CL][kBatch];
+#pragma unroll
+                for (int p = 0; p < CL; ++p)
+#pragma unroll
+                    for (int i = 0; i < kBatch; ++i) {
+                        const uint32_t at = from[p] + 4 * BM * min(c + (b + i) * kEvery, c_end - 1);
+                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(g[p][i]) : "r"(at) : "memory");
+                        if (GATED) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(u[p][i]) : "r"(at + 4 * kRows) : "memory");
+                    }
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    v[b + i] = g[0][i];
+                    up[b + i] = u[0][i];
+#pragma unroll
+                    for (int p = 1; p < CL; ++p) {
+                        v[b + i] += g[p][i];
+                        if (GATED) up[b + i] += u[p][i];
+                    }
+                    v[b + i] += bias;
+                }
+            }
+            activate8(v, a.act);
+            O* out = static_cast<O*>(a.out) + (t0 + c) * a.ld_out + nn;
+#pragma unroll
+            for (int i = 0; i < 8; ++i, out += kEvery * a.ld_out) {
+                if (c + i * kEvery >= c_end) break;
+                float y = GATED ? v[i] * (up[i] + bias_up) : v[i];
+                if (a.residual) y += (float)res[i];
+                store_out(out, y);
+            }
+            load(c + 8 * kEvery);
+        }
+    }
+};
+
+template <typename O, bool GATED, int CL>
+__global__ void __launch_bounds__(kSplitThreads, 2)
 linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_u, const __grid_constant__ CUtensorMap map_x,
-                    const __grid_constant__ LinearArgs a, int BN, int CL, int row_tiles) {
+                    const __grid_constant__ LinearArgs a, int BN, int row_tiles) {
     extern __shared__ unsigned char raw[];
-    SplitShared& sm = *reinterpret_cast<SplitShared*>(raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u));
+    unsigned char* ring = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
+    SplitShared& sm = *reinterpret_cast<SplitShared*>(ring + kSplitRoom);
     constexpr int kRows = GATED ? BM / 2 : BM;                             // outputs of a tile
     const int tid = threadIdx.x, lane = tid & 31, warp = warp_uniform(tid >> 5);
-    const int rank = (int)blockIdx.x % CL, tile = (int)blockIdx.x / CL;
-    const int n0 = tile % row_tiles * kRows, t0 = tile / row_tiles * BN;
+    const int rank = CL > 1 ? (int)blockIdx.x % CL : 0, tile = (int)blockIdx.x / CL;
+    const int n0 = tile % row_tiles * kRows, t0 = tile / row_tiles * BN, stages = split_stages(BN), stage_bytes = kABytes + BN * 128;
+    const int blocks = (a.K + 63) / 64, kb0 = (int)((long long)blocks * rank / CL), n = (int)((long long)blocks * (rank + 1) / CL) - kb0;
     volatile int* abort_flag = &sm.abort_flag;
+    if (warp == 1) {
+        for (int i = lane; i < n; i += 32) {
+            prefetch_2d(&map_w, (kb0 + i) * 64, n0);
+            if (GATED) prefetch_2d(&map_u, (kb0 + i) * 64, n0);
+        }
+    }
     if (tid == 0) {
-        for (int s = 0; s < kSplitStages; ++s) {
+        for (int s = 0; s < stages; ++s) {
             mbar_init(&sm.full[s], 1);
             mbar_init(&sm.empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&sm.acc_full[b], 1);
-            mbar_init(&sm.acc_empty[b], 8);
+            mbar_init(&sm.acc_empty[b], kSplitDrain);
         }
         mbar_init(&sm.drained, 1);
         sm.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 0) {
+    if (warp == 2) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem)), "r"(2 * kSplitTokens));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
     }
@@ -124,39 +206,44 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     const uint32_t tmem = sm.tmem;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int blocks = (a.K + 63) / 64, kb0 = (int)((long long)blocks * rank / CL), n = (int)((long long)blocks * (rank + 1) / CL) - kb0;
-    const uint32_t stage_bytes = (uint32_t)(kABytes + BN * 128);
-    const uint32_t full = smem_u32(sm.full), empty = smem_u32(sm.empty), acc_full = smem_u32(sm.acc_full), acc_empty = smem_u32(sm.acc_empty);
+    const uint32_t full = smem_u32(sm.full), empty = smem_u32(sm.empty), acc_full = smem_u32(sm.acc_full), acc_empty = smem_u32(sm.acc_empty), ring_at = smem_u32(ring);
     bool ok = true;
+    float acc[64];
     if (warp == 0) {
-        int i = 0;
+        int i = 0, s = 0, turn = 0;
         for (; i < n; ++i) {
-            const int s = i % kSplitStages;
-            if (i >= kSplitStages) ok = mbar_wait_warp(empty + 8 * s, (i / kSplitStages - 1) & 1, abort_flag, &g_linear_status);
+            if (turn > 0) ok = mbar_wait_warp(empty + 8 * s, (turn - 1) & 1, abort_flag, &g_linear_status);
             if (!ok) break;
             if (elect_one()) {
-                const uint32_t at = smem_u32(sm.ring[s]);
+                const uint32_t at = ring_at + s * stage_bytes;
                 const int k = (kb0 + i) * 64;
-                mbar_expect_tx(&sm.full[s], stage_bytes);
+                mbar_expect_tx(&sm.full[s], (uint32_t)stage_bytes);
                 tma_load_2d(at, &map_w, k, n0, &sm.full[s]);
                 if (GATED) tma_load_2d(at + kABytes / 2, &map_u, k, n0, &sm.full[s]);
                 tma_load_2d(at + kABytes, &map_x, k, t0, &sm.full[s]);
             }
             __syncwarp();
+            if (++s == stages) {
+                s = 0;
+                ++turn;
+            }
         }
-        if (!ok)
-            for (int j = max(0, i - kSplitStages); j < i; ++j) in_flight_end(full + 8 * (j % kSplitStages), (j / kSplitStages) & 1);
+        if (!ok)                                                           // the copies in flight end before their memory is used again
+            for (int j = 0; j < stages; ++j)
+                if (turn > 0 || j < s) in_flight_end(full + 8 * j, (j < s ? turn : turn - 1) & 1);
     } else if (warp == 1) {
         const uint32_t idesc = make_idesc(BN);
-        const uint64_t da0 = make_desc_b(smem_u32(sm.ring[0])), db0 = make_desc_b(smem_u32(sm.ring[0]) + kABytes);
+        const uint64_t da0 = make_desc_b(ring_at), db0 = make_desc_b(ring_at + kABytes);
+        int s = 0;
+        uint32_t turn = 0;
         for (int i = 0; i < n; ++i) {
-            const int s = i % kSplitStages, c = i / kChain, buf = c & 1;
+            const int c = i / kChain, buf = c & 1;
             if (i % kChain == 0 && c >= 2) ok = mbar_wait_warp(acc_empty + 8 * buf, (c / 2 - 1) & 1, abort_flag, &g_linear_status);
-            if (ok) ok = mbar_wait_warp(full + 8 * s, (i / kSplitStages) & 1, abort_flag, &g_linear_status);
+            if (ok) ok = mbar_wait_warp(full + 8 * s, turn, abort_flag, &g_linear_status);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
-                const uint64_t off = (uint64_t)(s * (kABytes + kSplitTokens * 128) >> 4);
+                const uint64_t off = (uint64_t)(s * stage_bytes >> 4);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)                                // K = 16: 32 bytes on
                     mma_one(tmem + buf * kSplitTokens, da0 + off + 2 * j, db0 + off + 2 * j, idesc, j > 0 || i % kChain > 0);
@@ -164,37 +251,37 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
                 if (i % kChain == kChain - 1 || i == n - 1) tc_commit_at(acc_full + 8 * buf);
             }
             __syncwarp();
+            if (++s == stages) {
+                s = 0;
+                turn ^= 1;
+            }
         }
         if (!ok) {                                                         // given up: the MMAs in flight end before their operands' memory is used again
             if (elect_one()) tc_commit_at(smem_u32(&sm.drained));
             __syncwarp();
             in_flight_end(smem_u32(&sm.drained), 0);
         }
-    }
-    float acc[64];
-    const int quarter = warp & 3, half = (warp - 4) >> 2, cw = BN / 2;     // drain warps: half of the columns, on their 32 lanes
-    if (warp >= 4) {
+    } else if (warp >= 4) {
         const int chains = (n + kChain - 1) / kChain;
-        if (chains == 0)
-#pragma unroll
-            for (int i = 0; i < 64; ++i) acc[i] = 0.f;
         for (int c = 0; c < chains; ++c) {
             const int buf = c & 1;
             ok = mbar_wait_warp(acc_full + 8 * buf, (c >> 1) & 1, abort_flag, &g_linear_status);
             if (!ok) break;
             tc_fence_after();
-            drain(tmem + ((uint32_t)(32 * quarter) << 16) + buf * kSplitTokens + half * cw, cw, c == 0, acc);
+            drain(tmem + ((uint32_t)(32 * (warp & 3)) << 16) + buf * kSplitTokens, BN, c == 0, acc);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_at(acc_empty + 8 * buf);
         }
     }
+    Finish<O, GATED, CL> finish(a, n0, t0, rank, BN, tid);
     __syncthreads();                                                       // the ring has been read (or is given up), the accumulators too
-    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kSplitTokens));
+    if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kSplitTokens));
     if (warp >= 4) {
+        float* part = reinterpret_cast<float*>(ring) + 32 * (warp & 3) + lane;
 #pragma unroll
         for (int i = 0; i < 64; ++i)
-            if (i < cw) sm.part[half * cw + i][32 * quarter + lane] = acc[i];
+            if (i < BN) part[i * BM] = acc[i];
     }
     if (CL > 1) {
         cluster_arrive();
@@ -202,63 +289,24 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     } else {
         __syncthreads();
     }
-    if (warp >= 4) {
-        // a CTA finishes a CL-th of the tile's tokens; a thread one output of every (256 / kRows)-th of them, four at a time
-        const int u = tid - 128, row = u % kRows, share = (BN + CL - 1) / CL, c_end = min(BN, (rank + 1) * share), nn = n0 + row;
-        constexpr int kStep = 256 / kRows;
-        const float bias = a.bias && nn < a.N ? a.bias[nn] : 0.f, bias_up = GATED && a.bias_up && nn < a.N ? a.bias_up[nn] : 0.f;
-        const uint32_t part = smem_u32(sm.part);
-        for (int c0 = rank * share + u / kRows; c0 < c_end && nn < a.N; c0 += 4 * kStep) {
-            float v[4], up[4], res[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int c = c0 + i * kStep;
-                const long long t = t0 + c;
-                v[i] = up[i] = res[i] = 0.f;
-                if (c < c_end && t < a.T && a.residual) res[i] = load_out<O>(a.residual, t * a.ld_res + nn);
-            }
-            for (int p = 0; p < CL; ++p) {
-                const uint32_t from = at_rank(part, p);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int c = min(c0 + i * kStep, c_end - 1);
-                    float g;
-                    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(g) : "r"(from + 4 * (c * BM + row)) : "memory");
-                    v[i] += g;
-                    if (GATED) {
-                        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(g) : "r"(from + 4 * (c * BM + BM / 2 + row)) : "memory");
-                        up[i] += g;
-                    }
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int c = c0 + i * kStep;
-                const long long t = t0 + c;
-                if (c >= c_end || t >= a.T) continue;
-                float y = activate(v[i] + bias, a.act);
-                if (GATED) y *= up[i] + bias_up;
-                store_out(static_cast<O*>(a.out) + t * a.ld_out + nn, y + res[i]);
-            }
-        }
-    }
+    finish(ring_at);
     if (CL > 1) {
         cluster_arrive();                                                  // nobody reads this CTA's shared memory any more
         cluster_wait();
     }
 }
 
-template <typename O, bool GATED>
-int launch_split(const LinearArgs& a, int BN, int CL, cudaStream_t st) {
+template <typename O, bool GATED, int CL>
+int launch_split(const LinearArgs& a, int BN, cudaStream_t st) {
     constexpr int kRows = GATED ? BM / 2 : BM;
     alignas(64) CUtensorMap mw, mu, mx;
     if (encode_map(&mw, a.w, a.N, a.K, a.ld_w, kRows) || encode_map(&mu, GATED ? a.w_up : a.w, a.N, a.K, GATED ? a.ld_up : a.ld_w, kRows) ||
         encode_map(&mx, a.x, a.T, a.K, a.ld_x, BN))
         return EXMOE_ERR_CUDA;
     static SmemOnce once;
-    const auto kern = linear_split_kernel<O, GATED>;
-    constexpr int smem = (int)sizeof(SplitShared) + 1024;
-    static_assert(smem <= 227 * 1024, "shared memory");
+    const auto kern = linear_split_kernel<O, GATED, CL>;
+    constexpr int smem = kSplitRoom + (int)sizeof(SplitShared) + 1024;
+    static_assert(2 * (smem + 1024) <= 228 * 1024, "shared memory of two CTAs");
     if (!allow_smem(kern, smem, once)) return EXMOE_ERR_CUDA;
     const int row_tiles = (a.N + kRows - 1) / kRows;
     const long long ctas = (long long)row_tiles * ((a.T + BN - 1) / BN) * CL;
@@ -272,15 +320,15 @@ int launch_split(const LinearArgs& a, int BN, int CL, cudaStream_t st) {
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)CL;
+    attr[1].val.clusterDim.x = CL;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     lc.attrs = attr;
-    lc.numAttrs = 2;
+    lc.numAttrs = CL > 1 ? 2 : 1;
 #ifdef EXMOE_DISABLE_PDL
     lc.attrs = attr + 1;
     --lc.numAttrs;
 #endif
-    if (cudaLaunchKernelEx(&lc, kern, mw, mu, mx, a, BN, CL, row_tiles) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&lc, kern, mw, mu, mx, a, BN, row_tiles) != cudaSuccess) {
         cudaGetLastError();
         return EXMOE_ERR_CUDA;
     }
@@ -367,27 +415,6 @@ struct Outputs {
         }
     }
 };
-__device__ __forceinline__ void activate8(float (&v)[8], int act) {
-    switch (act) {
-        case EXMOE_ACT_RELU:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_RELU);
-            break;
-        case EXMOE_ACT_GELU:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_GELU);
-            break;
-        case EXMOE_ACT_GELU_TANH:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_GELU_TANH);
-            break;
-        case EXMOE_ACT_SILU:
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_SILU);
-            break;
-    }
-}
-
 // The pairs work side by side on tiles of kGroup rows of tiles and as many columns as it takes: what they read at a time is then few weights and few
 // tokens (8192 x 8192 -> 8192 outputs: TODO us instead of 805 along whole columns).
 constexpr int kGroup = 8;
@@ -660,28 +687,33 @@ int launch_pair(const LinearArgs& a, int BN, cudaStream_t st) {
     return EXMOE_OK;
 }
 
+// Which form, and its tile.  Both cost models are in clocks of an SM, from what was measured: a stage of the split form takes 300 with up to 64 tokens (its 24 KB
+// come at 80 bytes a clock), a pair's k-step of 16 what shared memory takes for its operands, 64 + BN / 4.
 template <typename O, bool GATED>
 int launch_tc(const LinearArgs& a, cudaStream_t st) {
     const int row_tiles = (a.N + (GATED ? 63 : 127)) / (GATED ? 64 : 128), blocks = (a.K + 63) / 64;
     const long long pair_rows = (row_tiles + 1) / 2;
-    if (pair_rows * ((a.T + 255) / 256) >= kSms / 4) {
-        int best = 256;
-        long long least = INT64_MAX;
-        for (int BN = 256; BN >= 96; BN -= 32) {
-            const long long rounds = (pair_rows * ((a.T + BN - 1) / BN) + kSms / 2 - 1) / (kSms / 2), cost = rounds * (blocks * (long long)(256 + BN) + 1500);
-            if (cost < least) {
-                least = cost;
-                best = BN;
-            }
+    int best = 256;
+    long long pair_cost = INT64_MAX;
+    for (int BN = 256; BN >= 64; BN -= 32) {
+        const long long rounds = (pair_rows * ((a.T + BN - 1) / BN) + kSms / 2 - 1) / (kSms / 2), cost = rounds * (blocks * (long long)(256 + BN) + 1500) + 6000;
+        if (cost < pair_cost) {
+            pair_cost = cost;
+            best = BN;
         }
-        return launch_pair<O, GATED>(a, best, st);
     }
-    int BN = 128;
-    if (a.T <= 128) BN = (a.T + 31) / 32 * 32;
+    const int BN = a.T >= 64 ? 64 : (a.T + 31) / 32 * 32;
     const long long tiles = (long long)row_tiles * ((a.T + BN - 1) / BN);
     int CL = 8;
-    while (CL > 1 && (tiles * CL > kSms || blocks < 2 * CL)) CL /= 2;
-    return launch_split<O, GATED>(a, BN, CL, st);
+    while (CL > 1 && (tiles * CL > 2 * kSms || blocks < 2 * CL)) CL /= 2;
+    const long long per_sm = (tiles * CL + kSms - 1) / kSms, split_cost = per_sm * ((blocks + CL - 1) / CL) * 300 + 3000 * ((per_sm + 1) / 2) + (CL > 1 ? 4000 : 2000);
+    if (pair_cost < split_cost) return launch_pair<O, GATED>(a, best, st);
+    switch (CL) {
+        case 8: return launch_split<O, GATED, 8>(a, BN, st);
+        case 4: return launch_split<O, GATED, 4>(a, BN, st);
+        case 2: return launch_split<O, GATED, 2>(a, BN, st);
+        default: return launch_split<O, GATED, 1>(a, BN, st);
+    }
 }
 
 }  // namespace
