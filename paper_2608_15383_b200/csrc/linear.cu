@@ -16,35 +16,36 @@ constexpr int kMaxTokens = 1 << 29, kMaxDim = 1 << 30;
 // tokens are read in the same order.
 constexpr int kFewThreads = 256, kFewWarps = kFewThreads / 32;
 
+// A CTA goes through groups of rows; a warp has its next weights and tokens on their way while the group's parts are added up.
 template <typename O, int NT, bool GATED>
 __global__ void __launch_bounds__(kFewThreads, 2)
-linear_few_kernel(const __grid_constant__ LinearArgs a, int rows) {
-    constexpr int kFewAhead = NT == 1 ? 8 : 4;
-    __shared__ float part[kFewWarps][NT][16][9];
+linear_few_kernel(const __grid_constant__ LinearArgs a, int rows, int groups) {
+    constexpr int kAhead = NT == 1 ? 8 : 4;
+    __shared__ float part[2][kFewWarps][NT][16][9];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
-    const long long n0 = (long long)blockIdx.x * rows, t0 = (long long)blockIdx.y * 8 * NT;
-    const int n_rows = (int)min((long long)rows, a.N - n0);
-    if (tid < (GATED ? 2 : 1) * n_rows) {                                  // into L2, before the wait (the kernel in front may be writing them: L2 has what it writes)
-        const __nv_bfloat16* row = tid < n_rows ? a.w + (n0 + tid) * a.ld_w : a.w_up + (n0 + tid - n_rows) * a.ld_up;
-        asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(row), "r"(2 * min(a.K, 1 << 19)) : "memory");
+    const long long t0 = (long long)blockIdx.y * 8 * NT;
+    {   // into L2, before the wait (the kernel in front may be writing them: L2 has what it writes)
+        const long long n0 = (long long)blockIdx.x * rows;
+        const int n_rows = (int)min((long long)rows, a.N - n0);
+        if (tid < (GATED ? 2 : 1) * n_rows) {
+            const __nv_bfloat16* row = tid < n_rows ? a.w + (n0 + tid) * a.ld_w : a.w_up + (n0 + tid - n_rows) * a.ld_up;
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(row), "r"(2 * min(a.K, 1 << 19)) : "memory");
+        }
     }
     grid_dependency_wait();
     grid_launch_dependents();
     const uint4 zero = make_uint4(0, 0, 0, 0);
-    const bool row_a = g < n_rows, row_b = GATED ? row_a : 8 + g < n_rows;
-    const __nv_bfloat16* wa = a.w + (n0 + g) * a.ld_w + 8 * c;
-    const __nv_bfloat16* wb = GATED ? a.w_up + (n0 + g) * a.ld_up + 8 * c : a.w + (n0 + 8 + g) * a.ld_w + 8 * c;
-    float acc[NT][4];
+    const int blocks = (a.K + 31) / 32, batches = max(1, (blocks + kFewWarps * kAhead - 1) / (kFewWarps * kAhead));
+    uint4 va[kAhead], vb[kAhead], vx[kAhead][NT];
+    const auto load = [&](int group, int batch) {
+        const long long n0 = (long long)group * rows;
+        const int n_rows = (int)min((long long)rows, a.N - n0);
+        const bool row_a = g < n_rows, row_b = GATED ? row_a : 8 + g < n_rows;
+        const __nv_bfloat16* wa = a.w + (n0 + g) * a.ld_w + 8 * c;
+        const __nv_bfloat16* wb = GATED ? a.w_up + (n0 + g) * a.ld_up + 8 * c : a.w + (n0 + 8 + g) * a.ld_w + 8 * c;
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
-    const int blocks = (a.K + 31) / 32;
-    for (int b0 = warp; b0 < blocks; b0 += kFewWarps * kFewAhead) {
-        uint4 va[kFewAhead], vb[kFewAhead], vx[kFewAhead][NT];
-#pragma unroll
-        for (int u = 0; u < kFewAhead; ++u) {
-            const int k = (b0 + u * kFewWarps) * 32;
+        for (int u = 0; u < kAhead; ++u) {
+            const int k = (warp + (batch * kAhead + u) * kFewWarps) * 32;
             const bool in = k + 8 * c < a.K;
             va[u] = in && row_a ? *reinterpret_cast<const uint4*>(wa + k) : zero;
             vb[u] = in && row_b ? *reinterpret_cast<const uint4*>(wb + k) : zero;
@@ -54,36 +55,53 @@ linear_few_kernel(const __grid_constant__ LinearArgs a, int rows) {
                 vx[u][i] = in && t < a.T ? *reinterpret_cast<const uint4*>(a.x + t * a.ld_x + 8 * c + k) : zero;
             }
         }
+    };
+    int group = blockIdx.x;
+    if (group < groups) load(group, 0);
+    for (int turn = 0; group < groups; turn ^= 1) {
+        float acc[NT][4];
 #pragma unroll
-        for (int u = 0; u < kFewAhead; ++u)
+        for (int i = 0; i < NT; ++i)
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                mma_m16n8k16(acc[i], va[u].x, vb[u].x, va[u].y, vb[u].y, vx[u][i].x, vx[u][i].y);
-                mma_m16n8k16(acc[i], va[u].z, vb[u].z, va[u].w, vb[u].w, vx[u][i].z, vx[u][i].w);
-            }
-    }
+            for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+        const int next = group + (int)gridDim.x;
+        for (int batch = 0; batch < batches; ++batch) {
 #pragma unroll
-    for (int i = 0; i < NT; ++i) {
-        part[warp][i][g][2 * c] = acc[i][0];
-        part[warp][i][g][2 * c + 1] = acc[i][1];
-        part[warp][i][8 + g][2 * c] = acc[i][2];
-        part[warp][i][8 + g][2 * c + 1] = acc[i][3];
-    }
-    __syncthreads();
-    for (int i = tid; i < NT * 8 * n_rows; i += kFewThreads) {
-        const int r = i % n_rows, tt = i / n_rows, nt = tt >> 3, col = tt & 7;
-        const long long n = n0 + r, t = t0 + tt;
-        if (t >= a.T) continue;
-        float v = 0.f, u = 0.f;
+            for (int u = 0; u < kAhead; ++u)
 #pragma unroll
-        for (int w = 0; w < kFewWarps; ++w) {
-            v += part[w][nt][r][col];
-            if (GATED) u += part[w][nt][8 + r][col];
+                for (int i = 0; i < NT; ++i) {
+                    mma_m16n8k16(acc[i], va[u].x, vb[u].x, va[u].y, vb[u].y, vx[u][i].x, vx[u][i].y);
+                    mma_m16n8k16(acc[i], va[u].z, vb[u].z, va[u].w, vb[u].w, vx[u][i].z, vx[u][i].w);
+                }
+            if (batch + 1 < batches) load(group, batch + 1);
+            else if (next < groups) load(next, 0);
         }
-        v = activate(v + (a.bias ? a.bias[n] : 0.f), a.act);
-        if (GATED) v *= u + (a.bias_up ? a.bias_up[n] : 0.f);
-        if (a.residual) v += load_out<O>(a.residual, t * a.ld_res + n);
-        store_out(static_cast<O*>(a.out) + t * a.ld_out + n, v);
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            part[turn][warp][i][g][2 * c] = acc[i][0];
+            part[turn][warp][i][g][2 * c + 1] = acc[i][1];
+            part[turn][warp][i][8 + g][2 * c] = acc[i][2];
+            part[turn][warp][i][8 + g][2 * c + 1] = acc[i][3];
+        }
+        __syncthreads();                                                   // (a warp writes these parts again behind the next one: all have read them by then)
+        const long long n0 = (long long)group * rows;
+        const int n_rows = (int)min((long long)rows, a.N - n0);
+        for (int i = tid; i < NT * 8 * n_rows; i += kFewThreads) {
+            const int r = i % n_rows, tt = i / n_rows, nt = tt >> 3, col = tt & 7;
+            const long long n = n0 + r, t = t0 + tt;
+            if (t >= a.T) continue;
+            float v = 0.f, u = 0.f;
+#pragma unroll
+            for (int w = 0; w < kFewWarps; ++w) {
+                v += part[turn][w][nt][r][col];
+                if (GATED) u += part[turn][w][nt][8 + r][col];
+            }
+            v = activate(v + (a.bias ? a.bias[n] : 0.f), a.act);
+            if (GATED) v *= u + (a.bias_up ? a.bias_up[n] : 0.f);
+            if (a.residual) v += load_out<O>(a.residual, t * a.ld_res + n);
+            store_out(static_cast<O*>(a.out) + t * a.ld_out + n, v);
+        }
+        group = next;
     }
 }
 
@@ -93,7 +111,8 @@ int launch_few(const LinearArgs& a, cudaStream_t st) {
     constexpr int most = GATED ? 8 : 16;
     const long long turns = (a.N + most * 148ll - 1) / (most * 148ll), rows = (a.N + 148 * turns - 1) / (148 * turns);
     cudaLaunchConfig_t lc{};
-    lc.gridDim = dim3((unsigned)((a.N + rows - 1) / rows), (unsigned)((a.T + 8 * NT - 1) / (8 * NT)));
+    const long long groups = (a.N + rows - 1) / rows;
+    lc.gridDim = dim3((unsigned)std::min(groups, 2 * 148ll), (unsigned)((a.T + 8 * NT - 1) / (8 * NT)));
     lc.blockDim = dim3(kFewThreads);
     lc.stream = st;
     cudaLaunchAttribute attr[1];
@@ -104,7 +123,7 @@ int launch_few(const LinearArgs& a, cudaStream_t st) {
 #ifdef EXMOE_DISABLE_PDL
     lc.numAttrs = 0;
 #endif
-    if (cudaLaunchKernelEx(&lc, linear_few_kernel<O, NT, GATED>, a, (int)rows) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&lc, linear_few_kernel<O, NT, GATED>, a, (int)rows, (int)groups) != cudaSuccess) {
         cudaGetLastError();
         return EXMOE_ERR_CUDA;
     }

@@ -704,7 +704,7 @@ int launch_tc(const LinearArgs& a, cudaStream_t st) {
     }
     const int BN = a.T >= 64 ? 64 : (a.T + 31) / 32 * 32;
     const long long tiles = (long long)row_tiles * ((a.T + BN - 1) / BN);
-    int CL = 8;
+    int CL = tiles <= 4 ? 8 : 4;                                           // (clusters of eight start late: 64 tokens, 2048 x 2048, 9.0 us instead of 6.3)
     while (CL > 1 && (tiles * CL > 2 * kSms || blocks < 2 * CL)) CL /= 2;
     const long long per_sm = (tiles * CL + kSms - 1) / kSms, split_cost = per_sm * ((blocks + CL - 1) / CL) * 300 + 3000 * ((per_sm + 1) / 2) + (CL > 1 ? 4000 : 2000);
     if (pair_cost < split_cost) return launch_pair<O, GATED>(a, best, st);
