@@ -9,18 +9,19 @@ namespace exmoe {
 
 namespace {
 
-constexpr int kMaxTokens = 1 << 29, kMaxDim = 1 << 30;
+constexpr int kMaxTokens = 1 << 29, kMaxDim = 1 << 30, kSms = 148;
 
 // Few tokens.  A CTA takes 16 rows of W (8 of W and 8 of U: the two factors meet in one lane) and 8 NT tokens; its warps split K.
 // Weights are the MMA's rows: a lane's 16 bytes of a row are k = 8 c .. 8 c + 7 of every 32, the k that two MMAs take from it, and the
 // tokens are read in the same order.
-constexpr int kFewThreads = 256, kFewWarps = kFewThreads / 32;
-
 // A CTA goes through groups of rows; a warp has its next weights and tokens on their way while the group's parts are added up.
-template <typename O, int NT, bool GATED>
-__global__ void __launch_bounds__(kFewThreads, 2)
+// WARPS: 8, two CTAs per SM, or, where the SMs have a group each at most, 16 that share it (us, replayed from a graph, 8 / 16 warps: 2048 -> 2048 outputs 3.5 / 3.2,
+// 5632 -> 2048 7.4 / 6.2, 16 tokens 9.6 / 8.2; 2048 -> 5632 6.2 / 7.5, gated 8.7 / 10.2, 8192 -> 8192 22.4 / 25.8).  Either way an SM has 128 KB
+// (NT = 2: 64) of weights on their way.
+template <typename O, int NT, bool GATED, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS, 16 / WARPS)
 linear_few_kernel(const __grid_constant__ LinearArgs a, int rows, int groups) {
-    constexpr int kAhead = NT == 1 ? 8 : 4;
+    constexpr int kFewThreads = 32 * WARPS, kFewWarps = WARPS, kAhead = (NT == 1 ? 64 : 32) / WARPS;
     __shared__ float part[2][kFewWarps][NT][16][9];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
     const long long t0 = (long long)blockIdx.y * 8 * NT;
@@ -105,15 +106,16 @@ linear_few_kernel(const __grid_constant__ LinearArgs a, int rows, int groups) {
     }
 }
 
-template <typename O, int NT, bool GATED>
+template <typename O, int NT, bool GATED, int WARPS>
 int launch_few(const LinearArgs& a, cudaStream_t st) {
-    // as many rows, up to 16 (8 of each matrix), as spread evenly over the SMs
+    // as many rows, up to 16 (8 of each matrix), as spread evenly over the CTAs that the chip holds
     constexpr int most = GATED ? 8 : 16;
-    const long long turns = (a.N + most * 148ll - 1) / (most * 148ll), rows = (a.N + 148 * turns - 1) / (148 * turns);
+    constexpr long long ctas = kSms * (16 / WARPS);
+    const long long turns = (a.N + most * ctas - 1) / (most * ctas), rows = (a.N + ctas * turns - 1) / (ctas * turns);
     cudaLaunchConfig_t lc{};
     const long long groups = (a.N + rows - 1) / rows;
-    lc.gridDim = dim3((unsigned)std::min(groups, 2 * 148ll), (unsigned)((a.T + 8 * NT - 1) / (8 * NT)));
-    lc.blockDim = dim3(kFewThreads);
+    lc.gridDim = dim3((unsigned)std::min(groups, ctas), (unsigned)((a.T + 8 * NT - 1) / (8 * NT)));
+    lc.blockDim = dim3(32 * WARPS);
     lc.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -123,18 +125,18 @@ int launch_few(const LinearArgs& a, cudaStream_t st) {
 #ifdef EXMOE_DISABLE_PDL
     lc.numAttrs = 0;
 #endif
-    if (cudaLaunchKernelEx(&lc, linear_few_kernel<O, NT, GATED>, a, (int)rows, (int)groups) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&lc, linear_few_kernel<O, NT, GATED, WARPS>, a, (int)rows, (int)groups) != cudaSuccess) {
         cudaGetLastError();
         return EXMOE_ERR_CUDA;
     }
     count_launch();
     return EXMOE_OK;
 }
-// Tokens that the form for few takes: four times eight would hold four weights' fragments per 16 bytes of them.
 constexpr int kFewTokens = 16;
 template <typename O, bool GATED>
 int launch_few_tokens(const LinearArgs& a, cudaStream_t st) {
-    return a.T <= 8 ? launch_few<O, 1, GATED>(a, st) : launch_few<O, 2, GATED>(a, st);
+    if (a.N <= kSms * (GATED ? 8 : 16)) return a.T <= 8 ? launch_few<O, 1, GATED, 16>(a, st) : launch_few<O, 2, GATED, 16>(a, st);
+    return a.T <= 8 ? launch_few<O, 1, GATED, 8>(a, st) : launch_few<O, 2, GATED, 8>(a, st);
 }
 
 }  // namespace
