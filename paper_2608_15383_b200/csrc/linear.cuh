@@ -31,23 +31,25 @@ __device__ __forceinline__ float activate(float v, int act) {
         default: return v;
     }
 }
-__device__ __forceinline__ void activate8(float (&v)[8], int act) {
+// (One branch for all: the code of the others is not fetched.)
+template <int N>
+__device__ __forceinline__ void activate_all(float (&v)[N], int act) {
     switch (act) {
         case EXMOE_ACT_RELU:
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_RELU);
+            for (int i = 0; i < N; ++i) v[i] = activate(v[i], EXMOE_ACT_RELU);
             break;
         case EXMOE_ACT_GELU:
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_GELU);
+            for (int i = 0; i < N; ++i) v[i] = activate(v[i], EXMOE_ACT_GELU);
             break;
         case EXMOE_ACT_GELU_TANH:
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_GELU_TANH);
+            for (int i = 0; i < N; ++i) v[i] = activate(v[i], EXMOE_ACT_GELU_TANH);
             break;
         case EXMOE_ACT_SILU:
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = activate(v[i], EXMOE_ACT_SILU);
+            for (int i = 0; i < N; ++i) v[i] = activate(v[i], EXMOE_ACT_SILU);
             break;
     }
 }

@@ -9,6 +9,7 @@
 //
 // With a second matrix a tile's 128 rows are 64 of W and the same 64 of U: a row's two factors are 64 lanes of tensor memory apart and meet in shared memory.
 #include <algorithm>
+#include <mutex>
 
 #include "common.cuh"
 #include "frag.cuh"
@@ -73,14 +74,14 @@ __device__ __forceinline__ void drain(uint32_t at, int cols, bool first, float (
 // 128 rows by up to 64 tokens; a CTA takes a CL-th of K.  Two CTAs fit an SM, so that one loads while another finishes, and so that the next call's can
 // be set up while this one's are at work.  The weights are requested into L2 before the wait for the kernel in front (which may still be writing them: L2 has
 // what it writes), and read behind it.
-constexpr int kSplitThreads = 256, kSplitTokens = 64, kSplitDrain = 4, kSplitRoom = 104 * 1024;
-__host__ __device__ constexpr int split_stages(int BN) { return kSplitRoom / (kABytes + BN * 128); }
-struct SplitShared {                                                       // behind the ring, which then holds the CTA's part of the tile: float [BN][BM]
-    uint64_t full[8], empty[8], acc_full[2], acc_empty[2], drained;
+constexpr int kSplitThreads = 256, kSplitTokens = 64, kSplitDrain = 4, kSplitStages = 11;
+constexpr int kSplitRoom = 104 * 1024, kSplitRoomWide = 208 * 1024;        // of the ring: of two CTAs per SM, of one
+struct SplitShared {                                                       // in front of the ring, which then holds the CTA's part of the tile: float [BN][BM]
+    uint64_t full[kSplitStages], empty[kSplitStages], acc_full[2], acc_empty[2], drained;
     uint32_t tmem;
     int abort_flag;
 };
-static_assert(kSplitTokens * BM * 4 <= kSplitRoom && split_stages(16) <= 8, "room");
+static_assert(kSplitTokens * BM * 4 <= kSplitRoom && sizeof(SplitShared) <= 1024, "room");
 
 __device__ __forceinline__ void mma_one(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
@@ -94,16 +95,18 @@ __device__ __forceinline__ void prefetch_2d(const CUtensorMap* map, int x, int y
     asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y) : "memory");
 }
 
-// The CTA's share of the tile's tokens, summed over the cluster in order and finished: a thread has one output of every (256 / kRows)-th token, eight at a time.
-// before: the residuals of the first eight, requested before the others' parts were there.
-template <typename O, bool GATED, int CL>
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(map)) : "memory"); }
+
+// The CTA's share of the tile's tokens, summed over the cluster's CL <= PEERS CTAs in order and finished: a thread has one output of every (256 / kRows)-th
+// token, as many at a time as it has of a usual share, so that all parts are on their way together; their residuals are requested before the parts are there.
+template <typename O, bool GATED, int PEERS>
 struct Finish {
-    static constexpr int kRows = GATED ? BM / 2 : BM, kEvery = kSplitThreads / kRows;
+    static constexpr int kRows = GATED ? BM / 2 : BM, kEvery = kSplitThreads / kRows, kBatch = (PEERS == 2 ? 16 : PEERS == 4 ? 12 : 8) / (GATED ? 2 : 1);
     const LinearArgs& a;
-    int nn, row, c0, c_end;
+    int nn, row, c0, c_end, CL;
     long long t0;
-    O res[8];
-    __device__ __forceinline__ Finish(const LinearArgs& args, int n0, long long tile_t0, int rank, int BN, int tid) : a(args), t0(tile_t0) {
+    O res[kBatch];
+    __device__ __forceinline__ Finish(const LinearArgs& args, int n0, long long tile_t0, int rank, int cluster, int BN, int tid) : a(args), CL(cluster), t0(tile_t0) {
         const int share = (BN + CL - 1) / CL;
         row = tid % kRows;
         nn = n0 + row;
@@ -114,69 +117,67 @@ struct Finish {
     }
     __device__ __forceinline__ void load(int from) {
         if (!a.residual) return;
+        const O* p = static_cast<const O*>(a.residual) + (t0 + from) * a.ld_res + nn;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (from + i * kEvery < c_end) res[i] = static_cast<const O*>(a.residual)[(t0 + from + i * kEvery) * a.ld_res + nn];
+        for (int i = 0; i < kBatch; ++i, p += kEvery * a.ld_res)
+            if (from + i * kEvery < c_end) res[i] = *p;
     }
     __device__ __forceinline__ void operator()(uint32_t part) {
         if (c0 >= c_end) return;
         const float bias = a.bias ? a.bias[nn] : 0.f, bias_up = GATED && a.bias_up ? a.bias_up[nn] : 0.f;
-        uint32_t from[CL];
+        for (int c = c0; c < c_end; c += kBatch * kEvery) {
+            float g[PEERS][kBatch], u[PEERS][kBatch];
 #pragma unroll
-        for (int p = 0; p < CL; ++p) from[p] = (CL > 1 ? at_rank(part, p) : part) + 4 * row;
-        constexpr int kBatch = CL * (GATED ? 2 : 1) > 4 ? 4 : 8;           // loads in flight: at most 64
-        for (int c = c0; c < c_end; c += 8 * kEvery) {
-            float v[8], up[8];
+            for (int p = 0; p < PEERS; ++p)
+                if (p < CL) {
+                    const uint32_t from = at_rank(part, p) + 4 * row;
 #pragma unroll
-            for (int b = 0; b < 8; b += kBatch) {
-                float g[CL][kBatch], u[CL][kBatch];
-#pragma unroll
-                for (int p = 0; p < CL; ++p)
-#pragma unroll
-                    for (int i = 0; i < kBatch; ++i) {
-                        const uint32_t at = from[p] + 4 * BM * min(c + (b + i) * kEvery, c_end - 1);
+                    for (int i = 0; i < kBatch; ++i) {                     // (again the last one behind the end)
+                        const uint32_t at = from + 4 * BM * min(c + i * kEvery, c_end - 1);
                         asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(g[p][i]) : "r"(at) : "memory");
                         if (GATED) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(u[p][i]) : "r"(at + 4 * kRows) : "memory");
                     }
-#pragma unroll
-                for (int i = 0; i < kBatch; ++i) {
-                    v[b + i] = g[0][i];
-                    up[b + i] = u[0][i];
-#pragma unroll
-                    for (int p = 1; p < CL; ++p) {
-                        v[b + i] += g[p][i];
-                        if (GATED) up[b + i] += u[p][i];
-                    }
-                    v[b + i] += bias;
                 }
-            }
-            activate8(v, a.act);
+#pragma unroll
+            for (int p = 1; p < PEERS; ++p)
+                if (p < CL)
+#pragma unroll
+                    for (int i = 0; i < kBatch; ++i) {
+                        g[0][i] += g[p][i];
+                        if (GATED) u[0][i] += u[p][i];
+                    }
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) g[0][i] += bias;
+            activate_all(g[0], a.act);
+            if (GATED)
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) g[0][i] *= u[0][i] + bias_up;
+            if (a.residual)
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) g[0][i] += (float)res[i];
             O* out = static_cast<O*>(a.out) + (t0 + c) * a.ld_out + nn;
 #pragma unroll
-            for (int i = 0; i < 8; ++i, out += kEvery * a.ld_out) {
-                if (c + i * kEvery >= c_end) break;
-                float y = GATED ? v[i] * (up[i] + bias_up) : v[i];
-                if (a.residual) y += (float)res[i];
-                store_out(out, y);
-            }
-            load(c + 8 * kEvery);
+            for (int i = 0; i < kBatch; ++i, out += kEvery * a.ld_out)
+                if (c + i * kEvery < c_end) store_out(out, g[0][i]);
+            load(c + kBatch * kEvery);
         }
     }
 };
 
-template <typename O, bool GATED, int CL>
+template <typename O, bool GATED, int PEERS>
 __global__ void __launch_bounds__(kSplitThreads, 2)
 linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_u, const __grid_constant__ CUtensorMap map_x,
-                    const __grid_constant__ LinearArgs a, int BN, int row_tiles) {
+                    const __grid_constant__ LinearArgs a, int BN, int CL, int row_tiles, int stages) {
     extern __shared__ unsigned char raw[];
-    unsigned char* ring = raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u);
-    SplitShared& sm = *reinterpret_cast<SplitShared*>(ring + kSplitRoom);
+    SplitShared& sm = *reinterpret_cast<SplitShared*>(raw + ((1024u - (smem_u32(raw) & 1023u)) & 1023u));
+    unsigned char* ring = reinterpret_cast<unsigned char*>(&sm) + 1024;
     constexpr int kRows = GATED ? BM / 2 : BM;                             // outputs of a tile
     const int tid = threadIdx.x, lane = tid & 31, warp = warp_uniform(tid >> 5);
-    const int rank = CL > 1 ? (int)blockIdx.x % CL : 0, tile = (int)blockIdx.x / CL;
-    const int n0 = tile % row_tiles * kRows, t0 = tile / row_tiles * BN, stages = split_stages(BN), stage_bytes = kABytes + BN * 128;
+    const int rank = (int)blockIdx.x % CL, tile = (int)blockIdx.x / CL;
+    const int n0 = tile % row_tiles * kRows, t0 = tile / row_tiles * BN, stage_bytes = kABytes + BN * 128;
     const int blocks = (a.K + 63) / 64, kb0 = (int)((long long)blocks * rank / CL), n = (int)((long long)blocks * (rank + 1) / CL) - kb0;
     volatile int* abort_flag = &sm.abort_flag;
+    if (warp == 0 && lane < 3) prefetch_map(lane == 0 ? &map_w : lane == 1 ? &map_x : &map_u);
     if (warp == 1) {
         for (int i = lane; i < n; i += 32) {
             prefetch_2d(&map_w, (kb0 + i) * 64, n0);
@@ -274,7 +275,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
             if (lane == 0) mbar_arrive_at(acc_empty + 8 * buf);
         }
     }
-    Finish<O, GATED, CL> finish(a, n0, t0, rank, BN, tid);
+    Finish<O, GATED, PEERS> finish(a, n0, t0, rank, CL, BN, tid);
     __syncthreads();                                                       // the ring has been read (or is given up), the accumulators too
     if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kSplitTokens));
     if (warp >= 4) {
@@ -296,31 +297,31 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_cons
     }
 }
 
-template <typename O, bool GATED, int CL>
-int launch_split(const LinearArgs& a, int BN, cudaStream_t st) {
+template <typename O, bool GATED, int PEERS>
+int launch_split(const LinearArgs& a, int BN, int CL, bool wide, cudaStream_t st) {
     constexpr int kRows = GATED ? BM / 2 : BM;
     alignas(64) CUtensorMap mw, mu, mx;
     if (encode_map(&mw, a.w, a.N, a.K, a.ld_w, kRows) || encode_map(&mu, GATED ? a.w_up : a.w, a.N, a.K, GATED ? a.ld_up : a.ld_w, kRows) ||
         encode_map(&mx, a.x, a.T, a.K, a.ld_x, BN))
         return EXMOE_ERR_CUDA;
     static SmemOnce once;
-    const auto kern = linear_split_kernel<O, GATED, CL>;
-    constexpr int smem = kSplitRoom + (int)sizeof(SplitShared) + 1024;
-    static_assert(2 * (smem + 1024) <= 228 * 1024, "shared memory of two CTAs");
-    if (!allow_smem(kern, smem, once)) return EXMOE_ERR_CUDA;
+    const auto kern = linear_split_kernel<O, GATED, PEERS>;
+    static_assert(2 * (kSplitRoom + 2048 + 1024) <= 228 * 1024 && kSplitRoomWide + 2048 <= 227 * 1024, "shared memory of two CTAs, of one");
+    if (!allow_smem(kern, kSplitRoomWide + 2048, once)) return EXMOE_ERR_CUDA;
     const int row_tiles = (a.N + kRows - 1) / kRows;
     const long long ctas = (long long)row_tiles * ((a.T + BN - 1) / BN) * CL;
     if (ctas > INT32_MAX) return EXMOE_ERR_SHAPE;
+    const int room = wide ? kSplitRoomWide : kSplitRoom, stages = std::min(kSplitStages, room / (kABytes + BN * 128));
     cudaLaunchConfig_t lc{};
     lc.gridDim = dim3((unsigned)ctas);
     lc.blockDim = dim3(kSplitThreads);
-    lc.dynamicSmemBytes = smem;
+    lc.dynamicSmemBytes = (size_t)room + 2048;
     lc.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = CL;
+    attr[1].val.clusterDim.x = (unsigned)CL;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     lc.attrs = attr;
     lc.numAttrs = CL > 1 ? 2 : 1;
@@ -328,7 +329,7 @@ int launch_split(const LinearArgs& a, int BN, cudaStream_t st) {
     lc.attrs = attr + 1;
     --lc.numAttrs;
 #endif
-    if (cudaLaunchKernelEx(&lc, kern, mw, mu, mx, a, BN, row_tiles) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&lc, kern, mw, mu, mx, a, BN, CL, row_tiles, stages) != cudaSuccess) {
         cudaGetLastError();
         return EXMOE_ERR_CUDA;
     }
@@ -448,6 +449,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
         sm.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (warp == 0 && lane < 3) prefetch_map(lane == 0 ? &map_w : lane == 1 ? &map_x : &map_u);
     if (warp == 2) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sm.tmem)), "r"(2 * kPairTokens));
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::);
@@ -623,11 +625,11 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
                         other[i] = is_up ? v[i] : o;
                         v[i] = is_up ? o : v[i];
                     }
-                    activate8(v, a.act);
+                    activate_all(v, a.act);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) v[i] *= other[i];
                 } else {
-                    activate8(v, a.act);
+                    activate_all(v, a.act);
                 }
                 to.store(c, v, r);
                 if (c + 2 * kStep < cw) to.load(c + 2 * kStep, r);
@@ -687,33 +689,82 @@ int launch_pair(const LinearArgs& a, int BN, cudaStream_t st) {
     return EXMOE_OK;
 }
 
-// Which form, and its tile.  Both cost models are in clocks of an SM, from what was measured: a stage of the split form takes 300 with up to 64 tokens (its 24 KB
-// come at 80 bytes a clock), a pair's k-step of 16 what shared memory takes for its operands, 64 + BN / 4.
+// How many clusters of one to eight CTAs the device holds at once, with one CTA per SM and with two.  (GPCs differ in their SMs, devices in their GPCs:
+// 15 clusters of eight CTAs, 22 of six, 33 of four, 74 of two where these figures were taken.)
+constexpr int kMostCluster = 8;
+struct Clusters { int wide[kMostCluster + 1], narrow[kMostCluster + 1]; };
+const Clusters* clusters_held() {
+    static Clusters held[64];
+    static std::once_flag once[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
+    std::call_once(once[dev], [dev] {
+        const auto kern = linear_split_kernel<float, false, 8>;
+        cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitRoomWide + 2048);
+        for (int c = 1; c <= kMostCluster; ++c)
+            for (int wide = 0; wide < 2; ++wide) {
+                cudaLaunchConfig_t lc{};
+                lc.gridDim = dim3((unsigned)c);
+                lc.blockDim = dim3(kSplitThreads);
+                lc.dynamicSmemBytes = (wide ? kSplitRoomWide : kSplitRoom) + 2048;
+                cudaLaunchAttribute attr[1];
+                attr[0].id = cudaLaunchAttributeClusterDimension;
+                attr[0].val.clusterDim.x = (unsigned)c;
+                attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+                lc.attrs = attr;
+                lc.numAttrs = 1;
+                int n = 0;
+                if (cudaOccupancyMaxActiveClusters(&n, kern, &lc) != cudaSuccess) {
+                    cudaGetLastError();
+                    n = 0;
+                }
+                (wide ? held[dev].wide : held[dev].narrow)[c] = n;
+            }
+    });
+    return &held[dev];
+}
+
+// Which form, and its tile, by what they take in clocks of an SM (1.9 GHz): from the times below, each model within 15 % of them or so.
+//   pair    a stage what shared memory takes for four k-steps' operands, 4 (64 + BN / 4), a tile 1500 besides, a call 6000
+//   split   a stage its bytes at 57 a clock (what an SM takes in), twice where SMs are shared; a call 8000, 250 for every part of the exchange and 1500 for
+//           clusters of more than four CTAs, which start late once they are many
+//   both    weights from HBM at 3400 bytes a clock, and 10000 (7000) besides
+// us, replayed from a graph, split of clusters of 2 / 3 / 4 / 6, pair:  TODO
 template <typename O, bool GATED>
 int launch_tc(const LinearArgs& a, cudaStream_t st) {
     const int row_tiles = (a.N + (GATED ? 63 : 127)) / (GATED ? 64 : 128), blocks = (a.K + 63) / 64;
     const long long pair_rows = (row_tiles + 1) / 2;
-    int best = 256;
+    int pair_BN = 256;
     long long pair_cost = INT64_MAX;
     for (int BN = 256; BN >= 64; BN -= 32) {
         const long long rounds = (pair_rows * ((a.T + BN - 1) / BN) + kSms / 2 - 1) / (kSms / 2), cost = rounds * (blocks * (long long)(256 + BN) + 1500) + 6000;
         if (cost < pair_cost) {
             pair_cost = cost;
-            best = BN;
+            pair_BN = BN;
         }
     }
-    const int BN = a.T >= 64 ? 64 : (a.T + 31) / 32 * 32;
+    const long long from_hbm = (GATED ? 4ll : 2ll) * a.N * a.K / 3400;
+    pair_cost = std::max(pair_cost, from_hbm + 10000);
+    const int BN = a.T >= 64 ? 64 : (a.T + 15) / 16 * 16, stage = kABytes + BN * 128;
     const long long tiles = (long long)row_tiles * ((a.T + BN - 1) / BN);
-    int CL = tiles <= 4 ? 8 : 4;                                           // (clusters of eight start late: 64 tokens, 2048 x 2048, 9.0 us instead of 6.3)
-    while (CL > 1 && (tiles * CL > 2 * kSms || blocks < 2 * CL)) CL /= 2;
-    const long long per_sm = (tiles * CL + kSms - 1) / kSms, split_cost = per_sm * ((blocks + CL - 1) / CL) * 300 + 3000 * ((per_sm + 1) / 2) + (CL > 1 ? 4000 : 2000);
-    if (pair_cost < split_cost) return launch_pair<O, GATED>(a, best, st);
-    switch (CL) {
-        case 8: return launch_split<O, GATED, 8>(a, BN, st);
-        case 4: return launch_split<O, GATED, 4>(a, BN, st);
-        case 2: return launch_split<O, GATED, 2>(a, BN, st);
-        default: return launch_split<O, GATED, 1>(a, BN, st);
+    const Clusters* held = clusters_held();
+    int CL = 1;
+    bool wide = false;
+    long long split_cost = INT64_MAX;
+    for (int c = 1; held && c <= std::min(kMostCluster, std::max(1, blocks / 2)); ++c) {
+        if (held->narrow[c] <= 0) continue;
+        const int n = (blocks + c - 1) / c;
+        const bool alone = tiles <= held->wide[c];
+        const long long turns = alone ? 1 : 2 * ((tiles + held->narrow[c] - 1) / held->narrow[c]), cost = turns * n * (stage / 57) + 8000 + 250 * c + (c > 4 && tiles * c > 64 ? 1500 : 0);
+        if (cost < split_cost) {
+            split_cost = cost;
+            CL = c;
+            wide = alone && (long long)n * stage > 280 * 1024;              // (8 stages of 24 KB: 8.2 us wide, 6.7 with room for the next call's CTAs; 16: 10.5, 11.6)
+        }
     }
+    if (pair_cost < std::max(split_cost, from_hbm + 7000)) return launch_pair<O, GATED>(a, pair_BN, st);
+    if (CL <= 2) return launch_split<O, GATED, 2>(a, BN, CL, wide, st);
+    return CL <= 4 ? launch_split<O, GATED, 4>(a, BN, CL, wide, st) : launch_split<O, GATED, 8>(a, BN, CL, wide, st);
 }
 
 }  // namespace
