@@ -190,6 +190,10 @@ __device__ __forceinline__ double cta_sum(double v, double* room) {
     return v;
 }
 
+struct Open { int tile, last, s; };                                       // a sequence, its first and last tile
+constexpr int kMostTiles = 8 * kSms;
+constexpr size_t join_smem(int threads) { return (size_t)(threads / 32) * (32 * 8 + 4) + 16 + 2 * kMostTiles * sizeof(Open); }
+
 // Second step: the sequences that tiles share, and the losses.  By the CTAs of one cluster.
 __device__ void join_tiles(const BalanceArgs& a, int cta, int ctas, unsigned char* smem) {
     __shared__ double room[32];
@@ -197,11 +201,36 @@ __device__ void join_tiles(const BalanceArgs& a, int cta, int ctas, unsigned cha
     float* red_sum = reinterpret_cast<float*>(smem);                       // [warps][32]
     int32_t* red_count = reinterpret_cast<int32_t*>(red_sum + 32 * warps); // [warps][32]
     int32_t* red_kept = red_count + 32 * warps;                            // [warps]
+    Open* open = reinterpret_cast<Open*>(red_kept + ((warps + 3) & ~3));   // [kMostTiles]
+    Open* ordered = open + kMostTiles;                                     // [kMostTiles]
     constexpr int kFew = 16;                                               // tiles of a sequence that one warp adds up
     const int chunks = (a.E + 31) / 32;
     double loss = 0.0;
     int some = 0, bad = 0;
-    auto last_tile = [&](int s) { return (min(max(a.offsets ? __ldcg(a.offsets + s + 1) : a.T, 1), a.T) - 1) / a.rows; };
+    // the sequences that go on behind the tile they begin in: few, and those over many tiles
+    __shared__ int n_open, n_long;
+    if (tid == 0) n_open = n_long = 0;
+    __syncthreads();
+    for (int tile = tid; tile < a.tiles; tile += threads) {
+        const int s = __ldcg(a.tile_open + tile);
+        if (s < 0) continue;
+        const int last = (min(max(a.offsets ? __ldcg(a.offsets + s + 1) : a.T, 1), a.T) - 1) / a.rows;
+        const bool far = last - tile >= kFew;
+        const int at = far ? kMostTiles - 1 - atomicAdd(&n_long, 1) : atomicAdd(&n_open, 1);
+        open[at] = Open{tile, last, s};
+    }
+    __syncthreads();
+    // (in the order of their tiles, so that every call adds up alike)
+    const auto in_order = [&](Open* list, int n) {
+        for (int i = tid; i < n; i += threads) {
+            int before = 0;
+            for (int j = 0; j < n; ++j) before += list[j].tile < list[i].tile;
+            ordered[(int)(list - open) + before] = list[i];
+        }
+    };
+    in_order(open, n_open);
+    in_order(open + kMostTiles - n_long, n_long);
+    __syncthreads();
     auto finish = [&](int s, int c, float sum, int count, int n) {         // by one warp
         const int e = 32 * c + lane;
         if (e < a.E) {
@@ -214,41 +243,31 @@ __device__ void join_tiles(const BalanceArgs& a, int cta, int ctas, unsigned cha
             some += n > 0;
         }
     };
-    for (int i = cta * warps + warp; i < a.tiles * chunks; i += ctas * warps) {     // sequences over few tiles: a warp per 32 experts
-        const int tile = i / chunks, c = i % chunks, s = __ldcg(a.tile_open + tile);
-        if (s < 0) continue;
-        const int last = last_tile(s);
-        if (last - tile >= kFew) continue;
+    const auto add_tiles = [&](const Open& o, int c, int first, int step, float& sum, int& count, int& n) {
         const int e = min(32 * c + lane, a.E - 1);
-        float sum = 0.f;
-        int count = 0, n = 0;
-#pragma unroll 4
-        for (int t = tile; t <= last; ++t) {
-            const size_t at = 2 * (size_t)t + (t == tile);
-            sum += __ldcg(a.part_sums + at * a.E + e);
-            count += __ldcg(a.part_counts + at * a.E + e);
-            n += __ldcg(a.part_kept + at);
-        }
-        finish(s, c, sum, count, n);
-    }
-    for (int i = cta; i < a.tiles * chunks; i += ctas) {                   // over many: the CTA's warps share its tiles
-        const int tile = i / chunks, c = i % chunks, s = __ldcg(a.tile_open + tile);
-        if (s < 0) {
-            i += (chunks - 1 - c) / ctas * ctas;                           // on to the next tile
-            continue;
-        }
-        const int last = last_tile(s);
-        if (last - tile < kFew) continue;
-        const int e = min(32 * c + lane, a.E - 1);
-        float sum = 0.f;
-        int count = 0, n = 0;
+        sum = 0.f;
+        count = n = 0;
 #pragma unroll 8
-        for (int t = tile + warp; t <= last; t += warps) {
-            const size_t at = 2 * (size_t)t + (t == tile);
+        for (int t = o.tile + first; t <= o.last; t += step) {
+            const size_t at = 2 * (size_t)t + (t == o.tile);
             sum += __ldcg(a.part_sums + at * a.E + e);
             count += __ldcg(a.part_counts + at * a.E + e);
             n += __ldcg(a.part_kept + at);
         }
+    };
+    for (int i = cta * warps + warp; i < n_open * chunks; i += ctas * warps) {     // over few tiles: a warp per 32 experts
+        const Open o = ordered[i / chunks];
+        float sum;
+        int count, n;
+        add_tiles(o, i % chunks, 0, 1, sum, count, n);
+        finish(o.s, i % chunks, sum, count, n);
+    }
+    for (int i = cta; i < n_long * chunks; i += ctas) {                    // over many: the CTA's warps share its tiles
+        const Open o = ordered[kMostTiles - n_long + i / chunks];
+        const int c = i % chunks;
+        float sum;
+        int count, n;
+        add_tiles(o, c, warp, warps, sum, count, n);
         red_sum[32 * warp + lane] = sum;
         red_count[32 * warp + lane] = count;
         if (lane == 0) red_kept[warp] = n;
@@ -259,7 +278,7 @@ __device__ void join_tiles(const BalanceArgs& a, int cta, int ctas, unsigned cha
                 count += red_count[32 * w + lane];
                 n += red_kept[w];
             }
-            finish(s, c, sum, count, n);
+            finish(o.s, c, sum, count, n);
         }
         __syncthreads();
     }
@@ -303,7 +322,7 @@ __device__ void join_tiles(const BalanceArgs& a, int cta, int ctas, unsigned cha
 
 __global__ void __launch_bounds__(kJoinThreads)
 balance_join_kernel(const __grid_constant__ BalanceArgs a) {
-    __shared__ __align__(16) unsigned char smem[(kJoinThreads / 32) * (32 * 8 + 4)];
+    extern __shared__ __align__(16) unsigned char smem[];
     grid_dependency_wait();
     grid_launch_dependents();
     join_tiles(a, (int)blockIdx.x, (int)gridDim.x, smem);
@@ -679,12 +698,12 @@ size_t scratch_bytes(int E, const Tiling& t) {
 template <typename Z, int W, int L, int V>
 int launch_balance(const BalanceArgs& a, bool fused, cudaStream_t st) {
     static SmemOnce once[2];
-    constexpr size_t smem = std::max(balance_smem<L, V>(), (size_t)(Team<L>::kWarps) * (32 * 8 + 4));
-    if (fused) return launch(balance_kernel<Z, W, L, V, true>, (unsigned)a.tiles, Team<L>::kThreads, a.tiles, smem, once[0], st, a);
+    constexpr size_t smem = balance_smem<L, V>(), fused_smem = std::max(smem, join_smem(Team<L>::kThreads));
+    if (fused) return launch(balance_kernel<Z, W, L, V, true>, (unsigned)a.tiles, Team<L>::kThreads, a.tiles, fused_smem, once[0], st, a);
     const int rc = launch(balance_kernel<Z, W, L, V, false>, (unsigned)a.tiles, Team<L>::kThreads, 1, smem, once[1], st, a);
     if (rc) return rc;
     static SmemOnce join;
-    return launch(balance_join_kernel, kJoinCtas, kJoinThreads, kJoinCtas, 0, join, st, a);
+    return launch(balance_join_kernel, kJoinCtas, kJoinThreads, kJoinCtas, join_smem(kJoinThreads), join, st, a);
 }
 template <typename Z, int W>
 int launch_balance(const BalanceArgs& a, bool fused, cudaStream_t st) {
