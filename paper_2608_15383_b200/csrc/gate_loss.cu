@@ -28,47 +28,41 @@ template <> __device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat
 
 // A team of L lanes per row, each with V experts in runs of W: expert (j L + lane) W + i.  Up to 32 lanes they are (part of) a warp, beyond
 // that the whole CTA.
+constexpr int kMostSums = 5;
 template <int L>
 struct Team {
     static constexpr bool kCta = L > 32;
     static constexpr int kThreads = kCta ? L : 512, kWarps = kThreads / 32, kTeams = kThreads / L;
     int lane, index;                   // in the team; of the team in its CTA
-    float* room;                       // [2 kWarps], for teams of several warps
+    float* room;                       // [kMostSums kWarps], for teams of several warps
     __device__ Team(float* r) : lane((int)threadIdx.x % L), index((int)threadIdx.x / L), room(r) {}
     __device__ __forceinline__ void sync() const {
         if constexpr (kCta) __syncthreads();
         else __syncwarp();
     }
-    __device__ __forceinline__ float max(float v) const {
+    // the largest / the sum over the team of each of N values, in one go
+    template <int N>
+    __device__ __forceinline__ void max(float (&v)[N]) const { reduce(v, [](float a, float b) { return fmaxf(a, b); }, -INFINITY); }
+    template <int N>
+    __device__ __forceinline__ void sum(float (&v)[N]) const { reduce(v, [](float a, float b) { return a + b; }, 0.f); }
+    template <int N, typename F>
+    __device__ __forceinline__ void reduce(float (&v)[N], F f, float none) const {
+        static_assert(N <= kMostSums, "room");
 #pragma unroll
-        for (int m = (kCta ? 32 : L) / 2; m >= 1; m >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, m));
+        for (int m = (kCta ? 32 : L) / 2; m >= 1; m >>= 1)
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = f(v[i], __shfl_xor_sync(0xffffffffu, v[i], m));
         if constexpr (kCta) {
             __syncthreads();
-            if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = v;
+            if ((threadIdx.x & 31) == 0)
+#pragma unroll
+                for (int i = 0; i < N; ++i) room[i * kWarps + (threadIdx.x >> 5)] = v[i];
             __syncthreads();
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) v = fmaxf(v, room[w]);
-        }
-        return v;
-    }
-    __device__ __forceinline__ void sum2(float& a, float& b) const {
+            for (int i = 0; i < N; ++i) {
+                v[i] = none;
 #pragma unroll
-        for (int m = (kCta ? 32 : L) / 2; m >= 1; m >>= 1) {
-            a += __shfl_xor_sync(0xffffffffu, a, m);
-            b += __shfl_xor_sync(0xffffffffu, b, m);
-        }
-        if constexpr (kCta) {
-            __syncthreads();
-            if ((threadIdx.x & 31) == 0) {
-                room[threadIdx.x >> 5] = a;
-                room[kWarps + (threadIdx.x >> 5)] = b;
-            }
-            __syncthreads();
-            a = b = 0.f;
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                a += room[w];
-                b += room[kWarps + w];
+                for (int w = 0; w < kWarps; ++w) v[i] = f(v[i], room[i * kWarps + w]);
             }
         }
     }
@@ -120,16 +114,23 @@ __device__ __forceinline__ void store_row(Z* row, int E, int lane, const float (
     }
 }
 
+// exp(x) for x <= 0 by the hardware's 2^x: off by 2 units of 2^-23 and by the product's rounding, |x| 2^-24 (which with that of the difference that x is
+// is what a score far below the largest is off by; the function with the exact argument takes three times the instructions, which
+// would bound these kernels).  Results below 2^-126 are 0.
+__device__ __forceinline__ float exp_below(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * 1.4426950408889634f));
+    return y;
+}
 // A sigmoid times exp(-c) (see the top; c <= 0), and 1 - sigmoid.
 __device__ __forceinline__ float scaled_sigmoid(float z, float c, float& rest) {
-    const float u = expf(-fabsf(z)), inv = __fdividef(1.f, 1.f + u);
-    rest = z >= 0.f ? u * inv : inv;
-    if (z != z) rest = z;
-    return (c < 0.f ? expf(z - c) : z >= 0.f ? 1.f : u) * inv;
+    const float u = exp_below(-fabsf(z)), inv = __fdividef(1.f, 1.f + u), small = u * inv;
+    rest = z < 0.f ? inv : small;                                          // (NaN: both are)
+    return c < 0.f ? exp_below(z - c) * inv : z < 0.f ? small : inv;
 }
 // The logarithm of a row's sum of exponentials; 0 for a row without any expert left.
-__device__ __forceinline__ float log_sum(float base, float sum) { return sum == 0.f ? 0.f : base + logf(sum); }
-__device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : 1.f / sum; }
+__device__ __forceinline__ float log_sum(float base, float sum) { return sum == 0.f ? 0.f : base + __logf(sum); }
+__device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : __fdividef(1.f, sum); }
 
 // The first sequence that ends at t or behind it, by a warp: offsets [S + 1] ascend.  Whatever they hold, the answer is in [0, S].
 __device__ __forceinline__ int first_ending_at(const int32_t* offsets, int S, int t, int lane) {
@@ -169,74 +170,101 @@ struct BalanceArgs {
     int32_t* part_kept;                // [tiles][2]
     int32_t *tile_kept, *tile_some;    // [tiles] tokens that count; its sequences that have any
     int32_t* tile_open;                // [tiles] the sequence that begins in it and goes on behind it, or -1
-    int32_t* joined_some;              // [2 kJoinCtas]
 };
 
-__device__ __forceinline__ double loss_factor(int E, int k, int n) { return n ? (double)E / ((double)k * n * n) : 0.0; }
+__device__ __forceinline__ float loss_factor(int E, int k, int n) { return n ? (float)E / ((float)k * (float)n * (float)n) : 0.f; }
 
 __device__ __forceinline__ void cluster_sync() {
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-// The sum of a value over the CTA, for thread 0, in a fixed order.
-__device__ __forceinline__ double cta_sum(double v, double* room) {
-    v = warp_sum_f64(v);
+// Sums of N values over the CTA, for thread 0, in a fixed order.
+template <int N, int THREADS>
+__device__ __forceinline__ void cta_sums(double (&v)[N]) {
+    constexpr int WARPS = THREADS / 32;
+    __shared__ double room[N][WARPS];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = warp_sum_f64(v[i]);
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = v;
+    if (lane == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) room[i][warp] = v[i];
     __syncthreads();
-    if (threadIdx.x == 0)
-        for (int w = 1; w < (int)blockDim.x >> 5; ++w) v += room[w];
-    return v;
+    if (warp == 0)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = warp_sum_f64(lane < WARPS ? room[i][lane] : 0.0);
 }
 
-struct Open { int tile, last, s; };                                       // a sequence, its first and last tile
+struct Open { int tile, last, s; };                                       // a sequence that goes on behind the tile it begins in, and its last tile
 constexpr int kMostTiles = 8 * kSms;
-constexpr size_t join_smem(int threads) { return (size_t)(threads / 32) * (32 * 8 + 4) + 16 + 2 * kMostTiles * sizeof(Open); }
+constexpr size_t join_smem(int threads) { return (size_t)(threads / 32) * (32 * 8 + 4) + kMostTiles * sizeof(Open); }
+
+__device__ __forceinline__ bool ascends(const BalanceArgs& a, int first, int step) {
+    bool ok = true;
+    if (a.offsets)
+        for (int s = first; s < a.S; s += step) {
+            const int from = __ldcg(a.offsets + s), to = __ldcg(a.offsets + s + 1);
+            ok = ok && from >= 0 && from <= to && to <= a.T;
+        }
+    return ok;
+}
+__device__ __forceinline__ void write_losses(const BalanceArgs& a, double balance, double some, double squares, double n, bool wrong) {
+    a.losses[0] = wrong ? NAN : some > 0 ? (float)(balance / some) : 0.f;
+    a.losses[1] = wrong ? NAN : n > 0 ? (float)(squares / n) : 0.f;
+}
 
 // Second step: the sequences that tiles share, and the losses.  By the CTAs of one cluster.
-__device__ void join_tiles(const BalanceArgs& a, int cta, int ctas, unsigned char* smem) {
-    __shared__ double room[32];
-    const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31, warp = tid >> 5, warps = threads >> 5;
-    float* red_sum = reinterpret_cast<float*>(smem);                       // [warps][32]
-    int32_t* red_count = reinterpret_cast<int32_t*>(red_sum + 32 * warps); // [warps][32]
-    int32_t* red_kept = red_count + 32 * warps;                            // [warps]
-    Open* open = reinterpret_cast<Open*>(red_kept + ((warps + 3) & ~3));   // [kMostTiles]
-    Open* ordered = open + kMostTiles;                                     // [kMostTiles]
-    constexpr int kFew = 16;                                               // tiles of a sequence that one warp adds up
+template <int THREADS>
+__device__ __forceinline__ void join_tiles(const BalanceArgs& a, int cta, int ctas, unsigned char* smem) {
+    constexpr int WARPS = THREADS / 32;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    float* red_sum = reinterpret_cast<float*>(smem);                       // [WARPS][32]
+    int32_t* red_count = reinterpret_cast<int32_t*>(red_sum + 32 * WARPS); // [WARPS][32]
+    int32_t* red_kept = red_count + 32 * WARPS;                            // [WARPS]
+    Open* open = reinterpret_cast<Open*>(red_kept + WARPS);                // [kMostTiles], in the order of their tiles
+    __shared__ int before[WARPS + 1];
     const int chunks = (a.E + 31) / 32;
-    double loss = 0.0;
-    int some = 0, bad = 0;
-    // the sequences that go on behind the tile they begin in: few, and those over many tiles
-    __shared__ int n_open, n_long;
-    if (tid == 0) n_open = n_long = 0;
-    __syncthreads();
-    for (int tile = tid; tile < a.tiles; tile += threads) {
-        const int s = __ldcg(a.tile_open + tile);
-        if (s < 0) continue;
-        const int last = (min(max(a.offsets ? __ldcg(a.offsets + s + 1) : a.T, 1), a.T) - 1) / a.rows;
-        const bool far = last - tile >= kFew;
-        const int at = far ? kMostTiles - 1 - atomicAdd(&n_long, 1) : atomicAdd(&n_open, 1);
-        open[at] = Open{tile, last, s};
-    }
-    __syncthreads();
-    // (in the order of their tiles, so that every call adds up alike)
-    const auto in_order = [&](Open* list, int n) {
-        for (int i = tid; i < n; i += threads) {
-            int before = 0;
-            for (int j = 0; j < n; ++j) before += list[j].tile < list[i].tile;
-            ordered[(int)(list - open) + before] = list[i];
+    // what the tiles have found of the losses, on its way while the rest is added up: by the first CTA
+    double z = 0.0, n_all = 0.0, loss = 0.0, some = 0.0;
+    if (cta == 0)
+        for (int t = tid; t < a.tiles; t += THREADS) {
+            loss += __ldcg(a.tile_loss + t);
+            z += __ldcg(a.tile_z + t);
+            n_all += (double)__ldcg(a.tile_kept + t);
+            some += (double)__ldcg(a.tile_some + t);
         }
-    };
-    in_order(open, n_open);
-    in_order(open + kMostTiles - n_long, n_long);
-    __syncthreads();
-    auto finish = [&](int s, int c, float sum, int count, int n) {         // by one warp
+    int n_open = 0;
+    if (!a.offsets) {
+        const int last = (max(a.T, 1) - 1) / a.rows;                       // (a cluster may have tiles behind it, without tokens)
+        n_open = last > 0;
+        if (tid == 0) open[0] = Open{0, last, 0};
+        __syncthreads();
+    } else {
+        for (int t0 = 0; t0 < a.tiles; t0 += THREADS) {
+            const int t = t0 + tid, s = t < a.tiles ? __ldcg(a.tile_open + t) : -1;
+            const unsigned mine = __ballot_sync(0xffffffffu, s >= 0);
+            __syncthreads();
+            if (lane == 0) before[warp + 1] = __popc(mine);
+            __syncthreads();
+            int at = n_open + __popc(mine & ((1u << lane) - 1u)), all = 0;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                if (w < warp) at += before[w + 1];
+                all += before[w + 1];
+            }
+            if (s >= 0) open[at] = Open{t, (min(max(__ldcg(a.offsets + s + 1), 1), a.T) - 1) / a.rows, s};
+            n_open += all;
+        }
+        __syncthreads();
+    }
+    const auto finish = [&](int s, int c, float sum, int count, int n) {   // by one warp
         const int e = 32 * c + lane;
         if (e < a.E) {
             a.sums[(size_t)s * a.E + e] = sum;
             a.counts[(size_t)s * a.E + e] = count;
-            loss += (double)count * (double)sum * loss_factor(a.E, a.k, n);
+            loss += (double)((float)count * loss_factor(a.E, a.k, n)) * (double)sum;
         }
         if (c == 0 && lane == 0) {
             a.kept[s] = n;
@@ -255,69 +283,51 @@ __device__ void join_tiles(const BalanceArgs& a, int cta, int ctas, unsigned cha
             n += __ldcg(a.part_kept + at);
         }
     };
-    for (int i = cta * warps + warp; i < n_open * chunks; i += ctas * warps) {     // over few tiles: a warp per 32 experts
-        const Open o = ordered[i / chunks];
+    // A warp per 32 experts of a sequence; where there are few of these, or the sequence covers many tiles, a CTA's warps share its tiles.
+    const int far = n_open * chunks >= 64 ? 64 : 4;
+    for (int i = cta * WARPS + warp; i < n_open * chunks; i += ctas * WARPS) {
+        const Open o = open[i / chunks];
+        if (o.last - o.tile >= far) continue;
         float sum;
         int count, n;
         add_tiles(o, i % chunks, 0, 1, sum, count, n);
         finish(o.s, i % chunks, sum, count, n);
     }
-    for (int i = cta; i < n_long * chunks; i += ctas) {                    // over many: the CTA's warps share its tiles
-        const Open o = ordered[kMostTiles - n_long + i / chunks];
-        const int c = i % chunks;
+    for (int i = cta; i < n_open * chunks; i += ctas) {
+        const Open o = open[i / chunks];
+        if (o.last - o.tile < far) continue;
         float sum;
         int count, n;
-        add_tiles(o, c, warp, warps, sum, count, n);
+        add_tiles(o, i % chunks, warp, WARPS, sum, count, n);
         red_sum[32 * warp + lane] = sum;
         red_count[32 * warp + lane] = count;
         if (lane == 0) red_kept[warp] = n;
         __syncthreads();
         if (warp == 0) {
-            for (int w = 1; w < warps; ++w) {
+#pragma unroll
+            for (int w = 1; w < WARPS; ++w) {
                 sum += red_sum[32 * w + lane];
                 count += red_count[32 * w + lane];
                 n += red_kept[w];
             }
-            finish(o.s, c, sum, count, n);
+            finish(o.s, i % chunks, sum, count, n);
         }
         __syncthreads();
     }
-    if (a.offsets)
-        for (int s = cta * threads + tid; s < a.S; s += ctas * threads) {
-            const int from = __ldcg(a.offsets + s), to = __ldcg(a.offsets + s + 1);
-            bad |= from < 0 || from > to || to > a.T;
-        }
-    bad = __syncthreads_or(bad);
-    loss = cta_sum(loss, room);
-    const double all_some = cta_sum((double)some, room);
+    const bool bad = __syncthreads_or(!ascends(a, cta * THREADS + tid, ctas * THREADS));
+    double v[4] = {loss, some, z, n_all};
+    cta_sums<4, THREADS>(v);
     if (tid == 0) {
-        __stcg(a.joined + cta, loss);
-        __stcg(a.joined_some + cta, (int)all_some);
-        __stcg(a.joined_some + kJoinCtas + cta, bad);
+        __stcg(a.joined + cta, v[0]);
+        __stcg(a.joined + kJoinCtas + cta, bad ? -1.0 : v[1]);
     }
     cluster_sync();
-    if (cta) return;
-    double z = 0.0, n = 0.0, in_tiles = 0.0, n_seq = 0.0;
-    for (int t = tid; t < a.tiles; t += threads) {
-        in_tiles += __ldcg(a.tile_loss + t);
-        z += __ldcg(a.tile_z + t);
-        n += (double)__ldcg(a.tile_kept + t);
-        n_seq += (double)__ldcg(a.tile_some + t);
-    }
-    in_tiles = cta_sum(in_tiles, room);
-    z = cta_sum(z, room);
-    n = cta_sum(n, room);
-    n_seq = cta_sum(n_seq, room);
-    if (tid == 0) {
-        int wrong = 0;
-        for (int c = 0; c < ctas; ++c) {
-            in_tiles += __ldcg(a.joined + c);
-            n_seq += (double)__ldcg(a.joined_some + c);
-            wrong |= __ldcg(a.joined_some + kJoinCtas + c);
-        }
-        a.losses[0] = wrong ? NAN : n_seq > 0 ? (float)(in_tiles / n_seq) : 0.f;
-        a.losses[1] = wrong ? NAN : n > 0 ? (float)(z / n) : 0.f;
-    }
+    if (cta || warp) return;
+    double balance = lane < ctas ? __ldcg(a.joined + lane) : 0.0, n_seq = lane < ctas ? __ldcg(a.joined + kJoinCtas + lane) : 0.0;
+    const bool wrong = __any_sync(0xffffffffu, n_seq < 0.0);
+    balance = warp_sum_f64(balance);
+    n_seq = warp_sum_f64(n_seq);
+    if (lane == 0) write_losses(a, balance, n_seq, v[2], v[3], wrong);
 }
 
 __global__ void __launch_bounds__(kJoinThreads)
@@ -325,7 +335,7 @@ balance_join_kernel(const __grid_constant__ BalanceArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
     grid_dependency_wait();
     grid_launch_dependents();
-    join_tiles(a, (int)blockIdx.x, (int)gridDim.x, smem);
+    join_tiles<kJoinThreads>(a, (int)blockIdx.x, (int)gridDim.x, smem);
 }
 
 template <int L, int V>
@@ -339,8 +349,7 @@ balance_kernel(const __grid_constant__ BalanceArgs a) {
     extern __shared__ __align__(16) unsigned char smem[];
     float* red = reinterpret_cast<float*>(smem);                           // [warp][L V] column sums
     int32_t* hist = reinterpret_cast<int32_t*>(red + (TM::kCta ? 1 : TM::kWarps) * L * V);   // [L V]
-    __shared__ float room[2 * TM::kWarps];
-    __shared__ double room64[32];
+    __shared__ float room[kMostSums * TM::kWarps];
     __shared__ int32_t window[kWindow + 1];
     __shared__ int n_kept;
     const TM team(room);
@@ -375,51 +384,77 @@ balance_kernel(const __grid_constant__ BalanceArgs a) {
 #pragma unroll
         for (int j = 0; j < V; ++j) acc[j] = 0.f;
         int mine = 0;
-        for (long long base = (long long)lo + (TM::kCta ? 0 : warp * (32 / L)); base < hi; base += TM::kTeams) {
-            const long long t = base + (TM::kCta ? 0 : lane / L);
-            const bool on = t < hi && (!a.mask || a.mask[t]);
-            if constexpr (TM::kCta) {
-                if (!on) continue;
-            }
-            float v[V];
-            if (on) {
-                load_row<Z, W, L, V>(z + t * a.ld, E, team.lane, v);
-                for (int j = team.lane; j < k; j += L) {
-                    const int id = a.ids[t * k + j];
-                    if ((unsigned)id < (unsigned)E) atomicAdd(hist + id, 1);
-                }
-                mine += team.lane == 0;
+        // a row's logits and first ids are requested before the row before it is worked on
+        const int lane_row = TM::kCta ? 0 : lane / L;
+        const long long first = (long long)lo + (TM::kCta ? 0 : warp * (32 / L));
+        float v[V];
+        int id = -1;
+        bool on = false;
+        const auto request = [&](long long t, float (&to)[V], int& to_id) {
+            const bool counts = t < hi && (!a.mask || a.mask[t]);
+            if (counts) {
+                load_row<Z, W, L, V>(z + t * a.ld, E, team.lane, to);
+                to_id = team.lane < k ? a.ids[t * k + team.lane] : -1;
             } else {
 #pragma unroll
-                for (int j = 0; j < V; ++j) v[j] = -INFINITY;
+                for (int j = 0; j < V; ++j) to[j] = -INFINITY;
+                to_id = -1;
             }
-            float mx = v[0];
+            return counts;
+        };
+        if (first < hi) on = request(first + lane_row, v, id);
+        for (long long base = first; base < hi; base += TM::kTeams) {
+            float next[V];
+            int next_id = -1;
+            bool next_on = false;
+            if (base + TM::kTeams < hi) next_on = request(base + TM::kTeams + lane_row, next, next_id);
+            if ((unsigned)id < (unsigned)E) atomicAdd(hist + id, 1);
+            if (on && k > L)
+                for (int j = team.lane + L; j < k; j += L) {
+                    const int more = a.ids[(base + lane_row) * k + j];
+                    if ((unsigned)more < (unsigned)E) atomicAdd(hist + more, 1);
+                }
+            mine += on && team.lane == 0;
+            float mx[1] = {v[0]};
 #pragma unroll
-            for (int j = 1; j < V; ++j) mx = fmaxf(mx, v[j]);
-            mx = team.max(mx);
-            const float top = mx == -INFINITY ? 0.f : mx;
-            float sum = 0.f, scores = 0.f;
+            for (int j = 1; j < V; ++j) mx[0] = fmaxf(mx[0], v[j]);
+            team.max(mx);
+            const float top = mx[0] == -INFINITY ? 0.f : mx[0];
+            float sum = 0.f, inv;
             if (a.sigmoid) {
                 const float c = fminf(top, 0.f);
+                float s2[2] = {0.f, 0.f};
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
                     float rest;
-                    sum += expf(v[j] - top);
+                    s2[0] += exp_below(v[j] - top);
                     v[j] = scaled_sigmoid(v[j], c, rest);
-                    scores += v[j];
+                    s2[1] += v[j];
                 }
+                team.sum(s2);
+                sum = s2[0];
+                inv = inverse(s2[1]);
             } else {
+                float s1[1] = {0.f};
 #pragma unroll
                 for (int j = 0; j < V; ++j) {
-                    v[j] = expf(v[j] - top);
-                    sum += v[j];
+                    v[j] = exp_below(v[j] - top);
+                    s1[0] += v[j];
                 }
+                team.sum(s1);
+                sum = s1[0];
+                inv = inverse(sum);
             }
-            team.sum2(sum, scores);
-            const float inv = inverse(a.sigmoid ? scores : sum), lse = log_sum(top, sum);
+            const float lse = log_sum(top, sum);
 #pragma unroll
             for (int j = 0; j < V; ++j) acc[j] = fmaf(v[j], inv, acc[j]);
             if (team.lane == 0) sq = fmaf(lse, lse, sq);
+            if (base + TM::kTeams < hi) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[j] = next[j];
+                id = next_id;
+            }
+            on = next_on;
         }
         squares += (double)sq;
         // the sequence's (part of the) sums: over the warp's teams, over the warps
@@ -443,7 +478,7 @@ balance_kernel(const __grid_constant__ BalanceArgs a) {
         const size_t at = whole ? (size_t)s : 2 * (size_t)blockIdx.x + (from >= t0);
         float* sums = (whole ? a.sums : a.part_sums) + at * E;
         int32_t* counts = (whole ? a.counts : a.part_counts) + at * E;
-        const double factor = whole ? loss_factor(E, k, n) : 0.0;
+        const float factor = whole ? loss_factor(E, k, n) : 0.f;
         for (int e = tid; e < E; e += TM::kThreads) {
             float sum = 0.f;
 #pragma unroll
@@ -452,7 +487,7 @@ balance_kernel(const __grid_constant__ BalanceArgs a) {
             sums[e] = sum;
             counts[e] = count;
             hist[e] = 0;
-            if (whole) loss += (double)count * (double)sum * factor;
+            if (whole) loss += (double)((float)count * factor) * (double)sum;
         }
         if (tid == 0) (whole ? a.kept : a.part_kept)[at] = n;
         total += n;
@@ -462,11 +497,18 @@ balance_kernel(const __grid_constant__ BalanceArgs a) {
         if (tid == 0) n_kept = 0;
         __syncthreads();
     }
-    loss = cta_sum(loss, room64);
-    squares = cta_sum(squares, room64);
+    double v2[2] = {loss, squares};
+    cta_sums<2, TM::kThreads>(v2);
+    if constexpr (FUSED) {
+        if (gridDim.x == 1) {                                              // the only tile
+            const bool bad = __syncthreads_or(!ascends(a, tid, TM::kThreads));
+            if (tid == 0) write_losses(a, v2[0], some, v2[1], total, bad);
+            return;
+        }
+    }
     if (tid == 0) {
-        a.tile_loss[blockIdx.x] = loss;
-        a.tile_z[blockIdx.x] = squares;
+        a.tile_loss[blockIdx.x] = v2[0];
+        a.tile_z[blockIdx.x] = v2[1];
         a.tile_kept[blockIdx.x] = total;
         a.tile_some[blockIdx.x] = some;
         a.tile_open[blockIdx.x] = open;
@@ -474,7 +516,7 @@ balance_kernel(const __grid_constant__ BalanceArgs a) {
     if constexpr (FUSED) {
         __threadfence();
         cluster_sync();
-        join_tiles(a, (int)blockIdx.x, (int)gridDim.x, smem);
+        join_tiles<TM::kThreads>(a, (int)blockIdx.x, (int)gridDim.x, smem);
     }
 }
 
@@ -504,8 +546,7 @@ __global__ void __launch_bounds__(Team<L>::kThreads)
 gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
     using TM = Team<L>;
     extern __shared__ __align__(16) unsigned char smem[];
-    __shared__ float room[2 * TM::kWarps];
-    __shared__ double room64[32];
+    __shared__ float room[kMostSums * TM::kWarps];
     __shared__ float loss_scale[2];
     const TM team(room);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, E = a.E, k = a.k;
@@ -514,38 +555,74 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
     grid_dependency_wait();
     grid_launch_dependents();
     if (a.d_losses) {                                                      // S' and N
-        double n = 0.0, some = 0.0;
-        for (int s = tid; s < a.S; s += TM::kThreads) {
-            const int m = a.kept[s];
-            n += m;
-            some += m > 0;
+        double v[2] = {0.0, 0.0};
+        if (a.S == 1) {
+            v[0] = (double)a.kept[0];
+            v[1] = v[0] > 0;
+        } else {
+            for (int s = tid; s < a.S; s += TM::kThreads) {
+                const int m = a.kept[s];
+                v[0] += m;
+                v[1] += m > 0;
+            }
+            cta_sums<2, TM::kThreads>(v);
         }
-        n = cta_sum(n, room64);
-        some = cta_sum(some, room64);
         if (tid == 0) {
-            loss_scale[0] = some > 0 ? (float)(a.d_losses[0] * (double)E / (some * k)) : 0.f;
-            loss_scale[1] = n > 0 ? (float)(2.0 * a.d_losses[1] / n) : 0.f;
+            loss_scale[0] = v[1] > 0 ? a.d_losses[0] * (float)E / ((float)v[1] * (float)k) : 0.f;
+            loss_scale[1] = v[0] > 0 ? 2.f * a.d_losses[1] / (float)v[0] : 0.f;
         }
     }
     __syncthreads();
     const long long unit = TM::kCta ? blockIdx.x : (long long)blockIdx.x * TM::kWarps + warp;
     const long long t_begin = unit * a.rows, t_end = min((long long)a.T, t_begin + a.rows);
-    const bool losses = a.d_losses != nullptr;
+    const bool losses = a.d_losses != nullptr, weights = a.d_weights != nullptr, one = k <= L;
     const float balance = losses ? loss_scale[0] : 0.f, z_scale = losses ? loss_scale[1] : 0.f;
     const Z* z = static_cast<const Z*>(a.z);
-    float g[V];                                                            // G / balance of the sequence
+    float g[V];                                                            // G of the sequence
 #pragma unroll
     for (int j = 0; j < V; ++j) g[j] = 0.f;
     int s = -1, s_from = 0, s_to = 0;
     if (losses && t_begin < t_end) s = a.offsets ? first_ending_at(a.offsets, a.S, (int)t_begin + 1, lane) - 1 : -1;
-    for (long long base = t_begin; base < t_end; base += TM::kCta ? 1 : 32 / L) {
-        const long long t = base + (TM::kCta ? 0 : lane / L);
-        const bool in = t < t_end, on = in && (!a.mask || a.mask[t]);
-        float v[V];
-        if (on) load_row<Z, W, L, V>(z + t * a.ld, E, team.lane, v);
-        else
+    constexpr int kStep = TM::kCta ? 1 : 32 / L;
+    const int lane_row = TM::kCta ? 0 : lane / L;
+    // a row's logits, ids and weights' gradients are requested before the row before it is worked on
+    float v[V], d0 = 0.f;
+    int id0 = -1;
+    bool on = false;
+    const auto request = [&](long long t, float (&to)[V], int& id, float& d) {
+        const bool counts = t < t_end && (!a.mask || a.mask[t]);
+        id = -1;
+        if (counts) {
+            load_row<Z, W, L, V>(z + t * a.ld, E, team.lane, to);
+            if (weights && team.lane < k) {
+                id = a.ids[t * k + team.lane];
+                d = a.d_weights[t * k + team.lane];
+            }
+        } else {
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = -INFINITY;
+            for (int j = 0; j < V; ++j) to[j] = -INFINITY;
+        }
+        return counts;
+    };
+    if (t_begin < t_end) on = request(t_begin + lane_row, v, id0, d0);
+    for (long long base = t_begin; base < t_end; base += kStep) {
+        const long long t = base + lane_row;
+        const bool in = t < t_end;
+        float next[V], next_d = 0.f;
+        int next_id = -1;
+        bool next_on = false;
+        if (base + kStep < t_end) next_on = request(t + kStep, next, next_id, next_d);
+        // f(expert, its logit, scale times its weight's gradient) of the team's lanes' chosen experts
+        const auto each = [&](auto f) {
+            if (one) {
+                if ((unsigned)id0 < (unsigned)E) f(id0, to_float(z[t * a.ld + id0]), a.scale * d0, team.lane);
+            } else if (on) {
+                for (int j = team.lane; j < k; j += L) {
+                    const int id = a.ids[t * k + j];
+                    if ((unsigned)id < (unsigned)E) f(id, to_float(z[t * a.ld + id]), a.scale * a.d_weights[t * k + j], j);
+                }
+            }
+        };
         bool counts = losses && on;
         if (counts && t >= s_to) {                                         // the next sequence that ends behind t
             do {
@@ -561,116 +638,124 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
             }
         }
         counts = counts && s < a.S && t >= s_from;
-        float mx = v[0];
+        float mx[2] = {v[0], -INFINITY};
 #pragma unroll
-        for (int j = 1; j < V; ++j) mx = fmaxf(mx, v[j]);
-        mx = team.max(mx);
-        const float top = mx == -INFINITY ? 0.f : mx, c = a.sigmoid ? fminf(top, 0.f) : 0.f;
-        float dz[V];
-        float sum = 0.f, dot = 0.f;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            dz[j] = expf(v[j] - top);
-            sum += dz[j];
-            dot = fmaf(dz[j], g[j], dot);
+        for (int j = 1; j < V; ++j) mx[0] = fmaxf(mx[0], v[j]);
+        if (weights && a.renorm) {
+            each([&](int, float zj, float, int) { mx[1] = fmaxf(mx[1], zj); });
+            team.max(mx);
+        } else {
+            float m1[1] = {mx[0]};
+            team.max(m1);
+            mx[0] = m1[0];
         }
-        team.sum2(sum, dot);
-        const float inv = inverse(sum), lse = log_sum(top, sum);
-        // what is to be added at the chosen ones, and (softmax) the sum of p d
-        float chosen = 0.f;
-        if (a.d_weights) {
-            float most = -INFINITY;
-            if (a.renorm) {
-                if (on)
-                    for (int j = team.lane; j < k; j += L) {
-                        const int id = a.ids[t * k + j];
-                        if ((unsigned)id < (unsigned)E) most = fmaxf(most, to_float(z[t * a.ld + id]));
-                    }
-                most = team.max(most);
-            }
-            const float least = most == -INFINITY ? 0.f : a.sigmoid ? fminf(most, 0.f) : most;
-            float shares = 0.f, d_sum = 0.f;
-            bool twice = false;
-            if (on)
-                for (int j = team.lane; j < k; j += L) {
-                    const int id = a.ids[t * k + j];
-                    if ((unsigned)id >= (unsigned)E) continue;
-                    const float zj = to_float(z[t * a.ld + id]), d = a.scale * a.d_weights[t * k + j];
+        const float top = mx[0] == -INFINITY ? 0.f : mx[0], most = mx[1] == -INFINITY ? 0.f : mx[1];
+        const float c = fminf(top, 0.f), c_chosen = a.renorm ? fminf(most, 0.f) : 0.f;
+        // scores: times exp(-c) / exp(-top), with 1 - s (sigmoid); sums: of the scores, of scores G, of exponentials (z loss), of the chosen ones' shares, of shares d
+        float dz[V], p[V], sums[5] = {0.f, 0.f, 0.f, 0.f, 0.f};
+        const bool with_z = z_scale != 0.f;
+        if (a.sigmoid) {
+            if (losses) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
                     float rest;
-                    const float share = !a.renorm && !a.sigmoid ? expf(zj - top) * inv : a.sigmoid ? scaled_sigmoid(zj, a.renorm ? least : 0.f, rest) : expf(zj - least);
-                    shares += share;
-                    d_sum = fmaf(share, d, d_sum);
-                    row_add[id] = __int_as_float(j + 1);
+                    const float sg = scaled_sigmoid(v[j], c, rest);
+                    sums[0] += sg;
+                    sums[1] = fmaf(sg, g[j], sums[1]);
+                    dz[j] = sg * rest;
                 }
-            team.sum2(shares, d_sum);
-            team.sync();
-            if (on)
-                for (int j = team.lane; j < k; j += L) {
-                    const int id = a.ids[t * k + j];
-                    if ((unsigned)id < (unsigned)E) twice |= __float_as_int(row_add[id]) != j + 1;
-                }
-            twice = team.any(twice);                                       // an expert that is named twice: one after the other
-            if (twice) {
-                if (on)
-                    for (int j = team.lane; j < k; j += L) {
-                        const int id = a.ids[t * k + j];
-                        if ((unsigned)id < (unsigned)E) row_add[id] = 0.f;
+                if (with_z)
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        p[j] = exp_below(v[j] - top);
+                        sums[2] += p[j];
                     }
-                team.sync();
             }
-            const float share_inv = a.renorm ? inverse(shares) : 1.f, mean = a.renorm ? d_sum * share_inv : 0.f;
-            if (!a.renorm && !a.sigmoid) chosen = d_sum;
-            if (on)
-                for (int j = twice ? (team.lane ? k : 0) : team.lane; j < k; j += twice ? 1 : L) {
-                    const int id = a.ids[t * k + j];
-                    if ((unsigned)id >= (unsigned)E) continue;
-                    const float zj = to_float(z[t * a.ld + id]), d = a.scale * a.d_weights[t * k + j];
-                    float rest = 1.f;
-                    const float share = !a.renorm && !a.sigmoid ? expf(zj - top) * inv : a.sigmoid ? scaled_sigmoid(zj, a.renorm ? least : 0.f, rest) : expf(zj - least);
-                    const float add = share * share_inv * rest * (d - mean);
-                    row_add[id] = twice ? row_add[id] + add : add;
-                }
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                dz[j] = exp_below(v[j] - top);
+                sums[0] += dz[j];
+                sums[1] = fmaf(dz[j], g[j], sums[1]);
+            }
+        }
+        const auto share_of = [&](float zj, float& rest) {
+            rest = 1.f;
+            return a.sigmoid ? scaled_sigmoid(zj, c_chosen, rest) : exp_below(zj - (a.renorm ? most : top));
+        };
+        if (weights)
+            each([&](int id, float zj, float d, int j) {
+                float rest;
+                const float share = share_of(zj, rest);
+                sums[3] += share;
+                sums[4] = fmaf(share, d, sums[4]);
+                row_add[id] = __int_as_float(j + 1);
+            });
+        team.sum(sums);
+        const float inv = inverse(sums[0]), mean = sums[1] * inv;
+        if (weights) {
+            // The chosen ones' part goes through row_add; where an expert is named twice, one after the other.
+            team.sync();
+            bool twice = false;
+            each([&](int id, float, float, int j) { twice |= __float_as_int(row_add[id]) != j + 1; });
+            twice = team.any(twice);
+            const float share_scale = a.renorm ? inverse(sums[3]) : a.sigmoid ? 1.f : inv, d_mean = a.renorm ? sums[4] * share_scale : 0.f;
+            const auto part = [&](float zj, float d) {
+                float rest;
+                const float share = share_of(zj, rest);
+                return share * share_scale * rest * (d - d_mean);
+            };
+            if (!twice) {
+                each([&](int id, float zj, float d, int) { row_add[id] = part(zj, d); });
+            } else {
+                each([&](int id, float, float, int) { row_add[id] = 0.f; });
+                team.sync();
+                if (on && team.lane == 0)
+                    for (int j = 0; j < k; ++j) {
+                        const int id = a.ids[t * k + j];
+                        if ((unsigned)id < (unsigned)E) row_add[id] += part(to_float(z[t * a.ld + id]), a.scale * a.d_weights[t * k + j]);
+                    }
+            }
             team.sync();
         }
         if (a.sigmoid) {
-            float scores = 0.f;
-            dot = 0.f;
-            const float zl = counts ? z_scale * lse * inv : 0.f;
+            const float scale = counts ? inv : 0.f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                float rest;
-                const float sg = scaled_sigmoid(v[j], c, rest);
-                scores += sg;
-                dot = fmaf(sg, g[j], dot);
-            }
-            team.sum2(scores, dot);
-            const float sinv = counts ? inverse(scores) : 0.f, mean = dot * sinv;
+            for (int j = 0; j < V; ++j) dz[j] = losses ? dz[j] * scale * (g[j] - mean) : 0.f;
+            if (with_z && losses) {
+                const float zl = counts ? z_scale * log_sum(top, sums[2]) * inverse(sums[2]) : 0.f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                float rest;
-                const float sg = scaled_sigmoid(v[j], c, rest);
-                dz[j] = fmaf(dz[j], zl, sg * sinv * rest * (g[j] - mean));
+                for (int j = 0; j < V; ++j) dz[j] = fmaf(p[j], zl, dz[j]);
             }
         } else {
-            const float zl = counts ? z_scale * lse : 0.f, mean = dot * inv, on_g = counts ? 1.f : 0.f;
+            const float zl = (counts && with_z ? z_scale * log_sum(top, sums[0]) : 0.f) - (weights && !a.renorm ? sums[4] * inv : 0.f) - (counts ? mean : 0.f);
+            const float on_g = counts ? inv : 0.f, rest = zl * inv;
 #pragma unroll
-            for (int j = 0; j < V; ++j) dz[j] = dz[j] * inv * (on_g * (g[j] - mean) + zl - chosen);
+            for (int j = 0; j < V; ++j) dz[j] *= fmaf(on_g, g[j], rest);
         }
-        if (a.d_weights) {
+        if (weights) {
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const int e = (j / W * L + team.lane) * W + j % W;
-                dz[j] += row_add[e];
+            for (int j = 0; j < V / W; ++j) {
+                const float* at = row_add + (j * L + team.lane) * W;
+                if constexpr (W == 4) {
+                    const float4 r = *reinterpret_cast<const float4*>(at);
+                    dz[4 * j] += r.x, dz[4 * j + 1] += r.y, dz[4 * j + 2] += r.z, dz[4 * j + 3] += r.w;
+                } else {
+                    dz[j] += *at;
+                }
             }
             team.sync();
-            if (on)
-                for (int j = team.lane; j < k; j += L) {
-                    const int id = a.ids[t * k + j];
-                    if ((unsigned)id < (unsigned)E) row_add[id] = 0.f;
-                }
+            each([&](int id, float, float, int) { row_add[id] = 0.f; });
             team.sync();
         }
         if (in) store_row<Z, W, L, V>(static_cast<Z*>(a.out) + t * a.ld_out, E, team.lane, dz);
+        if (base + kStep < t_end) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[j] = next[j];
+            id0 = next_id;
+            d0 = next_d;
+        }
+        on = next_on;
     }
 }
 
@@ -692,7 +777,7 @@ Tiling tiling(int T, int E) {
     return {rows, (int)(((long long)T + rows - 1) / rows), false};
 }
 size_t scratch_bytes(int E, const Tiling& t) {
-    return 8 * (2 * (size_t)t.tiles + 2 * kJoinCtas) + 4 * (4 * (size_t)t.tiles * E + 2 * (size_t)t.tiles + 3 * (size_t)t.tiles + 2 * kJoinCtas);
+    return 8 * (2 * (size_t)t.tiles + 2 * kJoinCtas) + 4 * (4 * (size_t)t.tiles * E + 2 * (size_t)t.tiles + 3 * (size_t)t.tiles);
 }
 
 template <typename Z, int W, int L, int V>
@@ -719,9 +804,9 @@ template <typename Z, int W, int L, int V>
 int launch_backward(BackwardArgs a, cudaStream_t st) {
     using TM = Team<L>;
     static SmemOnce once;
-    // rows per warp (CTA): as many as leave every SM four CTAs
-    constexpr int at_once = TM::kCta ? 1 : 32 / L;
-    const long long units = (long long)kSms * 4 * (TM::kCta ? 1 : TM::kWarps);
+    // rows per warp (CTA): as many as leave every SM its share of the CTAs that it holds at once
+    constexpr int at_once = TM::kCta ? 1 : 32 / L, per_sm = TM::kCta ? 1024 / TM::kThreads : 2;
+    const long long units = (long long)kSms * per_sm * (TM::kCta ? 1 : TM::kWarps);
     const long long turns = ((long long)a.T + units * at_once - 1) / (units * at_once);
     a.rows = (int)std::min<long long>(turns * at_once, a.T);
     const long long per_cta = (long long)a.rows * (TM::kCta ? 1 : TM::kWarps);
@@ -779,7 +864,6 @@ extern "C" int exmoe_balance_loss(const exmoe_shape* shape, const exmoe_gate* ga
     a.tile_kept = a.part_kept + 2 * n;
     a.tile_some = a.tile_kept + n;
     a.tile_open = a.tile_some + n;
-    a.joined_some = a.tile_open + n;
     cudaStream_t st = (cudaStream_t)stream;
     const bool fours = in_fours(logits, row_stride, T, g.E, es);
     if (type == EXMOE_F32) return fours ? launch_balance<float, 4>(a, t.fused, st) : launch_balance<float, 1>(a, t.fused, st);
