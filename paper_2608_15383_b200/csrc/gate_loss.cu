@@ -29,10 +29,10 @@ template <> __device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat
 // A team of L lanes per row, each with V experts in runs of W: expert (j L + lane) W + i.  Up to 32 lanes they are (part of) a warp, beyond
 // that the whole CTA.
 constexpr int kMostSums = 5;
-template <int L>
+template <int L, int THREADS>
 struct Team {
     static constexpr bool kCta = L > 32;
-    static constexpr int kThreads = kCta ? L : 512, kWarps = kThreads / 32, kTeams = kThreads / L;
+    static constexpr int kThreads = kCta ? L : THREADS, kWarps = kThreads / 32, kTeams = kThreads / L;
     int lane, index;                   // in the team; of the team in its CTA
     float* room;                       // [kMostSums kWarps], for teams of several warps
     __device__ Team(float* r) : lane((int)threadIdx.x % L), index((int)threadIdx.x / L), room(r) {}
@@ -275,12 +275,28 @@ __device__ __forceinline__ void join_tiles(const BalanceArgs& a, int cta, int ct
         const int e = min(32 * c + lane, a.E - 1);
         sum = 0.f;
         count = n = 0;
-#pragma unroll 8
-        for (int t = o.tile + first; t <= o.last; t += step) {
-            const size_t at = 2 * (size_t)t + (t == o.tile);
-            sum += __ldcg(a.part_sums + at * a.E + e);
-            count += __ldcg(a.part_counts + at * a.E + e);
-            n += __ldcg(a.part_kept + at);
+        constexpr int kFlight = 10;
+        for (int t0 = o.tile + first; t0 <= o.last; t0 += kFlight * step) {
+            float f[kFlight];
+            int m[kFlight], l[kFlight];
+#pragma unroll
+            for (int u = 0; u < kFlight; ++u) {
+                const int t = t0 + u * step;
+                f[u] = 0.f;
+                m[u] = l[u] = 0;
+                if (t <= o.last) {
+                    const size_t at = 2 * (size_t)t + (t == o.tile);
+                    f[u] = __ldcg(a.part_sums + at * a.E + e);
+                    m[u] = __ldcg(a.part_counts + at * a.E + e);
+                    l[u] = __ldcg(a.part_kept + at);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kFlight; ++u) {
+                sum += f[u];
+                count += m[u];
+                n += l[u];
+            }
         }
     };
     // A warp per 32 experts of a sequence; where there are few of these, or the sequence covers many tiles, a CTA's warps share its tiles.
@@ -338,14 +354,19 @@ balance_join_kernel(const __grid_constant__ BalanceArgs a) {
     join_tiles<kJoinThreads>(a, (int)blockIdx.x, (int)gridDim.x, smem);
 }
 
+// Threads of a CTA: as many as registers allow (three rows' worth of V per lane: this one's, the next one's, the sums).
+__host__ __device__ constexpr int balance_threads(int V) { return V <= 8 ? 1024 : 512; }
 template <int L, int V>
-constexpr size_t balance_smem() { return (size_t)(Team<L>::kCta ? 1 : Team<L>::kWarps) * L * V * 4 + (size_t)L * V * 4; }
+constexpr size_t balance_smem() {
+    using TM = Team<L, balance_threads(V)>;
+    return (size_t)(TM::kCta ? 1 : TM::kWarps) * L * V * 4 + (size_t)L * V * 4;
+}
 
 // First step: a CTA per tile.  FUSED: the grid is one cluster, which goes on with the second.
 template <typename Z, int W, int L, int V, bool FUSED>
-__global__ void __launch_bounds__(Team<L>::kThreads)
+__global__ void __launch_bounds__(Team<L, balance_threads(V)>::kThreads)
 balance_kernel(const __grid_constant__ BalanceArgs a) {
-    using TM = Team<L>;
+    using TM = Team<L, balance_threads(V)>;
     extern __shared__ __align__(16) unsigned char smem[];
     float* red = reinterpret_cast<float*>(smem);                           // [warp][L V] column sums
     int32_t* hist = reinterpret_cast<int32_t*>(red + (TM::kCta ? 1 : TM::kWarps) * L * V);   // [L V]
@@ -384,34 +405,60 @@ balance_kernel(const __grid_constant__ BalanceArgs a) {
 #pragma unroll
         for (int j = 0; j < V; ++j) acc[j] = 0.f;
         int mine = 0;
-        // a row's logits and first ids are requested before the row before it is worked on
-        const int lane_row = TM::kCta ? 0 : lane / L;
-        const long long first = (long long)lo + (TM::kCta ? 0 : warp * (32 / L));
+        // A row's logits and first ids are requested before the row before it is worked on (unless that takes too many registers).
+        constexpr bool kAhead = V <= 16;
+        const int rows = hi - lo, row0 = TM::kCta ? 0 : warp * (32 / L), own = TM::kCta ? 0 : lane / L;
+        const Z* z_row = z + ((long long)lo + row0 + own) * a.ld;
+        const int32_t* id_row = a.ids + ((long long)lo + row0 + own) * k + team.lane;
+        const uint8_t* mask_row = a.mask ? a.mask + lo + row0 + own : nullptr;
+        const long long z_step = TM::kTeams * a.ld, id_step = (long long)TM::kTeams * k;
+        const bool has_id = team.lane < k;
         float v[V];
         int id = -1;
         bool on = false;
-        const auto request = [&](long long t, float (&to)[V], int& to_id) {
-            const bool counts = t < hi && (!a.mask || a.mask[t]);
+        // the row that the pointers are at, row r of this sequence's
+        const auto request = [&](int r, float (&to)[V], int& to_id) {
+            const bool counts = r < rows && (!mask_row || *mask_row);
+            to_id = -1;
             if (counts) {
-                load_row<Z, W, L, V>(z + t * a.ld, E, team.lane, to);
-                to_id = team.lane < k ? a.ids[t * k + team.lane] : -1;
+                load_row<Z, W, L, V>(z_row, E, team.lane, to);
+                if (has_id) to_id = *id_row;
             } else {
 #pragma unroll
                 for (int j = 0; j < V; ++j) to[j] = -INFINITY;
-                to_id = -1;
             }
             return counts;
         };
-        if (first < hi) on = request(first + lane_row, v, id);
-        for (long long base = first; base < hi; base += TM::kTeams) {
-            float next[V];
+        const auto advance = [&] {
+            z_row += z_step;
+            id_row += id_step;
+            if (mask_row) mask_row += TM::kTeams;
+        };
+        if (kAhead && row0 < rows) {
+            on = request(row0 + own, v, id);
+            advance();
+        }
+        for (int base = row0; base < rows; base += TM::kTeams) {
+            float next[kAhead ? V : 1];
+            if constexpr (kAhead) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) next[j] = -INFINITY;
+            }
             int next_id = -1;
             bool next_on = false;
-            if (base + TM::kTeams < hi) next_on = request(base + TM::kTeams + lane_row, next, next_id);
+            if constexpr (kAhead) {
+                if (base + TM::kTeams < rows) {
+                    next_on = request(base + TM::kTeams + own, next, next_id);
+                    advance();
+                }
+            } else {
+                on = request(base + own, v, id);
+                advance();
+            }
             if ((unsigned)id < (unsigned)E) atomicAdd(hist + id, 1);
             if (on && k > L)
                 for (int j = team.lane + L; j < k; j += L) {
-                    const int more = a.ids[(base + lane_row) * k + j];
+                    const int more = a.ids[((long long)lo + base + own) * k + j];
                     if ((unsigned)more < (unsigned)E) atomicAdd(hist + more, 1);
                 }
             mine += on && team.lane == 0;
@@ -449,12 +496,12 @@ balance_kernel(const __grid_constant__ BalanceArgs a) {
 #pragma unroll
             for (int j = 0; j < V; ++j) acc[j] = fmaf(v[j], inv, acc[j]);
             if (team.lane == 0) sq = fmaf(lse, lse, sq);
-            if (base + TM::kTeams < hi) {
+            if constexpr (kAhead) {
 #pragma unroll
                 for (int j = 0; j < V; ++j) v[j] = next[j];
                 id = next_id;
+                on = next_on;
             }
-            on = next_on;
         }
         squares += (double)sq;
         // the sequence's (part of the) sums: over the warp's teams, over the warps
@@ -542,9 +589,9 @@ struct BackwardArgs {
 // The chosen ones' logits are read again and their shares taken from their own largest: they may all be lost beside the row's.  What goes to
 // single experts passes through a row of shared memory that is zero between rows.
 template <typename Z, int W, int L, int V>
-__global__ void __launch_bounds__(Team<L>::kThreads)
+__global__ void __launch_bounds__(Team<L, 512>::kThreads, V <= 8 ? 1024 / Team<L, 512>::kThreads : 1)
 gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
-    using TM = Team<L>;
+    using TM = Team<L, 512>;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ float room[kMostSums * TM::kWarps];
     __shared__ float loss_scale[2];
@@ -586,15 +633,19 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
     constexpr int kStep = TM::kCta ? 1 : 32 / L;
     const int lane_row = TM::kCta ? 0 : lane / L;
     // a row's logits, ids and weights' gradients are requested before the row before it is worked on
+    const Z* z_row = z + (t_begin + lane_row) * a.ld;
+    Z* out_row = static_cast<Z*>(a.out) + (t_begin + lane_row) * a.ld_out;
+    const long long z_step = kStep * a.ld, out_step = kStep * a.ld_out;
+    const bool has_id = weights && team.lane < k;
     float v[V], d0 = 0.f;
     int id0 = -1;
     bool on = false;
-    const auto request = [&](long long t, float (&to)[V], int& id, float& d) {
+    const auto request = [&](long long t, const Z* row, float (&to)[V], int& id, float& d) {
         const bool counts = t < t_end && (!a.mask || a.mask[t]);
         id = -1;
         if (counts) {
-            load_row<Z, W, L, V>(z + t * a.ld, E, team.lane, to);
-            if (weights && team.lane < k) {
+            load_row<Z, W, L, V>(row, E, team.lane, to);
+            if (has_id) {
                 id = a.ids[t * k + team.lane];
                 d = a.d_weights[t * k + team.lane];
             }
@@ -604,24 +655,26 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
         }
         return counts;
     };
-    if (t_begin < t_end) on = request(t_begin + lane_row, v, id0, d0);
-    for (long long base = t_begin; base < t_end; base += kStep) {
+    if (t_begin < t_end) on = request(t_begin + lane_row, z_row, v, id0, d0);
+    for (long long base = t_begin; base < t_end; base += kStep, z_row += z_step, out_row += out_step) {
         const long long t = base + lane_row;
-        const bool in = t < t_end;
-        float next[V], next_d = 0.f;
+        const bool in = t < t_end, first = (unsigned)id0 < (unsigned)E;
+        const float zj0 = first ? to_float(z_row[id0]) : 0.f;              // of this lane's chosen expert
+        d0 *= a.scale;
+        float next[V], next_d = 0.f, share0 = 0.f, rest0 = 1.f;
         int next_id = -1;
         bool next_on = false;
-        if (base + kStep < t_end) next_on = request(t + kStep, next, next_id, next_d);
-        // f(expert, its logit, scale times its weight's gradient) of the team's lanes' chosen experts
-        const auto each = [&](auto f) {
-            if (one) {
-                if ((unsigned)id0 < (unsigned)E) f(id0, to_float(z[t * a.ld + id0]), a.scale * d0, team.lane);
-            } else if (on) {
-                for (int j = team.lane; j < k; j += L) {
+        if (base + kStep < t_end) next_on = request(t + kStep, z_row + z_step, next, next_id, next_d);
+        else
+#pragma unroll
+            for (int j = 0; j < V; ++j) next[j] = -INFINITY;
+        // f(expert, its logit, scale times its weight's gradient, place) of the team's lanes' chosen experts behind the first one of each
+        const auto others = [&](auto f) {
+            if (on)
+                for (int j = team.lane + L; j < k; j += L) {
                     const int id = a.ids[t * k + j];
-                    if ((unsigned)id < (unsigned)E) f(id, to_float(z[t * a.ld + id]), a.scale * a.d_weights[t * k + j], j);
+                    if ((unsigned)id < (unsigned)E) f(id, to_float(z_row[id]), a.scale * a.d_weights[t * k + j], j);
                 }
-            }
         };
         bool counts = losses && on;
         if (counts && t >= s_to) {                                         // the next sequence that ends behind t
@@ -642,7 +695,8 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
 #pragma unroll
         for (int j = 1; j < V; ++j) mx[0] = fmaxf(mx[0], v[j]);
         if (weights && a.renorm) {
-            each([&](int, float zj, float, int) { mx[1] = fmaxf(mx[1], zj); });
+            if (first) mx[1] = zj0;
+            if (!one) others([&](int, float zj, float, int) { mx[1] = fmaxf(mx[1], zj); });
             team.max(mx);
         } else {
             float m1[1] = {mx[0]};
@@ -652,7 +706,7 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
         const float top = mx[0] == -INFINITY ? 0.f : mx[0], most = mx[1] == -INFINITY ? 0.f : mx[1];
         const float c = fminf(top, 0.f), c_chosen = a.renorm ? fminf(most, 0.f) : 0.f;
         // scores: times exp(-c) / exp(-top), with 1 - s (sigmoid); sums: of the scores, of scores G, of exponentials (z loss), of the chosen ones' shares, of shares d
-        float dz[V], p[V], sums[5] = {0.f, 0.f, 0.f, 0.f, 0.f};
+        float dz[V], sums[5] = {0.f, 0.f, 0.f, 0.f, 0.f};
         const bool with_z = z_scale != 0.f;
         if (a.sigmoid) {
             if (losses) {
@@ -666,10 +720,7 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
                 }
                 if (with_z)
 #pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        p[j] = exp_below(v[j] - top);
-                        sums[2] += p[j];
-                    }
+                    for (int j = 0; j < V; ++j) sums[2] += exp_below(v[j] - top);
             }
         } else {
 #pragma unroll
@@ -683,21 +734,29 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
             rest = 1.f;
             return a.sigmoid ? scaled_sigmoid(zj, c_chosen, rest) : exp_below(zj - (a.renorm ? most : top));
         };
-        if (weights)
-            each([&](int id, float zj, float d, int j) {
-                float rest;
-                const float share = share_of(zj, rest);
-                sums[3] += share;
-                sums[4] = fmaf(share, d, sums[4]);
-                row_add[id] = __int_as_float(j + 1);
-            });
+        if (weights) {
+            if (first) {
+                share0 = share_of(zj0, rest0);
+                sums[3] = share0;
+                sums[4] = share0 * d0;
+                row_add[id0] = __int_as_float(team.lane + 1);
+            }
+            if (!one)
+                others([&](int id, float zj, float d, int j) {
+                    float rest;
+                    const float share = share_of(zj, rest);
+                    sums[3] += share;
+                    sums[4] = fmaf(share, d, sums[4]);
+                    row_add[id] = __int_as_float(j + 1);
+                });
+        }
         team.sum(sums);
         const float inv = inverse(sums[0]), mean = sums[1] * inv;
         if (weights) {
             // The chosen ones' part goes through row_add; where an expert is named twice, one after the other.
             team.sync();
-            bool twice = false;
-            each([&](int id, float, float, int j) { twice |= __float_as_int(row_add[id]) != j + 1; });
+            bool twice = first && __float_as_int(row_add[id0]) != team.lane + 1;
+            if (!one) others([&](int id, float, float, int j) { twice |= __float_as_int(row_add[id]) != j + 1; });
             twice = team.any(twice);
             const float share_scale = a.renorm ? inverse(sums[3]) : a.sigmoid ? 1.f : inv, d_mean = a.renorm ? sums[4] * share_scale : 0.f;
             const auto part = [&](float zj, float d) {
@@ -706,14 +765,16 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
                 return share * share_scale * rest * (d - d_mean);
             };
             if (!twice) {
-                each([&](int id, float zj, float d, int) { row_add[id] = part(zj, d); });
+                if (first) row_add[id0] = share0 * share_scale * rest0 * (d0 - d_mean);
+                if (!one) others([&](int id, float zj, float d, int) { row_add[id] = part(zj, d); });
             } else {
-                each([&](int id, float, float, int) { row_add[id] = 0.f; });
+                if (first) row_add[id0] = 0.f;
+                if (!one) others([&](int id, float, float, int) { row_add[id] = 0.f; });
                 team.sync();
                 if (on && team.lane == 0)
                     for (int j = 0; j < k; ++j) {
                         const int id = a.ids[t * k + j];
-                        if ((unsigned)id < (unsigned)E) row_add[id] += part(to_float(z[t * a.ld + id]), a.scale * a.d_weights[t * k + j]);
+                        if ((unsigned)id < (unsigned)E) row_add[id] += part(to_float(z_row[id]), a.scale * a.d_weights[t * k + j]);
                     }
             }
             team.sync();
@@ -725,7 +786,7 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
             if (with_z && losses) {
                 const float zl = counts ? z_scale * log_sum(top, sums[2]) * inverse(sums[2]) : 0.f;
 #pragma unroll
-                for (int j = 0; j < V; ++j) dz[j] = fmaf(p[j], zl, dz[j]);
+                for (int j = 0; j < V; ++j) dz[j] = fmaf(exp_below(v[j] - top), zl, dz[j]);
             }
         } else {
             const float zl = (counts && with_z ? z_scale * log_sum(top, sums[0]) : 0.f) - (weights && !a.renorm ? sums[4] * inv : 0.f) - (counts ? mean : 0.f);
@@ -745,16 +806,15 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
                 }
             }
             team.sync();
-            each([&](int id, float, float, int) { row_add[id] = 0.f; });
+            if (first) row_add[id0] = 0.f;
+            if (!one) others([&](int id, float, float, int) { row_add[id] = 0.f; });
             team.sync();
         }
-        if (in) store_row<Z, W, L, V>(static_cast<Z*>(a.out) + t * a.ld_out, E, team.lane, dz);
-        if (base + kStep < t_end) {
+        if (in) store_row<Z, W, L, V>(out_row, E, team.lane, dz);
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = next[j];
-            id0 = next_id;
-            d0 = next_d;
-        }
+        for (int j = 0; j < V; ++j) v[j] = next[j];
+        id0 = next_id;
+        d0 = next_d;
         on = next_on;
     }
 }
@@ -762,10 +822,9 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
 // ---- host ------------------------------------------------------------------------------------------------------------
 
 struct Tiling { int rows, tiles; bool fused; };
-// Small calls are one cluster, whose CTAs take a tile each and then join them; others a tile per CTA that the chip holds at once.
+// Small calls are one cluster, whose CTAs take a tile each and then join them; others a tile per SM (two where a CTA has half of its threads).
 Tiling tiling(int T, int E) {
-    const int at_once = E <= 64 ? 64 : E <= 128 ? 32 : E <= 512 ? 16 : 1;  // rows that a CTA has in hand
-    const int most = kSms * (E <= 512 ? 2 : E <= 1024 ? 8 : 2);
+    const int at_once = E <= 64 ? 128 : E <= 128 ? 64 : E <= 256 ? 32 : E <= 1024 ? 16 : 1;    // rows that a CTA has in hand
     const long long small = T / (2 * at_once);
     if (small <= 8) {
         int ctas = 1;
@@ -773,7 +832,7 @@ Tiling tiling(int T, int E) {
         const int rows = std::max(1, (T + ctas - 1) / ctas);
         return {rows, ctas, true};
     }
-    const int rows = std::max(2 * at_once, (int)(((long long)T + most - 1) / most));
+    const int rows = std::max(at_once, (int)(((long long)T + kSms - 1) / kSms));
     return {rows, (int)(((long long)T + rows - 1) / rows), false};
 }
 size_t scratch_bytes(int E, const Tiling& t) {
@@ -782,10 +841,11 @@ size_t scratch_bytes(int E, const Tiling& t) {
 
 template <typename Z, int W, int L, int V>
 int launch_balance(const BalanceArgs& a, bool fused, cudaStream_t st) {
+    using TM = Team<L, balance_threads(V)>;
     static SmemOnce once[2];
-    constexpr size_t smem = balance_smem<L, V>(), fused_smem = std::max(smem, join_smem(Team<L>::kThreads));
-    if (fused) return launch(balance_kernel<Z, W, L, V, true>, (unsigned)a.tiles, Team<L>::kThreads, a.tiles, fused_smem, once[0], st, a);
-    const int rc = launch(balance_kernel<Z, W, L, V, false>, (unsigned)a.tiles, Team<L>::kThreads, 1, smem, once[1], st, a);
+    constexpr size_t smem = balance_smem<L, V>(), fused_smem = std::max(smem, join_smem(TM::kThreads));
+    if (fused) return launch(balance_kernel<Z, W, L, V, true>, (unsigned)a.tiles, TM::kThreads, a.tiles, fused_smem, once[0], st, a);
+    const int rc = launch(balance_kernel<Z, W, L, V, false>, (unsigned)a.tiles, TM::kThreads, 1, smem, once[1], st, a);
     if (rc) return rc;
     static SmemOnce join;
     return launch(balance_join_kernel, kJoinCtas, kJoinThreads, kJoinCtas, join_smem(kJoinThreads), join, st, a);
@@ -796,16 +856,16 @@ int launch_balance(const BalanceArgs& a, bool fused, cudaStream_t st) {
     if (a.E <= 128) return launch_balance<Z, W, 16, 8>(a, fused, st);
     if (a.E <= 256) return launch_balance<Z, W, 32, 8>(a, fused, st);
     if (a.E <= 512) return launch_balance<Z, W, 32, 16>(a, fused, st);
-    if (a.E <= 1024) return launch_balance<Z, W, 128, 8>(a, fused, st);
+    if (a.E <= 1024) return launch_balance<Z, W, 32, 32>(a, fused, st);
     return launch_balance<Z, W, 512, 8>(a, fused, st);
 }
 
 template <typename Z, int W, int L, int V>
 int launch_backward(BackwardArgs a, cudaStream_t st) {
-    using TM = Team<L>;
+    using TM = Team<L, 512>;
     static SmemOnce once;
     // rows per warp (CTA): as many as leave every SM its share of the CTAs that it holds at once
-    constexpr int at_once = TM::kCta ? 1 : 32 / L, per_sm = TM::kCta ? 1024 / TM::kThreads : 2;
+    constexpr int at_once = TM::kCta ? 1 : 32 / L, per_sm = V <= 8 ? 1024 / TM::kThreads : 1;
     const long long units = (long long)kSms * per_sm * (TM::kCta ? 1 : TM::kWarps);
     const long long turns = ((long long)a.T + units * at_once - 1) / (units * at_once);
     a.rows = (int)std::min<long long>(turns * at_once, a.T);
