@@ -21,6 +21,7 @@ namespace {
 constexpr int kMaxTokens = 1 << 29, kMaxExperts = 4096;
 constexpr int kSms = 148;
 constexpr int kJoinThreads = 512, kJoinCtas = 8, kWindow = 512;
+constexpr int kTurnsAlone = 8;
 
 template <typename Z> __device__ __forceinline__ float to_float(Z v);
 template <> __device__ __forceinline__ float to_float<float>(float v) { return v; }
@@ -42,7 +43,14 @@ struct Team {
     }
     // the largest / the sum over the team of each of N values, in one go
     template <int N>
-    __device__ __forceinline__ void max(float (&v)[N]) const { reduce(v, [](float a, float b) { return fmaxf(a, b); }, -INFINITY); }
+    __device__ __forceinline__ void max(float (&v)[N]) const {
+        if constexpr (L == 32) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) asm("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(v[i]));
+        } else {
+            reduce(v, [](float a, float b) { return fmaxf(a, b); }, -INFINITY);
+        }
+    }
     template <int N>
     __device__ __forceinline__ void sum(float (&v)[N]) const { reduce(v, [](float a, float b) { return a + b; }, 0.f); }
     template <int N, typename F>
@@ -72,14 +80,14 @@ struct Team {
     }
 };
 
-// A row's logits, -infinity behind the last expert.
+// A row's logits; what v holds behind the last expert stays.
 template <typename Z, int W, int L, int V>
 __device__ __forceinline__ void load_row(const Z* row, int E, int lane, float (&v)[V]) {
 #pragma unroll
     for (int j = 0; j < V / W; ++j) {
         const int e = (j * L + lane) * W;
         if constexpr (W == 1) {
-            v[j] = e < E ? to_float(row[e]) : -INFINITY;
+            if (e < E) v[j] = to_float(row[e]);
         } else {                                                           // E is a multiple of W
             if (e < E) {
                 if constexpr (sizeof(Z) == 4) {
@@ -90,8 +98,6 @@ __device__ __forceinline__ void load_row(const Z* row, int E, int lane, float (&
                     v[4 * j] = __uint_as_float(r.x << 16), v[4 * j + 1] = __uint_as_float(r.x & 0xffff0000u);
                     v[4 * j + 2] = __uint_as_float(r.y << 16), v[4 * j + 3] = __uint_as_float(r.y & 0xffff0000u);
                 }
-            } else {
-                v[4 * j] = v[4 * j + 1] = v[4 * j + 2] = v[4 * j + 3] = -INFINITY;
             }
         }
     }
@@ -114,23 +120,114 @@ __device__ __forceinline__ void store_row(Z* row, int E, int lane, const float (
     }
 }
 
+constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float exp2_of(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 // exp(x) for x <= 0 by the hardware's 2^x: off by 2 units of 2^-23 and by the product's rounding, |x| 2^-24 (which with that of the difference that x is
 // is what a score far below the largest is off by; the function with the exact argument takes three times the instructions, which
 // would bound these kernels).  Results below 2^-126 are 0.
-__device__ __forceinline__ float exp_below(float x) {
+__device__ __forceinline__ float exp_below(float x) { return exp2_of(x * kLog2e); }
+__device__ __forceinline__ float recip(float x) {
     float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * 1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// Pairs of binary32 numbers: two operations in one instruction.
+struct Two { unsigned long long bits; };
+__device__ __forceinline__ Two two(float a, float b) {
+    Two r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.bits) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void split(Two v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v.bits)); }
+__device__ __forceinline__ Two operator+(Two a, Two b) {
+    Two r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
+    return r;
+}
+__device__ __forceinline__ Two operator*(Two a, Two b) {
+    Two r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits));
+    return r;
+}
+__device__ __forceinline__ Two fma(Two a, Two b, Two c) {
+    Two r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.bits) : "l"(a.bits), "l"(b.bits), "l"(c.bits));
+    return r;
+}
+__device__ __forceinline__ float both(Two v) {
+    float a, b;
+    split(v, a, b);
+    return a + b;
+}
+// e = exp(v - top) and their sum, top the largest.  In one product and sum: what top's product is rounded by is a factor that all of a row's terms
+// have in common, so that shares do not see it, and the logarithm no more than top's own last place.
+template <int V>
+__device__ __forceinline__ float exps_below(const float (&v)[V], float top, float (&e)[V]) {
+    if (fabsf(top) < 1e38f) {
+        const Two shift = two(-top * kLog2e, -top * kLog2e), scale = two(kLog2e, kLog2e);
+        Two sum = two(0.f, 0.f);
+#pragma unroll
+        for (int j = 0; j < V; j += 2) {
+            float a, b;
+            split(fma(two(v[j], v[j + 1]), scale, shift), a, b);
+            e[j] = exp2_of(a);
+            e[j + 1] = exp2_of(b);
+            sum = sum + two(e[j], e[j + 1]);
+        }
+        return both(sum);
+    }
+    float sum = 0.f;                                                       // the product would leave binary32 (or top is NaN)
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        e[j] = exp_below(v[j] - top);
+        sum += e[j];
+    }
+    return sum;
 }
 // A sigmoid times exp(-c) (see the top; c <= 0), and 1 - sigmoid.
 __device__ __forceinline__ float scaled_sigmoid(float z, float c, float& rest) {
-    const float u = exp_below(-fabsf(z)), inv = __fdividef(1.f, 1.f + u), small = u * inv;
+    const float u = exp_below(-fabsf(z)), inv = recip(1.f + u), small = u * inv;
     rest = z < 0.f ? inv : small;                                          // (NaN: both are)
     return c < 0.f ? exp_below(z - c) * inv : z < 0.f ? small : inv;
 }
+// All of a row's: the sigmoids s, s (1 - s) = u / (1 + u)^2, and the sum of the former; both times exp(-c).
+template <int V>
+__device__ __forceinline__ float sigmoids(const float (&v)[V], float c, float (&s)[V], float (&slope)[V]) {
+    if (c < 0.f) {
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            float rest;
+            s[j] = scaled_sigmoid(v[j], c, rest);
+            slope[j] = s[j] * rest;
+            sum += s[j];
+        }
+        return sum;
+    }
+    const Two one = two(1.f, 1.f);
+    Two sum = two(0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < V; j += 2) {
+        const Two u = two(exp_below(-fabsf(v[j])), exp_below(-fabsf(v[j + 1])));
+        float a, b, x, y;
+        split(one + u, a, b);
+        const Two inv = two(recip(a), recip(b)), small = u * inv;
+        split(inv, a, b);
+        split(small, x, y);
+        s[j] = v[j] < 0.f ? x : a;
+        s[j + 1] = v[j + 1] < 0.f ? y : b;
+        split(small * inv, slope[j], slope[j + 1]);
+        sum = sum + two(s[j], s[j + 1]);
+    }
+    return both(sum);
+}
 // The logarithm of a row's sum of exponentials; 0 for a row without any expert left.
 __device__ __forceinline__ float log_sum(float base, float sum) { return sum == 0.f ? 0.f : base + __logf(sum); }
-__device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : __fdividef(1.f, sum); }
+__device__ __forceinline__ float inverse(float sum) { return sum == 0.f ? 0.f : recip(sum); }
 
 // The first sequence that ends at t or behind it, by a warp: offsets [S + 1] ascend.  Whatever they hold, the answer is in [0, S].
 __device__ __forceinline__ int first_ending_at(const int32_t* offsets, int S, int t, int lane) {
@@ -198,7 +295,7 @@ __device__ __forceinline__ void cta_sums(double (&v)[N]) {
 }
 
 struct Open { int tile, last, s; };                                       // a sequence that goes on behind the tile it begins in, and its last tile
-constexpr int kMostTiles = 8 * kSms;
+constexpr int kMostTiles = kSms;
 constexpr size_t join_smem(int threads) { return (size_t)(threads / 32) * (32 * 8 + 4) + kMostTiles * sizeof(Open); }
 
 __device__ __forceinline__ bool ascends(const BalanceArgs& a, int first, int step) {
@@ -362,8 +459,8 @@ constexpr size_t balance_smem() {
     return (size_t)(TM::kCta ? 1 : TM::kWarps) * L * V * 4 + (size_t)L * V * 4;
 }
 
-// First step: a CTA per tile.  FUSED: the grid is one cluster, which goes on with the second.
-template <typename Z, int W, int L, int V, bool FUSED>
+// First step: a CTA per tile.  ONLY: there is one, and no second step.
+template <typename Z, int W, int L, int V, bool ONLY>
 __global__ void __launch_bounds__(Team<L, balance_threads(V)>::kThreads)
 balance_kernel(const __grid_constant__ BalanceArgs a) {
     using TM = Team<L, balance_threads(V)>;
@@ -373,6 +470,7 @@ balance_kernel(const __grid_constant__ BalanceArgs a) {
     __shared__ float room[kMostSums * TM::kWarps];
     __shared__ int32_t window[kWindow + 1];
     __shared__ int n_kept;
+    constexpr int U = V <= 8 && !TM::kCta ? 2 : 1;
     const TM team(room);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, E = a.E, k = a.k;
     const int t0 = (int)min((long long)a.T, (long long)blockIdx.x * a.rows), t1 = (int)min((long long)a.T, (long long)t0 + a.rows);
@@ -405,103 +503,73 @@ balance_kernel(const __grid_constant__ BalanceArgs a) {
 #pragma unroll
         for (int j = 0; j < V; ++j) acc[j] = 0.f;
         int mine = 0;
-        // A row's logits and first ids are requested before the row before it is worked on (unless that takes too many registers).
-        constexpr bool kAhead = V <= 16;
+        // A team takes U rows at a time: their loads are on their way together, and one's sums over the team while another's are.
         const int rows = hi - lo, row0 = TM::kCta ? 0 : warp * (32 / L), own = TM::kCta ? 0 : lane / L;
         const Z* z_row = z + ((long long)lo + row0 + own) * a.ld;
         const int32_t* id_row = a.ids + ((long long)lo + row0 + own) * k + team.lane;
-        const uint8_t* mask_row = a.mask ? a.mask + lo + row0 + own : nullptr;
         const long long z_step = TM::kTeams * a.ld, id_step = (long long)TM::kTeams * k;
-        const bool has_id = team.lane < k;
-        float v[V];
-        int id = -1;
-        bool on = false;
-        // the row that the pointers are at, row r of this sequence's
-        const auto request = [&](int r, float (&to)[V], int& to_id) {
-            const bool counts = r < rows && (!mask_row || *mask_row);
-            to_id = -1;
-            if (counts) {
-                load_row<Z, W, L, V>(z_row, E, team.lane, to);
-                if (has_id) to_id = *id_row;
-            } else {
+        for (int r = row0; r < rows; r += U * TM::kTeams) {
+            float v[U][V], mx[U], sums[2 * U];
+            bool on[U];
+            int id[U];
 #pragma unroll
-                for (int j = 0; j < V; ++j) to[j] = -INFINITY;
-            }
-            return counts;
-        };
-        const auto advance = [&] {
-            z_row += z_step;
-            id_row += id_step;
-            if (mask_row) mask_row += TM::kTeams;
-        };
-        if (kAhead && row0 < rows) {
-            on = request(row0 + own, v, id);
-            advance();
-        }
-        for (int base = row0; base < rows; base += TM::kTeams) {
-            float next[kAhead ? V : 1];
-            if constexpr (kAhead) {
+            for (int u = 0; u < U; ++u, z_row += z_step, id_row += id_step) {
+                const int at = r + u * TM::kTeams + own;
+                on[u] = at < rows;
+                id[u] = -1;
 #pragma unroll
-                for (int j = 0; j < V; ++j) next[j] = -INFINITY;
-            }
-            int next_id = -1;
-            bool next_on = false;
-            if constexpr (kAhead) {
-                if (base + TM::kTeams < rows) {
-                    next_on = request(base + TM::kTeams + own, next, next_id);
-                    advance();
+                for (int j = 0; j < V; ++j) v[u][j] = -INFINITY;
+                if (on[u]) {                                               // (a masked row too: what it holds goes nowhere)
+                    load_row<Z, W, L, V>(z_row, E, team.lane, v[u]);
+                    if (team.lane < k) id[u] = *id_row;
+                    if (a.mask) on[u] = a.mask[lo + at];
+                    if (k > L && on[u])
+                        for (int j = L; team.lane + j < k; j += L) {
+                            const int more = id_row[j];
+                            if ((unsigned)more < (unsigned)E) atomicAdd(hist + more, 1);
+                        }
                 }
-            } else {
-                on = request(base + own, v, id);
-                advance();
             }
-            if ((unsigned)id < (unsigned)E) atomicAdd(hist + id, 1);
-            if (on && k > L)
-                for (int j = team.lane + L; j < k; j += L) {
-                    const int more = a.ids[((long long)lo + base + own) * k + j];
-                    if ((unsigned)more < (unsigned)E) atomicAdd(hist + more, 1);
-                }
-            mine += on && team.lane == 0;
-            float mx[1] = {v[0]};
 #pragma unroll
-            for (int j = 1; j < V; ++j) mx[0] = fmaxf(mx[0], v[j]);
+            for (int u = 0; u < U; ++u) {
+                mx[u] = v[u][0];
+#pragma unroll
+                for (int j = 1; j < V; ++j) mx[u] = fmaxf(mx[u], v[u][j]);
+            }
             team.max(mx);
-            const float top = mx[0] == -INFINITY ? 0.f : mx[0];
-            float sum = 0.f, inv;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (on[u] && (unsigned)id[u] < (unsigned)E) atomicAdd(hist + id[u], 1);
+                mine += on[u] && team.lane == 0;
+                mx[u] = mx[u] == -INFINITY ? 0.f : mx[u];
+                float e[V];
+                sums[u] = exps_below(v[u], mx[u], e);
+                if (a.sigmoid) {
+                    float slope[V];
+                    sums[U + u] = sigmoids(v[u], fminf(mx[u], 0.f), e, slope);
+                }
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[u][j] = e[j];
+            }
             if (a.sigmoid) {
-                const float c = fminf(top, 0.f);
-                float s2[2] = {0.f, 0.f};
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    float rest;
-                    s2[0] += exp_below(v[j] - top);
-                    v[j] = scaled_sigmoid(v[j], c, rest);
-                    s2[1] += v[j];
-                }
-                team.sum(s2);
-                sum = s2[0];
-                inv = inverse(s2[1]);
+                team.sum(sums);
             } else {
-                float s1[1] = {0.f};
+                float one[U];
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    v[j] = exp_below(v[j] - top);
-                    s1[0] += v[j];
+                for (int u = 0; u < U; ++u) one[u] = sums[u];
+                team.sum(one);
+#pragma unroll
+                for (int u = 0; u < U; ++u) sums[u] = sums[U + u] = one[u];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (on[u]) {
+                    const float lse = log_sum(mx[u], sums[u]), inv = inverse(sums[U + u]);
+                    const Two scale = two(inv, inv);
+#pragma unroll
+                    for (int j = 0; j < V; j += 2) split(fma(two(v[u][j], v[u][j + 1]), scale, two(acc[j], acc[j + 1])), acc[j], acc[j + 1]);
+                    if (team.lane == 0) sq = fmaf(lse, lse, sq);
                 }
-                team.sum(s1);
-                sum = s1[0];
-                inv = inverse(sum);
-            }
-            const float lse = log_sum(top, sum);
-#pragma unroll
-            for (int j = 0; j < V; ++j) acc[j] = fmaf(v[j], inv, acc[j]);
-            if (team.lane == 0) sq = fmaf(lse, lse, sq);
-            if constexpr (kAhead) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) v[j] = next[j];
-                id = next_id;
-                on = next_on;
-            }
         }
         squares += (double)sq;
         // the sequence's (part of the) sums: over the warp's teams, over the warps
@@ -546,25 +614,23 @@ balance_kernel(const __grid_constant__ BalanceArgs a) {
     }
     double v2[2] = {loss, squares};
     cta_sums<2, TM::kThreads>(v2);
-    if constexpr (FUSED) {
-        if (gridDim.x == 1) {                                              // the only tile
-            const bool bad = __syncthreads_or(!ascends(a, tid, TM::kThreads));
-            if (tid == 0) write_losses(a, v2[0], some, v2[1], total, bad);
-            return;
-        }
-    }
-    if (tid == 0) {
+    if constexpr (ONLY) {
+        const bool bad = __syncthreads_or(!ascends(a, tid, TM::kThreads));
+        if (tid == 0) write_losses(a, v2[0], some, v2[1], total, bad);
+    } else if (tid == 0) {
         a.tile_loss[blockIdx.x] = v2[0];
         a.tile_z[blockIdx.x] = v2[1];
         a.tile_kept[blockIdx.x] = total;
         a.tile_some[blockIdx.x] = some;
         a.tile_open[blockIdx.x] = open;
     }
-    if constexpr (FUSED) {
-        __threadfence();
-        cluster_sync();
-        join_tiles<TM::kThreads>(a, (int)blockIdx.x, (int)gridDim.x, smem);
-    }
+}
+
+constexpr int kBackThreads = 256, kBackPerSm = 768;                        // threads of a CTA, of an SM: 80 registers each (128 for V = 16)
+template <int L, int V>
+__host__ __device__ constexpr int back_ctas() {
+    constexpr int threads = Team<L, kBackThreads>::kThreads, all = V <= 8 ? kBackPerSm : 512;
+    return all > threads ? all / threads : 1;
 }
 
 struct BackwardArgs {
@@ -589,9 +655,9 @@ struct BackwardArgs {
 // The chosen ones' logits are read again and their shares taken from their own largest: they may all be lost beside the row's.  What goes to
 // single experts passes through a row of shared memory that is zero between rows.
 template <typename Z, int W, int L, int V>
-__global__ void __launch_bounds__(Team<L, 512>::kThreads, V <= 8 ? 1024 / Team<L, 512>::kThreads : 1)
+__global__ void __launch_bounds__(Team<L, kBackThreads>::kThreads, back_ctas<L, V>())
 gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
-    using TM = Team<L, 512>;
+    using TM = Team<L, kBackThreads>;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ float room[kMostSums * TM::kWarps];
     __shared__ float loss_scale[2];
@@ -632,48 +698,39 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
     if (losses && t_begin < t_end) s = a.offsets ? first_ending_at(a.offsets, a.S, (int)t_begin + 1, lane) - 1 : -1;
     constexpr int kStep = TM::kCta ? 1 : 32 / L;
     const int lane_row = TM::kCta ? 0 : lane / L;
-    // a row's logits, ids and weights' gradients are requested before the row before it is worked on
     const Z* z_row = z + (t_begin + lane_row) * a.ld;
     Z* out_row = static_cast<Z*>(a.out) + (t_begin + lane_row) * a.ld_out;
-    const long long z_step = kStep * a.ld, out_step = kStep * a.ld_out;
+    const int32_t* id_row = weights ? a.ids + (t_begin + lane_row) * k + team.lane : nullptr;
+    const float* dw_row = weights ? a.d_weights + (t_begin + lane_row) * k + team.lane : nullptr;
+    const long long z_step = kStep * a.ld, out_step = kStep * a.ld_out, id_step = (long long)kStep * k;
     const bool has_id = weights && team.lane < k;
-    float v[V], d0 = 0.f;
-    int id0 = -1;
-    bool on = false;
-    const auto request = [&](long long t, const Z* row, float (&to)[V], int& id, float& d) {
-        const bool counts = t < t_end && (!a.mask || a.mask[t]);
-        id = -1;
-        if (counts) {
-            load_row<Z, W, L, V>(row, E, team.lane, to);
+    const int rows = t_end > t_begin ? (int)(t_end - t_begin) : 0;
+    float v[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = -INFINITY;
+    for (int r = 0; r < rows; r += kStep, z_row += z_step, out_row += out_step, id_row += id_step, dw_row += id_step) {
+        const bool in = r + lane_row < rows;
+        const long long t = t_begin + r + lane_row;
+        int id0 = -1;
+        float d0 = 0.f;
+        bool on = in;
+        if (in) {
+            load_row<Z, W, L, V>(z_row, E, team.lane, v);
             if (has_id) {
-                id = a.ids[t * k + team.lane];
-                d = a.d_weights[t * k + team.lane];
+                id0 = *id_row;
+                d0 = a.scale * *dw_row;
             }
-        } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j) to[j] = -INFINITY;
+            if (a.mask) on = a.mask[t];
         }
-        return counts;
-    };
-    if (t_begin < t_end) on = request(t_begin + lane_row, z_row, v, id0, d0);
-    for (long long base = t_begin; base < t_end; base += kStep, z_row += z_step, out_row += out_step) {
-        const long long t = base + lane_row;
-        const bool in = t < t_end, first = (unsigned)id0 < (unsigned)E;
+        const bool first = on && (unsigned)id0 < (unsigned)E;
         const float zj0 = first ? to_float(z_row[id0]) : 0.f;              // of this lane's chosen expert
-        d0 *= a.scale;
-        float next[V], next_d = 0.f, share0 = 0.f, rest0 = 1.f;
-        int next_id = -1;
-        bool next_on = false;
-        if (base + kStep < t_end) next_on = request(t + kStep, z_row + z_step, next, next_id, next_d);
-        else
-#pragma unroll
-            for (int j = 0; j < V; ++j) next[j] = -INFINITY;
+        float share0 = 0.f, rest0 = 1.f;
         // f(expert, its logit, scale times its weight's gradient, place) of the team's lanes' chosen experts behind the first one of each
         const auto others = [&](auto f) {
             if (on)
-                for (int j = team.lane + L; j < k; j += L) {
-                    const int id = a.ids[t * k + j];
-                    if ((unsigned)id < (unsigned)E) f(id, to_float(z_row[id]), a.scale * a.d_weights[t * k + j], j);
+                for (int j = L; team.lane + j < k; j += L) {
+                    const int id = id_row[j];
+                    if ((unsigned)id < (unsigned)E) f(id, to_float(z_row[id]), a.scale * dw_row[j], team.lane + j);
                 }
         };
         bool counts = losses && on;
@@ -691,7 +748,7 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
             }
         }
         counts = counts && s < a.S && t >= s_from;
-        float mx[2] = {v[0], -INFINITY};
+        float mx[2] = {v[0], -INFINITY};                                   // of the row, of the chosen
 #pragma unroll
         for (int j = 1; j < V; ++j) mx[0] = fmaxf(mx[0], v[j]);
         if (weights && a.renorm) {
@@ -710,25 +767,20 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
         const bool with_z = z_scale != 0.f;
         if (a.sigmoid) {
             if (losses) {
+                if (with_z) sums[2] = exps_below(v, top, dz);
+                float sg[V];
+                sums[0] = sigmoids(v, c, sg, dz);
+                Two dot = two(0.f, 0.f);
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    float rest;
-                    const float sg = scaled_sigmoid(v[j], c, rest);
-                    sums[0] += sg;
-                    sums[1] = fmaf(sg, g[j], sums[1]);
-                    dz[j] = sg * rest;
-                }
-                if (with_z)
-#pragma unroll
-                    for (int j = 0; j < V; ++j) sums[2] += exp_below(v[j] - top);
+                for (int j = 0; j < V; j += 2) dot = fma(two(sg[j], sg[j + 1]), two(g[j], g[j + 1]), dot);
+                sums[1] = both(dot);
             }
         } else {
+            sums[0] = exps_below(v, top, dz);
+            Two dot = two(0.f, 0.f);
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                dz[j] = exp_below(v[j] - top);
-                sums[0] += dz[j];
-                sums[1] = fmaf(dz[j], g[j], sums[1]);
-            }
+            for (int j = 0; j < V; j += 2) dot = fma(two(dz[j], dz[j + 1]), two(g[j], g[j + 1]), dot);
+            sums[1] = both(dot);
         }
         const auto share_of = [&](float zj, float& rest) {
             rest = 1.f;
@@ -750,7 +802,13 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
                     row_add[id] = __int_as_float(j + 1);
                 });
         }
-        team.sum(sums);
+        if (weights) {
+            team.sum(sums);
+        } else {
+            float three[3] = {sums[0], sums[1], sums[2]};
+            team.sum(three);
+            sums[0] = three[0], sums[1] = three[1], sums[2] = three[2];
+        }
         const float inv = inverse(sums[0]), mean = sums[1] * inv;
         if (weights) {
             // The chosen ones' part goes through row_add; where an expert is named twice, one after the other.
@@ -773,26 +831,38 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
                 team.sync();
                 if (on && team.lane == 0)
                     for (int j = 0; j < k; ++j) {
-                        const int id = a.ids[t * k + j];
-                        if ((unsigned)id < (unsigned)E) row_add[id] += part(to_float(z_row[id]), a.scale * a.d_weights[t * k + j]);
+                        const int id = id_row[j];
+                        if ((unsigned)id < (unsigned)E) row_add[id] += part(to_float(z_row[id]), a.scale * dw_row[j]);
                     }
             }
             team.sync();
         }
         if (a.sigmoid) {
-            const float scale = counts ? inv : 0.f;
+            if (counts) {
+                const Two scale = two(inv, inv), shift = two(-mean * inv, -mean * inv);
 #pragma unroll
-            for (int j = 0; j < V; ++j) dz[j] = losses ? dz[j] * scale * (g[j] - mean) : 0.f;
-            if (with_z && losses) {
-                const float zl = counts ? z_scale * log_sum(top, sums[2]) * inverse(sums[2]) : 0.f;
+                for (int j = 0; j < V; j += 2) split(two(dz[j], dz[j + 1]) * fma(two(g[j], g[j + 1]), scale, shift), dz[j], dz[j + 1]);
+                if (with_z) {
+                    float e[V];
+                    exps_below(v, top, e);
+                    const float zl = z_scale * log_sum(top, sums[2]) * inverse(sums[2]);
+                    const Two z2 = two(zl, zl);
 #pragma unroll
-                for (int j = 0; j < V; ++j) dz[j] = fmaf(exp_below(v[j] - top), zl, dz[j]);
+                    for (int j = 0; j < V; j += 2) split(fma(two(e[j], e[j + 1]), z2, two(dz[j], dz[j + 1])), dz[j], dz[j + 1]);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) dz[j] = 0.f;
             }
-        } else {
+        } else if (on) {
             const float zl = (counts && with_z ? z_scale * log_sum(top, sums[0]) : 0.f) - (weights && !a.renorm ? sums[4] * inv : 0.f) - (counts ? mean : 0.f);
-            const float on_g = counts ? inv : 0.f, rest = zl * inv;
+            const float on_g = counts ? inv : 0.f;
+            const Two scale = two(on_g, on_g), shift = two(zl * inv, zl * inv);
 #pragma unroll
-            for (int j = 0; j < V; ++j) dz[j] *= fmaf(on_g, g[j], rest);
+            for (int j = 0; j < V; j += 2) split(two(dz[j], dz[j + 1]) * fma(two(g[j], g[j + 1]), scale, shift), dz[j], dz[j + 1]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j) dz[j] = 0.f;
         }
         if (weights) {
 #pragma unroll
@@ -811,61 +881,50 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
             team.sync();
         }
         if (in) store_row<Z, W, L, V>(out_row, E, team.lane, dz);
-#pragma unroll
-        for (int j = 0; j < V; ++j) v[j] = next[j];
-        id0 = next_id;
-        d0 = next_d;
-        on = next_on;
     }
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------------
 
-struct Tiling { int rows, tiles; bool fused; };
-// Small calls are one cluster, whose CTAs take a tile each and then join them; others a tile per SM (two where a CTA has half of its threads).
+struct Tiling { int rows, tiles; };
+// One CTA where it has few rows in turn, else one per SM.
 Tiling tiling(int T, int E) {
     const int at_once = E <= 64 ? 128 : E <= 128 ? 64 : E <= 256 ? 32 : E <= 1024 ? 16 : 1;    // rows that a CTA has in hand
-    const long long small = T / (2 * at_once);
-    if (small <= 8) {
-        int ctas = 1;
-        while (ctas < 8 && ctas * 2 <= small) ctas *= 2;
-        const int rows = std::max(1, (T + ctas - 1) / ctas);
-        return {rows, ctas, true};
-    }
+    if (T <= kTurnsAlone * at_once) return {std::max(1, T), 1};
     const int rows = std::max(at_once, (int)(((long long)T + kSms - 1) / kSms));
-    return {rows, (int)(((long long)T + rows - 1) / rows), false};
+    return {rows, (int)(((long long)T + rows - 1) / rows)};
 }
 size_t scratch_bytes(int E, const Tiling& t) {
     return 8 * (2 * (size_t)t.tiles + 2 * kJoinCtas) + 4 * (4 * (size_t)t.tiles * E + 2 * (size_t)t.tiles + 3 * (size_t)t.tiles);
 }
 
 template <typename Z, int W, int L, int V>
-int launch_balance(const BalanceArgs& a, bool fused, cudaStream_t st) {
+int launch_balance(const BalanceArgs& a, cudaStream_t st) {
     using TM = Team<L, balance_threads(V)>;
     static SmemOnce once[2];
-    constexpr size_t smem = balance_smem<L, V>(), fused_smem = std::max(smem, join_smem(TM::kThreads));
-    if (fused) return launch(balance_kernel<Z, W, L, V, true>, (unsigned)a.tiles, TM::kThreads, a.tiles, fused_smem, once[0], st, a);
+    constexpr size_t smem = balance_smem<L, V>();
+    if (a.tiles == 1) return launch(balance_kernel<Z, W, L, V, true>, 1, TM::kThreads, 1, smem, once[0], st, a);
     const int rc = launch(balance_kernel<Z, W, L, V, false>, (unsigned)a.tiles, TM::kThreads, 1, smem, once[1], st, a);
     if (rc) return rc;
     static SmemOnce join;
     return launch(balance_join_kernel, kJoinCtas, kJoinThreads, kJoinCtas, join_smem(kJoinThreads), join, st, a);
 }
 template <typename Z, int W>
-int launch_balance(const BalanceArgs& a, bool fused, cudaStream_t st) {
-    if (a.E <= 64) return launch_balance<Z, W, 8, 8>(a, fused, st);
-    if (a.E <= 128) return launch_balance<Z, W, 16, 8>(a, fused, st);
-    if (a.E <= 256) return launch_balance<Z, W, 32, 8>(a, fused, st);
-    if (a.E <= 512) return launch_balance<Z, W, 32, 16>(a, fused, st);
-    if (a.E <= 1024) return launch_balance<Z, W, 32, 32>(a, fused, st);
-    return launch_balance<Z, W, 512, 8>(a, fused, st);
+int launch_balance(const BalanceArgs& a, cudaStream_t st) {
+    if (a.E <= 64) return launch_balance<Z, W, 8, 8>(a, st);
+    if (a.E <= 128) return launch_balance<Z, W, 16, 8>(a, st);
+    if (a.E <= 256) return launch_balance<Z, W, 32, 8>(a, st);
+    if (a.E <= 512) return launch_balance<Z, W, 32, 16>(a, st);
+    if (a.E <= 1024) return launch_balance<Z, W, 32, 32>(a, st);
+    return launch_balance<Z, W, 512, 8>(a, st);
 }
 
 template <typename Z, int W, int L, int V>
 int launch_backward(BackwardArgs a, cudaStream_t st) {
-    using TM = Team<L, 512>;
+    using TM = Team<L, kBackThreads>;
     static SmemOnce once;
     // rows per warp (CTA): as many as leave every SM its share of the CTAs that it holds at once
-    constexpr int at_once = TM::kCta ? 1 : 32 / L, per_sm = V <= 8 ? 1024 / TM::kThreads : 1;
+    constexpr int at_once = TM::kCta ? 1 : 32 / L, per_sm = back_ctas<L, V>();
     const long long units = (long long)kSms * per_sm * (TM::kCta ? 1 : TM::kWarps);
     const long long turns = ((long long)a.T + units * at_once - 1) / (units * at_once);
     a.rows = (int)std::min<long long>(turns * at_once, a.T);
@@ -926,8 +985,8 @@ extern "C" int exmoe_balance_loss(const exmoe_shape* shape, const exmoe_gate* ga
     a.tile_open = a.tile_some + n;
     cudaStream_t st = (cudaStream_t)stream;
     const bool fours = in_fours(logits, row_stride, T, g.E, es);
-    if (type == EXMOE_F32) return fours ? launch_balance<float, 4>(a, t.fused, st) : launch_balance<float, 1>(a, t.fused, st);
-    return fours ? launch_balance<__nv_bfloat16, 4>(a, t.fused, st) : launch_balance<__nv_bfloat16, 1>(a, t.fused, st);
+    if (type == EXMOE_F32) return fours ? launch_balance<float, 4>(a, st) : launch_balance<float, 1>(a, st);
+    return fours ? launch_balance<__nv_bfloat16, 4>(a, st) : launch_balance<__nv_bfloat16, 1>(a, st);
 }
 
 extern "C" int exmoe_gate_backward(const exmoe_shape* shape, const exmoe_gate* gate, const void* logits, int type, int64_t row_stride, const int32_t* topk_ids,
