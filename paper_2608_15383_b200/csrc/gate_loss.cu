@@ -266,7 +266,7 @@ struct BalanceArgs {
     int32_t* part_counts;              // [tiles][2][E]
     int32_t* part_kept;                // [tiles][2]
     int32_t *tile_kept, *tile_some;    // [tiles] tokens that count; its sequences that have any
-    int32_t* tile_open;                // [tiles] the sequence that begins in it and goes on behind it, or -1
+    int32_t* tile_open;                // [tiles][2] the sequence that begins in it and goes on behind it, or -1, and its last tile
 };
 
 __device__ __forceinline__ float loss_factor(int E, int k, int n) { return n ? (float)E / ((float)k * (float)n * (float)n) : 0.f; }
@@ -340,7 +340,7 @@ __device__ __forceinline__ void join_tiles(const BalanceArgs& a, int cta, int ct
         __syncthreads();
     } else {
         for (int t0 = 0; t0 < a.tiles; t0 += THREADS) {
-            const int t = t0 + tid, s = t < a.tiles ? __ldcg(a.tile_open + t) : -1;
+            const int t = t0 + tid, s = t < a.tiles ? __ldcg(a.tile_open + 2 * t) : -1, last = t < a.tiles ? __ldcg(a.tile_open + 2 * t + 1) : 0;
             const unsigned mine = __ballot_sync(0xffffffffu, s >= 0);
             __syncthreads();
             if (lane == 0) before[warp + 1] = __popc(mine);
@@ -351,7 +351,7 @@ __device__ __forceinline__ void join_tiles(const BalanceArgs& a, int cta, int ct
                 if (w < warp) at += before[w + 1];
                 all += before[w + 1];
             }
-            if (s >= 0) open[at] = Open{t, (min(max(__ldcg(a.offsets + s + 1), 1), a.T) - 1) / a.rows, s};
+            if (s >= 0) open[at] = Open{t, last, s};
             n_open += all;
         }
         __syncthreads();
@@ -372,7 +372,7 @@ __device__ __forceinline__ void join_tiles(const BalanceArgs& a, int cta, int ct
         const int e = min(32 * c + lane, a.E - 1);
         sum = 0.f;
         count = n = 0;
-        constexpr int kFlight = 10;
+        constexpr int kFlight = 16;
         for (int t0 = o.tile + first; t0 <= o.last; t0 += kFlight * step) {
             float f[kFlight];
             int m[kFlight], l[kFlight];
@@ -451,19 +451,17 @@ balance_join_kernel(const __grid_constant__ BalanceArgs a) {
     join_tiles<kJoinThreads>(a, (int)blockIdx.x, (int)gridDim.x, smem);
 }
 
-// Threads of a CTA: as many as registers allow (three rows' worth of V per lane: this one's, the next one's, the sums).
-__host__ __device__ constexpr int balance_threads(int V) { return V <= 8 ? 1024 : 512; }
-template <int L, int V>
+template <int L, int V, int THREADS>
 constexpr size_t balance_smem() {
-    using TM = Team<L, balance_threads(V)>;
+    using TM = Team<L, THREADS>;
     return (size_t)(TM::kCta ? 1 : TM::kWarps) * L * V * 4 + (size_t)L * V * 4;
 }
 
 // First step: a CTA per tile.  ONLY: there is one, and no second step.
-template <typename Z, int W, int L, int V, bool ONLY>
-__global__ void __launch_bounds__(Team<L, balance_threads(V)>::kThreads)
+template <typename Z, int W, int L, int V, int THREADS, bool ONLY>
+__global__ void __launch_bounds__(Team<L, THREADS>::kThreads)
 balance_kernel(const __grid_constant__ BalanceArgs a) {
-    using TM = Team<L, balance_threads(V)>;
+    using TM = Team<L, THREADS>;
     extern __shared__ __align__(16) unsigned char smem[];
     float* red = reinterpret_cast<float*>(smem);                           // [warp][L V] column sums
     int32_t* hist = reinterpret_cast<int32_t*>(red + (TM::kCta ? 1 : TM::kWarps) * L * V);   // [L V]
@@ -481,12 +479,26 @@ balance_kernel(const __grid_constant__ BalanceArgs a) {
     grid_launch_dependents();
     const Z* z = static_cast<const Z*>(a.z);
     double loss = 0.0, squares = 0.0;
-    int some = 0, total = 0, open = -1;                                    // of the tile (the same in all threads)
-    int s = a.offsets ? first_ending_at(a.offsets, a.S, t0, lane) : 0, in_window = kWindow;
+    int some = 0, total = 0, open = -1, open_last = 0;                                    // of the tile (the same in all threads)
+    int s = 0, in_window = kWindow;
+    if (a.offsets) {
+        if (a.S <= kWindow) {                                              // all of them at once
+            __shared__ int first_seq;
+            if (tid == 0) first_seq = a.S;
+            for (int i = tid; i <= a.S; i += TM::kThreads) window[i] = __ldcg(a.offsets + i);
+            __syncthreads();
+            for (int i = tid; i < a.S; i += TM::kThreads)
+                if (window[i + 1] >= t0 && (i == 0 || window[i] < t0)) atomicMin(&first_seq, i);
+            __syncthreads();
+            s = in_window = first_seq;
+        } else {
+            s = first_ending_at(a.offsets, a.S, t0, lane);
+        }
+    }
     for (; s < a.S; ++s, ++in_window) {
         int from = 0, to = a.T;
         if (a.offsets) {
-            if (in_window == kWindow) {
+            if (in_window == kWindow) {                                    // (never where all are there: S is at most that)
                 __syncthreads();
                 for (int i = tid; i <= kWindow; i += TM::kThreads) window[i] = s + i <= a.S ? __ldcg(a.offsets + s + i) : 0;
                 in_window = 0;
@@ -607,7 +619,10 @@ balance_kernel(const __grid_constant__ BalanceArgs a) {
         if (tid == 0) (whole ? a.kept : a.part_kept)[at] = n;
         total += n;
         if (whole) some += n > 0;
-        else if (from >= t0) open = s;
+        else if (from >= t0) {
+            open = s;
+            open_last = (to - 1) / a.rows;
+        }
         __syncthreads();
         if (tid == 0) n_kept = 0;
         __syncthreads();
@@ -622,7 +637,8 @@ balance_kernel(const __grid_constant__ BalanceArgs a) {
         a.tile_z[blockIdx.x] = v2[1];
         a.tile_kept[blockIdx.x] = total;
         a.tile_some[blockIdx.x] = some;
-        a.tile_open[blockIdx.x] = open;
+        a.tile_open[2 * blockIdx.x] = open;
+        a.tile_open[2 * blockIdx.x + 1] = open_last;
     }
 }
 
@@ -708,22 +724,34 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
     float v[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) v[j] = -INFINITY;
-    for (int r = 0; r < rows; r += kStep, z_row += z_step, out_row += out_step, id_row += id_step, dw_row += id_step) {
-        const bool in = r + lane_row < rows;
-        const long long t = t_begin + r + lane_row;
-        int id0 = -1;
-        float d0 = 0.f;
-        bool on = in;
-        if (in) {
-            load_row<Z, W, L, V>(z_row, E, team.lane, v);
+    // A row's ids, weights' gradients and mask come a row ahead of it, and its logits into L1.
+    int next_id = -1;
+    float next_d = 0.f;
+    bool next_on = false;
+    const auto request = [&](int r, const Z* row, const int32_t* ids, const float* dw) {
+        next_on = r + lane_row < rows;
+        next_id = -1;
+        if (next_on) {
+#pragma unroll
+            for (int j = 0; j < V / W; ++j)
+                if ((j * L + team.lane) * W < E) asm volatile("prefetch.global.L1 [%0];" ::"l"(row + (j * L + team.lane) * W));
             if (has_id) {
-                id0 = *id_row;
-                d0 = a.scale * *dw_row;
+                next_id = *ids;
+                next_d = *dw;
             }
-            if (a.mask) on = a.mask[t];
+            if (a.mask) next_on = a.mask[t_begin + r + lane_row];
         }
+    };
+    if (rows > 0) request(0, z_row, id_row, dw_row);
+    for (int r = 0; r < rows; r += kStep, z_row += z_step, out_row += out_step, id_row += id_step, dw_row += id_step) {
+        const bool in = r + lane_row < rows, on = next_on;
+        const long long t = t_begin + r + lane_row;
+        const int id0 = next_id;
+        const float d0 = a.scale * next_d;
+        if (in) load_row<Z, W, L, V>(z_row, E, team.lane, v);
         const bool first = on && (unsigned)id0 < (unsigned)E;
         const float zj0 = first ? to_float(z_row[id0]) : 0.f;              // of this lane's chosen expert
+        if (r + kStep < rows) request(r + kStep, z_row + z_step, id_row + id_step, dw_row + id_step);
         float share0 = 0.f, rest0 = 1.f;
         // f(expert, its logit, scale times its weight's gradient, place) of the team's lanes' chosen experts behind the first one of each
         const auto others = [&](auto f) {
@@ -886,37 +914,44 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
 
 // ---- host ------------------------------------------------------------------------------------------------------------
 
-struct Tiling { int rows, tiles; };
-// One CTA where it has few rows in turn, else one per SM.
-Tiling tiling(int T, int E) {
-    const int at_once = E <= 64 ? 128 : E <= 128 ? 64 : E <= 256 ? 32 : E <= 1024 ? 16 : 1;    // rows that a CTA has in hand
-    if (T <= kTurnsAlone * at_once) return {std::max(1, T), 1};
+struct Tiling { int rows, tiles; bool wide; };
+// One CTA where it has few rows in turn, else one per SM: of 512 threads, which start and meet sooner, or, for sequences of many rows and where registers
+// allow, of 1024 (us, 512 / 1024, replayed from a graph: 4096 x 64 7.4 / 8.8, 65536 x 128 in 2000 sequences 63 / 74, 131072 x 64 17.8 / 16.7).
+Tiling tiling(int T, int E, int S) {
+    const int at_once = E <= 64 ? 64 : E <= 128 ? 32 : E <= 1024 ? 16 : 1;     // rows that 512 threads have in hand
+    if (T <= kTurnsAlone * at_once) return {std::max(1, T), 1, false};
     const int rows = std::max(at_once, (int)(((long long)T + kSms - 1) / kSms));
-    return {rows, (int)(((long long)T + rows - 1) / rows)};
+    return {rows, (int)(((long long)T + rows - 1) / rows), E <= 256 && rows >= 4 * at_once && T / S >= 4 * at_once};
 }
 size_t scratch_bytes(int E, const Tiling& t) {
-    return 8 * (2 * (size_t)t.tiles + 2 * kJoinCtas) + 4 * (4 * (size_t)t.tiles * E + 2 * (size_t)t.tiles + 3 * (size_t)t.tiles);
+    return 8 * (2 * (size_t)t.tiles + 2 * kJoinCtas) + 4 * (4 * (size_t)t.tiles * E + 2 * (size_t)t.tiles + 4 * (size_t)t.tiles);
 }
 
 template <typename Z, int W, int L, int V>
-int launch_balance(const BalanceArgs& a, cudaStream_t st) {
-    using TM = Team<L, balance_threads(V)>;
-    static SmemOnce once[2];
-    constexpr size_t smem = balance_smem<L, V>();
-    if (a.tiles == 1) return launch(balance_kernel<Z, W, L, V, true>, 1, TM::kThreads, 1, smem, once[0], st, a);
-    const int rc = launch(balance_kernel<Z, W, L, V, false>, (unsigned)a.tiles, TM::kThreads, 1, smem, once[1], st, a);
+int launch_balance(const BalanceArgs& a, bool wide, cudaStream_t st) {
+    static SmemOnce once[3];
+    constexpr int threads = Team<L, 512>::kThreads;
+    constexpr size_t smem = balance_smem<L, V, 512>();
+    if (a.tiles == 1) return launch(balance_kernel<Z, W, L, V, 512, true>, 1, threads, 1, smem, once[0], st, a);
+    int rc;
+    if constexpr (L * V <= 256) {
+        if (wide) rc = launch(balance_kernel<Z, W, L, V, 1024, false>, (unsigned)a.tiles, 1024, 1, balance_smem<L, V, 1024>(), once[1], st, a);
+        else rc = launch(balance_kernel<Z, W, L, V, 512, false>, (unsigned)a.tiles, threads, 1, smem, once[2], st, a);
+    } else {
+        rc = launch(balance_kernel<Z, W, L, V, 512, false>, (unsigned)a.tiles, threads, 1, smem, once[2], st, a);
+    }
     if (rc) return rc;
     static SmemOnce join;
     return launch(balance_join_kernel, kJoinCtas, kJoinThreads, kJoinCtas, join_smem(kJoinThreads), join, st, a);
 }
 template <typename Z, int W>
-int launch_balance(const BalanceArgs& a, cudaStream_t st) {
-    if (a.E <= 64) return launch_balance<Z, W, 8, 8>(a, st);
-    if (a.E <= 128) return launch_balance<Z, W, 16, 8>(a, st);
-    if (a.E <= 256) return launch_balance<Z, W, 32, 8>(a, st);
-    if (a.E <= 512) return launch_balance<Z, W, 32, 16>(a, st);
-    if (a.E <= 1024) return launch_balance<Z, W, 32, 32>(a, st);
-    return launch_balance<Z, W, 512, 8>(a, st);
+int launch_balance(const BalanceArgs& a, bool wide, cudaStream_t st) {
+    if (a.E <= 64) return launch_balance<Z, W, 8, 8>(a, wide, st);
+    if (a.E <= 128) return launch_balance<Z, W, 16, 8>(a, wide, st);
+    if (a.E <= 256) return launch_balance<Z, W, 32, 8>(a, wide, st);
+    if (a.E <= 512) return launch_balance<Z, W, 32, 16>(a, wide, st);
+    if (a.E <= 1024) return launch_balance<Z, W, 32, 32>(a, wide, st);
+    return launch_balance<Z, W, 512, 8>(a, wide, st);
 }
 
 template <typename Z, int W, int L, int V>
@@ -957,7 +992,7 @@ int check_loss(const exmoe_shape* shape, const exmoe_gate* gate, int type, int64
 extern "C" int exmoe_balance_scratch_bytes(const exmoe_shape* shape, int T, size_t* bytes) {
     if (!shape || !bytes || T < 0 || T > kMaxTokens) return EXMOE_ERR_ARG;
     if (shape->num_experts <= 0 || shape->num_experts > kMaxExperts) return EXMOE_ERR_SHAPE;
-    *bytes = scratch_bytes(shape->num_experts, tiling(T, shape->num_experts));
+    *bytes = scratch_bytes(shape->num_experts, tiling(T, shape->num_experts, 1));   // (as many tiles whatever the sequences are)
     return EXMOE_OK;
 }
 
@@ -970,7 +1005,7 @@ extern "C" int exmoe_balance_loss(const exmoe_shape* shape, const exmoe_gate* ga
     if ((T && (!logits || !topk_ids)) || !losses || !counts || !score_sums || !kept || !scratch) return EXMOE_ERR_ARG;
     const int es = type == EXMOE_F32 ? 4 : 2;
     if (!aligned(es, logits) || !aligned(4, topk_ids, offsets, losses, counts, score_sums, kept) || !aligned(8, scratch)) return EXMOE_ERR_ARG;
-    const Tiling t = tiling(T, g.E);
+    const Tiling t = tiling(T, g.E, num_sequences);
     BalanceArgs a{logits, row_stride, topk_ids, mask, offsets, num_sequences, T, g.E, g.k, g.sigmoid, t.rows, t.tiles, losses, counts, score_sums, kept};
     double* d = static_cast<double*>(scratch);
     const size_t n = (size_t)t.tiles;
@@ -985,8 +1020,8 @@ extern "C" int exmoe_balance_loss(const exmoe_shape* shape, const exmoe_gate* ga
     a.tile_open = a.tile_some + n;
     cudaStream_t st = (cudaStream_t)stream;
     const bool fours = in_fours(logits, row_stride, T, g.E, es);
-    if (type == EXMOE_F32) return fours ? launch_balance<float, 4>(a, st) : launch_balance<float, 1>(a, st);
-    return fours ? launch_balance<__nv_bfloat16, 4>(a, st) : launch_balance<__nv_bfloat16, 1>(a, st);
+    if (type == EXMOE_F32) return fours ? launch_balance<float, 4>(a, t.wide, st) : launch_balance<float, 1>(a, t.wide, st);
+    return fours ? launch_balance<__nv_bfloat16, 4>(a, t.wide, st) : launch_balance<__nv_bfloat16, 1>(a, t.wide, st);
 }
 
 extern "C" int exmoe_gate_backward(const exmoe_shape* shape, const exmoe_gate* gate, const void* logits, int type, int64_t row_stride, const int32_t* topk_ids,
