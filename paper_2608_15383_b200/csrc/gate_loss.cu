@@ -296,7 +296,17 @@ __device__ __forceinline__ void cta_sums(double (&v)[N]) {
 
 struct Open { int tile, last, s; };                                       // a sequence that goes on behind the tile it begins in, and its last tile
 constexpr int kMostTiles = kSms;
-constexpr size_t join_smem(int threads) { return (size_t)(threads / 32) * (32 * 8 + 4) + kMostTiles * sizeof(Open); }
+
+// A lane's expert of tile t of a sequence; zeros behind its last.
+__device__ __forceinline__ void load_part(const BalanceArgs& a, const Open& o, int chunk, int t, int lane, float& sum, int& count, int& n) {
+    sum = 0.f;
+    count = n = 0;
+    if (t > o.last) return;
+    const size_t at = 2 * (size_t)t + (t == o.tile), e = at * a.E + min(32 * chunk + lane, a.E - 1);
+    sum = __ldcg(a.part_sums + e);
+    count = __ldcg(a.part_counts + e);
+    n = __ldcg(a.part_kept + at);
+}
 
 __device__ __forceinline__ bool ascends(const BalanceArgs& a, int first, int step) {
     bool ok = true;
@@ -312,50 +322,47 @@ __device__ __forceinline__ void write_losses(const BalanceArgs& a, double balanc
     a.losses[1] = wrong ? NAN : n > 0 ? (float)(squares / n) : 0.f;
 }
 
-// Second step: the sequences that tiles share, and the losses.  By the CTAs of one cluster.
-template <int THREADS>
-__device__ __forceinline__ void join_tiles(const BalanceArgs& a, int cta, int ctas, unsigned char* smem) {
-    constexpr int WARPS = THREADS / 32;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    float* red_sum = reinterpret_cast<float*>(smem);                       // [WARPS][32]
-    int32_t* red_count = reinterpret_cast<int32_t*>(red_sum + 32 * WARPS); // [WARPS][32]
-    int32_t* red_kept = red_count + 32 * WARPS;                            // [WARPS]
-    Open* open = reinterpret_cast<Open*>(red_kept + WARPS);                // [kMostTiles], in the order of their tiles
-    __shared__ int before[WARPS + 1];
+// Second step: the sequences that tiles share, and the losses.  A cluster, whose CTAs have a part each: a warp per 32 experts of a sequence, or several where there are few
+// of these.  Bound by the latencies of what depends on one another: the wait, the list, the
+// parts, the exchange.
+__global__ void __launch_bounds__(kJoinThreads)
+balance_join_kernel(const __grid_constant__ BalanceArgs a) {
+    constexpr int WARPS = kJoinThreads / 32;
+    __shared__ float red_sum[WARPS][32];
+    __shared__ int32_t red_count[WARPS][32], red_kept[WARPS], before[(kMostTiles + 31) / 32];
+    __shared__ Open open[kMostTiles];                                      // in the order of their tiles
+    const int cta = (int)blockIdx.x, ctas = (int)gridDim.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    grid_dependency_wait();
+    grid_launch_dependents();
     const int chunks = (a.E + 31) / 32;
     // what the tiles have found of the losses, on its way while the rest is added up: by the first CTA
-    double z = 0.0, n_all = 0.0, loss = 0.0, some = 0.0;
-    if (cta == 0)
-        for (int t = tid; t < a.tiles; t += THREADS) {
-            loss += __ldcg(a.tile_loss + t);
-            z += __ldcg(a.tile_z + t);
-            n_all += (double)__ldcg(a.tile_kept + t);
-            some += (double)__ldcg(a.tile_some + t);
-        }
-    int n_open = 0;
+    double tile_loss = 0.0, tile_z = 0.0, tile_kept = 0.0, tile_some = 0.0;
+    if (cta == 0 && tid < a.tiles) {
+        tile_loss = __ldcg(a.tile_loss + tid);
+        tile_z = __ldcg(a.tile_z + tid);
+        tile_kept = (double)__ldcg(a.tile_kept + tid);
+        tile_some = (double)__ldcg(a.tile_some + tid);
+    }
+    int n_open;
     if (!a.offsets) {
-        const int last = (max(a.T, 1) - 1) / a.rows;                       // (a cluster may have tiles behind it, without tokens)
-        n_open = last > 0;
-        if (tid == 0) open[0] = Open{0, last, 0};
-        __syncthreads();
+        n_open = a.tiles > 1;
     } else {
-        for (int t0 = 0; t0 < a.tiles; t0 += THREADS) {
-            const int t = t0 + tid, s = t < a.tiles ? __ldcg(a.tile_open + 2 * t) : -1, last = t < a.tiles ? __ldcg(a.tile_open + 2 * t + 1) : 0;
-            const unsigned mine = __ballot_sync(0xffffffffu, s >= 0);
-            __syncthreads();
-            if (lane == 0) before[warp + 1] = __popc(mine);
-            __syncthreads();
-            int at = n_open + __popc(mine & ((1u << lane) - 1u)), all = 0;
+        static_assert(kMostTiles <= kJoinThreads, "a tile per thread");
+        const int s = tid < a.tiles ? __ldcg(a.tile_open + 2 * tid) : -1, last = tid < a.tiles ? __ldcg(a.tile_open + 2 * tid + 1) : 0;
+        const unsigned mine = __ballot_sync(0xffffffffu, s >= 0);
+        if (lane == 0 && warp < (kMostTiles + 31) / 32) before[warp] = __popc(mine);
+        __syncthreads();
+        int at = __popc(mine & ((1u << lane) - 1u));
+        n_open = 0;
 #pragma unroll
-            for (int w = 0; w < WARPS; ++w) {
-                if (w < warp) at += before[w + 1];
-                all += before[w + 1];
-            }
-            if (s >= 0) open[at] = Open{t, last, s};
-            n_open += all;
+        for (int w = 0; w < (kMostTiles + 31) / 32; ++w) {
+            if (w < warp) at += before[w];
+            n_open += before[w];
         }
+        if (s >= 0) open[at] = Open{tid, last, s};
         __syncthreads();
     }
+    double loss = 0.0, some = 0.0;
     const auto finish = [&](int s, int c, float sum, int count, int n) {   // by one warp
         const int e = 32 * c + lane;
         if (e < a.E) {
@@ -368,26 +375,23 @@ __device__ __forceinline__ void join_tiles(const BalanceArgs& a, int cta, int ct
             some += n > 0;
         }
     };
-    const auto add_tiles = [&](const Open& o, int c, int first, int step, float& sum, int& count, int& n) {
-        const int e = min(32 * c + lane, a.E - 1);
-        sum = 0.f;
-        count = n = 0;
-        constexpr int kFlight = 16;
-        for (int t0 = o.tile + first; t0 <= o.last; t0 += kFlight * step) {
+    // An item: 32 experts of a sequence.  As many warps share its tiles (a power of two, inside a CTA) as there are for each.
+    const int items = n_open * chunks, all = ctas * WARPS;
+    int share = 1;
+    while (share < WARPS && 2 * share * items <= all) share *= 2;
+    const int group = (cta * WARPS + warp) / share, in_group = warp & (share - 1), groups = all / share;
+    for (int i0 = 0; i0 < items; i0 += groups) {
+        const int i = i0 + group, at = i < items ? i / chunks : 0, c = i - at * chunks;
+        Open o{0, -1, 0};
+        if (i < items) o = a.offsets ? open[at] : Open{0, a.tiles - 1, 0};
+        constexpr int kFlight = 12;
+        float sum = 0.f;
+        int count = 0, n = 0;
+        for (int t0 = o.tile + in_group; t0 <= o.last; t0 += kFlight * share) {
             float f[kFlight];
             int m[kFlight], l[kFlight];
 #pragma unroll
-            for (int u = 0; u < kFlight; ++u) {
-                const int t = t0 + u * step;
-                f[u] = 0.f;
-                m[u] = l[u] = 0;
-                if (t <= o.last) {
-                    const size_t at = 2 * (size_t)t + (t == o.tile);
-                    f[u] = __ldcg(a.part_sums + at * a.E + e);
-                    m[u] = __ldcg(a.part_counts + at * a.E + e);
-                    l[u] = __ldcg(a.part_kept + at);
-                }
-            }
+            for (int u = 0; u < kFlight; ++u) load_part(a, o, c, t0 + u * share, lane, f[u], m[u], l[u]);
 #pragma unroll
             for (int u = 0; u < kFlight; ++u) {
                 sum += f[u];
@@ -395,60 +399,39 @@ __device__ __forceinline__ void join_tiles(const BalanceArgs& a, int cta, int ct
                 n += l[u];
             }
         }
-    };
-    // A warp per 32 experts of a sequence; where there are few of these, or the sequence covers many tiles, a CTA's warps share its tiles.
-    const int far = n_open * chunks >= 64 ? 64 : 4;
-    for (int i = cta * WARPS + warp; i < n_open * chunks; i += ctas * WARPS) {
-        const Open o = open[i / chunks];
-        if (o.last - o.tile >= far) continue;
-        float sum;
-        int count, n;
-        add_tiles(o, i % chunks, 0, 1, sum, count, n);
-        finish(o.s, i % chunks, sum, count, n);
-    }
-    for (int i = cta; i < n_open * chunks; i += ctas) {
-        const Open o = open[i / chunks];
-        if (o.last - o.tile < far) continue;
-        float sum;
-        int count, n;
-        add_tiles(o, i % chunks, warp, WARPS, sum, count, n);
-        red_sum[32 * warp + lane] = sum;
-        red_count[32 * warp + lane] = count;
-        if (lane == 0) red_kept[warp] = n;
-        __syncthreads();
-        if (warp == 0) {
-#pragma unroll
-            for (int w = 1; w < WARPS; ++w) {
-                sum += red_sum[32 * w + lane];
-                count += red_count[32 * w + lane];
-                n += red_kept[w];
-            }
-            finish(o.s, i % chunks, sum, count, n);
+        if (share > 1) {
+            red_sum[warp][lane] = sum;
+            red_count[warp][lane] = count;
+            if (lane == 0) red_kept[warp] = n;
+            __syncthreads();
+            if (in_group == 0)
+                for (int w = 1; w < share; ++w) {
+                    sum += red_sum[warp + w][lane];
+                    count += red_count[warp + w][lane];
+                    n += red_kept[warp + w];
+                }
+            __syncthreads();
         }
-        __syncthreads();
+        if (i < items && in_group == 0) finish(o.s, c, sum, count, n);
     }
-    const bool bad = __syncthreads_or(!ascends(a, cta * THREADS + tid, ctas * THREADS));
-    double v[4] = {loss, some, z, n_all};
-    cta_sums<4, THREADS>(v);
-    if (tid == 0) {
+    const bool bad = __syncthreads_or(!ascends(a, cta * kJoinThreads + tid, ctas * kJoinThreads));
+    double v[4] = {loss + tile_loss, some + tile_some, tile_z, tile_kept};
+    cta_sums<4, kJoinThreads>(v);
+    if (bad) v[1] = -1e300;
+    if (cta && tid == 0) {
         __stcg(a.joined + cta, v[0]);
-        __stcg(a.joined + kJoinCtas + cta, bad ? -1.0 : v[1]);
+        __stcg(a.joined + kJoinCtas + cta, v[1]);
     }
-    cluster_sync();
+    if (ctas > 1) cluster_sync();
     if (cta || warp) return;
-    double balance = lane < ctas ? __ldcg(a.joined + lane) : 0.0, n_seq = lane < ctas ? __ldcg(a.joined + kJoinCtas + lane) : 0.0;
-    const bool wrong = __any_sync(0xffffffffu, n_seq < 0.0);
-    balance = warp_sum_f64(balance);
-    n_seq = warp_sum_f64(n_seq);
-    if (lane == 0) write_losses(a, balance, n_seq, v[2], v[3], wrong);
-}
-
-__global__ void __launch_bounds__(kJoinThreads)
-balance_join_kernel(const __grid_constant__ BalanceArgs a) {
-    extern __shared__ __align__(16) unsigned char smem[];
-    grid_dependency_wait();
-    grid_launch_dependents();
-    join_tiles<kJoinThreads>(a, (int)blockIdx.x, (int)gridDim.x, smem);
+    if (lane) v[0] = v[1] = 0.0;
+    if (lane > 0 && lane < ctas) {
+        v[0] = __ldcg(a.joined + lane);
+        v[1] = __ldcg(a.joined + kJoinCtas + lane);
+    }
+    v[0] = warp_sum_f64(v[0]);
+    v[1] = warp_sum_f64(v[1]);
+    if (lane == 0) write_losses(a, v[0], v[1], v[2], v[3], v[1] < 0.0);
 }
 
 template <int L, int V, int THREADS>
@@ -724,7 +707,9 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
     float v[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) v[j] = -INFINITY;
-    // A row's ids, weights' gradients and mask come a row ahead of it, and its logits into L1.
+    // With a whole warp per row, its ids, weights' gradients and mask come a row ahead of it, and its logits into L1.  (With several rows per warp that
+    // takes longer: 131072 x 64 31.9 us instead of 29.6.)
+    constexpr bool kAhead = L >= 32;
     int next_id = -1;
     float next_d = 0.f;
     bool next_on = false;
@@ -732,6 +717,7 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
         next_on = r + lane_row < rows;
         next_id = -1;
         if (next_on) {
+            if constexpr (kAhead)
 #pragma unroll
             for (int j = 0; j < V / W; ++j)
                 if ((j * L + team.lane) * W < E) asm volatile("prefetch.global.L1 [%0];" ::"l"(row + (j * L + team.lane) * W));
@@ -742,8 +728,9 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
             if (a.mask) next_on = a.mask[t_begin + r + lane_row];
         }
     };
-    if (rows > 0) request(0, z_row, id_row, dw_row);
+    if (kAhead && rows > 0) request(0, z_row, id_row, dw_row);
     for (int r = 0; r < rows; r += kStep, z_row += z_step, out_row += out_step, id_row += id_step, dw_row += id_step) {
+        if constexpr (!kAhead) request(r, z_row, id_row, dw_row);
         const bool in = r + lane_row < rows, on = next_on;
         const long long t = t_begin + r + lane_row;
         const int id0 = next_id;
@@ -751,7 +738,7 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
         if (in) load_row<Z, W, L, V>(z_row, E, team.lane, v);
         const bool first = on && (unsigned)id0 < (unsigned)E;
         const float zj0 = first ? to_float(z_row[id0]) : 0.f;              // of this lane's chosen expert
-        if (r + kStep < rows) request(r + kStep, z_row + z_step, id_row + id_step, dw_row + id_step);
+        if (kAhead && r + kStep < rows) request(r + kStep, z_row + z_step, id_row + id_step, dw_row + id_step);
         float share0 = 0.f, rest0 = 1.f;
         // f(expert, its logit, scale times its weight's gradient, place) of the team's lanes' chosen experts behind the first one of each
         const auto others = [&](auto f) {
@@ -942,7 +929,8 @@ int launch_balance(const BalanceArgs& a, bool wide, cudaStream_t st) {
     }
     if (rc) return rc;
     static SmemOnce join;
-    return launch(balance_join_kernel, kJoinCtas, kJoinThreads, kJoinCtas, join_smem(kJoinThreads), join, st, a);
+    const int ctas = a.offsets ? kJoinCtas : std::min(kJoinCtas, (a.E + 31) / 32);
+    return launch(balance_join_kernel, (unsigned)ctas, kJoinThreads, ctas, 0, join, st, a);
 }
 template <typename Z, int W>
 int launch_balance(const BalanceArgs& a, bool wide, cudaStream_t st) {
