@@ -447,6 +447,10 @@ int exmoe_debug_read_slot(exmoe_cache* cache, int layer, int slot, void* host_ou
  * barrier that nothing completes.  *gave_up gets bit 0 = the wait returned "expired", bit 1 = the abort flag was
  * raised; exmoe_status() then reports EXMOE_ERR_TIMEOUT.  Synchronous. */
 int exmoe_debug_wait_timeout(exmoe_cache* cache, long long budget_cycles, int* gave_up);
+/* The same of exmoe_linear's tensor-core kernels: one call (BF16, one matrix, rows without gaps, T > 16, d_in >= 1024), whose form is the one that the sizes have in
+ * exmoe_linear, with a barrier that nothing completes and a budget of 2,000,000 ticks.  exmoe_linear_status then reports EXMOE_ERR_TIMEOUT; what was written (no
+ * more than `out`) is not to be used.  Asynchronous on `stream`; EXMOE_ERR_SHAPE for other sizes. */
+int exmoe_debug_linear_timeout(const exmoe_linear_shape* shape, const void* x, const void* w, int T, void* out, void* stream);
 /* The same of the kernels of the gate and of the adapters that wait: one call of exmoe_route_gated's tensor-core form (E <= 64, d_model >= 1024, no bias, addend or
  * balance) and one of exmoe_lora (BF16, no base, rows without gaps, rank <= 64, T < 592, few enough tiles for clusters) with a barrier that nothing completes and a
  * budget of 2,000,000 ticks.  exmoe_gate_status and exmoe_lora_plan_status then report EXMOE_ERR_TIMEOUT; what was written is not to be used.  Asynchronous on `stream`;

@@ -89,6 +89,7 @@ _SIGNATURES = {
                            c_int64, c_void_p, c_int64, c_int, c_void_p]),
     "exmoe_debug_gate_timeout": (c_int, [POINTER(exmoe_shape), POINTER(exmoe_gate), c_void_p, c_void_p, c_int] + [c_void_p] * 3),
     "exmoe_debug_lora_timeout": (c_int, [POINTER(exmoe_lora_shape)] + [c_void_p] * 5 + [c_int, c_void_p, c_void_p]),
+    "exmoe_debug_linear_timeout": (c_int, [POINTER(exmoe_linear_shape), c_void_p, c_void_p, c_int, c_void_p, c_void_p]),
     "exmoe_cache_get_state": (c_int, [c_void_p, c_int, c_void_p, c_void_p, c_void_p, c_void_p]),
     "exmoe_debug_last_plan": (c_int, [c_void_p, c_int] + [c_void_p] * 9),
     "exmoe_debug_last_path": (c_int, [c_void_p]),

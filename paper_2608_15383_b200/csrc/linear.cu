@@ -141,9 +141,9 @@ int launch_few_tokens(const LinearArgs& a, cudaStream_t st) {
 
 }  // namespace
 
-extern "C" int exmoe_linear(const exmoe_linear_shape* shape, const void* x, int64_t ld_x, const void* w, int64_t ld_w, const float* bias, const void* w_up,
-                            int64_t ld_w_up, const float* bias_up, int T, const void* residual, int64_t ld_residual, void* out, int64_t ld_out, int type,
-                            void* stream) {
+static int linear_call(const exmoe_linear_shape* shape, const void* x, int64_t ld_x, const void* w, int64_t ld_w, const float* bias, const void* w_up,
+                       int64_t ld_w_up, const float* bias_up, int T, const void* residual, int64_t ld_residual, void* out, int64_t ld_out, int type, bool stuck,
+                       void* stream) {
     if (!shape || T < 0 || T > kMaxTokens || (type != EXMOE_F32 && type != EXMOE_BF16)) return EXMOE_ERR_ARG;
     const int K = shape->d_in, N = shape->d_out;
     if (shape->activation < EXMOE_ACT_NONE || shape->activation > EXMOE_ACT_SILU) return EXMOE_ERR_ARG;
@@ -161,9 +161,21 @@ extern "C" int exmoe_linear(const exmoe_linear_shape* shape, const void* x, int6
     const LinearArgs a{(const __nv_bfloat16*)x, (const __nv_bfloat16*)w, (const __nv_bfloat16*)w_up, bias, bias_up, residual, out, ld_x, ld_w, ld_w_up,
                        ld_residual, ld_out, T, K, N, shape->activation};
     cudaStream_t st = (cudaStream_t)stream;
+    if (stuck) return T > kFewTokens && K >= 1024 ? launch_linear_tc_stuck(a, st) : EXMOE_ERR_SHAPE;
     if (T > kFewTokens) return launch_linear_tc(a, type, st);
     if (type == EXMOE_F32) return w_up ? launch_few_tokens<float, true>(a, st) : launch_few_tokens<float, false>(a, st);
     return w_up ? launch_few_tokens<__nv_bfloat16, true>(a, st) : launch_few_tokens<__nv_bfloat16, false>(a, st);
+}
+
+extern "C" int exmoe_linear(const exmoe_linear_shape* shape, const void* x, int64_t ld_x, const void* w, int64_t ld_w, const float* bias, const void* w_up,
+                            int64_t ld_w_up, const float* bias_up, int T, const void* residual, int64_t ld_residual, void* out, int64_t ld_out, int type,
+                            void* stream) {
+    return linear_call(shape, x, ld_x, w, ld_w, bias, w_up, ld_w_up, bias_up, T, residual, ld_residual, out, ld_out, type, false, stream);
+}
+
+extern "C" int exmoe_debug_linear_timeout(const exmoe_linear_shape* shape, const void* x, const void* w, int T, void* out, void* stream) {
+    if (!shape || T == 0) return EXMOE_ERR_ARG;
+    return linear_call(shape, x, shape->d_in, w, shape->d_in, nullptr, nullptr, 0, nullptr, T, nullptr, 0, out, shape->d_out, EXMOE_BF16, true, stream);
 }
 
 }  // namespace exmoe

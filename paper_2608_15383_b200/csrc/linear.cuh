@@ -62,5 +62,6 @@ __device__ __forceinline__ void store_out(__nv_bfloat16* p, float v) { *p = __fl
 
 // More than a few tokens, on tensor cores (linear_tc.cu).
 int launch_linear_tc(const LinearArgs& a, int type, cudaStream_t st);
+int launch_linear_tc_stuck(const LinearArgs& a, cudaStream_t st);
 
 }  // namespace exmoe
