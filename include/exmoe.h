@@ -259,7 +259,7 @@ int exmoe_gate_status(void);
  *                  [offsets[s], offsets[s + 1]), which may be none; tokens outside all of them count nowhere.  With offsets that do not ascend in
  *                  [0, T] both losses are NaN and the other outputs are not to be used
  *   losses       : dev, float32 [2]        counts : dev, int32 [S, E]        score_sums : dev, float32 [S, E]        kept : dev, int32 [S]
- *   scratch      : dev, exmoe_balance_scratch_bytes(), 8-byte aligned; calls that may overlap need one each
+ *   scratch      : dev, exmoe_balance_scratch_bytes(), 8-byte aligned, NULL where that is 0; calls that may overlap need one each
  * All outputs are fully overwritten and overlap nothing.  Uses num_experts (<= 4096), top_k, and of the gate score (the whole gate is checked).  Sums are binary32 in a
  * fixed order: the same call gives the same bits.  Asynchronous on `stream`; allocates nothing. */
 int exmoe_balance_scratch_bytes(const exmoe_shape* shape, int T, size_t* bytes);

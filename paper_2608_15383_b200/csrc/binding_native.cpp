@@ -498,11 +498,11 @@ PyObject* balance_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const OnStream on(a[7], st);
         if (a[6] == Py_None)
             for (int i = 0; i < 4; ++i) o[i] = empty_on(*in.z, sizes[i], types[i]);
-        const at::Tensor scratch = empty_on(*in.z, {(int64_t)bytes}, at::kByte);
+        const at::Tensor scratch = bytes ? empty_on(*in.z, {(int64_t)bytes}, at::kByte) : at::Tensor();
         Py_BEGIN_ALLOW_THREADS
         rc = g_balance_loss(&in.s, &in.g, in.z->data_ptr(), in.type(), pitch(*in.z), in.ids_data(), in.mask_data(), in.offsets_data(), in.S, in.T,
                             static_cast<float*>(o[0].data_ptr()), static_cast<int32_t*>(o[1].data_ptr()), static_cast<float*>(o[2].data_ptr()),
-                            static_cast<int32_t*>(o[3].data_ptr()), scratch.data_ptr(), st);
+                            static_cast<int32_t*>(o[3].data_ptr()), bytes ? scratch.data_ptr() : nullptr, st);
         Py_END_ALLOW_THREADS
         if (rc) return PyLong_FromLong(rc);
         if (a[6] != Py_None) return Py_NewRef(a[6]);

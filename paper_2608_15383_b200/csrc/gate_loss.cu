@@ -911,6 +911,7 @@ Tiling tiling(int T, int E, int S) {
     return {rows, (int)(((long long)T + rows - 1) / rows), E <= 256 && rows >= 4 * at_once && T / S >= 4 * at_once};
 }
 size_t scratch_bytes(int E, const Tiling& t) {
+    if (t.tiles == 1) return 0;
     return 8 * (2 * (size_t)t.tiles + 2 * kJoinCtas) + 4 * (4 * (size_t)t.tiles * E + 2 * (size_t)t.tiles + 4 * (size_t)t.tiles);
 }
 
@@ -990,10 +991,10 @@ extern "C" int exmoe_balance_loss(const exmoe_shape* shape, const exmoe_gate* ga
     GateArgs g;
     const int rc = check_loss(shape, gate, type, row_stride, T, num_sequences, offsets, &g);
     if (rc) return rc;
-    if ((T && (!logits || !topk_ids)) || !losses || !counts || !score_sums || !kept || !scratch) return EXMOE_ERR_ARG;
+    const Tiling t = tiling(T, g.E, num_sequences);
+    if ((T && (!logits || !topk_ids)) || !losses || !counts || !score_sums || !kept || (!scratch && scratch_bytes(g.E, t))) return EXMOE_ERR_ARG;
     const int es = type == EXMOE_F32 ? 4 : 2;
     if (!aligned(es, logits) || !aligned(4, topk_ids, offsets, losses, counts, score_sums, kept) || !aligned(8, scratch)) return EXMOE_ERR_ARG;
-    const Tiling t = tiling(T, g.E, num_sequences);
     BalanceArgs a{logits, row_stride, topk_ids, mask, offsets, num_sequences, T, g.E, g.k, g.sigmoid, t.rows, t.tiles, losses, counts, score_sums, kept};
     double* d = static_cast<double*>(scratch);
     const size_t n = (size_t)t.tiles;

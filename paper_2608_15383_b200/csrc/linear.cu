@@ -24,7 +24,6 @@ linear_few_kernel(const __grid_constant__ LinearArgs a, int rows, int groups) {
     constexpr int kFewThreads = 32 * WARPS, kFewWarps = WARPS, kAhead = (NT == 1 ? 64 : 32) / WARPS;
     __shared__ float part[2][kFewWarps][NT][16][9];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
-    const long long t0 = (long long)blockIdx.y * 8 * NT;
     {   // into L2, before the wait (the kernel in front may be writing them: L2 has what it writes)
         const long long n0 = (long long)blockIdx.x * rows;
         const int n_rows = (int)min((long long)rows, a.N - n0);
@@ -52,7 +51,7 @@ linear_few_kernel(const __grid_constant__ LinearArgs a, int rows, int groups) {
             vb[u] = in && row_b ? *reinterpret_cast<const uint4*>(wb + k) : zero;
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
-                const long long t = t0 + 8 * i + g;
+                const int t = 8 * i + g;
                 vx[u][i] = in && t < a.T ? *reinterpret_cast<const uint4*>(a.x + t * a.ld_x + 8 * c + k) : zero;
             }
         }
@@ -89,8 +88,8 @@ linear_few_kernel(const __grid_constant__ LinearArgs a, int rows, int groups) {
         const int n_rows = (int)min((long long)rows, a.N - n0);
         for (int i = tid; i < NT * 8 * n_rows; i += kFewThreads) {
             const int r = i % n_rows, tt = i / n_rows, nt = tt >> 3, col = tt & 7;
-            const long long n = n0 + r, t = t0 + tt;
-            if (t >= a.T) continue;
+            const long long n = n0 + r;
+            if (tt >= a.T) continue;
             float v = 0.f, u = 0.f;
 #pragma unroll
             for (int w = 0; w < kFewWarps; ++w) {
@@ -99,8 +98,8 @@ linear_few_kernel(const __grid_constant__ LinearArgs a, int rows, int groups) {
             }
             v = activate(v + (a.bias ? a.bias[n] : 0.f), a.act);
             if (GATED) v *= u + (a.bias_up ? a.bias_up[n] : 0.f);
-            if (a.residual) v += load_out<O>(a.residual, t * a.ld_res + n);
-            store_out(static_cast<O*>(a.out) + t * a.ld_out + n, v);
+            if (a.residual) v += load_out<O>(a.residual, tt * a.ld_res + n);
+            store_out(static_cast<O*>(a.out) + tt * a.ld_out + n, v);
         }
         group = next;
     }
@@ -114,7 +113,7 @@ int launch_few(const LinearArgs& a, cudaStream_t st) {
     const long long turns = (a.N + most * ctas - 1) / (most * ctas), rows = (a.N + ctas * turns - 1) / (ctas * turns);
     cudaLaunchConfig_t lc{};
     const long long groups = (a.N + rows - 1) / rows;
-    lc.gridDim = dim3((unsigned)std::min(groups, ctas), (unsigned)((a.T + 8 * NT - 1) / (8 * NT)));
+    lc.gridDim = dim3((unsigned)std::min(groups, ctas));
     lc.blockDim = dim3(32 * WARPS);
     lc.stream = st;
     cudaLaunchAttribute attr[1];
