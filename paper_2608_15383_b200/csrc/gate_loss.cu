@@ -666,35 +666,10 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
     for (int i = tid; i < TM::kTeams * L * V; i += TM::kThreads) reinterpret_cast<float*>(smem)[i] = 0.f;
     grid_dependency_wait();
     grid_launch_dependents();
-    if (a.d_losses) {                                                      // S' and N
-        double v[2] = {0.0, 0.0};
-        if (a.S == 1) {
-            v[0] = (double)a.kept[0];
-            v[1] = v[0] > 0;
-        } else {
-            for (int s = tid; s < a.S; s += TM::kThreads) {
-                const int m = a.kept[s];
-                v[0] += m;
-                v[1] += m > 0;
-            }
-            cta_sums<2, TM::kThreads>(v);
-        }
-        if (tid == 0) {
-            loss_scale[0] = v[1] > 0 ? a.d_losses[0] * (float)E / ((float)v[1] * (float)k) : 0.f;
-            loss_scale[1] = v[0] > 0 ? 2.f * a.d_losses[1] / (float)v[0] : 0.f;
-        }
-    }
-    __syncthreads();
     const long long unit = TM::kCta ? blockIdx.x : (long long)blockIdx.x * TM::kWarps + warp;
     const long long t_begin = unit * a.rows, t_end = min((long long)a.T, t_begin + a.rows);
     const bool losses = a.d_losses != nullptr, weights = a.d_weights != nullptr, one = k <= L;
-    const float balance = losses ? loss_scale[0] : 0.f, z_scale = losses ? loss_scale[1] : 0.f;
     const Z* z = static_cast<const Z*>(a.z);
-    float g[V];                                                            // G of the sequence
-#pragma unroll
-    for (int j = 0; j < V; ++j) g[j] = 0.f;
-    int s = -1, s_from = 0, s_to = 0;
-    if (losses && t_begin < t_end) s = a.offsets ? first_ending_at(a.offsets, a.S, (int)t_begin + 1, lane) - 1 : -1;
     constexpr int kStep = TM::kCta ? 1 : 32 / L;
     const int lane_row = TM::kCta ? 0 : lane / L;
     const Z* z_row = z + (t_begin + lane_row) * a.ld;
@@ -708,7 +683,7 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
 #pragma unroll
     for (int j = 0; j < V; ++j) v[j] = -INFINITY;
     // With a whole warp per row, its ids, weights' gradients and mask come a row ahead of it, and its logits into L1.  (With several rows per warp that
-    // takes longer: 131072 x 64 31.9 us instead of 29.6.)
+    // takes longer: 131072 x 64 31.9 us instead of 29.6.)  The first one is on its way before the sums over the sequences.
     constexpr bool kAhead = L >= 32;
     int next_id = -1;
     float next_d = 0.f;
@@ -729,6 +704,31 @@ gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
         }
     };
     if (kAhead && rows > 0) request(0, z_row, id_row, dw_row);
+    if (a.d_losses) {                                                      // S' and N
+        double all[2] = {0.0, 0.0};
+        if (a.S == 1) {
+            all[0] = (double)a.kept[0];
+            all[1] = all[0] > 0;
+        } else {
+            for (int s = tid; s < a.S; s += TM::kThreads) {
+                const int m = a.kept[s];
+                all[0] += m;
+                all[1] += m > 0;
+            }
+            cta_sums<2, TM::kThreads>(all);
+        }
+        if (tid == 0) {
+            loss_scale[0] = all[1] > 0 ? a.d_losses[0] * (float)E / ((float)all[1] * (float)k) : 0.f;
+            loss_scale[1] = all[0] > 0 ? 2.f * a.d_losses[1] / (float)all[0] : 0.f;
+        }
+    }
+    __syncthreads();
+    const float balance = losses ? loss_scale[0] : 0.f, z_scale = losses ? loss_scale[1] : 0.f;
+    float g[V];                                                            // G of the sequence
+#pragma unroll
+    for (int j = 0; j < V; ++j) g[j] = 0.f;
+    int s = -1, s_from = 0, s_to = 0;
+    if (losses && t_begin < t_end) s = a.offsets ? first_ending_at(a.offsets, a.S, (int)t_begin + 1, lane) - 1 : -1;
     for (int r = 0; r < rows; r += kStep, z_row += z_step, out_row += out_step, id_row += id_step, dw_row += id_step) {
         if constexpr (!kAhead) request(r, z_row, id_row, dw_row);
         const bool in = r + lane_row < rows, on = next_on;
