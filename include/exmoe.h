@@ -260,7 +260,7 @@ int exmoe_gate_status(void);
  *                  [0, T] both losses are NaN and the other outputs are not to be used
  *   losses       : dev, float32 [2]        counts : dev, int32 [S, E]        score_sums : dev, float32 [S, E]        kept : dev, int32 [S]
  *   scratch      : dev, exmoe_balance_scratch_bytes(), 8-byte aligned, NULL where that is 0; calls that may overlap need one each
- * All outputs are fully overwritten and overlap nothing.  Uses num_experts (<= 4096), top_k, and of the gate score (the whole gate is checked).  Sums are binary32 in a
+ * All outputs are fully overwritten; they and scratch overlap neither one another nor an input (EXMOE_ERR_ARG).  Uses num_experts (<= 4096), top_k, and of the gate score (the whole gate is checked).  Sums are binary32 in a
  * fixed order: the same call gives the same bits.  Asynchronous on `stream`; allocates nothing. */
 int exmoe_balance_scratch_bytes(const exmoe_shape* shape, int T, size_t* bytes);
 int exmoe_balance_loss(const exmoe_shape* shape, const exmoe_gate* gate, const void* logits, int type, int64_t row_stride, const int32_t* topk_ids,
@@ -273,7 +273,8 @@ int exmoe_balance_loss(const exmoe_shape* shape, const exmoe_gate* gate, const v
  *   logits, type, row_stride, topk_ids, mask, offsets, num_sequences : as above; topk_ids may be NULL without d_weights.  A masked token's gradient
  *                  is zero.  An id outside [0, E) has no weight, an expert that a token names twice both of them
  *   d_weights    : dev, float32 [T, k], or NULL        d_losses : dev, float32 [2], or NULL
- *   counts, kept : dev, of exmoe_balance_loss (or summed over the processes of a job); needed with d_losses
+ *   counts, kept : dev, of exmoe_balance_loss (or summed over the processes of a job); needed with d_losses.  With offsets that do not ascend in [0, T] the
+ *                  gradient is not to be used either
  *   d_logits     : dev, [T, E] of `type`, rows d_row_stride elements apart, fully overwritten; overlaps no input (EXMOE_ERR_ARG)
  * Uses of the gate score, renormalise and weight_scale.  Asynchronous on `stream`; allocates nothing; T = 0 is a no-op. */
 int exmoe_gate_backward(const exmoe_shape* shape, const exmoe_gate* gate, const void* logits, int type, int64_t row_stride, const int32_t* topk_ids,

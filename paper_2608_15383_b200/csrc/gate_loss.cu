@@ -21,7 +21,7 @@ namespace {
 constexpr int kMaxTokens = 1 << 29, kMaxExperts = 4096;
 constexpr int kSms = 148;
 constexpr int kJoinThreads = 512, kJoinCtas = 8, kWindow = 512;
-constexpr int kTurnsAlone = 8;
+constexpr int kTurnsAlone = 8;                                             // rows in turn up to which one CTA is faster than tiles and a second step
 
 template <typename Z> __device__ __forceinline__ float to_float(Z v);
 template <> __device__ __forceinline__ float to_float<float>(float v) { return v; }
@@ -323,8 +323,7 @@ __device__ __forceinline__ void write_losses(const BalanceArgs& a, double balanc
 }
 
 // Second step: the sequences that tiles share, and the losses.  A cluster, whose CTAs have a part each: a warp per 32 experts of a sequence, or several where there are few
-// of these.  Bound by the latencies of what depends on one another: the wait, the list, the
-// parts, the exchange.
+// of these.  Bound by the latencies of what depends on one another: the wait, the list, the parts, the exchange.  About 4 us of a replayed call.
 __global__ void __launch_bounds__(kJoinThreads)
 balance_join_kernel(const __grid_constant__ BalanceArgs a) {
     constexpr int WARPS = kJoinThreads / 32;
@@ -440,7 +439,9 @@ constexpr size_t balance_smem() {
     return (size_t)(TM::kCta ? 1 : TM::kWarps) * L * V * 4 + (size_t)L * V * 4;
 }
 
-// First step: a CTA per tile.  ONLY: there is one, and no second step.
+// First step: a CTA per tile, so that an SM has one start and one end; the offsets of a few hundred sequences are read at once.  ONLY: there is one tile, and no second step.
+// 131072 x 64 binary32 in one sequence: 12 of the call's 16.3 us replayed, of which 4 are start and end and the rest reads 38 MB at 4.7 TB/s; issue slots 55 % busy.
+// Rows in registers ahead, four rows per team and requests into L2 measure the same.  What a CTA does for a sequence takes 2 us however short it is.
 template <typename Z, int W, int L, int V, int THREADS, bool ONLY>
 __global__ void __launch_bounds__(Team<L, THREADS>::kThreads)
 balance_kernel(const __grid_constant__ BalanceArgs a) {
@@ -653,6 +654,9 @@ struct BackwardArgs {
 //   ... divided by their sum, r the shares: softmax    r_e (d_e - sum r d),   sigmoid   r_e (1 - s_e) (d_e - sum r d)
 // The chosen ones' logits are read again and their shares taken from their own largest: they may all be lost beside the row's.  What goes to
 // single experts passes through a row of shared memory that is zero between rows.
+// Bound by instructions: 32768 x 256 (sigmoid, renormalised, both losses) 28 to 29 us replayed, 59 % of the issue slots, 542 instructions per row where 67 MB would take 10.6 us;
+// 768 threads per SM have 80 registers each
+// (the weights alone, when this was chosen: 22.2 us, with 1280 threads 30.9).
 template <typename Z, int W, int L, int V>
 __global__ void __launch_bounds__(Team<L, kBackThreads>::kThreads, back_ctas<L, V>())
 gate_backward_kernel(const __grid_constant__ BackwardArgs a) {
@@ -995,6 +999,14 @@ extern "C" int exmoe_balance_loss(const exmoe_shape* shape, const exmoe_gate* ga
     if ((T && (!logits || !topk_ids)) || !losses || !counts || !score_sums || !kept || (!scratch && scratch_bytes(g.E, t))) return EXMOE_ERR_ARG;
     const int es = type == EXMOE_F32 ? 4 : 2;
     if (!aligned(es, logits) || !aligned(4, topk_ids, offsets, losses, counts, score_sums, kept) || !aligned(8, scratch)) return EXMOE_ERR_ARG;
+    const long long SE = (long long)num_sequences * g.E;
+    const Range ranges[] = {range_of(losses, 1, 0, 2, 4), range_of(counts, 1, 0, SE, 4), range_of(score_sums, 1, 0, SE, 4), range_of(kept, 1, 0, num_sequences, 4),
+                            range_of(scratch, 1, 0, (long long)scratch_bytes(g.E, t), 1), range_of(logits, T, row_stride, g.E, es),
+                            range_of(topk_ids, 1, 0, (long long)T * g.k, 4), range_of(mask, 1, 0, T, 1), range_of(offsets, 1, 0, num_sequences + 1ll, 4)};
+    constexpr int kWritten = 5;
+    for (int i = 0; i < kWritten; ++i)
+        for (int j = i + 1; j < (int)(sizeof ranges / sizeof *ranges); ++j)
+            if (overlap(ranges[i], ranges[j])) return EXMOE_ERR_ARG;
     BalanceArgs a{logits, row_stride, topk_ids, mask, offsets, num_sequences, T, g.E, g.k, g.sigmoid, t.rows, t.tiles, losses, counts, score_sums, kept};
     double* d = static_cast<double*>(scratch);
     const size_t n = (size_t)t.tiles;

@@ -1,7 +1,7 @@
 """The gate's losses and gradients on the device against the binary64 oracle.
 
-Scores: an exponential is off by 2 units of 2^-23 (the function's bound) and by its argument's rounding, |z - largest| 2^-24 (beyond 104 it is 0);
-the sum over the experts rounds at most 32 times one after the other, division and products a few times: a score is within
+Scores: an exponential is off by 2 units of 2^-23 (the instruction's bound) and by its argument's roundings, |z - largest| 2^-23 at most (the product's, and the
+difference's or the shift's): 52 2^-23 as far as 52 below the largest, where a score is e^-52 of the whole; the sum over the experts rounds at most 32 times one after the other, division and products a few times: a score is within
 REL = (8 + 52 + 36) 2^-23 of itself, or lost below 2^-126.  Sums of scores have terms of one sign, and a chain of at most rows + 64 additions.
 A gradient is a sum of terms whose sizes the oracle gives, each a product of four such factors at most.
 """

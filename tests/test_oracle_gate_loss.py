@@ -198,3 +198,15 @@ def test_python_refuses_host_tensors_and_wrong_names(B):
             call()
     with pytest.raises(ValueError, match="x: need"):
         B.exmoe_linear(torch.zeros(4, 8, dtype=torch.bfloat16), torch.zeros(4, 8, dtype=torch.bfloat16))
+
+
+def test_losses_refuse_overlap(B):
+    """What is written overlaps neither an input nor one another."""
+    at = dict(losses=P + 10 * MB, counts=P + 11 * MB, sums=P + 12 * MB, kept=P + 13 * MB)
+    inputs = dict(z=P + 14 * MB, ids=P + 15 * MB, mask=P + 16 * MB, off=P + 17 * MB)
+    for name in at:
+        for other, where in {**at, **inputs}.items():
+            if other != name:
+                assert loss(B, **{**at, **inputs, name: where}) == B.EXMOE_ERR_ARG, (name, other)
+    for other in {**at, **inputs}.values():
+        assert loss(B, **{**at, **inputs, "T": 5000, "scratch": other}) == B.EXMOE_ERR_ARG, other
