@@ -17,7 +17,8 @@ constexpr int kMaxTokens = 1 << 29, kMaxDim = 1 << 30, kSms = 148;
 // A CTA goes through groups of rows; a warp has its next weights and tokens on their way while the group's parts are added up.
 // WARPS: 8, two CTAs per SM, or, where the SMs have a group each at most, 16 that share it (us, replayed from a graph, 8 / 16 warps: 2048 -> 2048 outputs 3.5 / 3.2,
 // 5632 -> 2048 7.4 / 6.2, 16 tokens 9.6 / 8.2; 2048 -> 5632 6.2 / 7.5, gated 8.7 / 10.2, 8192 -> 8192 22.4 / 25.8).  Either way an SM has 128 KB
-// (NT = 2: 64) of weights on their way.
+// (NT = 2: 64) of weights on their way.  Bound by HBM and by 2 us of launch and latency: one token, two matrices 2048 -> 5632, 46 MB in 8.7 us (5.3 TB/s); 5632 -> 2048, 23 MB in
+// 6.2 us (3.7 TB/s).
 template <typename O, int NT, bool GATED, int WARPS>
 __global__ void __launch_bounds__(32 * WARPS, 16 / WARPS)
 linear_few_kernel(const __grid_constant__ LinearArgs a, int rows, int groups) {
@@ -131,7 +132,7 @@ int launch_few(const LinearArgs& a, cudaStream_t st) {
     count_launch();
     return EXMOE_OK;
 }
-constexpr int kFewTokens = 16;
+constexpr int kFewTokens = 16;                                             // (two MMAs of 8: 16 tokens 2048 -> 2048 4.1 us; on tcgen05 17 take 5.6)
 template <typename O, bool GATED>
 int launch_few_tokens(const LinearArgs& a, cudaStream_t st) {
     if (a.N <= kSms * (GATED ? 8 : 16)) return a.T <= 8 ? launch_few<O, 1, GATED, 16>(a, st) : launch_few<O, 2, GATED, 16>(a, st);
