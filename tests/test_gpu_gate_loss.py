@@ -317,3 +317,18 @@ def test_refusals(B):
         B.exmoe_gate_backward(s, g, z, out=z)                              # in place
     with pytest.raises(B.ExmoeError):
         B.exmoe_balance_loss(shape(E, 17), g, z, torch.zeros(T, 17, dtype=torch.int32, device="cuda"))
+
+
+@pytest.mark.parametrize("S,E", [(1, 8), (3, 60), (20, 64), (40, 256)])
+def test_results_are_tensors_of_their_own(B, S, E):
+    """Few small results or many: shapes, types and strides of theirs, and what is written to one is in no other."""
+    T, k = 64, 2
+    z, ids, _, offsets, _ = inputs(T, E, k, 11, S=S)
+    want = [t.clone() for t in B.exmoe_balance_loss(shape(E, k), gate(), z, ids, offsets=offsets)]
+    for i in range(4):
+        got = B.exmoe_balance_loss(shape(E, k), gate(), z, ids, offsets=offsets)
+        assert [tuple(t.shape) for t in got] == [(2,), (S, E), (S, E), (S,)] and all(t.is_contiguous() and t.data_ptr() % 16 == 0 for t in got)
+        assert [t.dtype for t in got] == [torch.float32, torch.int32, torch.float32, torch.int32]
+        got[i].fill_(7)
+        assert all(torch.equal(g, w) for j, (g, w) in enumerate(zip(got, want)) if j != i)
+        assert not any(t.requires_grad for t in got) and torch.equal(got[i].cpu() + 0, torch.full_like(want[i], 7).cpu())
