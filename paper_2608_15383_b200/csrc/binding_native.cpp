@@ -96,7 +96,7 @@ bool stream_of(PyObject* o, void** st) {
 at::Tensor empty_on(const at::Tensor& like, at::IntArrayRef sizes, at::ScalarType dt) {
     return at::detail::empty_cuda(sizes, dt, like.device(), std::nullopt);
 }
-// Several results: in one allocation where they are small (an allocation takes the host 0.8 us, 6.7 us being a whole call of four results), else one each, so that
+// Several results: in one allocation where they are small (a call of 16 tokens 5.5 us instead of 6.9), else one each, so that
 // who keeps one of them does not keep the others' memory.
 template <int N>
 void empties_on(const at::Tensor& like, const std::vector<int64_t> (&sizes)[N], const at::ScalarType (&types)[N], at::Tensor (&out)[N]) {
