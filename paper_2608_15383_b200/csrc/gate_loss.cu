@@ -459,6 +459,7 @@ balance_kernel(const __grid_constant__ BalanceArgs a) {
     const bool last = (int)blockIdx.x == a.tiles - 1;
     for (int e = tid; e < L * V; e += TM::kThreads) hist[e] = 0;
     if (tid == 0) n_kept = 0;
+    __syncthreads();                                                       // warps of one sequence meet nowhere else before they count
     grid_dependency_wait();
     grid_launch_dependents();
     const Z* z = static_cast<const Z*>(a.z);
