@@ -163,30 +163,22 @@ __device__ __forceinline__ float both(Two v) {
     split(v, a, b);
     return a + b;
 }
-// e = exp(v - top) and their sum, top the largest.  In one product and sum: what top's product is rounded by is a factor that all of a row's terms
-// have in common, so that shares do not see it, and the logarithm no more than top's own last place.
+// e = exp(v - top) and their sum, top the largest.  The difference comes first, exact next to top: what v log2(e) - top log2(e) in one step takes from the
+// rounding of top log2(e) is a factor on all of a row's terms, 1 % at logits of 1e5, and outside of binary32 from 1.5e9 on.  Each term is exp_below's, bit
+// by bit, so that a chosen expert's own is in proportion to the sum.
 template <int V>
 __device__ __forceinline__ float exps_below(const float (&v)[V], float top, float (&e)[V]) {
-    if (fabsf(top) < 1e38f) {
-        const Two shift = two(-top * kLog2e, -top * kLog2e), scale = two(kLog2e, kLog2e);
-        Two sum = two(0.f, 0.f);
+    const Two shift = two(-top, -top), scale = two(kLog2e, kLog2e);
+    Two sum = two(0.f, 0.f);
 #pragma unroll
-        for (int j = 0; j < V; j += 2) {
-            float a, b;
-            split(fma(two(v[j], v[j + 1]), scale, shift), a, b);
-            e[j] = exp2_of(a);
-            e[j + 1] = exp2_of(b);
-            sum = sum + two(e[j], e[j + 1]);
-        }
-        return both(sum);
+    for (int j = 0; j < V; j += 2) {
+        float a, b;
+        split((two(v[j], v[j + 1]) + shift) * scale, a, b);
+        e[j] = exp2_of(a);
+        e[j + 1] = exp2_of(b);
+        sum = sum + two(e[j], e[j + 1]);
     }
-    float sum = 0.f;                                                       // the product would leave binary32 (or top is NaN)
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        e[j] = exp_below(v[j] - top);
-        sum += e[j];
-    }
-    return sum;
+    return both(sum);
 }
 // A sigmoid times exp(-c) (see the top; c <= 0), and 1 - sigmoid.
 __device__ __forceinline__ float scaled_sigmoid(float z, float c, float& rest) {
