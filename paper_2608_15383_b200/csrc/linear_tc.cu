@@ -5,7 +5,7 @@
 // the cluster's shared memory in a fixed order.  `linear_pair_kernel`: persistent pairs of CTAs (cta_group::2), 256 rows by up to 256 tokens.
 // Both: TMA into a ring of 64-wide stages with the 128-byte swizzle, one warp issuing the MMAs, two accumulators in turn.  An MMA truncates what it adds
 // (a few units of 2^-24 of all that its chain has summed): over a whole K of thousands that would show in a binary32 result.  So chains of kChain stages (32 MMAs)
-// start from zero, and warps take them out of tensor memory and add them to binary32 sums in registers; only the pairs' BF16 results come from one chain.
+// start from zero, and warps take them out of tensor memory and add them to binary32 sums in registers; only the pairs' BF16 results come from chains of up to 1024 MMAs.
 //
 // With a second matrix a tile's 128 rows are 64 of W and the same 64 of U: a row's two factors are 64 lanes of tensor memory apart and meet in shared memory.
 #include <algorithm>
@@ -429,7 +429,8 @@ __device__ __forceinline__ TileAt tile_at(int tile, int row_tiles, int token_til
     return {group * kGroup + in_group % rows, in_group / rows};
 }
 
-template <typename O, bool GATED, bool STUCK>
+// CHAIN: stages of a chain of MMAs; 0: all of K is one.
+template <typename O, bool GATED, int CHAIN, bool STUCK>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kPairThreads, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_u, const __grid_constant__ CUtensorMap map_x,
                    const __grid_constant__ LinearArgs a, int BN, int row_tiles, int token_tiles) {
@@ -466,10 +467,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     const uint32_t tmem = sm.tmem;
     grid_dependency_wait();
     grid_launch_dependents();
-    // In front of a BF16 result the whole K is one chain, which stays in tensor memory until it is finished: what truncation takes (K / 16 MMAs,
-    // 2^-8 of a BF16 step each at most) does not show.
-    constexpr bool kChained = sizeof(O) == 4;
-    const int blocks = (a.K + 63) / 64, per_chain = kChained ? kChain : blocks, chains = (blocks + per_chain - 1) / per_chain;
+    constexpr bool kChained = CHAIN > 0;
+    const int blocks = (a.K + 63) / 64, per_chain = kChained ? CHAIN : blocks, chains = (blocks + per_chain - 1) / per_chain;
     const uint32_t full = smem_u32(sm.full), empty = smem_u32(sm.empty), acc_full = smem_u32(sm.acc_full), acc_empty = smem_u32(sm.acc_empty);
     const uint32_t ring = smem_u32(sm.ring[0]);
     bool ok = true;
@@ -645,7 +644,10 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     if (warp == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kPairTokens));
 }
 
-template <typename O, bool GATED, bool STUCK = false>
+// Chains in front of a BF16 result are as long as K up to kLongChain stages, 1024 MMAs, and stay in tensor memory until they are finished.  Each truncates by
+// 1e-7 of what it has summed (measured: 1e-4 over 1024 of them where all products have one sign, a fortieth of a BF16 half step; 6e-3, more than a whole one, over 65536).
+constexpr int kLongChain = 256;
+template <typename O, bool GATED, int CHAIN, bool STUCK>
 int launch_pair(const LinearArgs& a, int BN, cudaStream_t st) {
     using S = PairShared<GATED>;
     constexpr int kRows = GATED ? BM / 2 : BM;
@@ -654,7 +656,7 @@ int launch_pair(const LinearArgs& a, int BN, cudaStream_t st) {
         encode_map(&mx, a.x, a.T, a.K, a.ld_x, BN / 2))
         return EXMOE_ERR_CUDA;
     static SmemOnce once;
-    const auto kern = linear_pair_kernel<O, GATED, STUCK>;
+    const auto kern = linear_pair_kernel<O, GATED, CHAIN, STUCK>;
     constexpr int smem = (int)sizeof(S) + 1024;
     static_assert(smem <= 227 * 1024, "shared memory");
     if (!allow_smem(kern, smem, once)) return EXMOE_ERR_CUDA;
@@ -756,7 +758,10 @@ int launch_tc(const LinearArgs& a, cudaStream_t st) {
             wide = alone && (long long)n * stage > 280 * 1024;              // (8 stages of 24 KB: 8.2 us wide, 6.7 with room for the next call's CTAs; 16: 10.5, 11.6)
         }
     }
-    if (pair_cost < std::max(split_cost, from_hbm + 7000)) return launch_pair<O, GATED, STUCK>(a, pair_BN, st);
+    if (pair_cost < std::max(split_cost, from_hbm + 7000)) {
+        if constexpr (sizeof(O) == 4) return launch_pair<O, GATED, kChain, STUCK>(a, pair_BN, st);
+        else return blocks <= kLongChain ? launch_pair<O, GATED, 0, STUCK>(a, pair_BN, st) : launch_pair<O, GATED, kLongChain, STUCK>(a, pair_BN, st);
+    }
     if constexpr (STUCK) return launch_split<O, GATED, 8, true>(a, BN, CL, wide, st);
     if (CL <= 2) return launch_split<O, GATED, 2>(a, BN, CL, wide, st);
     return CL <= 4 ? launch_split<O, GATED, 4>(a, BN, CL, wide, st) : launch_split<O, GATED, 8>(a, BN, CL, wide, st);

@@ -1,0 +1,47 @@
+"""Products over a long K, of inputs of one sign, where truncations add up: sums are made of chains of bounded length.
+
+A chain of n MMAs is off by 5.25 n units of 2^-23 of its sum at most (each sums 16 products and truncates); chains, and warps' parts, are added in binary32, half a unit of 2^-23 each.
+"""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2608_15383_b200 import binding, build
+    build.build()
+    binding.lib()
+    return binding
+
+
+def inputs(T, K, N, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return [torch.rand(n, K, generator=g, device="cuda").add_(0.01).bfloat16() for n in (T, N, N)]
+
+
+def exact(x, w):
+    y = torch.zeros(x.shape[0], w.shape[0], dtype=torch.float64, device="cuda")
+    for k in range(0, x.shape[1], 32768):
+        y += x[:, k:k + 32768].double() @ w[:, k:k + 32768].double().t()
+    return y
+
+
+def check(out, want, rel):
+    tol = rel + torch.finfo(out.dtype).eps / 2 * (1 + rel)
+    err = (out.double() / want - 1).abs().max().item()
+    assert err <= tol, (err, tol)
+
+
+@pytest.mark.parametrize("T,K,N", [(1200, 16384, 512), (1200, 16392, 512), (1200, 262144, 512), (700, 262144 + 24, 300)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_bf16_results_of_many_tokens(B, T, K, N, gated):
+    """No chain is longer than 1024 MMAs."""
+    x, w, u = inputs(T, K, N, K + T)
+    rel = (5.25 * 1024 + K / 16384 / 2 + 1) * 2.0 ** -23
+    want = exact(x, w)
+    if gated:
+        want, rel = want * exact(x, u), 2 * rel + rel * rel + 2.0 ** -23
+    check(B.exmoe_linear(x, w, w_up=u if gated else None), want, rel)
+    assert B.exmoe_linear_status() == B.EXMOE_OK
