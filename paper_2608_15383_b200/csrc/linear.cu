@@ -10,6 +10,7 @@ namespace exmoe {
 namespace {
 
 constexpr int kMaxTokens = 1 << 29, kMaxDim = 1 << 30, kSms = 148;
+__host__ __device__ constexpr int few_chain(int warps) { return 32 * 16 * warps; }        // the K that chains of 32 MMAs of a CTA's warps make
 
 // Few tokens.  A CTA takes 16 rows of W (8 of W and 8 of U: the two factors meet in one lane) and 8 NT tokens; its warps split K.
 // Weights are the MMA's rows: a lane's 16 bytes of a row are k = 8 c .. 8 c + 7 of every 32, the k that two MMAs take from it, and the
@@ -19,10 +20,13 @@ constexpr int kMaxTokens = 1 << 29, kMaxDim = 1 << 30, kSms = 148;
 // 5632 -> 2048 7.4 / 6.2, 16 tokens 9.6 / 8.2; 2048 -> 5632 6.2 / 7.5, gated 8.7 / 10.2, 8192 -> 8192 22.4 / 25.8).  Either way an SM has 128 KB
 // (NT = 2: 64) of weights on their way.  Bound by HBM and by 2 us of launch and latency: one token, two matrices 2048 -> 5632, 46 MB in 8.7 us (5.3 TB/s); 5632 -> 2048, 23 MB in
 // 6.2 us (3.7 TB/s).
-template <typename O, int NT, bool GATED, int WARPS>
+// LONG: chains of 32 MMAs, added in binary32 in shared memory.  The instructions truncate what they add (3.5e-4 over 8192 of them where all products have
+// one sign).  (In a form of its own: the loop around it takes calls with one chain 0.3 us, FP32 8192 -> 8192 outputs 0.7.)
+template <typename O, int NT, bool GATED, int WARPS, bool LONG>
 __global__ void __launch_bounds__(32 * WARPS, 16 / WARPS)
 linear_few_kernel(const __grid_constant__ LinearArgs a, int rows, int groups) {
     constexpr int kFewThreads = 32 * WARPS, kFewWarps = WARPS, kAhead = (NT == 1 ? 64 : 32) / WARPS;
+    constexpr int kChain = few_chain(WARPS) / (32 * WARPS * kAhead);              // batches of a chain
     __shared__ float part[2][kFewWarps][NT][16][9];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
     {   // into L2, before the wait (the kernel in front may be writing them: L2 has what it writes)
@@ -60,30 +64,34 @@ linear_few_kernel(const __grid_constant__ LinearArgs a, int rows, int groups) {
     int group = blockIdx.x;
     if (group < groups) load(group, 0);
     for (int turn = 0; group < groups; turn ^= 1) {
-        float acc[NT][4];
-#pragma unroll
-        for (int i = 0; i < NT; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
         const int next = group + (int)gridDim.x;
-        for (int batch = 0; batch < batches; ++batch) {
+        int first = 0;
+        do {
+            float acc[NT][4];
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u)
+            for (int i = 0; i < NT; ++i)
 #pragma unroll
-                for (int i = 0; i < NT; ++i) {
-                    mma_m16n8k16(acc[i], va[u].x, vb[u].x, va[u].y, vb[u].y, vx[u][i].x, vx[u][i].y);
-                    mma_m16n8k16(acc[i], va[u].z, vb[u].z, va[u].w, vb[u].w, vx[u][i].z, vx[u][i].w);
+                for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+            for (int batch = first; batch < (LONG ? min(batches, first + kChain) : batches); ++batch) {
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                    for (int i = 0; i < NT; ++i) {
+                        mma_m16n8k16(acc[i], va[u].x, vb[u].x, va[u].y, vb[u].y, vx[u][i].x, vx[u][i].y);
+                        mma_m16n8k16(acc[i], va[u].z, vb[u].z, va[u].w, vb[u].w, vx[u][i].z, vx[u][i].w);
+                    }
+                if (batch + 1 < batches) load(group, batch + 1);
+                else if (next < groups) load(next, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float& p = part[turn][warp][i][g + 8 * (j >> 1)][2 * c + (j & 1)];
+                    p = LONG && first ? p + acc[i][j] : acc[i][j];
                 }
-            if (batch + 1 < batches) load(group, batch + 1);
-            else if (next < groups) load(next, 0);
-        }
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-            part[turn][warp][i][g][2 * c] = acc[i][0];
-            part[turn][warp][i][g][2 * c + 1] = acc[i][1];
-            part[turn][warp][i][8 + g][2 * c] = acc[i][2];
-            part[turn][warp][i][8 + g][2 * c + 1] = acc[i][3];
-        }
+            first += kChain;
+        } while (LONG && first < batches);
         __syncthreads();                                                   // (a warp writes these parts again behind the next one: all have read them by then)
         const long long n0 = (long long)group * rows;
         const int n_rows = (int)min((long long)rows, a.N - n0);
@@ -106,7 +114,7 @@ linear_few_kernel(const __grid_constant__ LinearArgs a, int rows, int groups) {
     }
 }
 
-template <typename O, int NT, bool GATED, int WARPS>
+template <typename O, int NT, bool GATED, int WARPS, bool LONG>
 int launch_few(const LinearArgs& a, cudaStream_t st) {
     // as many rows, up to 16 (8 of each matrix), as spread evenly over the CTAs that the chip holds
     constexpr int most = GATED ? 8 : 16;
@@ -125,7 +133,7 @@ int launch_few(const LinearArgs& a, cudaStream_t st) {
 #ifdef EXMOE_DISABLE_PDL
     lc.numAttrs = 0;
 #endif
-    if (cudaLaunchKernelEx(&lc, linear_few_kernel<O, NT, GATED, WARPS>, a, (int)rows, (int)groups) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&lc, linear_few_kernel<O, NT, GATED, WARPS, LONG>, a, (int)rows, (int)groups) != cudaSuccess) {
         cudaGetLastError();
         return EXMOE_ERR_CUDA;
     }
@@ -133,10 +141,15 @@ int launch_few(const LinearArgs& a, cudaStream_t st) {
     return EXMOE_OK;
 }
 constexpr int kFewTokens = 16;                                             // (two MMAs of 8: 16 tokens 2048 -> 2048 4.1 us; on tcgen05 17 take 5.6)
+template <typename O, bool GATED, int WARPS>
+int launch_few_tokens(const LinearArgs& a, cudaStream_t st) {
+    constexpr int kMostShort = few_chain(WARPS) * (sizeof(O) == 4 ? 1 : 32);    // (in front of a BF16 result 1024 MMAs: 1e-4, a fortieth of half a step)
+    if (a.K <= kMostShort) return a.T <= 8 ? launch_few<O, 1, GATED, WARPS, false>(a, st) : launch_few<O, 2, GATED, WARPS, false>(a, st);
+    return a.T <= 8 ? launch_few<O, 1, GATED, WARPS, true>(a, st) : launch_few<O, 2, GATED, WARPS, true>(a, st);
+}
 template <typename O, bool GATED>
 int launch_few_tokens(const LinearArgs& a, cudaStream_t st) {
-    if (a.N <= kSms * (GATED ? 8 : 16)) return a.T <= 8 ? launch_few<O, 1, GATED, 16>(a, st) : launch_few<O, 2, GATED, 16>(a, st);
-    return a.T <= 8 ? launch_few<O, 1, GATED, 8>(a, st) : launch_few<O, 2, GATED, 8>(a, st);
+    return a.N <= kSms * (GATED ? 8 : 16) ? launch_few_tokens<O, GATED, 16>(a, st) : launch_few_tokens<O, GATED, 8>(a, st);
 }
 
 }  // namespace

@@ -45,3 +45,27 @@ def test_bf16_results_of_many_tokens(B, T, K, N, gated):
         want, rel = want * exact(x, u), 2 * rel + rel * rel + 2.0 ** -23
     check(B.exmoe_linear(x, w, w_up=u if gated else None), want, rel)
     assert B.exmoe_linear_status() == B.EXMOE_OK
+
+
+@pytest.mark.parametrize("T,K,N", [(1, 8200, 40), (5, 16384, 64), (8, 262144, 64), (16, 262144 + 40, 33), (3, 1 << 20, 64), (12, 1 << 20, 2500)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_fp32_results_of_few_tokens(B, T, K, N, gated):
+    """No chain is longer than 32 MMAs; a warp has an eighth of K at most, and 16 parts are added at most."""
+    x, w, u = inputs(T, K, N, K + T)
+    rel = (5.25 * 32 + K / 16 / 32 / 8 / 2 + 1 + 8) * 2.0 ** -23
+    want = exact(x, w)
+    if gated:
+        want, rel = want * exact(x, u), 2 * rel + rel * rel + 2.0 ** -23
+    check(B.exmoe_linear(x, w, w_up=u if gated else None, out_dtype=torch.float32), want, rel)
+
+
+@pytest.mark.parametrize("T,K,N", [(2, 65536, 64), (8, 65544, 64), (5, 131080, 2500), (16, 1 << 20, 64)])
+@pytest.mark.parametrize("gated", [False, True])
+def test_bf16_results_of_few_tokens(B, T, K, N, gated):
+    """No chain is longer than 1024 MMAs."""
+    x, w, u = inputs(T, K, N, K + T)
+    rel = (5.25 * 1024 + K / 16 / 32 / 8 / 2 + 1 + 8) * 2.0 ** -23
+    want = exact(x, w)
+    if gated:
+        want, rel = want * exact(x, u), 2 * rel + rel * rel + 2.0 ** -23
+    check(B.exmoe_linear(x, w, w_up=u if gated else None), want, rel)
