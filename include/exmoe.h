@@ -272,7 +272,7 @@ int exmoe_balance_loss(const exmoe_shape* shape, const exmoe_gate* gate, const v
  * with counts held fixed, as the balance loss is meant.
  *   logits, type, row_stride, topk_ids, mask, offsets, num_sequences : as above; topk_ids may be NULL without d_weights.  A masked token's gradient
  *                  is zero.  An id outside [0, E) has no weight, an expert that a token names twice both of them
- *   d_weights    : dev, float32 [T, k], or NULL        d_losses : dev, float32 [2], or NULL
+ *   d_weights    : dev, float32 [T, k], the caller's (the output's gradient times each chosen expert's output), or NULL        d_losses : dev, float32 [2], or NULL
  *   counts, kept : dev, of exmoe_balance_loss (or summed over the processes of a job); needed with d_losses.  With offsets that do not ascend in [0, T] the
  *                  gradient is not to be used either
  *   d_logits     : dev, [T, E] of `type`, rows d_row_stride elements apart, fully overwritten; overlaps no input (EXMOE_ERR_ARG)
@@ -286,7 +286,7 @@ int exmoe_gate_backward(const exmoe_shape* shape, const exmoe_gate* gate, const 
  *   out_t = residual_t + act(W x_t + bias)                       or, with a second matrix,
  *   out_t = residual_t + act(W x_t + bias) * (W_up x_t + bias_up)
  * Products are summed in binary32, the epilogue is binary32, and the result is rounded once, to the type of `out`.  (In which order and how often the sums
- * are rounded depends on T, K and N.  SiLU and the tanh form are off by units of their last place, a few and as many as their exponential's argument is large;
+ * are rounded depends on T, K and N, and where clusters of CTAs split K on how many of these the device holds.  SiLU and the tanh form are off by units of their last place, a few and as many as their exponential's argument is large;
  * GELU by 3e-7 |v|, at most 6e-7 of itself above 0 and more of itself far below, 2e-3 at -5.) */
 enum { EXMOE_ACT_NONE = 0, EXMOE_ACT_RELU = 1, EXMOE_ACT_GELU = 2 /* v Phi(v) */, EXMOE_ACT_GELU_TANH = 3, EXMOE_ACT_SILU = 4 };
 typedef struct {

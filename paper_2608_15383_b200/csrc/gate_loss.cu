@@ -432,7 +432,7 @@ constexpr size_t balance_smem() {
 }
 
 // First step: a CTA per tile, so that an SM has one start and one end; the offsets of a few hundred sequences are read at once.  ONLY: there is one tile, and no second step.
-// 131072 x 64 binary32 in one sequence: 12 of the call's 16.3 us replayed, of which 4 are start and end and the rest reads 38 MB at 4.7 TB/s; issue slots 55 % busy.
+// 131072 x 64 binary32 in one sequence: 12 of the call's 16.5 us replayed, of which 4 are start and end and the rest reads 38 MB at 4.7 TB/s; issue slots 55 % busy.
 // Rows in registers ahead, four rows per team and requests into L2 measure the same.  What a CTA does for a sequence takes 2 us however short it is.
 template <typename Z, int W, int L, int V, int THREADS, bool ONLY>
 __global__ void __launch_bounds__(Team<L, THREADS>::kThreads)
@@ -647,7 +647,7 @@ struct BackwardArgs {
 //   ... divided by their sum, r the shares: softmax    r_e (d_e - sum r d),   sigmoid   r_e (1 - s_e) (d_e - sum r d)
 // The chosen ones' logits are read again and their shares taken from their own largest: they may all be lost beside the row's.  What goes to
 // single experts passes through a row of shared memory that is zero between rows.
-// Bound by instructions: 32768 x 256 (sigmoid, renormalised, both losses) 28 to 29 us replayed, 59 % of the issue slots, 542 instructions per row where 67 MB would take 10.6 us;
+// Bound by instructions: 32768 x 256 (sigmoid, renormalised, both losses) 28.5 us replayed, 56 % of the issue slots, 551 instructions per row where 67 MB would take 10.6 us;
 // 768 threads per SM have 80 registers each
 // (the weights alone, when this was chosen: 22.2 us, with 1280 threads 30.9).
 template <typename Z, int W, int L, int V>
