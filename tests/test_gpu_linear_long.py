@@ -2,6 +2,8 @@
 
 A chain of n MMAs is off by 5.25 n units of 2^-23 of its sum at most (each sums 16 products and truncates); chains, and warps' parts, are added in binary32, half a unit of 2^-23 each.
 """
+from ctypes import byref
+
 import pytest
 import torch
 
@@ -69,3 +71,17 @@ def test_bf16_results_of_few_tokens(B, T, K, N, gated):
     if gated:
         want, rel = want * exact(x, u), 2 * rel + rel * rel + 2.0 ** -23
     check(B.exmoe_linear(x, w, w_up=u if gated else None), want, rel)
+
+
+def test_a_wait_of_long_chains_that_runs_out(B):
+    """The form of pairs that adds chains gives up as the others do: the call returns and says so, writes nothing outside of its result, and the next one is right."""
+    T, K, N = 1200, 16448, 512
+    x, w, _ = inputs(T, K, N, 1)
+    want = B.exmoe_linear(x, w)
+    wide = torch.full((T + 2, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    assert B.exmoe_linear_status() == B.EXMOE_OK
+    rc = B.lib().exmoe_debug_linear_timeout(byref(B.exmoe_linear_shape(K, N, 0)), x.data_ptr(), w.data_ptr(), T, wide[1:T + 1].data_ptr(), torch.cuda.current_stream().cuda_stream)
+    assert rc == B.EXMOE_OK
+    assert B.exmoe_linear_status() == B.EXMOE_ERR_TIMEOUT and B.exmoe_linear_status() == B.EXMOE_OK
+    assert (wide[[0, T + 1]] == 7.0).all()
+    assert torch.equal(B.exmoe_linear(x, w), want)
